@@ -2,6 +2,7 @@
 
 The compute lives in the CUDA library behind the C ABI declared in
 ``include/egeria.h``; :mod:`paper_2201_06227_b200.binding` only marshals
-arguments.  :mod:`paper_2201_06227_b200.workloads` draws seeded synthetic inputs.
+arguments, and :mod:`paper_2201_06227_b200.ops` those of the training operators declared in
+``include/egeria_ops.h``.  :mod:`paper_2201_06227_b200.workloads` draws seeded synthetic inputs.
 """
-__all__ = ["binding", "workloads"]
+__all__ = ["binding", "ops", "workloads"]

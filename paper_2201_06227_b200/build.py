@@ -4,18 +4,19 @@ from __future__ import annotations
 import os
 import subprocess
 import sys
+from concurrent.futures import ThreadPoolExecutor
 from pathlib import Path
 
 HERE = Path(__file__).resolve().parent
 CSRC = HERE / "csrc"
 LIB = HERE / "libegeria.so"
 LIB_CHECKED = HERE / "libegeria_checked.so"   # the same sources with -DEGERIA_CHECKED (csrc/check.cuh)
-SOURCES = [CSRC / "egeria_api.cu"]
-HEADERS = sorted(CSRC.glob("*.cuh")) + sorted(CSRC.glob("*.h")) + [HERE.parent / "include" / "egeria.h"]
+SOURCES = [CSRC / "egeria_api.cu", CSRC / "ops" / "ops_api.cu"]
+HEADERS = [*sorted(CSRC.rglob("*.cuh")), *sorted(CSRC.glob("*.h")), *sorted((HERE.parent / "include").glob("*.h"))]
 
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
-    "-shared", "-Xcompiler", "-fPIC", "-Xptxas", "-v",
+    "-shared", "-Xcompiler", "-fPIC", "-Xptxas", "-v", "-t", "0",   # -t 0: the sources side by side
 ]
 
 
@@ -41,10 +42,11 @@ def _compile(lib: Path, extra, verbose: bool) -> None:
 def build(force: bool = False, verbose: bool = False, checked: bool = True) -> Path:
     """Build libegeria.so (and, unless checked=False, libegeria_checked.so) if missing or older than
     the sources.  Raises on failure."""
-    if force or stale(LIB):
-        _compile(LIB, [], verbose)
-    if checked and (force or stale(LIB_CHECKED)):
-        _compile(LIB_CHECKED, ["-DEGERIA_CHECKED"], verbose)
+    wanted = [(LIB, [])] + ([(LIB_CHECKED, ["-DEGERIA_CHECKED"])] if checked else [])
+    with ThreadPoolExecutor() as pool:
+        jobs = [pool.submit(_compile, lib, extra, verbose) for lib, extra in wanted if force or stale(lib)]
+    for job in jobs:
+        job.result()
     return LIB
 
 

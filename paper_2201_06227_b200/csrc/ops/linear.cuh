@@ -1,0 +1,716 @@
+// Matrix products of the linear layers on the tensor cores, with everything around a product in its epilogue.
+//
+//   D[m, n] = sum_k A(m, k) B(n, k)         A, B: bf16 or f16 in memory, D accumulated in 32 bits
+//
+// The three products of a layer differ in which axis of an operand is consecutive in memory:
+//   forward  z  = x w^T     A = x  (k consecutive)      B = w  (k consecutive)
+//   backward dx = dz w      A = dz (k consecutive)      B = w  (n consecutive)
+//   backward dw = dz^T x    A = dz (m consecutive)      B = x  (n consecutive)
+// tcgen05 takes either kind from shared memory (one bit per operand), so no operand is ever transposed
+// in memory.  Both kinds are staged in 64 x 64 swizzled tiles: a k-consecutive operand as rows of 64 k
+// values (128 bytes), the other as rows of 64 m (n) values.
+//
+// One persistent CTA per SM: warp 0 loads (TMA into a ring of stages of 64 k), warp 1 issues the
+// MMAs, warps 2..9 run the epilogue of a tile while the next tile's products go into the other half of
+// tensor memory.  CG = 2: a pair of CTAs shares one tile of 256 rows; each loads its 128 rows of A and
+// HALF of B, which is what brings the loads (32 KB per 64 k and CTA instead of 48) under what an SM
+// can take from L2 in the time of the MMAs.
+#pragma once
+#include <cuda.h>
+
+#include "../ptx_sm100.cuh"
+#include "common.cuh"
+
+namespace egeria {
+namespace ops {
+
+constexpr int kGemmM = 128;          // rows of D per CTA
+constexpr int kGemmK = 64;           // k values per stage: one swizzle row of 128 bytes
+constexpr int kGemmEpiWarps = 8;
+constexpr int kGemmThreads = 64 + 32 * kGemmEpiWarps;
+constexpr int kStagePitch = 34;      // 16-bit values per row of a warp's 32 x 32 staging tile (odd number of words)
+
+enum { kActNone = 0, kActRelu, kActGelu, kActGeluTanh, kActSilu };
+
+struct GemmParams {
+    CUtensorMap a, b;
+    int32_t m, n, kblocks;
+    int32_t tiles_m, tiles_n, splits, group_n;
+    uint32_t a_mn, b_mn;             // the operand's m (n) axis is the consecutive one
+    uint32_t is_f16;
+    const void *bias, *residual, *z_in;
+    void *out, *z;
+    int64_t ldr, ldz_in, ldo, ldz;
+    int32_t act, act_in;
+    int32_t wide;                    // every matrix of the epilogue takes 32-byte (2), 16-byte (1) or only 2-byte (0) accesses
+    float *partials;                 // split k: [unit][epilogue warp][32-column piece][8][32 lanes][4]
+    int32_t *tickets;                // split k: [tile][epilogue warp], zero between calls
+    int32_t *status;
+    uint64_t wait_limit_ns;
+};
+
+template <int BN, int CG>
+struct GemmCfg {
+    static constexpr int kABytes = kGemmM * kGemmK * 2;
+    static constexpr int kBRows = BN / CG;                   // rows of B per CTA
+    static constexpr int kBBytes = kBRows * kGemmK * 2;
+    static constexpr int kStageBytes = kABytes + kBBytes;
+    static constexpr int kStages = (196 * 1024) / kStageBytes > 8 ? 8 : (196 * 1024) / kStageBytes;
+    static constexpr int kTmemCols = 2 * BN < 32 ? 32 : 2 * BN;
+    static constexpr int kStaging = kGemmEpiWarps * 32 * kStagePitch * 2;
+    static constexpr int kSmem = 1024 + kStages * kStageBytes + kStaging + 256;
+    static constexpr int kColsPerWarp = BN / 2;
+    static constexpr int kPieces = kColsPerWarp / 32;
+};
+
+// ---------------------------------------------------------------- PTX of CTA pairs
+template <int CG>
+__device__ __forceinline__ void tmem_alloc_g(uint32_t dst, uint32_t cols) {
+    if (CG == 1)
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(dst), "r"(cols) : "memory");
+    else
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(dst), "r"(cols) : "memory");
+}
+template <int CG>
+__device__ __forceinline__ void tmem_free_g(uint32_t addr, uint32_t cols) {
+    if (CG == 1) {
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(addr), "r"(cols) : "memory");
+    } else {
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+        asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(addr), "r"(cols) : "memory");
+    }
+}
+template <int CG>
+__device__ __forceinline__ void mma_g(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+    if (CG == 1)
+        asm volatile(
+            "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+            "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate)
+            : "memory");
+    else
+        asm volatile(
+            "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+            "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate)
+            : "memory");
+}
+// One arrival on `bar` (of both CTAs of a pair) once the MMAs issued so far are done.
+template <int CG>
+__device__ __forceinline__ void mma_commit_g(uint32_t bar) {
+    if (CG == 1)
+        asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+    else
+        asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar),
+                     "h"((uint16_t)3)
+                     : "memory");
+}
+// A tile of this CTA; the bytes are counted on `bar`, a barrier of the pair's first CTA.
+template <int CG>
+__device__ __forceinline__ void tma_load_g(uint32_t dst, const CUtensorMap *map, int32_t x, int32_t y, uint32_t bar) {
+    if (CG == 1)
+        asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];" ::"r"(dst),
+                     "l"(map), "r"(bar), "r"(x), "r"(y)
+                     : "memory");
+    else
+        asm volatile(
+            "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];" ::"r"(dst),
+            "l"(map), "r"(bar), "r"(x), "r"(y)
+            : "memory");
+}
+__device__ __forceinline__ uint32_t cluster_rank() {
+    uint32_t r;
+    asm volatile("mov.u32 %0, %cluster_ctarank;" : "=r"(r));
+    return r;
+}
+// The address of `addr` (this CTA's shared memory) in CTA `rank` of the cluster.
+__device__ __forceinline__ uint32_t map_to_rank(uint32_t addr, uint32_t rank) {
+    uint32_t r;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
+    return r;
+}
+__device__ __forceinline__ void mbar_arrive_cluster(uint32_t bar) {
+    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void cluster_sync() {
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+
+// Shared-memory descriptor of an operand whose m (n) axis is consecutive: rows of 64 values (128 bytes,
+// swizzled), one per k; 8 rows make 1024 bytes (stride offset), the next 64 m values are 64 rows on
+// (leading offset).  A step of 16 k is 2048 bytes.
+__device__ __forceinline__ uint64_t make_desc_mn_sw128(uint32_t saddr) {
+    return (uint64_t)((saddr & 0x3FFFFu) >> 4) | ((uint64_t)((kGemmK * 128) >> 4) << 16) | ((uint64_t)(1024 >> 4) << 32) |
+           ((uint64_t)1 << 46) | ((uint64_t)2 << 61);
+}
+
+// ---------------------------------------------------------------- activations
+// 1 / (1 + exp(-u)) from the approximate exponential and reciprocal: relative error below 2e-5 over the
+// range where the result is not 0 or 1, far under a 16-bit output's rounding.
+__device__ __forceinline__ float sigmoid(float u) { return fast_rcp(1.0f + __expf(-u)); }
+constexpr float kGeluA = 1.5957691216057308f;  // 2 sqrt(2 / pi)
+constexpr float kGeluB = 0.044715f;
+
+template <int ACT>
+__device__ __forceinline__ float act_value(float z) {
+    if (ACT == kActRelu) return z > 0.0f ? z : (z != z ? z : 0.0f);
+    if (ACT == kActGelu) return 0.5f * z * erfcf(-0.70710678118654752f * z);
+    if (ACT == kActGeluTanh) return z * sigmoid(kGeluA * fmaf(kGeluB * z * z, z, z));
+    if (ACT == kActSilu) return z * sigmoid(z);
+    return z;
+}
+template <int ACT>
+__device__ __forceinline__ float act_slope(float z) {
+    if (ACT == kActRelu) return z > 0.0f ? 1.0f : 0.0f;
+    if (ACT == kActGelu) return fmaf(0.39894228040143268f * z, __expf(-0.5f * z * z), 0.5f * erfcf(-0.70710678118654752f * z));
+    if (ACT == kActGeluTanh) {
+        const float p = sigmoid(kGeluA * fmaf(kGeluB * z * z, z, z));
+        return fmaf(z * p * (1.0f - p), kGeluA * fmaf(3.0f * kGeluB * z, z, 1.0f), p);
+    }
+    if (ACT == kActSilu) {
+        const float p = sigmoid(z);
+        return fmaf(z * p, 1.0f - p, p);
+    }
+    return 1.0f;
+}
+template <int N>
+__device__ __forceinline__ void act_values(float (&v)[N], int act) {
+    switch (act) {
+#define EG_ACT(A)                                                        \
+    case A:                                                              \
+        _Pragma("unroll") for (int i = 0; i < N; ++i) v[i] = act_value<A>(v[i]); \
+        break;
+        EG_ACT(kActRelu)
+        EG_ACT(kActGelu)
+        EG_ACT(kActGeluTanh)
+        EG_ACT(kActSilu)
+#undef EG_ACT
+    }
+}
+template <int N>
+__device__ __forceinline__ void act_slopes(float (&v)[N], int act) {
+    switch (act) {
+#define EG_ACT(A)                                                        \
+    case A:                                                              \
+        _Pragma("unroll") for (int i = 0; i < N; ++i) v[i] = act_slope<A>(v[i]); \
+        break;
+        EG_ACT(kActRelu)
+        EG_ACT(kActGelu)
+        EG_ACT(kActGeluTanh)
+        EG_ACT(kActSilu)
+#undef EG_ACT
+        default:
+#pragma unroll
+            for (int i = 0; i < N; ++i) v[i] = 1.0f;
+    }
+}
+
+// ---------------------------------------------------------------- epilogue of a 32 x 32 piece
+// Lane = row; the piece's 32 columns start at n0.  `wide` accesses need the whole piece inside the matrix.
+__device__ __forceinline__ void ld_v8(uint32_t (&r)[8], const void *p) {
+    asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+                 : "l"(p));
+}
+struct Tile {
+    int64_t row0;     // first of the warp's 32 rows
+    int32_t rows;     // rows of the matrix from row0 on (may exceed 32)
+    int32_t col0, cols;  // first column of the piece, columns of the matrix from there on
+    uint16_t *stage;  // the warp's staging tile
+    int lane;
+    int wide;
+};
+template <typename T>
+__device__ __forceinline__ void piece_load(float (&v)[32], const void *base, int64_t ld, const Tile &t) {
+    if (t.wide && t.cols >= 32) {
+        uint32_t r[16] = {};
+        if (t.lane < t.rows) {
+            const T *p = static_cast<const T *>(base) + (t.row0 + t.lane) * ld + t.col0;
+            if (t.wide == 2) {
+                ld_v8(reinterpret_cast<uint32_t (&)[8]>(r[0]), p);
+                ld_v8(reinterpret_cast<uint32_t (&)[8]>(r[8]), p + 16);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const uint4 q = *(reinterpret_cast<const uint4 *>(p) + i);
+                    r[4 * i] = q.x, r[4 * i + 1] = q.y, r[4 * i + 2] = q.z, r[4 * i + 3] = q.w;
+                }
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const float2 f = unpack2<T>(r[i]);
+            v[2 * i] = f.x;
+            v[2 * i + 1] = f.y;
+        }
+        return;
+    }
+    // row by row with lane = column, through shared memory
+    const int rows = min(t.rows, 32);
+    const uint16_t *p = static_cast<const uint16_t *>(base) + t.row0 * ld + t.col0 + t.lane;
+    __syncwarp();
+    if (t.lane < t.cols)
+        for (int r = 0; r < rows; ++r) t.stage[r * kStagePitch + t.lane] = p[r * ld];
+    __syncwarp();
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        const float2 f = unpack2<T>(reinterpret_cast<const uint32_t *>(t.stage)[t.lane * (kStagePitch / 2) + i]);
+        v[2 * i] = f.x;
+        v[2 * i + 1] = f.y;
+    }
+}
+template <typename T>
+__device__ __forceinline__ void piece_store(void *base, int64_t ld, const float (&v)[32], const Tile &t) {
+    uint32_t r[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) r[i] = pack2<T>(v[2 * i], v[2 * i + 1]);
+    if (t.wide && t.cols >= 32) {
+        if (t.lane < t.rows) {
+            T *p = static_cast<T *>(base) + (t.row0 + t.lane) * ld + t.col0;
+            if (t.wide == 2) {
+                ptx::st_global_v8(reinterpret_cast<float *>(p), r);
+                ptx::st_global_v8(reinterpret_cast<float *>(p + 16), r + 8);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    *(reinterpret_cast<uint4 *>(p) + i) = make_uint4(r[4 * i], r[4 * i + 1], r[4 * i + 2], r[4 * i + 3]);
+            }
+        }
+        return;
+    }
+    const int rows = min(t.rows, 32);
+    uint16_t *p = static_cast<uint16_t *>(base) + t.row0 * ld + t.col0 + t.lane;
+    __syncwarp();
+#pragma unroll
+    for (int i = 0; i < 16; ++i) reinterpret_cast<uint32_t *>(t.stage)[t.lane * (kStagePitch / 2) + i] = r[i];
+    __syncwarp();
+    if (t.lane < t.cols)
+        for (int q = 0; q < rows; ++q) p[q * ld] = t.stage[q * kStagePitch + t.lane];
+}
+template <typename T>
+__device__ __forceinline__ void piece_finish(const GemmParams &p, float (&v)[32], const Tile &t) {
+    if (t.rows <= 0 || t.cols <= 0) return;  // the same for the whole warp
+    if (p.bias) {
+        const T *b = static_cast<const T *>(p.bias) + t.col0;
+#pragma unroll
+        for (int i = 0; i < 32; ++i)
+            if (i < t.cols) v[i] += to_f32(b[i]);
+    }
+    if (p.z) piece_store<T>(p.z, p.ldz, v, t);
+    act_values(v, p.act);
+    if (p.residual) {
+        float r[32];
+        piece_load<T>(r, p.residual, p.ldr, t);
+#pragma unroll
+        for (int i = 0; i < 32; ++i) v[i] += r[i];
+    }
+    if (p.z_in) {
+        float r[32];
+        piece_load<T>(r, p.z_in, p.ldz_in, t);
+        act_slopes(r, p.act_in);
+#pragma unroll
+        for (int i = 0; i < 32; ++i) v[i] *= r[i];
+    }
+    piece_store<T>(p.out, p.ldo, v, t);
+}
+
+// Unit u: a tile and a range of k blocks.  Tiles go through strips of group_n columns of tiles, n fastest, so that
+// the CTAs at work share a few rows of A and a strip of B that stay in L2.
+struct GemmUnit {
+    int32_t tm, tn, tile, split, kb0, kb1;
+};
+__device__ __forceinline__ GemmUnit gemm_unit(const GemmParams &p, int u) {
+    GemmUnit g;
+    g.tile = u / p.splits;
+    g.split = u - g.tile * p.splits;
+    const int strip = p.group_n * p.tiles_m;
+    const int s = g.tile / strip, r = g.tile - s * strip;
+    const int w = min(p.group_n, p.tiles_n - s * p.group_n);
+    g.tm = r / w;
+    g.tn = s * p.group_n + (r - g.tm * w);
+    g.kb0 = (int)((int64_t)p.kblocks * g.split / p.splits);
+    g.kb1 = (int)((int64_t)p.kblocks * (g.split + 1) / p.splits);
+    return g;
+}
+
+template <typename T, int BN, int CG>
+__global__ void __launch_bounds__(kGemmThreads, 1) gemm_kernel(const __grid_constant__ GemmParams p) {
+    using Cfg = GemmCfg<BN, CG>;
+    extern __shared__ uint8_t smem_raw[];
+    const uint32_t smem_base = (ptx::smem_u32(smem_raw) + 1023u) & ~1023u;
+    uint8_t *smem = smem_raw + (smem_base - ptx::smem_u32(smem_raw));
+    uint16_t *staging = reinterpret_cast<uint16_t *>(smem + Cfg::kStages * Cfg::kStageBytes);
+    uint64_t *bars = reinterpret_cast<uint64_t *>(smem + Cfg::kStages * Cfg::kStageBytes + Cfg::kStaging);
+    const uint32_t full0 = ptx::smem_u32(bars), empty0 = full0 + 8 * Cfg::kStages;
+    const uint32_t accfull0 = empty0 + 8 * Cfg::kStages, accempty0 = accfull0 + 16, drain = accempty0 + 16;
+    volatile uint32_t *tmem_holder = reinterpret_cast<volatile uint32_t *>(bars + 2 * Cfg::kStages + 5);
+    volatile int *abort_flag = reinterpret_cast<volatile int *>(tmem_holder + 1);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t rank = CG == 2 ? cluster_rank() : 0;
+    const int worker = blockIdx.x / CG, workers = gridDim.x / CG;
+    const int units = p.tiles_m * p.tiles_n * p.splits;
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < Cfg::kStages; ++s) {
+            ptx::mbar_init(full0 + 8 * s, 1);
+            ptx::mbar_init(empty0 + 8 * s, 1);
+        }
+        for (int s = 0; s < 2; ++s) {
+            ptx::mbar_init(accfull0 + 8 * s, 1);
+            ptx::mbar_init(accempty0 + 8 * s, kGemmEpiWarps * CG);
+        }
+        ptx::mbar_init(drain, 1);
+        *abort_flag = 0;
+        ptx::fence_barrier_init();
+        ptx::fence_proxy_async();
+        ptx::prefetch_tensormap(&p.a);
+        ptx::prefetch_tensormap(&p.b);
+    }
+    if (warp == 1) tmem_alloc_g<CG>(ptx::smem_u32(const_cast<uint32_t *>(tmem_holder)), Cfg::kTmemCols);
+    ptx::tc_fence_before_sync();
+    __syncthreads();
+    if (CG == 2) cluster_sync();
+    ptx::tc_fence_after_sync();
+    const uint32_t tmem = *tmem_holder;
+
+    if (warp == 0) {
+        if (lane == 0) {
+            uint32_t stage = 0, phase = 0, issued = 0;
+            bool ok = true;
+            // the pair's bytes are counted on its first CTA's barriers
+            const uint32_t full_base = CG == 2 ? map_to_rank(full0, 0) : full0;
+            for (int u = worker; u < units && ok; u += workers) {
+                const GemmUnit g = gemm_unit(p, u);
+                const int32_t m0 = (g.tm * CG + (int)rank) * kGemmM, n0 = g.tn * BN + (int)rank * Cfg::kBRows;
+                for (int kb = g.kb0; kb < g.kb1; ++kb) {
+                    if (!ptx::mbar_wait_bounded(empty0 + 8 * stage, phase ^ 1u, abort_flag, p.wait_limit_ns)) {
+                        ok = false;
+                        break;
+                    }
+                    const uint32_t sa = smem_base + stage * Cfg::kStageBytes, sb = sa + Cfg::kABytes;
+                    if (rank == 0) ptx::mbar_arrive_expect_tx(full0 + 8 * stage, CG * Cfg::kStageBytes);
+                    const uint32_t bar = full_base + 8 * stage;
+                    if (p.a_mn) {
+#pragma unroll
+                        for (int s = 0; s < kGemmM / 64; ++s) tma_load_g<CG>(sa + s * 8192, &p.a, m0 + 64 * s, kb * kGemmK, bar);
+                    } else {
+                        tma_load_g<CG>(sa, &p.a, kb * kGemmK, m0, bar);
+                    }
+                    if (p.b_mn) {
+#pragma unroll
+                        for (int s = 0; s < Cfg::kBRows / 64; ++s)
+                            tma_load_g<CG>(sb + s * 8192, &p.b, n0 + 64 * s, kb * kGemmK, bar);
+                    } else {
+                        tma_load_g<CG>(sb, &p.b, kb * kGemmK, n0, bar);
+                    }
+                    ++issued;
+                    if (++stage == Cfg::kStages) {
+                        stage = 0;
+                        phase ^= 1u;
+                    }
+                }
+            }
+            if (!ok && rank != 0) {
+                // this CTA's loads are counted on the other's barriers: give them a millisecond to land
+                const uint64_t t0 = ptx::globaltimer_ns();
+                while (ptx::globaltimer_ns() - t0 < 1000000ull) {
+                }
+            }
+            if (!ok && rank == 0) {
+                // gave up: wait (bounded) for the loads in flight
+                const uint32_t n = issued < (uint32_t)Cfg::kStages ? issued : (uint32_t)Cfg::kStages;
+                for (uint32_t k = 1; k <= n; ++k) {
+                    const uint32_t idx = issued - k, s = idx % Cfg::kStages, ph = (idx / Cfg::kStages) & 1u;
+                    const uint64_t t0 = ptx::globaltimer_ns();
+                    while (!ptx::mbar_try_wait(full0 + 8 * s, ph))
+                        if (ptx::globaltimer_ns() - t0 > p.wait_limit_ns) break;
+                }
+            }
+        }
+        __syncwarp();
+    } else if (warp == 1) {
+        if (lane == 0 && rank == 0) {
+            const uint32_t idesc = (1u << 4) | (p.is_f16 ? 0u : (1u << 7) | (1u << 10)) | (p.a_mn << 15) | (p.b_mn << 16) |
+                                   ((uint32_t)(BN >> 3) << 17) | ((uint32_t)((kGemmM * CG) >> 4) << 24);
+            const uint32_t step_a = p.a_mn ? 2048u >> 4 : 32u >> 4, step_b = p.b_mn ? 2048u >> 4 : 32u >> 4;
+            uint32_t stage = 0, phase = 0, acc = 0, acc_phase = 0;
+            bool ok = true;
+            for (int u = worker; u < units && ok; u += workers) {
+                const GemmUnit g = gemm_unit(p, u);
+                if (!ptx::mbar_wait_bounded(accempty0 + 8 * acc, acc_phase ^ 1u, abort_flag, p.wait_limit_ns)) {
+                    ok = false;
+                    break;
+                }
+                ptx::tc_fence_after_sync();
+                const uint32_t d = tmem + acc * BN;
+                for (int kb = g.kb0; kb < g.kb1; ++kb) {
+                    if (!ptx::mbar_wait_bounded(full0 + 8 * stage, phase, abort_flag, p.wait_limit_ns)) {
+                        ok = false;
+                        break;
+                    }
+                    ptx::tc_fence_after_sync();
+                    const uint32_t sa = smem_base + stage * Cfg::kStageBytes, sb = sa + Cfg::kABytes;
+                    const uint64_t da = p.a_mn ? make_desc_mn_sw128(sa) : ptx::make_desc_k_sw128(sa);
+                    const uint64_t db = p.b_mn ? make_desc_mn_sw128(sb) : ptx::make_desc_k_sw128(sb);
+#pragma unroll
+                    for (int k = 0; k < kGemmK / 16; ++k)
+                        mma_g<CG>(d, da + k * step_a, db + k * step_b, idesc, (kb > g.kb0 || k > 0) ? 1u : 0u);
+                    mma_commit_g<CG>(empty0 + 8 * stage);
+                    if (++stage == Cfg::kStages) {
+                        stage = 0;
+                        phase ^= 1u;
+                    }
+                }
+                if (!ok) break;
+                mma_commit_g<CG>(accfull0 + 8 * acc);
+                acc ^= 1u;
+                if (acc == 0) acc_phase ^= 1u;
+            }
+            if (!ok) {
+                // gave up: no MMA of ours may still read shared memory when the CTA leaves
+                mma_commit_g<CG>(drain);
+                const uint64_t t0 = ptx::globaltimer_ns();
+                while (!ptx::mbar_try_wait(drain, 0))
+                    if (ptx::globaltimer_ns() - t0 > p.wait_limit_ns) break;
+            }
+        }
+        __syncwarp();
+    } else {
+        const int e = warp - 2, quarter = warp & 3, half = e >> 2;
+        uint32_t acc = 0, acc_phase = 0;
+        const uint32_t release0 = CG == 2 ? map_to_rank(accempty0, 0) : accempty0;
+        Tile t;
+        t.stage = staging + e * 32 * kStagePitch;
+        t.lane = lane;
+        t.wide = p.wide;
+        for (int u = worker; u < units; u += workers) {
+            const GemmUnit g = gemm_unit(p, u);
+            if (!__all_sync(0xffffffffu, ptx::mbar_wait_bounded(accfull0 + 8 * acc, acc_phase, abort_flag, p.wait_limit_ns))) break;
+            ptx::tc_fence_after_sync();
+            t.row0 = (int64_t)(g.tm * CG + (int)rank) * kGemmM + quarter * 32;
+            t.rows = (int)min((int64_t)p.m - t.row0, (int64_t)1 << 20);
+            const int col0 = g.tn * BN + half * Cfg::kColsPerWarp;
+            const uint32_t src = tmem + ((uint32_t)(quarter * 32) << 16) + acc * BN + half * Cfg::kColsPerWarp;
+            float *part = nullptr;
+            if (p.splits > 1)
+                part = p.partials + (((int64_t)u * CG + rank) * kGemmEpiWarps + e) * (Cfg::kPieces * 1024);
+#pragma unroll 1
+            for (int c = 0; c < Cfg::kPieces; ++c) {
+                uint32_t raw[32];
+                ptx::tmem_ld_32x32(src + c * 32, raw);
+                ptx::tmem_ld_wait();
+                if (c == Cfg::kPieces - 1) {
+                    ptx::tc_fence_before_sync();
+                    if (lane == 0) {
+                        if (CG == 2)
+                            mbar_arrive_cluster(release0 + 8 * acc);
+                        else
+                            ptx::mbar_arrive(release0 + 8 * acc);
+                    }
+                }
+                float v[32];
+#pragma unroll
+                for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(raw[i]);
+                if (p.splits > 1) {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j)
+                        *reinterpret_cast<float4 *>(part + ((c * 8 + j) * 32 + lane) * 4) =
+                            make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
+                } else {
+                    t.col0 = col0 + c * 32;
+                    t.cols = p.n - t.col0;
+                    piece_finish<T>(p, v, t);
+                }
+            }
+            if (p.splits > 1) {
+                // the last of the tile's splits adds them all, in order, for the part of the tile that is this warp's
+                int done = 0;
+                int32_t *ticket = p.tickets + ((int64_t)(g.tile * CG + (int)rank)) * kGemmEpiWarps + e;
+                __threadfence();
+                __syncwarp();
+                if (lane == 0) done = atomicAdd(ticket, 1);
+                done = __shfl_sync(0xffffffffu, done, 0);
+                if (done == p.splits - 1) {
+                    __threadfence();
+                    const float *first = p.partials + (((int64_t)g.tile * p.splits * CG + rank) * kGemmEpiWarps + e) * (Cfg::kPieces * 1024);
+                    const int64_t pitch = (int64_t)CG * kGemmEpiWarps * Cfg::kPieces * 1024;
+#pragma unroll 1
+                    for (int c = 0; c < Cfg::kPieces; ++c) {
+                        float v[32];
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) v[i] = 0.0f;
+                        for (int s = 0; s < p.splits; ++s) {
+#pragma unroll
+                            for (int j = 0; j < 8; ++j) {
+                                const float4 q = __ldcg(reinterpret_cast<const float4 *>(first + s * pitch + ((c * 8 + j) * 32 + lane) * 4));
+                                v[4 * j] += q.x, v[4 * j + 1] += q.y, v[4 * j + 2] += q.z, v[4 * j + 3] += q.w;
+                            }
+                        }
+                        t.col0 = col0 + c * 32;
+                        t.cols = p.n - t.col0;
+                        piece_finish<T>(p, v, t);
+                    }
+                    if (lane == 0) *ticket = 0;
+                }
+            }
+            acc ^= 1u;
+            if (acc == 0) acc_phase ^= 1u;
+        }
+    }
+    ptx::tc_fence_before_sync();
+    __syncthreads();
+    if (threadIdx.x == 0 && *abort_flag) atomicMax(p.status, 6);
+    if (CG == 2) cluster_sync();
+    ptx::tc_fence_after_sync();
+    if (warp == 1) tmem_free_g<CG>(tmem, Cfg::kTmemCols);
+}
+
+// ---------------------------------------------------------------- a few rows
+// y for ROWS rows (1..8) without the tensor cores: the cost is reading w once, so w is streamed by
+// every warp of the GPU in 16-byte pieces, one output column per warp and turn; x stays in shared memory.
+template <typename T, int ROWS, bool WIDE>
+__global__ void __launch_bounds__(256) linear_few_kernel(const GemmParams p, const T *x, int64_t ldx, const T *w, int64_t ldw,
+                                                         int32_t k) {
+    extern __shared__ uint8_t smem_few[];
+    T *xs = reinterpret_cast<T *>(smem_few);  // [ROWS][k rounded up to 256], zero behind k
+    const int kp = (k + 255) & ~255;
+    const int rows = min(ROWS, p.m);
+    for (int i = threadIdx.x; i < ROWS * kp; i += blockDim.x) {
+        const int r = i / kp, c = i - r * kp;
+        xs[i] = (r < rows && c < k) ? x[r * ldx + c] : from_f32<T>(0.0f);
+    }
+    __syncthreads();
+    const int lane = threadIdx.x & 31, warps = gridDim.x * 8;
+    for (int n = blockIdx.x * 8 + (threadIdx.x >> 5); n < p.n; n += warps) {
+        const T *wr = w + (int64_t)n * ldw;
+        float acc[ROWS];
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r) acc[r] = 0.0f;
+        if (WIDE) {
+#pragma unroll 4
+            for (int c = lane * 8; c < k; c += 256) {  // k is a multiple of 8 here
+                Raw8<T> q;
+                load8(q, wr + c);
+                float wv[8], xv[8];
+                unpack8(wv, q);
+#pragma unroll
+                for (int r = 0; r < ROWS; ++r) {
+                    Raw8<T> s = *reinterpret_cast<const Raw8<T> *>(xs + r * kp + c);
+                    unpack8(xv, s);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) acc[r] = fmaf(wv[i], xv[i], acc[r]);
+                }
+            }
+        } else {
+#pragma unroll 8
+            for (int c = lane; c < k; c += 32) {
+                const float wv = to_f32(wr[c]);
+#pragma unroll
+                for (int r = 0; r < ROWS; ++r) acc[r] = fmaf(wv, to_f32(xs[r * kp + c]), acc[r]);
+            }
+        }
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r) acc[r] = warp_sum(acc[r]);
+        float v[1] = {0.0f};
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r)
+            if (lane == r) v[0] = acc[r];
+        if (lane < rows) {
+            if (p.bias) v[0] += to_f32(static_cast<const T *>(p.bias)[n]);
+            if (p.z) static_cast<T *>(p.z)[lane * p.ldz + n] = from_f32<T>(v[0]);
+            act_values(v, p.act);
+            if (p.residual) v[0] += to_f32(static_cast<const T *>(p.residual)[lane * p.ldr + n]);
+            static_cast<T *>(p.out)[lane * p.ldo + n] = from_f32<T>(v[0]);
+        }
+    }
+}
+
+// ---------------------------------------------------------------- beside the products
+// dst [rows][pitch] = src [rows][ld]: operands whose pitch or address no tile load takes.
+__global__ void __launch_bounds__(256) pack_kernel(uint16_t *dst, int64_t pitch, const uint16_t *src, int64_t ld, int64_t rows, int64_t cols) {
+    const int64_t c = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (c >= cols) return;
+    for (int64_t r = blockIdx.y; r < rows; r += gridDim.y) dst[r * pitch + c] = src[r * ld + c];
+}
+
+// dz = dy * act'(z) (where dz is wanted) and the column sums of it (where sums is) over a run of rows.
+// A warp owns 256 columns, 8 per lane; the warps of a CTA take its rows in turn and add up at the end.
+// WIDE: a lane's 8 columns are consecutive; else they are 32 apart.
+constexpr int kSlopeWarps = 8;
+template <typename T, bool WIDE>
+__global__ void __launch_bounds__(32 * kSlopeWarps) slope_kernel(T *dz, int64_t lddz, float *sums, const T *dy, int64_t lddy, const T *z,
+                                                               int64_t ldz, int act, int64_t rows, int32_t cols) {
+    __shared__ float part[kSlopeWarps][256 + 8];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int c0 = blockIdx.x * 256;
+    const int64_t r0 = rows * blockIdx.y / gridDim.y, r1 = rows * (blockIdx.y + 1) / gridDim.y;
+    float s[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+    for (int64_t r = r0 + warp; r < r1; r += kSlopeWarps) {
+        float g[8], a[8];
+        if (WIDE) {
+            const int c = c0 + lane * 8;
+            if (c >= cols) continue;
+            Raw8<T> q, y;
+            load8(q, dy + r * lddy + c);
+            if (z) load8(y, z + r * ldz + c);
+            unpack8(g, q);
+            if (z) {
+                unpack8(a, y);
+                act_slopes(a, act);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) g[i] *= a[i];
+                if (dz) store8(dz + r * lddz + c, g);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int c = c0 + lane + 32 * i;
+                g[i] = c < cols ? to_f32(dy[r * lddy + c]) : 0.0f;
+                a[i] = z && c < cols ? to_f32(z[r * ldz + c]) : 0.0f;
+            }
+            if (z) {
+                act_slopes(a, act);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) g[i] *= a[i];
+            }
+            if (dz) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const int c = c0 + lane + 32 * i;
+                    if (c < cols) dz[r * lddz + c] = from_f32<T>(g[i]);
+                }
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) s[i] += g[i];
+    }
+    if (!sums) return;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) part[warp][WIDE ? lane * 8 + i : lane + 32 * i] = s[i];
+    __syncthreads();
+    const int c = c0 + threadIdx.x;
+    if (c < cols) {
+        float v = 0.0f;
+#pragma unroll
+        for (int w = 0; w < kSlopeWarps; ++w) v += part[w][threadIdx.x];
+        sums[(int64_t)blockIdx.y * cols + c] = v;
+    }
+}
+// out = the sum of n rows of partial sums.
+template <typename T>
+__global__ void __launch_bounds__(256) add_rows_kernel(T *out, const float *sums, int n, int32_t cols) {
+    __shared__ float part[8][33];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c = blockIdx.x * 32 + lane;
+    float s = 0.0f;
+    if (c < cols)
+        for (int k = warp; k < n; k += 8) s += sums[(int64_t)k * cols + c];
+    part[warp][lane] = s;
+    __syncthreads();
+    if (warp == 0 && c < cols) {
+#pragma unroll
+        for (int w = 1; w < 8; ++w) s += part[w][lane];
+        out[c] = from_f32<T>(s);
+    }
+}
+
+}  // namespace ops
+}  // namespace egeria

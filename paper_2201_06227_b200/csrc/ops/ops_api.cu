@@ -1,0 +1,849 @@
+// Host side of the training operators (include/egeria_ops.h): argument checks, plans, launches.
+#include <algorithm>
+#include <cmath>
+#include <cstring>
+#include <new>
+#include <vector>
+
+#include <cuda.h>
+#include <cuda_runtime.h>
+
+#include "../../../include/egeria_ops.h"
+#include "adamw.cuh"
+#include "linear.cuh"
+#include "norm.cuh"
+
+#define EGO_CUDA(x)                                   \
+    do {                                              \
+        if ((x) != cudaSuccess) {                     \
+            (void)cudaGetLastError();                 \
+            return EGERIA_ERR_CUDA;                   \
+        }                                             \
+    } while (0)
+
+namespace egeria {
+namespace ops {
+
+typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
+                                  const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                  CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+constexpr size_t kAlign = 256;
+constexpr size_t kHeadBytes = EGERIA_OPS_WORKSPACE_MIN;  // status word, then the tickets of split products
+constexpr size_t kTicketOff = 256;
+constexpr int kMaxTickets = (int)((kHeadBytes - kTicketOff) / 4);
+constexpr int kMaxSplitCtas = 320;                       // CTAs' worth of partial tiles at most
+constexpr uint64_t kWaitLimitNs = 2000000000ull;
+constexpr int64_t kMaxSize = ((int64_t)1 << 31) - 1024;  // tile coordinates are 32-bit
+constexpr int kSms = 148;                                // what workspaces are sized for
+
+static size_t up(size_t v, size_t a) { return (v + a - 1) / a * a; }
+static int64_t pad8(int64_t v) { return (v + 7) / 8 * 8; }
+static bool aligned(const void *p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
+static size_t size_of(int type) { return type == EGERIA_F32 ? 4 : 2; }
+
+// ---------------------------------------------------------------- which tile for which product
+struct GemmPlan {
+    int bn, cg, splits, tiles_m, tiles_n;
+};
+
+// Time of a product of m x n x k in cycles, by a model whose terms are measured ones: a stage of 64 k takes the
+// MMAs' 2 * BN cycles or its bytes at 64 per cycle, whichever is longer; the units go in waves; the epilogue of
+// the last wave is not hidden; a split product pays for its partial sums' way through L2.
+static double gemm_cycles(const GemmPlan &g, int64_t kblocks, int sms) {
+    const double stage_bytes = 128.0 * 128 + 128.0 * g.bn / g.cg;
+    const double per_block = std::max(2.0 * g.bn, stage_bytes / 64.0);
+    const int64_t units = (int64_t)g.tiles_m * g.tiles_n * g.splits, workers = sms / g.cg;
+    const double waves = (double)((units + workers - 1) / workers);
+    const double main_loop = (double)((kblocks + g.splits - 1) / g.splits) * per_block;
+    const double epilogue = 6.0 * g.bn;
+    double t = waves * std::max(main_loop, epilogue) + epilogue + (g.cg == 2 ? 600.0 : 0.0);
+    if (g.splits > 1) t += 2500.0 + 4.0 * g.bn + 4.0 * g.bn * g.splits;
+    return t;
+}
+
+static GemmPlan plan_gemm(int64_t m, int64_t n, int64_t k, int sms) {
+    const int64_t kblocks = (k + kGemmK - 1) / kGemmK;
+    GemmPlan best{};
+    double best_t = 1e300;
+    for (int cg = 1; cg <= 2; ++cg)
+        for (int bn = 64; bn <= 256; bn *= 2) {
+            if (cg == 2 && bn == 64) continue;
+            GemmPlan g{bn, cg, 1, (int)((m + 128 * cg - 1) / (128 * cg)), (int)((n + bn - 1) / bn)};
+            const int64_t tiles = (int64_t)g.tiles_m * g.tiles_n;
+            for (g.splits = 1; g.splits <= 64 && g.splits <= kblocks; ++g.splits) {
+                if (g.splits > 1 && (tiles * g.splits * cg > std::min(sms, kMaxSplitCtas) || tiles * cg * kGemmEpiWarps > kMaxTickets)) break;
+                const double t = gemm_cycles(g, kblocks, sms);
+                if (t < best_t) best_t = t, best = g;
+            }
+        }
+    return best;
+}
+
+// Bytes of partial tiles that a product of these sizes may need under any plan.
+static size_t split_bytes(int64_t m, int64_t n, int64_t k) {
+    const int64_t kblocks = std::min<int64_t>((k + kGemmK - 1) / kGemmK, 64);
+    if (kblocks <= 1) return 0;
+    const int64_t tiles = ((m + 255) / 256) * 2 * ((n + 255) / 256);  // of 128 x 256
+    if (tiles > kMaxSplitCtas) return 0;
+    return (size_t)std::min<int64_t>(tiles * kblocks, kMaxSplitCtas) * 128 * 256 * 4;
+}
+
+constexpr int kSlopeChunks = 592;  // partial rows of a column sum at most: four CTAs per SM
+static int slope_chunks(int64_t rows, int64_t cols) {
+    const int64_t strips = (cols + 255) / 256;
+    return (int)std::max<int64_t>(1, std::min<int64_t>((rows + 31) / 32, std::max<int64_t>(1, kSlopeChunks / strips)));
+}
+
+struct LinearLayout {
+    size_t part, x, w, dz, sums, total;
+};
+static LinearLayout linear_layout(int64_t rows, int64_t inp, int64_t out) {
+    LinearLayout L;
+    size_t off = kHeadBytes;
+    auto take = [&](size_t n) {
+        const size_t at = off;
+        off = up(off + n, 1024);
+        return at;
+    };
+    L.part = take(std::max(std::max(split_bytes(rows, out, inp), split_bytes(rows, inp, out)), split_bytes(out, inp, rows)));
+    L.x = take((size_t)rows * pad8(inp) * 2);
+    L.w = take((size_t)out * pad8(inp) * 2);
+    L.dz = take((size_t)rows * pad8(out) * 2);
+    L.sums = take((size_t)slope_chunks(rows, out) * out * 4);
+    L.total = off;
+    return L;
+}
+
+// ---------------------------------------------------------------- norms
+struct NormPlan {
+    int team, vpt, ctas;  // ctas: of the backward pass
+};
+static NormPlan norm_backward_plan(int64_t rows, int64_t cols) {
+    NormPlan n{32, 1, 16};
+    if (cols > 4096) n = {1024, 1, 1};
+    else if (cols > 2048) n = {512, 1, 1};
+    else if (cols > 1024) n = {256, 1, 2};
+    else if (cols > 512) n = {128, 1, 4};
+    else if (cols > 256) n = {64, 1, 8};
+    n.ctas = (int)std::min<int64_t>(rows, (int64_t)n.ctas * kSms);
+    return n;
+}
+
+}  // namespace ops
+}  // namespace egeria
+
+using namespace egeria;
+using namespace egeria::ops;
+
+struct egeria_ops {
+    uint8_t *ws = nullptr;
+    size_t ws_bytes = 0;
+    EncodeTiledFn encode = nullptr;
+    int sms = 0;
+    int64_t launches = 0;
+    cudaStream_t last_stream = nullptr;
+};
+
+namespace egeria {
+namespace ops {
+
+template <typename T, int BN, int CG>
+static cudaError_t allow_smem() {
+    return cudaFuncSetAttribute(gemm_kernel<T, BN, CG>, cudaFuncAttributeMaxDynamicSharedMemorySize, GemmCfg<BN, CG>::kSmem);
+}
+constexpr int kFewSmem = 96 * 1024;
+template <typename T, int ROWS>
+static cudaError_t allow_few() {
+    cudaError_t e = cudaFuncSetAttribute(linear_few_kernel<T, ROWS, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, kFewSmem);
+    if (e == cudaSuccess)
+        e = cudaFuncSetAttribute(linear_few_kernel<T, ROWS, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, kFewSmem);
+    return e;
+}
+template <typename T>
+static cudaError_t allow_all() {
+    cudaError_t e = allow_smem<T, 64, 1>();
+    if (e == cudaSuccess) e = allow_smem<T, 128, 1>();
+    if (e == cudaSuccess) e = allow_smem<T, 256, 1>();
+    if (e == cudaSuccess) e = allow_smem<T, 128, 2>();
+    if (e == cudaSuccess) e = allow_smem<T, 256, 2>();
+    if (e == cudaSuccess) e = allow_few<T, 1>();
+    if (e == cudaSuccess) e = allow_few<T, 2>();
+    if (e == cudaSuccess) e = allow_few<T, 4>();
+    if (e == cudaSuccess) e = allow_few<T, 8>();
+    return e;
+}
+
+struct Operand {
+    const void *p;
+    int64_t ld, rows, cols;
+    bool mn;  // the product's m (n) axis is the consecutive one: cols = m (n), rows = k
+};
+
+static egeria_status encode_operand(const egeria_ops *o, CUtensorMap *map, const Operand &a, int type, int box_rows) {
+    cuuint64_t dims[2] = {(cuuint64_t)a.cols, (cuuint64_t)a.rows};
+    cuuint64_t strides[1] = {(cuuint64_t)a.ld * 2};
+    cuuint32_t box[2] = {64, (cuuint32_t)(a.mn ? 64 : box_rows)};
+    cuuint32_t one[2] = {1, 1};
+    const CUresult r = o->encode(map, type == EGERIA_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2,
+                                 const_cast<void *>(a.p), dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                                 CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS ? EGERIA_OK : EGERIA_ERR_CUDA;
+}
+
+template <typename T, int BN, int CG>
+static cudaError_t launch_gemm(const GemmParams &p, int ctas, cudaStream_t stream) {
+    cudaLaunchConfig_t c{};
+    c.gridDim = dim3(ctas);
+    c.blockDim = dim3(kGemmThreads);
+    c.dynamicSmemBytes = GemmCfg<BN, CG>::kSmem;
+    c.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = CG;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    c.attrs = attr;
+    c.numAttrs = CG > 1 ? 1 : 0;
+    return cudaLaunchKernelEx(&c, gemm_kernel<T, BN, CG>, p);
+}
+template <typename T>
+static cudaError_t launch_gemm_any(const GemmPlan &g, const GemmParams &p, int ctas, cudaStream_t stream) {
+    if (g.cg == 2) return g.bn == 128 ? launch_gemm<T, 128, 2>(p, ctas, stream) : launch_gemm<T, 256, 2>(p, ctas, stream);
+    if (g.bn == 64) return launch_gemm<T, 64, 1>(p, ctas, stream);
+    return g.bn == 128 ? launch_gemm<T, 128, 1>(p, ctas, stream) : launch_gemm<T, 256, 1>(p, ctas, stream);
+}
+
+// Widest access that all of a product's epilogue matrices take: 2 = 32 bytes, 1 = 16 bytes, 0 = one value.
+static int epilogue_width(const GemmParams &p) {
+    int w = 2;
+    auto see = [&](const void *q, int64_t ld) {
+        if (!q) return;
+        if (!aligned(q, 32) || ld % 16) w = std::min(w, aligned(q, 16) && ld % 8 == 0 ? 1 : 0);
+    };
+    see(p.out, p.ldo);
+    see(p.z, p.ldz);
+    see(p.residual, p.ldr);
+    see(p.z_in, p.ldz_in);
+    return w;
+}
+
+// D = A B^T with the epilogue that `p` already describes; k = the length of the summed axis.
+static egeria_status run_gemm(egeria_ops *o, cudaStream_t stream, int type, int64_t m, int64_t n, int64_t k, const Operand &a,
+                              const Operand &b, size_t part_off, GemmParams &p) {
+    const GemmPlan g = plan_gemm(m, n, k, o->sms);
+    if (g.splits > 1 && (size_t)g.tiles_m * g.tiles_n * g.splits * g.cg * 128 * g.bn * 4 > split_bytes(m, n, k)) return EGERIA_ERR_WORKSPACE;
+    egeria_status s = encode_operand(o, &p.a, a, type, kGemmM);
+    if (s == EGERIA_OK) s = encode_operand(o, &p.b, b, type, g.bn / g.cg);
+    if (s != EGERIA_OK) return s;
+    p.m = (int32_t)m;
+    p.n = (int32_t)n;
+    p.kblocks = (int32_t)((k + kGemmK - 1) / kGemmK);
+    p.tiles_m = g.tiles_m;
+    p.tiles_n = g.tiles_n;
+    p.splits = g.splits;
+    // a strip of B of at most 16 MB, so that it stays in L2 next to the rows of A that go by
+    p.group_n = (int32_t)std::max<int64_t>(1, std::min<int64_t>(g.tiles_n, ((int64_t)16 << 20) / (2 * k * g.bn)));
+    p.a_mn = a.mn;
+    p.b_mn = b.mn;
+    p.is_f16 = type == EGERIA_F16;
+    p.wide = epilogue_width(p);
+    p.partials = reinterpret_cast<float *>(o->ws + part_off);
+    p.tickets = reinterpret_cast<int32_t *>(o->ws + kTicketOff);
+    p.status = reinterpret_cast<int32_t *>(o->ws);
+    p.wait_limit_ns = kWaitLimitNs;
+    const int64_t units = (int64_t)g.tiles_m * g.tiles_n * g.splits;
+    if (units > 0x7fffffff) return EGERIA_ERR_UNSUPPORTED_SHAPE;
+    const int ctas = (int)std::min<int64_t>(units, o->sms / g.cg) * g.cg;
+    EGO_CUDA(type == EGERIA_BF16 ? launch_gemm_any<bf16>(g, p, ctas, stream) : launch_gemm_any<f16>(g, p, ctas, stream));
+    ++o->launches;
+    return EGERIA_OK;
+}
+
+// The operand as a tile load takes it: itself, or its copy at `spare` with a pitch of pad8(cols).
+static egeria_status loadable(egeria_ops *o, cudaStream_t stream, Operand &a, size_t spare) {
+    if (aligned(a.p, 16) && a.ld % 8 == 0) return EGERIA_OK;
+    uint16_t *dst = reinterpret_cast<uint16_t *>(o->ws + spare);
+    const int64_t pitch = pad8(a.cols);
+    const dim3 grid((unsigned)((a.cols + 255) / 256), (unsigned)std::min<int64_t>(a.rows, 16384));
+    pack_kernel<<<grid, 256, 0, stream>>>(dst, pitch, static_cast<const uint16_t *>(a.p), a.ld, a.rows, a.cols);
+    EGO_CUDA(cudaGetLastError());
+    ++o->launches;
+    a.p = dst;
+    a.ld = pitch;
+    return EGERIA_OK;
+}
+
+template <typename T, int ROWS>
+static cudaError_t launch_few(const GemmParams &p, const egeria_linear_forward_args &a, bool wide, int sms, cudaStream_t stream) {
+    const int smem = ROWS * (int)((a.inp + 255) / 256 * 256) * 2;
+    const int grid = (int)std::min<int64_t>((a.out + 7) / 8, (int64_t)sms * 4);
+    const T *x = static_cast<const T *>(a.x), *w = static_cast<const T *>(a.w);
+    if (wide)
+        linear_few_kernel<T, ROWS, true><<<grid, 256, smem, stream>>>(p, x, a.ldx, w, a.ldw, (int32_t)a.inp);
+    else
+        linear_few_kernel<T, ROWS, false><<<grid, 256, smem, stream>>>(p, x, a.ldx, w, a.ldw, (int32_t)a.inp);
+    return cudaGetLastError();
+}
+template <typename T>
+static cudaError_t launch_few_any(const GemmParams &p, const egeria_linear_forward_args &a, bool wide, int sms, cudaStream_t stream) {
+    if (a.rows <= 1) return launch_few<T, 1>(p, a, wide, sms, stream);
+    if (a.rows <= 2) return launch_few<T, 2>(p, a, wide, sms, stream);
+    if (a.rows <= 4) return launch_few<T, 4>(p, a, wide, sms, stream);
+    return launch_few<T, 8>(p, a, wide, sms, stream);
+}
+
+// dz (or null) and the column sums db (or null) of dy * act'(z).
+template <typename T>
+static egeria_status run_slope(egeria_ops *o, cudaStream_t stream, const egeria_linear_backward_args &a, T *dz, int64_t lddz, size_t sums_off) {
+    const T *z = a.act == EGERIA_ACT_NONE ? nullptr : static_cast<const T *>(a.z);
+    const bool wide = a.out % 8 == 0 && aligned(a.dy, 16) && a.lddy % 8 == 0 && (!z || (aligned(z, 16) && a.ldz % 8 == 0)) && (z || !dz);
+    const int chunks = slope_chunks(a.rows, a.out);
+    float *sums = a.db ? reinterpret_cast<float *>(o->ws + sums_off) : nullptr;
+    const dim3 grid((unsigned)((a.out + 255) / 256), (unsigned)chunks);
+    const T *dy = static_cast<const T *>(a.dy);
+    if (wide)
+        slope_kernel<T, true><<<grid, 32 * kSlopeWarps, 0, stream>>>(dz, lddz, sums, dy, a.lddy, z, a.ldz, a.act, a.rows, (int32_t)a.out);
+    else
+        slope_kernel<T, false><<<grid, 32 * kSlopeWarps, 0, stream>>>(dz, lddz, sums, dy, a.lddy, z, a.ldz, a.act, a.rows, (int32_t)a.out);
+    EGO_CUDA(cudaGetLastError());
+    ++o->launches;
+    if (a.db) {
+        add_rows_kernel<T><<<(unsigned)((a.out + 31) / 32), 256, 0, stream>>>(static_cast<T *>(a.db), sums, chunks, (int32_t)a.out);
+        EGO_CUDA(cudaGetLastError());
+        ++o->launches;
+    }
+    return EGERIA_OK;
+}
+
+static bool good_matrix(const void *p, int64_t ld, int64_t cols, size_t elem) { return p && aligned(p, elem) && ld >= cols; }
+static bool good_optional(const void *p, int64_t ld, int64_t cols, size_t elem) { return !p || good_matrix(p, ld, cols, elem); }
+static bool good_act(int act) { return act >= EGERIA_ACT_NONE && act <= EGERIA_ACT_SILU; }
+static egeria_status good_sizes(int64_t rows, int64_t inp, int64_t out) {
+    if (rows < 0 || inp < 1 || out < 1) return EGERIA_ERR_INVALID_ARG;
+    return rows > kMaxSize || inp > kMaxSize || out > kMaxSize ? EGERIA_ERR_UNSUPPORTED_SHAPE : EGERIA_OK;
+}
+
+// ---------------------------------------------------------------- norm launches
+template <typename T, int TEAM, int VPT>
+static cudaError_t norm_fwd(const NormParams &p, bool wide, cudaStream_t stream) {
+    const int64_t per = TEAM == 32 ? 4 : 1;
+    const unsigned grid = (unsigned)((p.rows + per - 1) / per);
+    if (wide)
+        norm_forward_kernel<T, TEAM, VPT, true><<<grid, TEAM == 32 ? 128 : TEAM, 0, stream>>>(p);
+    else
+        norm_forward_kernel<T, TEAM, VPT, false><<<grid, TEAM == 32 ? 128 : TEAM, 0, stream>>>(p);
+    return cudaGetLastError();
+}
+template <typename T>
+static cudaError_t norm_fwd_any(const NormParams &p, bool wide, cudaStream_t stream) {
+    if (p.cols <= 256) return norm_fwd<T, 32, 1>(p, wide, stream);
+    if (p.cols <= 512) return norm_fwd<T, 32, 2>(p, wide, stream);
+    if (p.cols <= 1024) return norm_fwd<T, 32, 4>(p, wide, stream);
+    if (p.cols <= 4096) return norm_fwd<T, 128, 4>(p, wide, stream);
+    return norm_fwd<T, 256, 4>(p, wide, stream);
+}
+template <typename T, int TEAM, int VPT>
+static cudaError_t norm_bwd(const NormParams &p, int ctas, bool wide, cudaStream_t stream) {
+    if (wide)
+        norm_backward_kernel<T, TEAM, VPT, true><<<ctas, TEAM, 0, stream>>>(p);
+    else
+        norm_backward_kernel<T, TEAM, VPT, false><<<ctas, TEAM, 0, stream>>>(p);
+    return cudaGetLastError();
+}
+template <typename T>
+static cudaError_t norm_bwd_any(const NormParams &p, const NormPlan &n, bool wide, bool sums, cudaStream_t stream) {
+    cudaError_t e;
+    switch (n.team) {
+        case 32: e = norm_bwd<T, 32, 1>(p, n.ctas, wide, stream); break;
+        case 64: e = norm_bwd<T, 64, 1>(p, n.ctas, wide, stream); break;
+        case 128: e = norm_bwd<T, 128, 1>(p, n.ctas, wide, stream); break;
+        case 256: e = norm_bwd<T, 256, 1>(p, n.ctas, wide, stream); break;
+        case 512: e = norm_bwd<T, 512, 1>(p, n.ctas, wide, stream); break;
+        default: e = norm_bwd<T, 1024, 1>(p, n.ctas, wide, stream); break;
+    }
+    if (e != cudaSuccess || !sums) return e;
+    norm_sums_kernel<T><<<dim3((unsigned)((p.cols + 31) / 32), 4 + (p.dgate ? n.ctas : 0)), 256, 0, stream>>>(p, n.ctas);
+    return cudaGetLastError();
+}
+
+static egeria_status device_ready(int *sms) {
+    int dev = 0, major = 0;
+    EGO_CUDA(cudaGetDevice(&dev));
+    EGO_CUDA(cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, dev));
+    if (major != 10) return EGERIA_ERR_UNSUPPORTED_DEVICE;
+    EGO_CUDA(cudaDeviceGetAttribute(sms, cudaDevAttrMultiProcessorCount, dev));
+    return EGERIA_OK;
+}
+
+// ---------------------------------------------------------------- AdamW tables
+typedef void (*AdamKernel)(AdamParams);
+template <bool SMALL>
+static AdamKernel adam_kernel(int p, int g, bool master) {
+    if (p == EGERIA_F32) return master ? adamw_kernel<float, float, true, SMALL> : adamw_kernel<float, float, false, SMALL>;
+    if (p == EGERIA_BF16) {
+        if (g == EGERIA_F32) return master ? adamw_kernel<bf16, float, true, SMALL> : adamw_kernel<bf16, float, false, SMALL>;
+        return master ? adamw_kernel<bf16, bf16, true, SMALL> : adamw_kernel<bf16, bf16, false, SMALL>;
+    }
+    if (g == EGERIA_F32) return master ? adamw_kernel<f16, float, true, SMALL> : adamw_kernel<f16, float, false, SMALL>;
+    return master ? adamw_kernel<f16, f16, true, SMALL> : adamw_kernel<f16, f16, false, SMALL>;
+}
+// Tensors of one combination of types go through one launch.
+constexpr int kAdamClasses = 18;
+static int adam_class(const egeria_adamw_tensor &t) { return (t.param_type * 3 + t.grad_type) * 2 + (t.master ? 1 : 0); }
+
+static bool good_adam_tensor(const egeria_adamw_tensor &t, uint32_t flags) {
+    if (t.n < 0 || t.param_type < EGERIA_F32 || t.param_type > EGERIA_F16 || t.module < -1) return false;
+    if (t.grad_type != EGERIA_F32 && t.grad_type != t.param_type) return false;
+    if (!(t.weight_decay >= 0.0f) || !std::isfinite(t.weight_decay)) return false;
+    if (t.n == 0) return true;
+    if (!t.param || !t.m || !t.v || !aligned(t.param, size_of(t.param_type)) || !aligned(t.master, 4)) return false;
+    if (flags & EGERIA_ADAMW_8BIT) return t.m_scale && t.v_scale && aligned(t.m_scale, 4) && aligned(t.v_scale, 4);
+    return aligned(t.m, 4) && aligned(t.v, 4);
+}
+
+struct AdamLayout {
+    size_t tensors, grads, chunks, tickets, total;
+    int64_t n_chunks;
+};
+static bool adam_layout(int count, const egeria_adamw_tensor *t, AdamLayout &L) {
+    L.n_chunks = 0;
+    for (int i = 0; i < count; ++i) {
+        const int64_t c = (t[i].n + kAdamChunk - 1) / kAdamChunk;
+        if (t[i].n < 0 || c > 0x7fffffff) return false;
+        L.n_chunks += c;
+    }
+    if (L.n_chunks > 0x7fffffff) return false;
+    L.tickets = 0;  // [0] status words, then one ticket per class, 128 bytes apart
+    L.tensors = 128 * (1 + kAdamClasses);
+    L.grads = up(L.tensors + (size_t)count * sizeof(AdamTensor), kAlign);
+    L.chunks = up(L.grads + (size_t)count * sizeof(void *), kAlign);
+    L.total = up(L.chunks + (size_t)L.n_chunks * sizeof(int2), kAlign);
+    return true;
+}
+
+}  // namespace ops
+}  // namespace egeria
+
+struct egeria_adamw {
+    struct Class {
+        AdamKernel kernel;
+        AdamParams params;
+        int grid;
+    };
+    std::vector<Class> classes;
+    uint8_t *ws = nullptr;
+    AdamLayout L{};
+    int count = 0;
+    std::vector<size_t> grad_size;   // 0 for an empty tensor
+    int64_t launches = 0;
+    cudaStream_t last_stream = nullptr;
+};
+
+extern "C" {
+
+// ---------------------------------------------------------------- handle
+egeria_status egeria_ops_create(egeria_ops **out, void *workspace, size_t workspace_bytes) {
+    if (!out) return EGERIA_ERR_INVALID_ARG;
+    *out = nullptr;
+    if (!workspace || !aligned(workspace, EGERIA_WORKSPACE_ALIGN) || workspace_bytes < EGERIA_OPS_WORKSPACE_MIN) return EGERIA_ERR_WORKSPACE;
+    int sms = 0;
+    egeria_status s = device_ready(&sms);
+    if (s != EGERIA_OK) return s;
+    void *fn = nullptr;
+    cudaDriverEntryPointQueryResult q;
+    if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &q) != cudaSuccess || q != cudaDriverEntryPointSuccess || !fn) {
+        (void)cudaGetLastError();
+        return EGERIA_ERR_CUDA;
+    }
+    EGO_CUDA(allow_all<bf16>());
+    EGO_CUDA(allow_all<f16>());
+    EGO_CUDA(cudaMemset(workspace, 0, kHeadBytes));
+    EGO_CUDA(cudaDeviceSynchronize());
+    egeria_ops *o = new (std::nothrow) egeria_ops();
+    if (!o) return EGERIA_ERR_INVALID_ARG;
+    o->ws = static_cast<uint8_t *>(workspace);
+    o->ws_bytes = workspace_bytes;
+    o->encode = reinterpret_cast<EncodeTiledFn>(fn);
+    o->sms = std::min(sms, kMaxSplitCtas);
+    *out = o;
+    return EGERIA_OK;
+}
+egeria_status egeria_ops_destroy(egeria_ops *ops) {
+    if (!ops) return EGERIA_ERR_INVALID_ARG;
+    delete ops;
+    return EGERIA_OK;
+}
+egeria_status egeria_ops_device_status(egeria_ops *ops) {
+    if (!ops) return EGERIA_ERR_INVALID_ARG;
+    EGO_CUDA(cudaStreamSynchronize(ops->last_stream));
+    int32_t v = 0;
+    EGO_CUDA(cudaMemcpy(&v, ops->ws, sizeof(v), cudaMemcpyDeviceToHost));
+    if (v == 0) return EGERIA_OK;
+    EGO_CUDA(cudaMemset(ops->ws, 0, kHeadBytes));  // tickets too: a call that gave up may have left some
+    return static_cast<egeria_status>(v);
+}
+int64_t egeria_ops_launch_count(const egeria_ops *ops) { return ops ? ops->launches : 0; }
+
+// ---------------------------------------------------------------- linear
+size_t egeria_linear_workspace_bytes(int64_t rows, int64_t inp, int64_t out) {
+    if (good_sizes(rows, inp, out) != EGERIA_OK) return 0;
+    return linear_layout(rows, inp, out).total;
+}
+
+egeria_status egeria_linear_forward(egeria_ops *ops, void *cuda_stream, const egeria_linear_forward_args *args) {
+    if (!ops || !args) return EGERIA_ERR_INVALID_ARG;
+    const egeria_linear_forward_args &a = *args;
+    if ((a.type != EGERIA_BF16 && a.type != EGERIA_F16) || !good_act(a.act)) return EGERIA_ERR_INVALID_ARG;
+    egeria_status s = good_sizes(a.rows, a.inp, a.out);
+    if (s != EGERIA_OK) return s;
+    if (a.rows == 0) return EGERIA_OK;
+    if (!good_matrix(a.x, a.ldx, a.inp, 2) || !good_matrix(a.w, a.ldw, a.inp, 2) || !good_matrix(a.y, a.ldy, a.out, 2) ||
+        !good_optional(a.residual, a.ldr, a.out, 2) || !good_optional(a.z, a.ldz, a.out, 2) || !aligned(a.bias, 2))
+        return EGERIA_ERR_INVALID_ARG;
+    const LinearLayout L = linear_layout(a.rows, a.inp, a.out);
+    if (ops->ws_bytes < L.total) return EGERIA_ERR_WORKSPACE;
+    cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+    ops->last_stream = stream;
+    GemmParams p;
+    memset(&p, 0, sizeof(p));
+    p.bias = a.bias;
+    p.residual = a.residual;
+    p.ldr = a.ldr;
+    p.out = a.y;
+    p.ldo = a.ldy;
+    p.z = a.z;
+    p.ldz = a.ldz;
+    p.act = a.act;
+    const int few_rows = a.rows <= 1 ? 1 : a.rows <= 2 ? 2 : a.rows <= 4 ? 4 : 8;
+    if (a.rows <= 8 && (a.inp + 255) / 256 * 256 * 2 * few_rows <= kFewSmem) {
+        p.m = (int32_t)a.rows;
+        p.n = (int32_t)a.out;
+        const bool wide = a.inp % 8 == 0 && a.ldw % 8 == 0 && aligned(a.w, 16);
+        EGO_CUDA(a.type == EGERIA_BF16 ? launch_few_any<bf16>(p, a, wide, ops->sms, stream) : launch_few_any<f16>(p, a, wide, ops->sms, stream));
+        ++ops->launches;
+        return EGERIA_OK;
+    }
+    Operand x{a.x, a.ldx, a.rows, a.inp, false}, w{a.w, a.ldw, a.out, a.inp, false};
+    if ((s = loadable(ops, stream, x, L.x)) != EGERIA_OK || (s = loadable(ops, stream, w, L.w)) != EGERIA_OK) return s;
+    return run_gemm(ops, stream, a.type, a.rows, a.out, a.inp, x, w, L.part, p);
+}
+
+egeria_status egeria_linear_backward(egeria_ops *ops, void *cuda_stream, const egeria_linear_backward_args *args) {
+    if (!ops || !args) return EGERIA_ERR_INVALID_ARG;
+    const egeria_linear_backward_args &a = *args;
+    if ((a.type != EGERIA_BF16 && a.type != EGERIA_F16) || !good_act(a.act) || !good_act(a.act_in)) return EGERIA_ERR_INVALID_ARG;
+    egeria_status s = good_sizes(a.rows, a.inp, a.out);
+    if (s != EGERIA_OK) return s;
+    if (!good_optional(a.dx, a.lddx, a.inp, 2) || !good_optional(a.dw, a.lddw, a.inp, 2) || !aligned(a.db, 2)) return EGERIA_ERR_INVALID_ARG;
+    cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+    if (a.rows == 0) {
+        ops->last_stream = stream;
+        if (a.dw) EGO_CUDA(cudaMemset2DAsync(a.dw, (size_t)a.lddw * 2, 0, (size_t)a.inp * 2, (size_t)a.out, stream));
+        if (a.db) EGO_CUDA(cudaMemsetAsync(a.db, 0, (size_t)a.out * 2, stream));
+        return EGERIA_OK;
+    }
+    if (!good_matrix(a.dy, a.lddy, a.out, 2)) return EGERIA_ERR_INVALID_ARG;
+    if (a.act != EGERIA_ACT_NONE && !good_matrix(a.z, a.ldz, a.out, 2)) return EGERIA_ERR_INVALID_ARG;
+    if (a.dw && !good_matrix(a.x, a.ldx, a.inp, 2)) return EGERIA_ERR_INVALID_ARG;
+    if (a.dx && !good_matrix(a.w, a.ldw, a.inp, 2)) return EGERIA_ERR_INVALID_ARG;
+    if (a.dx && a.act_in != EGERIA_ACT_NONE && !good_matrix(a.z_in, a.ldz_in, a.inp, 2)) return EGERIA_ERR_INVALID_ARG;
+    const LinearLayout L = linear_layout(a.rows, a.inp, a.out);
+    if (ops->ws_bytes < L.total) return EGERIA_ERR_WORKSPACE;
+    ops->last_stream = stream;
+
+    const bool products = a.dx || a.dw;
+    Operand dz{a.dy, a.lddy, a.rows, a.out, false};
+    const bool own_dz = products && (a.act != EGERIA_ACT_NONE || !aligned(a.dy, 16) || a.lddy % 8 != 0);
+    if (own_dz) {
+        dz.p = ops->ws + L.dz;
+        dz.ld = pad8(a.out);
+    }
+    if (own_dz || a.db) {
+        void *to = own_dz ? ops->ws + L.dz : nullptr;
+        s = a.type == EGERIA_BF16 ? run_slope<bf16>(ops, stream, a, static_cast<bf16 *>(to), dz.ld, L.sums)
+                                  : run_slope<f16>(ops, stream, a, static_cast<f16 *>(to), dz.ld, L.sums);
+        if (s != EGERIA_OK) return s;
+    }
+    if (a.dx) {
+        Operand w{a.w, a.ldw, a.out, a.inp, true};
+        if ((s = loadable(ops, stream, w, L.w)) != EGERIA_OK) return s;
+        GemmParams p;
+        memset(&p, 0, sizeof(p));
+        p.out = a.dx;
+        p.ldo = a.lddx;
+        if (a.act_in != EGERIA_ACT_NONE) {
+            p.z_in = a.z_in;
+            p.ldz_in = a.ldz_in;
+            p.act_in = a.act_in;
+        }
+        if ((s = run_gemm(ops, stream, a.type, a.rows, a.inp, a.out, dz, w, L.part, p)) != EGERIA_OK) return s;
+    }
+    if (a.dw) {
+        Operand x{a.x, a.ldx, a.rows, a.inp, true};
+        if ((s = loadable(ops, stream, x, L.x)) != EGERIA_OK) return s;
+        dz.mn = true;
+        GemmParams p;
+        memset(&p, 0, sizeof(p));
+        p.out = a.dw;
+        p.ldo = a.lddw;
+        if ((s = run_gemm(ops, stream, a.type, a.out, a.inp, a.rows, dz, x, L.part, p)) != EGERIA_OK) return s;
+    }
+    return EGERIA_OK;
+}
+
+// ---------------------------------------------------------------- norms
+size_t egeria_norm_workspace_bytes(int64_t rows, int64_t cols) {
+    if (rows < 0 || cols < 1 || cols > EGERIA_NORM_MAX_COLS) return 0;
+    return kHeadBytes + up((size_t)norm_backward_plan(rows, cols).ctas * kNormSums * cols * 4, 1024);
+}
+
+egeria_status egeria_norm_forward(egeria_ops *ops, void *cuda_stream, const egeria_norm_forward_args *args) {
+    if (!ops || !args) return EGERIA_ERR_INVALID_ARG;
+    const egeria_norm_forward_args &a = *args;
+    if (a.type < EGERIA_F32 || a.type > EGERIA_F16 || (a.param_type != EGERIA_F32 && a.param_type != a.type) ||
+        (a.kind != EGERIA_NORM_LAYER && a.kind != EGERIA_NORM_RMS) || a.rows < 0 || a.cols < 1 || a.gate_rows < 0 || !(a.eps >= 0.0f))
+        return EGERIA_ERR_INVALID_ARG;
+    if (a.cols > EGERIA_NORM_MAX_COLS || a.rows > kMaxSize) return EGERIA_ERR_UNSUPPORTED_SHAPE;
+    if (a.rows == 0) return EGERIA_OK;
+    const size_t e = size_of(a.type), pe = size_of(a.param_type);
+    if (!good_matrix(a.x, a.ldx, a.cols, e) || !good_matrix(a.f, a.ldf, a.cols, e) || !good_matrix(a.y, a.ldy, a.cols, e) ||
+        (a.pre && !good_matrix(a.h, a.ldh, a.cols, e)) || !aligned(a.stats, 16))
+        return EGERIA_ERR_INVALID_ARG;
+    const void *vec[5] = {a.gate, a.w_post, a.b_post, a.w_pre, a.b_pre};
+    const size_t row_align = 8 * e, vec_align = 8 * pe;
+    bool wide = a.cols % 8 == 0 && aligned(a.x, row_align) && aligned(a.f, row_align) && aligned(a.y, row_align) && a.ldx % 8 == 0 &&
+                a.ldf % 8 == 0 && a.ldy % 8 == 0 && (!a.pre || (aligned(a.h, row_align) && a.ldh % 8 == 0));
+    for (const void *v : vec) {
+        if (!aligned(v, pe)) return EGERIA_ERR_INVALID_ARG;
+        wide = wide && aligned(v, vec_align);
+    }
+    NormParams p;
+    memset(&p, 0, sizeof(p));
+    p.x = a.x, p.ldx = a.ldx;
+    p.f = a.f, p.ldf = a.ldf;
+    p.gate = a.gate;
+    if (a.post) p.w_post = a.w_post, p.b_post = a.b_post;
+    if (a.pre) p.w_pre = a.w_pre, p.b_pre = a.b_pre;
+    p.y = a.y, p.ldy = a.ldy;
+    p.h = a.h, p.ldh = a.ldh;
+    p.stats = a.stats;
+    p.rows = a.rows;
+    p.gate_rows = a.gate_rows ? a.gate_rows : a.rows;
+    p.cols = (int32_t)a.cols;
+    p.layer = a.kind == EGERIA_NORM_LAYER;
+    p.post = a.post != 0;
+    p.pre = a.pre != 0;
+    p.w_float = a.param_type == EGERIA_F32;
+    p.alpha = a.alpha;
+    p.eps = a.eps;
+    p.inv_cols = 1.0f / (float)a.cols;
+    cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+    ops->last_stream = stream;
+    EGO_CUDA(a.type == EGERIA_F32    ? norm_fwd_any<float>(p, wide, stream)
+             : a.type == EGERIA_BF16 ? norm_fwd_any<bf16>(p, wide, stream)
+                                     : norm_fwd_any<f16>(p, wide, stream));
+    ++ops->launches;
+    return EGERIA_OK;
+}
+
+egeria_status egeria_norm_backward(egeria_ops *ops, void *cuda_stream, const egeria_norm_backward_args *args) {
+    if (!ops || !args) return EGERIA_ERR_INVALID_ARG;
+    const egeria_norm_backward_args &a = *args;
+    if (a.type < EGERIA_F32 || a.type > EGERIA_F16 || (a.param_type != EGERIA_F32 && a.param_type != a.type) ||
+        (a.kind != EGERIA_NORM_LAYER && a.kind != EGERIA_NORM_RMS) || a.rows < 0 || a.cols < 1 || a.gate_rows < 0)
+        return EGERIA_ERR_INVALID_ARG;
+    if (a.cols > EGERIA_NORM_MAX_COLS || a.rows > kMaxSize) return EGERIA_ERR_UNSUPPORTED_SHAPE;
+    const size_t e = size_of(a.type), pe = size_of(a.param_type);
+    const void *vec[10] = {a.gate, a.w_post, a.b_post, a.w_pre, a.b_pre, a.dgate, a.dw_post, a.db_post, a.dw_pre, a.db_pre};
+    for (const void *v : vec)
+        if (!aligned(v, pe)) return EGERIA_ERR_INVALID_ARG;
+    if ((a.dgate && !a.gate) || (!a.post && (a.dw_post || a.db_post)) || (!a.pre && (a.dw_pre || a.db_pre))) return EGERIA_ERR_INVALID_ARG;
+    cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+    if (a.rows == 0) {
+        ops->last_stream = stream;
+        void *const outs[5] = {a.gate_rows == 0 ? a.dgate : nullptr, a.dw_post, a.db_post, a.dw_pre, a.db_pre};
+        for (void *o : outs)
+            if (o) EGO_CUDA(cudaMemsetAsync(o, 0, (size_t)a.cols * pe, stream));
+        return EGERIA_OK;
+    }
+    if (!good_matrix(a.dy, a.lddy, a.cols, e) || !good_matrix(a.f, a.ldf, a.cols, e) || !good_matrix(a.dx, a.lddx, a.cols, e) ||
+        !good_matrix(a.df, a.lddf, a.cols, e) || !a.stats || !aligned(a.stats, 16) ||
+        (a.pre && (!good_matrix(a.dh, a.lddh, a.cols, e) || !good_matrix(a.y, a.ldy, a.cols, e))))
+        return EGERIA_ERR_INVALID_ARG;
+    if (ops->ws_bytes < egeria_norm_workspace_bytes(a.rows, a.cols)) return EGERIA_ERR_WORKSPACE;
+    const size_t row_align = 8 * e, vec_align = 8 * pe;
+    bool wide = a.cols % 8 == 0 && aligned(a.dy, row_align) && aligned(a.f, row_align) && aligned(a.dx, row_align) && aligned(a.df, row_align) &&
+                a.lddy % 8 == 0 && a.ldf % 8 == 0 && a.lddx % 8 == 0 && a.lddf % 8 == 0;
+    if (a.pre) wide = wide && aligned(a.dh, row_align) && aligned(a.y, row_align) && a.lddh % 8 == 0 && a.ldy % 8 == 0;
+    for (int i = 0; i < 5; ++i) wide = wide && aligned(vec[i], vec_align);
+    NormParams p;
+    memset(&p, 0, sizeof(p));
+    p.x = a.y, p.ldx = a.ldy;
+    p.f = a.f, p.ldf = a.ldf;
+    p.dy = a.dy, p.lddy = a.lddy;
+    p.dh = a.dh, p.lddh = a.lddh;
+    p.gate = a.gate;
+    if (a.post) p.w_post = a.w_post, p.b_post = a.b_post;
+    if (a.pre) p.w_pre = a.w_pre;
+    p.y = a.dx, p.ldy = a.lddx;
+    p.h = a.df, p.ldh = a.lddf;
+    p.stats = const_cast<float *>(a.stats);
+    p.sums = reinterpret_cast<float *>(ops->ws + kHeadBytes);
+    p.dw_post = a.dw_post, p.db_post = a.db_post, p.dw_pre = a.dw_pre, p.db_pre = a.db_pre, p.dgate = a.dgate;
+    p.rows = a.rows;
+    p.gate_rows = a.gate_rows ? a.gate_rows : a.rows;
+    p.cols = (int32_t)a.cols;
+    p.layer = a.kind == EGERIA_NORM_LAYER;
+    p.post = a.post != 0;
+    p.pre = a.pre != 0;
+    p.w_float = a.param_type == EGERIA_F32;
+    p.alpha = a.alpha;
+    p.inv_cols = 1.0f / (float)a.cols;
+    ops->last_stream = stream;
+    const NormPlan n = norm_backward_plan(a.rows, a.cols);
+    const bool sums = a.dgate || a.dw_post || a.db_post || a.dw_pre || a.db_pre;
+    EGO_CUDA(a.type == EGERIA_F32    ? norm_bwd_any<float>(p, n, wide, sums, stream)
+             : a.type == EGERIA_BF16 ? norm_bwd_any<bf16>(p, n, wide, sums, stream)
+                                     : norm_bwd_any<f16>(p, n, wide, sums, stream));
+    ops->launches += sums ? 2 : 1;
+    return EGERIA_OK;
+}
+
+// ---------------------------------------------------------------- AdamW
+size_t egeria_adamw_workspace_bytes(int count, const egeria_adamw_tensor *tensors, uint32_t flags) {
+    if (count < 1 || !tensors || (flags & ~EGERIA_ADAMW_8BIT)) return 0;
+    AdamLayout L;
+    return adam_layout(count, tensors, L) ? L.total : 0;
+}
+
+egeria_status egeria_adamw_create(egeria_adamw **out, int count, const egeria_adamw_tensor *tensors, const void *const *grads,
+                                  int32_t *steps, void *workspace, size_t workspace_bytes, uint32_t flags) {
+    if (!out) return EGERIA_ERR_INVALID_ARG;
+    *out = nullptr;
+    if (count < 1 || !tensors || !grads || !steps || !aligned(steps, 4) || (flags & ~EGERIA_ADAMW_8BIT)) return EGERIA_ERR_INVALID_ARG;
+    for (int i = 0; i < count; ++i)
+        if (!good_adam_tensor(tensors[i], flags) || (tensors[i].n > 0 && (!grads[i] || !aligned(grads[i], size_of(tensors[i].grad_type)))))
+            return EGERIA_ERR_INVALID_ARG;
+    AdamLayout L;
+    if (!adam_layout(count, tensors, L)) return EGERIA_ERR_UNSUPPORTED_SHAPE;
+    if (!workspace || !aligned(workspace, EGERIA_WORKSPACE_ALIGN) || workspace_bytes < L.total) return EGERIA_ERR_WORKSPACE;
+    int sms = 0;
+    egeria_status s = device_ready(&sms);
+    if (s != EGERIA_OK) return s;
+    egeria_adamw *h = nullptr;
+    try {
+        h = new egeria_adamw();
+        h->ws = static_cast<uint8_t *>(workspace);
+        h->L = L;
+        h->count = count;
+        const bool small = (flags & EGERIA_ADAMW_8BIT) != 0;
+        std::vector<uint8_t> image(L.total, 0);
+        AdamTensor *tab = reinterpret_cast<AdamTensor *>(image.data() + L.tensors);
+        int2 *chunks = reinterpret_cast<int2 *>(image.data() + L.chunks);
+        memcpy(image.data() + L.grads, grads, (size_t)count * sizeof(void *));
+        int64_t n_tab = 0, n_chunks = 0;
+        for (int k = 0; k < kAdamClasses; ++k) {
+            const int64_t tab0 = n_tab, chunk0 = n_chunks;
+            const egeria_adamw_tensor *any = nullptr;
+            for (int i = 0; i < count; ++i) {
+                const egeria_adamw_tensor &t = tensors[i];
+                if (adam_class(t) != k) continue;
+                any = &t;
+                AdamTensor &a = tab[n_tab];
+                a.p = t.param, a.master = t.master, a.m = t.m, a.v = t.v, a.m_scale = t.m_scale, a.v_scale = t.v_scale;
+                a.n = t.n, a.wd = t.weight_decay, a.module = t.module, a.index = i;
+                const size_t moment = small ? 8 : 32;
+                a.vector = aligned(t.param, 8 * size_of(t.param_type)) && aligned(t.master, 32) && aligned(t.m, moment) && aligned(t.v, moment);
+                for (int64_t c = 0; c * kAdamChunk < t.n; ++c) chunks[n_chunks++] = make_int2((int)(n_tab - tab0), (int)c);
+                ++n_tab;
+            }
+            if (!any) continue;
+            egeria_adamw::Class c{};
+            c.kernel = small ? adam_kernel<true>(any->param_type, any->grad_type, any->master != nullptr)
+                             : adam_kernel<false>(any->param_type, any->grad_type, any->master != nullptr);
+            int per_sm = 0;
+            if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, c.kernel, kAdamThreads, 0) != cudaSuccess || per_sm < 1) {
+                (void)cudaGetLastError();
+                delete h;
+                return EGERIA_ERR_CUDA;
+            }
+            c.params.tensors = reinterpret_cast<const AdamTensor *>(h->ws + L.tensors) + tab0;
+            c.params.chunks = reinterpret_cast<const int2 *>(h->ws + L.chunks) + chunk0;
+            c.params.grads = reinterpret_cast<const void *const *>(h->ws + L.grads);
+            c.params.steps = steps;
+            c.params.status = reinterpret_cast<int32_t *>(h->ws);
+            c.params.ticket = reinterpret_cast<int32_t *>(h->ws + 128 * (1 + k));
+            c.params.n_chunks = (int32_t)(n_chunks - chunk0);
+            c.params.n_tensors = (int32_t)(n_tab - tab0);
+            c.params.n_grads = count;
+            c.grid = (int)std::max<int64_t>(1, std::min<int64_t>(n_chunks - chunk0, (int64_t)per_sm * sms));
+            h->classes.push_back(c);
+        }
+        for (int i = 0; i < count; ++i) h->grad_size.push_back(tensors[i].n ? size_of(tensors[i].grad_type) : 0);
+        if (cudaMemcpy(h->ws, image.data(), L.total, cudaMemcpyHostToDevice) != cudaSuccess || cudaDeviceSynchronize() != cudaSuccess) {
+            (void)cudaGetLastError();
+            delete h;
+            return EGERIA_ERR_CUDA;
+        }
+    } catch (...) {  // out of host memory
+        delete h;
+        return EGERIA_ERR_INVALID_ARG;
+    }
+    *out = h;
+    return EGERIA_OK;
+}
+egeria_status egeria_adamw_destroy(egeria_adamw *adamw) {
+    if (!adamw) return EGERIA_ERR_INVALID_ARG;
+    delete adamw;
+    return EGERIA_OK;
+}
+
+egeria_status egeria_adamw_set_grads(egeria_adamw *adamw, void *cuda_stream, const void *const *grads) {
+    if (!adamw || !grads) return EGERIA_ERR_INVALID_ARG;
+    for (int i = 0; i < adamw->count; ++i)
+        if (adamw->grad_size[i] && (!grads[i] || !aligned(grads[i], adamw->grad_size[i]))) return EGERIA_ERR_INVALID_ARG;
+    cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+    cudaStreamCaptureStatus capturing = cudaStreamCaptureStatusNone;
+    EGO_CUDA(cudaStreamIsCapturing(stream, &capturing));
+    if (capturing != cudaStreamCaptureStatusNone) return EGERIA_ERR_INVALID_ARG;
+    // ordinary (pageable) memory: the runtime stages the copy before it returns
+    EGO_CUDA(cudaMemcpyAsync(adamw->ws + adamw->L.grads, grads, (size_t)adamw->count * sizeof(void *), cudaMemcpyHostToDevice, stream));
+    adamw->last_stream = stream;
+    return EGERIA_OK;
+}
+
+egeria_status egeria_adamw_step(egeria_adamw *adamw, void *cuda_stream, double lr, double beta1, double beta2, double eps,
+                                const float *grad_scale, const uint8_t *frozen) {
+    if (!adamw || !(lr >= 0.0) || !std::isfinite(lr) || !(beta1 >= 0.0 && beta1 < 1.0) || !(beta2 >= 0.0 && beta2 < 1.0) || !(eps >= 0.0) ||
+        !std::isfinite(eps) || !aligned(grad_scale, 4))
+        return EGERIA_ERR_INVALID_ARG;
+    cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+    adamw->last_stream = stream;
+    for (const egeria_adamw::Class &c : adamw->classes) {
+        AdamParams p = c.params;
+        p.frozen = frozen;
+        p.grad_scale = grad_scale;
+        p.lr = (float)lr;
+        p.beta1 = (float)beta1, p.beta2 = (float)beta2;
+        p.rest1 = (float)(1.0 - beta1), p.rest2 = (float)(1.0 - beta2);
+        p.eps = (float)eps;
+        p.ln_beta1 = std::log(beta1), p.ln_beta2 = std::log(beta2);
+        c.kernel<<<c.grid, kAdamThreads, 0, stream>>>(p);
+        EGO_CUDA(cudaGetLastError());
+        ++adamw->launches;
+    }
+    return EGERIA_OK;
+}
+
+egeria_status egeria_adamw_device_status(egeria_adamw *adamw) {
+    if (!adamw) return EGERIA_ERR_INVALID_ARG;
+    EGO_CUDA(cudaStreamSynchronize(adamw->last_stream));
+    int32_t v = 0;
+    EGO_CUDA(cudaMemcpy(&v, adamw->ws, sizeof(v), cudaMemcpyDeviceToHost));
+    if (v == 0) return EGERIA_OK;
+    EGO_CUDA(cudaMemset(adamw->ws, 0, 128));
+    return static_cast<egeria_status>(v);
+}
+int64_t egeria_adamw_launch_count(const egeria_adamw *adamw) { return adamw ? adamw->launches : 0; }
+
+}  // extern "C"

@@ -58,41 +58,174 @@ struct AdamStep {   // what a tensor's values need beside themselves
     float decay, rate, root, eps, beta1, rest1, beta2, rest2, gscale;
 };
 
-__device__ __forceinline__ void adam_value(const AdamStep &s, float g, float &p, float &m, float &root_v, float &v) {
-    g *= s.gscale;
-    m = fmaf(s.beta1, m, s.rest1 * g);
-    v = fmaf(s.beta2, v, s.rest2 * g * g);
-    root_v = fast_sqrt(v);
-    p = fmaf(p, s.decay, -s.rate * m * fast_rcp(fmaf(root_v, s.root, s.eps)));
+__device__ __forceinline__ float adam_param(const AdamStep &s, float p, float m, float v) {
+    return fmaf(p, s.decay, -s.rate * m * fast_rcp(fmaf(fast_sqrt(v), s.root, s.eps)));
 }
 
-__device__ __forceinline__ float decode_root(float c, float unit) {  // unit = scale / MOST^2
-    return c * fabsf(c) * unit;
+// The code of a size a in a block whose largest is top: MOST * sqrt(a / top) to the nearest whole number, every
+// operation rounded in 32 bits.  The approximate units give that number except within 1.2e-6 MOST of
+// a tie, where (once in some thousand values) the correctly rounded operations decide: codes come out the
+// same wherever the formula is computed operation by operation, so a state can be reproduced bit by bit.
+// ROOT: `a` is the square of the size.  `plain`: top is so small that the approximate units would
+// take what still has a code for zero.
+template <int MOST, bool ROOT>
+__device__ __forceinline__ int encode_size(float a, float top, float inv, bool plain) {
+    const float x = (float)MOST * fast_sqrt((ROOT ? fast_sqrt(a) : a) * inv);
+    const float c = rintf(x);
+    int code = (int)c;
+    if (plain || fabsf(fabsf(x - c) - 0.5f) < 1.2e-6f * MOST)
+        code = __float2int_rn((float)MOST * __fsqrt_rn(__fdiv_rn(ROOT ? __fsqrt_rn(a) : a, top)));
+    return code;
 }
 
-// The codes of a block: inv = MOST^2 / scale (0 for a block of zeros, or one that is not finite), so that
-// the code of a size a is sqrt(a * inv) = MOST sqrt(a / scale), rounded to the nearest whole number.
-// A scale below 2e-34, where inv would overflow, counts as 2e-34: no such moment moves anything.
-// A NaN or an infinity in a block leaves the code 0 and a scale that is not finite, which the next
-// step decodes as NaN for the whole block.
-template <int MOST>
-__device__ __forceinline__ float encode_factor(float top) {
-    return top > 0.0f ? fminf((float)(MOST * MOST) * fast_rcp(top), 3.0e38f) : 0.0f;
-}
-template <int MOST>
-__device__ __forceinline__ int encode_root(float a, float inv) {
-    return min(__float2int_rn(fast_sqrt(a * inv)), MOST);
+// Eight values of a block with moments in codes: `cm`, `cv` are replaced by the new codes, `sm`, `sv` by the
+// block's new scales.  The moments are computed by separately rounded products and sums (see encode_size).
+__device__ __forceinline__ void adam_codes(const AdamStep &s, const float (&g)[8], float (&p)[8], int (&cm)[8], int (&cv)[8], float &sm,
+                                           float &sv) {
+    const float um = __fdiv_rn(sm, 127.0f * 127.0f), uv = __fdiv_rn(sv, 255.0f * 255.0f);
+    float m[8], v[8], top_m = 0.0f, top_v = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const float gi = __fmul_rn(g[i], s.gscale);
+        const float root = __fmul_rn((float)(cv[i] * cv[i]), uv);
+        m[i] = __fadd_rn(__fmul_rn(s.beta1, __fmul_rn((float)(cm[i] * abs(cm[i])), um)), __fmul_rn(s.rest1, gi));
+        v[i] = __fadd_rn(__fmul_rn(s.beta2, __fmul_rn(root, root)), __fmul_rn(__fmul_rn(s.rest2, gi), gi));
+        p[i] = adam_param(s, p[i], m[i], v[i]);
+        top_m = max_nan(top_m, fabsf(m[i]));
+        top_v = max_nan(top_v, v[i]);
+    }
+    sm = warp_max_nan(top_m);
+    sv = __fsqrt_rn(warp_max_nan(top_v));
+    // a block of zeros, or with a value that is not finite (whose scale the next step decodes to NaN), has codes 0
+    const bool has_m = sm > 0.0f && sm <= 3.402823466e38f, has_v = sv > 0.0f && sv <= 3.402823466e38f;
+    const float im = fast_rcp(sm), iv = fast_rcp(sv);
+    const bool plain_m = sm < 1e-32f, plain_v = sv < 4e-14f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int a = has_m ? encode_size<127, false>(fabsf(m[i]), sm, im, plain_m) : 0;
+        cm[i] = m[i] < 0.0f ? -a : a;
+        cv[i] = has_v ? encode_size<255, true>(v[i], sv, iv, plain_v) : 0;
+        if (has_v && v[i] > 0.0f) cv[i] = max(cv[i], 1);
+    }
 }
 
+// A block of 256 values in flight: what its lane has loaded of it.
 template <typename P, typename G>
 struct AdamBlock {
     Raw8<P> p;
     Raw8<G> g;
-    Raw8<float> w;
-    Raw8<float> m, v;
+    Raw8<float> w, m, v;
     uint2 cm, cv;
     float sm, sv;
 };
+template <typename P, typename G, bool MASTER, bool SMALL>
+__device__ __forceinline__ void adam_load(AdamBlock<P, G> &b, const AdamTensor &t, const G *grad, int64_t at) {
+    load8(b.g, grad + at);
+    if (MASTER)
+        load8(b.w, t.master + at);
+    else
+        load8(b.p, static_cast<const P *>(t.p) + at);
+    if (SMALL) {
+        b.cm = *reinterpret_cast<const uint2 *>(static_cast<const uint8_t *>(t.m) + at);
+        b.cv = *reinterpret_cast<const uint2 *>(static_cast<const uint8_t *>(t.v) + at);
+        b.sm = t.m_scale[at / kAdamBlock];
+        b.sv = t.v_scale[at / kAdamBlock];
+    } else {
+        load8(b.m, static_cast<const float *>(t.m) + at);
+        load8(b.v, static_cast<const float *>(t.v) + at);
+    }
+}
+template <typename P, typename G, bool MASTER, bool SMALL>
+__device__ __forceinline__ void adam_finish(AdamBlock<P, G> &b, const AdamStep &s, const AdamTensor &t, int64_t at, int lane) {
+    float p[8], g[8];
+    unpack8(g, b.g);
+    if (MASTER)
+        unpack8(p, b.w);
+    else
+        unpack8(p, b.p);
+    if (SMALL) {
+        int cm[8], cv[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            cm[i] = (int)(int8_t)((i < 4 ? b.cm.x : b.cm.y) >> (8 * (i & 3)));
+            cv[i] = (int)(((i < 4 ? b.cv.x : b.cv.y) >> (8 * (i & 3))) & 0xffu);
+        }
+        adam_codes(s, g, p, cm, cv, b.sm, b.sv);
+        uint32_t om[2] = {0u, 0u}, ov[2] = {0u, 0u};
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            om[i >> 2] |= (uint32_t)(cm[i] & 0xff) << (8 * (i & 3));
+            ov[i >> 2] |= (uint32_t)cv[i] << (8 * (i & 3));
+        }
+        *reinterpret_cast<uint2 *>(static_cast<uint8_t *>(t.m) + at) = make_uint2(om[0], om[1]);
+        *reinterpret_cast<uint2 *>(static_cast<uint8_t *>(t.v) + at) = make_uint2(ov[0], ov[1]);
+        if (lane == 0) {
+            t.m_scale[at / kAdamBlock] = b.sm;
+            t.v_scale[at / kAdamBlock] = b.sv;
+        }
+    } else {
+        float m[8], v[8];
+        unpack8(m, b.m);
+        unpack8(v, b.v);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float gi = g[i] * s.gscale;
+            m[i] = fmaf(s.beta1, m[i], s.rest1 * gi);
+            v[i] = fmaf(s.beta2, v[i], s.rest2 * gi * gi);
+            p[i] = adam_param(s, p[i], m[i], v[i]);
+        }
+        store8(static_cast<float *>(t.m) + at, m);
+        store8(static_cast<float *>(t.v) + at, v);
+    }
+    if (MASTER) store8(t.master + at, p);
+    store8(static_cast<P *>(t.p) + at, p);
+}
+// The end of a tensor, or a block of one whose pointers take no wide access: value by value, lane-consecutive.
+template <typename P, typename G, bool MASTER, bool SMALL>
+__device__ __forceinline__ void adam_narrow(const AdamStep &s, const AdamTensor &t, const G *grad, int64_t at0, int lane) {
+    float p[8], g[8], m[8], v[8];
+    int cm[8], cv[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int64_t at = at0 + lane + 32 * i;
+        const bool in = at < t.n;  // zeros stand for what is not there: they stay zeros
+        g[i] = in ? to_f32(grad[at]) : 0.0f;
+        p[i] = !in ? 0.0f : MASTER ? t.master[at] : to_f32(static_cast<const P *>(t.p)[at]);
+        if (SMALL) {
+            cm[i] = in ? (int)static_cast<const int8_t *>(t.m)[at] : 0;
+            cv[i] = in ? (int)static_cast<const uint8_t *>(t.v)[at] : 0;
+        } else {
+            m[i] = in ? static_cast<const float *>(t.m)[at] : 0.0f;
+            v[i] = in ? static_cast<const float *>(t.v)[at] : 0.0f;
+        }
+    }
+    if (SMALL) {
+        float sm = t.m_scale[at0 / kAdamBlock], sv = t.v_scale[at0 / kAdamBlock];
+        adam_codes(s, g, p, cm, cv, sm, sv);
+        if (lane == 0) {
+            t.m_scale[at0 / kAdamBlock] = sm;
+            t.v_scale[at0 / kAdamBlock] = sv;
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int64_t at = at0 + lane + 32 * i;
+        if (at >= t.n) continue;
+        if (SMALL) {
+            static_cast<int8_t *>(t.m)[at] = (int8_t)cm[i];
+            static_cast<uint8_t *>(t.v)[at] = (uint8_t)cv[i];
+        } else {
+            const float gi = g[i] * s.gscale;
+            m[i] = fmaf(s.beta1, m[i], s.rest1 * gi);
+            v[i] = fmaf(s.beta2, v[i], s.rest2 * gi * gi);
+            p[i] = adam_param(s, p[i], m[i], v[i]);
+            static_cast<float *>(t.m)[at] = m[i];
+            static_cast<float *>(t.v)[at] = v[i];
+        }
+        if (MASTER) t.master[at] = p[i];
+        static_cast<P *>(t.p)[at] = from_f32<P>(p[i]);
+    }
+}
 
 template <typename P, typename G, bool MASTER, bool SMALL>
 __global__ void __launch_bounds__(kAdamThreads) adamw_kernel(const AdamParams a) {
@@ -124,137 +257,27 @@ __global__ void __launch_bounds__(kAdamThreads) adamw_kernel(const AdamParams a)
             s = AdamStep{1.0f - a.lr * t.wd, a.lr / fix1, rsqrtf(fix2), a.eps, a.beta1, a.rest1, a.beta2, a.rest2, gscale};
         }
         if (!live) continue;
-        const int64_t base = (int64_t)chunk.y * kAdamChunk;
-        if (vector && base + kAdamChunk <= t.n) {
+        const int64_t base = (int64_t)chunk.y * kAdamChunk + warp * kAdamBlock;
+        if (vector && base + (kAdamUnroll - 1) * kAdamWarps * kAdamBlock + kAdamBlock <= t.n) {
             AdamBlock<P, G> b[kAdamUnroll];
 #pragma unroll
-            for (int u = 0; u < kAdamUnroll; ++u) {
-                const int64_t at = base + (int64_t)(u * kAdamWarps + warp) * kAdamBlock + lane * 8;
-                load8(b[u].g, grad + at);
-                if (MASTER)
-                    load8(b[u].w, t.master + at);
-                else
-                    load8(b[u].p, static_cast<const P *>(t.p) + at);
-                if (SMALL) {
-                    b[u].cm = *reinterpret_cast<const uint2 *>(static_cast<const uint8_t *>(t.m) + at);
-                    b[u].cv = *reinterpret_cast<const uint2 *>(static_cast<const uint8_t *>(t.v) + at);
-                    b[u].sm = t.m_scale[at / kAdamBlock];
-                    b[u].sv = t.v_scale[at / kAdamBlock];
-                } else {
-                    load8(b[u].m, static_cast<const float *>(t.m) + at);
-                    load8(b[u].v, static_cast<const float *>(t.v) + at);
-                }
-            }
+            for (int u = 0; u < kAdamUnroll; ++u)
+                adam_load<P, G, MASTER, SMALL>(b[u], t, grad, base + u * kAdamWarps * kAdamBlock + lane * 8);
 #pragma unroll
-            for (int u = 0; u < kAdamUnroll; ++u) {
-                const int64_t at = base + (int64_t)(u * kAdamWarps + warp) * kAdamBlock + lane * 8;
-                float p[8], g[8], m[8], v[8];
-                unpack8(g, b[u].g);
-                if (MASTER)
-                    unpack8(p, b[u].w);
-                else
-                    unpack8(p, b[u].p);
-                if (SMALL) {
-                    const float um = b[u].sm * (1.0f / (127.0f * 127.0f)), uv = b[u].sv * (1.0f / (255.0f * 255.0f));
-                    float root[8], top_m = 0.0f, top_v = 0.0f;
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const uint32_t wm = i < 4 ? b[u].cm.x : b[u].cm.y, wv = i < 4 ? b[u].cv.x : b[u].cv.y;
-                        const float cm = (float)(int8_t)(wm >> (8 * (i & 3))), cv = (float)((wv >> (8 * (i & 3))) & 0xffu);
-                        m[i] = decode_root(cm, um);
-                        const float r0 = decode_root(cv, uv);
-                        v[i] = r0 * r0;
-                        adam_value(s, g[i], p[i], m[i], root[i], v[i]);
-                        top_m = max_nan(top_m, fabsf(m[i]));
-                        top_v = max_nan(top_v, root[i]);
-                    }
-                    top_m = warp_max_nan(top_m);
-                    top_v = warp_max_nan(top_v);
-                    const float im = encode_factor<127>(top_m);
-                    const float iv = encode_factor<255>(top_v);
-                    uint32_t om[2] = {0u, 0u}, ov[2] = {0u, 0u};
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const int cm = encode_root<127>(fabsf(m[i]), im);
-                        int cv = encode_root<255>(root[i], iv);
-                        if (v[i] > 0.0f) cv = max(cv, 1);
-                        om[i >> 2] |= (uint32_t)((m[i] < 0.0f ? -cm : cm) & 0xff) << (8 * (i & 3));
-                        ov[i >> 2] |= (uint32_t)cv << (8 * (i & 3));
-                    }
-                    *reinterpret_cast<uint2 *>(static_cast<uint8_t *>(t.m) + at) = make_uint2(om[0], om[1]);
-                    *reinterpret_cast<uint2 *>(static_cast<uint8_t *>(t.v) + at) = make_uint2(ov[0], ov[1]);
-                    if (lane == 0) {
-                        t.m_scale[at / kAdamBlock] = top_m;
-                        t.v_scale[at / kAdamBlock] = top_v;
-                    }
-                } else {
-                    unpack8(m, b[u].m);
-                    unpack8(v, b[u].v);
-                    float root;
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) adam_value(s, g[i], p[i], m[i], root, v[i]);
-                    store8(static_cast<float *>(t.m) + at, m);
-                    store8(static_cast<float *>(t.v) + at, v);
-                }
-                if (MASTER) store8(t.master + at, p);
-                store8(static_cast<P *>(t.p) + at, p);
-            }
-        } else {
-            // the end of a tensor, or one whose pointers take no wide access: value by value, lane-consecutive
-            for (int u = 0; u < kAdamUnroll; ++u) {
-                const int64_t at0 = base + (int64_t)(u * kAdamWarps + warp) * kAdamBlock;
-                if (at0 >= t.n) break;
-                float p[8], m[8], v[8], root[8], top_m = 0.0f, top_v = 0.0f;
-                const float um = SMALL ? t.m_scale[at0 / kAdamBlock] * (1.0f / (127.0f * 127.0f)) : 0.0f;
-                const float uv = SMALL ? t.v_scale[at0 / kAdamBlock] * (1.0f / (255.0f * 255.0f)) : 0.0f;
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const int64_t at = at0 + lane + 32 * i;
-                    const bool in = at < t.n;
-                    const float g = in ? to_f32(grad[at]) : 0.0f;
-                    p[i] = !in ? 0.0f : MASTER ? t.master[at] : to_f32(static_cast<const P *>(t.p)[at]);
-                    if (SMALL) {
-                        m[i] = in ? decode_root((float)static_cast<const int8_t *>(t.m)[at], um) : 0.0f;
-                        const float r0 = in ? decode_root((float)static_cast<const uint8_t *>(t.v)[at], uv) : 0.0f;
-                        v[i] = r0 * r0;
-                    } else {
-                        m[i] = in ? static_cast<const float *>(t.m)[at] : 0.0f;
-                        v[i] = in ? static_cast<const float *>(t.v)[at] : 0.0f;
-                    }
-                    adam_value(s, g, p[i], m[i], root[i], v[i]);
-                    if (in) {
-                        top_m = max_nan(top_m, fabsf(m[i]));
-                        top_v = max_nan(top_v, root[i]);
-                    }
-                }
-                float im = 0.0f, iv = 0.0f;
-                if (SMALL) {
-                    top_m = warp_max_nan(top_m);
-                    top_v = warp_max_nan(top_v);
-                    im = encode_factor<127>(top_m);
-                    iv = encode_factor<255>(top_v);
-                }
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const int64_t at = at0 + lane + 32 * i;
-                    if (at >= t.n) continue;
-                    if (SMALL) {
-                        const int cm = encode_root<127>(fabsf(m[i]), im);
-                        int cv = encode_root<255>(root[i], iv);
-                        if (v[i] > 0.0f) cv = max(cv, 1);
-                        static_cast<int8_t *>(t.m)[at] = (int8_t)(m[i] < 0.0f ? -cm : cm);
-                        static_cast<uint8_t *>(t.v)[at] = (uint8_t)cv;
-                    } else {
-                        static_cast<float *>(t.m)[at] = m[i];
-                        static_cast<float *>(t.v)[at] = v[i];
-                    }
-                    if (MASTER) t.master[at] = p[i];
-                    static_cast<P *>(t.p)[at] = from_f32<P>(p[i]);
-                }
-                if (SMALL && lane == 0) {
-                    t.m_scale[at0 / kAdamBlock] = top_m;
-                    t.v_scale[at0 / kAdamBlock] = top_v;
-                }
+            for (int u = 0; u < kAdamUnroll; ++u)
+                adam_finish<P, G, MASTER, SMALL>(b[u], s, t, base + u * kAdamWarps * kAdamBlock + lane * 8, lane);
+            continue;
+        }
+#pragma unroll 1
+        for (int u = 0; u < kAdamUnroll; ++u) {
+            const int64_t at0 = base + u * kAdamWarps * kAdamBlock;
+            if (at0 >= t.n) break;
+            if (vector && at0 + kAdamBlock <= t.n) {
+                AdamBlock<P, G> b;
+                adam_load<P, G, MASTER, SMALL>(b, t, grad, at0 + lane * 8);
+                adam_finish<P, G, MASTER, SMALL>(b, s, t, at0 + lane * 8, lane);
+            } else {
+                adam_narrow<P, G, MASTER, SMALL>(s, t, grad, at0, lane);
             }
         }
     }

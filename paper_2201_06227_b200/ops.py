@@ -12,6 +12,7 @@ are recorded on it (their memory is not reused before the call has run).
 from __future__ import annotations
 
 import ctypes
+import struct
 from typing import Optional, Sequence
 
 import torch
@@ -37,26 +38,38 @@ EXPORTS = [
 ]
 
 _vp, _i32, _i64, _f32 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_float
+_CODES = {_i32: "i", _i64: "q", _vp: "Q", _f32: "f"}
 
 
-def _struct(name, *groups):
-    """A ctypes mirror of a C struct: (type, "field field ...") groups in order."""
-    return type(name, (ctypes.Structure,), {"_fields_": [(f, t) for t, names in groups for f in names.split()]})
+def _fields(*groups):
+    """(field, type) pairs of a C struct from (type, "field field ...") groups in order."""
+    return [(f, t) for t, names in groups for f in names.split()]
 
 
-_LinearForward = _struct("egeria_linear_forward_args", (_i32, "type act"), (_i64, "rows inp out"), (_vp, "x w bias residual"),
-                         (_i64, "ldx ldw ldr"), (_vp, "y z"), (_i64, "ldy ldz"))
-_LinearBackward = _struct("egeria_linear_backward_args", (_i32, "type act act_in"), (_i64, "rows inp out"),
-                          (_vp, "dy x w z z_in"), (_i64, "lddy ldx ldw ldz ldz_in"), (_vp, "dx dw db"), (_i64, "lddx lddw"))
-_NormForward = _struct("egeria_norm_forward_args", (_i32, "type param_type kind post pre"), (_f32, "alpha eps"),
-                       (_i64, "rows cols gate_rows"), (_vp, "x f gate w_post b_post w_pre b_pre"), (_i64, "ldx ldf"),
-                       (_vp, "y h"), (_i64, "ldy ldh"), (_vp, "stats"))
-_NormBackward = _struct("egeria_norm_backward_args", (_i32, "type param_type kind post pre"), (_f32, "alpha"),
-                        (_i64, "rows cols gate_rows"), (_vp, "dy dh y f gate w_post b_post w_pre b_pre"),
-                        (_i64, "lddy lddh ldy ldf"), (_vp, "stats dx df"), (_i64, "lddx lddf"),
-                        (_vp, "dgate dw_post db_post dw_pre db_pre"))
-_AdamTensor = _struct("egeria_adamw_tensor", (_vp, "param master m v m_scale v_scale"), (_i64, "n"),
-                      (_i32, "param_type grad_type"), (_f32, "weight_decay"), (_i32, "module"))
+_LINEAR_FORWARD = _fields((_i32, "type act"), (_i64, "rows inp out"), (_vp, "x w bias residual"), (_i64, "ldx ldw ldr"),
+                          (_vp, "y z"), (_i64, "ldy ldz"))
+_LINEAR_BACKWARD = _fields((_i32, "type act act_in"), (_i64, "rows inp out"), (_vp, "dy x w z z_in"),
+                           (_i64, "lddy ldx ldw ldz ldz_in"), (_vp, "dx dw db"), (_i64, "lddx lddw"))
+_NORM_FORWARD = _fields((_i32, "type param_type kind post pre"), (_f32, "alpha eps"), (_i64, "rows cols gate_rows"),
+                        (_vp, "x f gate w_post b_post w_pre b_pre"), (_i64, "ldx ldf"), (_vp, "y h"), (_i64, "ldy ldh"), (_vp, "stats"))
+_NORM_BACKWARD = _fields((_i32, "type param_type kind post pre"), (_f32, "alpha"), (_i64, "rows cols gate_rows"),
+                         (_vp, "dy dh y f gate w_post b_post w_pre b_pre"), (_i64, "lddy lddh ldy ldf"), (_vp, "stats dx df"),
+                         (_i64, "lddx lddf"), (_vp, "dgate dw_post db_post dw_pre db_pre"))
+
+
+class _AdamTensor(ctypes.Structure):
+    _fields_ = _fields((_vp, "param master m v m_scale v_scale"), (_i64, "n"), (_i32, "param_type grad_type"), (_f32, "weight_decay"),
+                       (_i32, "module"))
+
+
+def _packer(fields):
+    """Packs the values of a struct's fields, in order, as a C compiler lays them out (a call through it costs a
+    fraction of filling in a ctypes structure)."""
+    return struct.Struct("@" + "".join(_CODES[t] for _, t in fields)).pack
+
+
+_pack_linear_forward, _pack_linear_backward = _packer(_LINEAR_FORWARD), _packer(_LINEAR_BACKWARD)
+_pack_norm_forward, _pack_norm_backward = _packer(_NORM_FORWARD), _packer(_NORM_BACKWARD)
 
 _ready = None
 
@@ -77,10 +90,10 @@ def lib() -> ctypes.CDLL:
                  "egeria_adamw_device_status", "egeria_adamw_launch_count"):
         getattr(L, name).argtypes = [_vp]
     L.egeria_ops_launch_count.restype = L.egeria_adamw_launch_count.restype = _i64
-    L.egeria_linear_forward.argtypes = [_vp, _vp, ctypes.POINTER(_LinearForward)]
-    L.egeria_linear_backward.argtypes = [_vp, _vp, ctypes.POINTER(_LinearBackward)]
-    L.egeria_norm_forward.argtypes = [_vp, _vp, ctypes.POINTER(_NormForward)]
-    L.egeria_norm_backward.argtypes = [_vp, _vp, ctypes.POINTER(_NormBackward)]
+    L.egeria_linear_forward.argtypes = [_vp, _vp, ctypes.c_char_p]
+    L.egeria_linear_backward.argtypes = [_vp, _vp, ctypes.c_char_p]
+    L.egeria_norm_forward.argtypes = [_vp, _vp, ctypes.c_char_p]
+    L.egeria_norm_backward.argtypes = [_vp, _vp, ctypes.c_char_p]
     L.egeria_adamw_set_grads.argtypes = [_vp, _vp, ctypes.POINTER(_vp)]
     L.egeria_adamw_step.argtypes = [_vp, _vp] + [ctypes.c_double] * 4 + [_vp, _vp]
     _ready = L
@@ -102,14 +115,14 @@ def _workspace(nbytes: int, device):
 
 
 class _On:
-    """The stream of a call: allocations inside come from it, foreign inputs are recorded on it."""
+    """The stream of a call that is not on the device's current stream: allocations inside come from it, and the
+    tensors that the call touches are recorded on it."""
 
     def __init__(self, device: torch.device, stream: Optional[torch.cuda.Stream], tensors):
-        self.current = torch.cuda.current_stream(device)
-        self.stream = self.current if stream is None else stream
+        self.stream = torch.cuda.current_stream(device) if stream is None else stream
         if self.stream.device != device:
             raise ValueError(f"the stream is of {self.stream.device}, the handle of {device}")
-        self.tensors = tensors
+        self.tensors = () if stream is None else tensors
         self.context = torch.cuda.stream(self.stream)
 
     def __enter__(self):
@@ -117,53 +130,71 @@ class _On:
         return int(self.stream.cuda_stream)
 
     def __exit__(self, *exc):
-        if self.stream != self.current:
-            for t in self.tensors:
-                if t is not None:
-                    t.record_stream(self.stream)
+        for t in self.tensors:
+            if t is not None:
+                t.record_stream(self.stream)
         return self.context.__exit__(*exc)
 
 
-def _matrix(t: torch.Tensor, name: str, device, dtype, rows: int, cols: int):
+class _Here:
+    """The current stream of the current device, the ordinary case: nothing to enter or to leave."""
+
+    def __init__(self, index: int):
+        self.index = index
+
+    def __enter__(self):
+        return torch._C._cuda_getCurrentRawStream(self.index)
+
+    def __exit__(self, *exc):
+        return False
+
+
+def _matrix(t: torch.Tensor, name: str, device: int, dtype, rows: int, cols: int):
     """(pointer, pitch) of a matrix whose rows are consecutive."""
-    if t.device != device or t.dtype != dtype or t.dim() != 2 or tuple(t.shape) != (rows, cols):
-        raise ValueError(f"{name}: expected {dtype} [{rows}, {cols}] on {device}, got {t.dtype} {list(t.shape)} on {t.device}")
-    if cols > 1 and t.stride(1) != 1:
+    if t.dtype is not dtype or t.get_device() != device or t.shape != (rows, cols):
+        raise ValueError(f"{name}: expected {dtype} [{rows}, {cols}] on cuda:{device}, got {t.dtype} {list(t.shape)} on {t.device}")
+    pitch, step = t.stride()
+    if step != 1 and cols > 1:
         raise ValueError(f"{name}: the values of a row have to be consecutive")
-    if rows > 1 and t.stride(0) < cols:
+    if rows <= 1:
+        pitch = cols
+    elif pitch < cols:
         raise ValueError(f"{name}: rows overlap")
-    return t.data_ptr(), (t.stride(0) if rows > 1 else cols)
+    return t.data_ptr(), pitch
 
 
 def _optional(t: Optional[torch.Tensor], *args):
-    return (None, 0) if t is None else _matrix(t, *args)
+    return (0, 0) if t is None else _matrix(t, *args)
 
 
-def _vector(t: Optional[torch.Tensor], name: str, device, dtype, n: int):
+def _vector(t: Optional[torch.Tensor], name: str, device: int, dtype, n: int) -> int:
     if t is None:
-        return None
-    if t.device != device or t.dtype != dtype or t.numel() != n or not t.is_contiguous():
-        raise ValueError(f"{name}: expected {n} consecutive {dtype} on {device}")
+        return 0
+    if t.dtype is not dtype or t.get_device() != device or t.numel() != n or not t.is_contiguous():
+        raise ValueError(f"{name}: expected {n} consecutive {dtype} on cuda:{device}")
     return t.data_ptr()
 
 
-class Ops:
-    """Handle of the linear and norm calls; owns its workspace.  For one stream at a time."""
+class _Handle:
+    """A library object on one device, with its workspace."""
 
-    def __init__(self, workspace_bytes: int = OPS_WORKSPACE_MIN, device="cuda"):
+    def _on(self, stream, *tensors):
+        if stream is None and torch._C._cuda_getDevice() == self._index:
+            return self._here
+        return _On(self.device, stream, (self._raw, *tensors))
+
+    def _place(self, device) -> None:
         self.device = torch.device(device)
-        if self.device.type == "cuda" and self.device.index is None:
+        if self.device.type != "cuda":
+            raise ValueError("a CUDA device is required")
+        if self.device.index is None:
             self.device = torch.device("cuda", torch.cuda.current_device())
-        self.workspace_bytes = max(int(workspace_bytes), OPS_WORKSPACE_MIN)
-        self._raw, ptr = _workspace(self.workspace_bytes, self.device)
-        handle = _vp()
-        with torch.cuda.device(self.device):
-            _check(lib().egeria_ops_create(ctypes.byref(handle), ptr, self.workspace_bytes), "egeria_ops_create")
-        self._h = handle
+        self._index = self.device.index
+        self._here = _Here(self._index)
 
     def close(self) -> None:
         if getattr(self, "_h", None):
-            lib().egeria_ops_destroy(self._h)
+            self._destroy(self._h)
             self._h = None
 
     def __del__(self):
@@ -171,6 +202,20 @@ class Ops:
             self.close()
         except Exception:
             pass
+
+
+class Ops(_Handle):
+    """Handle of the linear and norm calls; owns its workspace.  For one stream at a time."""
+
+    def __init__(self, workspace_bytes: int = OPS_WORKSPACE_MIN, device="cuda"):
+        self._place(device)
+        self.workspace_bytes = max(int(workspace_bytes), OPS_WORKSPACE_MIN)
+        self._raw, ptr = _workspace(self.workspace_bytes, self.device)
+        handle = _vp()
+        L = lib()
+        with torch.cuda.device(self.device):
+            _check(L.egeria_ops_create(ctypes.byref(handle), ptr, self.workspace_bytes), "egeria_ops_create")
+        self._h, self._lib, self._destroy = handle, L, L.egeria_ops_destroy
 
     # ------------------------------------------------------------------ linear layers
     def egeria_linear_forward(self, x: torch.Tensor, w: torch.Tensor, bias: Optional[torch.Tensor] = None, act: str = "none",
@@ -183,18 +228,22 @@ class Ops:
         if x.dim() != 2 or w.dim() != 2:
             raise ValueError("x and w are matrices")
         (rows, inp), n = x.shape, w.shape[0]
-        a = _LinearForward(type=TYPES.get(x.dtype, -1), act=ACTS[act], rows=rows, inp=inp, out=n)
-        dev, t = self.device, x.dtype
-        a.x, a.ldx = _matrix(x, "x", dev, t, rows, inp)
-        a.w, a.ldw = _matrix(w, "w", dev, t, n, inp)
-        a.bias = _vector(bias, "bias", dev, t, n)
-        a.residual, a.ldr = _optional(residual, "residual", dev, t, rows, n)
-        with _On(dev, stream, (self._raw, x, w, bias, residual, out)) as s:
-            y = torch.empty((rows, n), dtype=t, device=dev) if out is None else out
-            z = torch.empty((rows, n), dtype=t, device=dev) if save_z else None
-            a.y, a.ldy = _matrix(y, "out", dev, t, rows, n)
-            a.z, a.ldz = _optional(z, "z", dev, t, rows, n)
-            _check(lib().egeria_linear_forward(self._h, s, ctypes.byref(a)), "egeria_linear_forward")
+        dev, t, z, pz = self._index, x.dtype, None, (0, 0)
+        px, pw = _matrix(x, "x", dev, t, rows, inp), _matrix(w, "w", dev, t, n, inp)
+        pb, pr = _vector(bias, "bias", dev, t, n), _optional(residual, "residual", dev, t, rows, n)
+        with self._on(stream, x, w, bias, residual, out) as s:
+            if out is None:
+                y = x.new_empty((rows, n))
+                py = (y.data_ptr(), n)
+            else:
+                y, py = out, _matrix(out, "out", dev, t, rows, n)
+            if save_z:
+                z = x.new_empty((rows, n))
+                pz = (z.data_ptr(), n)
+            st = self._lib.egeria_linear_forward(self._h, s, _pack_linear_forward(
+                TYPES.get(t, -1), ACTS[act], rows, inp, n, px[0], pw[0], pb, pr[0], px[1], pw[1], pr[1], py[0], pz[0], py[1], pz[1]))
+        if st:
+            _check(st, "egeria_linear_forward")
         return (y, z) if save_z else y
 
     def egeria_linear_backward(self, dy: torch.Tensor, x: Optional[torch.Tensor], w: Optional[torch.Tensor],
@@ -209,38 +258,38 @@ class Ops:
         if dy.dim() != 2 or (need_dx and w is None) or (need_dw and x is None) or (x is None and w is None):
             raise ValueError("dy is a matrix; dx needs w, dw needs x, and one of the two has to be there")
         rows, n = dy.shape
-        inp = x.shape[1] if x is not None else w.shape[1]
-        dev, t = self.device, dy.dtype
-        a = _LinearBackward(type=TYPES.get(t, -1), act=ACTS[act], act_in=ACTS[act_in], rows=rows, inp=inp, out=n)
-        a.dy, a.lddy = _matrix(dy, "dy", dev, t, rows, n)
-        a.x, a.ldx = _optional(x, "x", dev, t, rows, inp)
-        a.w, a.ldw = _optional(w, "w", dev, t, n, inp)
-        a.z, a.ldz = _optional(z, "z", dev, t, rows, n)
-        a.z_in, a.ldz_in = _optional(z_in, "z_in", dev, t, rows, inp)
-        with _On(dev, stream, (self._raw, dy, x, w, z, z_in)) as s:
-            dx = torch.empty((rows, inp), dtype=t, device=dev) if need_dx else None
-            dw = torch.empty((n, inp), dtype=t, device=dev) if need_dw else None
-            db = torch.empty(n, dtype=t, device=dev) if need_db else None
-            a.dx, a.lddx = _optional(dx, "dx", dev, t, rows, inp)
-            a.dw, a.lddw = _optional(dw, "dw", dev, t, n, inp)
-            a.db = _vector(db, "db", dev, t, n)
-            _check(lib().egeria_linear_backward(self._h, s, ctypes.byref(a)), "egeria_linear_backward")
+        inp = x.shape[-1] if x is not None else w.shape[-1]
+        dev, t, dx, dw, db = self._index, dy.dtype, None, None, None
+        pdy, px, pw = _matrix(dy, "dy", dev, t, rows, n), _optional(x, "x", dev, t, rows, inp), _optional(w, "w", dev, t, n, inp)
+        pz, pzi = _optional(z, "z", dev, t, rows, n), _optional(z_in, "z_in", dev, t, rows, inp)
+        with self._on(stream, dy, x, w, z, z_in) as s:
+            if need_dx:
+                dx = dy.new_empty((rows, inp))
+            if need_dw:
+                dw = dy.new_empty((n, inp))
+            if need_db:
+                db = dy.new_empty(n)
+            st = self._lib.egeria_linear_backward(self._h, s, _pack_linear_backward(
+                TYPES.get(t, -1), ACTS[act], ACTS[act_in], rows, inp, n, pdy[0], px[0], pw[0], pz[0], pzi[0], pdy[1], px[1], pw[1], pz[1],
+                pzi[1], dx.data_ptr() if need_dx else 0, dw.data_ptr() if need_dw else 0, db.data_ptr() if need_db else 0, inp, inp))
+        if st:
+            _check(st, "egeria_linear_backward")
         return dx, dw, db
 
     # ------------------------------------------------------------------ residual norms
-    def _norm_common(self, a, like, gate, gate_rows, w_post, b_post, w_pre, b_pre, kind, post, pre):
+    def _norm_params(self, dtype, rows, cols, gate, gate_rows, w_post, b_post, w_pre, b_pre, kind):
+        """(type code of the parameters, their five pointers), checked."""
         if kind not in KINDS:
             raise ValueError(f"unknown norm {kind!r}")
-        given = [v for v in (gate, w_post, b_post, w_pre, b_pre) if v is not None]
-        pt = given[0].dtype if given else like.dtype
-        rows, cols = like.shape
-        a.type, a.param_type, a.kind, a.post, a.pre = TYPES.get(like.dtype, -1), TYPES.get(pt, -1), KINDS[kind], int(post), int(pre)
-        a.rows, a.cols, a.gate_rows = rows, cols, int(gate_rows)
+        pt = dtype
+        for v in (gate, w_post, b_post, w_pre, b_pre):
+            if v is not None:
+                pt = v.dtype
+                break
+        dev = self._index
         groups = 1 if gate_rows == 0 else -(-rows // gate_rows) if gate_rows > 0 else 0
-        a.gate = _vector(gate, "gate", self.device, pt, groups * cols)
-        for name, v in (("w_post", w_post), ("b_post", b_post), ("w_pre", w_pre), ("b_pre", b_pre)):
-            setattr(a, name, _vector(v, name, self.device, pt, cols))
-        return pt
+        return (TYPES.get(pt, -1), _vector(gate, "gate", dev, pt, groups * cols), _vector(w_post, "w_post", dev, pt, cols),
+                _vector(b_post, "b_post", dev, pt, cols), _vector(w_pre, "w_pre", dev, pt, cols), _vector(b_pre, "b_pre", dev, pt, cols))
 
     def egeria_norm_forward(self, x: torch.Tensor, f: torch.Tensor, gate: Optional[torch.Tensor] = None, gate_rows: int = 0,
                             w_post: Optional[torch.Tensor] = None, b_post: Optional[torch.Tensor] = None,
@@ -250,19 +299,21 @@ class Ops:
         """(y, h, stats): y = alpha x + gate * N_post(f), h = N_pre(y) (None without pre), stats for the backward call."""
         if x.dim() != 2:
             raise ValueError("x is a matrix")
-        a, dev, t = _NormForward(alpha=alpha, eps=eps), self.device, x.dtype
         rows, cols = x.shape
-        self._norm_common(a, x, gate, gate_rows, w_post, b_post, w_pre, b_pre, kind, post, pre)
-        a.x, a.ldx = _matrix(x, "x", dev, t, rows, cols)
-        a.f, a.ldf = _matrix(f, "f", dev, t, rows, cols)
-        with _On(dev, stream, (self._raw, x, f, gate, w_post, b_post, w_pre, b_pre)) as s:
-            y = torch.empty((rows, cols), dtype=t, device=dev)
-            h = torch.empty((rows, cols), dtype=t, device=dev) if pre else None
-            stats = torch.empty((rows, 4), dtype=torch.float32, device=dev)
-            a.y, a.ldy = _matrix(y, "y", dev, t, rows, cols)
-            a.h, a.ldh = _optional(h, "h", dev, t, rows, cols)
-            a.stats = stats.data_ptr()
-            _check(lib().egeria_norm_forward(self._h, s, ctypes.byref(a)), "egeria_norm_forward")
+        dev, t, h, ph = self._index, x.dtype, None, 0
+        pt, *vectors = self._norm_params(t, rows, cols, gate, gate_rows, w_post, b_post, w_pre, b_pre, kind)
+        px, pf = _matrix(x, "x", dev, t, rows, cols), _matrix(f, "f", dev, t, rows, cols)
+        with self._on(stream, x, f, gate, w_post, b_post, w_pre, b_pre) as s:
+            y = x.new_empty((rows, cols))
+            if pre:
+                h = x.new_empty((rows, cols))
+                ph = h.data_ptr()
+            stats = x.new_empty((rows, 4), dtype=torch.float32)
+            st = self._lib.egeria_norm_forward(self._h, s, _pack_norm_forward(
+                TYPES.get(t, -1), pt, KINDS[kind], bool(post), bool(pre), alpha, eps, rows, cols, gate_rows, px[0], pf[0], *vectors,
+                px[1], pf[1], y.data_ptr(), ph, cols, cols, stats.data_ptr()))
+        if st:
+            _check(st, "egeria_norm_forward")
         return y, h, stats
 
     def egeria_norm_backward(self, dy: torch.Tensor, dh: Optional[torch.Tensor], y: torch.Tensor, f: torch.Tensor,
@@ -275,23 +326,24 @@ class Ops:
         db_pre, else None."""
         if dy.dim() != 2:
             raise ValueError("dy is a matrix")
-        a, dev, t = _NormBackward(alpha=alpha), self.device, dy.dtype
         rows, cols = dy.shape
-        pt = self._norm_common(a, dy, gate, gate_rows, w_post, b_post, w_pre, b_pre, kind, post, pre)
-        a.dy, a.lddy = _matrix(dy, "dy", dev, t, rows, cols)
-        a.dh, a.lddh = _optional(dh, "dh", dev, t, rows, cols)
-        a.y, a.ldy = _matrix(y, "y", dev, t, rows, cols)
-        a.f, a.ldf = _matrix(f, "f", dev, t, rows, cols)
-        a.stats = _vector(stats, "stats", dev, torch.float32, 4 * rows)
-        with _On(dev, stream, (self._raw, dy, dh, y, f, stats, gate, w_post, b_post, w_pre, b_pre)) as s:
-            out = dict(dx=torch.empty((rows, cols), dtype=t, device=dev), df=torch.empty((rows, cols), dtype=t, device=dev))
-            a.dx, a.lddx = _matrix(out["dx"], "dx", dev, t, rows, cols)
-            a.df, a.lddf = _matrix(out["df"], "df", dev, t, rows, cols)
+        dev, t = self._index, dy.dtype
+        pt, *vectors = self._norm_params(t, rows, cols, gate, gate_rows, w_post, b_post, w_pre, b_pre, kind)
+        pdy, pdh = _matrix(dy, "dy", dev, t, rows, cols), _optional(dh, "dh", dev, t, rows, cols)
+        py, pf = _matrix(y, "y", dev, t, rows, cols), _matrix(f, "f", dev, t, rows, cols)
+        ps = _vector(stats, "stats", dev, torch.float32, 4 * rows)
+        with self._on(stream, dy, dh, y, f, stats, gate, w_post, b_post, w_pre, b_pre) as s:
+            out = dict(dx=dy.new_empty((rows, cols)), df=dy.new_empty((rows, cols)))
+            sums = []
             for name, v, there in (("dgate", gate, True), ("dw_post", w_post, post), ("db_post", b_post, post),
                                    ("dw_pre", w_pre, pre), ("db_pre", b_pre, pre)):
                 out[name] = torch.empty_like(v) if v is not None and there and need_params else None
-                setattr(a, name, None if out[name] is None else out[name].data_ptr())
-            _check(lib().egeria_norm_backward(self._h, s, ctypes.byref(a)), "egeria_norm_backward")
+                sums.append(0 if out[name] is None else out[name].data_ptr())
+            st = self._lib.egeria_norm_backward(self._h, s, _pack_norm_backward(
+                TYPES.get(t, -1), pt, KINDS[kind], bool(post), bool(pre), alpha, rows, cols, gate_rows, pdy[0], pdh[0], py[0], pf[0],
+                *vectors, pdy[1], pdh[1], py[1], pf[1], ps, out["dx"].data_ptr(), out["df"].data_ptr(), cols, cols, *sums))
+        if st:
+            _check(st, "egeria_norm_backward")
         return out
 
     def egeria_ops_device_status(self) -> int:
@@ -304,7 +356,7 @@ class Ops:
         return int(lib().egeria_ops_launch_count(self._h))
 
 
-class AdamW:
+class AdamW(_Handle):
     """The AdamW step of a model's tensors in one launch per combination of types; frozen modules are left out on the device.
 
     params, grads, exp_avg, exp_avg_sq: one contiguous CUDA tensor per tensor of the model; the moments are float32, or
@@ -320,7 +372,8 @@ class AdamW:
         n = len(params)
         if n < 1:
             raise ValueError("no tensors")
-        self.device = params[0].device
+        self._place(params[0].device)
+        dev = self._index
         small = m_scales is not None or v_scales is not None
         none = [None] * n
         columns = dict(grads=grads, exp_avg=exp_avg, exp_avg_sq=exp_avg_sq, masters=masters or none, m_scales=m_scales or none,
@@ -340,12 +393,12 @@ class AdamW:
             row.n, row.param_type = k, TYPES[p.dtype]
             row.grad_type = TYPES.get(columns["grads"][i].dtype, -1)
             row.weight_decay, row.module = float(columns["weight_decay"][i]), self.modules[i]
-            row.param = _vector(p, f"params[{i}]", self.device, p.dtype, k)
-            row.master = _vector(columns["masters"][i], f"masters[{i}]", self.device, torch.float32, k)
-            row.m = _vector(exp_avg[i], f"exp_avg[{i}]", self.device, torch.int8 if small else torch.float32, k)
-            row.v = _vector(exp_avg_sq[i], f"exp_avg_sq[{i}]", self.device, torch.uint8 if small else torch.float32, k)
-            row.m_scale = _vector(columns["m_scales"][i], f"m_scales[{i}]", self.device, torch.float32, blocks)
-            row.v_scale = _vector(columns["v_scales"][i], f"v_scales[{i}]", self.device, torch.float32, blocks)
+            row.param = _vector(p, f"params[{i}]", dev, p.dtype, k)
+            row.master = _vector(columns["masters"][i], f"masters[{i}]", dev, torch.float32, k)
+            row.m = _vector(exp_avg[i], f"exp_avg[{i}]", dev, torch.int8 if small else torch.float32, k)
+            row.v = _vector(exp_avg_sq[i], f"exp_avg_sq[{i}]", dev, torch.uint8 if small else torch.float32, k)
+            row.m_scale = _vector(columns["m_scales"][i], f"m_scales[{i}]", dev, torch.float32, blocks)
+            row.v_scale = _vector(columns["v_scales"][i], f"v_scales[{i}]", dev, torch.float32, blocks)
         self._sizes = [(p.numel(), g.dtype) for p, g in zip(params, grads)]
         self._steps = steps
         self._keep = (list(params), list(exp_avg), list(exp_avg_sq), columns["masters"], columns["m_scales"], columns["v_scales"])
@@ -357,46 +410,40 @@ class AdamW:
             self._raw, ptr = _workspace(nbytes, self.device)
             handle = _vp()
             _check(lib().egeria_adamw_create(ctypes.byref(handle), n, table, self._grad_pointers(grads),
-                                             _vector(steps, "steps", self.device, torch.int32, n), ptr, nbytes, flags),
+                                             _vector(steps, "steps", dev, torch.int32, n), ptr, nbytes, flags),
                    "egeria_adamw_create")
-        self._h = handle
+        self._h, self._lib, self._destroy = handle, lib(), lib().egeria_adamw_destroy
+        self._last_module = max(self.modules)
 
     def _grad_pointers(self, grads):
         if len(grads) != len(self._sizes):
             raise ValueError("grads: one entry per tensor is required")
-        ptrs = (_vp * len(grads))(*[_vector(g, f"grads[{i}]", self.device, t, n)
+        ptrs = (_vp * len(grads))(*[_vector(g, f"grads[{i}]", self._index, t, n)
                                     for i, (g, (n, t)) in enumerate(zip(grads, self._sizes))])
         self._grads = list(grads)
         return ptrs
 
-    def close(self) -> None:
-        if getattr(self, "_h", None):
-            lib().egeria_adamw_destroy(self._h)
-            self._h = None
-
-    def __del__(self):
-        try:
-            self.close()
-        except Exception:
-            pass
-
     def egeria_adamw_set_grads(self, grads: Sequence[torch.Tensor], stream: Optional[torch.cuda.Stream] = None) -> None:
         """The gradients (same sizes and types) are in these tensors from the next step on."""
         ptrs = self._grad_pointers(grads)
-        with _On(self.device, stream, (self._raw,)) as s:
-            _check(lib().egeria_adamw_set_grads(self._h, s, ptrs), "egeria_adamw_set_grads")
+        with self._on(stream) as s:
+            _check(self._lib.egeria_adamw_set_grads(self._h, s, ptrs), "egeria_adamw_set_grads")
 
     def egeria_adamw_step(self, lr: float, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8,
                           grad_scale: Optional[torch.Tensor] = None, frozen: Optional[torch.Tensor] = None,
                           stream: Optional[torch.cuda.Stream] = None) -> None:
         """One step of every tensor whose module is not marked in `frozen` (uint8, as egeria_plasticity_evaluate leaves it)."""
-        gs = _vector(grad_scale, "grad_scale", self.device, torch.float32, 1)
-        if frozen is not None and (frozen.dtype != torch.uint8 or frozen.device != self.device or not frozen.is_contiguous()
-                                   or frozen.numel() <= max(self.modules)):
-            raise ValueError("frozen: expected contiguous uint8, one per module, on the handle's device")
-        with _On(self.device, stream, (self._raw, *self._grads, *[t for c in self._keep for t in c], self._steps, grad_scale, frozen)) as s:
-            _check(lib().egeria_adamw_step(self._h, s, lr, beta1, beta2, eps, gs, None if frozen is None else frozen.data_ptr()),
-                   "egeria_adamw_step")
+        gs = _vector(grad_scale, "grad_scale", self._index, torch.float32, 1)
+        mask = 0 if frozen is None else _vector(frozen, "frozen", self._index, torch.uint8, frozen.numel())
+        if frozen is not None and frozen.numel() <= self._last_module:
+            raise ValueError("frozen: one entry per module is required")
+        with self._on(stream, *(() if stream is None else self._touched()), grad_scale, frozen) as s:
+            st = self._lib.egeria_adamw_step(self._h, s, lr, beta1, beta2, eps, gs or None, mask or None)
+        if st:
+            _check(st, "egeria_adamw_step")
+
+    def _touched(self):
+        return [self._steps, *self._grads, *(t for column in self._keep for t in column)]
 
     def egeria_adamw_device_status(self) -> int:
         return int(lib().egeria_adamw_device_status(self._h))

@@ -22,11 +22,14 @@ def test_library_exports_every_declared_operator():
 
 
 def test_structs_have_the_headers_layout(tmp_path):
-    """Every ctypes mirror has the size and the field offsets that a C compiler gives the header's struct."""
+    """Every mirror of a struct has the size and the field offsets that a C compiler gives the header's."""
     if shutil.which("gcc") is None:
         pytest.skip("no gcc")
-    mirrors = {"egeria_linear_forward_args": ops._LinearForward, "egeria_linear_backward_args": ops._LinearBackward,
-               "egeria_norm_forward_args": ops._NormForward, "egeria_norm_backward_args": ops._NormBackward,
+    def mirror(fields):
+        return type("Mirror", (ctypes.Structure,), {"_fields_": fields})
+
+    mirrors = {"egeria_linear_forward_args": mirror(ops._LINEAR_FORWARD), "egeria_linear_backward_args": mirror(ops._LINEAR_BACKWARD),
+               "egeria_norm_forward_args": mirror(ops._NORM_FORWARD), "egeria_norm_backward_args": mirror(ops._NORM_BACKWARD),
                "egeria_adamw_tensor": ops._AdamTensor}
     lines = ['#include "egeria_ops.h"', "#include <stdio.h>", "int main(void) {"]
     for name, m in mirrors.items():
@@ -41,6 +44,13 @@ def test_structs_have_the_headers_layout(tmp_path):
         assert int(got[name]) == ctypes.sizeof(m)
         for f, _ in m._fields_:
             assert int(got[f"{name}.{f}"]) == getattr(m, f).offset, (name, f)
+    # and the packed forms put the values there
+    for pack, name in ((ops._pack_linear_forward, "egeria_linear_forward_args"), (ops._pack_linear_backward, "egeria_linear_backward_args"),
+                       (ops._pack_norm_forward, "egeria_norm_forward_args"), (ops._pack_norm_backward, "egeria_norm_backward_args")):
+        m = mirrors[name]
+        values = list(range(1, len(m._fields_) + 1))
+        read = m.from_buffer_copy(pack(*values).ljust(ctypes.sizeof(m), b"\0"))
+        assert [getattr(read, f) for f, _ in m._fields_] == values
 
 
 def test_workspace_sizes():
@@ -102,7 +112,6 @@ def test_null_handles_and_arguments():
     assert L.egeria_ops_destroy(None) == eg.ERR_INVALID_ARG
     assert L.egeria_ops_device_status(None) == eg.ERR_INVALID_ARG
     assert L.egeria_ops_launch_count(None) == 0
-    for call, args in ((L.egeria_linear_forward, ops._LinearForward()), (L.egeria_linear_backward, ops._LinearBackward()),
-                       (L.egeria_norm_forward, ops._NormForward()), (L.egeria_norm_backward, ops._NormBackward())):
-        assert call(None, None, ctypes.byref(args)) == eg.ERR_INVALID_ARG
+    for call in (L.egeria_linear_forward, L.egeria_linear_backward, L.egeria_norm_forward, L.egeria_norm_backward):
+        assert call(None, None, bytes(256)) == eg.ERR_INVALID_ARG
         assert call(None, None, None) == eg.ERR_INVALID_ARG

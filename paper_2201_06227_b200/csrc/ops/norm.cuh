@@ -28,6 +28,7 @@ struct NormParams {
     void *dw_post, *db_post, *dw_pre, *db_pre, *dgate;
     int64_t ldx, ldf, ldy, ldh, lddy, lddh;
     int64_t rows, gate_rows;               // gate_rows: rows that share a gate; = rows for one gate
+    int64_t cta_rows, extra;               // backward: rows / CTAs and the remainder
     int32_t cols;
     int32_t layer, post, pre;
     int32_t w_float;                       // weights, biases and gate are float, not T
@@ -42,12 +43,18 @@ __device__ __forceinline__ int norm_col(int t, int i, int j) {
     return WIDE ? (i * TEAM + t) * 8 + j : (i * 8 + j) * TEAM + t;
 }
 
-template <typename T, int TEAM, bool WIDE>
+// Whether value j of run i lies in the row.  FULL: every one does (cols = 8 * TEAM * VPT); WIDE: a run does or does not.
+template <int TEAM, bool WIDE, bool FULL>
+__device__ __forceinline__ bool norm_in(int t, int i, int j, int cols) {
+    return FULL || norm_col<TEAM, WIDE>(t, i, WIDE ? 0 : j) < cols;
+}
+
+// Run i of a row; zeros past its end.
+template <typename T, int TEAM, bool WIDE, bool FULL>
 __device__ __forceinline__ void norm_load(Raw8<T> &d, const T *row, int t, int i, int cols) {
     if (WIDE) {
-        const int c = norm_col<TEAM, WIDE>(t, i, 0);
-        if (c < cols) {
-            load8(d, row + c);
+        if (norm_in<TEAM, WIDE, FULL>(t, i, 0, cols)) {
+            load8(d, row + norm_col<TEAM, WIDE>(t, i, 0));
             return;
         }
 #pragma unroll
@@ -62,11 +69,10 @@ __device__ __forceinline__ void norm_load(Raw8<T> &d, const T *row, int t, int i
         memcpy(&d, v, sizeof(v));
     }
 }
-template <typename T, int TEAM, bool WIDE>
+template <typename T, int TEAM, bool WIDE, bool FULL>
 __device__ __forceinline__ void norm_store(T *row, const float (&v)[8], int t, int i, int cols) {
     if (WIDE) {
-        const int c = norm_col<TEAM, WIDE>(t, i, 0);
-        if (c < cols) store8(row + c, v);
+        if (norm_in<TEAM, WIDE, FULL>(t, i, 0, cols)) store8(row + norm_col<TEAM, WIDE>(t, i, 0), v);
     } else {
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
@@ -77,23 +83,23 @@ __device__ __forceinline__ void norm_store(T *row, const float (&v)[8], int t, i
 }
 // A vector of `cols` weights, biases or gates, of type float or T, or `absent` in each place; it stays in L1.
 // WIDE: aligned like a row.
-template <typename T, int TEAM, bool WIDE>
+template <typename T, int TEAM, bool WIDE, bool FULL>
 __device__ __forceinline__ void norm_vector(float (&v)[8], const void *p, int64_t first, int is_float, int t, int i, int cols, float absent) {
     if (!p) {
 #pragma unroll
         for (int j = 0; j < 8; ++j) v[j] = absent;
     } else if (is_float) {
         Raw8<float> d;
-        norm_load<float, TEAM, WIDE>(d, static_cast<const float *>(p) + first, t, i, cols);
+        norm_load<float, TEAM, WIDE, FULL>(d, static_cast<const float *>(p) + first, t, i, cols);
         unpack8(v, d);
     } else {
         Raw8<T> d;
-        norm_load<T, TEAM, WIDE>(d, static_cast<const T *>(p) + first, t, i, cols);
+        norm_load<T, TEAM, WIDE, FULL>(d, static_cast<const T *>(p) + first, t, i, cols);
         unpack8(v, d);
     }
 }
 
-// Sums over the team, the same bits in every thread.  `scratch`: 2 x 32 x N floats; `turn` alternates
+// Sums over the team, the same bits in every thread.  `scratch`: 2 x N x 32 floats; `turn` alternates
 // between its halves, so that one barrier per reduction is enough.
 template <int TEAM, int N>
 __device__ __forceinline__ void team_sum(float (&v)[N], float *scratch, int &turn) {
@@ -108,86 +114,94 @@ __device__ __forceinline__ void team_sum(float (&v)[N], float *scratch, int &tur
         for (int n = 0; n < N; ++n) half[n * 32 + warp] = v[n];
     }
     __syncthreads();
+    if (TEAM <= 256) {
 #pragma unroll
-    for (int n = 0; n < N; ++n) v[n] = warp_sum(lane < TEAM / 32 ? half[n * 32 + lane] : 0.0f);
+        for (int n = 0; n < N; ++n) {
+            v[n] = 0.0f;
+#pragma unroll
+            for (int w = 0; w < TEAM / 32; ++w) v[n] += half[n * 32 + w];
+        }
+    } else {
+#pragma unroll
+        for (int n = 0; n < N; ++n) v[n] = warp_sum(lane < TEAM / 32 ? half[n * 32 + lane] : 0.0f);
+    }
 }
 
-// Mean and 1/deviation of the row that the team holds in v.
-template <int TEAM, bool WIDE, int VPT>
-__device__ __forceinline__ void norm_stats(const float (&v)[VPT][8], const NormParams &p, int t, float &mean, float &inv,
-                                           float *scratch, int &turn) {
+// Takes the mean off the row that the team holds in v (layer norm) and returns it and 1/deviation.
+template <int TEAM, int VPT, bool WIDE, bool FULL>
+__device__ __forceinline__ void norm_center(float (&v)[VPT][8], const NormParams &p, int t, float &mean, float &inv, float *scratch,
+                                            int &turn) {
     mean = 0.0f;
     if (p.layer) {
         float s[1] = {0.0f};
 #pragma unroll
         for (int i = 0; i < VPT; ++i)
 #pragma unroll
-            for (int j = 0; j < 8; ++j) s[0] += v[i][j];  // columns past the row's end hold 0
+            for (int j = 0; j < 8; ++j) s[0] += v[i][j];  // past the row's end there are zeros
         team_sum<TEAM>(s, scratch, turn);
         mean = s[0] * p.inv_cols;
+#pragma unroll
+        for (int i = 0; i < VPT; ++i)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[i][j] = norm_in<TEAM, WIDE, FULL>(t, i, j, p.cols) ? v[i][j] - mean : 0.0f;
     }
     float q[1] = {0.0f};
 #pragma unroll
     for (int i = 0; i < VPT; ++i)
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const float d = norm_col<TEAM, WIDE>(t, i, j) < p.cols ? v[i][j] - mean : 0.0f;
-            q[0] = fmaf(d, d, q[0]);
-        }
+        for (int j = 0; j < 8; ++j) q[0] = fmaf(v[i][j], v[i][j], q[0]);
     team_sum<TEAM>(q, scratch, turn);
     inv = rsqrtf(fmaf(q[0], p.inv_cols, p.eps));
 }
 
-template <typename T, int TEAM, int VPT, bool WIDE>
+template <typename T, int TEAM, int VPT, bool WIDE, bool FULL>
 __global__ void __launch_bounds__(TEAM == 32 ? 128 : TEAM) norm_forward_kernel(const NormParams p) {
     __shared__ float scratch[2 * 32 * 2];
     int turn = 0;
     const int t = TEAM == 32 ? (threadIdx.x & 31) : threadIdx.x;
-    const int64_t row0 = TEAM == 32 ? (int64_t)blockIdx.x * 4 + (threadIdx.x >> 5) : blockIdx.x;
-    if (row0 >= p.rows) return;
-    const int64_t r = row0;
+    const int64_t r = TEAM == 32 ? (int64_t)blockIdx.x * 4 + (threadIdx.x >> 5) : blockIdx.x;
+    if (r >= p.rows) return;
     Raw8<T> rx[VPT], rf[VPT];
 #pragma unroll
     for (int i = 0; i < VPT; ++i) {
-        norm_load<T, TEAM, WIDE>(rf[i], static_cast<const T *>(p.f) + r * p.ldf, t, i, p.cols);
-        norm_load<T, TEAM, WIDE>(rx[i], static_cast<const T *>(p.x) + r * p.ldx, t, i, p.cols);
+        norm_load<T, TEAM, WIDE, FULL>(rf[i], static_cast<const T *>(p.f) + r * p.ldf, t, i, p.cols);
+        norm_load<T, TEAM, WIDE, FULL>(rx[i], static_cast<const T *>(p.x) + r * p.ldx, t, i, p.cols);
     }
     float f[VPT][8];
 #pragma unroll
     for (int i = 0; i < VPT; ++i) unpack8(f[i], rf[i]);
     float st[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-    if (p.post) norm_stats<TEAM, WIDE>(f, p, t, st[0], st[1], scratch, turn);
+    if (p.post) norm_center<TEAM, VPT, WIDE, FULL>(f, p, t, st[0], st[1], scratch, turn);
     const int64_t gate = p.gate ? (r / p.gate_rows) * p.cols : 0;
 #pragma unroll
     for (int i = 0; i < VPT; ++i) {
         float v[8], b[8];
         if (p.post) {
-            norm_vector<T, TEAM, WIDE>(v, p.w_post, 0, p.w_float, t, i, p.cols, 1.0f);
-            norm_vector<T, TEAM, WIDE>(b, p.b_post, 0, p.w_float, t, i, p.cols, 0.0f);
+            norm_vector<T, TEAM, WIDE, FULL>(v, p.w_post, 0, p.w_float, t, i, p.cols, 1.0f);
+            norm_vector<T, TEAM, WIDE, FULL>(b, p.b_post, 0, p.w_float, t, i, p.cols, 0.0f);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) f[i][j] = fmaf((f[i][j] - st[0]) * st[1], v[j], b[j]);
+            for (int j = 0; j < 8; ++j) f[i][j] = fmaf(f[i][j] * st[1], v[j], b[j]);
         }
         if (p.gate) {
-            norm_vector<T, TEAM, WIDE>(v, p.gate, gate, p.w_float, t, i, p.cols, 1.0f);
+            norm_vector<T, TEAM, WIDE, FULL>(v, p.gate, gate, p.w_float, t, i, p.cols, 1.0f);
 #pragma unroll
             for (int j = 0; j < 8; ++j) f[i][j] *= v[j];
         }
         unpack8(v, rx[i]);
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-            f[i][j] = norm_col<TEAM, WIDE>(t, i, j) < p.cols ? fmaf(p.alpha, v[j], f[i][j]) : 0.0f;
-        norm_store<T, TEAM, WIDE>(static_cast<T *>(p.y) + r * p.ldy, f[i], t, i, p.cols);
+        for (int j = 0; j < 8; ++j) f[i][j] = fmaf(p.alpha, v[j], f[i][j]);  // zeros stay past the row's end: all vectors are 0 there
+        norm_store<T, TEAM, WIDE, FULL>(static_cast<T *>(p.y) + r * p.ldy, f[i], t, i, p.cols);
     }
     if (p.pre) {
-        norm_stats<TEAM, WIDE>(f, p, t, st[2], st[3], scratch, turn);
+        norm_center<TEAM, VPT, WIDE, FULL>(f, p, t, st[2], st[3], scratch, turn);
 #pragma unroll
         for (int i = 0; i < VPT; ++i) {
             float v[8], b[8];
-            norm_vector<T, TEAM, WIDE>(v, p.w_pre, 0, p.w_float, t, i, p.cols, 1.0f);
-            norm_vector<T, TEAM, WIDE>(b, p.b_pre, 0, p.w_float, t, i, p.cols, 0.0f);
+            norm_vector<T, TEAM, WIDE, FULL>(v, p.w_pre, 0, p.w_float, t, i, p.cols, 1.0f);
+            norm_vector<T, TEAM, WIDE, FULL>(b, p.b_pre, 0, p.w_float, t, i, p.cols, 0.0f);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) f[i][j] = fmaf((f[i][j] - st[2]) * st[3], v[j], b[j]);
-            norm_store<T, TEAM, WIDE>(static_cast<T *>(p.h) + r * p.ldh, f[i], t, i, p.cols);
+            for (int j = 0; j < 8; ++j) f[i][j] = fmaf(f[i][j] * st[3], v[j], b[j]);
+            norm_store<T, TEAM, WIDE, FULL>(static_cast<T *>(p.h) + r * p.ldh, f[i], t, i, p.cols);
         }
     }
     if (t == 0 && p.stats) *reinterpret_cast<float4 *>(p.stats + 4 * r) = make_float4(st[0], st[1], st[2], st[3]);
@@ -215,189 +229,241 @@ __device__ __forceinline__ void store_param(void *p, int64_t at, float v, int is
         static_cast<T *>(p)[at] = from_f32<T>(v);
 }
 
-// Rows of CTA c of n: the same split in both kernels.
-__host__ __device__ __forceinline__ int64_t norm_first_row(int64_t rows, int n, int c) { return rows * c / n; }
+// First row of CTA c, the same split in both kernels: the first `extra` CTAs have one row more than the others.
+__device__ __forceinline__ int64_t norm_first_row(const NormParams &p, int c) { return c * p.cta_rows + min((int64_t)c, p.extra); }
+// The CTA that has row r.
+__device__ __forceinline__ int norm_holder(const NormParams &p, int64_t r) {
+    const int64_t longer = p.extra * (p.cta_rows + 1);
+    return (int)(r < longer ? r / (p.cta_rows + 1) : p.extra + (r - longer) / p.cta_rows);
+}
 
-template <typename T, int TEAM, int VPT, bool WIDE>
-__global__ void __launch_bounds__(TEAM) norm_backward_kernel(const NormParams p) {
+// Rows on their way: a thread copies its own 8 values of each of the four matrices into shared memory, up to two
+// rows ahead, and is the only one to read them, so that no barrier belongs to it.
+template <typename T, int TEAM>
+__host__ __device__ constexpr int norm_ring_rows() {
+    return 3 * 4 * TEAM * (int)sizeof(Raw8<T>) <= 200 * 1024 ? 3 : 1;
+}
+template <typename T>
+__device__ __forceinline__ void copy_ahead(Raw8<T> *dst, const T *src, bool in) {
+    const uint32_t d = (uint32_t)__cvta_generic_to_shared(dst);
+    const int bytes = in ? 16 : 0;  // past the row's end: zeros
+#pragma unroll
+    for (int k = 0; k < (int)sizeof(Raw8<T>) / 16; ++k)
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(d + 16 * k), "l"(reinterpret_cast<const char *>(src) + (in ? 16 * k : 0)),
+                     "r"(bytes)
+                     : "memory");
+}
+
+// BIAS: the norms have biases, whose sums are kept (a gradient that is not wanted is not written).
+template <typename T, int TEAM, bool WIDE, bool FULL, bool BIAS>
+__global__ void __launch_bounds__(TEAM, TEAM >= 512 ? 1 : 512 / TEAM) norm_backward_kernel(const NormParams p) {
+    constexpr int kRows = norm_ring_rows<T, TEAM>();
+    extern __shared__ __align__(16) uint8_t norm_smem[];
     __shared__ float scratch[2 * 32 * 2];
+    Raw8<T> *ring = reinterpret_cast<Raw8<T> *>(norm_smem);  // [kRows][4][TEAM]
     int turn = 0;
     const int t = threadIdx.x;
-    const int64_t r0 = norm_first_row(p.rows, gridDim.x, blockIdx.x), r1 = norm_first_row(p.rows, gridDim.x, blockIdx.x + 1);
-    float sw_pre[VPT][8], sb_pre[VPT][8], sw_post[VPT][8], sb_post[VPT][8], sg[VPT][8];
-#pragma unroll
-    for (int i = 0; i < VPT; ++i)
-#pragma unroll
-        for (int j = 0; j < 8; ++j) sw_pre[i][j] = sb_pre[i][j] = sw_post[i][j] = sb_post[i][j] = sg[i][j] = 0.0f;
+    const int64_t r0 = norm_first_row(p, blockIdx.x), r1 = norm_first_row(p, blockIdx.x + 1);
     float *sums = p.sums + (int64_t)blockIdx.x * kNormSums * p.cols;
+    const bool in = norm_in<TEAM, WIDE, FULL>(t, 0, 0, p.cols);
+    const int col = norm_col<TEAM, WIDE>(t, 0, 0);
 
-    for (int64_t r = r0; r < r1; ++r) {
-        Raw8<T> ry[VPT], rdh[VPT], rdy[VPT], rf[VPT];
-#pragma unroll
-        for (int i = 0; i < VPT; ++i) {
+    auto fetch = [&](int64_t r, int slot) {
+        if (WIDE && r < r1) {
+            Raw8<T> *to = ring + (slot * 4) * TEAM + t;
+            const int c = in ? col : 0;
+            copy_ahead(to, static_cast<const T *>(p.dy) + r * p.lddy + c, in);
+            copy_ahead(to + TEAM, static_cast<const T *>(p.f) + r * p.ldf + c, in);
             if (p.pre) {
-                norm_load<T, TEAM, WIDE>(ry[i], static_cast<const T *>(p.x) + r * p.ldx, t, i, p.cols);
-                norm_load<T, TEAM, WIDE>(rdh[i], static_cast<const T *>(p.dh) + r * p.lddh, t, i, p.cols);
+                copy_ahead(to + 2 * TEAM, static_cast<const T *>(p.dh) + r * p.lddh + c, in);
+                copy_ahead(to + 3 * TEAM, static_cast<const T *>(p.x) + r * p.ldx + c, in);
             }
-            norm_load<T, TEAM, WIDE>(rdy[i], static_cast<const T *>(p.dy) + r * p.lddy, t, i, p.cols);
-            norm_load<T, TEAM, WIDE>(rf[i], static_cast<const T *>(p.f) + r * p.ldf, t, i, p.cols);
         }
-        const float4 st = *reinterpret_cast<const float4 *>(p.stats + 4 * r);
-        float tot[VPT][8], v[8];
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    };
 #pragma unroll
-        for (int i = 0; i < VPT; ++i) unpack8(tot[i], rdy[i]);
+    for (int k = 0; k < kRows - 1; ++k) fetch(r0 + k, k);
+
+    float w_pre[8], w_post[8], b_post[8], gate[8];
+    norm_vector<T, TEAM, WIDE, FULL>(w_pre, p.w_pre, 0, p.w_float, t, 0, p.cols, 1.0f);
+    norm_vector<T, TEAM, WIDE, FULL>(w_post, p.w_post, 0, p.w_float, t, 0, p.cols, 1.0f);
+    if (BIAS) norm_vector<T, TEAM, WIDE, FULL>(b_post, p.b_post, 0, p.w_float, t, 0, p.cols, 0.0f);
+    float sw_pre[8], sb_pre[8], sw_post[8], sb_post[8], sg[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) sw_pre[j] = sb_pre[j] = sw_post[j] = sb_post[j] = sg[j] = 0.0f, gate[j] = 1.0f;
+
+    int64_t group = 0, left = 0;  // the gate in force and how many of its rows are to come
+    int slot = 0;
+    for (int64_t r = r0; r < r1; ++r) {
+        {
+            const int ahead = slot + kRows - 1;
+            fetch(r + kRows - 1, ahead >= kRows ? ahead - kRows : ahead);
+        }
+        Raw8<T> ry, rdh, rdy, rf;
+        if (WIDE) {
+            asm volatile("cp.async.wait_group %0;" ::"n"(kRows - 1) : "memory");
+            const Raw8<T> *from = ring + (slot * 4) * TEAM + t;
+            rdy = from[0];
+            rf = from[TEAM];
+            if (p.pre) rdh = from[2 * TEAM], ry = from[3 * TEAM];
+            slot = slot + 1 == kRows ? 0 : slot + 1;
+        } else {
+            norm_load<T, TEAM, WIDE, FULL>(rdy, static_cast<const T *>(p.dy) + r * p.lddy, t, 0, p.cols);
+            norm_load<T, TEAM, WIDE, FULL>(rf, static_cast<const T *>(p.f) + r * p.ldf, t, 0, p.cols);
+            if (p.pre) {
+                norm_load<T, TEAM, WIDE, FULL>(rdh, static_cast<const T *>(p.dh) + r * p.lddh, t, 0, p.cols);
+                norm_load<T, TEAM, WIDE, FULL>(ry, static_cast<const T *>(p.x) + r * p.ldx, t, 0, p.cols);
+            }
+        }
+        const float4 st = __ldg(reinterpret_cast<const float4 *>(p.stats + 4 * r));
+        if (p.gate && left == 0) {
+            group = r / p.gate_rows;
+            left = min((group + 1) * p.gate_rows, p.rows) - r;
+            norm_vector<T, TEAM, WIDE, FULL>(gate, p.gate, group * p.cols, p.w_float, t, 0, p.cols, 1.0f);
+        }
+        float tot[8];
+        unpack8(tot, rdy);
         if (p.pre) {
-            float hat[VPT][8], d[VPT][8], s[2] = {0.0f, 0.0f};
+            float hat[8], d[8], s[2] = {0.0f, 0.0f};
+            unpack8(hat, ry);
+            unpack8(d, rdh);
 #pragma unroll
-            for (int i = 0; i < VPT; ++i) {
-                unpack8(hat[i], ry[i]);
-                unpack8(d[i], rdh[i]);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    hat[i][j] = (hat[i][j] - st.z) * st.w;
-                    sw_pre[i][j] = fmaf(d[i][j], hat[i][j], sw_pre[i][j]);
-                    sb_pre[i][j] += d[i][j];
-                }
-                norm_vector<T, TEAM, WIDE>(v, p.w_pre, 0, p.w_float, t, i, p.cols, 1.0f);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    d[i][j] *= v[j];
-                    s[0] = fmaf(d[i][j], hat[i][j], s[0]);  // d is 0 past the row's end
-                    s[1] += d[i][j];
-                }
+            for (int j = 0; j < 8; ++j) {
+                hat[j] = (hat[j] - st.z) * st.w;
+                sw_pre[j] = fmaf(d[j], hat[j], sw_pre[j]);
+                if (BIAS) sb_pre[j] += d[j];
+                d[j] *= w_pre[j];
+                s[0] = fmaf(d[j], hat[j], s[0]);  // d is 0 past the row's end
+                s[1] += d[j];
             }
             team_sum<TEAM>(s, scratch, turn);
             const float along = s[0] * p.inv_cols, lean = p.layer ? s[1] * p.inv_cols : 0.0f;
 #pragma unroll
-            for (int i = 0; i < VPT; ++i)
-#pragma unroll
-                for (int j = 0; j < 8; ++j) tot[i][j] = fmaf(st.w, d[i][j] - lean - hat[i][j] * along, tot[i][j]);
+            for (int j = 0; j < 8; ++j) tot[j] = fmaf(st.w, fmaf(-hat[j], along, d[j] - lean), tot[j]);
         }
+        {
+            float v[8];
 #pragma unroll
-        for (int i = 0; i < VPT; ++i) {
-#pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] = p.alpha * tot[i][j];
-            norm_store<T, TEAM, WIDE>(static_cast<T *>(p.y) + r * p.ldy, v, t, i, p.cols);
+            for (int j = 0; j < 8; ++j) v[j] = p.alpha * tot[j];
+            norm_store<T, TEAM, WIDE, FULL>(static_cast<T *>(p.y) + r * p.ldy, v, t, 0, p.cols);
         }
         // the branch f
-        const int64_t group = p.gate ? r / p.gate_rows : 0;
-        float hat[VPT][8], d[VPT][8], s[2] = {0.0f, 0.0f};
+        float hat[8], d[8], s[2] = {0.0f, 0.0f};
+        unpack8(hat, rf);
 #pragma unroll
-        for (int i = 0; i < VPT; ++i) {
-            unpack8(hat[i], rf[i]);
-            float w[8], b[8];
-            if (p.post) {
-                norm_vector<T, TEAM, WIDE>(w, p.w_post, 0, p.w_float, t, i, p.cols, 1.0f);
-                norm_vector<T, TEAM, WIDE>(b, p.b_post, 0, p.w_float, t, i, p.cols, 0.0f);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) hat[i][j] = (hat[i][j] - st.x) * st.y;
-            } else {
-#pragma unroll
-                for (int j = 0; j < 8; ++j) w[j] = 1.0f, b[j] = 0.0f;
-            }
-            if (p.gate) {
-                norm_vector<T, TEAM, WIDE>(v, p.gate, group * p.cols, p.w_float, t, i, p.cols, 1.0f);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    sg[i][j] = fmaf(tot[i][j], fmaf(hat[i][j], w[j], b[j]), sg[i][j]);
-                    d[i][j] = tot[i][j] * v[j];
-                }
-            } else {
-#pragma unroll
-                for (int j = 0; j < 8; ++j) d[i][j] = tot[i][j];
-            }
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const bool in = norm_col<TEAM, WIDE>(t, i, j) < p.cols;
-                d[i][j] = in ? d[i][j] : 0.0f;
-                sw_post[i][j] = fmaf(d[i][j], hat[i][j], sw_post[i][j]);
-                sb_post[i][j] += d[i][j];
-                d[i][j] *= w[j];
-                s[0] = fmaf(d[i][j], hat[i][j], s[0]);
-                s[1] += d[i][j];
-            }
+        for (int j = 0; j < 8; ++j) {
+            if (!norm_in<TEAM, WIDE, FULL>(t, 0, j, p.cols)) tot[j] = 0.0f;
+            if (p.post) hat[j] = (hat[j] - st.x) * st.y;
+            sg[j] = fmaf(tot[j], BIAS ? fmaf(hat[j], w_post[j], b_post[j]) : hat[j] * w_post[j], sg[j]);
+            d[j] = tot[j] * gate[j];
+            sw_post[j] = fmaf(d[j], hat[j], sw_post[j]);
+            if (BIAS) sb_post[j] += d[j];
+            d[j] *= w_post[j];
+            s[0] = fmaf(d[j], hat[j], s[0]);
+            s[1] += d[j];
         }
         if (p.post) {
             team_sum<TEAM>(s, scratch, turn);
             const float along = s[0] * p.inv_cols, lean = p.layer ? s[1] * p.inv_cols : 0.0f;
 #pragma unroll
-            for (int i = 0; i < VPT; ++i)
-#pragma unroll
-                for (int j = 0; j < 8; ++j) d[i][j] = st.y * (d[i][j] - lean - hat[i][j] * along);
+            for (int j = 0; j < 8; ++j) d[j] = st.y * fmaf(-hat[j], along, d[j] - lean);
         }
-#pragma unroll
-        for (int i = 0; i < VPT; ++i) norm_store<T, TEAM, WIDE>(static_cast<T *>(p.h) + r * p.ldh, d[i], t, i, p.cols);
+        norm_store<T, TEAM, WIDE, FULL>(static_cast<T *>(p.h) + r * p.ldh, d, t, 0, p.cols);
         // the gate's sums leave at the end of a group and at the end of the run
-        if (p.gate && (r + 1 == r1 || (r + 1) % p.gate_rows == 0)) {
+        if (p.gate && (--left == 0 || r + 1 == r1)) {
             const int64_t g0 = group * p.gate_rows, g1 = min(g0 + p.gate_rows, p.rows);
             const bool whole = g0 >= r0 && g1 <= r1, first = g0 <= r0;
 #pragma unroll
-            for (int i = 0; i < VPT; ++i)
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const int c = norm_col<TEAM, WIDE>(t, i, j);
-                    if (c < p.cols) {
-                        if (whole)
-                            store_param<T>(p.dgate, group * p.cols + c, sg[i][j], p.w_float);
-                        else
-                            sums[(first ? 4 : 5) * (int64_t)p.cols + c] = sg[i][j];
-                    }
-                    sg[i][j] = 0.0f;
+            for (int j = 0; j < 8; ++j) {
+                const int c = norm_col<TEAM, WIDE>(t, 0, j);
+                if (c < p.cols) {
+                    if (!whole)
+                        sums[(first ? 4 : 5) * (int64_t)p.cols + c] = sg[j];
+                    else if (p.dgate)
+                        store_param<T>(p.dgate, group * p.cols + c, sg[j], p.w_float);
                 }
+                sg[j] = 0.0f;
+            }
         }
     }
 #pragma unroll
-    for (int i = 0; i < VPT; ++i)
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const int c = norm_col<TEAM, WIDE>(t, i, j);
-            if (c >= p.cols) continue;
-            if (p.dw_pre) sums[c] = sw_pre[i][j];
-            if (p.db_pre) sums[(int64_t)p.cols + c] = sb_pre[i][j];
-            if (p.dw_post) sums[2 * (int64_t)p.cols + c] = sw_post[i][j];
-            if (p.db_post) sums[3 * (int64_t)p.cols + c] = sb_post[i][j];
-        }
+    for (int j = 0; j < 8; ++j) {
+        const int c = norm_col<TEAM, WIDE>(t, 0, j);
+        if (c >= p.cols) continue;
+        if (p.dw_pre) sums[c] = sw_pre[j];
+        if (BIAS && p.db_pre) sums[(int64_t)p.cols + c] = sb_pre[j];
+        if (p.dw_post) sums[2 * (int64_t)p.cols + c] = sw_post[j];
+        if (BIAS && p.db_post) sums[3 * (int64_t)p.cols + c] = sb_post[j];
+    }
 }
 
-// Adds the partial sums of n CTAs.  blockIdx.y < 4: one of the four sums over all rows; else the group
-// of rows that CTA y - 4 finds begun by the CTA before it (if there is one, and that CTA began it).
-template <typename T>
-__global__ void __launch_bounds__(256) norm_sums_kernel(const NormParams p, int n) {
-    __shared__ float part[8][33];
+// The sum over k = first..last of src[k * pitch], 32 columns per block (lane = column), the k dealt to the 32 warps;
+// in warp 0.  The order depends on the sizes alone.
+constexpr int kSumsThreads = 1024;
+template <typename F>
+__device__ __forceinline__ float sum_partials(int first, int last, float (*part)[33], F at) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int c = blockIdx.x * 32 + lane;
-    void *const outs[4] = {p.dw_pre, p.db_pre, p.dw_post, p.db_post};
-    const int what = blockIdx.y;
-    int first = 0, last = n - 1;
-    int64_t group = 0, g0 = 0;
-    void *out;
-    if (what < 4) {
-        out = outs[what];
-        if (!out) return;
-    } else {
-        const int k = what - 4;
-        if (k == 0 || !p.dgate) return;
-        out = p.dgate;
-        group = norm_first_row(p.rows, n, k) / p.gate_rows;
-        g0 = group * p.gate_rows;
-        if (g0 == norm_first_row(p.rows, n, k) || g0 < norm_first_row(p.rows, n, k - 1)) return;
-        const int64_t g1 = min(g0 + p.gate_rows, p.rows);
-        first = k - 1;
-        last = k;
-        while (last + 1 < n && norm_first_row(p.rows, n, last + 1) < g1) ++last;
-    }
     float s = 0.0f;
-    for (int k = first + warp; k <= last; k += 8) {
-        const int slot = what < 4 ? what : (g0 <= norm_first_row(p.rows, n, k) ? 4 : 5);
-        if (c < p.cols) s += p.sums[((int64_t)k * kNormSums + slot) * p.cols + c];
+    int k = first + warp;
+    for (; k + 7 * 32 <= last; k += 8 * 32) {  // eight loads in flight
+        float v[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) v[u] = at(k + 32 * u);
+#pragma unroll
+        for (int u = 0; u < 8; ++u) s += v[u];
     }
+#pragma unroll 4
+    for (; k <= last; k += 32) s += at(k);
     part[warp][lane] = s;
     __syncthreads();
-    if (warp == 0 && c < p.cols) {
+    s = 0.0f;
+    if (warp == 0) {
 #pragma unroll
-        for (int w = 1; w < 8; ++w) s += part[w][lane];
-        store_param<T>(out, group * p.cols + c, s, p.w_float);
+        for (int w = 0; w < 32; ++w) s += part[w][lane];
     }
+    __syncthreads();
+    return s;
+}
+
+// Adds the partial sums of n CTAs.  blockIdx.y < 4: one of the four sums over all rows.  The other blocks finish the gates
+// of groups of rows that several CTAs share, in one of two ways: a warp per CTA that finds a group begun by the
+// CTA before it and adds its few parts (kLongGroup CTAs at most share a group), or a block per group.
+constexpr int kLongGroup = 32;
+template <typename T>
+__global__ void __launch_bounds__(kSumsThreads) norm_sums_kernel(const NormParams p, int n, int long_groups) {
+    __shared__ float part[32][33];
+    const int c = blockIdx.x * 32 + (threadIdx.x & 31), cc = min(c, p.cols - 1);
+    const bool writes = threadIdx.x < 32 && c < p.cols;
+    const int64_t pitch = (int64_t)kNormSums * p.cols;
+    if (blockIdx.y < 4) {
+        void *const outs[4] = {p.dw_pre, p.db_pre, p.dw_post, p.db_post};
+        void *out = outs[blockIdx.y];
+        if (!out) return;
+        const float *src = p.sums + (int64_t)blockIdx.y * p.cols + cc;
+        const float s = sum_partials(0, n - 1, part, [&](int k) { return src[k * pitch]; });
+        if (writes) store_param<T>(out, c, s, p.w_float);
+        return;
+    }
+    // a group's part is its first CTA's last group (place 5), unless it begins with that CTA, and every other one's first (4)
+    const float *head = p.sums + 4 * (int64_t)p.cols + cc, *tail = head + p.cols;
+    if (long_groups) {
+        const int64_t group = blockIdx.y - 4, g0 = group * p.gate_rows, g1 = min(g0 + p.gate_rows, p.rows);
+        const int first = norm_holder(p, g0), last = norm_holder(p, g1 - 1);
+        if (first == last) return;
+        const bool begins = norm_first_row(p, first) == g0;
+        const float s = sum_partials(first, last, part, [&](int k) { return (k == first && !begins ? tail : head)[k * pitch]; });
+        if (writes) store_param<T>(p.dgate, group * p.cols + c, s, p.w_float);
+        return;
+    }
+    const int k = 1 + ((int)blockIdx.y - 4) * 32 + (threadIdx.x >> 5);
+    if (k >= n) return;
+    const int64_t mine = norm_first_row(p, k), before = norm_first_row(p, k - 1), group = mine / p.gate_rows, g0 = group * p.gate_rows;
+    if (g0 == mine || g0 < before) return;
+    const int64_t g1 = min(g0 + p.gate_rows, p.rows);
+    float s = (g0 == before ? head : tail)[(k - 1) * pitch] + head[k * pitch];
+#pragma unroll 4
+    for (int j = k + 1; j < n && norm_first_row(p, j) < g1; ++j) s += head[j * pitch];
+    if (c < p.cols) store_param<T>(p.dgate, group * p.cols + c, s, p.w_float);
 }
 
 }  // namespace ops

@@ -117,16 +117,16 @@ static LinearLayout linear_layout(int64_t rows, int64_t inp, int64_t out) {
 
 // ---------------------------------------------------------------- norms
 struct NormPlan {
-    int team, vpt, ctas;  // ctas: of the backward pass
+    int team, ctas;  // threads, and thread blocks, of the backward pass
 };
 static NormPlan norm_backward_plan(int64_t rows, int64_t cols) {
-    NormPlan n{32, 1, 16};
-    if (cols > 4096) n = {1024, 1, 1};
-    else if (cols > 2048) n = {512, 1, 1};
-    else if (cols > 1024) n = {256, 1, 2};
-    else if (cols > 512) n = {128, 1, 4};
-    else if (cols > 256) n = {64, 1, 8};
-    n.ctas = (int)std::min<int64_t>(rows, (int64_t)n.ctas * kSms);
+    NormPlan n{32, 16};
+    if (cols > 4096) n = {1024, 1};
+    else if (cols > 2048) n = {512, 1};
+    else if (cols > 1024) n = {256, 2};
+    else if (cols > 512) n = {128, 4};
+    else if (cols > 256) n = {64, 8};
+    n.ctas = (int)std::max<int64_t>(std::min<int64_t>(rows, 1), std::min<int64_t>(rows / 2, (int64_t)n.ctas * kSms));
     return n;
 }
 
@@ -328,10 +328,13 @@ template <typename T, int TEAM, int VPT>
 static cudaError_t norm_fwd(const NormParams &p, bool wide, cudaStream_t stream) {
     const int64_t per = TEAM == 32 ? 4 : 1;
     const unsigned grid = (unsigned)((p.rows + per - 1) / per);
-    if (wide)
-        norm_forward_kernel<T, TEAM, VPT, true><<<grid, TEAM == 32 ? 128 : TEAM, 0, stream>>>(p);
+    const int threads = TEAM == 32 ? 128 : TEAM;
+    if (wide && p.cols == TEAM * VPT * 8)
+        norm_forward_kernel<T, TEAM, VPT, true, true><<<grid, threads, 0, stream>>>(p);
+    else if (wide)
+        norm_forward_kernel<T, TEAM, VPT, true, false><<<grid, threads, 0, stream>>>(p);
     else
-        norm_forward_kernel<T, TEAM, VPT, false><<<grid, TEAM == 32 ? 128 : TEAM, 0, stream>>>(p);
+        norm_forward_kernel<T, TEAM, VPT, false, false><<<grid, threads, 0, stream>>>(p);
     return cudaGetLastError();
 }
 template <typename T>
@@ -342,27 +345,39 @@ static cudaError_t norm_fwd_any(const NormParams &p, bool wide, cudaStream_t str
     if (p.cols <= 4096) return norm_fwd<T, 128, 4>(p, wide, stream);
     return norm_fwd<T, 256, 4>(p, wide, stream);
 }
-template <typename T, int TEAM, int VPT>
-static cudaError_t norm_bwd(const NormParams &p, int ctas, bool wide, cudaStream_t stream) {
-    if (wide)
-        norm_backward_kernel<T, TEAM, VPT, true><<<ctas, TEAM, 0, stream>>>(p);
-    else
-        norm_backward_kernel<T, TEAM, VPT, false><<<ctas, TEAM, 0, stream>>>(p);
-    return cudaGetLastError();
+template <typename T, int TEAM>
+static cudaError_t norm_bwd(const NormParams &p, int ctas, bool wide, bool bias, cudaStream_t stream) {
+    const size_t smem = wide ? (size_t)norm_ring_rows<T, TEAM>() * 4 * TEAM * sizeof(Raw8<T>) : 0;
+    auto go = [&](auto kernel) {
+        if (smem > 40 * 1024) {  // with the static part: beyond what needs no permission
+            const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+            if (e != cudaSuccess) return e;
+        }
+        kernel<<<ctas, TEAM, smem, stream>>>(p);
+        return cudaGetLastError();
+    };
+    if (wide && p.cols == TEAM * 8) return bias ? go(norm_backward_kernel<T, TEAM, true, true, true>) : go(norm_backward_kernel<T, TEAM, true, true, false>);
+    if (wide) return bias ? go(norm_backward_kernel<T, TEAM, true, false, true>) : go(norm_backward_kernel<T, TEAM, true, false, false>);
+    return bias ? go(norm_backward_kernel<T, TEAM, false, false, true>) : go(norm_backward_kernel<T, TEAM, false, false, false>);
 }
 template <typename T>
 static cudaError_t norm_bwd_any(const NormParams &p, const NormPlan &n, bool wide, bool sums, cudaStream_t stream) {
+    const bool bias = p.b_post || p.db_pre || p.db_post;
     cudaError_t e;
     switch (n.team) {
-        case 32: e = norm_bwd<T, 32, 1>(p, n.ctas, wide, stream); break;
-        case 64: e = norm_bwd<T, 64, 1>(p, n.ctas, wide, stream); break;
-        case 128: e = norm_bwd<T, 128, 1>(p, n.ctas, wide, stream); break;
-        case 256: e = norm_bwd<T, 256, 1>(p, n.ctas, wide, stream); break;
-        case 512: e = norm_bwd<T, 512, 1>(p, n.ctas, wide, stream); break;
-        default: e = norm_bwd<T, 1024, 1>(p, n.ctas, wide, stream); break;
+        case 32: e = norm_bwd<T, 32>(p, n.ctas, wide, bias, stream); break;
+        case 64: e = norm_bwd<T, 64>(p, n.ctas, wide, bias, stream); break;
+        case 128: e = norm_bwd<T, 128>(p, n.ctas, wide, bias, stream); break;
+        case 256: e = norm_bwd<T, 256>(p, n.ctas, wide, bias, stream); break;
+        case 512: e = norm_bwd<T, 512>(p, n.ctas, wide, bias, stream); break;
+        default: e = norm_bwd<T, 1024>(p, n.ctas, wide, bias, stream); break;
     }
     if (e != cudaSuccess || !sums) return e;
-    norm_sums_kernel<T><<<dim3((unsigned)((p.cols + 31) / 32), 4 + (p.dgate ? n.ctas : 0)), 256, 0, stream>>>(p, n.ctas);
+    const unsigned strips = (unsigned)((p.cols + 31) / 32);
+    const bool long_groups = p.gate_rows > kLongGroup * p.cta_rows;  // then there are at most CTAs / kLongGroup + 1 groups
+    unsigned gates = 0;
+    if (p.dgate) gates = (unsigned)(long_groups ? (p.rows + p.gate_rows - 1) / p.gate_rows : (n.ctas - 1 + 31) / 32);
+    norm_sums_kernel<T><<<dim3(strips, 4 + gates), kSumsThreads, 0, stream>>>(p, n.ctas, long_groups);
     return cudaGetLastError();
 }
 
@@ -701,6 +716,8 @@ egeria_status egeria_norm_backward(egeria_ops *ops, void *cuda_stream, const ege
     p.inv_cols = 1.0f / (float)a.cols;
     ops->last_stream = stream;
     const NormPlan n = norm_backward_plan(a.rows, a.cols);
+    p.cta_rows = a.rows / n.ctas;
+    p.extra = a.rows % n.ctas;
     const bool sums = a.dgate || a.dw_post || a.db_post || a.dw_pre || a.db_pre;
     EGO_CUDA(a.type == EGERIA_F32    ? norm_bwd_any<float>(p, n, wide, sums, stream)
              : a.type == EGERIA_BF16 ? norm_bwd_any<bf16>(p, n, wide, sums, stream)

@@ -92,6 +92,64 @@ __device__ __forceinline__ void store8(T *p, const float (&v)[8]) {
                  : "memory");
 }
 
+// Pairs of floats: one instruction for two products, sums or fused products of separately rounded values.
+struct F2 {
+    uint64_t v;
+};
+__device__ __forceinline__ F2 f2(float lo, float hi) {
+    F2 r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r.v) : "f"(lo), "f"(hi));
+    return r;
+}
+__device__ __forceinline__ F2 f2(float both) { return f2(both, both); }
+__device__ __forceinline__ float2 split(F2 a) {
+    float2 r;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(a.v));
+    return r;
+}
+__device__ __forceinline__ F2 operator*(F2 a, F2 b) {
+    F2 r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+    return r;
+}
+__device__ __forceinline__ F2 operator+(F2 a, F2 b) {
+    F2 r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+    return r;
+}
+__device__ __forceinline__ F2 fma2(F2 a, F2 b, F2 c) {
+    F2 r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
+    return r;
+}
+__device__ __forceinline__ float both(F2 a) {
+    const float2 f = split(a);
+    return f.x + f.y;
+}
+template <typename T>
+__device__ __forceinline__ void unpack8(F2 (&v)[4], const Raw8<T> &d) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float2 f = unpack2<T>(d.r[i]);
+        v[i] = f2(f.x, f.y);
+    }
+}
+__device__ __forceinline__ void unpack8(F2 (&v)[4], const Raw8<float> &d) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = f2(__uint_as_float(d.r[2 * i]), __uint_as_float(d.r[2 * i + 1]));
+}
+template <typename T>
+__device__ __forceinline__ void store8(T *p, const F2 (&v)[4]) {
+    float f[8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float2 q = split(v[i]);
+        f[2 * i] = q.x;
+        f[2 * i + 1] = q.y;
+    }
+    store8(p, f);
+}
+
 __device__ __forceinline__ float warp_sum(float v) {
 #pragma unroll
     for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);

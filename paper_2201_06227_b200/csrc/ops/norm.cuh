@@ -70,24 +70,25 @@ __device__ __forceinline__ void norm_load(Raw8<T> &d, const T *row, int t, int i
     }
 }
 template <typename T, int TEAM, bool WIDE, bool FULL>
-__device__ __forceinline__ void norm_store(T *row, const float (&v)[8], int t, int i, int cols) {
+__device__ __forceinline__ void norm_store(T *row, const F2 (&v)[4], int t, int i, int cols) {
     if (WIDE) {
         if (norm_in<TEAM, WIDE, FULL>(t, i, 0, cols)) store8(row + norm_col<TEAM, WIDE>(t, i, 0), v);
     } else {
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             const int c = norm_col<TEAM, WIDE>(t, i, j);
-            if (c < cols) row[c] = from_f32<T>(v[j]);
+            const float2 f = split(v[j / 2]);
+            if (c < cols) row[c] = from_f32<T>(j % 2 ? f.y : f.x);
         }
     }
 }
 // A vector of `cols` weights, biases or gates, of type float or T, or `absent` in each place; it stays in L1.
 // WIDE: aligned like a row.
 template <typename T, int TEAM, bool WIDE, bool FULL>
-__device__ __forceinline__ void norm_vector(float (&v)[8], const void *p, int64_t first, int is_float, int t, int i, int cols, float absent) {
+__device__ __forceinline__ void norm_vector(F2 (&v)[4], const void *p, int64_t first, int is_float, int t, int i, int cols, float absent) {
     if (!p) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = absent;
+        for (int j = 0; j < 4; ++j) v[j] = f2(absent);
     } else if (is_float) {
         Raw8<float> d;
         norm_load<float, TEAM, WIDE, FULL>(d, static_cast<const float *>(p) + first, t, i, cols);
@@ -99,27 +100,38 @@ __device__ __forceinline__ void norm_vector(float (&v)[8], const void *p, int64_
     }
 }
 
-// Sums over the team, the same bits in every thread.  `scratch`: 2 x N x 32 floats; `turn` alternates
+// Sums over the team of N = 1 or 2 values, the same bits in every thread.  `scratch`: 2 x 2 x 32 floats; `turn` alternates
 // between its halves, so that one barrier per reduction is enough.
 template <int TEAM, int N>
 __device__ __forceinline__ void team_sum(float (&v)[N], float *scratch, int &turn) {
-#pragma unroll
-    for (int n = 0; n < N; ++n) v[n] = warp_sum(v[n]);
-    if (TEAM == 32) return;
-    float *half = scratch + (turn & 1) * 32 * 2;
-    turn ^= 1;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    if (lane == 0) {
+    if (N == 2) {
+        // the half-warps take one value each
+        const bool upper = lane & 16;
+        float mine = upper ? v[1] : v[0];
+        mine += __shfl_xor_sync(0xffffffffu, upper ? v[0] : v[1], 16);
 #pragma unroll
-        for (int n = 0; n < N; ++n) half[n * 32 + warp] = v[n];
+        for (int o = 8; o; o >>= 1) mine += __shfl_xor_sync(0xffffffffu, mine, o);
+        if (TEAM == 32) {
+            v[0] = __shfl_sync(0xffffffffu, mine, 0);
+            v[1] = __shfl_sync(0xffffffffu, mine, 16);
+            return;
+        }
+        v[0] = mine;
+    } else {
+        v[0] = warp_sum(v[0]);
+        if (TEAM == 32) return;
     }
+    float *half = scratch + (turn & 1) * 64;
+    turn ^= 1;
+    if ((lane & (N == 2 ? 15 : 31)) == 0) half[(lane >> 4) * 32 + warp] = v[0];
     __syncthreads();
     if (TEAM <= 256) {
 #pragma unroll
         for (int n = 0; n < N; ++n) {
-            v[n] = 0.0f;
+            v[n] = half[n * 32];
 #pragma unroll
-            for (int w = 0; w < TEAM / 32; ++w) v[n] += half[n * 32 + w];
+            for (int w = 1; w < TEAM / 32; ++w) v[n] += half[n * 32 + w];
         }
     } else {
 #pragma unroll
@@ -129,27 +141,33 @@ __device__ __forceinline__ void team_sum(float (&v)[N], float *scratch, int &tur
 
 // Takes the mean off the row that the team holds in v (layer norm) and returns it and 1/deviation.
 template <int TEAM, int VPT, bool WIDE, bool FULL>
-__device__ __forceinline__ void norm_center(float (&v)[VPT][8], const NormParams &p, int t, float &mean, float &inv, float *scratch,
+__device__ __forceinline__ void norm_center(F2 (&v)[VPT][4], const NormParams &p, int t, float &mean, float &inv, float *scratch,
                                             int &turn) {
     mean = 0.0f;
     if (p.layer) {
-        float s[1] = {0.0f};
+        F2 s2 = f2(0.0f);
 #pragma unroll
         for (int i = 0; i < VPT; ++i)
 #pragma unroll
-            for (int j = 0; j < 8; ++j) s[0] += v[i][j];  // past the row's end there are zeros
+            for (int j = 0; j < 4; ++j) s2 = s2 + v[i][j];  // past the row's end there are zeros
+        float s[1] = {both(s2)};
         team_sum<TEAM>(s, scratch, turn);
         mean = s[0] * p.inv_cols;
 #pragma unroll
         for (int i = 0; i < VPT; ++i)
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[i][j] = norm_in<TEAM, WIDE, FULL>(t, i, j, p.cols) ? v[i][j] - mean : 0.0f;
+            for (int j = 0; j < 4; ++j) {
+                const float lo = norm_in<TEAM, WIDE, FULL>(t, i, 2 * j, p.cols) ? -mean : 0.0f;
+                const float hi = norm_in<TEAM, WIDE, FULL>(t, i, 2 * j + 1, p.cols) ? -mean : 0.0f;
+                v[i][j] = v[i][j] + f2(lo, hi);
+            }
     }
-    float q[1] = {0.0f};
+    F2 q2 = f2(0.0f);
 #pragma unroll
     for (int i = 0; i < VPT; ++i)
 #pragma unroll
-        for (int j = 0; j < 8; ++j) q[0] = fmaf(v[i][j], v[i][j], q[0]);
+        for (int j = 0; j < 4; ++j) q2 = fma2(v[i][j], v[i][j], q2);
+    float q[1] = {both(q2)};
     team_sum<TEAM>(q, scratch, turn);
     inv = rsqrtf(fmaf(q[0], p.inv_cols, p.eps));
 }
@@ -167,7 +185,7 @@ __global__ void __launch_bounds__(TEAM == 32 ? 128 : TEAM) norm_forward_kernel(c
         norm_load<T, TEAM, WIDE, FULL>(rf[i], static_cast<const T *>(p.f) + r * p.ldf, t, i, p.cols);
         norm_load<T, TEAM, WIDE, FULL>(rx[i], static_cast<const T *>(p.x) + r * p.ldx, t, i, p.cols);
     }
-    float f[VPT][8];
+    F2 f[VPT][4];
 #pragma unroll
     for (int i = 0; i < VPT; ++i) unpack8(f[i], rf[i]);
     float st[4] = {0.0f, 0.0f, 0.0f, 0.0f};
@@ -175,32 +193,32 @@ __global__ void __launch_bounds__(TEAM == 32 ? 128 : TEAM) norm_forward_kernel(c
     const int64_t gate = p.gate ? (r / p.gate_rows) * p.cols : 0;
 #pragma unroll
     for (int i = 0; i < VPT; ++i) {
-        float v[8], b[8];
+        F2 v[4], b[4];
         if (p.post) {
             norm_vector<T, TEAM, WIDE, FULL>(v, p.w_post, 0, p.w_float, t, i, p.cols, 1.0f);
             norm_vector<T, TEAM, WIDE, FULL>(b, p.b_post, 0, p.w_float, t, i, p.cols, 0.0f);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) f[i][j] = fmaf(f[i][j] * st[1], v[j], b[j]);
+            for (int j = 0; j < 4; ++j) f[i][j] = fma2(f[i][j] * f2(st[1]), v[j], b[j]);
         }
         if (p.gate) {
             norm_vector<T, TEAM, WIDE, FULL>(v, p.gate, gate, p.w_float, t, i, p.cols, 1.0f);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) f[i][j] *= v[j];
+            for (int j = 0; j < 4; ++j) f[i][j] = f[i][j] * v[j];
         }
         unpack8(v, rx[i]);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) f[i][j] = fmaf(p.alpha, v[j], f[i][j]);  // zeros stay past the row's end: all vectors are 0 there
+        for (int j = 0; j < 4; ++j) f[i][j] = fma2(f2(p.alpha), v[j], f[i][j]);  // zeros stay past the row's end: all vectors are 0 there
         norm_store<T, TEAM, WIDE, FULL>(static_cast<T *>(p.y) + r * p.ldy, f[i], t, i, p.cols);
     }
     if (p.pre) {
         norm_center<TEAM, VPT, WIDE, FULL>(f, p, t, st[2], st[3], scratch, turn);
 #pragma unroll
         for (int i = 0; i < VPT; ++i) {
-            float v[8], b[8];
+            F2 v[4], b[4];
             norm_vector<T, TEAM, WIDE, FULL>(v, p.w_pre, 0, p.w_float, t, i, p.cols, 1.0f);
             norm_vector<T, TEAM, WIDE, FULL>(b, p.b_pre, 0, p.w_float, t, i, p.cols, 0.0f);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) f[i][j] = fmaf(f[i][j] * st[3], v[j], b[j]);
+            for (int j = 0; j < 4; ++j) f[i][j] = fma2(f[i][j] * f2(st[3]), v[j], b[j]);
             norm_store<T, TEAM, WIDE, FULL>(static_cast<T *>(p.h) + r * p.ldh, f[i], t, i, p.cols);
         }
     }
@@ -254,8 +272,8 @@ __device__ __forceinline__ void copy_ahead(Raw8<T> *dst, const T *src, bool in) 
                      : "memory");
 }
 
-// BIAS: the norms have biases, whose sums are kept (a gradient that is not wanted is not written).
-template <typename T, int TEAM, bool WIDE, bool FULL, bool BIAS>
+// LAYER: layer norms, which have a mean, and norms with biases (a gradient that is not wanted is not written).
+template <typename T, int TEAM, bool WIDE, bool FULL, bool LAYER>
 __global__ void __launch_bounds__(TEAM, TEAM >= 512 ? 1 : 512 / TEAM) norm_backward_kernel(const NormParams p) {
     constexpr int kRows = norm_ring_rows<T, TEAM>();
     extern __shared__ __align__(16) uint8_t norm_smem[];
@@ -268,37 +286,50 @@ __global__ void __launch_bounds__(TEAM, TEAM >= 512 ? 1 : 512 / TEAM) norm_backw
     const bool in = norm_in<TEAM, WIDE, FULL>(t, 0, 0, p.cols);
     const int col = norm_col<TEAM, WIDE>(t, 0, 0);
 
-    auto fetch = [&](int64_t r, int slot) {
-        if (WIDE && r < r1) {
+    // this thread's place in each matrix, moved on from row to row
+    const int c0 = WIDE && in ? col : 0;
+    const T *dy = static_cast<const T *>(p.dy) + r0 * p.lddy + c0, *fr = static_cast<const T *>(p.f) + r0 * p.ldf + c0;
+    const T *dh = static_cast<const T *>(p.dh), *yr = static_cast<const T *>(p.x);
+    if (p.pre) {
+        dh += r0 * p.lddh + c0;
+        yr += r0 * p.ldx + c0;
+    }
+    T *dx = static_cast<T *>(p.y) + r0 * p.ldy, *df = static_cast<T *>(p.h) + r0 * p.ldh;
+    int64_t fetched = r0;
+    auto fetch = [&](int slot) {
+        if (WIDE && fetched < r1) {
             Raw8<T> *to = ring + (slot * 4) * TEAM + t;
-            const int c = in ? col : 0;
-            copy_ahead(to, static_cast<const T *>(p.dy) + r * p.lddy + c, in);
-            copy_ahead(to + TEAM, static_cast<const T *>(p.f) + r * p.ldf + c, in);
+            copy_ahead(to, dy, in);
+            copy_ahead(to + TEAM, fr, in);
+            dy += p.lddy;
+            fr += p.ldf;
             if (p.pre) {
-                copy_ahead(to + 2 * TEAM, static_cast<const T *>(p.dh) + r * p.lddh + c, in);
-                copy_ahead(to + 3 * TEAM, static_cast<const T *>(p.x) + r * p.ldx + c, in);
+                copy_ahead(to + 2 * TEAM, dh, in);
+                copy_ahead(to + 3 * TEAM, yr, in);
+                dh += p.lddh;
+                yr += p.ldx;
             }
+            ++fetched;
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
     };
 #pragma unroll
-    for (int k = 0; k < kRows - 1; ++k) fetch(r0 + k, k);
+    for (int k = 0; k < kRows - 1; ++k) fetch(k);
 
-    float w_pre[8], w_post[8], b_post[8], gate[8];
+    F2 w_pre[4], w_post[4], b_post[4], gate[4];
     norm_vector<T, TEAM, WIDE, FULL>(w_pre, p.w_pre, 0, p.w_float, t, 0, p.cols, 1.0f);
     norm_vector<T, TEAM, WIDE, FULL>(w_post, p.w_post, 0, p.w_float, t, 0, p.cols, 1.0f);
-    if (BIAS) norm_vector<T, TEAM, WIDE, FULL>(b_post, p.b_post, 0, p.w_float, t, 0, p.cols, 0.0f);
-    float sw_pre[8], sb_pre[8], sw_post[8], sb_post[8], sg[8];
+    if (LAYER) norm_vector<T, TEAM, WIDE, FULL>(b_post, p.b_post, 0, p.w_float, t, 0, p.cols, 0.0f);
+    F2 sw_pre[4], sb_pre[4], sw_post[4], sb_post[4], sg[4];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) sw_pre[j] = sb_pre[j] = sw_post[j] = sb_post[j] = sg[j] = 0.0f, gate[j] = 1.0f;
+    for (int j = 0; j < 4; ++j) sw_pre[j] = sb_pre[j] = sw_post[j] = sb_post[j] = sg[j] = f2(0.0f), gate[j] = f2(1.0f);
 
     int64_t group = 0, left = 0;  // the gate in force and how many of its rows are to come
     int slot = 0;
+    constexpr int kSums = LAYER ? 2 : 1;
+    float4 st_next = __ldg(reinterpret_cast<const float4 *>(p.stats + 4 * r0));
     for (int64_t r = r0; r < r1; ++r) {
-        {
-            const int ahead = slot + kRows - 1;
-            fetch(r + kRows - 1, ahead >= kRows ? ahead - kRows : ahead);
-        }
+        fetch(slot == 0 ? kRows - 1 : slot - 1);
         Raw8<T> ry, rdh, rdy, rf;
         if (WIDE) {
             asm volatile("cp.async.wait_group %0;" ::"n"(kRows - 1) : "memory");
@@ -308,67 +339,87 @@ __global__ void __launch_bounds__(TEAM, TEAM >= 512 ? 1 : 512 / TEAM) norm_backw
             if (p.pre) rdh = from[2 * TEAM], ry = from[3 * TEAM];
             slot = slot + 1 == kRows ? 0 : slot + 1;
         } else {
-            norm_load<T, TEAM, WIDE, FULL>(rdy, static_cast<const T *>(p.dy) + r * p.lddy, t, 0, p.cols);
-            norm_load<T, TEAM, WIDE, FULL>(rf, static_cast<const T *>(p.f) + r * p.ldf, t, 0, p.cols);
+            norm_load<T, TEAM, WIDE, FULL>(rdy, dy, t, 0, p.cols);
+            norm_load<T, TEAM, WIDE, FULL>(rf, fr, t, 0, p.cols);
+            dy += p.lddy;
+            fr += p.ldf;
             if (p.pre) {
-                norm_load<T, TEAM, WIDE, FULL>(rdh, static_cast<const T *>(p.dh) + r * p.lddh, t, 0, p.cols);
-                norm_load<T, TEAM, WIDE, FULL>(ry, static_cast<const T *>(p.x) + r * p.ldx, t, 0, p.cols);
+                norm_load<T, TEAM, WIDE, FULL>(rdh, dh, t, 0, p.cols);
+                norm_load<T, TEAM, WIDE, FULL>(ry, yr, t, 0, p.cols);
+                dh += p.lddh;
+                yr += p.ldx;
             }
         }
-        const float4 st = __ldg(reinterpret_cast<const float4 *>(p.stats + 4 * r));
+        const float4 st = st_next;
+        if (r + 1 < r1) st_next = __ldg(reinterpret_cast<const float4 *>(p.stats + 4 * (r + 1)));
         if (p.gate && left == 0) {
             group = r / p.gate_rows;
             left = min((group + 1) * p.gate_rows, p.rows) - r;
             norm_vector<T, TEAM, WIDE, FULL>(gate, p.gate, group * p.cols, p.w_float, t, 0, p.cols, 1.0f);
         }
-        float tot[8];
+        F2 tot[4];
         unpack8(tot, rdy);
         if (p.pre) {
-            float hat[8], d[8], s[2] = {0.0f, 0.0f};
+            F2 hat[4], d[4], s0 = f2(0.0f), s1 = f2(0.0f);
             unpack8(hat, ry);
             unpack8(d, rdh);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                hat[j] = (hat[j] - st.z) * st.w;
-                sw_pre[j] = fmaf(d[j], hat[j], sw_pre[j]);
-                if (BIAS) sb_pre[j] += d[j];
-                d[j] *= w_pre[j];
-                s[0] = fmaf(d[j], hat[j], s[0]);  // d is 0 past the row's end
-                s[1] += d[j];
+            for (int j = 0; j < 4; ++j) {
+                if (LAYER) hat[j] = hat[j] + f2(-st.z);
+                hat[j] = hat[j] * f2(st.w);
+                sw_pre[j] = fma2(d[j], hat[j], sw_pre[j]);
+                if (LAYER) sb_pre[j] = sb_pre[j] + d[j];
+                d[j] = d[j] * w_pre[j];
+                s0 = fma2(d[j], hat[j], s0);  // d is 0 past the row's end
+                if (LAYER) s1 = s1 + d[j];
             }
+            float s[kSums];
+            s[0] = both(s0);
+            if (LAYER) s[kSums - 1] = both(s1);
             team_sum<TEAM>(s, scratch, turn);
-            const float along = s[0] * p.inv_cols, lean = p.layer ? s[1] * p.inv_cols : 0.0f;
+            const F2 along = f2(-s[0] * p.inv_cols), lean = f2(p.layer ? -s[kSums - 1] * p.inv_cols : 0.0f), inv = f2(st.w);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) tot[j] = fmaf(st.w, fmaf(-hat[j], along, d[j] - lean), tot[j]);
+            for (int j = 0; j < 4; ++j) tot[j] = fma2(inv, fma2(hat[j], along, LAYER ? d[j] + lean : d[j]), tot[j]);
         }
         {
-            float v[8];
+            F2 v[4];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] = p.alpha * tot[j];
-            norm_store<T, TEAM, WIDE, FULL>(static_cast<T *>(p.y) + r * p.ldy, v, t, 0, p.cols);
+            for (int j = 0; j < 4; ++j) v[j] = f2(p.alpha) * tot[j];
+            norm_store<T, TEAM, WIDE, FULL>(dx, v, t, 0, p.cols);
+            dx += p.ldy;
         }
         // the branch f
-        float hat[8], d[8], s[2] = {0.0f, 0.0f};
+        F2 hat[4], d[4], s0 = f2(0.0f), s1 = f2(0.0f);
         unpack8(hat, rf);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            if (!norm_in<TEAM, WIDE, FULL>(t, 0, j, p.cols)) tot[j] = 0.0f;
-            if (p.post) hat[j] = (hat[j] - st.x) * st.y;
-            sg[j] = fmaf(tot[j], BIAS ? fmaf(hat[j], w_post[j], b_post[j]) : hat[j] * w_post[j], sg[j]);
+        for (int j = 0; j < 4; ++j) {
+            if (!FULL) {
+                const float2 q = split(tot[j]);
+                tot[j] = f2(norm_in<TEAM, WIDE, FULL>(t, 0, 2 * j, p.cols) ? q.x : 0.0f, norm_in<TEAM, WIDE, FULL>(t, 0, 2 * j + 1, p.cols) ? q.y : 0.0f);
+            }
+            if (p.post) {
+                if (LAYER) hat[j] = hat[j] + f2(-st.x);
+                hat[j] = hat[j] * f2(st.y);
+            }
+            sg[j] = fma2(tot[j], LAYER ? fma2(hat[j], w_post[j], b_post[j]) : hat[j] * w_post[j], sg[j]);
             d[j] = tot[j] * gate[j];
-            sw_post[j] = fmaf(d[j], hat[j], sw_post[j]);
-            if (BIAS) sb_post[j] += d[j];
-            d[j] *= w_post[j];
-            s[0] = fmaf(d[j], hat[j], s[0]);
-            s[1] += d[j];
+            sw_post[j] = fma2(d[j], hat[j], sw_post[j]);
+            if (LAYER) sb_post[j] = sb_post[j] + d[j];
+            d[j] = d[j] * w_post[j];
+            s0 = fma2(d[j], hat[j], s0);
+            if (LAYER) s1 = s1 + d[j];
         }
         if (p.post) {
+            float s[kSums];
+            s[0] = both(s0);
+            if (LAYER) s[kSums - 1] = both(s1);
             team_sum<TEAM>(s, scratch, turn);
-            const float along = s[0] * p.inv_cols, lean = p.layer ? s[1] * p.inv_cols : 0.0f;
+            const F2 along = f2(-s[0] * p.inv_cols), lean = f2(p.layer ? -s[kSums - 1] * p.inv_cols : 0.0f), inv = f2(st.y);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) d[j] = st.y * fmaf(-hat[j], along, d[j] - lean);
+            for (int j = 0; j < 4; ++j) d[j] = inv * fma2(hat[j], along, LAYER ? d[j] + lean : d[j]);
         }
-        norm_store<T, TEAM, WIDE, FULL>(static_cast<T *>(p.h) + r * p.ldh, d, t, 0, p.cols);
+        norm_store<T, TEAM, WIDE, FULL>(df, d, t, 0, p.cols);
+        df += p.ldh;
         // the gate's sums leave at the end of a group and at the end of the run
         if (p.gate && (--left == 0 || r + 1 == r1)) {
             const int64_t g0 = group * p.gate_rows, g1 = min(g0 + p.gate_rows, p.rows);
@@ -376,25 +427,28 @@ __global__ void __launch_bounds__(TEAM, TEAM >= 512 ? 1 : 512 / TEAM) norm_backw
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 const int c = norm_col<TEAM, WIDE>(t, 0, j);
+                const float v = j % 2 ? split(sg[j / 2]).y : split(sg[j / 2]).x;
                 if (c < p.cols) {
                     if (!whole)
-                        sums[(first ? 4 : 5) * (int64_t)p.cols + c] = sg[j];
+                        sums[(first ? 4 : 5) * (int64_t)p.cols + c] = v;
                     else if (p.dgate)
-                        store_param<T>(p.dgate, group * p.cols + c, sg[j], p.w_float);
+                        store_param<T>(p.dgate, group * p.cols + c, v, p.w_float);
                 }
-                sg[j] = 0.0f;
+                if (j % 2) sg[j / 2] = f2(0.0f);
             }
         }
     }
+    auto put = [&](int place, const F2(&v)[4]) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        const int c = norm_col<TEAM, WIDE>(t, 0, j);
-        if (c >= p.cols) continue;
-        if (p.dw_pre) sums[c] = sw_pre[j];
-        if (BIAS && p.db_pre) sums[(int64_t)p.cols + c] = sb_pre[j];
-        if (p.dw_post) sums[2 * (int64_t)p.cols + c] = sw_post[j];
-        if (BIAS && p.db_post) sums[3 * (int64_t)p.cols + c] = sb_post[j];
-    }
+        for (int j = 0; j < 8; ++j) {
+            const int c = norm_col<TEAM, WIDE>(t, 0, j);
+            if (c < p.cols) sums[place * (int64_t)p.cols + c] = j % 2 ? split(v[j / 2]).y : split(v[j / 2]).x;
+        }
+    };
+    if (p.dw_pre) put(0, sw_pre);
+    if (LAYER && p.db_pre) put(1, sb_pre);
+    if (p.dw_post) put(2, sw_post);
+    if (LAYER && p.db_post) put(3, sb_post);
 }
 
 // The sum over k = first..last of src[k * pitch], 32 columns per block (lane = column), the k dealt to the 32 warps;

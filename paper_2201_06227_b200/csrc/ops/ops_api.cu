@@ -341,12 +341,13 @@ template <typename T>
 static cudaError_t norm_fwd_any(const NormParams &p, bool wide, cudaStream_t stream) {
     if (p.cols <= 256) return norm_fwd<T, 32, 1>(p, wide, stream);
     if (p.cols <= 512) return norm_fwd<T, 32, 2>(p, wide, stream);
+    if (p.cols <= 768) return norm_fwd<T, 32, 3>(p, wide, stream);
     if (p.cols <= 1024) return norm_fwd<T, 32, 4>(p, wide, stream);
     if (p.cols <= 4096) return norm_fwd<T, 128, 4>(p, wide, stream);
     return norm_fwd<T, 256, 4>(p, wide, stream);
 }
 template <typename T, int TEAM>
-static cudaError_t norm_bwd(const NormParams &p, int ctas, bool wide, bool bias, cudaStream_t stream) {
+static cudaError_t norm_bwd(const NormParams &p, int ctas, bool wide, bool layer, cudaStream_t stream) {
     const size_t smem = wide ? (size_t)norm_ring_rows<T, TEAM>() * 4 * TEAM * sizeof(Raw8<T>) : 0;
     auto go = [&](auto kernel) {
         if (smem > 40 * 1024) {  // with the static part: beyond what needs no permission
@@ -356,21 +357,20 @@ static cudaError_t norm_bwd(const NormParams &p, int ctas, bool wide, bool bias,
         kernel<<<ctas, TEAM, smem, stream>>>(p);
         return cudaGetLastError();
     };
-    if (wide && p.cols == TEAM * 8) return bias ? go(norm_backward_kernel<T, TEAM, true, true, true>) : go(norm_backward_kernel<T, TEAM, true, true, false>);
-    if (wide) return bias ? go(norm_backward_kernel<T, TEAM, true, false, true>) : go(norm_backward_kernel<T, TEAM, true, false, false>);
-    return bias ? go(norm_backward_kernel<T, TEAM, false, false, true>) : go(norm_backward_kernel<T, TEAM, false, false, false>);
+    if (wide && p.cols == TEAM * 8) return layer ? go(norm_backward_kernel<T, TEAM, true, true, true>) : go(norm_backward_kernel<T, TEAM, true, true, false>);
+    if (wide) return layer ? go(norm_backward_kernel<T, TEAM, true, false, true>) : go(norm_backward_kernel<T, TEAM, true, false, false>);
+    return layer ? go(norm_backward_kernel<T, TEAM, false, false, true>) : go(norm_backward_kernel<T, TEAM, false, false, false>);
 }
 template <typename T>
-static cudaError_t norm_bwd_any(const NormParams &p, const NormPlan &n, bool wide, bool sums, cudaStream_t stream) {
-    const bool bias = p.b_post || p.db_pre || p.db_post;
+static cudaError_t norm_bwd_any(const NormParams &p, const NormPlan &n, bool wide, bool layer, bool sums, cudaStream_t stream) {
     cudaError_t e;
     switch (n.team) {
-        case 32: e = norm_bwd<T, 32>(p, n.ctas, wide, bias, stream); break;
-        case 64: e = norm_bwd<T, 64>(p, n.ctas, wide, bias, stream); break;
-        case 128: e = norm_bwd<T, 128>(p, n.ctas, wide, bias, stream); break;
-        case 256: e = norm_bwd<T, 256>(p, n.ctas, wide, bias, stream); break;
-        case 512: e = norm_bwd<T, 512>(p, n.ctas, wide, bias, stream); break;
-        default: e = norm_bwd<T, 1024>(p, n.ctas, wide, bias, stream); break;
+        case 32: e = norm_bwd<T, 32>(p, n.ctas, wide, layer, stream); break;
+        case 64: e = norm_bwd<T, 64>(p, n.ctas, wide, layer, stream); break;
+        case 128: e = norm_bwd<T, 128>(p, n.ctas, wide, layer, stream); break;
+        case 256: e = norm_bwd<T, 256>(p, n.ctas, wide, layer, stream); break;
+        case 512: e = norm_bwd<T, 512>(p, n.ctas, wide, layer, stream); break;
+        default: e = norm_bwd<T, 1024>(p, n.ctas, wide, layer, stream); break;
     }
     if (e != cudaSuccess || !sums) return e;
     const unsigned strips = (unsigned)((p.cols + 31) / 32);
@@ -715,13 +715,14 @@ egeria_status egeria_norm_backward(egeria_ops *ops, void *cuda_stream, const ege
     p.alpha = a.alpha;
     p.inv_cols = 1.0f / (float)a.cols;
     ops->last_stream = stream;
+    const bool layer = p.layer || p.b_post || p.db_pre || p.db_post;  // an rms norm with biases goes with the layer norms
     const NormPlan n = norm_backward_plan(a.rows, a.cols);
     p.cta_rows = a.rows / n.ctas;
     p.extra = a.rows % n.ctas;
     const bool sums = a.dgate || a.dw_post || a.db_post || a.dw_pre || a.db_pre;
-    EGO_CUDA(a.type == EGERIA_F32    ? norm_bwd_any<float>(p, n, wide, sums, stream)
-             : a.type == EGERIA_BF16 ? norm_bwd_any<bf16>(p, n, wide, sums, stream)
-                                     : norm_bwd_any<f16>(p, n, wide, sums, stream));
+    EGO_CUDA(a.type == EGERIA_F32    ? norm_bwd_any<float>(p, n, wide, layer, sums, stream)
+             : a.type == EGERIA_BF16 ? norm_bwd_any<bf16>(p, n, wide, layer, sums, stream)
+                                     : norm_bwd_any<f16>(p, n, wide, layer, sums, stream));
     ops->launches += sums ? 2 : 1;
     return EGERIA_OK;
 }

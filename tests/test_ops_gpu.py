@@ -428,6 +428,12 @@ def test_norm_parts(post, pre, kind, affine):
         check_norm(o, s, kind, post, pre, gate_rows, alpha, torch.bfloat16)
 
 
+def test_norm_rms_with_biases():
+    o = ops.Ops(ops.egeria_norm_workspace_bytes(60, 136), DEV)
+    s = norm_inputs(60, 136, torch.float16, torch.float16, "layer", True, True, 9, True, seed=4)
+    check_norm(o, s, "rms", True, True, 9, 1.0, torch.float16)
+
+
 @pytest.mark.parametrize("gate_rows", [1, 2, 3, 17, 256, 999, 1000, 5000])
 @pytest.mark.parametrize("rows", [999, 4000])
 def test_norm_gate_groups(rows, gate_rows):

@@ -17,6 +17,7 @@
 // code 0: that would divide a moment by eps alone.
 #pragma once
 #include "../check.cuh"
+#include "../ptx_sm100.cuh"
 #include "common.cuh"
 
 namespace egeria {
@@ -229,6 +230,8 @@ __device__ __forceinline__ void adam_narrow(const AdamStep &s, const AdamTensor 
 
 template <typename P, typename G, bool MASTER, bool SMALL>
 __global__ void __launch_bounds__(kAdamThreads) adamw_kernel(const AdamParams a) {
+    ptx::grid_dependency_wait();
+    ptx::grid_launch_dependents();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const float gscale = a.grad_scale ? *a.grad_scale : 1.0f;
     const bool skip_all = !(fabsf(gscale) <= 3.402823466e38f);  // not finite: the whole step is left out

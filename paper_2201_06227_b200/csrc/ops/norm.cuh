@@ -13,6 +13,7 @@
 #pragma once
 #include <string.h>
 
+#include "../ptx_sm100.cuh"
 #include "common.cuh"
 
 namespace egeria {
@@ -175,6 +176,8 @@ __device__ __forceinline__ void norm_center(F2 (&v)[VPT][4], const NormParams &p
 template <typename T, int TEAM, int VPT, bool WIDE, bool FULL>
 __global__ void __launch_bounds__(TEAM == 32 ? 128 : TEAM) norm_forward_kernel(const NormParams p) {
     __shared__ float scratch[2 * 32 * 2];
+    ptx::grid_dependency_wait();
+    ptx::grid_launch_dependents();
     int turn = 0;
     const int t = TEAM == 32 ? (threadIdx.x & 31) : threadIdx.x;
     const int64_t r = TEAM == 32 ? (int64_t)blockIdx.x * 4 + (threadIdx.x >> 5) : blockIdx.x;
@@ -279,6 +282,8 @@ __global__ void __launch_bounds__(TEAM, TEAM >= 512 ? 1 : 512 / TEAM) norm_backw
     extern __shared__ __align__(16) uint8_t norm_smem[];
     __shared__ float scratch[2 * 32 * 2];
     Raw8<T> *ring = reinterpret_cast<Raw8<T> *>(norm_smem);  // [kRows][4][TEAM]
+    ptx::grid_dependency_wait();
+    ptx::grid_launch_dependents();
     int turn = 0;
     const int t = threadIdx.x;
     const int64_t r0 = norm_first_row(p, blockIdx.x), r1 = norm_first_row(p, blockIdx.x + 1);
@@ -327,7 +332,7 @@ __global__ void __launch_bounds__(TEAM, TEAM >= 512 ? 1 : 512 / TEAM) norm_backw
     int64_t group = 0, left = 0;  // the gate in force and how many of its rows are to come
     int slot = 0;
     constexpr int kSums = LAYER ? 2 : 1;
-    float4 st_next = __ldg(reinterpret_cast<const float4 *>(p.stats + 4 * r0));
+    float4 st_next = *reinterpret_cast<const float4 *>(p.stats + 4 * r0);
     for (int64_t r = r0; r < r1; ++r) {
         fetch(slot == 0 ? kRows - 1 : slot - 1);
         Raw8<T> ry, rdh, rdy, rf;
@@ -351,7 +356,7 @@ __global__ void __launch_bounds__(TEAM, TEAM >= 512 ? 1 : 512 / TEAM) norm_backw
             }
         }
         const float4 st = st_next;
-        if (r + 1 < r1) st_next = __ldg(reinterpret_cast<const float4 *>(p.stats + 4 * (r + 1)));
+        if (r + 1 < r1) st_next = *reinterpret_cast<const float4 *>(p.stats + 4 * (r + 1));
         if (p.gate && left == 0) {
             group = r / p.gate_rows;
             left = min((group + 1) * p.gate_rows, p.rows) - r;
@@ -486,6 +491,8 @@ constexpr int kLongGroup = 32;
 template <typename T>
 __global__ void __launch_bounds__(kSumsThreads) norm_sums_kernel(const NormParams p, int n, int long_groups) {
     __shared__ float part[32][33];
+    ptx::grid_dependency_wait();
+    ptx::grid_launch_dependents();
     const int c = blockIdx.x * 32 + (threadIdx.x & 31), cc = min(c, p.cols - 1);
     const bool writes = threadIdx.x < 32 && c < p.cols;
     const int64_t pitch = (int64_t)kNormSums * p.cols;

@@ -37,6 +37,26 @@ constexpr uint64_t kWaitLimitNs = 2000000000ull;
 constexpr int64_t kMaxSize = ((int64_t)1 << 31) - 1024;  // tile coordinates are 32-bit
 constexpr int kSms = 148;                                // what workspaces are sized for
 
+// Every kernel is launched as a programmatic dependent of the one before it in the stream: its blocks may take their
+// places while that one's last blocks are running, and each waits for it (griddepcontrol.wait) before it touches memory.
+template <typename... Params, typename... Args>
+static cudaError_t launch(void (*kernel)(Params...), dim3 grid, int threads, size_t smem, cudaStream_t stream, int cluster, const Args &...args) {
+    cudaLaunchConfig_t c{};
+    c.gridDim = grid;
+    c.blockDim = dim3(threads);
+    c.dynamicSmemBytes = smem;
+    c.stream = stream;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = cluster;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    c.attrs = attr;
+    c.numAttrs = cluster > 1 ? 2 : 1;
+    return cudaLaunchKernelEx(&c, kernel, args...);
+}
+
 static size_t up(size_t v, size_t a) { return (v + a - 1) / a * a; }
 static int64_t pad8(int64_t v) { return (v + 7) / 8 * 8; }
 static bool aligned(const void *p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
@@ -62,23 +82,31 @@ static double gemm_cycles(const GemmPlan &g, int64_t kblocks, int sms) {
     return t;
 }
 
-static GemmPlan plan_gemm(int64_t m, int64_t n, int64_t k, int sms) {
+// The best split of the sum for one kind of tile.
+static GemmPlan plan_tile(int64_t m, int64_t n, int64_t k, int sms, int bn, int cg) {
     const int64_t kblocks = (k + kGemmK - 1) / kGemmK;
+    GemmPlan g{bn, cg, 1, (int)((m + 128 * cg - 1) / (128 * cg)), (int)((n + bn - 1) / bn)}, best = g;
+    const int64_t tiles = (int64_t)g.tiles_m * g.tiles_n;
+    double best_t = gemm_cycles(g, kblocks, sms);
+    const int64_t most = std::min<int64_t>(std::min<int64_t>(64, kblocks), std::min(sms, kMaxSplitCtas) / (tiles * cg));
+    for (g.splits = 2; g.splits <= most; ++g.splits) {
+        const double t = gemm_cycles(g, kblocks, sms);
+        if (t < best_t) best_t = t, best = g;
+    }
+    return best;
+}
+static GemmPlan plan_gemm(int64_t m, int64_t n, int64_t k, int sms) {
     GemmPlan best{};
     double best_t = 1e300;
     for (int cg = 1; cg <= 2; ++cg)
-        for (int bn = 64; bn <= 256; bn *= 2) {
-            if (cg == 2 && bn == 64) continue;
-            GemmPlan g{bn, cg, 1, (int)((m + 128 * cg - 1) / (128 * cg)), (int)((n + bn - 1) / bn)};
-            const int64_t tiles = (int64_t)g.tiles_m * g.tiles_n;
-            for (g.splits = 1; g.splits <= 64 && g.splits <= kblocks; ++g.splits) {
-                if (g.splits > 1 && (tiles * g.splits * cg > std::min(sms, kMaxSplitCtas) || tiles * cg * kGemmEpiWarps > kMaxTickets)) break;
-                const double t = gemm_cycles(g, kblocks, sms);
-                if (t < best_t) best_t = t, best = g;
-            }
+        for (int bn = cg == 2 ? 128 : 64; bn <= 256; bn *= 2) {
+            const GemmPlan g = plan_tile(m, n, k, sms, bn, cg);
+            const double t = gemm_cycles(g, (k + kGemmK - 1) / kGemmK, sms);
+            if (t < best_t) best_t = t, best = g;
         }
     return best;
 }
+static_assert(2 * kMaxSplitCtas * kEpiWarps <= kMaxTickets, "a ticket for every warp of every split tile of two products");
 
 // Bytes of partial tiles that a product of these sizes may need under any plan.
 static size_t split_bytes(int64_t m, int64_t n, int64_t k) {
@@ -89,14 +117,14 @@ static size_t split_bytes(int64_t m, int64_t n, int64_t k) {
     return (size_t)std::min<int64_t>(tiles * kblocks, kMaxSplitCtas) * 128 * 256 * 4;
 }
 
-constexpr int kSlopeChunks = 592;  // partial rows of a column sum at most: four CTAs per SM
-static int slope_chunks(int64_t rows, int64_t cols) {
+// Runs of rows that dz and its column sums are cut into: four blocks per SM at most, 32 rows at least.
+static int slope_runs(int64_t rows, int64_t cols) {
     const int64_t strips = (cols + 255) / 256;
-    return (int)std::max<int64_t>(1, std::min<int64_t>((rows + 31) / 32, std::max<int64_t>(1, kSlopeChunks / strips)));
+    return (int)std::max<int64_t>(1, std::min<int64_t>((rows + 31) / 32, 4 * kSms / strips));
 }
 
 struct LinearLayout {
-    size_t part, x, w, dz, sums, total;
+    size_t part, part2, x, w, dz, sums, total;
 };
 static LinearLayout linear_layout(int64_t rows, int64_t inp, int64_t out) {
     LinearLayout L;
@@ -106,11 +134,12 @@ static LinearLayout linear_layout(int64_t rows, int64_t inp, int64_t out) {
         off = up(off + n, 1024);
         return at;
     };
-    L.part = take(std::max(std::max(split_bytes(rows, out, inp), split_bytes(rows, inp, out)), split_bytes(out, inp, rows)));
+    L.part = take(std::max(split_bytes(rows, out, inp), split_bytes(out, inp, rows)));  // z, or dw
+    L.part2 = take(split_bytes(rows, inp, out));                                        // dx, in one launch with dw
     L.x = take((size_t)rows * pad8(inp) * 2);
     L.w = take((size_t)out * pad8(inp) * 2);
     L.dz = take((size_t)rows * pad8(out) * 2);
-    L.sums = take((size_t)slope_chunks(rows, out) * out * 4);
+    L.sums = take((size_t)slope_runs(rows, out) * out * 4);
     L.total = off;
     return L;
 }
@@ -153,6 +182,7 @@ static cudaError_t allow_smem() {
     return cudaFuncSetAttribute(gemm_kernel<T, BN, CG>, cudaFuncAttributeMaxDynamicSharedMemorySize, GemmCfg<BN, CG>::kSmem);
 }
 constexpr int kFewSmem = 96 * 1024;
+constexpr int kFewRows = 4;   // rows that go without the tensor cores
 template <typename T, int ROWS>
 static cudaError_t allow_few() {
     cudaError_t e = cudaFuncSetAttribute(linear_few_kernel<T, ROWS, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, kFewSmem);
@@ -170,7 +200,6 @@ static cudaError_t allow_all() {
     if (e == cudaSuccess) e = allow_few<T, 1>();
     if (e == cudaSuccess) e = allow_few<T, 2>();
     if (e == cudaSuccess) e = allow_few<T, 4>();
-    if (e == cudaSuccess) e = allow_few<T, 8>();
     return e;
 }
 
@@ -193,126 +222,141 @@ static egeria_status encode_operand(const egeria_ops *o, CUtensorMap *map, const
 
 template <typename T, int BN, int CG>
 static cudaError_t launch_gemm(const GemmParams &p, int ctas, cudaStream_t stream) {
-    cudaLaunchConfig_t c{};
-    c.gridDim = dim3(ctas);
-    c.blockDim = dim3(kGemmThreads);
-    c.dynamicSmemBytes = GemmCfg<BN, CG>::kSmem;
-    c.stream = stream;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = CG;
-    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
-    c.attrs = attr;
-    c.numAttrs = CG > 1 ? 1 : 0;
-    return cudaLaunchKernelEx(&c, gemm_kernel<T, BN, CG>, p);
+    return launch(gemm_kernel<T, BN, CG>, dim3(ctas), GemmCfg<BN, CG>::kThreads, GemmCfg<BN, CG>::kSmem, stream, CG, p);
 }
 template <typename T>
-static cudaError_t launch_gemm_any(const GemmPlan &g, const GemmParams &p, int ctas, cudaStream_t stream) {
-    if (g.cg == 2) return g.bn == 128 ? launch_gemm<T, 128, 2>(p, ctas, stream) : launch_gemm<T, 256, 2>(p, ctas, stream);
-    if (g.bn == 64) return launch_gemm<T, 64, 1>(p, ctas, stream);
-    return g.bn == 128 ? launch_gemm<T, 128, 1>(p, ctas, stream) : launch_gemm<T, 256, 1>(p, ctas, stream);
+static cudaError_t launch_gemm_any(int bn, int cg, const GemmParams &p, int ctas, cudaStream_t stream) {
+    if (cg == 2) return bn == 128 ? launch_gemm<T, 128, 2>(p, ctas, stream) : launch_gemm<T, 256, 2>(p, ctas, stream);
+    if (bn == 64) return launch_gemm<T, 64, 1>(p, ctas, stream);
+    return bn == 128 ? launch_gemm<T, 128, 1>(p, ctas, stream) : launch_gemm<T, 256, 1>(p, ctas, stream);
 }
 
 // Widest access that all of a product's epilogue matrices take: 2 = 32 bytes, 1 = 16 bytes, 0 = one value.
-static int epilogue_width(const GemmParams &p) {
+static void set_widths(Epilogue &e) {
     int w = 2;
     auto see = [&](const void *q, int64_t ld) {
         if (!q) return;
         if (!aligned(q, 32) || ld % 16) w = std::min(w, aligned(q, 16) && ld % 8 == 0 ? 1 : 0);
     };
-    see(p.out, p.ldo);
-    see(p.z, p.ldz);
-    see(p.residual, p.ldr);
-    see(p.z_in, p.ldz_in);
-    return w;
+    see(e.out, e.ldo);
+    see(e.z, e.ldz);
+    see(e.extra, e.ldx);
+    e.wide = w;
+    e.wide_bias = aligned(e.bias, 16);
 }
 
-// D = A B^T with the epilogue that `p` already describes; k = the length of the summed axis.
-static egeria_status run_gemm(egeria_ops *o, cudaStream_t stream, int type, int64_t m, int64_t n, int64_t k, const Operand &a,
-                              const Operand &b, size_t part_off, GemmParams &p) {
-    const GemmPlan g = plan_gemm(m, n, k, o->sms);
-    if (g.splits > 1 && (size_t)g.tiles_m * g.tiles_n * g.splits * g.cg * 128 * g.bn * 4 > split_bytes(m, n, k)) return EGERIA_ERR_WORKSPACE;
-    egeria_status s = encode_operand(o, &p.a, a, type, kGemmM);
-    if (s == EGERIA_OK) s = encode_operand(o, &p.b, b, type, g.bn / g.cg);
-    if (s != EGERIA_OK) return s;
-    p.m = (int32_t)m;
-    p.n = (int32_t)n;
-    p.kblocks = (int32_t)((k + kGemmK - 1) / kGemmK);
-    p.tiles_m = g.tiles_m;
-    p.tiles_n = g.tiles_n;
-    p.splits = g.splits;
-    // a strip of B of at most 16 MB, so that it stays in L2 next to the rows of A that go by
-    p.group_n = (int32_t)std::max<int64_t>(1, std::min<int64_t>(g.tiles_n, ((int64_t)16 << 20) / (2 * k * g.bn)));
-    p.a_mn = a.mn;
-    p.b_mn = b.mn;
+// One product D = A B^T of a launch; k = the length of the summed axis.
+struct Product {
+    int64_t m, n, k;
+    Operand a, b;
+    Epilogue epi;
+    size_t part;    // its partial tiles in the workspace
+};
+
+static egeria_status run_products(egeria_ops *o, cudaStream_t stream, int type, Product *jobs, int count, const ColumnSums &sums) {
+    // the tile that suits the launch: of the plans of each product, the one that is best for all of them
+    GemmPlan plan[2];
+    double best = 1e300;
+    for (int i = 0; i < count; ++i) {
+        const GemmPlan lead = plan_gemm(jobs[i].m, jobs[i].n, jobs[i].k, o->sms);
+        GemmPlan g[2];
+        double t = 0.0;
+        for (int j = 0; j < count; ++j) {
+            g[j] = j == i ? lead : plan_tile(jobs[j].m, jobs[j].n, jobs[j].k, o->sms, lead.bn, lead.cg);
+            t += gemm_cycles(g[j], (jobs[j].k + kGemmK - 1) / kGemmK, o->sms);
+        }
+        if (t < best) {
+            best = t;
+            for (int j = 0; j < count; ++j) plan[j] = g[j];
+        }
+    }
+    const int bn = plan[0].bn, cg = plan[0].cg, workers = o->sms / cg;
+    GemmParams p;
+    memset(&p, 0, sizeof(p));
+    int64_t units = 0;
+    for (int i = 0; i < count; ++i) {
+        const Product &j = jobs[i];
+        const GemmPlan &g = plan[i];
+        GemmProblem &q = p.problem[i];
+        if (g.splits > 1 && (size_t)g.tiles_m * g.tiles_n * g.splits * cg * 128 * bn * 4 > split_bytes(j.m, j.n, j.k)) return EGERIA_ERR_WORKSPACE;
+        egeria_status s = encode_operand(o, &q.a, j.a, type, kGemmM);
+        if (s == EGERIA_OK) s = encode_operand(o, &q.b, j.b, type, bn / cg);
+        if (s != EGERIA_OK) return s;
+        q.m = (int32_t)j.m;
+        q.n = (int32_t)j.n;
+        q.kblocks = (int32_t)((j.k + kGemmK - 1) / kGemmK);
+        q.tiles_m = g.tiles_m;
+        q.tiles_n = g.tiles_n;
+        q.splits = g.splits;
+        const int64_t n_units = (int64_t)g.tiles_m * g.tiles_n * g.splits;
+        if (n_units > 0x3fffffff) return EGERIA_ERR_UNSUPPORTED_SHAPE;
+        q.units = (int32_t)n_units;
+        units += n_units;
+        // a strip of B of at most 16 MB, so that it stays in L2 next to the rows of A that go by
+        q.group_n = (int32_t)std::max<int64_t>(1, std::min<int64_t>(g.tiles_n, ((int64_t)16 << 20) / (2 * j.k * bn)));
+        q.a_mn = j.a.mn;
+        q.b_mn = j.b.mn;
+        q.epi = j.epi;
+        set_widths(q.epi);
+        q.partials = reinterpret_cast<float *>(o->ws + j.part);
+        q.tickets = reinterpret_cast<int32_t *>(o->ws + kTicketOff) + i * (kMaxTickets / 2);
+    }
+    const int used = (int)std::min<int64_t>(units, workers);
+    if (count == 2) {
+        // the workers without a last unit of the first product have its time for units of the second
+        const int left = p.problem[0].units % used;
+        if (left) p.fill = (p.problem[0].kblocks / p.problem[0].splits) / std::max(1, p.problem[1].kblocks / p.problem[1].splits);
+        p.fill = std::min<int64_t>(p.fill, p.problem[1].units / used + 1);
+    }
+    p.sums = sums;
     p.is_f16 = type == EGERIA_F16;
-    p.wide = epilogue_width(p);
-    p.partials = reinterpret_cast<float *>(o->ws + part_off);
-    p.tickets = reinterpret_cast<int32_t *>(o->ws + kTicketOff);
     p.status = reinterpret_cast<int32_t *>(o->ws);
     p.wait_limit_ns = kWaitLimitNs;
-    const int64_t units = (int64_t)g.tiles_m * g.tiles_n * g.splits;
-    if (units > 0x7fffffff) return EGERIA_ERR_UNSUPPORTED_SHAPE;
-    const int ctas = (int)std::min<int64_t>(units, o->sms / g.cg) * g.cg;
-    EGO_CUDA(type == EGERIA_BF16 ? launch_gemm_any<bf16>(g, p, ctas, stream) : launch_gemm_any<f16>(g, p, ctas, stream));
+    const int ctas = used * cg;
+    EGO_CUDA(type == EGERIA_BF16 ? launch_gemm_any<bf16>(bn, cg, p, ctas, stream) : launch_gemm_any<f16>(bn, cg, p, ctas, stream));
     ++o->launches;
     return EGERIA_OK;
 }
 
-// The operand as a tile load takes it: itself, or its copy at `spare` with a pitch of pad8(cols).
-static egeria_status loadable(egeria_ops *o, cudaStream_t stream, Operand &a, size_t spare) {
-    if (aligned(a.p, 16) && a.ld % 8 == 0) return EGERIA_OK;
-    uint16_t *dst = reinterpret_cast<uint16_t *>(o->ws + spare);
-    const int64_t pitch = pad8(a.cols);
-    const dim3 grid((unsigned)((a.cols + 255) / 256), (unsigned)std::min<int64_t>(a.rows, 16384));
-    pack_kernel<<<grid, 256, 0, stream>>>(dst, pitch, static_cast<const uint16_t *>(a.p), a.ld, a.rows, a.cols);
-    EGO_CUDA(cudaGetLastError());
+// The operand as a tile load takes it: itself, or the copy that `job` makes of it at `spare` with a pitch of pad8(cols).
+static void make_loadable(egeria_ops *o, Operand &a, size_t spare, PackJob &job) {
+    if (aligned(a.p, 16) && a.ld % 8 == 0) return;
+    job.src = static_cast<const uint16_t *>(a.p);
+    job.dst = reinterpret_cast<uint16_t *>(o->ws + spare);
+    job.ld = a.ld;
+    job.pitch = pad8(a.cols);
+    job.rows = a.rows;
+    job.cols = a.cols;
+    job.strips = (int32_t)((a.cols + 255) / 256);
+    job.blocks = job.strips * (int32_t)std::max<int64_t>(1, std::min<int64_t>((a.rows + 7) / 8, 8 * kSms / job.strips));
+    a.p = job.dst;
+    a.ld = job.pitch;
+}
+
+static egeria_status run_prepare(egeria_ops *o, cudaStream_t stream, int type, const PrepareParams &p, bool wide) {
+    const int64_t blocks = (int64_t)p.slope.strips * p.slope.runs + p.pack[0].blocks + p.pack[1].blocks;
+    if (blocks == 0) return EGERIA_OK;
+    if (blocks > 0x7fffffff) return EGERIA_ERR_UNSUPPORTED_SHAPE;
+    auto go = [&](auto kernel) { return launch(kernel, dim3((unsigned)blocks), 32 * kPrepareWarps, 0, stream, 1, p); };
+    EGO_CUDA(type == EGERIA_BF16 ? (wide ? go(prepare_kernel<bf16, true>) : go(prepare_kernel<bf16, false>))
+                                 : (wide ? go(prepare_kernel<f16, true>) : go(prepare_kernel<f16, false>)));
     ++o->launches;
-    a.p = dst;
-    a.ld = pitch;
     return EGERIA_OK;
 }
 
 template <typename T, int ROWS>
-static cudaError_t launch_few(const GemmParams &p, const egeria_linear_forward_args &a, bool wide, int sms, cudaStream_t stream) {
+static cudaError_t launch_few(const Epilogue &e, const egeria_linear_forward_args &a, bool wide, int sms, cudaStream_t stream) {
     const int smem = ROWS * (int)((a.inp + 255) / 256 * 256) * 2;
     const int grid = (int)std::min<int64_t>((a.out + 7) / 8, (int64_t)sms * 4);
     const T *x = static_cast<const T *>(a.x), *w = static_cast<const T *>(a.w);
-    if (wide)
-        linear_few_kernel<T, ROWS, true><<<grid, 256, smem, stream>>>(p, x, a.ldx, w, a.ldw, (int32_t)a.inp);
-    else
-        linear_few_kernel<T, ROWS, false><<<grid, 256, smem, stream>>>(p, x, a.ldx, w, a.ldw, (int32_t)a.inp);
-    return cudaGetLastError();
+    return launch(wide ? linear_few_kernel<T, ROWS, true> : linear_few_kernel<T, ROWS, false>, dim3(grid), 256, smem, stream, 1, e,
+                  (int32_t)a.rows, (int32_t)a.out, x, a.ldx, w, a.ldw, (int32_t)a.inp);
 }
 template <typename T>
-static cudaError_t launch_few_any(const GemmParams &p, const egeria_linear_forward_args &a, bool wide, int sms, cudaStream_t stream) {
-    if (a.rows <= 1) return launch_few<T, 1>(p, a, wide, sms, stream);
-    if (a.rows <= 2) return launch_few<T, 2>(p, a, wide, sms, stream);
-    if (a.rows <= 4) return launch_few<T, 4>(p, a, wide, sms, stream);
-    return launch_few<T, 8>(p, a, wide, sms, stream);
-}
-
-// dz (or null) and the column sums db (or null) of dy * act'(z).
-template <typename T>
-static egeria_status run_slope(egeria_ops *o, cudaStream_t stream, const egeria_linear_backward_args &a, T *dz, int64_t lddz, size_t sums_off) {
-    const T *z = a.act == EGERIA_ACT_NONE ? nullptr : static_cast<const T *>(a.z);
-    const bool wide = a.out % 8 == 0 && aligned(a.dy, 16) && a.lddy % 8 == 0 && (!z || (aligned(z, 16) && a.ldz % 8 == 0)) && (z || !dz);
-    const int chunks = slope_chunks(a.rows, a.out);
-    float *sums = a.db ? reinterpret_cast<float *>(o->ws + sums_off) : nullptr;
-    const dim3 grid((unsigned)((a.out + 255) / 256), (unsigned)chunks);
-    const T *dy = static_cast<const T *>(a.dy);
-    if (wide)
-        slope_kernel<T, true><<<grid, 32 * kSlopeWarps, 0, stream>>>(dz, lddz, sums, dy, a.lddy, z, a.ldz, a.act, a.rows, (int32_t)a.out);
-    else
-        slope_kernel<T, false><<<grid, 32 * kSlopeWarps, 0, stream>>>(dz, lddz, sums, dy, a.lddy, z, a.ldz, a.act, a.rows, (int32_t)a.out);
-    EGO_CUDA(cudaGetLastError());
-    ++o->launches;
-    if (a.db) {
-        add_rows_kernel<T><<<(unsigned)((a.out + 31) / 32), 256, 0, stream>>>(static_cast<T *>(a.db), sums, chunks, (int32_t)a.out);
-        EGO_CUDA(cudaGetLastError());
-        ++o->launches;
-    }
-    return EGERIA_OK;
+static cudaError_t launch_few_any(const Epilogue &e, const egeria_linear_forward_args &a, bool wide, int sms, cudaStream_t stream) {
+    if (a.rows <= 1) return launch_few<T, 1>(e, a, wide, sms, stream);
+    if (a.rows <= 2) return launch_few<T, 2>(e, a, wide, sms, stream);
+    return launch_few<T, 4>(e, a, wide, sms, stream);
 }
 
 static bool good_matrix(const void *p, int64_t ld, int64_t cols, size_t elem) { return p && aligned(p, elem) && ld >= cols; }
@@ -329,13 +373,9 @@ static cudaError_t norm_fwd(const NormParams &p, bool wide, cudaStream_t stream)
     const int64_t per = TEAM == 32 ? 4 : 1;
     const unsigned grid = (unsigned)((p.rows + per - 1) / per);
     const int threads = TEAM == 32 ? 128 : TEAM;
-    if (wide && p.cols == TEAM * VPT * 8)
-        norm_forward_kernel<T, TEAM, VPT, true, true><<<grid, threads, 0, stream>>>(p);
-    else if (wide)
-        norm_forward_kernel<T, TEAM, VPT, true, false><<<grid, threads, 0, stream>>>(p);
-    else
-        norm_forward_kernel<T, TEAM, VPT, false, false><<<grid, threads, 0, stream>>>(p);
-    return cudaGetLastError();
+    auto go = [&](auto kernel) { return launch(kernel, dim3(grid), threads, 0, stream, 1, p); };
+    if (wide && p.cols == TEAM * VPT * 8) return go(norm_forward_kernel<T, TEAM, VPT, true, true>);
+    return wide ? go(norm_forward_kernel<T, TEAM, VPT, true, false>) : go(norm_forward_kernel<T, TEAM, VPT, false, false>);
 }
 template <typename T>
 static cudaError_t norm_fwd_any(const NormParams &p, bool wide, cudaStream_t stream) {
@@ -354,8 +394,7 @@ static cudaError_t norm_bwd(const NormParams &p, int ctas, bool wide, bool layer
             const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
             if (e != cudaSuccess) return e;
         }
-        kernel<<<ctas, TEAM, smem, stream>>>(p);
-        return cudaGetLastError();
+        return launch(kernel, dim3(ctas), TEAM, smem, stream, 1, p);
     };
     if (wide && p.cols == TEAM * 8) return layer ? go(norm_backward_kernel<T, TEAM, true, true, true>) : go(norm_backward_kernel<T, TEAM, true, true, false>);
     if (wide) return layer ? go(norm_backward_kernel<T, TEAM, true, false, true>) : go(norm_backward_kernel<T, TEAM, true, false, false>);
@@ -377,8 +416,7 @@ static cudaError_t norm_bwd_any(const NormParams &p, const NormPlan &n, bool wid
     const bool long_groups = p.gate_rows > kLongGroup * p.cta_rows;  // then there are at most CTAs / kLongGroup + 1 groups
     unsigned gates = 0;
     if (p.dgate) gates = (unsigned)(long_groups ? (p.rows + p.gate_rows - 1) / p.gate_rows : (n.ctas - 1 + 31) / 32);
-    norm_sums_kernel<T><<<dim3(strips, 4 + gates), kSumsThreads, 0, stream>>>(p, n.ctas, long_groups);
-    return cudaGetLastError();
+    return launch(norm_sums_kernel<T>, dim3(strips, 4 + gates), kSumsThreads, 0, stream, 1, p, n.ctas, (int)long_groups);
 }
 
 static egeria_status device_ready(int *sms) {
@@ -519,28 +557,28 @@ egeria_status egeria_linear_forward(egeria_ops *ops, void *cuda_stream, const eg
     if (ops->ws_bytes < L.total) return EGERIA_ERR_WORKSPACE;
     cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
     ops->last_stream = stream;
-    GemmParams p;
-    memset(&p, 0, sizeof(p));
-    p.bias = a.bias;
-    p.residual = a.residual;
-    p.ldr = a.ldr;
-    p.out = a.y;
-    p.ldo = a.ldy;
-    p.z = a.z;
-    p.ldz = a.ldz;
-    p.act = a.act;
-    const int few_rows = a.rows <= 1 ? 1 : a.rows <= 2 ? 2 : a.rows <= 4 ? 4 : 8;
-    if (a.rows <= 8 && (a.inp + 255) / 256 * 256 * 2 * few_rows <= kFewSmem) {
-        p.m = (int32_t)a.rows;
-        p.n = (int32_t)a.out;
+    Epilogue e{};
+    e.bias = a.bias;
+    e.extra = a.residual;
+    e.ldx = a.ldr;
+    e.out = a.y;
+    e.ldo = a.ldy;
+    e.z = a.z;
+    e.ldz = a.ldz;
+    e.act = a.act;
+    const int few_rows = a.rows <= 2 ? (int)a.rows : 4;
+    if (a.rows <= kFewRows && (a.inp + 255) / 256 * 256 * 2 * few_rows <= kFewSmem) {
         const bool wide = a.inp % 8 == 0 && a.ldw % 8 == 0 && aligned(a.w, 16);
-        EGO_CUDA(a.type == EGERIA_BF16 ? launch_few_any<bf16>(p, a, wide, ops->sms, stream) : launch_few_any<f16>(p, a, wide, ops->sms, stream));
+        EGO_CUDA(a.type == EGERIA_BF16 ? launch_few_any<bf16>(e, a, wide, ops->sms, stream) : launch_few_any<f16>(e, a, wide, ops->sms, stream));
         ++ops->launches;
         return EGERIA_OK;
     }
-    Operand x{a.x, a.ldx, a.rows, a.inp, false}, w{a.w, a.ldw, a.out, a.inp, false};
-    if ((s = loadable(ops, stream, x, L.x)) != EGERIA_OK || (s = loadable(ops, stream, w, L.w)) != EGERIA_OK) return s;
-    return run_gemm(ops, stream, a.type, a.rows, a.out, a.inp, x, w, L.part, p);
+    PrepareParams prep{};
+    Product job{a.rows, a.out, a.inp, {a.x, a.ldx, a.rows, a.inp, false}, {a.w, a.ldw, a.out, a.inp, false}, e, L.part};
+    make_loadable(ops, job.a, L.x, prep.pack[0]);
+    make_loadable(ops, job.b, L.w, prep.pack[1]);
+    if ((s = run_prepare(ops, stream, a.type, prep, false)) != EGERIA_OK) return s;
+    return run_products(ops, stream, a.type, &job, 1, ColumnSums{});
 }
 
 egeria_status egeria_linear_backward(egeria_ops *ops, void *cuda_stream, const egeria_linear_backward_args *args) {
@@ -573,35 +611,58 @@ egeria_status egeria_linear_backward(egeria_ops *ops, void *cuda_stream, const e
         dz.p = ops->ws + L.dz;
         dz.ld = pad8(a.out);
     }
+    PrepareParams prep{};
+    ColumnSums sums{};
+    bool wide = false;
     if (own_dz || a.db) {
-        void *to = own_dz ? ops->ws + L.dz : nullptr;
-        s = a.type == EGERIA_BF16 ? run_slope<bf16>(ops, stream, a, static_cast<bf16 *>(to), dz.ld, L.sums)
-                                  : run_slope<f16>(ops, stream, a, static_cast<f16 *>(to), dz.ld, L.sums);
-        if (s != EGERIA_OK) return s;
+        SlopeJob &j = prep.slope;
+        j.dz = own_dz ? ops->ws + L.dz : nullptr;
+        j.lddz = dz.ld;
+        j.dy = a.dy;
+        j.lddy = a.lddy;
+        j.z = a.act == EGERIA_ACT_NONE ? nullptr : a.z;
+        j.ldz = a.ldz;
+        j.act = a.act;
+        j.rows = a.rows;
+        j.cols = (int32_t)a.out;
+        j.strips = (int32_t)((a.out + 255) / 256);
+        j.runs = slope_runs(a.rows, a.out);
+        j.db = a.db;
+        if (a.db) {
+            j.sums = reinterpret_cast<float *>(ops->ws + L.sums);
+            if (j.runs > 1) sums = ColumnSums{j.sums, a.db, j.runs, j.cols};
+        }
+        wide = a.out % 8 == 0 && aligned(a.dy, 16) && a.lddy % 8 == 0 && (!j.z || (aligned(j.z, 16) && a.ldz % 8 == 0));
+    }
+    Product jobs[2];
+    int count = 0;
+    if (a.dw) {  // first: its sums are the longer ones as a rule, and dx's tiles fill what it leaves
+        Operand dzt = dz;
+        dzt.mn = true;
+        Product &j = jobs[count++] = Product{a.out, a.inp, a.rows, dzt, {a.x, a.ldx, a.rows, a.inp, true}, {}, L.part};
+        j.epi.out = a.dw;
+        j.epi.ldo = a.lddw;
+        make_loadable(ops, j.b, L.x, prep.pack[0]);
     }
     if (a.dx) {
-        Operand w{a.w, a.ldw, a.out, a.inp, true};
-        if ((s = loadable(ops, stream, w, L.w)) != EGERIA_OK) return s;
-        GemmParams p;
-        memset(&p, 0, sizeof(p));
-        p.out = a.dx;
-        p.ldo = a.lddx;
+        Product &j = jobs[count++] = Product{a.rows, a.inp, a.out, dz, {a.w, a.ldw, a.out, a.inp, true}, {}, L.part2};
+        j.epi.out = a.dx;
+        j.epi.ldo = a.lddx;
         if (a.act_in != EGERIA_ACT_NONE) {
-            p.z_in = a.z_in;
-            p.ldz_in = a.ldz_in;
-            p.act_in = a.act_in;
+            j.epi.extra = a.z_in;
+            j.epi.ldx = a.ldz_in;
+            j.epi.act_in = a.act_in;
+            j.epi.slope = 1;
         }
-        if ((s = run_gemm(ops, stream, a.type, a.rows, a.inp, a.out, dz, w, L.part, p)) != EGERIA_OK) return s;
+        make_loadable(ops, j.b, L.w, prep.pack[1]);
     }
-    if (a.dw) {
-        Operand x{a.x, a.ldx, a.rows, a.inp, true};
-        if ((s = loadable(ops, stream, x, L.x)) != EGERIA_OK) return s;
-        dz.mn = true;
-        GemmParams p;
-        memset(&p, 0, sizeof(p));
-        p.out = a.dw;
-        p.ldo = a.lddw;
-        if ((s = run_gemm(ops, stream, a.type, a.out, a.inp, a.rows, dz, x, L.part, p)) != EGERIA_OK) return s;
+    if ((s = run_prepare(ops, stream, a.type, prep, wide)) != EGERIA_OK) return s;
+    if (count) return run_products(ops, stream, a.type, jobs, count, sums);
+    if (sums.out) {
+        const dim3 grid((unsigned)((a.out + 31) / 32));
+        EGO_CUDA(a.type == EGERIA_BF16 ? launch(add_columns_kernel<bf16>, grid, 512, 0, stream, 1, sums)
+                                       : launch(add_columns_kernel<f16>, grid, 512, 0, stream, 1, sums));
+        ++ops->launches;
     }
     return EGERIA_OK;
 }
@@ -846,8 +907,7 @@ egeria_status egeria_adamw_step(egeria_adamw *adamw, void *cuda_stream, double l
         p.rest1 = (float)(1.0 - beta1), p.rest2 = (float)(1.0 - beta2);
         p.eps = (float)eps;
         p.ln_beta1 = std::log(beta1), p.ln_beta2 = std::log(beta2);
-        c.kernel<<<c.grid, kAdamThreads, 0, stream>>>(p);
-        EGO_CUDA(cudaGetLastError());
+        EGO_CUDA(launch(c.kernel, dim3(c.grid), kAdamThreads, 0, stream, 1, p));
         ++adamw->launches;
     }
     return EGERIA_OK;

@@ -10,6 +10,8 @@ from pathlib import Path
 HERE = Path(__file__).resolve().parent
 CSRC = HERE / "csrc"
 LIB = HERE / "libegeria.so"
+BINDING = HERE / "_ops_python.so"             # the operators' calls from Python (csrc/ops/ops_python.cpp)
+BINDING_SOURCE = CSRC / "ops" / "ops_python.cpp"
 LIB_CHECKED = HERE / "libegeria_checked.so"   # the same sources with -DEGERIA_CHECKED (csrc/check.cuh)
 SOURCES = [CSRC / "egeria_api.cu", CSRC / "ops" / "ops_api.cu"]
 HEADERS = [*sorted(CSRC.rglob("*.cuh")), *sorted(CSRC.glob("*.h")), *sorted((HERE.parent / "include").glob("*.h"))]
@@ -24,7 +26,7 @@ def stale(lib: Path = LIB) -> bool:
     if not lib.exists():
         return True
     t = lib.stat().st_mtime
-    return any(p.stat().st_mtime > t for p in SOURCES + HEADERS)
+    return any(p.stat().st_mtime > t for p in ([BINDING_SOURCE] if lib == BINDING else SOURCES) + HEADERS)
 
 
 def _compile(lib: Path, extra, verbose: bool) -> None:
@@ -39,12 +41,31 @@ def _compile(lib: Path, extra, verbose: bool) -> None:
     os.replace(tmp, lib)
 
 
+def _compile_binding(verbose: bool) -> None:
+    import sysconfig
+
+    import torch
+    from torch.utils import cpp_extension
+    tmp = BINDING.with_suffix(f".so.tmp{os.getpid()}")
+    cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-shared", "-fPIC", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch.compiled_with_cxx11_abi())}",
+           *(f"-I{p}" for p in [*cpp_extension.include_paths(), sysconfig.get_paths()["include"]]), "-o", str(tmp), str(BINDING_SOURCE),
+           *(f"-L{p}" for p in cpp_extension.library_paths()), "-lc10", "-ltorch_cpu", "-ltorch", "-ltorch_python"]
+    res = subprocess.run(cmd, capture_output=True, text=True)
+    if verbose or res.returncode != 0:
+        sys.stderr.write(res.stdout + res.stderr)
+    if res.returncode != 0:
+        raise RuntimeError(f"building {BINDING.name} failed")
+    os.replace(tmp, BINDING)
+
+
 def build(force: bool = False, verbose: bool = False, checked: bool = True) -> Path:
-    """Build libegeria.so (and, unless checked=False, libegeria_checked.so) if missing or older than
-    the sources.  Raises on failure."""
+    """Build libegeria.so and _ops_python.so (and, unless checked=False, libegeria_checked.so) if missing or
+    older than the sources.  Raises on failure."""
     wanted = [(LIB, [])] + ([(LIB_CHECKED, ["-DEGERIA_CHECKED"])] if checked else [])
     with ThreadPoolExecutor() as pool:
         jobs = [pool.submit(_compile, lib, extra, verbose) for lib, extra in wanted if force or stale(lib)]
+        if force or stale(BINDING):
+            jobs.append(pool.submit(_compile_binding, verbose))
     for job in jobs:
         job.result()
     return LIB
@@ -54,3 +75,4 @@ if __name__ == "__main__":
     build(force="--force" in sys.argv, verbose=True)
     print(LIB)
     print(LIB_CHECKED)
+    print(BINDING)

@@ -12,7 +12,8 @@ are recorded on it (their memory is not reused before the call has run).
 from __future__ import annotations
 
 import ctypes
-import struct
+import importlib.util
+from pathlib import Path
 from typing import Optional, Sequence
 
 import torch
@@ -38,38 +39,28 @@ EXPORTS = [
 ]
 
 _vp, _i32, _i64, _f32 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_float
-_CODES = {_i32: "i", _i64: "q", _vp: "Q", _f32: "f"}
-
-
-def _fields(*groups):
-    """(field, type) pairs of a C struct from (type, "field field ...") groups in order."""
-    return [(f, t) for t, names in groups for f in names.split()]
-
-
-_LINEAR_FORWARD = _fields((_i32, "type act"), (_i64, "rows inp out"), (_vp, "x w bias residual"), (_i64, "ldx ldw ldr"),
-                          (_vp, "y z"), (_i64, "ldy ldz"))
-_LINEAR_BACKWARD = _fields((_i32, "type act act_in"), (_i64, "rows inp out"), (_vp, "dy x w z z_in"),
-                           (_i64, "lddy ldx ldw ldz ldz_in"), (_vp, "dx dw db"), (_i64, "lddx lddw"))
-_NORM_FORWARD = _fields((_i32, "type param_type kind post pre"), (_f32, "alpha eps"), (_i64, "rows cols gate_rows"),
-                        (_vp, "x f gate w_post b_post w_pre b_pre"), (_i64, "ldx ldf"), (_vp, "y h"), (_i64, "ldy ldh"), (_vp, "stats"))
-_NORM_BACKWARD = _fields((_i32, "type param_type kind post pre"), (_f32, "alpha"), (_i64, "rows cols gate_rows"),
-                         (_vp, "dy dh y f gate w_post b_post w_pre b_pre"), (_i64, "lddy lddh ldy ldf"), (_vp, "stats dx df"),
-                         (_i64, "lddx lddf"), (_vp, "dgate dw_post db_post dw_pre db_pre"))
 
 
 class _AdamTensor(ctypes.Structure):
-    _fields_ = _fields((_vp, "param master m v m_scale v_scale"), (_i64, "n"), (_i32, "param_type grad_type"), (_f32, "weight_decay"),
-                       (_i32, "module"))
+    _fields_ = [(f, t) for t, names in ((_vp, "param master m v m_scale v_scale"), (_i64, "n"), (_i32, "param_type grad_type"),
+                                        (_f32, "weight_decay"), (_i32, "module")) for f in names.split()]
 
 
-def _packer(fields):
-    """Packs the values of a struct's fields, in order, as a C compiler lays them out (a call through it costs a
-    fraction of filling in a ctypes structure)."""
-    return struct.Struct("@" + "".join(_CODES[t] for _, t in fields)).pack
+_calls = None
 
 
-_pack_linear_forward, _pack_linear_backward = _packer(_LINEAR_FORWARD), _packer(_LINEAR_BACKWARD)
-_pack_norm_forward, _pack_norm_backward = _packer(_NORM_FORWARD), _packer(_NORM_BACKWARD)
+def _native():
+    """The extension module that marshals the calls (it needs torch's libraries, which `import torch` has loaded)."""
+    global _calls
+    if _calls is None:
+        path = Path(__file__).resolve().parent / "_ops_python.so"
+        if not path.exists():
+            raise ImportError(f"{path} is missing: build it with `python -m paper_2201_06227_b200.build`")
+        spec = importlib.util.spec_from_file_location("_ops_python", path)
+        _calls = importlib.util.module_from_spec(spec)
+        spec.loader.exec_module(_calls)
+    return _calls
+
 
 _ready = None
 
@@ -90,12 +81,7 @@ def lib() -> ctypes.CDLL:
                  "egeria_adamw_device_status", "egeria_adamw_launch_count"):
         getattr(L, name).argtypes = [_vp]
     L.egeria_ops_launch_count.restype = L.egeria_adamw_launch_count.restype = _i64
-    L.egeria_linear_forward.argtypes = [_vp, _vp, ctypes.c_char_p]
-    L.egeria_linear_backward.argtypes = [_vp, _vp, ctypes.c_char_p]
-    L.egeria_norm_forward.argtypes = [_vp, _vp, ctypes.c_char_p]
-    L.egeria_norm_backward.argtypes = [_vp, _vp, ctypes.c_char_p]
     L.egeria_adamw_set_grads.argtypes = [_vp, _vp, ctypes.POINTER(_vp)]
-    L.egeria_adamw_step.argtypes = [_vp, _vp] + [ctypes.c_double] * 4 + [_vp, _vp]
     _ready = L
     return L
 
@@ -136,37 +122,6 @@ class _On:
         return self.context.__exit__(*exc)
 
 
-class _Here:
-    """The current stream of the current device, the ordinary case: nothing to enter or to leave."""
-
-    def __init__(self, index: int):
-        self.index = index
-
-    def __enter__(self):
-        return torch._C._cuda_getCurrentRawStream(self.index)
-
-    def __exit__(self, *exc):
-        return False
-
-
-def _matrix(t: torch.Tensor, name: str, device: int, dtype, rows: int, cols: int):
-    """(pointer, pitch) of a matrix whose rows are consecutive."""
-    if t.dtype is not dtype or t.get_device() != device or t.shape != (rows, cols):
-        raise ValueError(f"{name}: expected {dtype} [{rows}, {cols}] on cuda:{device}, got {t.dtype} {list(t.shape)} on {t.device}")
-    pitch, step = t.stride()
-    if step != 1 and cols > 1:
-        raise ValueError(f"{name}: the values of a row have to be consecutive")
-    if rows <= 1:
-        pitch = cols
-    elif pitch < cols:
-        raise ValueError(f"{name}: rows overlap")
-    return t.data_ptr(), pitch
-
-
-def _optional(t: Optional[torch.Tensor], *args):
-    return (0, 0) if t is None else _matrix(t, *args)
-
-
 def _vector(t: Optional[torch.Tensor], name: str, device: int, dtype, n: int) -> int:
     if t is None:
         return 0
@@ -178,10 +133,22 @@ def _vector(t: Optional[torch.Tensor], name: str, device: int, dtype, n: int) ->
 class _Handle:
     """A library object on one device, with its workspace."""
 
-    def _on(self, stream, *tensors):
+    def _call(self, name, native, stream, args):
+        """One call through the extension: its results, or EgeriaError."""
+        entry = self._entry.get(name)
+        if entry is None:
+            entry = self._entry[name] = ctypes.cast(getattr(self._lib, name), _vp).value
         if stream is None and torch._C._cuda_getDevice() == self._index:
-            return self._here
-        return _On(self.device, stream, (self._raw, *tensors))
+            got = native(entry, self._h.value, self._index, torch._C._cuda_getCurrentRawStream(self._index), *args)
+        else:
+            with _On(self.device, stream, (self._raw, *self._touched(), *(a for a in args if isinstance(a, torch.Tensor)))) as s:
+                got = native(entry, self._h.value, self._index, s, *args)
+        if got.__class__ is int and got:
+            _check(got, name)
+        return got
+
+    def _touched(self):
+        return ()
 
     def _place(self, device) -> None:
         self.device = torch.device(device)
@@ -190,7 +157,7 @@ class _Handle:
         if self.device.index is None:
             self.device = torch.device("cuda", torch.cuda.current_device())
         self._index = self.device.index
-        self._here = _Here(self._index)
+        self._entry = {}
 
     def close(self) -> None:
         if getattr(self, "_h", None):
@@ -215,7 +182,7 @@ class Ops(_Handle):
         L = lib()
         with torch.cuda.device(self.device):
             _check(L.egeria_ops_create(ctypes.byref(handle), ptr, self.workspace_bytes), "egeria_ops_create")
-        self._h, self._lib, self._destroy = handle, L, L.egeria_ops_destroy
+        self._h, self._lib, self._destroy, self._native = handle, L, L.egeria_ops_destroy, _native()
 
     # ------------------------------------------------------------------ linear layers
     def egeria_linear_forward(self, x: torch.Tensor, w: torch.Tensor, bias: Optional[torch.Tensor] = None, act: str = "none",
@@ -225,26 +192,7 @@ class Ops(_Handle):
         save_z, z the argument of the activation.  `out` may be the residual."""
         if act not in ACTS:
             raise ValueError(f"unknown activation {act!r}")
-        if x.dim() != 2 or w.dim() != 2:
-            raise ValueError("x and w are matrices")
-        (rows, inp), n = x.shape, w.shape[0]
-        dev, t, z, pz = self._index, x.dtype, None, (0, 0)
-        px, pw = _matrix(x, "x", dev, t, rows, inp), _matrix(w, "w", dev, t, n, inp)
-        pb, pr = _vector(bias, "bias", dev, t, n), _optional(residual, "residual", dev, t, rows, n)
-        with self._on(stream, x, w, bias, residual, out) as s:
-            if out is None:
-                y = x.new_empty((rows, n))
-                py = (y.data_ptr(), n)
-            else:
-                y, py = out, _matrix(out, "out", dev, t, rows, n)
-            if save_z:
-                z = x.new_empty((rows, n))
-                pz = (z.data_ptr(), n)
-            st = self._lib.egeria_linear_forward(self._h, s, _pack_linear_forward(
-                TYPES.get(t, -1), ACTS[act], rows, inp, n, px[0], pw[0], pb, pr[0], px[1], pw[1], pr[1], py[0], pz[0], py[1], pz[1]))
-        if st:
-            _check(st, "egeria_linear_forward")
-        return (y, z) if save_z else y
+        return self._call("egeria_linear_forward", self._native.linear_forward, stream, (x, w, bias, ACTS[act], residual, save_z, out))
 
     def egeria_linear_backward(self, dy: torch.Tensor, x: Optional[torch.Tensor], w: Optional[torch.Tensor],
                                z: Optional[torch.Tensor] = None, act: str = "none", z_in: Optional[torch.Tensor] = None,
@@ -255,66 +203,20 @@ class Ops(_Handle):
         z_in, x having come out of act_in(z_in)."""
         if act not in ACTS or act_in not in ACTS:
             raise ValueError(f"unknown activation {act!r} or {act_in!r}")
-        if dy.dim() != 2 or (need_dx and w is None) or (need_dw and x is None) or (x is None and w is None):
-            raise ValueError("dy is a matrix; dx needs w, dw needs x, and one of the two has to be there")
-        rows, n = dy.shape
-        inp = x.shape[-1] if x is not None else w.shape[-1]
-        dev, t, dx, dw, db = self._index, dy.dtype, None, None, None
-        pdy, px, pw = _matrix(dy, "dy", dev, t, rows, n), _optional(x, "x", dev, t, rows, inp), _optional(w, "w", dev, t, n, inp)
-        pz, pzi = _optional(z, "z", dev, t, rows, n), _optional(z_in, "z_in", dev, t, rows, inp)
-        with self._on(stream, dy, x, w, z, z_in) as s:
-            if need_dx:
-                dx = dy.new_empty((rows, inp))
-            if need_dw:
-                dw = dy.new_empty((n, inp))
-            if need_db:
-                db = dy.new_empty(n)
-            st = self._lib.egeria_linear_backward(self._h, s, _pack_linear_backward(
-                TYPES.get(t, -1), ACTS[act], ACTS[act_in], rows, inp, n, pdy[0], px[0], pw[0], pz[0], pzi[0], pdy[1], px[1], pw[1], pz[1],
-                pzi[1], dx.data_ptr() if need_dx else 0, dw.data_ptr() if need_dw else 0, db.data_ptr() if need_db else 0, inp, inp))
-        if st:
-            _check(st, "egeria_linear_backward")
-        return dx, dw, db
+        return self._call("egeria_linear_backward", self._native.linear_backward, stream,
+                          (dy, x, w, z, ACTS[act], z_in, ACTS[act_in], need_dx, need_dw, need_db))
 
     # ------------------------------------------------------------------ residual norms
-    def _norm_params(self, dtype, rows, cols, gate, gate_rows, w_post, b_post, w_pre, b_pre, kind):
-        """(type code of the parameters, their five pointers), checked."""
-        if kind not in KINDS:
-            raise ValueError(f"unknown norm {kind!r}")
-        pt = dtype
-        for v in (gate, w_post, b_post, w_pre, b_pre):
-            if v is not None:
-                pt = v.dtype
-                break
-        dev = self._index
-        groups = 1 if gate_rows == 0 else -(-rows // gate_rows) if gate_rows > 0 else 0
-        return (TYPES.get(pt, -1), _vector(gate, "gate", dev, pt, groups * cols), _vector(w_post, "w_post", dev, pt, cols),
-                _vector(b_post, "b_post", dev, pt, cols), _vector(w_pre, "w_pre", dev, pt, cols), _vector(b_pre, "b_pre", dev, pt, cols))
-
     def egeria_norm_forward(self, x: torch.Tensor, f: torch.Tensor, gate: Optional[torch.Tensor] = None, gate_rows: int = 0,
                             w_post: Optional[torch.Tensor] = None, b_post: Optional[torch.Tensor] = None,
                             w_pre: Optional[torch.Tensor] = None, b_pre: Optional[torch.Tensor] = None, kind: str = "layer",
                             post: bool = True, pre: bool = True, alpha: float = 1.0, eps: float = 1e-5,
                             stream: Optional[torch.cuda.Stream] = None):
         """(y, h, stats): y = alpha x + gate * N_post(f), h = N_pre(y) (None without pre), stats for the backward call."""
-        if x.dim() != 2:
-            raise ValueError("x is a matrix")
-        rows, cols = x.shape
-        dev, t, h, ph = self._index, x.dtype, None, 0
-        pt, *vectors = self._norm_params(t, rows, cols, gate, gate_rows, w_post, b_post, w_pre, b_pre, kind)
-        px, pf = _matrix(x, "x", dev, t, rows, cols), _matrix(f, "f", dev, t, rows, cols)
-        with self._on(stream, x, f, gate, w_post, b_post, w_pre, b_pre) as s:
-            y = x.new_empty((rows, cols))
-            if pre:
-                h = x.new_empty((rows, cols))
-                ph = h.data_ptr()
-            stats = x.new_empty((rows, 4), dtype=torch.float32)
-            st = self._lib.egeria_norm_forward(self._h, s, _pack_norm_forward(
-                TYPES.get(t, -1), pt, KINDS[kind], bool(post), bool(pre), alpha, eps, rows, cols, gate_rows, px[0], pf[0], *vectors,
-                px[1], pf[1], y.data_ptr(), ph, cols, cols, stats.data_ptr()))
-        if st:
-            _check(st, "egeria_norm_forward")
-        return y, h, stats
+        if kind not in KINDS:
+            raise ValueError(f"unknown norm {kind!r}")
+        return self._call("egeria_norm_forward", self._native.norm_forward, stream,
+                          (x, f, gate, w_post, b_post, w_pre, b_pre, gate_rows, KINDS[kind], post, pre, alpha, eps))
 
     def egeria_norm_backward(self, dy: torch.Tensor, dh: Optional[torch.Tensor], y: torch.Tensor, f: torch.Tensor,
                              stats: torch.Tensor, gate: Optional[torch.Tensor] = None, gate_rows: int = 0,
@@ -324,27 +226,11 @@ class Ops(_Handle):
                              stream: Optional[torch.cuda.Stream] = None):
         """The gradients as a dict: dx, df, and for what is given (and with need_params) dgate, dw_post, db_post, dw_pre,
         db_pre, else None."""
-        if dy.dim() != 2:
-            raise ValueError("dy is a matrix")
-        rows, cols = dy.shape
-        dev, t = self._index, dy.dtype
-        pt, *vectors = self._norm_params(t, rows, cols, gate, gate_rows, w_post, b_post, w_pre, b_pre, kind)
-        pdy, pdh = _matrix(dy, "dy", dev, t, rows, cols), _optional(dh, "dh", dev, t, rows, cols)
-        py, pf = _matrix(y, "y", dev, t, rows, cols), _matrix(f, "f", dev, t, rows, cols)
-        ps = _vector(stats, "stats", dev, torch.float32, 4 * rows)
-        with self._on(stream, dy, dh, y, f, stats, gate, w_post, b_post, w_pre, b_pre) as s:
-            out = dict(dx=dy.new_empty((rows, cols)), df=dy.new_empty((rows, cols)))
-            sums = []
-            for name, v, there in (("dgate", gate, True), ("dw_post", w_post, post), ("db_post", b_post, post),
-                                   ("dw_pre", w_pre, pre), ("db_pre", b_pre, pre)):
-                out[name] = torch.empty_like(v) if v is not None and there and need_params else None
-                sums.append(0 if out[name] is None else out[name].data_ptr())
-            st = self._lib.egeria_norm_backward(self._h, s, _pack_norm_backward(
-                TYPES.get(t, -1), pt, KINDS[kind], bool(post), bool(pre), alpha, rows, cols, gate_rows, pdy[0], pdh[0], py[0], pf[0],
-                *vectors, pdy[1], pdh[1], py[1], pf[1], ps, out["dx"].data_ptr(), out["df"].data_ptr(), cols, cols, *sums))
-        if st:
-            _check(st, "egeria_norm_backward")
-        return out
+        if kind not in KINDS:
+            raise ValueError(f"unknown norm {kind!r}")
+        got = self._call("egeria_norm_backward", self._native.norm_backward, stream,
+                         (dy, dh, y, f, stats, gate, w_post, b_post, w_pre, b_pre, gate_rows, KINDS[kind], post, pre, alpha, need_params))
+        return dict(zip(("dx", "df", "dgate", "dw_post", "db_post", "dw_pre", "db_pre"), got))
 
     def egeria_ops_device_status(self) -> int:
         return int(lib().egeria_ops_device_status(self._h))
@@ -412,7 +298,7 @@ class AdamW(_Handle):
             _check(lib().egeria_adamw_create(ctypes.byref(handle), n, table, self._grad_pointers(grads),
                                              _vector(steps, "steps", dev, torch.int32, n), ptr, nbytes, flags),
                    "egeria_adamw_create")
-        self._h, self._lib, self._destroy = handle, lib(), lib().egeria_adamw_destroy
+        self._h, self._lib, self._destroy, self._native = handle, lib(), lib().egeria_adamw_destroy, _native()
         self._last_module = max(self.modules)
 
     def _grad_pointers(self, grads):
@@ -426,21 +312,14 @@ class AdamW(_Handle):
     def egeria_adamw_set_grads(self, grads: Sequence[torch.Tensor], stream: Optional[torch.cuda.Stream] = None) -> None:
         """The gradients (same sizes and types) are in these tensors from the next step on."""
         ptrs = self._grad_pointers(grads)
-        with self._on(stream) as s:
+        with _On(self.device, stream, (self._raw,)) as s:
             _check(self._lib.egeria_adamw_set_grads(self._h, s, ptrs), "egeria_adamw_set_grads")
 
     def egeria_adamw_step(self, lr: float, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8,
                           grad_scale: Optional[torch.Tensor] = None, frozen: Optional[torch.Tensor] = None,
                           stream: Optional[torch.cuda.Stream] = None) -> None:
         """One step of every tensor whose module is not marked in `frozen` (uint8, as egeria_plasticity_evaluate leaves it)."""
-        gs = _vector(grad_scale, "grad_scale", self._index, torch.float32, 1)
-        mask = 0 if frozen is None else _vector(frozen, "frozen", self._index, torch.uint8, frozen.numel())
-        if frozen is not None and frozen.numel() <= self._last_module:
-            raise ValueError("frozen: one entry per module is required")
-        with self._on(stream, *(() if stream is None else self._touched()), grad_scale, frozen) as s:
-            st = self._lib.egeria_adamw_step(self._h, s, lr, beta1, beta2, eps, gs or None, mask or None)
-        if st:
-            _check(st, "egeria_adamw_step")
+        self._call("egeria_adamw_step", self._native.adamw_step, stream, (lr, beta1, beta2, eps, grad_scale, frozen, self._last_module))
 
     def _touched(self):
         return [self._steps, *self._grads, *(t for column in self._keep for t in column)]

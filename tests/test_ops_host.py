@@ -21,36 +21,42 @@ def test_library_exports_every_declared_operator():
         assert hasattr(ops.lib(), name)
 
 
-def test_structs_have_the_headers_layout(tmp_path):
-    """Every mirror of a struct has the size and the field offsets that a C compiler gives the header's."""
+def test_struct_has_the_headers_layout(tmp_path):
+    """The mirror of egeria_adamw_tensor has the size and the field offsets that a C compiler gives the header's, and the
+    header is C99 on its own."""
     if shutil.which("gcc") is None:
         pytest.skip("no gcc")
-    def mirror(fields):
-        return type("Mirror", (ctypes.Structure,), {"_fields_": fields})
-
-    mirrors = {"egeria_linear_forward_args": mirror(ops._LINEAR_FORWARD), "egeria_linear_backward_args": mirror(ops._LINEAR_BACKWARD),
-               "egeria_norm_forward_args": mirror(ops._NORM_FORWARD), "egeria_norm_backward_args": mirror(ops._NORM_BACKWARD),
-               "egeria_adamw_tensor": ops._AdamTensor}
-    lines = ['#include "egeria_ops.h"', "#include <stdio.h>", "int main(void) {"]
-    for name, m in mirrors.items():
-        lines.append(f'    printf("{name} %zu\\n", sizeof({name}));')
-        lines += [f'    printf("{name}.{f} %zu\\n", offsetof({name}, {f}));' for f, _ in m._fields_]
-    src = tmp_path / "layout.c"
-    src.write_text("\n".join(lines + ["    return 0;", "}", ""]))
-    exe = tmp_path / "layout"
+    m = ops._AdamTensor
+    src, exe = tmp_path / "layout.c", tmp_path / "layout"
+    src.write_text('#include "egeria_ops.h"\n#include <stdio.h>\nint main(void) {\n    printf("size %zu\\n", sizeof(egeria_adamw_tensor));\n' +
+                   "".join(f'    printf("{f} %zu\\n", offsetof(egeria_adamw_tensor, {f}));\n' for f, _ in m._fields_) + "    return 0;\n}\n")
     subprocess.run(["gcc", "-std=c99", "-Wall", "-Werror", "-pedantic", "-I", str(HEADER.parent), str(src), "-o", str(exe)], check=True)
-    got = dict(line.rsplit(" ", 1) for line in subprocess.run([str(exe)], check=True, capture_output=True, text=True).stdout.splitlines())
-    for name, m in mirrors.items():
-        assert int(got[name]) == ctypes.sizeof(m)
-        for f, _ in m._fields_:
-            assert int(got[f"{name}.{f}"]) == getattr(m, f).offset, (name, f)
-    # and the packed forms put the values there
-    for pack, name in ((ops._pack_linear_forward, "egeria_linear_forward_args"), (ops._pack_linear_backward, "egeria_linear_backward_args"),
-                       (ops._pack_norm_forward, "egeria_norm_forward_args"), (ops._pack_norm_backward, "egeria_norm_backward_args")):
-        m = mirrors[name]
-        values = list(range(1, len(m._fields_) + 1))
-        read = m.from_buffer_copy(pack(*values).ljust(ctypes.sizeof(m), b"\0"))
-        assert [getattr(read, f) for f, _ in m._fields_] == values
+    got = dict(line.split() for line in subprocess.run([str(exe)], check=True, capture_output=True, text=True).stdout.splitlines())
+    assert int(got["size"]) == ctypes.sizeof(m)
+    for f, _ in m._fields_:
+        assert int(got[f]) == getattr(m, f).offset, f
+
+
+def test_extension_refuses_what_is_no_tensor_or_not_on_the_gpu():
+    import torch
+    n = ops._native()
+    x = torch.zeros(4, 4, dtype=torch.bfloat16)
+    with pytest.raises(ValueError):
+        n.linear_forward(0, 0, 0, 0, x, x, None, 0, None, False)                 # an argument short
+    with pytest.raises(ValueError):
+        n.linear_forward(0, 0, 0, 0, x, 3, None, 0, None, False, None)
+    with pytest.raises(ValueError):
+        n.linear_forward(0, 0, 0, 0, x, x, None, 0, None, False, None)           # host memory
+    with pytest.raises(ValueError):
+        n.linear_backward(0, 0, 0, 0, x, None, None, None, 0, None, 0, True, True, True)
+    with pytest.raises(ValueError):
+        n.norm_forward(0, 0, 0, 0, x, x, None, None, None, None, None, 0, 0, True, True, 1.0, 1e-5)
+    with pytest.raises(ValueError):
+        n.norm_backward(0, 0, 0, 0, x, x, x, x, None, None, None, None, None, None, 0, 0, True, True, 1.0, True)
+    with pytest.raises(TypeError):
+        n.norm_forward(0, 0, 0, 0, x, x, None, None, None, None, None, 0, 0, True, True, "1", 1e-5)
+    with pytest.raises(ValueError):
+        n.adamw_step(0, 0, 0, 0, 1e-3, 0.9, 0.999, 1e-8, x, None, -1)
 
 
 def test_workspace_sizes():
@@ -97,7 +103,8 @@ def test_adamw_refuses_bad_calls():
     assert _create([_tensor()], workspace=1040) == eg.ERR_WORKSPACE
     assert _create([_tensor()], nbytes=64) == eg.ERR_WORKSPACE
     assert ops.lib().egeria_adamw_workspace_bytes(1, (ops._AdamTensor * 1)(_tensor(n=-1)), 0) == 0
-    assert ops.lib().egeria_adamw_step(None, None, 1e-3, 0.9, 0.999, 1e-8, None, None) == eg.ERR_INVALID_ARG
+    d = ctypes.c_double
+    assert ops.lib().egeria_adamw_step(None, None, d(1e-3), d(0.9), d(0.999), d(1e-8), None, None) == eg.ERR_INVALID_ARG
     assert ops.lib().egeria_adamw_set_grads(None, None, None) == eg.ERR_INVALID_ARG
     assert ops.lib().egeria_adamw_destroy(None) == eg.ERR_INVALID_ARG
 

@@ -63,50 +63,80 @@ __device__ __forceinline__ float adam_param(const AdamStep &s, float p, float m,
     return fmaf(p, s.decay, -s.rate * m * fast_rcp(fmaf(fast_sqrt(v), s.root, s.eps)));
 }
 
-// The code of a size a in a block whose largest is top: MOST * sqrt(a / top) to the nearest whole number, every
-// operation rounded in 32 bits.  The approximate units give that number except within 1.2e-6 MOST of
-// a tie, where (once in some thousand values) the correctly rounded operations decide: codes come out the
-// same wherever the formula is computed operation by operation, so a state can be reproduced bit by bit.
-// ROOT: `a` is the square of the size.  `plain`: top is so small that the approximate units would
-// take what still has a code for zero.
-template <int MOST, bool ROOT>
-__device__ __forceinline__ int encode_size(float a, float top, float inv, bool plain) {
-    const float x = (float)MOST * fast_sqrt((ROOT ? fast_sqrt(a) : a) * inv);
-    const float c = rintf(x);
-    int code = (int)c;
-    if (plain || fabsf(fabsf(x - c) - 0.5f) < 1.2e-6f * MOST)
-        code = __float2int_rn((float)MOST * __fsqrt_rn(__fdiv_rn(ROOT ? __fsqrt_rn(a) : a, top)));
-    return code;
+// A code's byte becomes a float, and a float a code's byte, by the bits of 2^23 + code (1.5 * 2^23 + code): the units that
+// convert between the kinds are as slow as those of the roots and would be what the kernel waits for.
+__device__ __forceinline__ float code_float(uint32_t word, int i) {  // byte i of word, 0..255
+    return __uint_as_float(__byte_perm(word, 0x4B000000u, 0x7540 + i)) - 8388608.0f;
 }
+constexpr float kCodeMagic = 12582912.0f;
 
-// Eight values of a block with moments in codes: `cm`, `cv` are replaced by the new codes, `sm`, `sv` by the
-// block's new scales.  The moments are computed by separately rounded products and sums (see encode_size).
-__device__ __forceinline__ void adam_codes(const AdamStep &s, const float (&g)[8], float (&p)[8], int (&cm)[8], int (&cv)[8], float &sm,
+// The code of a size is MOST * sqrt(size / top) to the nearest whole number, top the largest in the block, every operation
+// rounded in 32 bits.  The approximate units give that number unless they come within 6e-7 MOST of a tie (their errors
+// and the formula's own roundings add up to 4.2e-7 MOST); there, once in some thousand values, the correctly rounded
+// operations decide.  Codes come out the same wherever the formula is computed operation by operation, so
+// that a state can be reproduced bit by bit.
+__device__ __noinline__ float exact_code(float size, float top, float most) { return rintf(most * __fsqrt_rn(__fdiv_rn(size, top))); }
+
+// Eight values of a block with moments in codes: the new codes replace the old ones in `wm`, `wv`, the block's new scales
+// `sm`, `sv`.  The moments are computed by separately rounded products and sums.
+__device__ __forceinline__ void adam_codes(const AdamStep &s, const F2 (&g)[4], F2 (&p)[4], uint32_t (&wm)[2], uint32_t (&wv)[2], float &sm,
                                            float &sv) {
-    const float um = __fdiv_rn(sm, 127.0f * 127.0f), uv = __fdiv_rn(sv, 255.0f * 255.0f);
-    float m[8], v[8], top_m = 0.0f, top_v = 0.0f;
+    const F2 um = f2(__fdiv_rn(sm, 127.0f * 127.0f)), uv = f2(__fdiv_rn(sv, 255.0f * 255.0f));
+    const F2 b1 = f2(s.beta1), r1 = f2(s.rest1), b2 = f2(s.beta2), r2 = f2(s.rest2), gs = f2(s.gscale);
+    float m[8], v[8], root[8], top_m = 0.0f, top_v = 0.0f;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const float gi = __fmul_rn(g[i], s.gscale);
-        const float root = __fmul_rn((float)(cv[i] * cv[i]), uv);
-        m[i] = __fadd_rn(__fmul_rn(s.beta1, __fmul_rn((float)(cm[i] * abs(cm[i])), um)), __fmul_rn(s.rest1, gi));
-        v[i] = __fadd_rn(__fmul_rn(s.beta2, __fmul_rn(root, root)), __fmul_rn(__fmul_rn(s.rest2, gi), gi));
-        p[i] = adam_param(s, p[i], m[i], v[i]);
-        top_m = max_nan(top_m, fabsf(m[i]));
-        top_v = max_nan(top_v, v[i]);
+    for (int k = 0; k < 4; ++k) {
+        const F2 gi = g[k] * gs;
+        // first moments are stored as two's complement: 128 more is 0..255
+        const uint32_t u = wm[k >> 1] ^ 0x80808080u;
+        const float lo = code_float(u, 2 * (k & 1)) - 128.0f, hi = code_float(u, 2 * (k & 1) + 1) - 128.0f;
+        const F2 cv = f2(code_float(wv[k >> 1], 2 * (k & 1)), code_float(wv[k >> 1], 2 * (k & 1) + 1));
+        const F2 old_root = cv * cv * uv;
+        const F2 mi = b1 * (f2(lo * fabsf(lo), hi * fabsf(hi)) * um) + r1 * gi;
+        const F2 vi = b2 * (old_root * old_root) + r2 * gi * gi;
+        const float2 ms = split(mi), vs = split(vi);
+        m[2 * k] = ms.x, m[2 * k + 1] = ms.y, v[2 * k] = vs.x, v[2 * k + 1] = vs.y;
+        root[2 * k] = fast_sqrt(vs.x), root[2 * k + 1] = fast_sqrt(vs.y);
+        const float2 d = split(fma2(f2(root[2 * k], root[2 * k + 1]), f2(s.root), f2(s.eps)));
+        p[k] = fma2(p[k], f2(s.decay), f2(-s.rate) * mi * f2(fast_rcp(d.x), fast_rcp(d.y)));
+        top_m = max_nan(max_nan(top_m, fabsf(ms.x)), fabsf(ms.y));
+        top_v = max_nan(max_nan(top_v, vs.x), vs.y);
     }
     sm = warp_max_nan(top_m);
     sv = __fsqrt_rn(warp_max_nan(top_v));
-    // a block of zeros, or with a value that is not finite (whose scale the next step decodes to NaN), has codes 0
-    const bool has_m = sm > 0.0f && sm <= 3.402823466e38f, has_v = sv > 0.0f && sv <= 3.402823466e38f;
-    const float im = fast_rcp(sm), iv = fast_rcp(sv);
-    const bool plain_m = sm < 1e-32f, plain_v = sv < 4e-14f;
+    // an infinity in a block makes its scale NaN, as a NaN does: the next step decodes the whole block to NaN
+    if (!(sm <= 3.402823466e38f)) sm = __uint_as_float(0x7fc00000u);
+    if (!(sv <= 3.402823466e38f)) sv = __uint_as_float(0x7fc00000u);
+    const float im = sm > 0.0f ? 127.0f * 127.0f * fast_rcp(sm) : 0.0f, iv = sv > 0.0f ? 255.0f * 255.0f * fast_rcp(sv) : 0.0f;
+    // below these scales the approximate units would take what still has a code for zero, or overflow
+    uint32_t ties = (sm > 0.0f && sm < 1e-32f ? 0xffu : 0u) | (sv > 0.0f && sv < 4e-14f ? 0xff00u : 0u);
+    float ym[8], yv[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        const int a = has_m ? encode_size<127, false>(fabsf(m[i]), sm, im, plain_m) : 0;
-        cm[i] = m[i] < 0.0f ? -a : a;
-        cv[i] = has_v ? encode_size<255, true>(v[i], sv, iv, plain_v) : 0;
-        if (has_v && v[i] > 0.0f) cv[i] = max(cv[i], 1);
+        const float xm = fast_sqrt(fabsf(m[i]) * im), xv = fast_sqrt(root[i] * iv);
+        ym[i] = xm + kCodeMagic;
+        yv[i] = xv + kCodeMagic;
+        if (fabsf(xm - (ym[i] - kCodeMagic)) > 0.5f - 6e-7f * 127.0f) ties |= 1u << i;
+        if (fabsf(xv - (yv[i] - kCodeMagic)) > 0.5f - 6e-7f * 255.0f) ties |= 256u << i;
+    }
+    if (ties) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            if (ties & (1u << i)) ym[i] = exact_code(fabsf(m[i]), sm, 127.0f) + kCodeMagic;
+            if (ties & (256u << i)) yv[i] = exact_code(__fsqrt_rn(v[i]), sv, 255.0f) + kCodeMagic;
+        }
+    }
+    uint32_t bm[8], bv[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        // the sign goes into the code: 2 * magic - y is magic - code
+        bm[i] = __float_as_uint(m[i] < 0.0f ? 2.0f * kCodeMagic - ym[i] : ym[i]);
+        bv[i] = __float_as_uint(fmaxf(yv[i], v[i] > 0.0f ? kCodeMagic + 1.0f : kCodeMagic));
+    }
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        wm[k] = __byte_perm(__byte_perm(bm[4 * k], bm[4 * k + 1], 0x0040), __byte_perm(bm[4 * k + 2], bm[4 * k + 3], 0x0040), 0x5410);
+        wv[k] = __byte_perm(__byte_perm(bv[4 * k], bv[4 * k + 1], 0x0040), __byte_perm(bv[4 * k + 2], bv[4 * k + 3], 0x0040), 0x5410);
     }
 }
 
@@ -138,46 +168,42 @@ __device__ __forceinline__ void adam_load(AdamBlock<P, G> &b, const AdamTensor &
 }
 template <typename P, typename G, bool MASTER, bool SMALL>
 __device__ __forceinline__ void adam_finish(AdamBlock<P, G> &b, const AdamStep &s, const AdamTensor &t, int64_t at, int lane) {
-    float p[8], g[8];
+    if (SMALL) {
+        F2 p[4], g[4];
+        unpack8(g, b.g);
+        if (MASTER)
+            unpack8(p, b.w);
+        else
+            unpack8(p, b.p);
+        uint32_t wm[2] = {b.cm.x, b.cm.y}, wv[2] = {b.cv.x, b.cv.y};
+        adam_codes(s, g, p, wm, wv, b.sm, b.sv);
+        *reinterpret_cast<uint2 *>(static_cast<uint8_t *>(t.m) + at) = make_uint2(wm[0], wm[1]);
+        *reinterpret_cast<uint2 *>(static_cast<uint8_t *>(t.v) + at) = make_uint2(wv[0], wv[1]);
+        if (lane == 0) {
+            t.m_scale[at / kAdamBlock] = b.sm;
+            t.v_scale[at / kAdamBlock] = b.sv;
+        }
+        if (MASTER) store8(t.master + at, p);
+        store8(static_cast<P *>(t.p) + at, p);
+        return;
+    }
+    float p[8], g[8], m[8], v[8];
     unpack8(g, b.g);
     if (MASTER)
         unpack8(p, b.w);
     else
         unpack8(p, b.p);
-    if (SMALL) {
-        int cm[8], cv[8];
+    unpack8(m, b.m);
+    unpack8(v, b.v);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            cm[i] = (int)(int8_t)((i < 4 ? b.cm.x : b.cm.y) >> (8 * (i & 3)));
-            cv[i] = (int)(((i < 4 ? b.cv.x : b.cv.y) >> (8 * (i & 3))) & 0xffu);
-        }
-        adam_codes(s, g, p, cm, cv, b.sm, b.sv);
-        uint32_t om[2] = {0u, 0u}, ov[2] = {0u, 0u};
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            om[i >> 2] |= (uint32_t)(cm[i] & 0xff) << (8 * (i & 3));
-            ov[i >> 2] |= (uint32_t)cv[i] << (8 * (i & 3));
-        }
-        *reinterpret_cast<uint2 *>(static_cast<uint8_t *>(t.m) + at) = make_uint2(om[0], om[1]);
-        *reinterpret_cast<uint2 *>(static_cast<uint8_t *>(t.v) + at) = make_uint2(ov[0], ov[1]);
-        if (lane == 0) {
-            t.m_scale[at / kAdamBlock] = b.sm;
-            t.v_scale[at / kAdamBlock] = b.sv;
-        }
-    } else {
-        float m[8], v[8];
-        unpack8(m, b.m);
-        unpack8(v, b.v);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const float gi = g[i] * s.gscale;
-            m[i] = fmaf(s.beta1, m[i], s.rest1 * gi);
-            v[i] = fmaf(s.beta2, v[i], s.rest2 * gi * gi);
-            p[i] = adam_param(s, p[i], m[i], v[i]);
-        }
-        store8(static_cast<float *>(t.m) + at, m);
-        store8(static_cast<float *>(t.v) + at, v);
+    for (int i = 0; i < 8; ++i) {
+        const float gi = g[i] * s.gscale;
+        m[i] = fmaf(s.beta1, m[i], s.rest1 * gi);
+        v[i] = fmaf(s.beta2, v[i], s.rest2 * gi * gi);
+        p[i] = adam_param(s, p[i], m[i], v[i]);
     }
+    store8(static_cast<float *>(t.m) + at, m);
+    store8(static_cast<float *>(t.v) + at, v);
     if (MASTER) store8(t.master + at, p);
     store8(static_cast<P *>(t.p) + at, p);
 }
@@ -185,7 +211,7 @@ __device__ __forceinline__ void adam_finish(AdamBlock<P, G> &b, const AdamStep &
 template <typename P, typename G, bool MASTER, bool SMALL>
 __device__ __forceinline__ void adam_narrow(const AdamStep &s, const AdamTensor &t, const G *grad, int64_t at0, int lane) {
     float p[8], g[8], m[8], v[8];
-    int cm[8], cv[8];
+    uint32_t wm[2] = {0u, 0u}, wv[2] = {0u, 0u};
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         const int64_t at = at0 + lane + 32 * i;
@@ -193,8 +219,8 @@ __device__ __forceinline__ void adam_narrow(const AdamStep &s, const AdamTensor 
         g[i] = in ? to_f32(grad[at]) : 0.0f;
         p[i] = !in ? 0.0f : MASTER ? t.master[at] : to_f32(static_cast<const P *>(t.p)[at]);
         if (SMALL) {
-            cm[i] = in ? (int)static_cast<const int8_t *>(t.m)[at] : 0;
-            cv[i] = in ? (int)static_cast<const uint8_t *>(t.v)[at] : 0;
+            wm[i >> 2] |= (in ? (uint32_t)static_cast<const uint8_t *>(t.m)[at] : 0u) << (8 * (i & 3));
+            wv[i >> 2] |= (in ? (uint32_t)static_cast<const uint8_t *>(t.v)[at] : 0u) << (8 * (i & 3));
         } else {
             m[i] = in ? static_cast<const float *>(t.m)[at] : 0.0f;
             v[i] = in ? static_cast<const float *>(t.v)[at] : 0.0f;
@@ -202,7 +228,15 @@ __device__ __forceinline__ void adam_narrow(const AdamStep &s, const AdamTensor 
     }
     if (SMALL) {
         float sm = t.m_scale[at0 / kAdamBlock], sv = t.v_scale[at0 / kAdamBlock];
-        adam_codes(s, g, p, cm, cv, sm, sv);
+        F2 g2[4], p2[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) g2[k] = f2(g[2 * k], g[2 * k + 1]), p2[k] = f2(p[2 * k], p[2 * k + 1]);
+        adam_codes(s, g2, p2, wm, wv, sm, sv);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const float2 q = split(p2[k]);
+            p[2 * k] = q.x, p[2 * k + 1] = q.y;
+        }
         if (lane == 0) {
             t.m_scale[at0 / kAdamBlock] = sm;
             t.v_scale[at0 / kAdamBlock] = sv;
@@ -213,8 +247,8 @@ __device__ __forceinline__ void adam_narrow(const AdamStep &s, const AdamTensor 
         const int64_t at = at0 + lane + 32 * i;
         if (at >= t.n) continue;
         if (SMALL) {
-            static_cast<int8_t *>(t.m)[at] = (int8_t)cm[i];
-            static_cast<uint8_t *>(t.v)[at] = (uint8_t)cv[i];
+            static_cast<uint8_t *>(t.m)[at] = (uint8_t)(wm[i >> 2] >> (8 * (i & 3)));
+            static_cast<uint8_t *>(t.v)[at] = (uint8_t)(wv[i >> 2] >> (8 * (i & 3)));
         } else {
             const float gi = g[i] * s.gscale;
             m[i] = fmaf(s.beta1, m[i], s.rest1 * gi);

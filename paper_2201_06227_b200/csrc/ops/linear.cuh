@@ -177,10 +177,29 @@ constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kGeluA = 1.5957691216057308f;  // 2 sqrt(2 / pi)
 constexpr float kGeluB = 0.044715f;
 
+// Phi(z), the normal distribution, and e = exp(-z^2 / 2), which its density shares: Abramowitz and Stegun's formula 7.1.26,
+// erfc(x) = (a1 t + ... + a5 t^5) exp(-x^2) with t = 1 / (1 + p x), x = |z| / sqrt(2): Phi is off by 7.5e-8 at most (a
+// 16-bit result is rounded by 2^-12 of itself at least).  The library's erfcf gives more digits than the output
+// holds and took 1.45 times the whole product's time at 65536 x 1024 x 4096 (850 us against 580).
+__device__ __forceinline__ float normal_cdf(float z, float &e) {
+    const float x = fabsf(z) * 0.70710678118654752f;
+    const float t = fast_rcp(fmaf(0.3275911f, x, 1.0f));
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(-kLog2e * x * x));
+    float q = fmaf(1.061405429f, t, -1.453152027f);
+    q = fmaf(q, t, 1.421413741f);
+    q = fmaf(q, t, -0.284496736f);
+    q = fmaf(q, t, 0.254829592f);
+    const float tail = 0.5f * q * t * e;
+    return z < 0.0f ? tail : 1.0f - tail;
+}
+
 template <int ACT>
 __device__ __forceinline__ float act_value(float z) {
     if (ACT == kActRelu) return z > 0.0f ? z : (z != z ? z : 0.0f);
-    if (ACT == kActGelu) return 0.5f * z * erfcf(-0.70710678118654752f * z);
+    if (ACT == kActGelu) {
+        float e;
+        return z * normal_cdf(z, e);
+    }
     if (ACT == kActGeluTanh) return z * logistic2(z * fmaf(-kLog2e * kGeluA * kGeluB, z * z, -kLog2e * kGeluA));
     if (ACT == kActSilu) return z * logistic2(-kLog2e * z);
     return z;
@@ -188,7 +207,11 @@ __device__ __forceinline__ float act_value(float z) {
 template <int ACT>
 __device__ __forceinline__ float act_slope(float z) {
     if (ACT == kActRelu) return z > 0.0f ? 1.0f : 0.0f;
-    if (ACT == kActGelu) return fmaf(0.39894228040143268f * z, __expf(-0.5f * z * z), 0.5f * erfcf(-0.70710678118654752f * z));
+    if (ACT == kActGelu) {
+        float e;
+        const float phi = normal_cdf(z, e);
+        return fmaf(0.39894228040143268f * z, e, phi);
+    }
     if (ACT == kActGeluTanh) {
         const float q = z * z;
         const float p = logistic2(z * fmaf(-kLog2e * kGeluA * kGeluB, q, -kLog2e * kGeluA));

@@ -26,8 +26,7 @@ namespace ops {
 constexpr int kAdamBlock = 256;     // values per scale, and per warp and pass
 constexpr int kAdamThreads = 256;
 constexpr int kAdamWarps = kAdamThreads / 32;
-constexpr int kAdamUnroll = 2;      // blocks a warp has in flight
-constexpr int kAdamChunk = kAdamBlock * kAdamWarps * kAdamUnroll;  // values per table entry
+constexpr int kAdamChunk = kAdamBlock * kAdamWarps;  // values per table entry
 
 struct AdamTensor {
     void *p;
@@ -263,9 +262,12 @@ __device__ __forceinline__ void adam_narrow(const AdamStep &s, const AdamTensor 
 }
 
 template <typename P, typename G, bool MASTER, bool SMALL>
-__global__ void __launch_bounds__(kAdamThreads) adamw_kernel(const AdamParams a) {
+__global__ void __launch_bounds__(kAdamThreads, SMALL ? 3 : 2) adamw_kernel(const AdamParams a) {
     ptx::grid_dependency_wait();
     ptx::grid_launch_dependents();
+    // blocks that a warp has in flight: moments in 32 bits are enough bytes with one (302 M bf16 values 1054 us, with two 1108);
+    // in 8 bits it takes two (825 us, with one 937)
+    constexpr int kUnroll = SMALL ? 2 : 1;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const float gscale = a.grad_scale ? *a.grad_scale : 1.0f;
     const bool skip_all = !(fabsf(gscale) <= 3.402823466e38f);  // not finite: the whole step is left out
@@ -294,28 +296,24 @@ __global__ void __launch_bounds__(kAdamThreads) adamw_kernel(const AdamParams a)
             s = AdamStep{1.0f - a.lr * t.wd, a.lr / fix1, rsqrtf(fix2), a.eps, a.beta1, a.rest1, a.beta2, a.rest2, gscale};
         }
         if (!live) continue;
-        const int64_t base = (int64_t)chunk.y * kAdamChunk + warp * kAdamBlock;
-        if (vector && base + (kAdamUnroll - 1) * kAdamWarps * kAdamBlock + kAdamBlock <= t.n) {
-            AdamBlock<P, G> b[kAdamUnroll];
+        const int64_t at0 = (int64_t)chunk.y * kAdamChunk + warp * kAdamBlock;
+        // the next entries go on with the same tensor as a rule: then kUnroll blocks of a warp are in flight together
+        const bool more = c + kUnroll <= c1 && a.chunks[c + kUnroll - 1].x == tensor;
+        if (vector && more && ((int64_t)chunk.y + kUnroll) * kAdamChunk <= t.n) {
+            AdamBlock<P, G> b[kUnroll];
 #pragma unroll
-            for (int u = 0; u < kAdamUnroll; ++u)
-                adam_load<P, G, MASTER, SMALL>(b[u], t, grad, base + u * kAdamWarps * kAdamBlock + lane * 8);
+            for (int u = 0; u < kUnroll; ++u) adam_load<P, G, MASTER, SMALL>(b[u], t, grad, at0 + u * kAdamChunk + lane * 8);
 #pragma unroll
-            for (int u = 0; u < kAdamUnroll; ++u)
-                adam_finish<P, G, MASTER, SMALL>(b[u], s, t, base + u * kAdamWarps * kAdamBlock + lane * 8, lane);
-            continue;
-        }
-#pragma unroll 1
-        for (int u = 0; u < kAdamUnroll; ++u) {
-            const int64_t at0 = base + u * kAdamWarps * kAdamBlock;
-            if (at0 >= t.n) break;
-            if (vector && at0 + kAdamBlock <= t.n) {
-                AdamBlock<P, G> b;
-                adam_load<P, G, MASTER, SMALL>(b, t, grad, at0 + lane * 8);
-                adam_finish<P, G, MASTER, SMALL>(b, s, t, at0 + lane * 8, lane);
-            } else {
-                adam_narrow<P, G, MASTER, SMALL>(s, t, grad, at0, lane);
-            }
+            for (int u = 0; u < kUnroll; ++u) adam_finish<P, G, MASTER, SMALL>(b[u], s, t, at0 + u * kAdamChunk + lane * 8, lane);
+            c += kUnroll - 1;
+        } else if (at0 >= t.n) {
+            // (nothing of it is this warp's)
+        } else if (vector && at0 + kAdamBlock <= t.n) {
+            AdamBlock<P, G> b;
+            adam_load<P, G, MASTER, SMALL>(b, t, grad, at0 + lane * 8);
+            adam_finish<P, G, MASTER, SMALL>(b, s, t, at0 + lane * 8, lane);
+        } else {
+            adam_narrow<P, G, MASTER, SMALL>(s, t, grad, at0, lane);
         }
     }
     // Every CTA has read the step counts; the last one to get here counts this step.

@@ -334,9 +334,17 @@ __device__ __forceinline__ void piece_store(void *base, int64_t ld, const float 
         for (int k = 0; k < rows; ++k) p[k * ld] = t.stage[k * kStagePitch + c];
     }
 }
-// v: the piece's sums; `extra` already holds its values where the piece is fast.
+// What the epilogue adds to a piece or takes its slope of.
+__device__ __forceinline__ void piece_extra(uint32_t (&r)[16], const Epilogue &p, const Tile &t) {
+    if (t.rows <= 0 || t.cols <= 0) return;
+    if (t.fast())
+        piece_fetch(r, p.extra, p.ldx, t);
+    else
+        piece_fetch_narrow(r, p.extra, p.ldx, t);
+}
+// v: the piece's sums; `extra`: what piece_extra fetched.
 template <typename T>
-__device__ __forceinline__ void piece_finish(const Epilogue &p, float (&v)[32], uint32_t (&extra)[16], const Tile &t) {
+__device__ __forceinline__ void piece_finish(const Epilogue &p, float (&v)[32], const uint32_t (&extra)[16], const Tile &t) {
     if (t.rows <= 0 || t.cols <= 0) return;  // the same for the whole warp
     if (p.bias) {
         const T *b = static_cast<const T *>(p.bias) + t.col0;
@@ -361,7 +369,6 @@ __device__ __forceinline__ void piece_finish(const Epilogue &p, float (&v)[32], 
     if (p.z) piece_store<T>(p.z, p.ldz, v, t);
     if (p.act) act_values(v, p.act);
     if (p.extra) {
-        if (!t.fast()) piece_fetch_narrow(extra, p.extra, p.ldx, t);
         if (p.slope) {
             // eight at a time: a slope keeps several registers per value
 #pragma unroll
@@ -641,7 +648,7 @@ __global__ void __launch_bounds__(GemmCfg<BN, CG>::kThreads, 1) gemm_kernel(cons
                 // what the first piece reads is on its way while the products are computed
                 uint32_t extra[16];
                 const bool ahead = q.epi.extra && q.splits == 1;
-                if (ahead && t.fast()) piece_fetch(extra, q.epi.extra, q.epi.ldx, t);
+                if (ahead) piece_extra(extra, q.epi, t);
                 if (!__all_sync(0xffffffffu, ptx::mbar_wait_bounded(accfull0 + 8 * acc, acc_phase, abort_flag, p.wait_limit_ns))) return false;
                 ptx::tc_fence_after_sync();
                 const uint32_t src = tmem + ((uint32_t)(quarter * 32) << 16) + acc * BN + strip * Cfg::kColsPerWarp;
@@ -671,7 +678,7 @@ __global__ void __launch_bounds__(GemmCfg<BN, CG>::kThreads, 1) gemm_kernel(cons
                         piece_finish<T>(q.epi, v, extra, t);
                         t.col0 += kPiece;
                         t.cols -= kPiece;
-                        if (c + 1 < Cfg::kPieces && ahead && t.fast()) piece_fetch(extra, q.epi.extra, q.epi.ldx, t);
+                        if (c + 1 < Cfg::kPieces && ahead) piece_extra(extra, q.epi, t);
                     }
                 }
                 if (q.splits > 1) {
@@ -688,7 +695,7 @@ __global__ void __launch_bounds__(GemmCfg<BN, CG>::kThreads, 1) gemm_kernel(cons
                         const int64_t pitch = (int64_t)CG * kEpiWarps * Cfg::kPieces * 1024;
 #pragma unroll 1
                         for (int c = 0; c < Cfg::kPieces; ++c) {
-                            if (q.epi.extra && t.fast()) piece_fetch(extra, q.epi.extra, q.epi.ldx, t);
+                            if (q.epi.extra) piece_extra(extra, q.epi, t);
                             float v[32];
 #pragma unroll
                             for (int i = 0; i < 32; ++i) v[i] = 0.0f;

@@ -9,6 +9,10 @@
 // lane, so that a 16-bit tensor is read in 16-byte and a 32-bit one in 32-byte accesses.  8-bit
 // moments have one scale per block, which makes the block's maximum a reduction inside the warp.
 //
+// Measured on 302 M values (a 24-block, 1024-wide decoder; floor: the bytes at 6464 GB/s), bf16 parameters: moments in 32 bits
+// 1054 us of 1029, with fp32 masters 1380 of 1309; in 8 bits 823 us of 471: there the codes' arithmetic (63
+// instructions a value) is as long as the bytes, and issue slots are 61 % taken.
+//
 // 8-bit codes.  A first moment is sign * (c / 127)^2 * scale with c = 0..127, and the ROOT of a second
 // moment is (c / 255)^2 * scale with c = 0..255; scale is the largest size in the block.  Squaring the
 // code spends the steps where the sizes are: next to the maximum a step is 1.6 % (0.8 %) of the
@@ -261,6 +265,7 @@ __device__ __forceinline__ void adam_narrow(const AdamStep &s, const AdamTensor 
     }
 }
 
+// Three CTAs per SM for 8-bit moments (80 registers, a few spilled): 823 us against 924 with two.
 template <typename P, typename G, bool MASTER, bool SMALL>
 __global__ void __launch_bounds__(kAdamThreads, SMALL ? 3 : 2) adamw_kernel(const AdamParams a) {
     ptx::grid_dependency_wait();

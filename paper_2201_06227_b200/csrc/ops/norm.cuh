@@ -10,6 +10,11 @@
 // and df.  A row lives in the registers of its team of threads between its load and its stores, so the
 // means, the variances (of the differences from the mean, in 32 bits) and both norms cost no second
 // read.
+//
+// Measured at 65536 x 1024 bf16 (floor: the bytes at 6464 GB/s): forward with two layer norms 105 us of 83, with two rms
+// norms 87 of 83; backward with two rms norms 152 us of 125, with two layer norms 192 of 125.  What is left is
+// instructions: a value costs about 35 of them backward, and two more sums per row with means and biases.  A
+// row pitch that takes no 16-byte accesses costs 2.4 (forward) and 1.8 times that: 250 and 265 us at 1001 columns.
 #pragma once
 #include <string.h>
 
@@ -173,6 +178,8 @@ __device__ __forceinline__ void norm_center(F2 (&v)[VPT][4], const NormParams &p
     inv = rsqrtf(fmaf(q[0], p.inv_cols, p.eps));
 }
 
+// A warp per row up to 1024 columns (no barrier at all), 128 threads up to 4096, 256 beyond: wider teams with fewer values
+// per thread took 120 us against 107 at 16384 x 4096 and 136 against 115 at 8192 x 8192.
 template <typename T, int TEAM, int VPT, bool WIDE, bool FULL>
 __global__ void __launch_bounds__(TEAM == 32 ? 128 : TEAM) norm_forward_kernel(const NormParams p) {
     __shared__ float scratch[2 * 32 * 2];
@@ -239,6 +246,7 @@ __global__ void __launch_bounds__(TEAM == 32 ? 128 : TEAM) norm_forward_kernel(c
 // at the end of every group of rows: straight into dgate if the whole group was this CTA's, else
 // as a partial sum (a CTA has at most two groups that it shares: its first and its last).  A second
 // kernel adds the partial sums in a fixed order: results do not depend on timing.
+// 512 threads per SM in all (128 registers each): 640 of them at 96 registers spill and took 161 us against 151.
 // Partial sums per CTA: 6 x cols: dw_pre, db_pre, dw_post, db_post, first group, last group.
 constexpr int kNormSums = 6;
 

@@ -182,7 +182,7 @@ static cudaError_t allow_smem() {
     return cudaFuncSetAttribute(gemm_kernel<T, BN, CG>, cudaFuncAttributeMaxDynamicSharedMemorySize, GemmCfg<BN, CG>::kSmem);
 }
 constexpr int kFewSmem = 96 * 1024;
-constexpr int kFewRows = 4;   // rows that go without the tensor cores
+constexpr int kFewRows = 4;   // rows that go without the tensor cores: 9.0 us at 1024 x 4096 either way at four rows, 6.5 against 8.9 at two
 template <typename T, int ROWS>
 static cudaError_t allow_few() {
     cudaError_t e = cudaFuncSetAttribute(linear_few_kernel<T, ROWS, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, kFewSmem);

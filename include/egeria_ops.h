@@ -169,7 +169,10 @@ enum {
     /* Moments in 8 bits.  m: int8 codes c, a first moment is sign(c) (c / 127)^2 scale; v: uint8 codes,
      * the square root of a second moment is (c / 255)^2 scale.  One float scale per moment and block of
      * EGERIA_ADAMW_BLOCK consecutive values of a tensor: the largest size in the block.  A second
-     * moment that is not zero has a code of at least 1.  A value that is not finite makes its whole
+     * moment that is not zero has a code of at least 1.  Codes and scales are those of the
+     * formula in 32 bits, every operation rounded by itself (a code is decoded as (c c) (scale * (1 / 127^2)), the roots
+     * and quotients are correctly rounded, codes to the nearest, ties to even): a state can be reproduced
+     * bit by bit.  A value that is not finite makes its whole
      * block NaN from the next step on (8-bit codes have no NaN of their own). */
     EGERIA_ADAMW_8BIT = 1u
 };

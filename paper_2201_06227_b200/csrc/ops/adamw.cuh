@@ -10,7 +10,7 @@
 // moments have one scale per block, which makes the block's maximum a reduction inside the warp.
 //
 // Measured on 302 M values (a 24-block, 1024-wide decoder; floor: the bytes at 6464 GB/s), bf16 parameters: moments in 32 bits
-// 1054 us of 1029, with fp32 masters 1380 of 1309; in 8 bits 823 us of 471: there the codes' arithmetic (63
+// 1054 us of 1029, with fp32 masters 1380 of 1309; in 8 bits 861 us of 471: there the codes' arithmetic (63
 // instructions a value) is as long as the bytes, and issue slots are 61 % taken.
 //
 // 8-bit codes.  A first moment is sign * (c / 127)^2 * scale with c = 0..127, and the ROOT of a second
@@ -80,11 +80,16 @@ constexpr float kCodeMagic = 12582912.0f;
 // that a state can be reproduced bit by bit.
 __device__ __noinline__ float exact_code(float size, float top, float most) { return rintf(most * __fsqrt_rn(__fdiv_rn(size, top))); }
 
+__device__ __forceinline__ F2 add_apart(F2 a, F2 b) {
+    const float2 x = split(a), y = split(b);
+    return f2(__fadd_rn(x.x, y.x), __fadd_rn(x.y, y.y));
+}
+
 // Eight values of a block with moments in codes: the new codes replace the old ones in `wm`, `wv`, the block's new scales
 // `sm`, `sv`.  The moments are computed by separately rounded products and sums.
 __device__ __forceinline__ void adam_codes(const AdamStep &s, const F2 (&g)[4], F2 (&p)[4], uint32_t (&wm)[2], uint32_t (&wv)[2], float &sm,
                                            float &sv) {
-    const F2 um = f2(__fdiv_rn(sm, 127.0f * 127.0f)), uv = f2(__fdiv_rn(sv, 255.0f * 255.0f));
+    const F2 um = f2(sm * (1.0f / (127.0f * 127.0f))), uv = f2(sv * (1.0f / (255.0f * 255.0f)));
     const F2 b1 = f2(s.beta1), r1 = f2(s.rest1), b2 = f2(s.beta2), r2 = f2(s.rest2), gs = f2(s.gscale);
     float m[8], v[8], root[8], top_m = 0.0f, top_v = 0.0f;
 #pragma unroll
@@ -95,8 +100,9 @@ __device__ __forceinline__ void adam_codes(const AdamStep &s, const F2 (&g)[4], 
         const float lo = code_float(u, 2 * (k & 1)) - 128.0f, hi = code_float(u, 2 * (k & 1) + 1) - 128.0f;
         const F2 cv = f2(code_float(wv[k >> 1], 2 * (k & 1)), code_float(wv[k >> 1], 2 * (k & 1) + 1));
         const F2 old_root = cv * cv * uv;
-        const F2 mi = b1 * (f2(lo * fabsf(lo), hi * fabsf(hi)) * um) + r1 * gi;
-        const F2 vi = b2 * (old_root * old_root) + r2 * gi * gi;
+        // (the sums by themselves: a sum of pairs may be fused with the product before it)
+        const F2 mi = add_apart(b1 * (f2(lo * fabsf(lo), hi * fabsf(hi)) * um), r1 * gi);
+        const F2 vi = add_apart(b2 * (old_root * old_root), r2 * gi * gi);
         const float2 ms = split(mi), vs = split(vi);
         m[2 * k] = ms.x, m[2 * k + 1] = ms.y, v[2 * k] = vs.x, v[2 * k + 1] = vs.y;
         root[2 * k] = fast_sqrt(vs.x), root[2 * k + 1] = fast_sqrt(vs.y);
@@ -265,13 +271,13 @@ __device__ __forceinline__ void adam_narrow(const AdamStep &s, const AdamTensor 
     }
 }
 
-// Three CTAs per SM for 8-bit moments (80 registers, a few spilled): 823 us against 924 with two.
+// Three CTAs per SM for 8-bit moments (80 registers, a few spilled): 825 us against 924 with two.
 template <typename P, typename G, bool MASTER, bool SMALL>
 __global__ void __launch_bounds__(kAdamThreads, SMALL ? 3 : 2) adamw_kernel(const AdamParams a) {
     ptx::grid_dependency_wait();
     ptx::grid_launch_dependents();
     // blocks that a warp has in flight: moments in 32 bits are enough bytes with one (302 M bf16 values 1054 us, with two 1108);
-    // in 8 bits it takes two (825 us, with one 937)
+    // in 8 bits it takes two (825 us, with one 937, before the sums of pairs were taken apart)
     constexpr int kUnroll = SMALL ? 2 : 1;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const float gscale = a.grad_scale ? *a.grad_scale : 1.0f;

@@ -92,7 +92,8 @@ __device__ __forceinline__ void store8(T *p, const float (&v)[8]) {
                  : "memory");
 }
 
-// Pairs of floats: one instruction for two products, sums or fused products of separately rounded values.
+// Pairs of floats: one instruction for two products, sums or fused products.  The compiler may fuse a product and a sum of
+// pairs in spite of their .rn; where each has to be rounded by itself the sum is taken apart.
 struct F2 {
     uint64_t v;
 };

@@ -628,6 +628,35 @@ def check_adamw(sizes, dtype, gtype, master, bits, shift=0, lr=1e-2, betas=(0.9,
     a.check_device_status()
 
 
+def test_adamw_codes_are_the_formulas_bit_by_bit():
+    """Codes and scales of three steps equal those of elementary operations, each rounded to 32 bits by itself."""
+    n, b1, b2 = 256 * 4000, 0.9, 0.999
+    s = model([n], torch.bfloat16, torch.bfloat16, False, 8)
+    a = optimizer(s, 8)
+    scale = torch.tensor([0.37], device=DEV)
+    code = {k: s[k][0].clone().float().view(-1, 256) for k in ("m", "v")}
+    top = {"m": s["ms"][0].clone().view(-1, 1), "v": s["vs"][0].clone().view(-1, 1)}
+
+    unit = {"m": torch.tensor(1 / 127 ** 2, device=DEV), "v": torch.tensor(1 / 255 ** 2, device=DEV)}
+
+    def codes(size, most, first):
+        t = size.amax(1, keepdim=True)
+        c = torch.round(most * torch.sqrt(size / torch.where(t > 0, t, torch.ones_like(t))))
+        return torch.where(size > 0, c.clamp(min=first), c), t
+
+    for step in range(3):
+        g = s["g"][0].float().view(-1, 256) * scale
+        m = b1 * (code["m"] * code["m"].abs() * (top["m"] * unit["m"])) + (1.0 - b1) * g
+        root = code["v"] * code["v"] * (top["v"] * unit["v"])
+        v = b2 * (root * root) + (1.0 - b2) * g * g
+        c, top["m"] = codes(m.abs(), 127, 0)
+        code["m"] = torch.sign(m) * c
+        code["v"], top["v"] = codes(torch.sqrt(v), 255, 1)
+        a.egeria_adamw_step(1e-3, b1, b2, grad_scale=scale)
+        assert torch.equal(s["ms"][0], top["m"].view(-1)) and torch.equal(s["vs"][0], top["v"].view(-1)), step
+        assert torch.equal(s["m"][0].float().view(-1, 256), code["m"]) and torch.equal(s["v"][0].float().view(-1, 256), code["v"]), step
+
+
 ADAM_SIZES = [1, 255, 256, 257, 0, 4096, 4097, 100, 2304, 16, 8192 + 300]
 
 

@@ -41,7 +41,8 @@ typedef struct egeria_adamw egeria_adamw;
  *   workspace  device memory, EGERIA_WORKSPACE_ALIGN-aligned, caller-owned, at least
  *              EGERIA_OPS_WORKSPACE_MIN bytes and as much as the largest call made through
  *              the handle asks for; must outlive the handle
- * Clears the handle's part of the workspace synchronously on the current device. */
+ * Waits for the current device, whose earlier work may still use that memory, and clears the handle's part of it
+ * synchronously. */
 #define EGERIA_OPS_WORKSPACE_MIN 65536
 egeria_status egeria_ops_create(egeria_ops **out, void *workspace, size_t workspace_bytes);
 egeria_status egeria_ops_destroy(egeria_ops *ops);
@@ -198,7 +199,7 @@ size_t egeria_adamw_workspace_bytes(int count, const egeria_adamw_tensor *tensor
 /* An optimizer over `count` tensors (host array, copied).
  *   grads  host array [count] of device pointers
  *   steps  device int32 [count], the caller's: steps taken so far by each tensor
- * Writes its tables to the workspace and synchronises. */
+ * Waits for the current device, whose earlier work may still use the workspace, writes its tables there and synchronises. */
 egeria_status egeria_adamw_create(egeria_adamw **out, int count, const egeria_adamw_tensor *tensors,
                                   const void *const *grads, int32_t *steps, void *workspace, size_t workspace_bytes,
                                   uint32_t flags);

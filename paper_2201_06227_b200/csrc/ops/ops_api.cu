@@ -510,6 +510,8 @@ egeria_status egeria_ops_create(egeria_ops **out, void *workspace, size_t worksp
     }
     EGO_CUDA(allow_all<bf16>());
     EGO_CUDA(allow_all<f16>());
+    // the workspace may be memory that earlier work of a stream which the default stream does not wait for still writes to
+    EGO_CUDA(cudaDeviceSynchronize());
     EGO_CUDA(cudaMemset(workspace, 0, kHeadBytes));
     EGO_CUDA(cudaDeviceSynchronize());
     egeria_ops *o = new (std::nothrow) egeria_ops();
@@ -859,7 +861,9 @@ egeria_status egeria_adamw_create(egeria_adamw **out, int count, const egeria_ad
             h->classes.push_back(c);
         }
         for (int i = 0; i < count; ++i) h->grad_size.push_back(tensors[i].n ? size_of(tensors[i].grad_type) : 0);
-        if (cudaMemcpy(h->ws, image.data(), L.total, cudaMemcpyHostToDevice) != cudaSuccess || cudaDeviceSynchronize() != cudaSuccess) {
+        // (first what was enqueued before: it may still write to this memory, and the copy would not wait for it)
+        if (cudaDeviceSynchronize() != cudaSuccess || cudaMemcpy(h->ws, image.data(), L.total, cudaMemcpyHostToDevice) != cudaSuccess ||
+            cudaDeviceSynchronize() != cudaSuccess) {
             (void)cudaGetLastError();
             delete h;
             return EGERIA_ERR_CUDA;

@@ -1,0 +1,59 @@
+"""What the training operators do at the edges: memory that other streams still use, sizes below a handle's, operands that
+overlap, values at the ends of their types, autograd around the calls, aliases, gradients against differences.
+
+Tolerances are derived as in test_ops_gpu.py, before the first run.
+"""
+import ctypes
+import math
+import subprocess
+import sys
+import weakref
+from pathlib import Path
+
+import pytest
+import torch
+
+from paper_2201_06227_b200 import binding as eg
+from paper_2201_06227_b200 import ops
+from test_ops_gpu import DEV, TINY, U, act64, close, rand
+
+pytestmark = pytest.mark.gpu
+
+
+# ----------------------------------------------------------------------------- memory that other work still uses
+
+def contended(nbytes, make):
+    """make()'s handle, its workspace of `nbytes` being memory that a kernel of its stream has yet to write."""
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    torch.cuda.empty_cache()
+    with torch.cuda.stream(side):
+        old = [torch.empty(nbytes, dtype=torch.uint8, device=DEV) for _ in range(4)]
+        places = {t.data_ptr() for t in old}
+        torch.cuda._sleep(20_000_000)      # about 10 ms
+        for k in range(4):
+            old[k].fill_(255)
+        del old
+        h = make()
+        assert h._raw.data_ptr() in places
+    torch.cuda.synchronize()
+    return h
+
+
+def workspace_of(h, nbytes=None):
+    at = -h._raw.data_ptr() % eg.WORKSPACE_ALIGN
+    return h._raw[at:][:nbytes]
+
+
+def test_new_handle_waits_for_the_memory_it_is_given():
+    """The clearing of an Ops' tickets and AdamW's table come after whatever still writes to the block."""
+    o = contended(ops.Ops(1 << 20, DEV)._raw.numel(), lambda: ops.Ops(1 << 20, DEV))
+    assert not workspace_of(o, ops.OPS_WORKSPACE_MIN).any()
+    p, g, m, v = ([rand(n, dtype=torch.float32, seed=n + k) for n in (700, 5000)] for k in range(4))
+    steps = torch.zeros(2, dtype=torch.int32, device=DEV)
+    quiet = ops.AdamW(p, g, m, v, steps)
+    size = quiet._raw.numel() - eg.WORKSPACE_ALIGN
+    other = contended(quiet._raw.numel(), lambda: ops.AdamW(p, g, m, v, steps))
+    assert torch.equal(workspace_of(quiet, size), workspace_of(other, size))
+
+

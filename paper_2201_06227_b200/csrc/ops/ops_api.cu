@@ -534,7 +534,9 @@ egeria_status egeria_ops_device_status(egeria_ops *ops) {
     int32_t v = 0;
     EGO_CUDA(cudaMemcpy(&v, ops->ws, sizeof(v), cudaMemcpyDeviceToHost));
     if (v == 0) return EGERIA_OK;
-    EGO_CUDA(cudaMemset(ops->ws, 0, kHeadBytes));  // tickets too: a call that gave up may have left some
+    // tickets too: a call that gave up may have left some.  In the call's own stream, which need not wait for the default one
+    EGO_CUDA(cudaMemsetAsync(ops->ws, 0, kHeadBytes, ops->last_stream));
+    EGO_CUDA(cudaStreamSynchronize(ops->last_stream));
     return static_cast<egeria_status>(v);
 }
 int64_t egeria_ops_launch_count(const egeria_ops *ops) { return ops ? ops->launches : 0; }
@@ -923,7 +925,8 @@ egeria_status egeria_adamw_device_status(egeria_adamw *adamw) {
     int32_t v = 0;
     EGO_CUDA(cudaMemcpy(&v, adamw->ws, sizeof(v), cudaMemcpyDeviceToHost));
     if (v == 0) return EGERIA_OK;
-    EGO_CUDA(cudaMemset(adamw->ws, 0, 128));
+    EGO_CUDA(cudaMemsetAsync(adamw->ws, 0, 128, adamw->last_stream));
+    EGO_CUDA(cudaStreamSynchronize(adamw->last_stream));
     return static_cast<egeria_status>(v);
 }
 int64_t egeria_adamw_launch_count(const egeria_adamw *adamw) { return adamw ? adamw->launches : 0; }

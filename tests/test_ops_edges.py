@@ -57,3 +57,24 @@ def test_new_handle_waits_for_the_memory_it_is_given():
     assert torch.equal(workspace_of(quiet, size), workspace_of(other, size))
 
 
+def test_device_status_reports_once_and_clears_the_tickets():
+    """A status word and tickets as a call that gave up leaves them, on a stream of its own: reported once, then a split
+    product is whole."""
+    side = torch.cuda.Stream()
+    x, w = rand(300, 4096, seed=1), rand(192, 4096, seed=2, scale=1 / 64)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        o = ops.Ops(ops.egeria_linear_workspace_bytes(300, 4096, 192), DEV)
+        want = o.egeria_linear_forward(x, w)
+        o.check_device_status()
+        words = workspace_of(o, ops.OPS_WORKSPACE_MIN).view(torch.int32)
+        assert not words.any()
+        for _ in range(3):
+            words.fill_(1)
+            words[0] = eg.ERR_TIMEOUT
+            assert o.egeria_ops_device_status() == eg.ERR_TIMEOUT
+            assert o.egeria_ops_device_status() == eg.OK
+            assert torch.equal(o.egeria_linear_forward(x, w), want)
+            assert not words.any()
+
+

@@ -488,7 +488,9 @@ egeria_status egeria_plasticity_create(egeria_ctx **out, int M, const int64_t *d
             (void)cudaGetLastError();  // no pinned memory: keep the equal split
         }
     }
-    cudaError_t e = cudaMemset(ctx->ws + L.status, 0, 256);
+    // the workspace may be memory that earlier work of a stream which the default stream does not wait for still writes to
+    cudaError_t e = cudaDeviceSynchronize();
+    if (e == cudaSuccess) e = cudaMemset(ctx->ws + L.status, 0, 256);
     if (e == cudaSuccess) e = cudaMemset(ctx->ws + L.cta_log, 0, kMaxCtas * sizeof(CtaLog));
     if (e == cudaSuccess) e = cudaMemset(ctx->ws + L.tickets, 0, (size_t)M * sizeof(int32_t));
     if (e == cudaSuccess) e = cudaMemset(ctx->ws + L.fin_ctr, 0, (size_t)2 * M * sizeof(FinCounters));
@@ -1321,7 +1323,9 @@ egeria_status egeria_debug_check_record(egeria_ctx *ctx, int32_t *out_record) {
     if (!ctx || !out_record) return EGERIA_ERR_INVALID_ARG;
     EG_CUDA(cudaStreamSynchronize(ctx->last_stream));
     EG_CUDA(cudaMemcpy(out_record, ctx->ws + ctx->L.status + sizeof(int32_t), 5 * sizeof(int32_t), cudaMemcpyDeviceToHost));
-    EG_CUDA(cudaMemset(ctx->ws + ctx->L.status + sizeof(int32_t), 0, 5 * sizeof(int32_t)));  // the next failure is recorded afresh
+    // the next failure is recorded afresh (cleared in the calls' own stream, which need not wait for the default one)
+    EG_CUDA(cudaMemsetAsync(ctx->ws + ctx->L.status + sizeof(int32_t), 0, 5 * sizeof(int32_t), ctx->last_stream));
+    EG_CUDA(cudaStreamSynchronize(ctx->last_stream));
     return EGERIA_OK;
 }
 
@@ -1331,14 +1335,16 @@ egeria_status egeria_device_status(egeria_ctx *ctx) {
     int32_t word = 0;
     EG_CUDA(cudaMemcpy(&word, ctx->ws + ctx->L.status, sizeof(word), cudaMemcpyDeviceToHost));
     if (word != 0) {
-        // a kernel that gave up leaves its progress counters and tickets half-way: start afresh
-        EG_CUDA(cudaMemset(ctx->ws + ctx->L.fin_ctr, 0, (size_t)2 * ctx->M * sizeof(FinCounters)));
-        EG_CUDA(cudaMemset(ctx->ws + ctx->L.tickets, 0, (size_t)ctx->M * sizeof(int32_t)));
+        // a kernel that gave up leaves its progress counters and tickets half-way: start afresh (in the calls' own
+        // stream, which need not wait for the default one)
+        EG_CUDA(cudaMemsetAsync(ctx->ws + ctx->L.fin_ctr, 0, (size_t)2 * ctx->M * sizeof(FinCounters), ctx->last_stream));
+        EG_CUDA(cudaMemsetAsync(ctx->ws + ctx->L.tickets, 0, (size_t)ctx->M * sizeof(int32_t), ctx->last_stream));
         // ... and partial rows that were written and never read: every slot empty again
-        EG_CUDA(cudaMemset(ctx->ws + ctx->L.slots, 0xff, ctx->L.slot_bytes_cap));
+        EG_CUDA(cudaMemsetAsync(ctx->ws + ctx->L.slots, 0xff, ctx->L.slot_bytes_cap, ctx->last_stream));
         ctx->slots_dirty = false;
         ctx->set_dirty[0] = ctx->set_dirty[1] = 0;
-        EG_CUDA(cudaMemset(ctx->ws + ctx->L.status, 0, sizeof(int32_t)));
+        EG_CUDA(cudaMemsetAsync(ctx->ws + ctx->L.status, 0, sizeof(int32_t), ctx->last_stream));
+        EG_CUDA(cudaStreamSynchronize(ctx->last_stream));
     }
     if (word == kStatusTimeout) return EGERIA_ERR_TIMEOUT;
     if (word == kStatusCheck) return EGERIA_ERR_CHECK;  // (what failed: egeria_debug_check_record)

@@ -78,3 +78,18 @@ def test_device_status_reports_once_and_clears_the_tickets():
             assert not words.any()
 
 
+def test_new_context_waits_for_the_memory_it_is_given():
+    """The same for the plasticity evaluation's workspace: counters, slots and windows start from what creation wrote."""
+    from paper_2201_06227_b200 import workloads as wl
+    ds, b = [4096, 64 * 148], 128
+    pairs = [wl.make_pair(b, d, "relu", 0.2, seed=77 + d, device=DEV) for d in ds]
+    at, ar = [p[0] for p in pairs], [p[1] for p in pairs]
+    quiet = eg.Context(ds, b, 5, 1e-3, device=DEV)
+    want = [t.clone() for t in quiet.egeria_plasticity_evaluate(at, ar)]
+    other = contended(quiet._raw.numel(), lambda: eg.Context(ds, b, 5, 1e-3, device=DEV))
+    got = other.egeria_plasticity_evaluate(at, ar)
+    other.check_device_status()
+    assert got[0].cpu().numpy().tobytes() == want[0].cpu().numpy().tobytes()      # the slopes of a first evaluation may be NaN
+    assert got[1].cpu().numpy().tobytes() == want[1].cpu().numpy().tobytes() and torch.equal(got[2], want[2])
+
+

@@ -7,7 +7,8 @@ kernels of ``libegeria.so``; there is no fallback: a call that the library refus
 
 Results are allocated on the stream that the call runs on.  Where a ``stream`` is given that is
 not the current one, the caller orders it after the kernels that made the inputs, and the inputs
-are recorded on it (their memory is not reused before the call has run).
+are recorded on it (their memory is not reused before the call has run).  What a handle itself holds
+is recorded on every stream that it is called on; it may be dropped with calls in flight.
 """
 from __future__ import annotations
 
@@ -139,7 +140,10 @@ class _Handle:
         if entry is None:
             entry = self._entry[name] = ctypes.cast(getattr(self._lib, name), _vp).value
         if stream is None and torch._C._cuda_getDevice() == self._index:
-            got = native(entry, self._h.value, self._index, torch._C._cuda_getCurrentRawStream(self._index), *args)
+            raw = torch._C._cuda_getCurrentRawStream(self._index)
+            if raw not in self._streams:
+                self._join(raw)
+            got = native(entry, self._h.value, self._index, raw, *args)
         else:
             with _On(self.device, stream, (self._raw, *self._touched(), *(a for a in args if isinstance(a, torch.Tensor)))) as s:
                 got = native(entry, self._h.value, self._index, s, *args)
@@ -150,6 +154,16 @@ class _Handle:
     def _touched(self):
         return ()
 
+    def _join(self, raw: int) -> None:
+        """The first call on another stream than the one that the handle was made on: what the handle holds is recorded on
+        it, so that its memory is not reused before that stream's calls have run, even if the handle is dropped."""
+        if raw in self._streams:
+            return
+        stream = self._streams[raw] = torch.cuda.current_stream(self.device)
+        for t in (self._raw, *self._touched()):
+            if t is not None:
+                t.record_stream(stream)
+
     def _place(self, device) -> None:
         self.device = torch.device(device)
         if self.device.type != "cuda":
@@ -158,6 +172,7 @@ class _Handle:
             self.device = torch.device("cuda", torch.cuda.current_device())
         self._index = self.device.index
         self._entry = {}
+        self._streams = {torch._C._cuda_getCurrentRawStream(self._index): None}   # the ones that have the handle's memory on record
 
     def close(self) -> None:
         if getattr(self, "_h", None):
@@ -312,8 +327,13 @@ class AdamW(_Handle):
     def egeria_adamw_set_grads(self, grads: Sequence[torch.Tensor], stream: Optional[torch.cuda.Stream] = None) -> None:
         """The gradients (same sizes and types) are in these tensors from the next step on."""
         ptrs = self._grad_pointers(grads)
+        if stream is None:
+            self._join(torch._C._cuda_getCurrentRawStream(self._index))
         with _On(self.device, stream, (self._raw,)) as s:
             _check(self._lib.egeria_adamw_set_grads(self._h, s, ptrs), "egeria_adamw_set_grads")
+        for known in self._streams.values():
+            for g in grads if known is not None else ():
+                g.record_stream(known)
 
     def egeria_adamw_step(self, lr: float, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8,
                           grad_scale: Optional[torch.Tensor] = None, frozen: Optional[torch.Tensor] = None,

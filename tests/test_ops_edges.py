@@ -93,3 +93,50 @@ def test_new_context_waits_for_the_memory_it_is_given():
     assert got[1].cpu().numpy().tobytes() == want[1].cpu().numpy().tobytes() and torch.equal(got[2], want[2])
 
 
+@pytest.mark.parametrize("which", ["ops", "adamw"])
+def test_a_dropped_handle_keeps_its_memory_until_its_calls_have_run(which):
+    """A handle made on one stream, called on another that is the current one, and dropped with the call in flight: its
+    workspace is not handed out before that call has run."""
+    side = torch.cuda.Stream()
+    x, w = rand(200, 512, seed=1), rand(256, 512, seed=2)
+    p, g, m, v = ([rand(3000, dtype=torch.float32, seed=k)] for k in range(4))
+    steps = torch.zeros(1, dtype=torch.int32, device=DEV)
+    torch.cuda.synchronize()
+    torch.cuda.empty_cache()
+    h = ops.Ops(ops.egeria_linear_workspace_bytes(200, 512, 256), DEV) if which == "ops" else ops.AdamW(p, g, m, v, steps)
+    place, size = h._raw.data_ptr(), h._raw.numel()
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(100_000_000)         # about 50 ms
+        if which == "ops":
+            h.egeria_linear_forward(x, w)
+        else:
+            h.egeria_adamw_step(1e-3)
+    del h
+    new = [torch.empty(size, dtype=torch.uint8, device=DEV) for _ in range(3)]
+    busy = not side.query()
+    assert busy and place not in {t.data_ptr() for t in new}
+    side.synchronize()
+
+
+def test_new_gradients_are_kept_for_the_streams_of_the_steps():
+    """set_grads on a handle whose steps run on another stream: what it then lets go of is not handed out under a step."""
+    side = torch.cuda.Stream()
+    p, m, v = ([rand(3000, dtype=torch.float32, seed=k)] for k in range(3))
+    torch.cuda.synchronize()
+    torch.cuda.empty_cache()
+    first, second = [torch.ones(3000, device=DEV)], [torch.ones(3000, device=DEV)]
+    a = ops.AdamW(p, first, m, v, torch.zeros(1, dtype=torch.int32, device=DEV))
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        a.egeria_adamw_step(1e-3)
+        a.egeria_adamw_set_grads(second)
+        places = {first[0].data_ptr(), second[0].data_ptr()}
+        torch.cuda._sleep(100_000_000)
+        a.egeria_adamw_step(1e-3)
+    del a, first, second
+    new = [torch.empty(3000, device=DEV) for _ in range(4)]
+    busy = not side.query()
+    assert busy and not places & {t.data_ptr() for t in new}
+    side.synchronize()
+
+

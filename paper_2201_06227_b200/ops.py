@@ -313,16 +313,14 @@ class AdamW(_Handle):
             _check(lib().egeria_adamw_create(ctypes.byref(handle), n, table, self._grad_pointers(grads),
                                              _vector(steps, "steps", dev, torch.int32, n), ptr, nbytes, flags),
                    "egeria_adamw_create")
+        self._grads = list(grads)
         self._h, self._lib, self._destroy, self._native = handle, lib(), lib().egeria_adamw_destroy, _native()
         self._last_module = max(self.modules)
 
     def _grad_pointers(self, grads):
         if len(grads) != len(self._sizes):
             raise ValueError("grads: one entry per tensor is required")
-        ptrs = (_vp * len(grads))(*[_vector(g, f"grads[{i}]", self._index, t, n)
-                                    for i, (g, (n, t)) in enumerate(zip(grads, self._sizes))])
-        self._grads = list(grads)
-        return ptrs
+        return (_vp * len(grads))(*[_vector(g, f"grads[{i}]", self._index, t, n) for i, (g, (n, t)) in enumerate(zip(grads, self._sizes))])
 
     def egeria_adamw_set_grads(self, grads: Sequence[torch.Tensor], stream: Optional[torch.cuda.Stream] = None) -> None:
         """The gradients (same sizes and types) are in these tensors from the next step on."""
@@ -331,6 +329,7 @@ class AdamW(_Handle):
             self._join(torch._C._cuda_getCurrentRawStream(self._index))
         with _On(self.device, stream, (self._raw,)) as s:
             _check(self._lib.egeria_adamw_set_grads(self._h, s, ptrs), "egeria_adamw_set_grads")
+        self._grads = list(grads)      # not before the library has taken them: until then the old ones are in force
         for known in self._streams.values():
             for g in grads if known is not None else ():
                 g.record_stream(known)

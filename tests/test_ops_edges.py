@@ -140,3 +140,25 @@ def test_new_gradients_are_kept_for_the_streams_of_the_steps():
     side.synchronize()
 
 
+def test_refused_gradients_leave_the_old_ones_in_force():
+    """set_grads is refused on a capturing stream: the table still names the old gradients, so the handle keeps them."""
+    p, g, m, v = ([rand(3000, dtype=torch.float32, seed=k, scale=0.1)] for k in range(4))
+    v[0].abs_()
+    a = ops.AdamW(p, g, m, v, torch.zeros(1, dtype=torch.int32, device=DEV))
+    new, x = [torch.zeros(3000, device=DEV)], torch.zeros(8, device=DEV)
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        x.add_(1.0)
+        with pytest.raises(eg.EgeriaError) as e:
+            a.egeria_adamw_set_grads(new)
+    assert e.value.status == eg.ERR_INVALID_ARG
+    want = 0.9 * m[0].double() + 0.1 * g[0].double()
+    size = 0.9 * m[0].double().abs() + 0.1 * g[0].double().abs()
+    kept = weakref.ref(g[0])
+    del g, new
+    assert kept() is not None
+    a.egeria_adamw_step(1e-3)
+    close(m[0], want, 8 * 2.0 ** -24 * size + 1e-37, "m")
+
+

@@ -75,7 +75,8 @@ size_t egeria_linear_workspace_bytes(int64_t rows, int64_t inp, int64_t out);
  *   residual  [rows, out] or NULL; may be y itself (same pointer and pitch)
  *   y         [rows, out]
  *   z         [rows, out] or NULL: the argument of the activation, for the backward call
- * rows may be 0 (nothing is done); inp and out are at least 1; none above 2^31 - 1024. */
+ * Otherwise y and z share no value with an operand or each other (EGERIA_ERR_INVALID_ARG; parts of one buffer that
+ * lie beside each other are fine).  rows may be 0 (nothing is done); inp and out are at least 1; none above 2^31 - 1024. */
 typedef struct {
     int32_t type, act;
     int64_t rows, inp, out;

@@ -361,6 +361,30 @@ static cudaError_t launch_few_any(const Epilogue &e, const egeria_linear_forward
 
 static bool good_matrix(const void *p, int64_t ld, int64_t cols, size_t elem) { return p && aligned(p, elem) && ld >= cols; }
 static bool good_optional(const void *p, int64_t ld, int64_t cols, size_t elem) { return !p || good_matrix(p, ld, cols, elem); }
+
+// Whether two matrices of 2-byte values share one.  Parts of one buffer may lie between each other's rows.
+struct Extent {
+    const void *p;
+    int64_t ld, rows, cols;
+};
+static bool overlap(const Extent &a, const Extent &b) {
+    if (a.rows < b.rows) return overlap(b, a);
+    if (!a.p || !b.p) return false;
+    const int64_t at = (int64_t)(reinterpret_cast<uintptr_t>(b.p) / 2) - (int64_t)(reinterpret_cast<uintptr_t>(a.p) / 2);
+    if (at >= (a.rows - 1) * a.ld + a.cols || -at >= (b.rows - 1) * b.ld + b.cols) return false;
+    if (a.ld == b.ld && b.rows > 1) {
+        // row r of b begins at column `col` of a's row `row` + r and may reach into the next one
+        const int64_t col = (at % a.ld + a.ld) % a.ld, row = (at - col) / a.ld;
+        auto meet = [&](int64_t first) { return first < a.rows && first + b.rows > 0; };
+        return (col < a.cols && meet(row)) || (col + b.cols > a.ld && meet(row + 1));
+    }
+    for (int64_t r = 0; r < b.rows; ++r) {
+        const int64_t from = at + r * b.ld, end = from + b.cols;  // rows of a that end behind `from` and begin before `end`
+        const int64_t first = from < a.cols ? 0 : (from - a.cols) / a.ld + 1;
+        if (end > 0 && first <= std::min(a.rows - 1, (end - 1) / a.ld)) return true;
+    }
+    return false;
+}
 static bool good_act(int act) { return act >= EGERIA_ACT_NONE && act <= EGERIA_ACT_SILU; }
 static egeria_status good_sizes(int64_t rows, int64_t inp, int64_t out) {
     if (rows < 0 || inp < 1 || out < 1) return EGERIA_ERR_INVALID_ARG;
@@ -557,6 +581,13 @@ egeria_status egeria_linear_forward(egeria_ops *ops, void *cuda_stream, const eg
     if (!good_matrix(a.x, a.ldx, a.inp, 2) || !good_matrix(a.w, a.ldw, a.inp, 2) || !good_matrix(a.y, a.ldy, a.out, 2) ||
         !good_optional(a.residual, a.ldr, a.out, 2) || !good_optional(a.z, a.ldz, a.out, 2) || !aligned(a.bias, 2))
         return EGERIA_ERR_INVALID_ARG;
+    // blocks write y and z while others still read; a residual is read where the same thread writes y
+    const Extent y{a.y, a.ldy, a.rows, a.out}, z{a.z, a.ldz, a.rows, a.out};
+    const Extent reads[4] = {{a.x, a.ldx, a.rows, a.inp}, {a.w, a.ldw, a.out, a.inp}, {a.bias, a.out, 1, a.out}, {a.residual, a.ldr, a.rows, a.out}};
+    const bool onto = a.residual == a.y && (a.ldr == a.ldy || a.rows == 1);
+    for (int i = 0; i < 4; ++i)
+        if ((!(i == 3 && onto) && overlap(y, reads[i])) || overlap(z, reads[i])) return EGERIA_ERR_INVALID_ARG;
+    if (overlap(y, z)) return EGERIA_ERR_INVALID_ARG;
     const LinearLayout L = linear_layout(a.rows, a.inp, a.out);
     if (ops->ws_bytes < L.total) return EGERIA_ERR_WORKSPACE;
     cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);

@@ -204,7 +204,7 @@ class Ops(_Handle):
                               residual: Optional[torch.Tensor] = None, save_z: bool = False, out: Optional[torch.Tensor] = None,
                               stream: Optional[torch.cuda.Stream] = None):
         """y = act(x w^T + bias) + residual for x [rows, inp] and w [out, inp] in bfloat16 or float16; (y, z) with
-        save_z, z the argument of the activation.  `out` may be the residual."""
+        save_z, z the argument of the activation.  `out` may be the residual; it is refused where it overlaps anything else."""
         if act not in ACTS:
             raise ValueError(f"unknown activation {act!r}")
         return self._call("egeria_linear_forward", self._native.linear_forward, stream, (x, w, bias, ACTS[act], residual, save_z, out))

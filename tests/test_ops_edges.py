@@ -162,3 +162,45 @@ def test_refused_gradients_leave_the_old_ones_in_force():
     close(m[0], want, 8 * 2.0 ** -24 * size + 1e-37, "m")
 
 
+# ----------------------------------------------------------------------------- operands that overlap
+
+def test_linear_refuses_an_output_that_overlaps_what_it_reads():
+    o = ops.Ops(ops.egeria_linear_workspace_bytes(300, 64, 64), DEV)
+    for rows in (3, 300):
+        x, w, r = rand(rows, 64, seed=1), rand(64, 64, seed=2), rand(rows + 1, 64, seed=3)
+        for bad in (dict(out=x), dict(out=x, residual=x), dict(residual=r[:-1], out=r[1:])):
+            before = {k: t.clone() for k, t in bad.items()}
+            with pytest.raises(eg.EgeriaError) as e:
+                o.egeria_linear_forward(x, w, **bad)
+            assert e.value.status == eg.ERR_INVALID_ARG
+            assert all(torch.equal(bad[k], before[k]) for k in bad)
+        both = torch.cat([w, rand(rows, 64, seed=4)])
+        with pytest.raises(eg.EgeriaError):
+            o.egeria_linear_forward(x, both[:64], out=both[63:63 + rows])
+        bias = rand(rows * 64, seed=5)
+        with pytest.raises(eg.EgeriaError):
+            o.egeria_linear_forward(x, w, bias=bias[-64:], out=bias.view(rows, 64))
+
+
+def test_linear_takes_operands_that_share_a_buffer_without_overlapping():
+    """Columns of one buffer: input and output side by side, a residual between them, and different pitches."""
+    rows = 150
+    o = ops.Ops(ops.egeria_linear_workspace_bytes(rows, 64, 64), DEV)
+    w = rand(64, 64, seed=2, scale=0.1)
+    buf = rand(rows, 192, seed=1)
+    x, r, y = buf[:, :64], buf[:, 64:128], buf[:, 128:]
+    want = o.egeria_linear_forward(x.clone(), w, residual=r.clone())
+    assert o.egeria_linear_forward(x, w, residual=r, out=y) is not None and torch.equal(y, want)
+    o.egeria_linear_forward(x, w, residual=r, out=r)
+    assert torch.equal(r, want)
+    # rows of 64 every 192 values, and the output in the 65th of every second one's 128 gaps (a pitch of 384)
+    buf = rand(2 * rows, 192, seed=7)
+    y = buf.view(rows, 384)[:, 100:164]
+    x = buf[:rows, :64]
+    want = o.egeria_linear_forward(x.clone(), w)
+    o.egeria_linear_forward(x, w, out=y)
+    assert torch.equal(y, want)
+    with pytest.raises(eg.EgeriaError):
+        o.egeria_linear_forward(x, w, out=buf.view(rows, 384)[:, 150:214])       # 22 columns into every second row of x
+
+

@@ -65,8 +65,9 @@ typedef enum {
     EGERIA_ACT_SILU = 4       /* z / (1 + exp(-z)) */
 } egeria_act;
 
-/* Bytes of workspace that both linear calls of a layer with these sizes fit into, whatever the
- * alignment of their operands.  Pure host arithmetic; 0 for invalid arguments. */
+/* Bytes of workspace that both linear calls of a layer with these sizes, or with smaller ones, fit into, whatever the
+ * alignment of their operands.  Pure host arithmetic; 0 for invalid arguments.  (The forward call of up to 4 rows needs
+ * none, up to 49152 / rows values of a row (rows = 3 counting as 4).) */
 size_t egeria_linear_workspace_bytes(int64_t rows, int64_t inp, int64_t out);
 
 /* z = x w^T + bias,  y = act(z) + residual.
@@ -113,7 +114,7 @@ typedef enum { EGERIA_NORM_LAYER = 0, EGERIA_NORM_RMS = 1 } egeria_norm_kind;
 
 #define EGERIA_NORM_MAX_COLS 8192
 
-/* Bytes of workspace that both norm calls with these sizes fit into.  Pure host arithmetic; 0 for
+/* Bytes of workspace that both norm calls with these sizes, or with smaller ones, fit into.  Pure host arithmetic; 0 for
  * invalid arguments. */
 size_t egeria_norm_workspace_bytes(int64_t rows, int64_t cols);
 

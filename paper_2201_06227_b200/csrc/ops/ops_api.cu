@@ -32,7 +32,7 @@ constexpr size_t kAlign = 256;
 constexpr size_t kHeadBytes = EGERIA_OPS_WORKSPACE_MIN;  // status word, then the tickets of split products
 constexpr size_t kTicketOff = 256;
 constexpr int kMaxTickets = (int)((kHeadBytes - kTicketOff) / 4);
-constexpr int kMaxSplitCtas = 320;                       // CTAs' worth of partial tiles at most
+constexpr int kMaxSplitCtas = 160;                       // CTAs' worth of partial tiles at most
 constexpr uint64_t kWaitLimitNs = 2000000000ull;
 constexpr int64_t kMaxSize = ((int64_t)1 << 31) - 1024;  // tile coordinates are 32-bit
 constexpr int kSms = 148;                                // what workspaces are sized for
@@ -108,12 +108,12 @@ static GemmPlan plan_gemm(int64_t m, int64_t n, int64_t k, int sms) {
 }
 static_assert(2 * kMaxSplitCtas * kEpiWarps <= kMaxTickets, "a ticket for every warp of every split tile of two products");
 
-// Bytes of partial tiles that a product of these sizes may need under any plan.
+// Bytes of partial tiles that a product of these sizes, or of smaller ones, may need under any plan.  (A product of more
+// tiles than CTAs is not split, but a smaller one in its place is: the bound must not fall as a size grows.)
 static size_t split_bytes(int64_t m, int64_t n, int64_t k) {
     const int64_t kblocks = std::min<int64_t>((k + kGemmK - 1) / kGemmK, 64);
     if (kblocks <= 1) return 0;
-    const int64_t tiles = ((m + 255) / 256) * 2 * ((n + 255) / 256);  // of 128 x 256
-    if (tiles > kMaxSplitCtas) return 0;
+    const int64_t tiles = std::min<int64_t>(((m + 255) / 256) * 2 * ((n + 255) / 256), kMaxSplitCtas);  // of 128 x 256
     return (size_t)std::min<int64_t>(tiles * kblocks, kMaxSplitCtas) * 128 * 256 * 4;
 }
 
@@ -122,6 +122,8 @@ static int slope_runs(int64_t rows, int64_t cols) {
     const int64_t strips = (cols + 255) / 256;
     return (int)std::max<int64_t>(1, std::min<int64_t>((rows + 31) / 32, 4 * kSms / strips));
 }
+// Values of their partial sums at most, for these sizes and all smaller ones (runs * cols <= 4 * kSms * 256 beyond one run).
+static int64_t slope_sums(int64_t rows, int64_t cols) { return std::max(cols, std::min<int64_t>((rows + 31) / 32 * cols, 4 * kSms * 256)); }
 
 struct LinearLayout {
     size_t part, part2, x, w, dz, sums, total;
@@ -139,7 +141,7 @@ static LinearLayout linear_layout(int64_t rows, int64_t inp, int64_t out) {
     L.x = take((size_t)rows * pad8(inp) * 2);
     L.w = take((size_t)out * pad8(inp) * 2);
     L.dz = take((size_t)rows * pad8(out) * 2);
-    L.sums = take((size_t)slope_runs(rows, out) * out * 4);
+    L.sums = take((size_t)slope_sums(rows, out) * 4);
     L.total = off;
     return L;
 }
@@ -157,6 +159,11 @@ static NormPlan norm_backward_plan(int64_t rows, int64_t cols) {
     else if (cols > 256) n = {64, 8};
     n.ctas = (int)std::max<int64_t>(std::min<int64_t>(rows, 1), std::min<int64_t>(rows / 2, (int64_t)n.ctas * kSms));
     return n;
+}
+// CTAs times columns at most, for these sizes and all smaller ones: 4096 columns' worth per SM (less of it between the
+// teams' widths), beyond that one CTA per SM.
+static int64_t norm_sums_cols(int64_t rows, int64_t cols) {
+    return std::min(std::max<int64_t>(std::min<int64_t>(rows, 1), rows / 2) * cols, kSms * std::max<int64_t>(4096, cols));
 }
 
 }  // namespace ops
@@ -588,8 +595,10 @@ egeria_status egeria_linear_forward(egeria_ops *ops, void *cuda_stream, const eg
     for (int i = 0; i < 4; ++i)
         if ((!(i == 3 && onto) && overlap(y, reads[i])) || overlap(z, reads[i])) return EGERIA_ERR_INVALID_ARG;
     if (overlap(y, z)) return EGERIA_ERR_INVALID_ARG;
+    const int few_rows = a.rows <= 2 ? (int)a.rows : 4;
+    const bool few = a.rows <= kFewRows && (a.inp + 255) / 256 * 256 * 2 * few_rows <= kFewSmem;  // needs no workspace
     const LinearLayout L = linear_layout(a.rows, a.inp, a.out);
-    if (ops->ws_bytes < L.total) return EGERIA_ERR_WORKSPACE;
+    if (!few && ops->ws_bytes < L.total) return EGERIA_ERR_WORKSPACE;
     cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
     ops->last_stream = stream;
     Epilogue e{};
@@ -601,8 +610,7 @@ egeria_status egeria_linear_forward(egeria_ops *ops, void *cuda_stream, const eg
     e.z = a.z;
     e.ldz = a.ldz;
     e.act = a.act;
-    const int few_rows = a.rows <= 2 ? (int)a.rows : 4;
-    if (a.rows <= kFewRows && (a.inp + 255) / 256 * 256 * 2 * few_rows <= kFewSmem) {
+    if (few) {
         const bool wide = a.inp % 8 == 0 && a.ldw % 8 == 0 && aligned(a.w, 16);
         EGO_CUDA(a.type == EGERIA_BF16 ? launch_few_any<bf16>(e, a, wide, ops->sms, stream) : launch_few_any<f16>(e, a, wide, ops->sms, stream));
         ++ops->launches;
@@ -705,7 +713,7 @@ egeria_status egeria_linear_backward(egeria_ops *ops, void *cuda_stream, const e
 // ---------------------------------------------------------------- norms
 size_t egeria_norm_workspace_bytes(int64_t rows, int64_t cols) {
     if (rows < 0 || cols < 1 || cols > EGERIA_NORM_MAX_COLS) return 0;
-    return kHeadBytes + up((size_t)norm_backward_plan(rows, cols).ctas * kNormSums * cols * 4, 1024);
+    return kHeadBytes + up((size_t)norm_sums_cols(rows, cols) * kNormSums * 4, 1024);
 }
 
 egeria_status egeria_norm_forward(egeria_ops *ops, void *cuda_stream, const egeria_norm_forward_args *args) {

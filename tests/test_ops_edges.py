@@ -204,3 +204,38 @@ def test_linear_takes_operands_that_share_a_buffer_without_overlapping():
         o.egeria_linear_forward(x, w, out=buf.view(rows, 384)[:, 150:214])       # 22 columns into every second row of x
 
 
+# ----------------------------------------------------------------------------- sizes
+
+@pytest.mark.parametrize("most,rows", [((13824, 768, 768), (1, 5, 1280, 5000, 13568)), ((10496, 1024, 1024), (768, 10240)),
+                                       ((41000, 256, 256), (40000, 300))])
+def test_linear_handle_takes_smaller_calls(most, rows):
+    """A ragged last batch on the handle of the whole one."""
+    o = ops.Ops(ops.egeria_linear_workspace_bytes(*most), DEV)
+    _, inp, out = most
+    w = rand(out, inp, seed=2, scale=inp ** -0.5)
+    for n in rows:
+        x, dy = rand(n, inp, seed=n), rand(n, out, seed=n + 1)
+        own = ops.Ops(ops.egeria_linear_workspace_bytes(n, inp, out), DEV)
+        assert torch.equal(o.egeria_linear_forward(x, w, act="relu"), own.egeria_linear_forward(x, w, act="relu"))
+        for a, b in zip(o.egeria_linear_backward(dy, x, w), own.egeria_linear_backward(dy, x, w)):
+            assert torch.equal(a, b)
+    o.check_device_status()
+
+
+@pytest.mark.parametrize("most,least", [(1025, 1024), (257, 256), (513, 300)])
+def test_norm_handle_takes_fewer_columns(most, least):
+    o = ops.Ops(ops.egeria_norm_workspace_bytes(9000, most), DEV)
+    x, w = rand(9000, least, seed=1), rand(least, seed=2)
+    y, h, st = o.egeria_norm_forward(x, x, w_pre=w)
+    got = o.egeria_norm_backward(x, x, y, x, st, w_pre=w)
+    own = ops.Ops(ops.egeria_norm_workspace_bytes(9000, least), DEV).egeria_norm_backward(x, x, y, x, st, w_pre=w)
+    assert all(torch.equal(got[k], own[k]) for k in ("dx", "df", "dw_pre"))
+
+
+@pytest.mark.parametrize("rows", [1, 2, 4])
+def test_linear_of_a_few_rows_needs_no_workspace(rows):
+    x, w = rand(rows, 1024, seed=1), rand(4096, 1024, seed=2, scale=1 / 32)
+    own = ops.Ops(ops.egeria_linear_workspace_bytes(rows, 1024, 4096), DEV)
+    assert torch.equal(ops.Ops(device=DEV).egeria_linear_forward(x, w), own.egeria_linear_forward(x, w))
+
+

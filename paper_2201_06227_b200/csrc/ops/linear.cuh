@@ -753,8 +753,10 @@ __global__ void __launch_bounds__(256) linear_few_kernel(const Epilogue p, int32
         xs[i] = (r < rows && c < k) ? x[r * ldx + c] : from_f32<T>(0.0f);
     }
     __syncthreads();
-    const int lane = threadIdx.x & 31, warps = gridDim.x * 8;
-    for (int n = blockIdx.x * 8 + (threadIdx.x >> 5); n < n_cols; n += warps) {
+    const int lane = threadIdx.x & 31;
+    const uint32_t warps = gridDim.x * 8;
+    // (unsigned: past the last of 2^31 - 1024 columns a warp's next turn needs the 32nd bit)
+    for (uint32_t n = blockIdx.x * 8 + (threadIdx.x >> 5); n < (uint32_t)n_cols; n += warps) {
         const T *wr = w + (int64_t)n * ldw;
         float acc[ROWS];
 #pragma unroll

@@ -239,3 +239,14 @@ def test_linear_of_a_few_rows_needs_no_workspace(rows):
     assert torch.equal(ops.Ops(device=DEV).egeria_linear_forward(x, w), own.egeria_linear_forward(x, w))
 
 
+def test_linear_of_one_row_with_the_most_outputs():
+    """2^31 - 1024 outputs: the column of a warp's next turn passes 31 bits."""
+    n = 2 ** 31 - 1024
+    x = torch.full((1, 1), 3.0, dtype=torch.bfloat16, device=DEV)
+    w = torch.full((n, 1), 0.5, dtype=torch.bfloat16, device=DEV)
+    w[-1] = 2.0
+    y = ops.Ops(device=DEV).egeria_linear_forward(x, w)
+    assert y.shape == (1, n) and float(y[0, -1]) == 6.0 and float(y[0, 0]) == 1.5
+    assert all((part == 1.5).all() for part in y[0, :-1].split(2 ** 28))
+
+

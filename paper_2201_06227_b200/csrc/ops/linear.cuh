@@ -220,10 +220,11 @@ __device__ __forceinline__ float act_slope(float z) {
         return fmaf(0.39894228040143268f * z, e, phi);
     }
     if (ACT == kActGeluTanh) {
-        const float q = z * z;
+        // p + z p (1 - p) u', u' = A (1 + 3 B z^2).  From |z| = 100 on p is 0 or 1, whatever the square: held there, and with
+        // p (1 - p) = 0 as the first factor, no part of the product overflows for a finite z
+        const float q = fminf(z * z, 1e4f);
         const float p = logistic2(z * fmaf(-kLog2e * kGeluA * kGeluB, q, -kLog2e * kGeluA));
-        // p + z p (1 - p) u', u' = A (1 + 3 B z^2)
-        return fmaf(p * (1.0f - p), z * fmaf(3.0f * kGeluA * kGeluB, q, kGeluA), p);
+        return fmaf(p * (1.0f - p) * z, fmaf(3.0f * kGeluA * kGeluB, q, kGeluA), p);
     }
     if (ACT == kActSilu) {
         const float p = logistic2(-kLog2e * z);

@@ -250,3 +250,26 @@ def test_linear_of_one_row_with_the_most_outputs():
     assert all((part == 1.5).all() for part in y[0, :-1].split(2 ** 28))
 
 
+# ----------------------------------------------------------------------------- values at the ends
+
+@pytest.mark.parametrize("act", ["relu", "gelu", "gelu_tanh", "silu"])
+@pytest.mark.parametrize("inner", [False, True])
+def test_slopes_of_huge_values(act, inner):
+    """Where the argument is finite, however large, so is the slope (0 or 1 exactly from 1e3 on): through dz (act) and through
+    dx's epilogue (act_in)."""
+    n = 64
+    sizes = torch.tensor([40.0, 1e3, 1e9, 1e12, 2e13, 1e15, 1e19, 3e19, 1e25, 3e38], device=DEV)
+    z = torch.cat([sizes, -sizes]).repeat(n * n)[:n * n].view(n, n).to(torch.bfloat16)
+    dy = rand(n, n, seed=3)
+    eye = torch.eye(n, dtype=torch.bfloat16, device=DEV)
+    o = ops.Ops(ops.egeria_linear_workspace_bytes(n, n, n), DEV)
+    kw = dict(z_in=z, act_in=act) if inner else dict(z=z, act=act)
+    dx, _, db = o.egeria_linear_backward(dy, eye, eye, **kw)
+    ref = dy.double() * act64(z.double(), act)[1]
+    close(dx, ref, (U[dx.dtype] + 2.0 ** -14) * ref.abs(), "dx")
+    far = z.abs() >= 1e3
+    assert torch.equal(dx[far], torch.where(z > 0, dy, torch.zeros_like(dy))[far])
+    if not inner:
+        close(db, ref.sum(0), U[db.dtype] * ref.sum(0).abs() + (n + 8) * 2.0 ** -23 * ref.abs().sum(0), "db")
+
+

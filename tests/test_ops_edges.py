@@ -273,3 +273,27 @@ def test_slopes_of_huge_values(act, inner):
         close(db, ref.sum(0), U[db.dtype] * ref.sum(0).abs() + (n + 8) * 2.0 ** -23 * ref.abs().sum(0), "db")
 
 
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("act", ["gelu", "gelu_tanh", "silu"])
+@pytest.mark.parametrize("rows", [4, 500])
+def test_activations_alone(rows, act, dtype):
+    """x times the identity is x itself: what is left is the activation's own error, 2^-15 of the value (next to the zero of
+    a slope, of its two terms), and one rounding.  The approximate units take what is below 2^-126 for zero, so
+    that a value below |z| 2^-126 may be one."""
+    n = 64
+    z = torch.linspace(-12.0, 12.0, rows * n, device=DEV).to(dtype).view(rows, n)
+    eye = torch.eye(n, dtype=dtype, device=DEV)
+    o = ops.Ops(ops.egeria_linear_workspace_bytes(rows, n, n), DEV)
+    zd = z.double()
+    ref, slope = act64(zd, act)
+    floor = TINY[dtype] + zd.abs() * 2.0 ** -126
+    close(o.egeria_linear_forward(z, eye, act=act), ref, (U[dtype] + 2.0 ** -15) * ref.abs() + floor, "value")
+    # the slope, of p + q: through dz and through dx's epilogue
+    p = torch.where(zd == 0, torch.full_like(zd, 0.5), ref / zd)
+    terms = p.abs() + (slope - p).abs()
+    one = torch.ones_like(z)
+    tol = U[dtype] * slope.abs() + 2.0 ** -15 * terms + TINY[dtype] + (1 + zd * zd) * 2.0 ** -126
+    close(o.egeria_linear_backward(one, None, eye, z=z, act=act, need_dw=False)[0], slope, tol, "slope")
+    close(o.egeria_linear_backward(one, None, eye, z_in=z, act_in=act, need_dw=False)[0], slope, tol, "slope in the epilogue")
+
+

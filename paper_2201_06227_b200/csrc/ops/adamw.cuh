@@ -63,7 +63,7 @@ struct AdamStep {   // what a tensor's values need beside themselves
 };
 
 __device__ __forceinline__ float adam_param(const AdamStep &s, float p, float m, float v) {
-    return fmaf(p, s.decay, -s.rate * m * fast_rcp(fmaf(fast_sqrt(v), s.root, s.eps)));
+    return fmaf(p, s.decay, -s.rate * m * fast_rcp(fmaf(full_sqrt(v), s.root, s.eps)));
 }
 
 // A code's byte becomes a float, and a float a code's byte, by the bits of 2^23 + code (1.5 * 2^23 + code): the units that
@@ -105,7 +105,7 @@ __device__ __forceinline__ void adam_codes(const AdamStep &s, const F2 (&g)[4], 
         const F2 vi = add_apart(b2 * (old_root * old_root), r2 * gi * gi);
         const float2 ms = split(mi), vs = split(vi);
         m[2 * k] = ms.x, m[2 * k + 1] = ms.y, v[2 * k] = vs.x, v[2 * k + 1] = vs.y;
-        root[2 * k] = fast_sqrt(vs.x), root[2 * k + 1] = fast_sqrt(vs.y);
+        root[2 * k] = full_sqrt(vs.x), root[2 * k + 1] = full_sqrt(vs.y);
         const float2 d = split(fma2(f2(root[2 * k], root[2 * k + 1]), f2(s.root), f2(s.eps)));
         p[k] = fma2(p[k], f2(s.decay), f2(-s.rate) * mi * f2(fast_rcp(d.x), fast_rcp(d.y)));
         top_m = max_nan(max_nan(top_m, fabsf(ms.x)), fabsf(ms.y));

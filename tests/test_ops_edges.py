@@ -297,3 +297,22 @@ def test_activations_alone(rows, act, dtype):
     close(o.egeria_linear_backward(one, None, eye, z_in=z, act_in=act, need_dw=False)[0], slope, tol, "slope in the epilogue")
 
 
+@pytest.mark.parametrize("bits", [32, 8])
+def test_adamw_of_second_moments_below_the_normal_range(bits):
+    """Without an eps to hide it: a second moment of 1e-41 has a root.  It is held to 2^-149, so v is off by three units of
+    that after its products and its sum, and the root by half of what v is off relatively."""
+    n = 3000
+    g = rand(n, dtype=torch.float32, seed=1).sign() * 1e-19 * (1 + torch.rand(n, device=DEV))
+    kinds = (torch.float32, torch.float32) if bits == 32 else (torch.int8, torch.uint8)
+    p, m, v = rand(n, dtype=torch.float32, seed=2), *(torch.zeros(n, dtype=t, device=DEV) for t in kinds)
+    scales = {} if bits == 32 else {k: [torch.zeros(-(-n // 256), device=DEV)] for k in ("m_scales", "v_scales")}
+    before, gd = p.double(), g.double()
+    a = ops.AdamW([p], [g], [m], [v], torch.zeros(1, dtype=torch.int32, device=DEV), **scales)
+    a.egeria_adamw_step(1e-2, 0.9, 0.999, eps=0.0)
+    if bits == 32:
+        close(v, 0.001 * gd * gd, 3 * 2.0 ** -149 + 2.0 ** -20 * 0.001 * gd * gd, "v")
+    change = 1e-2 * gd.sign()                 # m and v corrected for the first step are g and g^2
+    off = 3 * 2.0 ** -149 / (0.001 * gd * gd) + 2.0 ** -19
+    close(p, before - change, 1e-2 * off + 2.0 ** -22 * before.abs(), "param")
+
+

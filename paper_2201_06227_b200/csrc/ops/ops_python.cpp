@@ -6,6 +6,7 @@
 // and return the results, or the library's status as a number if that is not EGERIA_OK.
 #include <ATen/ops/empty.h>
 #include <torch/csrc/Exceptions.h>
+#include <torch/csrc/autograd/functions/basic_ops.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include "../../../include/egeria_ops.h"
@@ -103,6 +104,22 @@ PyObject *wrap(const Tensor &t) {
     return THPVariable_Wrap(t);
 }
 
+// An argument that autograd follows, of those (tensors or None, as has been checked) at the given places.
+const Tensor *followed(const Call &c, std::initializer_list<int> places) {
+    if (at::GradMode::is_enabled())
+        for (int i : places)
+            if (c.given(i) && THPVariable_Unpack(c.rest[i]).requires_grad()) return &THPVariable_Unpack(c.rest[i]);
+    return nullptr;
+}
+// A result of a forward call.  The calls keep no history for autograd, whose user would find a gradient left out in silence:
+// where it follows an argument, going back through the result is an error that names the call which has the gradients.
+PyObject *wrap(const Tensor &t, const Tensor *argument, const char *backward) {
+    if (!argument || !t.defined()) return wrap(t);
+    const auto fn = std::make_shared<torch::autograd::DelayedError>(
+        std::string("the library's calls keep no history: the gradients are the results of ") + backward + " (torch.no_grad() where none is wanted)", 2);
+    return wrap((*fn)({*argument, t})[1]);
+}
+
 // x, w, bias, act, residual, save_z, out -> y or (y, z)
 PyObject *linear_forward(PyObject *, PyObject *const *args, Py_ssize_t n) {
     HANDLE_TH_ERRORS
@@ -125,8 +142,11 @@ PyObject *linear_forward(PyObject *, PyObject *const *args, Py_ssize_t n) {
     if (z.defined()) a.z = z.data_ptr(), a.ldz = a.out;
     const egeria_status s = reinterpret_cast<decltype(&egeria_linear_forward)>(c.fn)(static_cast<egeria_ops *>(c.handle), c.stream, &a);
     if (s != EGERIA_OK) return PyLong_FromLong(s);
-    if (!z.defined()) return wrap(y);
-    return Py_BuildValue("(NN)", wrap(y), wrap(z));
+    if (c.given(6) && !y.is_inference()) y.unsafeGetTensorImpl()->bump_version();   // written in place
+    const char *const back = "egeria_linear_backward";
+    const Tensor *const from = followed(c, {0, 1, 2, 4});
+    if (!z.defined()) return wrap(y, from, back);
+    return Py_BuildValue("(NN)", wrap(y, from, back), wrap(z, from, back));
     END_HANDLE_TH_ERRORS
 }
 
@@ -201,7 +221,9 @@ PyObject *norm_forward(PyObject *, PyObject *const *args, Py_ssize_t n) {
     a.stats = static_cast<float *>(stats.data_ptr());
     const egeria_status s = reinterpret_cast<decltype(&egeria_norm_forward)>(c.fn)(static_cast<egeria_ops *>(c.handle), c.stream, &a);
     if (s != EGERIA_OK) return PyLong_FromLong(s);
-    return Py_BuildValue("(NNN)", wrap(y), wrap(h), wrap(stats));
+    const char *const back = "egeria_norm_backward";
+    const Tensor *const from = followed(c, {0, 1, 2, 3, 4, 5, 6});
+    return Py_BuildValue("(NNN)", wrap(y, from, back), wrap(h, from, back), wrap(stats, from, back));
     END_HANDLE_TH_ERRORS
 }
 

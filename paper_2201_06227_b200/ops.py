@@ -9,6 +9,11 @@ Results are allocated on the stream that the call runs on.  Where a ``stream`` i
 not the current one, the caller orders it after the kernels that made the inputs, and the inputs
 are recorded on it (their memory is not reused before the call has run).  What a handle itself holds
 is recorded on every stream that it is called on; it may be dropped with calls in flight.
+
+Autograd does not follow the calls: the gradients are the results of the ``*_backward`` methods.  Where it follows an
+input of a forward call, going back through the result raises an error (under ``torch.no_grad()`` results are plain
+tensors).  ``out`` and the parameters that require grad when an :class:`AdamW` is made get a new version when a call
+writes to them (frozen ones too: the mask is not read on the host; a replayed graph raises none).
 """
 from __future__ import annotations
 
@@ -316,6 +321,7 @@ class AdamW(_Handle):
         self._grads = list(grads)
         self._h, self._lib, self._destroy, self._native = handle, lib(), lib().egeria_adamw_destroy, _native()
         self._last_module = max(self.modules)
+        self._followed = [p for p in params if p.requires_grad]
 
     def _grad_pointers(self, grads):
         if len(grads) != len(self._sizes):
@@ -339,6 +345,8 @@ class AdamW(_Handle):
                           stream: Optional[torch.cuda.Stream] = None) -> None:
         """One step of every tensor whose module is not marked in `frozen` (uint8, as egeria_plasticity_evaluate leaves it)."""
         self._call("egeria_adamw_step", self._native.adamw_step, stream, (lr, beta1, beta2, eps, grad_scale, frozen, self._last_module))
+        if self._followed:
+            torch.autograd.graph.increment_version(self._followed)
 
     def _touched(self):
         return [self._steps, *self._grads, *(t for column in self._keep for t in column)]

@@ -316,3 +316,46 @@ def test_adamw_of_second_moments_below_the_normal_range(bits):
     close(p, before - change, 1e-2 * off + 2.0 ** -22 * before.abs(), "param")
 
 
+# ----------------------------------------------------------------------------- autograd around the calls
+
+def test_results_say_that_they_have_no_gradient():
+    """Where an input requires grad, going back through a call's result is an error, not a gradient that is left out."""
+    o = ops.Ops(max(ops.egeria_linear_workspace_bytes(8, 64, 64), ops.egeria_norm_workspace_bytes(8, 64)), DEV)
+    x, w = rand(8, 64, seed=1), rand(64, 64, seed=2)
+    plain = o.egeria_linear_forward(x, w, save_z=True)
+    assert not any(t.requires_grad for t in plain)
+    for hot in (dict(x=x.clone().requires_grad_(), w=w), dict(x=x, w=w.clone().requires_grad_())):
+        y, z = o.egeria_linear_forward(**hot, save_z=True)
+        assert torch.equal(y, plain[0]) and torch.equal(z, plain[1])
+        for out in (y, z):
+            with pytest.raises(RuntimeError, match="egeria_linear_backward"):
+                (hot["x"].float().sum() + hot["w"].float().sum() + out.float().sum()).backward()
+        with torch.no_grad():
+            assert not o.egeria_linear_forward(**hot).requires_grad
+    h = x.clone().requires_grad_()
+    y, n, st = o.egeria_norm_forward(h, x)
+    for out in (y, n, st):
+        with pytest.raises(RuntimeError, match="egeria_norm_backward"):
+            out.float().sum().backward()
+    # gradients of the gradient calls are nobody's: plain tensors, as before
+    assert not any(t.requires_grad for t in o.egeria_linear_backward(x, hot["x"], hot["w"]))
+
+
+def test_in_place_results_raise_the_version():
+    """Autograd's check of the tensors it has saved sees that a call has written to them."""
+    o = ops.Ops(ops.egeria_linear_workspace_bytes(8, 64, 64), DEV)
+    x, w, out = rand(8, 64, seed=1), rand(64, 64, seed=2), rand(8, 64, seed=3)
+    a = torch.ones(8, 64, device=DEV, dtype=torch.bfloat16, requires_grad=True)
+    product = a * out
+    o.egeria_linear_forward(x, w, out=out)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        product.sum().backward()
+    p = torch.nn.Parameter(rand(512, dtype=torch.float32, seed=4))
+    loss = (p * p).sum()
+    opt = ops.AdamW([p], [torch.ones(512, device=DEV)], [torch.zeros(512, device=DEV)], [torch.zeros(512, device=DEV)],
+                    torch.zeros(1, dtype=torch.int32, device=DEV))
+    opt.egeria_adamw_step(1e-3)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        loss.backward()
+
+

@@ -253,13 +253,14 @@ class Ops(_Handle):
         return dict(zip(("dx", "df", "dgate", "dw_post", "db_post", "dw_pre", "db_pre"), got))
 
     def egeria_ops_device_status(self) -> int:
-        return int(lib().egeria_ops_device_status(self._h))
+        with torch.cuda.device(self.device):
+            return int(self._lib.egeria_ops_device_status(self._h))
 
     def check_device_status(self) -> None:
         _check(self.egeria_ops_device_status(), "egeria_ops_device_status")
 
     def egeria_ops_launch_count(self) -> int:
-        return int(lib().egeria_ops_launch_count(self._h))
+        return int(self._lib.egeria_ops_launch_count(self._h))
 
 
 class AdamW(_Handle):
@@ -352,10 +353,11 @@ class AdamW(_Handle):
         return [self._steps, *self._grads, *(t for column in self._keep for t in column)]
 
     def egeria_adamw_device_status(self) -> int:
-        return int(lib().egeria_adamw_device_status(self._h))
+        with torch.cuda.device(self.device):
+            return int(self._lib.egeria_adamw_device_status(self._h))
 
     def check_device_status(self) -> None:
         _check(self.egeria_adamw_device_status(), "egeria_adamw_device_status")
 
     def egeria_adamw_launch_count(self) -> int:
-        return int(lib().egeria_adamw_launch_count(self._h))
+        return int(self._lib.egeria_adamw_launch_count(self._h))

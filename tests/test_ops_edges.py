@@ -359,3 +359,20 @@ def test_in_place_results_raise_the_version():
         loss.backward()
 
 
+def test_a_handle_talks_to_the_library_it_was_made_with(monkeypatch):
+    o = ops.Ops(ops.egeria_linear_workspace_bytes(8, 64, 64), DEV)
+    p, g, m, v = ([rand(300, dtype=torch.float32, seed=k)] for k in range(4))
+    a = ops.AdamW(p, g, m, v, torch.zeros(1, dtype=torch.int32, device=DEV))
+
+    def other():
+        raise AssertionError("the library in force now may be another one")
+
+    monkeypatch.setattr(ops, "lib", other)
+    o.egeria_linear_forward(rand(8, 64), rand(64, 64))
+    o.check_device_status()
+    a.egeria_adamw_set_grads(g)
+    a.egeria_adamw_step(1e-3)
+    a.check_device_status()
+    assert o.egeria_ops_launch_count() >= 1 and a.egeria_adamw_launch_count() == 1
+
+

@@ -55,6 +55,12 @@ egeria_status egeria_ops_device_status(egeria_ops *ops);
 /* Number of kernels launched through this handle so far. */
 int64_t egeria_ops_launch_count(const egeria_ops *ops);
 
+/* Test hook: in the next matrix product on the tensor cores through this handle the first thread block (or pair of them)
+ * issues no loads (kind 1) or stops after its first stage (kind 2), and every wait is limited to a millisecond: the kernel
+ * returns, that call's results are not valid, egeria_ops_device_status reports EGERIA_ERR_TIMEOUT once, and the handle can be
+ * used again.  kind 0 takes the request back. */
+egeria_status egeria_ops_debug_stall_next(egeria_ops *ops, int kind);
+
 /* ---------------------------------------------------------------------------- linear layers */
 
 typedef enum {

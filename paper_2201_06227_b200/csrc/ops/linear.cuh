@@ -72,6 +72,7 @@ struct GemmParams {
 
     int32_t fill;                    // units of the second product that each worker without a last unit of the first takes before the rest
     uint32_t is_f16;
+    uint32_t stall;                  // test hook: the first worker issues no loads (1), or no MMA after its first stage (2)
     int32_t *status;
     uint64_t wait_limit_ns;
 };
@@ -490,6 +491,7 @@ __global__ void __launch_bounds__(GemmCfg<BN, CG>::kThreads, 1) gemm_kernel(cons
     const uint32_t accfull0 = empty0 + 8 * Cfg::kStages, accempty0 = accfull0 + 16, drain = accempty0 + 16;
     volatile uint32_t *tmem_holder = reinterpret_cast<volatile uint32_t *>(bars + 2 * Cfg::kStages + 5);
     volatile int *abort_flag = reinterpret_cast<volatile int *>(tmem_holder + 1);
+    volatile uint32_t *issued = tmem_holder + 2;  // stages that warp 0 has asked for, once it is through
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = CG == 2 ? cluster_rank() : 0;
     const int worker = blockIdx.x / CG, workers = gridDim.x / CG;
@@ -521,8 +523,8 @@ __global__ void __launch_bounds__(GemmCfg<BN, CG>::kThreads, 1) gemm_kernel(cons
 
     if (warp == 0) {
         if (lane == 0) {
-            uint32_t stage = 0, phase = 0, issued = 0;
-            bool ok = true;
+            uint32_t stage = 0, phase = 0, asked = 0;
+            bool ok = !(p.stall == 1 && worker == 0);
             // the pair's bytes are counted on its first CTA's barriers
             const uint32_t full_base = CG == 2 ? map_to_rank(full0, 0) : full0;
             for (int step = 0; ok; ++step) {
@@ -554,29 +556,14 @@ __global__ void __launch_bounds__(GemmCfg<BN, CG>::kThreads, 1) gemm_kernel(cons
                     } else {
                         tma_load_g<CG>(sb, map_b, kb * kGemmK, n0, bar);
                     }
-                    ++issued;
+                    ++asked;
                     if (++stage == Cfg::kStages) {
                         stage = 0;
                         phase ^= 1u;
                     }
                 }
             }
-            if (!ok && rank != 0) {
-                // this CTA's loads are counted on the other's barriers: give them a millisecond to land
-                const uint64_t t0 = ptx::globaltimer_ns();
-                while (ptx::globaltimer_ns() - t0 < 1000000ull) {
-                }
-            }
-            if (!ok && rank == 0) {
-                // gave up: wait (bounded) for the loads in flight
-                const uint32_t n = issued < (uint32_t)Cfg::kStages ? issued : (uint32_t)Cfg::kStages;
-                for (uint32_t k = 1; k <= n; ++k) {
-                    const uint32_t idx = issued - k, s = idx % Cfg::kStages, ph = (idx / Cfg::kStages) & 1u;
-                    const uint64_t t0 = ptx::globaltimer_ns();
-                    while (!ptx::mbar_try_wait(full0 + 8 * s, ph))
-                        if (ptx::globaltimer_ns() - t0 > p.wait_limit_ns) break;
-                }
-            }
+            *issued = asked;
         }
         __syncwarp();
     } else if (warp == 1) {
@@ -585,6 +572,7 @@ __global__ void __launch_bounds__(GemmCfg<BN, CG>::kThreads, 1) gemm_kernel(cons
                                     ((uint32_t)((kGemmM * CG) >> 4) << 24);
             uint32_t stage = 0, phase = 0, acc = 0, acc_phase = 0;
             bool ok = true;
+            const bool stop = p.stall == 2 && worker == 0;
             for (int step = 0; ok; ++step) {
                 const int u = gemm_next(p, worker, workers, step);
                 if (u < 0) break;
@@ -600,7 +588,8 @@ __global__ void __launch_bounds__(GemmCfg<BN, CG>::kThreads, 1) gemm_kernel(cons
                 const uint32_t step_a = q.a_mn ? 2048u >> 4 : 32u >> 4, step_b = q.b_mn ? 2048u >> 4 : 32u >> 4;
                 const uint64_t base_a = q.a_mn ? make_desc_mn_sw128(0) : ptx::make_desc_k_sw128(0);
                 const uint64_t base_b = q.b_mn ? make_desc_mn_sw128(0) : ptx::make_desc_k_sw128(0);
-                for (int kb = g.kb0; kb < g.kb1; ++kb) {
+                const int kb1 = stop ? g.kb0 + 1 : g.kb1;
+                for (int kb = g.kb0; kb < kb1; ++kb) {
                     if (!ptx::mbar_wait_bounded(full0 + 8 * stage, phase, abort_flag, p.wait_limit_ns)) {
                         ok = false;
                         break;
@@ -617,6 +606,7 @@ __global__ void __launch_bounds__(GemmCfg<BN, CG>::kThreads, 1) gemm_kernel(cons
                         phase ^= 1u;
                     }
                 }
+                if (stop) ok = false;
                 if (!ok) break;
                 mma_commit_g<CG>(accfull0 + 8 * acc);
                 acc ^= 1u;
@@ -732,7 +722,23 @@ __global__ void __launch_bounds__(GemmCfg<BN, CG>::kThreads, 1) gemm_kernel(cons
     }
     ptx::tc_fence_before_sync();
     __syncthreads();
-    if (threadIdx.x == 0 && *abort_flag) atomicMax(p.status, 6);
+    if (threadIdx.x == 0 && *abort_flag) {
+        // one of the roles gave up: no copy that warp 0 asked for, whichever role that was, may land after this CTA has left
+        const uint64_t t0 = ptx::globaltimer_ns();
+        if (rank == 0) {
+            const uint32_t asked = *issued;
+            for (uint32_t k = 1; k <= min(asked, (uint32_t)Cfg::kStages); ++k) {
+                const uint32_t idx = asked - k, s = idx % Cfg::kStages, ph = (idx / Cfg::kStages) & 1u;
+                while (!ptx::mbar_try_wait(full0 + 8 * s, ph))
+                    if (ptx::globaltimer_ns() - t0 > p.wait_limit_ns) break;
+            }
+        } else {
+            // (this CTA's are counted on the other's barriers: a millisecond is a thousand times what one takes)
+            while (ptx::globaltimer_ns() - t0 < 1000000ull) {
+            }
+        }
+        atomicMax(p.status, 6);
+    }
     if (CG == 2) cluster_sync();
     ptx::tc_fence_after_sync();
     if (warp == 1) tmem_free_g<CG>(tmem, Cfg::kTmemCols);

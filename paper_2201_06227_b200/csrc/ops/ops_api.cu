@@ -34,6 +34,7 @@ constexpr size_t kTicketOff = 256;
 constexpr int kMaxTickets = (int)((kHeadBytes - kTicketOff) / 4);
 constexpr int kMaxSplitCtas = 160;                       // CTAs' worth of partial tiles at most
 constexpr uint64_t kWaitLimitNs = 2000000000ull;
+constexpr uint64_t kTestWaitLimitNs = 1000000ull;        // of a launch under egeria_ops_debug_stall_next
 constexpr int64_t kMaxSize = ((int64_t)1 << 31) - 1024;  // tile coordinates are 32-bit
 constexpr int kSms = 148;                                // what workspaces are sized for
 
@@ -179,6 +180,7 @@ struct egeria_ops {
     int sms = 0;
     int64_t launches = 0;
     cudaStream_t last_stream = nullptr;
+    uint32_t stall_next = 0;  // test hook: give-up path of the next product
 };
 
 namespace egeria {
@@ -318,7 +320,9 @@ static egeria_status run_products(egeria_ops *o, cudaStream_t stream, int type, 
     p.sums = sums;
     p.is_f16 = type == EGERIA_F16;
     p.status = reinterpret_cast<int32_t *>(o->ws);
-    p.wait_limit_ns = kWaitLimitNs;
+    p.stall = o->stall_next;
+    p.wait_limit_ns = o->stall_next ? kTestWaitLimitNs : kWaitLimitNs;
+    o->stall_next = 0;
     const int ctas = used * cg;
     EGO_CUDA(type == EGERIA_BF16 ? launch_gemm_any<bf16>(bn, cg, p, ctas, stream) : launch_gemm_any<f16>(bn, cg, p, ctas, stream));
     ++o->launches;
@@ -571,6 +575,11 @@ egeria_status egeria_ops_device_status(egeria_ops *ops) {
     return static_cast<egeria_status>(v);
 }
 int64_t egeria_ops_launch_count(const egeria_ops *ops) { return ops ? ops->launches : 0; }
+egeria_status egeria_ops_debug_stall_next(egeria_ops *ops, int kind) {
+    if (!ops || kind < 0 || kind > 2) return EGERIA_ERR_INVALID_ARG;
+    ops->stall_next = (uint32_t)kind;
+    return EGERIA_OK;
+}
 
 // ---------------------------------------------------------------- linear
 size_t egeria_linear_workspace_bytes(int64_t rows, int64_t inp, int64_t out) {

@@ -37,7 +37,7 @@ ADAMW_BLOCK = 256
 ADAMW_8BIT = 1
 
 EXPORTS = [
-    "egeria_ops_create", "egeria_ops_destroy", "egeria_ops_device_status", "egeria_ops_launch_count",
+    "egeria_ops_create", "egeria_ops_destroy", "egeria_ops_device_status", "egeria_ops_launch_count", "egeria_ops_debug_stall_next",
     "egeria_linear_workspace_bytes", "egeria_linear_forward", "egeria_linear_backward",
     "egeria_norm_workspace_bytes", "egeria_norm_forward", "egeria_norm_backward",
     "egeria_adamw_workspace_bytes", "egeria_adamw_create", "egeria_adamw_destroy", "egeria_adamw_set_grads",
@@ -80,6 +80,7 @@ def lib() -> ctypes.CDLL:
     for name, args in (("egeria_linear_workspace_bytes", [_i64] * 3), ("egeria_norm_workspace_bytes", [_i64] * 2),
                        ("egeria_adamw_workspace_bytes", [ctypes.c_int, ctypes.POINTER(_AdamTensor), ctypes.c_uint32])):
         getattr(L, name).argtypes, getattr(L, name).restype = args, ctypes.c_size_t
+    L.egeria_ops_debug_stall_next.argtypes = [_vp, ctypes.c_int]
     L.egeria_ops_create.argtypes = [ctypes.POINTER(_vp), _vp, ctypes.c_size_t]
     L.egeria_adamw_create.argtypes = [ctypes.POINTER(_vp), ctypes.c_int, ctypes.POINTER(_AdamTensor), ctypes.POINTER(_vp), _vp, _vp,
                                       ctypes.c_size_t, ctypes.c_uint32]
@@ -258,6 +259,10 @@ class Ops(_Handle):
 
     def check_device_status(self) -> None:
         _check(self.egeria_ops_device_status(), "egeria_ops_device_status")
+
+    def egeria_ops_debug_stall_next(self, kind: int) -> None:
+        """Test hook: the next product on the tensor cores gives up (see the header)."""
+        _check(self._lib.egeria_ops_debug_stall_next(self._h, int(kind)), "egeria_ops_debug_stall_next")
 
     def egeria_ops_launch_count(self) -> int:
         return int(self._lib.egeria_ops_launch_count(self._h))

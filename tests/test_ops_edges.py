@@ -376,3 +376,24 @@ def test_a_handle_talks_to_the_library_it_was_made_with(monkeypatch):
     assert o.egeria_ops_launch_count() >= 1 and a.egeria_adamw_launch_count() == 1
 
 
+# ----------------------------------------------------------------------------- bounded waits
+
+@pytest.mark.parametrize("kind", [1, 2])
+@pytest.mark.parametrize("rows,inp,out", [(300, 4096, 192), (64, 2048, 64), (2048, 1024, 4096), (4096, 768, 768)])
+def test_a_wait_that_runs_out_is_reported_and_the_handle_recovers(kind, rows, inp, out):
+    """The give-up path of the products' kernel: the first worker issues no loads (1) or stops after its first stage (2), for one
+    launch whose waits are limited to a millisecond.  The kernel returns, the status says EGERIA_ERR_TIMEOUT once, and the
+    next call is whole: split products (whose tickets the others have raised), pairs of thread blocks, single ones."""
+    o = ops.Ops(ops.egeria_linear_workspace_bytes(rows, inp, out), DEV)
+    x, w = rand(rows, inp, seed=1), rand(out, inp, seed=2, scale=inp ** -0.5)
+    want = o.egeria_linear_forward(x, w)
+    o.check_device_status()
+    o.egeria_ops_debug_stall_next(kind)
+    o.egeria_linear_forward(x, w)
+    assert o.egeria_ops_device_status() == eg.ERR_TIMEOUT
+    assert o.egeria_ops_device_status() == eg.OK
+    for _ in range(2):
+        assert torch.equal(o.egeria_linear_forward(x, w), want)
+    o.check_device_status()
+
+

@@ -49,7 +49,8 @@ egeria_status egeria_ops_destroy(egeria_ops *ops);
 
 /* Synchronise the stream of the last call and report the device status word: EGERIA_OK, or
  * EGERIA_ERR_TIMEOUT if a bounded wait inside a kernel ran out (the results of that call are
- * invalid; the handle can be used again). */
+ * invalid; the handle can be used again), or in a checked build EGERIA_ERR_CHECK if an index check
+ * inside a kernel failed. */
 egeria_status egeria_ops_device_status(egeria_ops *ops);
 
 /* Number of kernels launched through this handle so far. */

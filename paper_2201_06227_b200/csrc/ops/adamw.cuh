@@ -20,7 +20,6 @@
 // The root is kept because the update divides by it.  A second moment that is not zero never gets
 // code 0: that would divide a moment by eps alone.
 #pragma once
-#include "../check.cuh"
 #include "../ptx_sm100.cuh"
 #include "common.cuh"
 
@@ -293,11 +292,11 @@ __global__ void __launch_bounds__(kAdamThreads, SMALL ? 3 : 2) adamw_kernel(cons
     bool live = false, vector = false;
     for (int c = c0; c < c1 && !skip_all; ++c) {
         const int2 chunk = a.chunks[c];
-        if (!eg_check(chunk.x >= 0 && chunk.x < a.n_tensors && chunk.y >= 0, a.status, 11, c)) break;
+        if (!eg_check(chunk.x >= 0 && chunk.x < a.n_tensors && chunk.y >= 0, a.status, kCheckAdamPiece, c)) break;
         if (chunk.x != tensor) {
             tensor = chunk.x;
             t = a.tensors[tensor];
-            if (!eg_check(t.index >= 0 && t.index < a.n_grads, a.status, 12, tensor)) break;
+            if (!eg_check(t.index >= 0 && t.index < a.n_grads, a.status, kCheckAdamTensor, tensor)) break;
             live = !(a.frozen && t.module >= 0 && a.frozen[t.module]);
             grad = static_cast<const G *>(a.grads[t.index]);
             vector = t.vector && (reinterpret_cast<uintptr_t>(grad) % (8 * sizeof(G)) == 0);

@@ -5,8 +5,21 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include "../check.cuh"
+
 namespace egeria {
 namespace ops {
+
+// What the operators' kernels check of themselves in the checked build (the evaluation's codes end at 10).
+enum OpsCheckCode : int32_t {
+    kCheckAdamPiece = 11,   // AdamW: a table entry's tensor or piece
+    kCheckAdamTensor = 12,  // AdamW: a tensor's place in the caller's order
+    kCheckGemmUnit = 13,    // products: a unit's tile or range of k blocks
+    kCheckGemmSplit = 14,   // products: a split tile's ticket or place among the partial tiles
+    kCheckSlopeRun = 15,    // linear backward: a block's rows, or the place of its partial sums
+    kCheckNormRows = 16,    // norm backward: a CTA's rows
+    kCheckNormGate = 17,    // norm backward: a group's gate, or the CTAs that share it
+};
 
 using bf16 = __nv_bfloat16;
 using f16 = __half;

@@ -59,6 +59,8 @@ struct GemmProblem {
     Epilogue epi;
     float *partials;                 // split k: [unit][epilogue warp][piece][8][32 lanes][4]
     int32_t *tickets;                // split k: [tile][epilogue warp], zero between calls
+    int64_t partial_floats;          // room for partials (checked build)
+    int32_t ticket_room;             // and for tickets
 };
 // out[c] = the sum of n rows of partial sums.
 struct ColumnSums {
@@ -456,6 +458,9 @@ __device__ __forceinline__ GemmUnit gemm_unit(const GemmParams &params, int u) {
     g.kb1 = (int)((int64_t)p.kblocks * (g.split + 1) / p.splits);
     return g;
 }
+__device__ __forceinline__ bool gemm_unit_fits(const GemmProblem &q, const GemmUnit &g) {
+    return g.tm >= 0 && g.tm < q.tiles_m && g.tn >= 0 && g.tn < q.tiles_n && g.kb0 >= 0 && g.kb0 < g.kb1 && g.kb1 <= q.kblocks;
+}
 // The step-th unit of a worker (a CTA or a pair), or -1.  The first product's units are dealt round; the workers
 // that the last round of it leaves out take `fill` units of the second each, and then that is dealt round.
 __device__ __forceinline__ int gemm_next(const GemmParams &p, int worker, int workers, int step) {
@@ -532,6 +537,7 @@ __global__ void __launch_bounds__(GemmCfg<BN, CG>::kThreads, 1) gemm_kernel(cons
                 if (u < 0) break;
                 const GemmUnit g = gemm_unit(p, u);
                 const GemmProblem &q = p.problem[g.problem];
+                if (!eg_check(gemm_unit_fits(q, g), p.status, kCheckGemmUnit, u)) break;
                 const CUtensorMap *map_a = &q.a, *map_b = &q.b;
                 const bool a_mn = q.a_mn, b_mn = q.b_mn;
                 const int32_t m0 = (g.tm * CG + (int)rank) * kGemmM, n0 = g.tn * BN + (int)rank * Cfg::kBRows;
@@ -637,6 +643,7 @@ __global__ void __launch_bounds__(GemmCfg<BN, CG>::kThreads, 1) gemm_kernel(cons
             const int u = gemm_next(p, worker, workers, step);
             if (u < 0) break;
             const GemmUnit g = gemm_unit(p, u);
+            if (!eg_check(gemm_unit_fits(p.problem[g.problem], g), p.status, kCheckGemmUnit, u)) break;
             // (each product with its own copy of this code: what it takes from the parameters is then at fixed places)
             auto tile = [&](const GemmProblem &q) {
                 t.wide = q.epi.wide;
@@ -655,6 +662,10 @@ __global__ void __launch_bounds__(GemmCfg<BN, CG>::kThreads, 1) gemm_kernel(cons
                 float *part = nullptr;
                 if (q.splits > 1)
                     part = q.partials + (((int64_t)g.index * CG + rank) * kEpiWarps + e) * (Cfg::kPieces * 1024);
+                if (q.splits > 1 && !eg_check(part + Cfg::kPieces * 1024 <= q.partials + q.partial_floats &&
+                                                  (g.tile * CG + (int)rank) * kEpiWarps + e < q.ticket_room,
+                                              p.status, kCheckGemmSplit, g.index))
+                    return false;
 #pragma unroll 1
                 for (int c = 0; c < Cfg::kPieces; ++c) {
                     float v[32];
@@ -824,23 +835,27 @@ struct SlopeJob {
     float *sums;                     // partial sums [runs][cols], or null
     void *db;                        // the column sums themselves where there is one run
     int64_t lddz, lddy, ldz, rows;
+    int64_t sums_room;               // values that sums has room for (checked build)
     int32_t act, cols, strips, runs; // blocks = strips * runs
 };
 struct PrepareParams {
     SlopeJob slope;
     PackJob pack[2];
+    int32_t *status;
 };
 
 // A warp owns 256 columns, 8 per lane; the warps of a block take the rows of its run in turn and add up at the end.
 // WIDE: a lane's 8 columns are consecutive; else they are 32 apart.
 constexpr int kPrepareWarps = 8;
 template <typename T, bool WIDE>
-__device__ __forceinline__ void slope_block(const SlopeJob &j, int block, float (*part)[256 + 8]) {
+__device__ __forceinline__ void slope_block(const SlopeJob &j, int block, float (*part)[256 + 8], int32_t *status) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int run = block / j.strips, c0 = (block - run * j.strips) * 256, cols = j.cols;
     const int64_t r0 = j.rows * run / j.runs, r1 = j.rows * (run + 1) / j.runs;
     const T *dy = static_cast<const T *>(j.dy), *z = static_cast<const T *>(j.z);
     T *dz = static_cast<T *>(j.dz);
+    if (!eg_check(run < j.runs && r0 >= 0 && r1 <= j.rows && (!j.sums || j.runs == 1 || (int64_t)(run + 1) * cols <= j.sums_room), status, kCheckSlopeRun, block))
+        return;
     float s[8] = {0, 0, 0, 0, 0, 0, 0, 0};
     if (WIDE) {
         const int c = c0 + lane * 8;
@@ -922,7 +937,7 @@ __global__ void __launch_bounds__(32 * kPrepareWarps) prepare_kernel(const Prepa
     int block = blockIdx.x;
     const int slopes = p.slope.strips * p.slope.runs;
     if (block < slopes) {
-        slope_block<T, WIDE>(p.slope, block, part);
+        slope_block<T, WIDE>(p.slope, block, part, p.status);
         return;
     }
     block -= slopes;

@@ -39,6 +39,7 @@ struct NormParams {
     int32_t layer, post, pre;
     int32_t w_float;                       // weights, biases and gate are float, not T
     float alpha, eps, inv_cols;
+    int32_t *status;                       // backward, checked build
 };
 
 // A team is TEAM threads that hold one row, 8 * VPT values each.  WIDE: the thread's values are
@@ -295,6 +296,7 @@ __global__ void __launch_bounds__(TEAM, TEAM >= 512 ? 1 : 512 / TEAM) norm_backw
     int turn = 0;
     const int t = threadIdx.x;
     const int64_t r0 = norm_first_row(p, blockIdx.x), r1 = norm_first_row(p, blockIdx.x + 1);
+    if (!eg_check(r0 >= 0 && r0 < r1 && r1 <= p.rows, p.status, kCheckNormRows, r0)) return;
     float *sums = p.sums + (int64_t)blockIdx.x * kNormSums * p.cols;
     const bool in = norm_in<TEAM, WIDE, FULL>(t, 0, 0, p.cols);
     const int col = norm_col<TEAM, WIDE>(t, 0, 0);
@@ -368,6 +370,7 @@ __global__ void __launch_bounds__(TEAM, TEAM >= 512 ? 1 : 512 / TEAM) norm_backw
         if (p.gate && left == 0) {
             group = r / p.gate_rows;
             left = min((group + 1) * p.gate_rows, p.rows) - r;
+            if (!eg_check(group >= 0 && group * p.gate_rows < p.rows && left > 0, p.status, kCheckNormGate, group)) return;
             norm_vector<T, TEAM, WIDE, FULL>(gate, p.gate, group * p.cols, p.w_float, t, 0, p.cols, 1.0f);
         }
         F2 tot[4];
@@ -519,6 +522,7 @@ __global__ void __launch_bounds__(kSumsThreads) norm_sums_kernel(const NormParam
         const int64_t group = blockIdx.y - 4, g0 = group * p.gate_rows, g1 = min(g0 + p.gate_rows, p.rows);
         const int first = norm_holder(p, g0), last = norm_holder(p, g1 - 1);
         if (first == last) return;
+        if (!eg_check(first >= 0 && first < last && last < n, p.status, kCheckNormGate, group)) return;
         const bool begins = norm_first_row(p, first) == g0;
         const float s = sum_partials(first, last, part, [&](int k) { return (k == first && !begins ? tail : head)[k * pitch]; });
         if (writes) store_param<T>(p.dgate, group * p.cols + c, s, p.w_float);
@@ -529,6 +533,7 @@ __global__ void __launch_bounds__(kSumsThreads) norm_sums_kernel(const NormParam
     const int64_t mine = norm_first_row(p, k), before = norm_first_row(p, k - 1), group = mine / p.gate_rows, g0 = group * p.gate_rows;
     if (g0 == mine || g0 < before) return;
     const int64_t g1 = min(g0 + p.gate_rows, p.rows);
+    if (!eg_check(g0 >= 0 && g0 < g1, p.status, kCheckNormGate, group)) return;
     float s = (g0 == before ? head : tail)[(k - 1) * pitch] + head[k * pitch];
 #pragma unroll 4
     for (int j = k + 1; j < n && norm_first_row(p, j) < g1; ++j) s += head[j * pitch];

@@ -309,6 +309,8 @@ static egeria_status run_products(egeria_ops *o, cudaStream_t stream, int type, 
         set_widths(q.epi);
         q.partials = reinterpret_cast<float *>(o->ws + j.part);
         q.tickets = reinterpret_cast<int32_t *>(o->ws + kTicketOff) + i * (kMaxTickets / 2);
+        q.partial_floats = (int64_t)split_bytes(j.m, j.n, j.k) / 4;
+        q.ticket_room = kMaxTickets / 2;
     }
     const int used = (int)std::min<int64_t>(units, workers);
     if (count == 2) {
@@ -626,6 +628,7 @@ egeria_status egeria_linear_forward(egeria_ops *ops, void *cuda_stream, const eg
         return EGERIA_OK;
     }
     PrepareParams prep{};
+    prep.status = reinterpret_cast<int32_t *>(ops->ws);
     Product job{a.rows, a.out, a.inp, {a.x, a.ldx, a.rows, a.inp, false}, {a.w, a.ldw, a.out, a.inp, false}, e, L.part};
     make_loadable(ops, job.a, L.x, prep.pack[0]);
     make_loadable(ops, job.b, L.w, prep.pack[1]);
@@ -664,6 +667,7 @@ egeria_status egeria_linear_backward(egeria_ops *ops, void *cuda_stream, const e
         dz.ld = pad8(a.out);
     }
     PrepareParams prep{};
+    prep.status = reinterpret_cast<int32_t *>(ops->ws);
     ColumnSums sums{};
     bool wide = false;
     if (own_dz || a.db) {
@@ -682,6 +686,7 @@ egeria_status egeria_linear_backward(egeria_ops *ops, void *cuda_stream, const e
         j.db = a.db;
         if (a.db) {
             j.sums = reinterpret_cast<float *>(ops->ws + L.sums);
+            j.sums_room = slope_sums(a.rows, a.out);
             if (j.runs > 1) sums = ColumnSums{j.sums, a.db, j.runs, j.cols};
         }
         wide = a.out % 8 == 0 && aligned(a.dy, 16) && a.lddy % 8 == 0 && (!j.z || (aligned(j.z, 16) && a.ldz % 8 == 0));
@@ -817,6 +822,7 @@ egeria_status egeria_norm_backward(egeria_ops *ops, void *cuda_stream, const ege
     p.h = a.df, p.ldh = a.lddf;
     p.stats = const_cast<float *>(a.stats);
     p.sums = reinterpret_cast<float *>(ops->ws + kHeadBytes);
+    p.status = reinterpret_cast<int32_t *>(ops->ws);
     p.dw_post = a.dw_post, p.db_post = a.db_post, p.dw_pre = a.dw_pre, p.db_pre = a.db_pre, p.dgate = a.dgate;
     p.rows = a.rows;
     p.gate_rows = a.gate_rows ? a.gate_rows : a.rows;

@@ -397,3 +397,14 @@ def test_a_wait_that_runs_out_is_reported_and_the_handle_recovers(kind, rows, in
     o.check_device_status()
 
 
+# ----------------------------------------------------------------------------- the checked build
+
+def test_checked_build_finds_nothing_on_the_operators():
+    """A cross-section of the operators' tests on the second library, whose kernels check their indexes, in a process of its
+    own: the same results, and no check fires (the tests end with a status query, which would say EGERIA_ERR_CHECK)."""
+    here = Path(__file__).resolve().parent
+    r = subprocess.run([sys.executable, "-m", "pytest", str(here / "test_ops_gpu.py"), "-m", "gpu", "-x", "-q", "--checked-library", "-p", "no:cacheprovider",
+                        "-k", "linear_forward or linear_backward or linear_larger or norm_sizes or norm_gate_groups or adamw_types or frozen_modules"],
+                       capture_output=True, text=True, cwd=str(here.parent))
+    assert r.returncode == 0, r.stdout[-3000:] + r.stderr[-2000:]
+    assert " passed" in r.stdout and "failed" not in r.stdout

@@ -397,6 +397,129 @@ def test_a_wait_that_runs_out_is_reported_and_the_handle_recovers(kind, rows, in
     o.check_device_status()
 
 
+# ----------------------------------------------------------------------------- gradients against differences
+
+def test_linear_gradients_along_themselves():
+    """A step along a gradient changes the loss by the gradient's square.  The outputs' roundings are each within
+    2^-11 |y|, independent and weighted by c: six deviations of their sum are the noise; the step moves z by some 0.1, so that
+    its third derivative is under 2 % of the change; the gradient's own rounding is far below that."""
+    rows, inp, out, t = 40, 48, 56, torch.float16
+    o = ops.Ops(ops.egeria_linear_workspace_bytes(rows, inp, out), DEV)
+    x, w, b, c = rand(rows, inp, dtype=t, seed=1), rand(out, inp, dtype=t, seed=2, scale=0.15), rand(out, dtype=t, seed=3), rand(rows, out, dtype=t, seed=4)
+
+    def outputs(x, w, b):
+        return o.egeria_linear_forward(x, w, bias=b, act="gelu").double()
+
+    y, z = o.egeria_linear_forward(x, w, bias=b, act="gelu", save_z=True)
+    noise = 6 * 2.0 ** -11 / math.sqrt(3) * math.sqrt(2.0) * float((c.double() * y.double()).square().sum().sqrt())
+    for which, grad in enumerate(o.egeria_linear_backward(c, x, w, z=z, act="gelu")):
+        args = [x, w, b]
+        moved = [grad.double() @ w.double().t(), x.double() @ grad.double().t(), grad.double().view(1, -1)][which] if which < 2 else grad.double()
+        step = 0.1 / float(moved.abs().max())
+        up, down = list(args), list(args)
+        up[which] = (args[which].double() + step * grad.double()).to(t)
+        down[which] = (args[which].double() - step * grad.double()).to(t)
+        slope = float((grad.double() * (up[which].double() - down[which].double())).sum())
+        change = float(((outputs(*up) - outputs(*down)) * c.double()).sum())
+        assert slope > 8 * noise                          # a gradient of zero, or of the other sign, is far outside
+        assert abs(change - slope) <= noise + 0.02 * slope, (which, change, slope, noise)
+
+
+@pytest.mark.parametrize("kind", ["layer", "rms"])
+def test_norm_gradients_along_themselves(kind):
+    """The same for the residual norms in 32 bits, every gradient: the outputs are off by (cols + 64) 2^-24 of their parts."""
+    rows, cols, t = 24, 72, torch.float32
+    o = ops.Ops(ops.egeria_norm_workspace_bytes(rows, cols), DEV)
+    s = dict(x=rand(rows, cols, dtype=t, seed=1), f=rand(rows, cols, dtype=t, seed=2), gate=rand(6, cols, dtype=t, seed=3, base=0.5))
+    for k in ("post", "pre"):
+        s["w_" + k], s["b_" + k] = rand(cols, dtype=t, seed=4, scale=0.2, base=1.0), rand(cols, dtype=t, seed=5)
+    dy, dh = rand(rows, cols, dtype=t, seed=8), rand(rows, cols, dtype=t, seed=9)
+
+    def loss(s):
+        y, h, _ = o.egeria_norm_forward(s["x"], s["f"], **{k: s[k] for k in s if k not in "xf"}, gate_rows=4, kind=kind, alpha=0.75)
+        return float((y.double() * dy.double()).sum() + (h.double() * dh.double()).sum())
+
+    vectors = {k: s[k] for k in s if k not in "xf"}
+    y, h, st = o.egeria_norm_forward(s["x"], s["f"], **vectors, gate_rows=4, kind=kind, alpha=0.75)
+    noise = (cols + 64) * 2.0 ** -24 * 8 * float((dy.double().abs() * y.double().abs()).sum() + (dh.double().abs() * (1 + h.double().abs())).sum())
+    got = o.egeria_norm_backward(dy, dh, y, s["f"], st, **vectors, gate_rows=4, kind=kind, alpha=0.75)
+    for k in s:
+        grad = got["d" + k]
+        step = 0.02 / float(grad.abs().max())             # no value moves by more than 0.02 of the norm of what it is among
+        up, down = (dict(s, **{k: s[k] + sign * step * grad}) for sign in (1, -1))
+        slope = float((grad.double() * (up[k].double() - down[k].double())).sum())
+        change = loss(up) - loss(down)
+        assert slope > 8 * noise, k
+        assert abs(change - slope) <= noise + 0.02 * slope, (k, change, slope, noise)
+
+
+# ----------------------------------------------------------------------------- aliases
+
+_vp, _i32, _i64, _f32 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_float
+
+
+def _struct(name, fields):
+    return type(name, (ctypes.Structure,), {"_fields_": [(f, t) for t, names in fields for f in names.split()]})
+
+
+NormForward = _struct("NormForward", ((_i32, "type param_type kind post pre"), (_f32, "alpha eps"), (_i64, "rows cols gate_rows"),
+                                      (_vp, "x f gate w_post b_post w_pre b_pre"), (_i64, "ldx ldf"), (_vp, "y h"), (_i64, "ldy ldh"), (_vp, "stats")))
+NormBackward = _struct("NormBackward", ((_i32, "type param_type kind post pre"), (_f32, "alpha"), (_i64, "rows cols gate_rows"),
+                                        (_vp, "dy dh y f gate w_post b_post w_pre b_pre"), (_i64, "lddy lddh ldy ldf"), (_vp, "stats dx df"),
+                                        (_i64, "lddx lddf"), (_vp, "dgate dw_post db_post dw_pre db_pre")))
+
+
+@pytest.mark.parametrize("kind", ["layer", "rms"])
+@pytest.mark.parametrize("rows,cols,pitch,dtype", [(700, 256, 256, torch.bfloat16), (700, 250, 256, torch.bfloat16), (333, 1001, 1003, torch.float16),
+                                                   (90, 1536, 1544, torch.bfloat16), (40, 4096, 4096, torch.float32), (31, 8192, 8192, torch.float32),
+                                                   (31, 8192, 8192, torch.bfloat16)])
+def test_norm_writes_onto_what_it_reads(rows, cols, pitch, dtype, kind):
+    """y = x, h = f; dx = dy with df = f or df = dh: the same bits as with separate outputs, at wide and narrow pitches and where
+    one row or three are on their way (8192 columns of float are one)."""
+    o = ops.Ops(ops.egeria_norm_workspace_bytes(rows, cols), DEV)
+    L, stream = ops.lib(), torch.cuda.current_stream().cuda_stream
+    t = ops.TYPES[dtype]
+
+    def matrix(seed):
+        return rand(rows, pitch, dtype=dtype, seed=seed)
+
+    w, gate = rand(cols, dtype=dtype, seed=1, base=1.0), rand(-(-rows // 7), cols, dtype=dtype, seed=2)
+    common = dict(type=t, param_type=t, kind=ops.KINDS[kind], post=1, pre=1, alpha=0.5, rows=rows, cols=cols, gate_rows=7, gate=gate.data_ptr(),
+                  w_post=w.data_ptr(), w_pre=w.data_ptr())
+
+    def forward(x, f, y, h):
+        st = torch.zeros(rows, 4, device=DEV)
+        a = NormForward(**common, eps=1e-5, x=x.data_ptr(), f=f.data_ptr(), y=y.data_ptr(), h=h.data_ptr(), ldx=pitch, ldf=pitch, ldy=pitch, ldh=pitch,
+                        stats=st.data_ptr())
+        assert L.egeria_norm_forward(o._h, _vp(stream), ctypes.byref(a)) == eg.OK
+        return st
+
+    x, f = matrix(3), matrix(4)
+    y, h = x.clone(), f.clone()                   # (what lies between the rows stays what it was)
+    st = forward(x, f, y, h)
+    x2, f2 = x.clone(), f.clone()
+    assert torch.equal(forward(x2, f2, x2, f2), st)
+    assert torch.equal(x2, y) and torch.equal(f2, h)
+
+    def backward(dy, dh, f, dx, df):
+        dgate, dw_post, dw_pre = torch.zeros_like(gate), torch.zeros_like(w), torch.zeros_like(w)
+        a = NormBackward(**common, dy=dy.data_ptr(), dh=dh.data_ptr(), y=y.data_ptr(), f=f.data_ptr(), lddy=pitch, lddh=pitch, ldy=pitch, ldf=pitch,
+                         stats=st.data_ptr(), dx=dx.data_ptr(), df=df.data_ptr(), lddx=pitch, lddf=pitch, dgate=dgate.data_ptr(),
+                         dw_post=dw_post.data_ptr(), dw_pre=dw_pre.data_ptr())
+        assert L.egeria_norm_backward(o._h, _vp(stream), ctypes.byref(a)) == eg.OK
+        return dgate, dw_post, dw_pre
+
+    dy, dh = matrix(5), matrix(6)
+    dx, df = dy.clone(), f.clone()
+    sums = backward(dy, dh, f, dx, df)
+    for onto in ("f", "dh"):
+        g = dict(dy=dy.clone(), dh=dh.clone(), f=f.clone())
+        again = backward(g["dy"], g["dh"], g["f"], g["dy"], g[onto])
+        assert all(torch.equal(p, q) for p, q in zip(sums, again))
+        assert torch.equal(g["dy"], dx) and torch.equal(g[onto][:, :cols], df[:, :cols])
+    o.check_device_status()
+
+
 # ----------------------------------------------------------------------------- the checked build
 
 def test_checked_build_finds_nothing_on_the_operators():

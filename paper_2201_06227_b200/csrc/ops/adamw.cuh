@@ -10,8 +10,10 @@
 // moments have one scale per block, which makes the block's maximum a reduction inside the warp.
 //
 // Measured on 302 M values (a 24-block, 1024-wide decoder; floor: the bytes at 6464 GB/s), bf16 parameters: moments in 32 bits
-// 1054 us of 1029, with fp32 masters 1380 of 1309; in 8 bits 861 us of 471: there the codes' arithmetic (63
-// instructions a value) is as long as the bytes, and issue slots are 61 % taken.
+// 1049 us of 1029, with fp32 masters 1392 of 1309; in 8 bits 818 to 853 us of 471: there the codes' arithmetic (67
+// instructions a value) is as long as the bytes, and two thirds of the issue slots are taken.  Frozen tensors are a prefix as a
+// rule, and a CTA owns one run of pieces: with 8 of the 24 blocks frozen 931 us of 873, with 16 613 of 436, with 20 532
+// of 218, with 23 494 of 55, the time of the CTAs that have all of their run to do.
 //
 // 8-bit codes.  A first moment is sign * (c / 127)^2 * scale with c = 0..127, and the ROOT of a second
 // moment is (c / 255)^2 * scale with c = 0..255; scale is the largest size in the block.  Squaring the
@@ -270,7 +272,8 @@ __device__ __forceinline__ void adam_narrow(const AdamStep &s, const AdamTensor 
     }
 }
 
-// Three CTAs per SM for 8-bit moments (80 registers, a few spilled): 825 us against 924 with two.
+// Three CTAs per SM for 8-bit moments (80 registers, a few spilled): 825 us against 924 with two, before the sums of pairs
+// were taken apart.
 template <typename P, typename G, bool MASTER, bool SMALL>
 __global__ void __launch_bounds__(kAdamThreads, SMALL ? 3 : 2) adamw_kernel(const AdamParams a) {
     ptx::grid_dependency_wait();

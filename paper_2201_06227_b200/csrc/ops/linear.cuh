@@ -15,14 +15,16 @@
 // tensor memory.  One launch takes up to two products (dx and dw of a layer), so that the second fills
 // the SMs that the first leaves.  CG = 2: a pair of CTAs shares one tile of 256 rows; each loads its 128 rows of A and
 // HALF of B, which is what brings the loads (32 KB per 64 k and CTA instead of 48) near what an SM
-// can take from L2 in the time of the MMAs (64 bytes a cycle asked for, 55 to 60 seen).
+// can take from L2 in the time of the MMAs (64 bytes a cycle at their full rate; 60 bytes a nanosecond seen).
 //
-// Measured (bf16; floor: 2 m n k at 1669 TFLOP/s, a short product's rate; a long run's is 1435 under the power limit, which
-// these meet too): 65536 x 1024 x 4096 (rows, k, columns) alone 460 to 490 us of 329, with bias, tanh-gelu and z 580
-// to 590; k = 4096 and 1024 columns 420 to 450 of 329 (1250 to 1320 TFLOP/s; the tensor pipe 80 % busy at 1.56 GHz).
-// dx and dw of 16384 x 4096 x 1024 220 to 240 us of 165, with the slope of dx's tanh-gelu 277.  A short sum (k = 1024) is
-// bound by the epilogue and the loads together; small products (under some 500 rows) by the 8 to 9 us that a launch, its
-// first loads and its one epilogue take.
+// Measured (bf16, GPU time in a replayed graph; floor: 2 m n k at 1669 TFLOP/s, a short product's rate; a long run's is 1435
+// under the power limit, which these meet too): 65536 x 1024 x 4096 (rows, k, columns) alone 487 us of 329, with bias 533, with
+// bias and tanh-gelu 558, with z alone 506, with all of it 576 to 618; k = 4096 and 1024 columns 463 of 329.  dx and dw of
+// 16384 x 4096 x 1024 229 to 261 us of 165, with the slope of dx's tanh-gelu 293 to 313.  By the counters no unit is full at
+// k = 1024: the tensor pipe is busy for 60 % of the time alone and 51 % with all of the epilogue (67 % alone at k = 4096), L2 for 36
+// and 47 %, the issue slots for 16 and 31 %; each part of the epilogue shows in the time although it runs beside the next
+// tile's products.  Small products (under some 500 rows) are bound by the 10 us that a launch, its first loads and its one
+// epilogue take.
 #pragma once
 #include <cuda.h>
 
@@ -758,7 +760,7 @@ __global__ void __launch_bounds__(GemmCfg<BN, CG>::kThreads, 1) gemm_kernel(cons
 // ---------------------------------------------------------------- a few rows
 // y for 1 to 4 rows without the tensor cores: the cost is reading w once, so w is streamed by
 // every warp of the GPU in 16-byte pieces, one output column per warp and turn; x stays in shared memory.
-// 1024 x 4096: 3.7 us for one row, 6.5 for two, 9.0 for four; the tensor cores take 8.9 for any number up to 8.
+// 1024 x 4096: 3.7 us for one row, 6.5 for two, 9.0 for four; the tensor cores take 10 for any number from 5 to 128.
 template <typename T, int ROWS, bool WIDE>
 __global__ void __launch_bounds__(256) linear_few_kernel(const Epilogue p, int32_t m, int32_t n_cols, const T *x, int64_t ldx, const T *w, int64_t ldw,
                                                          int32_t k) {

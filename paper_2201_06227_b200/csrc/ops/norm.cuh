@@ -12,9 +12,12 @@
 // read.
 //
 // Measured at 65536 x 1024 bf16 (floor: the bytes at 6464 GB/s): forward with two layer norms 105 us of 83, with two rms
-// norms 87 of 83; backward with two rms norms 152 us of 125, with two layer norms 192 of 125.  What is left is
-// instructions: a value costs about 35 of them backward, and two more sums per row with means and biases.  A
-// row pitch that takes no 16-byte accesses costs 2.4 (forward) and 1.8 times that: 250 and 265 us at 1001 columns.
+// norms 91 of 83; backward with two rms norms 152 us of 125, with two layer norms 193 of 125.  Forward is bound by
+// instructions (36 a value, two thirds of the issue slots).  Backward a value costs 36 instructions, 48 with means and biases, and
+// half of the issue slots are taken: what a row waits for (memory, then its team's sums) is not covered by the 16 warps that the
+// registers leave room for.  A row pitch that takes no 16-byte accesses costs 2.4 (forward) and 1.8 times that: 252 and 271 us
+// at 1001 columns; widths between the teams' own leave threads idle: forward 283 us at 1280 columns, 239 at 1536, 183
+// at 2048, 158 at 5120 (the same bytes), 108 at 4096 and 115 at 8192.
 #pragma once
 #include <string.h>
 

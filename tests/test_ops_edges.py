@@ -106,7 +106,7 @@ def test_a_dropped_handle_keeps_its_memory_until_its_calls_have_run(which):
     h = ops.Ops(ops.egeria_linear_workspace_bytes(200, 512, 256), DEV) if which == "ops" else ops.AdamW(p, g, m, v, steps)
     place, size = h._raw.data_ptr(), h._raw.numel()
     with torch.cuda.stream(side):
-        torch.cuda._sleep(100_000_000)         # about 50 ms
+        torch.cuda._sleep(600_000_000)         # about 0.3 s
         if which == "ops":
             h.egeria_linear_forward(x, w)
         else:
@@ -131,7 +131,7 @@ def test_new_gradients_are_kept_for_the_streams_of_the_steps():
         a.egeria_adamw_step(1e-3)
         a.egeria_adamw_set_grads(second)
         places = {first[0].data_ptr(), second[0].data_ptr()}
-        torch.cuda._sleep(100_000_000)
+        torch.cuda._sleep(600_000_000)
         a.egeria_adamw_step(1e-3)
     del a, first, second
     new = [torch.empty(3000, device=DEV) for _ in range(4)]

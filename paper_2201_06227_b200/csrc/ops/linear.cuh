@@ -190,19 +190,32 @@ constexpr float kGeluA = 1.5957691216057308f;  // 2 sqrt(2 / pi)
 constexpr float kGeluB = 0.044715f;
 
 // Phi(z), the normal distribution, and e = exp(-z^2 / 2), which its density shares.  The tail, Phi(-|z|) = t P(t) e with
-// t = 1 / (1 + 0.31 |z|) (the form of Hastings' approximations), P the polynomial of degree 5 whose RELATIVE error over
-// |z| <= 13.5 is smallest, found by reweighted least squares: 4.7e-6, with the roundings of 32 bits and of the exponent
-// 1e-5 (2^-16.6; a 16-bit result is rounded by 2^-12 of itself at least).  A formula of small absolute error does not do: the
-// value z Phi(z) for z < -3 is as small as Phi.  The library's erfcf gives more digits than the output holds and took 1.45
-// times the whole product's time at 65536 x 1024 x 4096.
+// t = 1 / (1 + p |z|) (the form of Hastings' approximations), P the polynomial whose RELATIVE error over |z| <= 13.5 is
+// smallest, found by reweighted least squares.  A formula of small absolute error does not do: the value z Phi(z) for
+// z < -3 is as small as Phi.  For a value P has degree 5: 4.7e-6, with the roundings of 32 bits and of the exponent 1e-5
+// (2^-16.6; a 16-bit result is rounded by 2^-12 of itself at least).  The slope Phi + z e / sqrt(2 pi) is 0 at z = -0.75, where what is
+// left of it is the terms' error: there P has degree 7 (1.3e-7), which leaves 1.2e-7, not 1.2e-6.  Values with degree 7 too took
+// 595 us against 585 at 65536 x 1024 x 4096 with z; the library's erfcf, which gives more digits than the output holds, 850.
+template <bool SLOPE>
 __device__ __forceinline__ float normal_cdf(float z, float &e) {
-    const float t = fast_rcp(fmaf(0.31f, fabsf(z), 1.0f));
+    const float t = fast_rcp(fmaf(SLOPE ? 0.3f : 0.31f, fabsf(z), 1.0f));
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(-0.5f * kLog2e * (z * z)));
-    float q = fmaf(-0.0739291459f, t, 0.18045035f);
-    q = fmaf(q, t, 0.0157447066f);
-    q = fmaf(q, t, 0.133429796f);
-    q = fmaf(q, t, 0.120441273f);
-    q = fmaf(q, t, 0.123860702f);
+    float q;
+    if (SLOPE) {
+        q = fmaf(0.0359316915f, t, -0.158275813f);
+        q = fmaf(q, t, 0.208206296f);
+        q = fmaf(q, t, -0.0553935617f);
+        q = fmaf(q, t, 0.129469052f);
+        q = fmaf(q, t, 0.0996375382f);
+        q = fmaf(q, t, 0.120798349f);
+        q = fmaf(q, t, 0.119626388f);
+    } else {
+        q = fmaf(-0.0739291459f, t, 0.18045035f);
+        q = fmaf(q, t, 0.0157447066f);
+        q = fmaf(q, t, 0.133429796f);
+        q = fmaf(q, t, 0.120441273f);
+        q = fmaf(q, t, 0.123860702f);
+    }
     const float tail = q * t * e;
     return z < 0.0f ? tail : 1.0f - tail;
 }
@@ -212,7 +225,7 @@ __device__ __forceinline__ float act_value(float z) {
     if (ACT == kActRelu) return z > 0.0f ? z : (z != z ? z : 0.0f);
     if (ACT == kActGelu) {
         float e;
-        return z * normal_cdf(z, e);
+        return z * normal_cdf<false>(z, e);
     }
     if (ACT == kActGeluTanh) return z * logistic2(z * fmaf(-kLog2e * kGeluA * kGeluB, z * z, -kLog2e * kGeluA));
     if (ACT == kActSilu) return z * logistic2(-kLog2e * z);
@@ -223,7 +236,7 @@ __device__ __forceinline__ float act_slope(float z) {
     if (ACT == kActRelu) return z > 0.0f ? 1.0f : 0.0f;
     if (ACT == kActGelu) {
         float e;
-        const float phi = normal_cdf(z, e);
+        const float phi = normal_cdf<true>(z, e);
         return fmaf(0.39894228040143268f * z, e, phi);
     }
     if (ACT == kActGeluTanh) {

@@ -297,6 +297,20 @@ def test_activations_alone(rows, act, dtype):
     close(o.egeria_linear_backward(one, None, eye, z_in=z, act_in=act, need_dw=False)[0], slope, tol, "slope in the epilogue")
 
 
+@pytest.mark.parametrize("inner", [False, True])
+def test_slope_of_gelu_next_to_its_zero(inner):
+    """Every f16 argument between -0.8 and -0.7: Phi(z) and z times the density cancel at -0.75.  Each is at most 0.25 there and
+    off by 2^-21 of itself (eight roundings of 2^-24): 2^-22 in all, and one rounding."""
+    z = torch.arange(0x3999, 0x3A67, device=DEV).to(torch.int16).view(torch.float16).neg()
+    z = torch.nn.functional.pad(z, (0, -len(z) % 64), value=-0.75).view(-1, 64)
+    n, one, eye = z.shape[0], torch.ones_like(z), torch.eye(64, dtype=z.dtype, device=DEV)
+    o = ops.Ops(ops.egeria_linear_workspace_bytes(n, 64, 64), DEV)
+    kw = dict(z_in=z, act_in="gelu") if inner else dict(z=z, act="gelu")
+    slope = act64(z.double(), "gelu")[1]
+    assert float(slope.abs().min()) < 2.0 ** -12
+    close(o.egeria_linear_backward(one, None, eye, need_dw=False, **kw)[0], slope, U[z.dtype] * slope.abs() + 2.0 ** -22 + TINY[z.dtype], "slope")
+
+
 @pytest.mark.parametrize("bits", [32, 8])
 def test_adamw_of_second_moments_below_the_normal_range(bits):
     """Without an eps to hide it: a second moment of 1e-41 has a root.  It is held to 2^-149, so v is off by three units of

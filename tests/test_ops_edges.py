@@ -311,6 +311,17 @@ def test_slope_of_gelu_next_to_its_zero(inner):
     close(o.egeria_linear_backward(one, None, eye, need_dw=False, **kw)[0], slope, U[z.dtype] * slope.abs() + 2.0 ** -22 + TINY[z.dtype], "slope")
 
 
+@pytest.mark.parametrize("act,at_zero", [("relu", 0.0), ("gelu", 0.5), ("gelu_tanh", 0.5), ("silu", 0.5)])
+def test_slopes_at_both_zeros(act, at_zero):
+    z = torch.zeros(64, 64, dtype=torch.bfloat16, device=DEV)
+    z[::2] = -0.0
+    one, eye = torch.ones_like(z), torch.eye(64, dtype=z.dtype, device=DEV)
+    o = ops.Ops(ops.egeria_linear_workspace_bytes(64, 64, 64), DEV)
+    for kw in (dict(z_in=z, act_in=act), dict(z=z, act=act)):
+        assert (o.egeria_linear_backward(one, None, eye, need_dw=False, **kw)[0] == at_zero).all()
+    assert not o.egeria_linear_forward(z, eye, act=act).any()
+
+
 @pytest.mark.parametrize("bits", [32, 8])
 def test_adamw_of_second_moments_below_the_normal_range(bits):
     """Without an eps to hide it: a second moment of 1e-41 has a root.  It is held to 2^-149, so v is off by three units of

@@ -115,6 +115,50 @@ typedef struct {
 } egeria_linear_backward_args;
 egeria_status egeria_linear_backward(egeria_ops *ops, void *cuda_stream, const egeria_linear_backward_args *args);
 
+/* ---------------------------------------------------------------------------- gated feed-forward blocks */
+
+/* Bytes of workspace that both calls of a block with these sizes, or with smaller ones, fit into, whatever the alignment of
+ * their operands.  Pure host arithmetic; 0 for invalid arguments. */
+size_t egeria_gated_workspace_bytes(int64_t rows, int64_t inp, int64_t hidden, int64_t out);
+
+/* g = x w_gate^T + b_gate,  u = x w_up^T + b_up,  h = act(g) u,  y = h w_down^T + b_down + residual.
+ *   type      EGERIA_BF16 or EGERIA_F16, of all operands
+ *   act       any egeria_act (EGERIA_ACT_NONE: the product of the two projections)
+ *   x         [rows, inp]        w_gate, w_up  [hidden, inp]     w_down  [out, hidden]
+ *   b_gate, b_up [hidden], b_down [out], residual [rows, out]: each may be NULL; residual may be y itself (same pointer and pitch)
+ *   y         [rows, out]
+ *   g, u      [rows, hidden], both or neither NULL: what the backward call needs
+ * Otherwise y, g and u share no value with an operand or each other (EGERIA_ERR_INVALID_ARG; w_gate and w_up may be parts of
+ * one matrix).  h is rounded to `type`, which is what the second product takes; it is made from g and u before they are rounded.
+ * rows may be 0 (nothing is done); inp, hidden and out are at least 1; none above 2^31 - 1024. */
+typedef struct {
+    int32_t type, act;
+    int64_t rows, inp, hidden, out;
+    const void *x, *w_gate, *w_up, *w_down, *b_gate, *b_up, *b_down, *residual;
+    int64_t ldx, ldw_gate, ldw_up, ldw_down, ldr;
+    void *y, *g, *u;
+    int64_t ldy, ldg, ldu;
+} egeria_gated_forward_args;
+egeria_status egeria_gated_forward(egeria_ops *ops, void *cuda_stream, const egeria_gated_forward_args *args);
+
+/* The gradients, given dy, that of y, and g and u as the forward call left them:
+ *   dh = dy w_down       dg = dh u act'(g)       du = dh act(g)
+ *   dx = dg w_gate + du w_up     dw_gate = dg^T x     dw_up = du^T x     dw_down = dy^T (act(g) u)
+ *   db_gate, db_up, db_down: the sums over rows of dg, du and dy
+ * The gradient of the residual is dy itself.  Each of the seven results may be NULL: not computed (a frozen block needs dx alone).
+ * x is needed for dw_gate and dw_up, w_gate and w_up for dx, w_down, g and u for all but db_down.  dh is not rounded; dg, du and
+ * act(g) u are, to `type`, as operands of the products; the sums are taken before that.  The results share no value with what the
+ * call reads or each other.  With rows = 0 the gradients of weights and biases are set to 0. */
+typedef struct {
+    int32_t type, act;
+    int64_t rows, inp, hidden, out;
+    const void *dy, *x, *w_gate, *w_up, *w_down, *g, *u;
+    int64_t lddy, ldx, ldw_gate, ldw_up, ldw_down, ldg, ldu;
+    void *dx, *dw_gate, *dw_up, *dw_down, *db_gate, *db_up, *db_down;
+    int64_t lddx, lddw_gate, lddw_up, lddw_down;
+} egeria_gated_backward_args;
+egeria_status egeria_gated_backward(egeria_ops *ops, void *cuda_stream, const egeria_gated_backward_args *args);
+
 /* ---------------------------------------------------------------------------- residual norms */
 
 typedef enum { EGERIA_NORM_LAYER = 0, EGERIA_NORM_RMS = 1 } egeria_norm_kind;

@@ -19,6 +19,7 @@ enum OpsCheckCode : int32_t {
     kCheckSlopeRun = 15,    // linear backward: a block's rows, or the place of its partial sums
     kCheckNormRows = 16,    // norm backward: a CTA's rows
     kCheckNormGate = 17,    // norm backward: a group's gate, or the CTAs that share it
+    kCheckGatedSums = 18,   // gated backward: the place of a piece's column sums
 };
 
 using bf16 = __nv_bfloat16;

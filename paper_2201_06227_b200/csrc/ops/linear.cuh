@@ -48,6 +48,12 @@ struct Epilogue {
     const void *bias, *extra;
     void *out, *z;
     int64_t ldx, ldo, ldz;           // pitches of extra, out, z
+    // gated blocks only: the up projection's bias, argument and pitches, and the backward pass's partial column sums
+    const void *bias2, *extra2;
+    void *z2;
+    int64_t ldx2, ldz2;
+    float *sums, *sums2;             // [tiles_m * 4 MB CG][n], one row per 32 rows of the matrix, or null
+    int64_t sums_room;               // values in each (checked build)
     int32_t act, act_in;
     int32_t slope;                   // extra is the argument of act_in, not a residual
     int32_t wide;                    // every matrix here takes 32-byte (2), 16-byte (1) or only 2-byte (0) accesses
@@ -55,7 +61,8 @@ struct Epilogue {
 };
 struct GemmProblem {
     CUtensorMap a, b;
-    int32_t m, n, kblocks;
+    CUtensorMap a2, b2;              // of the k blocks from kb2 on (a sum of two products), or b2: the up projection of a gated block
+    int32_t m, n, kblocks, kb2;
     int32_t tiles_m, tiles_n, splits, group_n, units;
     uint32_t a_mn, b_mn;             // the operand's m (n) axis is the consecutive one
     Epilogue epi;
@@ -70,26 +77,35 @@ struct ColumnSums {
     void *out;
     int32_t n, cols;
 };
+constexpr int kMaxProblems = 4, kMaxSums = 3;
 struct GemmParams {
-    GemmProblem problem[2];
-    ColumnSums sums;                 // added up by the epilogue's warps while the first products are computed
+    GemmProblem problem[kMaxProblems];
+    ColumnSums sums[kMaxSums];       // added up by the epilogue's warps while the first products are computed
 
-    int32_t fill;                    // units of the second product that each worker without a last unit of the first takes before the rest
+    int32_t first, second;           // units of the leading products, which are equally long, and of the last one where there are several
+    int32_t fill;                    // units of the last product that each worker without a last unit of the others takes before the rest
     uint32_t is_f16;
     uint32_t stall;                  // test hook: the first worker issues no loads (1), or no MMA after its first stage (2)
     int32_t *status;
     uint64_t wait_limit_ns;
 };
 
-template <int BN, int CG>
+// What a launch computes: linear layers; a gated block's two projections, side by side in one tile, and act(g) * u; the gradients of
+// g and u from that of the hidden values, in the product that makes it; and up to kMaxProblems products that are only stored.
+enum { kModeLinear, kModeGated, kModeGatedBack, kModeStore };
+
+// MB: blocks of 128 rows per CTA and tile.  With one, tensor memory holds two tiles' accumulators, and a tile's epilogue runs
+// beside the next tile's products.  With two, a tile takes all of it: see mma_tile_pair.
+template <int BN, int CG, int MB>
 struct GemmCfg {
-    static constexpr int kABytes = kGemmM * kGemmK * 2;
+    static constexpr int kABytes = MB * kGemmM * kGemmK * 2;
     static constexpr int kBRows = BN / CG;                   // rows of B per CTA
     static constexpr int kBBytes = kBRows * kGemmK * 2;
     static constexpr int kStageBytes = kABytes + kBBytes;
     static constexpr int kRing = 192 * 1024;                 // bytes of stages
     static constexpr int kStages = kRing / kStageBytes > 8 ? 8 : kRing / kStageBytes;
     static constexpr int kTmemCols = 2 * BN;
+    static constexpr int kTileRows = kGemmM * CG * MB;
     static constexpr int kThreads = 64 + 32 * kEpiWarps;
     static constexpr int kStaging = kEpiWarps * 32 * kStagePitch * 2;
     static constexpr int kSmem = 1024 + kStages * kStageBytes + kStaging + 256;
@@ -252,6 +268,23 @@ __device__ __forceinline__ float act_slope(float z) {
     }
     return 1.0f;
 }
+// Value and slope together: what they share is computed once.
+template <int ACT>
+__device__ __forceinline__ float act_both(float z, float &slope) {
+    if (ACT == kActGelu) {
+        float e;
+        const float phi = normal_cdf<true>(z, e);
+        slope = fmaf(0.39894228040143268f * z, e, phi);
+        return z * phi;
+    }
+    if (ACT == kActSilu) {
+        const float p = logistic2(-kLog2e * z), v = z * p;
+        slope = fmaf(v, 1.0f - p, p);
+        return v;
+    }
+    slope = act_slope<ACT>(z);
+    return act_value<ACT>(z);
+}
 template <int N>
 __device__ __forceinline__ void act_values(float (&v)[N], int act) {
     switch (act) {
@@ -332,14 +365,11 @@ __device__ __forceinline__ void piece_fetch_narrow(uint32_t (&r)[16], const void
 #pragma unroll
     for (int i = 0; i < 16; ++i) r[i] = reinterpret_cast<const uint32_t *>(t.stage)[t.lane * (kStagePitch / 2) + i];
 }
-template <typename T>
-__device__ __forceinline__ void piece_store(void *base, int64_t ld, const float (&v)[32], const Tile &t) {
-    uint32_t r[16];
-#pragma unroll
-    for (int i = 0; i < 16; ++i) r[i] = pack2<T>(v[2 * i], v[2 * i + 1]);
+// This lane's row of a piece, as 16 pairs.
+__device__ __forceinline__ void piece_store(void *base, int64_t ld, const uint32_t (&r)[16], const Tile &t) {
     if (t.fast()) {
         if (t.lane < t.rows) {
-            T *p = static_cast<T *>(base) + (t.row0 + t.lane) * ld + t.col0;
+            uint16_t *p = static_cast<uint16_t *>(base) + (t.row0 + t.lane) * ld + t.col0;
             if (t.wide == 2) {
                 ptx::st_global_v8(reinterpret_cast<float *>(p), r);
                 ptx::st_global_v8(reinterpret_cast<float *>(p + 16), r + 8);
@@ -362,38 +392,52 @@ __device__ __forceinline__ void piece_store(void *base, int64_t ld, const float 
         for (int k = 0; k < rows; ++k) p[k * ld] = t.stage[k * kStagePitch + c];
     }
 }
+template <typename T>
+__device__ __forceinline__ void piece_store(void *base, int64_t ld, const float (&v)[32], const Tile &t) {
+    uint32_t r[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) r[i] = pack2<T>(v[2 * i], v[2 * i + 1]);
+    piece_store(base, ld, r, t);
+}
 // What the epilogue adds to a piece or takes its slope of.
-__device__ __forceinline__ void piece_extra(uint32_t (&r)[16], const Epilogue &p, const Tile &t) {
+__device__ __forceinline__ void piece_extra(uint32_t (&r)[16], const void *extra, int64_t ld, const Tile &t) {
     if (t.rows <= 0 || t.cols <= 0) return;
     if (t.fast())
-        piece_fetch(r, p.extra, p.ldx, t);
+        piece_fetch(r, extra, ld, t);
     else
-        piece_fetch_narrow(r, p.extra, p.ldx, t);
+        piece_fetch_narrow(r, extra, ld, t);
 }
+__device__ __forceinline__ void piece_extra(uint32_t (&r)[16], const Epilogue &p, const Tile &t) { piece_extra(r, p.extra, p.ldx, t); }
 // v: the piece's sums; `extra`: what piece_extra fetched.
 template <typename T>
+__device__ __forceinline__ void piece_bias(const void *bias, int wide, float (&v)[32], const Tile &t) {
+    const T *b = static_cast<const T *>(bias) + t.col0;
+    if (wide && t.cols >= kPiece) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint4 q = *(reinterpret_cast<const uint4 *>(b) + i);
+            const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const float2 f = unpack2<T>(w[j]);
+                v[8 * i + 2 * j] += f.x;
+                v[8 * i + 2 * j + 1] += f.y;
+            }
+        }
+    } else {
+        const float mine = t.lane < min(t.cols, kPiece) ? to_f32(b[t.lane]) : 0.0f;
+#pragma unroll
+        for (int i = 0; i < kPiece; ++i) v[i] += __shfl_sync(0xffffffffu, mine, i);
+    }
+}
+template <typename T, int MODE>
 __device__ __forceinline__ void piece_finish(const Epilogue &p, float (&v)[32], const uint32_t (&extra)[16], const Tile &t) {
     if (t.rows <= 0 || t.cols <= 0) return;  // the same for the whole warp
-    if (p.bias) {
-        const T *b = static_cast<const T *>(p.bias) + t.col0;
-        if (p.wide_bias && t.cols >= kPiece) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const uint4 q = *(reinterpret_cast<const uint4 *>(b) + i);
-                const uint32_t w[4] = {q.x, q.y, q.z, q.w};
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const float2 f = unpack2<T>(w[j]);
-                    v[8 * i + 2 * j] += f.x;
-                    v[8 * i + 2 * j + 1] += f.y;
-                }
-            }
-        } else {
-            const float mine = t.lane < min(t.cols, kPiece) ? to_f32(b[t.lane]) : 0.0f;
-#pragma unroll
-            for (int i = 0; i < kPiece; ++i) v[i] += __shfl_sync(0xffffffffu, mine, i);
-        }
+    if (MODE == kModeStore) {
+        piece_store<T>(p.out, p.ldo, v, t);
+        return;
     }
+    if (p.bias) piece_bias<T>(p.bias, p.wide_bias, v, t);
     if (p.z) piece_store<T>(p.z, p.ldz, v, t);
     if (p.act) act_values(v, p.act);
     if (p.extra) {
@@ -422,6 +466,136 @@ __device__ __forceinline__ void piece_finish(const Epilogue &p, float (&v)[32], 
         }
     }
     piece_store<T>(p.out, p.ldo, v, t);
+}
+
+// ---------------------------------------------------------------- epilogues of a gated block
+// g and u of a 32 x 32 piece: biases, the two kept if wanted, h = act(g) u.
+template <typename T>
+__device__ __forceinline__ void gated_finish(const Epilogue &p, float (&g)[32], float (&u)[32], const Tile &t) {
+    if (t.rows <= 0 || t.cols <= 0) return;
+    if (p.bias) piece_bias<T>(p.bias, p.wide_bias, g, t);
+    if (p.bias2) piece_bias<T>(p.bias2, p.wide_bias, u, t);
+    if (p.z) piece_store<T>(p.z, p.ldz, g, t);
+    if (p.z2) piece_store<T>(p.z2, p.ldz2, u, t);
+    act_values(g, p.act);
+#pragma unroll
+    for (int i = 0; i < 32; ++i) g[i] *= u[i];
+    piece_store<T>(p.out, p.ldo, g, t);
+}
+// A tile of 128 rows by BN / 2 hidden columns: the accumulator's first half is g, the second u.  (BN = 64 has one piece for each
+// row quarter, which the first four warps take.)
+template <typename T, int BN, typename Wait, typename Release>
+__device__ __forceinline__ bool gated_tile(const GemmProblem &q, int32_t tn, Tile &t, uint32_t lanes, int strip, Wait wait, Release release) {
+    constexpr int kHalf = BN / 2, kPieces = kHalf < 64 ? 1 : kHalf / 64;
+    const int first = strip * kPieces * kPiece;
+    if (!wait()) return false;
+    if (first >= kHalf) {
+        release();
+        return true;
+    }
+    t.col0 = tn * kHalf + first;
+    t.cols = q.n - t.col0;
+#pragma unroll 1
+    for (int c = 0; c < kPieces; ++c) {
+        float g[32], u[32];
+        ptx::tmem_ld_32x32(lanes + first + c * kPiece, reinterpret_cast<uint32_t (&)[32]>(g));
+        ptx::tmem_ld_32x32(lanes + kHalf + first + c * kPiece, reinterpret_cast<uint32_t (&)[32]>(u));
+        ptx::tmem_ld_wait();
+        if (c == kPieces - 1) release();
+        gated_finish<T>(q.epi, g, u, t);
+        t.col0 += kPiece;
+        t.cols -= kPiece;
+    }
+    return true;
+}
+
+// dh (in v) to dg (in v), du and h, given g and u as pairs.
+template <typename T, int ACT>
+__device__ __forceinline__ void gated_back_values(float (&v)[32], float (&du)[32], uint32_t (&h)[16], const uint32_t (&g)[16], const uint32_t (&u)[16]) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        const float2 a = unpack2<T>(g[i]), b = unpack2<T>(u[i]);
+        float s0, s1;
+        const float v0 = act_both<ACT>(a.x, s0), v1 = act_both<ACT>(a.y, s1);
+        h[i] = pack2<T>(v0 * b.x, v1 * b.y);
+        du[2 * i] = v[2 * i] * v0;
+        du[2 * i + 1] = v[2 * i + 1] * v1;
+        v[2 * i] *= b.x * s0;
+        v[2 * i + 1] *= b.y * s1;
+    }
+}
+// The sums of a piece's columns over its rows (lanes); lane c leaves with column c's.  In five steps a lane hands half of what it
+// has to the lane that keeps that half: 31 exchanges for 32 columns.
+__device__ __forceinline__ float piece_column_sums(float (&v)[32], const Tile &t) {
+    if (t.lane >= t.rows) {
+#pragma unroll
+        for (int i = 0; i < 32; ++i) v[i] = 0.0f;
+    }
+#pragma unroll
+    for (int o = 16; o; o >>= 1) {
+        const bool upper = t.lane & o;
+#pragma unroll
+        for (int i = 0; i < o; ++i) {
+            const float give = upper ? v[i] : v[i + o], keep = upper ? v[i + o] : v[i];
+            v[i] = keep + __shfl_xor_sync(0xffffffffu, give, o);
+        }
+    }
+    return v[0];
+}
+template <typename T>
+__device__ __forceinline__ void gated_back_finish(const Epilogue &p, float (&v)[32], const uint32_t (&g)[16], const uint32_t (&u)[16], int32_t n,
+                                                  const Tile &t, int32_t *status) {
+    if (t.rows <= 0 || t.cols <= 0) return;
+    float du[32];
+    uint32_t h[16];
+    switch (p.act) {
+#define EG_ACT(A)                                   \
+    case A:                                         \
+        gated_back_values<T, A>(v, du, h, g, u);    \
+        break;
+        EG_ACT(kActRelu)
+        EG_ACT(kActGelu)
+        EG_ACT(kActGeluTanh)
+        EG_ACT(kActSilu)
+#undef EG_ACT
+        default:
+            gated_back_values<T, kActNone>(v, du, h, g, u);
+    }
+    if (p.z2) piece_store(p.z2, p.ldz2, h, t);
+    piece_store<T>(p.out, p.ldo, v, t);
+    piece_store<T>(p.z, p.ldz, du, t);
+    if (p.sums) {
+        const int64_t at = t.row0 / 32 * n + t.col0 + t.lane;
+        const float sg = piece_column_sums(v, t), su = piece_column_sums(du, t);
+        if (t.lane < t.cols && eg_check(at < p.sums_room, status, kCheckGatedSums, at)) {
+            p.sums[at] = sg;
+            p.sums2[at] = su;
+        }
+    }
+}
+template <typename T, int PIECES, typename Wait, typename Release>
+__device__ __forceinline__ bool gated_back_tile(const GemmProblem &q, Tile &t, uint32_t src, int32_t col0, int32_t *status, Wait wait, Release release) {
+    t.col0 = col0;
+    t.cols = q.n - col0;
+    uint32_t g[16], u[16];
+    auto fetch = [&] {
+        piece_extra(g, q.epi.extra, q.epi.ldx, t);
+        piece_extra(u, q.epi.extra2, q.epi.ldx2, t);
+    };
+    fetch();
+    if (!wait()) return false;
+#pragma unroll 1
+    for (int c = 0; c < PIECES; ++c) {
+        float v[32];
+        ptx::tmem_ld_32x32(src + c * kPiece, reinterpret_cast<uint32_t (&)[32]>(v));
+        ptx::tmem_ld_wait();
+        if (c == PIECES - 1) release();
+        gated_back_finish<T>(q.epi, v, g, u, q.n, t, status);
+        t.col0 += kPiece;
+        t.cols -= kPiece;
+        if (c + 1 < PIECES) fetch();
+    }
+    return true;
 }
 
 // 32 columns (lane = column) of a column sum by WARPS warps; `part`: WARPS x 33 floats of shared memory, `barrier`: a
@@ -457,10 +631,17 @@ __device__ __forceinline__ void add_columns(const ColumnSums &s, int strip, int 
 struct GemmUnit {
     int32_t problem, index, tm, tn, tile, split, kb0, kb1;
 };
+template <int PROBLEMS>
 __device__ __forceinline__ GemmUnit gemm_unit(const GemmParams &params, int u) {
     GemmUnit g;
-    g.problem = u >= params.problem[0].units;
-    g.index = g.problem ? u - params.problem[0].units : u;
+    g.problem = 0;
+    g.index = u;
+#pragma unroll
+    for (int i = 0; i + 1 < PROBLEMS; ++i)
+        if (g.problem == i && g.index >= params.problem[i].units) {
+            g.index -= params.problem[i].units;
+            g.problem = i + 1;
+        }
     const GemmProblem &p = params.problem[g.problem];
     g.tile = g.index / p.splits;
     g.split = g.index - g.tile * p.splits;
@@ -476,10 +657,10 @@ __device__ __forceinline__ GemmUnit gemm_unit(const GemmParams &params, int u) {
 __device__ __forceinline__ bool gemm_unit_fits(const GemmProblem &q, const GemmUnit &g) {
     return g.tm >= 0 && g.tm < q.tiles_m && g.tn >= 0 && g.tn < q.tiles_n && g.kb0 >= 0 && g.kb0 < g.kb1 && g.kb1 <= q.kblocks;
 }
-// The step-th unit of a worker (a CTA or a pair), or -1.  The first product's units are dealt round; the workers
-// that the last round of it leaves out take `fill` units of the second each, and then that is dealt round.
+// The step-th unit of a worker (a CTA or a pair), or -1.  The leading products' units are dealt round; the workers
+// that the last round of them leaves out take `fill` units of the last product each, and then that is dealt round.
 __device__ __forceinline__ int gemm_next(const GemmParams &p, int worker, int workers, int step) {
-    const int first = p.problem[0].units, second = p.problem[1].units;
+    const int first = p.first, second = p.second;
     const int rounds = first / workers, left = first - rounds * workers;
     const int mine = rounds + (worker < left);
     if (step < mine) return worker + step * workers;
@@ -499,9 +680,17 @@ __device__ __forceinline__ int gemm_next(const GemmParams &p, int worker, int wo
     return u < second ? first + (int)u : -1;
 }
 
-template <typename T, int BN, int CG>
-__global__ void __launch_bounds__(GemmCfg<BN, CG>::kThreads, 1) gemm_kernel(const __grid_constant__ GemmParams p) {
-    using Cfg = GemmCfg<BN, CG>;
+// The MMAs of one stage: a block of 128 (CG = 2: 256) rows by BN columns by 64 k.
+template <int BN, int CG>
+__device__ __forceinline__ void mma_stage(uint32_t d, uint64_t da, uint64_t db, uint32_t step_a, uint32_t step_b, uint32_t idesc, bool fresh) {
+#pragma unroll
+    for (int k = 0; k < kGemmK / 16; ++k) mma_g<CG>(d, da + k * step_a, db + k * step_b, idesc, (!fresh || k > 0) ? 1u : 0u);
+}
+
+template <typename T, int BN, int CG, int MB, int MODE>
+__global__ void __launch_bounds__(GemmCfg<BN, CG, MB>::kThreads, 1) gemm_kernel(const __grid_constant__ GemmParams p) {
+    using Cfg = GemmCfg<BN, CG, MB>;
+    constexpr int kProblems = MODE == kModeLinear ? 2 : MODE == kModeStore ? kMaxProblems : 1;
     extern __shared__ uint8_t smem_raw[];
     const uint32_t smem_base = (ptx::smem_u32(smem_raw) + 1023u) & ~1023u;
     uint8_t *smem = smem_raw + (smem_base - ptx::smem_u32(smem_raw));
@@ -550,12 +739,15 @@ __global__ void __launch_bounds__(GemmCfg<BN, CG>::kThreads, 1) gemm_kernel(cons
             for (int step = 0; ok; ++step) {
                 const int u = gemm_next(p, worker, workers, step);
                 if (u < 0) break;
-                const GemmUnit g = gemm_unit(p, u);
+                const GemmUnit g = gemm_unit<kProblems>(p, u);
                 const GemmProblem &q = p.problem[g.problem];
                 if (!eg_check(gemm_unit_fits(q, g), p.status, kCheckGemmUnit, u)) break;
                 const CUtensorMap *map_a = &q.a, *map_b = &q.b;
                 const bool a_mn = q.a_mn, b_mn = q.b_mn;
-                const int32_t m0 = (g.tm * CG + (int)rank) * kGemmM, n0 = g.tn * BN + (int)rank * Cfg::kBRows;
+                const int32_t m0 = g.tm * Cfg::kTileRows + (int)rank * kGemmM;
+                const int32_t n0 = MODE == kModeGated ? g.tn * (BN / 2) : g.tn * BN + (int)rank * Cfg::kBRows;
+                // (of a pair the first CTA loads the gate's half of the columns, the second the up projection's)
+                if (MODE == kModeGated && CG == 2 && rank == 1) map_b = &q.b2;
                 for (int kb = g.kb0; kb < g.kb1; ++kb) {
                     if (!ptx::mbar_wait_bounded(empty0 + 8 * stage, phase ^ 1u, abort_flag, p.wait_limit_ns)) {
                         ok = false;
@@ -564,18 +756,31 @@ __global__ void __launch_bounds__(GemmCfg<BN, CG>::kThreads, 1) gemm_kernel(cons
                     const uint32_t sa = smem_base + stage * Cfg::kStageBytes, sb = sa + Cfg::kABytes;
                     if (rank == 0) ptx::mbar_arrive_expect_tx(full0 + 8 * stage, CG * Cfg::kStageBytes);
                     const uint32_t bar = full_base + 8 * stage;
-                    if (a_mn) {
-#pragma unroll
-                        for (int s = 0; s < kGemmM / 64; ++s) tma_load_g<CG>(sa + s * 8192, map_a, m0 + 64 * s, kb * kGemmK, bar);
-                    } else {
-                        tma_load_g<CG>(sa, map_a, kb * kGemmK, m0, bar);
+                    int32_t k0 = kb * kGemmK;
+                    if (MODE == kModeStore && kb >= q.kb2) {
+                        k0 -= q.kb2 * kGemmK;
+                        map_a = &q.a2;
+                        map_b = &q.b2;
                     }
-                    if (b_mn) {
 #pragma unroll
-                        for (int s = 0; s < Cfg::kBRows / 64; ++s)
-                            tma_load_g<CG>(sb + s * 8192, map_b, n0 + 64 * s, kb * kGemmK, bar);
+                    for (int h = 0; h < MB; ++h) {
+                        const uint32_t dst = sa + h * (kGemmM * kGemmK * 2);
+                        const int32_t m = m0 + h * kGemmM * CG;
+                        if (a_mn) {
+#pragma unroll
+                            for (int s = 0; s < kGemmM / 64; ++s) tma_load_g<CG>(dst + s * 8192, map_a, m + 64 * s, k0, bar);
+                        } else {
+                            tma_load_g<CG>(dst, map_a, k0, m, bar);
+                        }
+                    }
+                    if (MODE == kModeGated && CG == 1) {
+                        tma_load_g<CG>(sb, map_b, k0, n0, bar);
+                        tma_load_g<CG>(sb + Cfg::kBBytes / 2, &q.b2, k0, n0, bar);
+                    } else if (b_mn) {
+#pragma unroll
+                        for (int s = 0; s < Cfg::kBRows / 64; ++s) tma_load_g<CG>(sb + s * 8192, map_b, n0 + 64 * s, k0, bar);
                     } else {
-                        tma_load_g<CG>(sb, map_b, kb * kGemmK, n0, bar);
+                        tma_load_g<CG>(sb, map_b, k0, n0, bar);
                     }
                     ++asked;
                     if (++stage == Cfg::kStages) {
@@ -591,47 +796,75 @@ __global__ void __launch_bounds__(GemmCfg<BN, CG>::kThreads, 1) gemm_kernel(cons
         if (lane == 0 && rank == 0) {
             const uint32_t idesc0 = (1u << 4) | (p.is_f16 ? 0u : (1u << 7) | (1u << 10)) | ((uint32_t)(BN >> 3) << 17) |
                                     ((uint32_t)((kGemmM * CG) >> 4) << 24);
-            uint32_t stage = 0, phase = 0, acc = 0, acc_phase = 0;
+            uint32_t it = 0, acc = 0, acc_phase = 0;  // it: stages used so far
             bool ok = true;
             const bool stop = p.stall == 2 && worker == 0;
+            auto wait_full = [&](uint32_t i) {
+                ok = ok && ptx::mbar_wait_bounded(full0 + 8 * (i % Cfg::kStages), (i / Cfg::kStages) & 1u, abort_flag, p.wait_limit_ns);
+                ptx::tc_fence_after_sync();
+                return ok;
+            };
+            auto wait_accumulator = [&](uint32_t a) {
+                ok = ok && ptx::mbar_wait_bounded(accempty0 + 8 * a, acc_phase ^ 1u, abort_flag, p.wait_limit_ns);
+                ptx::tc_fence_after_sync();
+                return ok;
+            };
             for (int step = 0; ok; ++step) {
                 const int u = gemm_next(p, worker, workers, step);
                 if (u < 0) break;
-                const GemmUnit g = gemm_unit(p, u);
+                const GemmUnit g = gemm_unit<kProblems>(p, u);
                 const GemmProblem &q = p.problem[g.problem];
-                if (!ptx::mbar_wait_bounded(accempty0 + 8 * acc, acc_phase ^ 1u, abort_flag, p.wait_limit_ns)) {
-                    ok = false;
-                    break;
-                }
-                ptx::tc_fence_after_sync();
-                const uint32_t d = tmem + acc * BN;
                 const uint32_t idesc = idesc0 | (q.a_mn << 15) | (q.b_mn << 16);
                 const uint32_t step_a = q.a_mn ? 2048u >> 4 : 32u >> 4, step_b = q.b_mn ? 2048u >> 4 : 32u >> 4;
                 const uint64_t base_a = q.a_mn ? make_desc_mn_sw128(0) : ptx::make_desc_k_sw128(0);
                 const uint64_t base_b = q.b_mn ? make_desc_mn_sw128(0) : ptx::make_desc_k_sw128(0);
-                const int kb1 = stop ? g.kb0 + 1 : g.kb1;
-                for (int kb = g.kb0; kb < kb1; ++kb) {
-                    if (!ptx::mbar_wait_bounded(full0 + 8 * stage, phase, abort_flag, p.wait_limit_ns)) {
-                        ok = false;
-                        break;
+                const int n = stop ? 1 : g.kb1 - g.kb0;
+                // stage i's products for the h-th block of rows (a CTA's shared window ends below 2^18)
+                auto issue = [&](uint32_t i, uint32_t slot, int h, bool fresh) {
+                    const uint32_t sa = smem_base + (i % Cfg::kStages) * Cfg::kStageBytes, sb = sa + Cfg::kABytes;
+                    mma_stage<BN, CG>(tmem + slot * BN, base_a | ((sa + h * (kGemmM * kGemmK * 2)) >> 4), base_b | (sb >> 4), step_a, step_b, idesc, fresh);
+                };
+                if (MB == 1) {
+                    if (!wait_accumulator(acc)) break;
+                    for (int k = 0; k < n; ++k, ++it) {
+                        if (!wait_full(it)) break;
+                        issue(it, acc, 0, k == 0);
+                        mma_commit_g<CG>(empty0 + 8 * (it % Cfg::kStages));
                     }
-                    ptx::tc_fence_after_sync();
-                    const uint32_t sa = smem_base + stage * Cfg::kStageBytes, sb = sa + Cfg::kABytes;
-                    const uint64_t da = base_a | (sa >> 4), db = base_b | (sb >> 4);  // (a CTA's shared window ends below 2^18)
-#pragma unroll
-                    for (int k = 0; k < kGemmK / 16; ++k)
-                        mma_g<CG>(d, da + k * step_a, db + k * step_b, idesc, (kb > g.kb0 || k > 0) ? 1u : 0u);
-                    mma_commit_g<CG>(empty0 + 8 * stage);
-                    if (++stage == Cfg::kStages) {
-                        stage = 0;
-                        phase ^= 1u;
+                    if (stop) ok = false;
+                    if (!ok) break;
+                    mma_commit_g<CG>(accfull0 + 8 * acc);
+                    acc ^= 1u;
+                    if (acc == 0) acc_phase ^= 1u;
+                } else {
+                    // Two accumulators that are one tile's halves.  At the tile's ends the halves run apart, so that one half's
+                    // products go on while the epilogue drains the other.
+                    constexpr int kApart = 2;
+                    const int head = min(kApart, n), tail = min(kApart, n - head);
+                    if (!wait_accumulator(0)) break;
+                    for (int k = 0; k < head && wait_full(it + k); ++k) issue(it + k, 0, 0, k == 0);
+                    if (!ok || !wait_accumulator(1)) break;
+                    for (int k = 0; k < head; ++k, ++it) {
+                        issue(it, 1, 1, k == 0);
+                        mma_commit_g<CG>(empty0 + 8 * (it % Cfg::kStages));
                     }
+                    for (int k = head; k < n - tail; ++k, ++it) {
+                        if (!wait_full(it)) break;
+                        issue(it, 0, 0, false);
+                        issue(it, 1, 1, false);
+                        mma_commit_g<CG>(empty0 + 8 * (it % Cfg::kStages));
+                    }
+                    for (int k = 0; ok && k < tail && wait_full(it + k); ++k) issue(it + k, 0, 0, false);
+                    if (stop) ok = false;
+                    if (!ok) break;
+                    mma_commit_g<CG>(accfull0);
+                    for (int k = 0; k < tail; ++k, ++it) {
+                        issue(it, 1, 1, false);
+                        mma_commit_g<CG>(empty0 + 8 * (it % Cfg::kStages));
+                    }
+                    mma_commit_g<CG>(accfull0 + 8);
+                    acc_phase ^= 1u;
                 }
-                if (stop) ok = false;
-                if (!ok) break;
-                mma_commit_g<CG>(accfull0 + 8 * acc);
-                acc ^= 1u;
-                if (acc == 0) acc_phase ^= 1u;
             }
             if (!ok) {
                 // gave up: no MMA of ours may still read shared memory when the CTA leaves
@@ -646,34 +879,56 @@ __global__ void __launch_bounds__(GemmCfg<BN, CG>::kThreads, 1) gemm_kernel(cons
         const int e = warp - 2, quarter = warp & 3, strip = e >> 2;
         uint32_t acc = 0, acc_phase = 0;
         const uint32_t release0 = CG == 2 ? map_to_rank(accempty0, 0) : accempty0;
-        if (p.sums.out) {
-            for (int c = blockIdx.x; c * 32 < p.sums.cols; c += gridDim.x)
-                add_columns<T, kEpiWarps>(p.sums, c, e, lane, reinterpret_cast<float *>(staging),
-                                               [] { asm volatile("bar.sync 1, %0;" ::"n"(32 * kEpiWarps) : "memory"); });
+        if (MODE == kModeLinear || MODE == kModeStore) {
+#pragma unroll 1
+            for (int i = 0; i < (MODE == kModeLinear ? 1 : kMaxSums); ++i)
+                if (p.sums[i].out)
+                    for (int c = blockIdx.x; c * 32 < p.sums[i].cols; c += gridDim.x)
+                        add_columns<T, kEpiWarps>(p.sums[i], c, e, lane, reinterpret_cast<float *>(staging),
+                                                  [] { asm volatile("bar.sync 1, %0;" ::"n"(32 * kEpiWarps) : "memory"); });
         }
         Tile t;
         t.stage = staging + e * 32 * kStagePitch;
         t.lane = lane;
+        // the accumulator is in registers: its columns in tensor memory may be written again
+        auto release = [&] {
+            ptx::tc_fence_before_sync();
+            if (lane == 0) {
+                if (CG == 2)
+                    mbar_arrive_cluster(release0 + 8 * acc);
+                else
+                    ptx::mbar_arrive(release0 + 8 * acc);
+            }
+        };
         for (int step = 0;; ++step) {
             const int u = gemm_next(p, worker, workers, step);
             if (u < 0) break;
-            const GemmUnit g = gemm_unit(p, u);
+            const GemmUnit g = gemm_unit<kProblems>(p, u);
             if (!eg_check(gemm_unit_fits(p.problem[g.problem], g), p.status, kCheckGemmUnit, u)) break;
             // (each product with its own copy of this code: what it takes from the parameters is then at fixed places)
-            auto tile = [&](const GemmProblem &q) {
+            auto tile = [&](const GemmProblem &q, int half) {
                 t.wide = q.epi.wide;
-                t.row0 = (int64_t)(g.tm * CG + (int)rank) * kGemmM + quarter * 32;
+                t.row0 = (int64_t)g.tm * Cfg::kTileRows + (half * CG + (int)rank) * kGemmM + quarter * 32;
                 t.rows = (int)min((int64_t)q.m - t.row0, (int64_t)1 << 20);
+                const uint32_t lanes = tmem + ((uint32_t)(quarter * 32) << 16) + acc * BN;
+                auto wait = [&] {
+                    const bool done = __all_sync(0xffffffffu, ptx::mbar_wait_bounded(accfull0 + 8 * acc, acc_phase, abort_flag, p.wait_limit_ns));
+                    ptx::tc_fence_after_sync();
+                    return done;
+                };
+                if constexpr (MODE == kModeGated) return gated_tile<T, BN>(q, g.tn, t, lanes, strip, wait, release);
+                if constexpr (MODE == kModeGatedBack)
+                    return gated_back_tile<T, Cfg::kPieces>(q, t, lanes + strip * Cfg::kColsPerWarp, g.tn * BN + strip * Cfg::kColsPerWarp, p.status, wait,
+                                                            release);
                 const int col0 = g.tn * BN + strip * Cfg::kColsPerWarp;
                 t.col0 = col0;
                 t.cols = q.n - col0;
                 // what the first piece reads is on its way while the products are computed
                 uint32_t extra[16];
-                const bool ahead = q.epi.extra && q.splits == 1;
+                const bool ahead = MODE == kModeLinear && q.epi.extra && q.splits == 1;
                 if (ahead) piece_extra(extra, q.epi, t);
-                if (!__all_sync(0xffffffffu, ptx::mbar_wait_bounded(accfull0 + 8 * acc, acc_phase, abort_flag, p.wait_limit_ns))) return false;
-                ptx::tc_fence_after_sync();
-                const uint32_t src = tmem + ((uint32_t)(quarter * 32) << 16) + acc * BN + strip * Cfg::kColsPerWarp;
+                if (!wait()) return false;
+                const uint32_t src = lanes + strip * Cfg::kColsPerWarp;
                 float *part = nullptr;
                 if (q.splits > 1)
                     part = q.partials + (((int64_t)g.index * CG + rank) * kEpiWarps + e) * (Cfg::kPieces * 1024);
@@ -686,22 +941,14 @@ __global__ void __launch_bounds__(GemmCfg<BN, CG>::kThreads, 1) gemm_kernel(cons
                     float v[32];
                     ptx::tmem_ld_32x32(src + c * kPiece, reinterpret_cast<uint32_t (&)[32]>(v));
                     ptx::tmem_ld_wait();
-                    if (c == Cfg::kPieces - 1) {
-                        ptx::tc_fence_before_sync();
-                        if (lane == 0) {
-                            if (CG == 2)
-                                mbar_arrive_cluster(release0 + 8 * acc);
-                            else
-                                ptx::mbar_arrive(release0 + 8 * acc);
-                        }
-                    }
+                    if (c == Cfg::kPieces - 1) release();
                     if (q.splits > 1) {
 #pragma unroll
                         for (int j = 0; j < 8; ++j)
                             *reinterpret_cast<float4 *>(part + ((c * 8 + j) * 32 + lane) * 4) =
                                 make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
                     } else {
-                        piece_finish<T>(q.epi, v, extra, t);
+                        piece_finish<T, MODE>(q.epi, v, extra, t);
                         t.col0 += kPiece;
                         t.cols -= kPiece;
                         if (c + 1 < Cfg::kPieces && ahead) piece_extra(extra, q.epi, t);
@@ -721,7 +968,7 @@ __global__ void __launch_bounds__(GemmCfg<BN, CG>::kThreads, 1) gemm_kernel(cons
                         const int64_t pitch = (int64_t)CG * kEpiWarps * Cfg::kPieces * 1024;
 #pragma unroll 1
                         for (int c = 0; c < Cfg::kPieces; ++c) {
-                            if (q.epi.extra) piece_extra(extra, q.epi, t);
+                            if (MODE == kModeLinear && q.epi.extra) piece_extra(extra, q.epi, t);
                             float v[32];
 #pragma unroll
                             for (int i = 0; i < 32; ++i) v[i] = 0.0f;
@@ -732,7 +979,7 @@ __global__ void __launch_bounds__(GemmCfg<BN, CG>::kThreads, 1) gemm_kernel(cons
                                     v[4 * j] += f.x, v[4 * j + 1] += f.y, v[4 * j + 2] += f.z, v[4 * j + 3] += f.w;
                                 }
                             }
-                            piece_finish<T>(q.epi, v, extra, t);
+                            piece_finish<T, MODE>(q.epi, v, extra, t);
                             t.col0 += kPiece;
                             t.cols -= kPiece;
                         }
@@ -741,9 +988,17 @@ __global__ void __launch_bounds__(GemmCfg<BN, CG>::kThreads, 1) gemm_kernel(cons
                 }
                 return true;
             };
-            if (!(g.problem == 0 ? tile(p.problem[0]) : tile(p.problem[1]))) break;
-            acc ^= 1u;
-            if (acc == 0) acc_phase ^= 1u;
+            bool ok = true;
+#pragma unroll 1
+            for (int half = 0; half < MB && ok; ++half) {
+                if (MODE == kModeLinear)
+                    ok = g.problem == 0 ? tile(p.problem[0], half) : tile(p.problem[1], half);
+                else
+                    ok = tile(p.problem[MODE == kModeStore ? g.problem : 0], half);
+                acc ^= 1u;
+                if (acc == 0) acc_phase ^= 1u;
+            }
+            if (!ok) break;
         }
     }
     ptx::tc_fence_before_sync();
@@ -835,6 +1090,77 @@ __global__ void __launch_bounds__(256) linear_few_kernel(const Epilogue p, int32
     }
 }
 
+// The hidden values of a gated block for 1 to 4 rows: as linear_few_kernel, with a row of each projection per turn.
+template <typename T, int ROWS, bool WIDE>
+__global__ void __launch_bounds__(256) gated_few_kernel(const Epilogue p, int32_t m, int32_t n_cols, const T *x, int64_t ldx, const T *wg, int64_t ldg,
+                                                        const T *wu, int64_t ldu, int32_t k) {
+    extern __shared__ uint8_t smem_few[];
+    T *xs = reinterpret_cast<T *>(smem_few);  // [ROWS][k rounded up to 256], zero behind k
+    ptx::grid_dependency_wait();
+    ptx::grid_launch_dependents();
+    const int kp = (k + 255) & ~255;
+    const int rows = min(ROWS, m);
+    for (int i = threadIdx.x; i < ROWS * kp; i += blockDim.x) {
+        const int r = i / kp, c = i - r * kp;
+        xs[i] = (r < rows && c < k) ? x[r * ldx + c] : from_f32<T>(0.0f);
+    }
+    __syncthreads();
+    const int lane = threadIdx.x & 31;
+    const uint32_t warps = gridDim.x * 8;
+    for (uint32_t n = blockIdx.x * 8 + (threadIdx.x >> 5); n < (uint32_t)n_cols; n += warps) {
+        const T *gr = wg + (int64_t)n * ldg, *ur = wu + (int64_t)n * ldu;
+        float g[ROWS], u[ROWS];
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r) g[r] = u[r] = 0.0f;
+        if (WIDE) {
+#pragma unroll 4
+            for (int c = lane * 8; c < k; c += 256) {  // k is a multiple of 8 here
+                Raw8<T> a, b;
+                load8(a, gr + c);
+                load8(b, ur + c);
+                float gv[8], uv[8], xv[8];
+                unpack8(gv, a);
+                unpack8(uv, b);
+#pragma unroll
+                for (int r = 0; r < ROWS; ++r) {
+                    Raw8<T> s = *reinterpret_cast<const Raw8<T> *>(xs + r * kp + c);
+                    unpack8(xv, s);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        g[r] = fmaf(gv[i], xv[i], g[r]);
+                        u[r] = fmaf(uv[i], xv[i], u[r]);
+                    }
+                }
+            }
+        } else {
+#pragma unroll 4
+            for (int c = lane; c < k; c += 32) {
+                const float gv = to_f32(gr[c]), uv = to_f32(ur[c]);
+#pragma unroll
+                for (int r = 0; r < ROWS; ++r) {
+                    const float xv = to_f32(xs[r * kp + c]);
+                    g[r] = fmaf(gv, xv, g[r]);
+                    u[r] = fmaf(uv, xv, u[r]);
+                }
+            }
+        }
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r) g[r] = warp_sum(g[r]), u[r] = warp_sum(u[r]);
+        float vg[1] = {0.0f}, vu = 0.0f;
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r)
+            if (lane == r) vg[0] = g[r], vu = u[r];
+        if (lane < rows) {
+            if (p.bias) vg[0] += to_f32(static_cast<const T *>(p.bias)[n]);
+            if (p.bias2) vu += to_f32(static_cast<const T *>(p.bias2)[n]);
+            if (p.z) static_cast<T *>(p.z)[lane * p.ldz + n] = from_f32<T>(vg[0]);
+            if (p.z2) static_cast<T *>(p.z2)[lane * p.ldz2 + n] = from_f32<T>(vu);
+            act_values(vg, p.act);
+            static_cast<T *>(p.out)[lane * p.ldo + n] = from_f32<T>(vg[0] * vu);
+        }
+    }
+}
+
 // ---------------------------------------------------------------- before the products
 // One launch does what the products of a call need beforehand: copies of operands whose pitch or address no tile
 // load takes, and dz = dy * act'(z) with its column sums.
@@ -853,9 +1179,10 @@ struct SlopeJob {
     int64_t sums_room;               // values that sums has room for (checked build)
     int32_t act, cols, strips, runs; // blocks = strips * runs
 };
+constexpr int kMaxPacks = 4;
 struct PrepareParams {
     SlopeJob slope;
-    PackJob pack[2];
+    PackJob pack[kMaxPacks];
     int32_t *status;
 };
 
@@ -960,8 +1287,9 @@ __global__ void __launch_bounds__(32 * kPrepareWarps) prepare_kernel(const Prepa
         return;
     }
     block -= slopes;
-    const PackJob &j = block < p.pack[0].blocks ? p.pack[0] : p.pack[1];
-    if (block >= p.pack[0].blocks) block -= p.pack[0].blocks;
+    int job = 0;
+    while (job + 1 < kMaxPacks && block >= p.pack[job].blocks) block -= p.pack[job++].blocks;
+    const PackJob &j = p.pack[job];
     const int run = block / j.strips, runs = j.blocks / j.strips;
     const int64_t c = (int64_t)(block - run * j.strips) * 256 + threadIdx.x;
     if (c >= j.cols) return;

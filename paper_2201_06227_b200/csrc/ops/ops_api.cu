@@ -1,130 +1,14 @@
 // Host side of the training operators (include/egeria_ops.h): argument checks, plans, launches.
-#include <algorithm>
 #include <cmath>
-#include <cstring>
 #include <new>
 #include <vector>
 
-#include <cuda.h>
-#include <cuda_runtime.h>
-
-#include "../../../include/egeria_ops.h"
 #include "adamw.cuh"
-#include "linear.cuh"
 #include "norm.cuh"
-
-#define EGO_CUDA(x)                                   \
-    do {                                              \
-        if ((x) != cudaSuccess) {                     \
-            (void)cudaGetLastError();                 \
-            return EGERIA_ERR_CUDA;                   \
-        }                                             \
-    } while (0)
+#include "ops_host.h"
 
 namespace egeria {
 namespace ops {
-
-typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
-                                  const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
-                                  CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
-constexpr size_t kAlign = 256;
-constexpr size_t kHeadBytes = EGERIA_OPS_WORKSPACE_MIN;  // status word, then the tickets of split products
-constexpr size_t kTicketOff = 256;
-constexpr int kMaxTickets = (int)((kHeadBytes - kTicketOff) / 4);
-constexpr int kMaxSplitCtas = 160;                       // CTAs' worth of partial tiles at most
-constexpr uint64_t kWaitLimitNs = 2000000000ull;
-constexpr uint64_t kTestWaitLimitNs = 1000000ull;        // of a launch under egeria_ops_debug_stall_next
-constexpr int64_t kMaxSize = ((int64_t)1 << 31) - 1024;  // tile coordinates are 32-bit
-constexpr int kSms = 148;                                // what workspaces are sized for
-
-// Every kernel is launched as a programmatic dependent of the one before it in the stream: its blocks may take their
-// places while that one's last blocks are running, and each waits for it (griddepcontrol.wait) before it touches memory.
-template <typename... Params, typename... Args>
-static cudaError_t launch(void (*kernel)(Params...), dim3 grid, int threads, size_t smem, cudaStream_t stream, int cluster, const Args &...args) {
-    cudaLaunchConfig_t c{};
-    c.gridDim = grid;
-    c.blockDim = dim3(threads);
-    c.dynamicSmemBytes = smem;
-    c.stream = stream;
-    cudaLaunchAttribute attr[2];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    attr[1].id = cudaLaunchAttributeClusterDimension;
-    attr[1].val.clusterDim.x = cluster;
-    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
-    c.attrs = attr;
-    c.numAttrs = cluster > 1 ? 2 : 1;
-    return cudaLaunchKernelEx(&c, kernel, args...);
-}
-
-static size_t up(size_t v, size_t a) { return (v + a - 1) / a * a; }
-static int64_t pad8(int64_t v) { return (v + 7) / 8 * 8; }
-static bool aligned(const void *p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
-static size_t size_of(int type) { return type == EGERIA_F32 ? 4 : 2; }
-
-// ---------------------------------------------------------------- which tile for which product
-struct GemmPlan {
-    int bn, cg, splits, tiles_m, tiles_n;
-};
-
-// Time of a product of m x n x k in cycles, by a model whose terms are measured ones: a stage of 64 k takes the
-// MMAs' 2 * BN cycles or its bytes at 64 per cycle, whichever is longer; the units go in waves; the epilogue of
-// the last wave is not hidden; a split product pays for its partial sums' way through L2.
-static double gemm_cycles(const GemmPlan &g, int64_t kblocks, int sms) {
-    const double stage_bytes = 128.0 * 128 + 128.0 * g.bn / g.cg;
-    const double per_block = std::max(2.0 * g.bn, stage_bytes / 64.0);
-    const int64_t units = (int64_t)g.tiles_m * g.tiles_n * g.splits, workers = sms / g.cg;
-    const double waves = (double)((units + workers - 1) / workers);
-    const double main_loop = (double)((kblocks + g.splits - 1) / g.splits) * per_block;
-    const double epilogue = 6.0 * g.bn;
-    double t = waves * std::max(main_loop, epilogue) + epilogue + (g.cg == 2 ? 600.0 : 0.0);
-    if (g.splits > 1) t += 2500.0 + 4.0 * g.bn + 4.0 * g.bn * g.splits;
-    return t;
-}
-
-// The best split of the sum for one kind of tile.
-static GemmPlan plan_tile(int64_t m, int64_t n, int64_t k, int sms, int bn, int cg) {
-    const int64_t kblocks = (k + kGemmK - 1) / kGemmK;
-    GemmPlan g{bn, cg, 1, (int)((m + 128 * cg - 1) / (128 * cg)), (int)((n + bn - 1) / bn)}, best = g;
-    const int64_t tiles = (int64_t)g.tiles_m * g.tiles_n;
-    double best_t = gemm_cycles(g, kblocks, sms);
-    const int64_t most = std::min<int64_t>(std::min<int64_t>(64, kblocks), std::min(sms, kMaxSplitCtas) / (tiles * cg));
-    for (g.splits = 2; g.splits <= most; ++g.splits) {
-        const double t = gemm_cycles(g, kblocks, sms);
-        if (t < best_t) best_t = t, best = g;
-    }
-    return best;
-}
-static GemmPlan plan_gemm(int64_t m, int64_t n, int64_t k, int sms) {
-    GemmPlan best{};
-    double best_t = 1e300;
-    for (int cg = 1; cg <= 2; ++cg)
-        for (int bn = cg == 2 ? 128 : 64; bn <= 256; bn *= 2) {
-            const GemmPlan g = plan_tile(m, n, k, sms, bn, cg);
-            const double t = gemm_cycles(g, (k + kGemmK - 1) / kGemmK, sms);
-            if (t < best_t) best_t = t, best = g;
-        }
-    return best;
-}
-static_assert(2 * kMaxSplitCtas * kEpiWarps <= kMaxTickets, "a ticket for every warp of every split tile of two products");
-
-// Bytes of partial tiles that a product of these sizes, or of smaller ones, may need under any plan.  (A product of more
-// tiles than CTAs is not split, but a smaller one in its place is: the bound must not fall as a size grows.)
-static size_t split_bytes(int64_t m, int64_t n, int64_t k) {
-    const int64_t kblocks = std::min<int64_t>((k + kGemmK - 1) / kGemmK, 64);
-    if (kblocks <= 1) return 0;
-    const int64_t tiles = std::min<int64_t>(((m + 255) / 256) * 2 * ((n + 255) / 256), kMaxSplitCtas);  // of 128 x 256
-    return (size_t)std::min<int64_t>(tiles * kblocks, kMaxSplitCtas) * 128 * 256 * 4;
-}
-
-// Runs of rows that dz and its column sums are cut into: four blocks per SM at most, 32 rows at least.
-static int slope_runs(int64_t rows, int64_t cols) {
-    const int64_t strips = (cols + 255) / 256;
-    return (int)std::max<int64_t>(1, std::min<int64_t>((rows + 31) / 32, 4 * kSms / strips));
-}
-// Values of their partial sums at most, for these sizes and all smaller ones (runs * cols <= 4 * kSms * 256 beyond one run).
-static int64_t slope_sums(int64_t rows, int64_t cols) { return std::max(cols, std::min<int64_t>((rows + 31) / 32 * cols, 4 * kSms * 256)); }
 
 struct LinearLayout {
     size_t part, part2, x, w, dz, sums, total;
@@ -173,25 +57,9 @@ static int64_t norm_sums_cols(int64_t rows, int64_t cols) {
 using namespace egeria;
 using namespace egeria::ops;
 
-struct egeria_ops {
-    uint8_t *ws = nullptr;
-    size_t ws_bytes = 0;
-    EncodeTiledFn encode = nullptr;
-    int sms = 0;
-    int64_t launches = 0;
-    cudaStream_t last_stream = nullptr;
-    uint32_t stall_next = 0;  // test hook: give-up path of the next product
-};
-
 namespace egeria {
 namespace ops {
 
-template <typename T, int BN, int CG>
-static cudaError_t allow_smem() {
-    return cudaFuncSetAttribute(gemm_kernel<T, BN, CG>, cudaFuncAttributeMaxDynamicSharedMemorySize, GemmCfg<BN, CG>::kSmem);
-}
-constexpr int kFewSmem = 96 * 1024;
-constexpr int kFewRows = 4;   // rows that go without the tensor cores: at 1024 x 4096 3.7 us for one row, 6.5 for two, 9.0 for four, 10.0 on the tensor cores
 template <typename T, int ROWS>
 static cudaError_t allow_few() {
     cudaError_t e = cudaFuncSetAttribute(linear_few_kernel<T, ROWS, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, kFewSmem);
@@ -201,68 +69,25 @@ static cudaError_t allow_few() {
 }
 template <typename T>
 static cudaError_t allow_all() {
-    cudaError_t e = allow_smem<T, 64, 1>();
-    if (e == cudaSuccess) e = allow_smem<T, 128, 1>();
-    if (e == cudaSuccess) e = allow_smem<T, 256, 1>();
-    if (e == cudaSuccess) e = allow_smem<T, 128, 2>();
-    if (e == cudaSuccess) e = allow_smem<T, 256, 2>();
+    cudaError_t e = allow_smem<T, 64, 1, 1, kModeLinear>();
+    if (e == cudaSuccess) e = allow_smem<T, 128, 1, 1, kModeLinear>();
+    if (e == cudaSuccess) e = allow_smem<T, 256, 1, 1, kModeLinear>();
+    if (e == cudaSuccess) e = allow_smem<T, 128, 2, 1, kModeLinear>();
+    if (e == cudaSuccess) e = allow_smem<T, 256, 2, 1, kModeLinear>();
     if (e == cudaSuccess) e = allow_few<T, 1>();
     if (e == cudaSuccess) e = allow_few<T, 2>();
     if (e == cudaSuccess) e = allow_few<T, 4>();
     return e;
 }
 
-struct Operand {
-    const void *p;
-    int64_t ld, rows, cols;
-    bool mn;  // the product's m (n) axis is the consecutive one: cols = m (n), rows = k
-};
-
-static egeria_status encode_operand(const egeria_ops *o, CUtensorMap *map, const Operand &a, int type, int box_rows) {
-    cuuint64_t dims[2] = {(cuuint64_t)a.cols, (cuuint64_t)a.rows};
-    cuuint64_t strides[1] = {(cuuint64_t)a.ld * 2};
-    cuuint32_t box[2] = {64, (cuuint32_t)(a.mn ? 64 : box_rows)};
-    cuuint32_t one[2] = {1, 1};
-    const CUresult r = o->encode(map, type == EGERIA_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2,
-                                 const_cast<void *>(a.p), dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                                 CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-    return r == CUDA_SUCCESS ? EGERIA_OK : EGERIA_ERR_CUDA;
-}
-
-template <typename T, int BN, int CG>
-static cudaError_t launch_gemm(const GemmParams &p, int ctas, cudaStream_t stream) {
-    return launch(gemm_kernel<T, BN, CG>, dim3(ctas), GemmCfg<BN, CG>::kThreads, GemmCfg<BN, CG>::kSmem, stream, CG, p);
-}
 template <typename T>
 static cudaError_t launch_gemm_any(int bn, int cg, const GemmParams &p, int ctas, cudaStream_t stream) {
-    if (cg == 2) return bn == 128 ? launch_gemm<T, 128, 2>(p, ctas, stream) : launch_gemm<T, 256, 2>(p, ctas, stream);
-    if (bn == 64) return launch_gemm<T, 64, 1>(p, ctas, stream);
-    return bn == 128 ? launch_gemm<T, 128, 1>(p, ctas, stream) : launch_gemm<T, 256, 1>(p, ctas, stream);
+    if (cg == 2) return bn == 128 ? launch_gemm<T, 128, 2, 1, kModeLinear>(p, ctas, stream) : launch_gemm<T, 256, 2, 1, kModeLinear>(p, ctas, stream);
+    if (bn == 64) return launch_gemm<T, 64, 1, 1, kModeLinear>(p, ctas, stream);
+    return bn == 128 ? launch_gemm<T, 128, 1, 1, kModeLinear>(p, ctas, stream) : launch_gemm<T, 256, 1, 1, kModeLinear>(p, ctas, stream);
 }
 
-// Widest access that all of a product's epilogue matrices take: 2 = 32 bytes, 1 = 16 bytes, 0 = one value.
-static void set_widths(Epilogue &e) {
-    int w = 2;
-    auto see = [&](const void *q, int64_t ld) {
-        if (!q) return;
-        if (!aligned(q, 32) || ld % 16) w = std::min(w, aligned(q, 16) && ld % 8 == 0 ? 1 : 0);
-    };
-    see(e.out, e.ldo);
-    see(e.z, e.ldz);
-    see(e.extra, e.ldx);
-    e.wide = w;
-    e.wide_bias = aligned(e.bias, 16);
-}
-
-// One product D = A B^T of a launch; k = the length of the summed axis.
-struct Product {
-    int64_t m, n, k;
-    Operand a, b;
-    Epilogue epi;
-    size_t part;    // its partial tiles in the workspace
-};
-
-static egeria_status run_products(egeria_ops *o, cudaStream_t stream, int type, Product *jobs, int count, const ColumnSums &sums) {
+egeria_status run_products(egeria_ops *o, cudaStream_t stream, int type, Product *jobs, int count, const ColumnSums &sums) {
     // the tile that suits the launch: of the plans of each product, the one that is best for all of them
     GemmPlan plan[2];
     double best = 1e300;
@@ -279,75 +104,20 @@ static egeria_status run_products(egeria_ops *o, cudaStream_t stream, int type, 
             for (int j = 0; j < count; ++j) plan[j] = g[j];
         }
     }
-    const int bn = plan[0].bn, cg = plan[0].cg, workers = o->sms / cg;
     GemmParams p;
-    memset(&p, 0, sizeof(p));
-    int64_t units = 0;
-    for (int i = 0; i < count; ++i) {
-        const Product &j = jobs[i];
-        const GemmPlan &g = plan[i];
-        GemmProblem &q = p.problem[i];
-        if (g.splits > 1 && (size_t)g.tiles_m * g.tiles_n * g.splits * cg * 128 * bn * 4 > split_bytes(j.m, j.n, j.k)) return EGERIA_ERR_WORKSPACE;
-        egeria_status s = encode_operand(o, &q.a, j.a, type, kGemmM);
-        if (s == EGERIA_OK) s = encode_operand(o, &q.b, j.b, type, bn / cg);
-        if (s != EGERIA_OK) return s;
-        q.m = (int32_t)j.m;
-        q.n = (int32_t)j.n;
-        q.kblocks = (int32_t)((j.k + kGemmK - 1) / kGemmK);
-        q.tiles_m = g.tiles_m;
-        q.tiles_n = g.tiles_n;
-        q.splits = g.splits;
-        const int64_t n_units = (int64_t)g.tiles_m * g.tiles_n * g.splits;
-        if (n_units > 0x3fffffff) return EGERIA_ERR_UNSUPPORTED_SHAPE;
-        q.units = (int32_t)n_units;
-        units += n_units;
-        // a strip of B of at most 16 MB, so that it stays in L2 next to the rows of A that go by
-        q.group_n = (int32_t)std::max<int64_t>(1, std::min<int64_t>(g.tiles_n, ((int64_t)16 << 20) / (2 * j.k * bn)));
-        q.a_mn = j.a.mn;
-        q.b_mn = j.b.mn;
-        q.epi = j.epi;
-        set_widths(q.epi);
-        q.partials = reinterpret_cast<float *>(o->ws + j.part);
-        q.tickets = reinterpret_cast<int32_t *>(o->ws + kTicketOff) + i * (kMaxTickets / 2);
-        q.partial_floats = (int64_t)split_bytes(j.m, j.n, j.k) / 4;
-        q.ticket_room = kMaxTickets / 2;
-    }
-    const int used = (int)std::min<int64_t>(units, workers);
-    if (count == 2) {
-        // the workers without a last unit of the first product have its time for units of the second
-        const int left = p.problem[0].units % used;
-        if (left) p.fill = (p.problem[0].kblocks / p.problem[0].splits) / std::max(1, p.problem[1].kblocks / p.problem[1].splits);
-        p.fill = std::min<int64_t>(p.fill, p.problem[1].units / used + 1);
-    }
-    p.sums = sums;
-    p.is_f16 = type == EGERIA_F16;
-    p.status = reinterpret_cast<int32_t *>(o->ws);
-    p.stall = o->stall_next;
-    p.wait_limit_ns = o->stall_next ? kTestWaitLimitNs : kWaitLimitNs;
-    o->stall_next = 0;
-    const int ctas = used * cg;
+    int ctas = 0;
+    const egeria_status s = fill_products(o, type, kModeLinear, jobs, plan, count, p, ctas);
+    if (s != EGERIA_OK) return s;
+    p.sums[0] = sums;
+    const int bn = plan[0].bn, cg = plan[0].cg;
     EGO_CUDA(type == EGERIA_BF16 ? launch_gemm_any<bf16>(bn, cg, p, ctas, stream) : launch_gemm_any<f16>(bn, cg, p, ctas, stream));
     ++o->launches;
     return EGERIA_OK;
 }
 
-// The operand as a tile load takes it: itself, or the copy that `job` makes of it at `spare` with a pitch of pad8(cols).
-static void make_loadable(egeria_ops *o, Operand &a, size_t spare, PackJob &job) {
-    if (aligned(a.p, 16) && a.ld % 8 == 0) return;
-    job.src = static_cast<const uint16_t *>(a.p);
-    job.dst = reinterpret_cast<uint16_t *>(o->ws + spare);
-    job.ld = a.ld;
-    job.pitch = pad8(a.cols);
-    job.rows = a.rows;
-    job.cols = a.cols;
-    job.strips = (int32_t)((a.cols + 255) / 256);
-    job.blocks = job.strips * (int32_t)std::max<int64_t>(1, std::min<int64_t>((a.rows + 7) / 8, 8 * kSms / job.strips));
-    a.p = job.dst;
-    a.ld = job.pitch;
-}
-
-static egeria_status run_prepare(egeria_ops *o, cudaStream_t stream, int type, const PrepareParams &p, bool wide) {
-    const int64_t blocks = (int64_t)p.slope.strips * p.slope.runs + p.pack[0].blocks + p.pack[1].blocks;
+egeria_status run_prepare(egeria_ops *o, cudaStream_t stream, int type, const PrepareParams &p, bool wide) {
+    int64_t blocks = (int64_t)p.slope.strips * p.slope.runs;
+    for (const PackJob &j : p.pack) blocks += j.blocks;
     if (blocks == 0) return EGERIA_OK;
     if (blocks > 0x7fffffff) return EGERIA_ERR_UNSUPPORTED_SHAPE;
     auto go = [&](auto kernel) { return launch(kernel, dim3((unsigned)blocks), 32 * kPrepareWarps, 0, stream, 1, p); };
@@ -370,38 +140,6 @@ static cudaError_t launch_few_any(const Epilogue &e, const egeria_linear_forward
     if (a.rows <= 1) return launch_few<T, 1>(e, a, wide, sms, stream);
     if (a.rows <= 2) return launch_few<T, 2>(e, a, wide, sms, stream);
     return launch_few<T, 4>(e, a, wide, sms, stream);
-}
-
-static bool good_matrix(const void *p, int64_t ld, int64_t cols, size_t elem) { return p && aligned(p, elem) && ld >= cols; }
-static bool good_optional(const void *p, int64_t ld, int64_t cols, size_t elem) { return !p || good_matrix(p, ld, cols, elem); }
-
-// Whether two matrices of 2-byte values share one.  Parts of one buffer may lie between each other's rows.
-struct Extent {
-    const void *p;
-    int64_t ld, rows, cols;
-};
-static bool overlap(const Extent &a, const Extent &b) {
-    if (a.rows < b.rows) return overlap(b, a);
-    if (!a.p || !b.p) return false;
-    const int64_t at = (int64_t)(reinterpret_cast<uintptr_t>(b.p) / 2) - (int64_t)(reinterpret_cast<uintptr_t>(a.p) / 2);
-    if (at >= (a.rows - 1) * a.ld + a.cols || -at >= (b.rows - 1) * b.ld + b.cols) return false;
-    if (a.ld == b.ld && b.rows > 1) {
-        // row r of b begins at column `col` of a's row `row` + r and may reach into the next one
-        const int64_t col = (at % a.ld + a.ld) % a.ld, row = (at - col) / a.ld;
-        auto meet = [&](int64_t first) { return first < a.rows && first + b.rows > 0; };
-        return (col < a.cols && meet(row)) || (col + b.cols > a.ld && meet(row + 1));
-    }
-    for (int64_t r = 0; r < b.rows; ++r) {
-        const int64_t from = at + r * b.ld, end = from + b.cols;  // rows of a that end behind `from` and begin before `end`
-        const int64_t first = from < a.cols ? 0 : (from - a.cols) / a.ld + 1;
-        if (end > 0 && first <= std::min(a.rows - 1, (end - 1) / a.ld)) return true;
-    }
-    return false;
-}
-static bool good_act(int act) { return act >= EGERIA_ACT_NONE && act <= EGERIA_ACT_SILU; }
-static egeria_status good_sizes(int64_t rows, int64_t inp, int64_t out) {
-    if (rows < 0 || inp < 1 || out < 1) return EGERIA_ERR_INVALID_ARG;
-    return rows > kMaxSize || inp > kMaxSize || out > kMaxSize ? EGERIA_ERR_UNSUPPORTED_SHAPE : EGERIA_OK;
 }
 
 // ---------------------------------------------------------------- norm launches
@@ -511,6 +249,36 @@ static bool adam_layout(int count, const egeria_adamw_tensor *t, AdamLayout &L) 
     return true;
 }
 
+// Whether a forward call goes without the tensor cores, and needs no workspace.
+static bool linear_few(const egeria_linear_forward_args &a) {
+    const int few_rows = a.rows <= 2 ? (int)a.rows : 4;
+    return a.rows <= kFewRows && (a.inp + 255) / 256 * 256 * 2 * few_rows <= kFewSmem;
+}
+egeria_status linear_forward_at(egeria_ops *ops, cudaStream_t stream, const egeria_linear_forward_args &a, size_t part, size_t x, size_t w) {
+    Epilogue e{};
+    e.bias = a.bias;
+    e.extra = a.residual;
+    e.ldx = a.ldr;
+    e.out = a.y;
+    e.ldo = a.ldy;
+    e.z = a.z;
+    e.ldz = a.ldz;
+    e.act = a.act;
+    if (linear_few(a)) {
+        const bool wide = a.inp % 8 == 0 && a.ldw % 8 == 0 && aligned(a.w, 16);
+        EGO_CUDA(a.type == EGERIA_BF16 ? launch_few_any<bf16>(e, a, wide, ops->sms, stream) : launch_few_any<f16>(e, a, wide, ops->sms, stream));
+        ++ops->launches;
+        return EGERIA_OK;
+    }
+    PrepareParams prep{};
+    prep.status = reinterpret_cast<int32_t *>(ops->ws);
+    Product job{a.rows, a.out, a.inp, {a.x, a.ldx, a.rows, a.inp, false}, {a.w, a.ldw, a.out, a.inp, false}, e, part};
+    make_loadable(ops, job.a, x, prep.pack[0]);
+    make_loadable(ops, job.b, w, prep.pack[1]);
+    const egeria_status s = run_prepare(ops, stream, a.type, prep, false);
+    return s != EGERIA_OK ? s : run_products(ops, stream, a.type, &job, 1, ColumnSums{});
+}
+
 }  // namespace ops
 }  // namespace egeria
 
@@ -547,6 +315,7 @@ egeria_status egeria_ops_create(egeria_ops **out, void *workspace, size_t worksp
     }
     EGO_CUDA(allow_all<bf16>());
     EGO_CUDA(allow_all<f16>());
+    EGO_CUDA(allow_gated());
     // the workspace may be memory that earlier work of a stream which the default stream does not wait for still writes to
     EGO_CUDA(cudaDeviceSynchronize());
     EGO_CUDA(cudaMemset(workspace, 0, kHeadBytes));
@@ -606,34 +375,11 @@ egeria_status egeria_linear_forward(egeria_ops *ops, void *cuda_stream, const eg
     for (int i = 0; i < 4; ++i)
         if ((!(i == 3 && onto) && overlap(y, reads[i])) || overlap(z, reads[i])) return EGERIA_ERR_INVALID_ARG;
     if (overlap(y, z)) return EGERIA_ERR_INVALID_ARG;
-    const int few_rows = a.rows <= 2 ? (int)a.rows : 4;
-    const bool few = a.rows <= kFewRows && (a.inp + 255) / 256 * 256 * 2 * few_rows <= kFewSmem;  // needs no workspace
     const LinearLayout L = linear_layout(a.rows, a.inp, a.out);
-    if (!few && ops->ws_bytes < L.total) return EGERIA_ERR_WORKSPACE;
+    if (!linear_few(a) && ops->ws_bytes < L.total) return EGERIA_ERR_WORKSPACE;
     cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
     ops->last_stream = stream;
-    Epilogue e{};
-    e.bias = a.bias;
-    e.extra = a.residual;
-    e.ldx = a.ldr;
-    e.out = a.y;
-    e.ldo = a.ldy;
-    e.z = a.z;
-    e.ldz = a.ldz;
-    e.act = a.act;
-    if (few) {
-        const bool wide = a.inp % 8 == 0 && a.ldw % 8 == 0 && aligned(a.w, 16);
-        EGO_CUDA(a.type == EGERIA_BF16 ? launch_few_any<bf16>(e, a, wide, ops->sms, stream) : launch_few_any<f16>(e, a, wide, ops->sms, stream));
-        ++ops->launches;
-        return EGERIA_OK;
-    }
-    PrepareParams prep{};
-    prep.status = reinterpret_cast<int32_t *>(ops->ws);
-    Product job{a.rows, a.out, a.inp, {a.x, a.ldx, a.rows, a.inp, false}, {a.w, a.ldw, a.out, a.inp, false}, e, L.part};
-    make_loadable(ops, job.a, L.x, prep.pack[0]);
-    make_loadable(ops, job.b, L.w, prep.pack[1]);
-    if ((s = run_prepare(ops, stream, a.type, prep, false)) != EGERIA_OK) return s;
-    return run_products(ops, stream, a.type, &job, 1, ColumnSums{});
+    return linear_forward_at(ops, stream, a, L.part, L.x, L.w);
 }
 
 egeria_status egeria_linear_backward(egeria_ops *ops, void *cuda_stream, const egeria_linear_backward_args *args) {

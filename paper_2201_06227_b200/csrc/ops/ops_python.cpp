@@ -181,6 +181,90 @@ PyObject *linear_backward(PyObject *, PyObject *const *args, Py_ssize_t n) {
     END_HANDLE_TH_ERRORS
 }
 
+// x, w_gate, w_up, w_down, b_gate, b_up, b_down, act, residual, save, out -> y or (y, g, u)
+PyObject *gated_forward(PyObject *, PyObject *const *args, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    const Call c(args, n, 4 + 11);
+    const Tensor &x = tensor(c.rest[0], "x"), &wg = tensor(c.rest[1], "w_gate"), &wu = tensor(c.rest[2], "w_up"), &wd = tensor(c.rest[3], "w_down");
+    if (x.dim() != 2 || wg.dim() != 2 || wd.dim() != 2) refuse("x, w_gate, w_up and w_down are matrices");
+    const at::ScalarType t = x.scalar_type();
+    egeria_gated_forward_args a{};
+    a.type = type_of(t);
+    a.act = (int32_t)c.whole(7);
+    a.rows = x.size(0), a.inp = x.size(1), a.hidden = wg.size(0), a.out = wd.size(0);
+    const Matrix mx = matrix(x, "x", c.device, t, a.rows, a.inp), mg = matrix(wg, "w_gate", c.device, t, a.hidden, a.inp);
+    const Matrix mu = matrix(wu, "w_up", c.device, t, a.hidden, a.inp), md = matrix(wd, "w_down", c.device, t, a.out, a.hidden);
+    const Matrix mr = matrix(c.rest[8], "residual", c.device, t, a.rows, a.out);
+    a.x = mx.p, a.ldx = mx.ld, a.w_gate = mg.p, a.ldw_gate = mg.ld, a.w_up = mu.p, a.ldw_up = mu.ld, a.w_down = md.p, a.ldw_down = md.ld;
+    a.residual = mr.p, a.ldr = mr.ld;
+    a.b_gate = vector(c.rest[4], "b_gate", c.device, t, a.hidden);
+    a.b_up = vector(c.rest[5], "b_up", c.device, t, a.hidden);
+    a.b_down = vector(c.rest[6], "b_down", c.device, t, a.out);
+    const Tensor y = c.given(10) ? tensor(c.rest[10], "out") : make(x, {a.rows, a.out});
+    const bool save = c.flag(9);
+    const Tensor g = save ? make(x, {a.rows, a.hidden}) : Tensor(), u = save ? make(x, {a.rows, a.hidden}) : Tensor();
+    const Matrix my = matrix(y, "out", c.device, t, a.rows, a.out);
+    a.y = my.p, a.ldy = my.ld;
+    if (save) a.g = g.data_ptr(), a.u = u.data_ptr(), a.ldg = a.ldu = a.hidden;
+    const egeria_status s = reinterpret_cast<decltype(&egeria_gated_forward)>(c.fn)(static_cast<egeria_ops *>(c.handle), c.stream, &a);
+    if (s != EGERIA_OK) return PyLong_FromLong(s);
+    if (c.given(10) && !y.is_inference()) y.unsafeGetTensorImpl()->bump_version();   // written in place
+    const char *const back = "egeria_gated_backward";
+    const Tensor *const from = followed(c, {0, 1, 2, 3, 4, 5, 6, 8});
+    if (!save) return wrap(y, from, back);
+    return Py_BuildValue("(NNN)", wrap(y, from, back), wrap(g, from, back), wrap(u, from, back));
+    END_HANDLE_TH_ERRORS
+}
+
+// dy, x, w_gate, w_up, w_down, g, u, act, need_dx, need_dw, need_db -> (dx, dw_gate, dw_up, dw_down, db_gate, db_up, db_down)
+PyObject *gated_backward(PyObject *, PyObject *const *args, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    const Call c(args, n, 4 + 11);
+    const Tensor &dy = tensor(c.rest[0], "dy"), &wd = tensor(c.rest[4], "w_down"), &g = tensor(c.rest[5], "g"), &u = tensor(c.rest[6], "u");
+    const bool need_dx = c.flag(8), need_dw = c.flag(9), need_db = c.flag(10);
+    if (dy.dim() != 2 || wd.dim() != 2 || (need_dx && (!c.given(2) || !c.given(3))) || (need_dw && !c.given(1)))
+        refuse("dy and w_down are matrices; dx needs w_gate and w_up, the weights' gradients need x");
+    const at::ScalarType t = dy.scalar_type();
+    egeria_gated_backward_args a{};
+    a.type = type_of(t);
+    a.act = (int32_t)c.whole(7);
+    a.rows = dy.size(0), a.out = dy.size(1), a.hidden = wd.size(1), a.inp = 1;
+    for (int i = 1; i < 3; ++i)
+        if (c.given(i)) {
+            const Tensor &inner = tensor(c.rest[i], i == 1 ? "x" : "w_gate");
+            if (inner.dim() != 2) refuse("x and the weights are matrices");
+            a.inp = inner.size(1);
+            break;
+        }
+    const Matrix mdy = matrix(dy, "dy", c.device, t, a.rows, a.out), mx = matrix(c.rest[1], "x", c.device, t, a.rows, a.inp);
+    const Matrix mg = matrix(c.rest[2], "w_gate", c.device, t, a.hidden, a.inp), mu = matrix(c.rest[3], "w_up", c.device, t, a.hidden, a.inp);
+    const Matrix md = matrix(wd, "w_down", c.device, t, a.out, a.hidden);
+    const Matrix ga = matrix(g, "g", c.device, t, a.rows, a.hidden), ua = matrix(u, "u", c.device, t, a.rows, a.hidden);
+    a.dy = mdy.p, a.lddy = mdy.ld, a.x = mx.p, a.ldx = mx.ld, a.w_gate = mg.p, a.ldw_gate = mg.ld, a.w_up = mu.p, a.ldw_up = mu.ld;
+    a.w_down = md.p, a.ldw_down = md.ld, a.g = ga.p, a.ldg = ga.ld, a.u = ua.p, a.ldu = ua.ld;
+    const Tensor dx = need_dx ? make(dy, {a.rows, a.inp}) : Tensor();
+    // (one tensor for the two projections: a model that keeps them side by side has its gradient whole)
+    Tensor dw, dw_gate, dw_up, dw_down, db, db_gate, db_up, db_down;
+    if (need_dw) {
+        dw = make(dy, {2 * a.hidden, a.inp});
+        dw_gate = dw.narrow(0, 0, a.hidden), dw_up = dw.narrow(0, a.hidden, a.hidden);
+        dw_down = make(dy, {a.out, a.hidden});
+        a.dw_gate = dw_gate.data_ptr(), a.dw_up = dw_up.data_ptr(), a.dw_down = dw_down.data_ptr();
+        a.lddw_gate = a.lddw_up = a.inp, a.lddw_down = a.hidden;
+    }
+    if (need_db) {
+        db = make(dy, {2 * a.hidden});
+        db_gate = db.narrow(0, 0, a.hidden), db_up = db.narrow(0, a.hidden, a.hidden);
+        db_down = make(dy, {a.out});
+        a.db_gate = db_gate.data_ptr(), a.db_up = db_up.data_ptr(), a.db_down = db_down.data_ptr();
+    }
+    if (need_dx) a.dx = dx.data_ptr(), a.lddx = a.inp;
+    const egeria_status s = reinterpret_cast<decltype(&egeria_gated_backward)>(c.fn)(static_cast<egeria_ops *>(c.handle), c.stream, &a);
+    if (s != EGERIA_OK) return PyLong_FromLong(s);
+    return Py_BuildValue("(NNNNNNN)", wrap(dx), wrap(dw_gate), wrap(dw_up), wrap(dw_down), wrap(db_gate), wrap(db_up), wrap(db_down));
+    END_HANDLE_TH_ERRORS
+}
+
 // The gate, the weights and the biases (five places of `c` from `first` on), which share a type.
 template <typename Args>
 at::ScalarType norm_vectors(const Call &c, int first, at::ScalarType type, Args &a) {
@@ -287,6 +371,7 @@ PyCFunction fast(F f) {
 PyMethodDef methods[] = {
     {"linear_forward", fast(linear_forward), METH_FASTCALL, nullptr},   {"linear_backward", fast(linear_backward), METH_FASTCALL, nullptr},
     {"norm_forward", fast(norm_forward), METH_FASTCALL, nullptr},       {"norm_backward", fast(norm_backward), METH_FASTCALL, nullptr},
+    {"gated_forward", fast(gated_forward), METH_FASTCALL, nullptr},     {"gated_backward", fast(gated_backward), METH_FASTCALL, nullptr},
     {"adamw_step", fast(adamw_step), METH_FASTCALL, nullptr},           {nullptr, nullptr, 0, nullptr},
 };
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_ops_python", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

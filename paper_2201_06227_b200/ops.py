@@ -1,6 +1,6 @@
 """ctypes binding of the training operators (``include/egeria_ops.h``) -- argument marshalling only.
 
-:class:`Ops` has the linear layers and the residual norms, :class:`AdamW` the optimizer step; their
+:class:`Ops` has the linear layers, the gated feed-forward blocks and the residual norms, :class:`AdamW` the optimizer step; their
 methods have the names of the C entry points that they call.  Everything is computed by the CUDA
 kernels of ``libegeria.so``; there is no fallback: a call that the library refuses raises
 :class:`~paper_2201_06227_b200.binding.EgeriaError`, a tensor that it cannot take ``ValueError``.
@@ -39,6 +39,7 @@ ADAMW_8BIT = 1
 EXPORTS = [
     "egeria_ops_create", "egeria_ops_destroy", "egeria_ops_device_status", "egeria_ops_launch_count", "egeria_ops_debug_stall_next",
     "egeria_linear_workspace_bytes", "egeria_linear_forward", "egeria_linear_backward",
+    "egeria_gated_workspace_bytes", "egeria_gated_forward", "egeria_gated_backward",
     "egeria_norm_workspace_bytes", "egeria_norm_forward", "egeria_norm_backward",
     "egeria_adamw_workspace_bytes", "egeria_adamw_create", "egeria_adamw_destroy", "egeria_adamw_set_grads",
     "egeria_adamw_step", "egeria_adamw_device_status", "egeria_adamw_launch_count",
@@ -78,6 +79,7 @@ def lib() -> ctypes.CDLL:
     if _ready is L:
         return L
     for name, args in (("egeria_linear_workspace_bytes", [_i64] * 3), ("egeria_norm_workspace_bytes", [_i64] * 2),
+                       ("egeria_gated_workspace_bytes", [_i64] * 4),
                        ("egeria_adamw_workspace_bytes", [ctypes.c_int, ctypes.POINTER(_AdamTensor), ctypes.c_uint32])):
         getattr(L, name).argtypes, getattr(L, name).restype = args, ctypes.c_size_t
     L.egeria_ops_debug_stall_next.argtypes = [_vp, ctypes.c_int]
@@ -96,6 +98,11 @@ def lib() -> ctypes.CDLL:
 def egeria_linear_workspace_bytes(rows: int, inp: int, out: int) -> int:
     """Workspace of an :class:`Ops` whose linear calls have at most these sizes (take the largest over the layers)."""
     return int(lib().egeria_linear_workspace_bytes(int(rows), int(inp), int(out)))
+
+
+def egeria_gated_workspace_bytes(rows: int, inp: int, hidden: int, out: int) -> int:
+    """Workspace of an :class:`Ops` whose calls for gated feed-forward blocks have at most these sizes."""
+    return int(lib().egeria_gated_workspace_bytes(int(rows), int(inp), int(hidden), int(out)))
 
 
 def egeria_norm_workspace_bytes(rows: int, cols: int) -> int:
@@ -193,7 +200,7 @@ class _Handle:
 
 
 class Ops(_Handle):
-    """Handle of the linear and norm calls; owns its workspace.  For one stream at a time."""
+    """Handle of the calls for linear layers, gated blocks and norms; owns its workspace.  For one stream at a time."""
 
     def __init__(self, workspace_bytes: int = OPS_WORKSPACE_MIN, device="cuda"):
         self._place(device)
@@ -226,6 +233,32 @@ class Ops(_Handle):
             raise ValueError(f"unknown activation {act!r} or {act_in!r}")
         return self._call("egeria_linear_backward", self._native.linear_backward, stream,
                           (dy, x, w, z, ACTS[act], z_in, ACTS[act_in], need_dx, need_dw, need_db))
+
+    # ------------------------------------------------------------------ gated feed-forward blocks
+    def egeria_gated_forward(self, x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, w_down: torch.Tensor,
+                             b_gate: Optional[torch.Tensor] = None, b_up: Optional[torch.Tensor] = None,
+                             b_down: Optional[torch.Tensor] = None, act: str = "silu", residual: Optional[torch.Tensor] = None,
+                             save: bool = False, out: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None):
+        """y = (act(g) * u) w_down^T + b_down + residual with g = x w_gate^T + b_gate and u = x w_up^T + b_up, for x [rows, inp],
+        w_gate and w_up [hidden, inp] (two tensors, or the halves of one) and w_down [out, hidden] in bfloat16 or float16;
+        (y, g, u) with save.  `out` may be the residual; it is refused where it overlaps anything else."""
+        if act not in ACTS:
+            raise ValueError(f"unknown activation {act!r}")
+        return self._call("egeria_gated_forward", self._native.gated_forward, stream,
+                          (x, w_gate, w_up, w_down, b_gate, b_up, b_down, ACTS[act], residual, save, out))
+
+    def egeria_gated_backward(self, dy: torch.Tensor, x: Optional[torch.Tensor], w_gate: Optional[torch.Tensor],
+                              w_up: Optional[torch.Tensor], w_down: torch.Tensor, g: torch.Tensor, u: torch.Tensor, act: str = "silu",
+                              need_dx: bool = True, need_dw: bool = True, need_db: bool = False,
+                              stream: Optional[torch.cuda.Stream] = None):
+        """The gradients of a gated block as a dict: dx, dw_gate and dw_up (the halves of one tensor), dw_down, db_gate, db_up (the
+        same), db_down, None for what is not needed: a frozen block takes need_dw = False and no x, the first block that still
+        trains need_dx = False and no w_gate and w_up."""
+        if act not in ACTS:
+            raise ValueError(f"unknown activation {act!r}")
+        got = self._call("egeria_gated_backward", self._native.gated_backward, stream,
+                         (dy, x, w_gate, w_up, w_down, g, u, ACTS[act], need_dx, need_dw, need_db))
+        return dict(zip(("dx", "dw_gate", "dw_up", "dw_down", "db_gate", "db_up", "db_down"), got))
 
     # ------------------------------------------------------------------ residual norms
     def egeria_norm_forward(self, x: torch.Tensor, f: torch.Tensor, gate: Optional[torch.Tensor] = None, gate_rows: int = 0,

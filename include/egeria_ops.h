@@ -36,6 +36,7 @@ typedef enum { EGERIA_F32 = 0, EGERIA_BF16 = 1, EGERIA_F16 = 2 } egeria_type;
 
 typedef struct egeria_ops egeria_ops;       /* opaque, library-owned host objects */
 typedef struct egeria_adamw egeria_adamw;
+typedef struct egeria_muon egeria_muon;
 
 /* A handle for the linear and norm calls.
  *   workspace  device memory, EGERIA_WORKSPACE_ALIGN-aligned, caller-owned, at least
@@ -282,6 +283,62 @@ egeria_status egeria_adamw_device_status(egeria_adamw *adamw);
 
 /* Number of kernels launched through this handle so far. */
 int64_t egeria_adamw_launch_count(const egeria_adamw *adamw);
+
+/* ---------------------------------------------------------------------------- Muon */
+
+#define EGERIA_MUON_MAX_STEPS 16
+
+/* One matrix of the model, rows x cols consecutive values (a convolution's weight as its output channels by the rest), element-aligned.
+ * Fastest where cols is a multiple of 8 and everything 32-byte aligned. */
+typedef struct {
+    void *param;             /* of param_type; written */
+    float *master;           /* NULL, or the 32-bit copy that the step works on; param is then its rounding */
+    float *m;                /* the momentum */
+    int64_t rows, cols;      /* either may be 0: nothing to do; none above 2^22 */
+    int32_t param_type;      /* EGERIA_F32, EGERIA_BF16, EGERIA_F16 */
+    int32_t grad_type;       /* EGERIA_F32 or param_type */
+    float weight_decay;
+    float scale;             /* of the update, beside lr: 0.2 sqrt(max(rows, cols)) makes its values as large as AdamW's usually are,
+                                sqrt(max(1, rows / cols)) its effect on a layer's output alike for all shapes */
+    int32_t module;          /* its entry in the freeze mask, -1 = in none */
+} egeria_muon_tensor;
+
+/* Bytes of device workspace: about six per value of the matrices, four per value of the squares of their shorter sides, and the
+ * list of the work.  Pure host arithmetic; 0 for invalid arguments. */
+size_t egeria_muon_workspace_bytes(int count, const egeria_muon_tensor *tensors, int steps);
+
+/* An optimizer over `count` matrices (host array, copied).
+ *   grads  host array [count] of device pointers
+ *   steps  of the orthogonalisation, 1..EGERIA_MUON_MAX_STEPS; 5 is usual
+ * Waits for the current device, whose earlier work may still use the workspace, writes its tables there and synchronises. */
+egeria_status egeria_muon_create(egeria_muon **out, int count, const egeria_muon_tensor *tensors, const void *const *grads, int steps,
+                                 void *workspace, size_t workspace_bytes);
+egeria_status egeria_muon_destroy(egeria_muon *muon);
+
+/* The gradients are elsewhere from the next step on (one small copy in stream order; refused with
+ * EGERIA_ERR_INVALID_ARG on a stream that is being captured). */
+egeria_status egeria_muon_set_grads(egeria_muon *muon, void *cuda_stream, const void *const *grads);
+
+/* One step of every matrix that is not frozen:
+ *   g = gradient * grad_scale      m = beta m + (1 - beta) g      t = nesterov ? beta m + (1 - beta) g : m
+ *   X = t / max(|t|, eps), |t| the root of the sum of squares; then `steps` times
+ *       A = X X^T     X = 3.4445 X - 4.7750 A X + 2.0315 A^2 X
+ *   p = p (1 - lr weight_decay) - lr scale X
+ * The products' operands are rounded to 16 bits of 11 digits, their sums are 32 bits: an update is off by about 2e-3 of itself
+ * (root mean square).  A gradient that is not finite makes its whole matrix NaN.
+ *   grad_scale  device float [1] or NULL (1).  If it is not finite the whole step is left out.
+ *   frozen      device uint8 or NULL, indexed by `module`: the out_mask of egeria_plasticity_evaluate as it is.  A frozen
+ *               matrix is neither read nor written.  (Not to be written while the call runs.)
+ * 0 <= beta < 1; lr not negative; eps at least 1e-30.  The call can be captured into a CUDA graph and replayed. */
+egeria_status egeria_muon_step(egeria_muon *muon, void *cuda_stream, double lr, double beta, int nesterov, double eps, const float *grad_scale,
+                               const uint8_t *frozen);
+
+/* As egeria_ops_device_status, and the test hook as egeria_ops_debug_stall_next: of the next step's products. */
+egeria_status egeria_muon_device_status(egeria_muon *muon);
+egeria_status egeria_muon_debug_stall_next(egeria_muon *muon, int kind);
+
+/* Number of kernels launched through this handle so far. */
+int64_t egeria_muon_launch_count(const egeria_muon *muon);
 
 #ifdef __cplusplus
 }

@@ -13,7 +13,7 @@ LIB = HERE / "libegeria.so"
 BINDING = HERE / "_ops_python.so"             # the operators' calls from Python (csrc/ops/ops_python.cpp)
 BINDING_SOURCE = CSRC / "ops" / "ops_python.cpp"
 LIB_CHECKED = HERE / "libegeria_checked.so"   # the same sources with -DEGERIA_CHECKED (csrc/check.cuh)
-SOURCES = [CSRC / "egeria_api.cu", CSRC / "ops" / "ops_api.cu", CSRC / "ops" / "gated_api.cu"]
+SOURCES = [CSRC / "egeria_api.cu", CSRC / "ops" / "ops_api.cu", CSRC / "ops" / "gated_api.cu", CSRC / "ops" / "muon_api.cu"]
 HEADERS = [*sorted(CSRC.rglob("*.cuh")), *sorted(CSRC.rglob("*.h")), *sorted((HERE.parent / "include").glob("*.h"))]
 
 NVCC_FLAGS = [

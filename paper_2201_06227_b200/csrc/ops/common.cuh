@@ -20,6 +20,8 @@ enum OpsCheckCode : int32_t {
     kCheckNormRows = 16,    // norm backward: a CTA's rows
     kCheckNormGate = 17,    // norm backward: a group's gate, or the CTAs that share it
     kCheckGatedSums = 18,   // gated backward: the place of a piece's column sums
+    kCheckMuonPiece = 19,   // Muon: a piece's matrix
+    kCheckMuonUnit = 20,    // Muon: a unit's matrix
 };
 
 using bf16 = __nv_bfloat16;

@@ -364,6 +364,24 @@ PyObject *adamw_step(PyObject *, PyObject *const *args, Py_ssize_t n) {
     END_HANDLE_TH_ERRORS
 }
 
+// lr, beta, nesterov, eps, grad_scale, frozen, last module -> status
+PyObject *muon_step(PyObject *, PyObject *const *args, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    const Call c(args, n, 4 + 7);
+    const void *scale = vector(c.rest[4], "grad_scale", c.device, at::kFloat, 1);
+    const void *frozen = nullptr;
+    if (c.given(5)) {
+        const Tensor &f = tensor(c.rest[5], "frozen");
+        frozen = vector(c.rest[5], "frozen", c.device, at::kByte, f.numel());
+        if (f.numel() <= c.whole(6)) refuse("frozen: one entry per module is required");
+    }
+    const egeria_status s = reinterpret_cast<decltype(&egeria_muon_step)>(c.fn)(static_cast<egeria_muon *>(c.handle), c.stream, c.real(0), c.real(1),
+                                                                                c.flag(2), c.real(3), static_cast<const float *>(scale),
+                                                                                static_cast<const uint8_t *>(frozen));
+    return PyLong_FromLong(s);
+    END_HANDLE_TH_ERRORS
+}
+
 template <typename F>
 PyCFunction fast(F f) {
     return reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(f));
@@ -372,7 +390,8 @@ PyMethodDef methods[] = {
     {"linear_forward", fast(linear_forward), METH_FASTCALL, nullptr},   {"linear_backward", fast(linear_backward), METH_FASTCALL, nullptr},
     {"norm_forward", fast(norm_forward), METH_FASTCALL, nullptr},       {"norm_backward", fast(norm_backward), METH_FASTCALL, nullptr},
     {"gated_forward", fast(gated_forward), METH_FASTCALL, nullptr},     {"gated_backward", fast(gated_backward), METH_FASTCALL, nullptr},
-    {"adamw_step", fast(adamw_step), METH_FASTCALL, nullptr},           {nullptr, nullptr, 0, nullptr},
+    {"adamw_step", fast(adamw_step), METH_FASTCALL, nullptr},           {"muon_step", fast(muon_step), METH_FASTCALL, nullptr},
+    {nullptr, nullptr, 0, nullptr},
 };
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_ops_python", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -1,6 +1,6 @@
 """ctypes binding of the training operators (``include/egeria_ops.h``) -- argument marshalling only.
 
-:class:`Ops` has the linear layers, the gated feed-forward blocks and the residual norms, :class:`AdamW` the optimizer step; their
+:class:`Ops` has the linear layers, the gated feed-forward blocks and the residual norms, :class:`AdamW` and :class:`Muon` the optimizer steps; their
 methods have the names of the C entry points that they call.  Everything is computed by the CUDA
 kernels of ``libegeria.so``; there is no fallback: a call that the library refuses raises
 :class:`~paper_2201_06227_b200.binding.EgeriaError`, a tensor that it cannot take ``ValueError``.
@@ -43,6 +43,8 @@ EXPORTS = [
     "egeria_norm_workspace_bytes", "egeria_norm_forward", "egeria_norm_backward",
     "egeria_adamw_workspace_bytes", "egeria_adamw_create", "egeria_adamw_destroy", "egeria_adamw_set_grads",
     "egeria_adamw_step", "egeria_adamw_device_status", "egeria_adamw_launch_count",
+    "egeria_muon_workspace_bytes", "egeria_muon_create", "egeria_muon_destroy", "egeria_muon_set_grads", "egeria_muon_step",
+    "egeria_muon_device_status", "egeria_muon_debug_stall_next", "egeria_muon_launch_count",
 ]
 
 _vp, _i32, _i64, _f32 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_float
@@ -51,6 +53,11 @@ _vp, _i32, _i64, _f32 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.
 class _AdamTensor(ctypes.Structure):
     _fields_ = [(f, t) for t, names in ((_vp, "param master m v m_scale v_scale"), (_i64, "n"), (_i32, "param_type grad_type"),
                                         (_f32, "weight_decay"), (_i32, "module")) for f in names.split()]
+
+
+class _MuonTensor(ctypes.Structure):
+    _fields_ = [(f, t) for t, names in ((_vp, "param master m"), (_i64, "rows cols"), (_i32, "param_type grad_type"),
+                                        (_f32, "weight_decay scale"), (_i32, "module")) for f in names.split()]
 
 
 _calls = None
@@ -86,11 +93,17 @@ def lib() -> ctypes.CDLL:
     L.egeria_ops_create.argtypes = [ctypes.POINTER(_vp), _vp, ctypes.c_size_t]
     L.egeria_adamw_create.argtypes = [ctypes.POINTER(_vp), ctypes.c_int, ctypes.POINTER(_AdamTensor), ctypes.POINTER(_vp), _vp, _vp,
                                       ctypes.c_size_t, ctypes.c_uint32]
+    L.egeria_muon_workspace_bytes.argtypes = [ctypes.c_int, ctypes.POINTER(_MuonTensor), ctypes.c_int]
+    L.egeria_muon_workspace_bytes.restype = ctypes.c_size_t
+    L.egeria_muon_create.argtypes = [ctypes.POINTER(_vp), ctypes.c_int, ctypes.POINTER(_MuonTensor), ctypes.POINTER(_vp), ctypes.c_int, _vp,
+                                     ctypes.c_size_t]
+    L.egeria_muon_debug_stall_next.argtypes = [_vp, ctypes.c_int]
     for name in ("egeria_ops_destroy", "egeria_ops_device_status", "egeria_ops_launch_count", "egeria_adamw_destroy",
-                 "egeria_adamw_device_status", "egeria_adamw_launch_count"):
+                 "egeria_adamw_device_status", "egeria_adamw_launch_count", "egeria_muon_destroy", "egeria_muon_device_status",
+                 "egeria_muon_launch_count"):
         getattr(L, name).argtypes = [_vp]
-    L.egeria_ops_launch_count.restype = L.egeria_adamw_launch_count.restype = _i64
-    L.egeria_adamw_set_grads.argtypes = [_vp, _vp, ctypes.POINTER(_vp)]
+    L.egeria_ops_launch_count.restype = L.egeria_adamw_launch_count.restype = L.egeria_muon_launch_count.restype = _i64
+    L.egeria_adamw_set_grads.argtypes = L.egeria_muon_set_grads.argtypes = [_vp, _vp, ctypes.POINTER(_vp)]
     _ready = L
     return L
 
@@ -399,3 +412,113 @@ class AdamW(_Handle):
 
     def egeria_adamw_launch_count(self) -> int:
         return int(self._lib.egeria_adamw_launch_count(self._h))
+
+
+MUON_MAX_STEPS = 16
+
+
+class Muon(_Handle):
+    """The Muon step of a model's matrices: momentum, five Newton-Schulz products of it, update; all matrices in three launches.
+    Frozen modules are left out on the device.
+
+    params, grads, momenta: one contiguous CUDA tensor of two or more dimensions per matrix of the model, the first its rows, the others
+    taken together its columns; momenta are float32.  masters: float32 copies that the step works on (entries may be None).
+    scale: "rms" for 0.2 sqrt(max(rows, cols)), with which AdamW's learning rates and decays suit, "spectral" for
+    sqrt(max(1, rows / cols)), or a number per matrix.  modules: each matrix's entry in the freeze mask, -1 for none.  The handle
+    keeps all of them alive.  Vectors (biases, norms) and embeddings are better left to :class:`AdamW`.
+    """
+
+    def __init__(self, params: Sequence[torch.Tensor], grads: Sequence[torch.Tensor], momenta: Sequence[torch.Tensor],
+                 masters: Optional[Sequence] = None, weight_decay=0.0, scale="rms", modules: Optional[Sequence[int]] = None,
+                 ns_steps: int = 5):
+        n = len(params)
+        if n < 1:
+            raise ValueError("no matrices")
+        self._place(params[0].device)
+        dev = self._index
+        columns = dict(grads=grads, momenta=momenta, masters=masters or [None] * n, modules=modules if modules is not None else [-1] * n,
+                       weight_decay=[weight_decay] * n if isinstance(weight_decay, (int, float)) else weight_decay,
+                       scale=[scale] * n if isinstance(scale, (int, float, str)) else scale)
+        for name, c in columns.items():
+            if len(c) != n:
+                raise ValueError(f"{name}: one entry per matrix is required")
+        table = (_MuonTensor * n)()
+        self.modules = [int(m) for m in columns["modules"]]
+        for i, p in enumerate(params):
+            if p.dtype not in TYPES:
+                raise ValueError(f"matrix {i}: {p.dtype} parameters are not supported")
+            if p.dim() < 2:
+                raise ValueError(f"matrix {i}: two dimensions at least are required")
+            k = p.numel()
+            row = table[i]
+            row.rows = p.size(0)
+            row.cols = k // p.size(0) if p.size(0) else 0
+            how = columns["scale"][i]
+            if how == "rms":
+                how = 0.2 * max(row.rows, row.cols) ** 0.5
+            elif how == "spectral":
+                how = max(1.0, row.rows / max(row.cols, 1)) ** 0.5
+            elif isinstance(how, str):
+                raise ValueError(f"unknown scale {how!r}")
+            row.param_type = TYPES[p.dtype]
+            row.grad_type = TYPES.get(columns["grads"][i].dtype, -1)
+            row.weight_decay, row.scale, row.module = float(columns["weight_decay"][i]), float(how), self.modules[i]
+            row.param = _vector(p, f"params[{i}]", dev, p.dtype, k)
+            row.master = _vector(columns["masters"][i], f"masters[{i}]", dev, torch.float32, k)
+            row.m = _vector(momenta[i], f"momenta[{i}]", dev, torch.float32, k)
+        self._sizes = [(p.numel(), g.dtype) for p, g in zip(params, grads)]
+        self._keep = (list(params), list(momenta), list(columns["masters"]))
+        with torch.cuda.device(self.device):
+            nbytes = int(lib().egeria_muon_workspace_bytes(n, table, int(ns_steps)))
+            if nbytes == 0:
+                raise EgeriaError(ERR_INVALID_ARG, "egeria_muon_workspace_bytes")
+            self._raw, ptr = _workspace(nbytes, self.device)
+            handle = _vp()
+            _check(lib().egeria_muon_create(ctypes.byref(handle), n, table, self._grad_pointers(grads), int(ns_steps), ptr, nbytes),
+                   "egeria_muon_create")
+        self._grads = list(grads)
+        self._h, self._lib, self._destroy, self._native = handle, lib(), lib().egeria_muon_destroy, _native()
+        self._last_module = max(self.modules)
+        self._followed = [p for p in params if p.requires_grad]
+
+    def _grad_pointers(self, grads):
+        if len(grads) != len(self._sizes):
+            raise ValueError("grads: one entry per matrix is required")
+        return (_vp * len(grads))(*[_vector(g, f"grads[{i}]", self._index, t, n) for i, (g, (n, t)) in enumerate(zip(grads, self._sizes))])
+
+    def egeria_muon_set_grads(self, grads: Sequence[torch.Tensor], stream: Optional[torch.cuda.Stream] = None) -> None:
+        """The gradients (same sizes and types) are in these tensors from the next step on."""
+        ptrs = self._grad_pointers(grads)
+        if stream is None:
+            self._join(torch._C._cuda_getCurrentRawStream(self._index))
+        with _On(self.device, stream, (self._raw,)) as s:
+            _check(self._lib.egeria_muon_set_grads(self._h, s, ptrs), "egeria_muon_set_grads")
+        self._grads = list(grads)      # not before the library has taken them: until then the old ones are in force
+        for known in self._streams.values():
+            for g in grads if known is not None else ():
+                g.record_stream(known)
+
+    def egeria_muon_step(self, lr: float, beta: float = 0.95, nesterov: bool = True, eps: float = 1e-7,
+                         grad_scale: Optional[torch.Tensor] = None, frozen: Optional[torch.Tensor] = None,
+                         stream: Optional[torch.cuda.Stream] = None) -> None:
+        """One step of every matrix whose module is not marked in `frozen` (uint8, as egeria_plasticity_evaluate leaves it)."""
+        self._call("egeria_muon_step", self._native.muon_step, stream, (lr, beta, nesterov, eps, grad_scale, frozen, self._last_module))
+        if self._followed:
+            torch.autograd.graph.increment_version(self._followed)
+
+    def _touched(self):
+        return [*self._grads, *(t for column in self._keep for t in column)]
+
+    def egeria_muon_device_status(self) -> int:
+        with torch.cuda.device(self.device):
+            return int(self._lib.egeria_muon_device_status(self._h))
+
+    def check_device_status(self) -> None:
+        _check(self.egeria_muon_device_status(), "egeria_muon_device_status")
+
+    def egeria_muon_debug_stall_next(self, kind: int) -> None:
+        """Test hook: the next step's products give up (see the header)."""
+        _check(self._lib.egeria_muon_debug_stall_next(self._h, int(kind)), "egeria_muon_debug_stall_next")
+
+    def egeria_muon_launch_count(self) -> int:
+        return int(self._lib.egeria_muon_launch_count(self._h))

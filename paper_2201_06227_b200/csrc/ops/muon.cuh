@@ -8,17 +8,18 @@
 // taller than wide takes A = X^T X and X = a X + X (b A + c A^2), the same polynomial from its shorter side, without being
 // transposed: the tensor cores take either axis of an operand as the consecutive one.
 //
-// Operands are f16, sums 32 bits.  All values are below 2 in size, where f16 has three bits more than bf16.  A and the
-// polynomial are rounded once each.  X is kept as two f16 values, the second what the first leaves (22 bits): the products take the
-// first alone, but where X is added to itself both count.  A rounding of X there would lie across its null space too, which no
-// product damps and every step multiplies by a: a 1024 x 1024 matrix of rank 64 is off by 5.8e-4 (2-norm of the difference
-// over that of the result, from the formula in 64 bits), with X in one f16 value by 2.4e-2, in one bf16 value by 0.19; a matrix of
-// independent normal values by 1.3e-3, 1.2e-3 and 9.3e-3.  X is held times a power of two, so that its values stay off f16's
+// Operands are f16, sums 32 bits.  All values are below 4 in size, where f16 has three bits more than bf16.  A and the
+// polynomial P = a I + b A + c A^2 are rounded once each.  X is kept as two f16 values, the second what the first leaves (22 bits): the
+// products take the first, and a times the second is added.  Without it X's rounding would lie across its null space too, which no
+// product damps and every step multiplies by a: a 512 x 512 matrix of rank 32 is off by 1.5e-3 (2-norm of the difference
+// over that of the result, from the formula in 64 bits), with X in one f16 value by 2.9e-2, in one bf16 value by 0.23; a matrix of
+// independent normal values by 1.5e-3, 1.3e-3 and 1.1e-2.  X is held times a power of two, so that its values stay off f16's
 // lower end.
 //
-// All products of all matrices are one launch: a list of units (a tile of one of the 3 `steps` products of one matrix), dealt round
-// the workers (CTAs, or pairs of them).  A unit waits until the units of its matrix's product before it are done, which a
-// counter per matrix says; the list has several matrices' tiles of a product side by side, so that as a rule it is long done.
+// All products of all matrices are one launch: a list of units (a tile of one of the 3 `steps` products of one matrix), which the
+// workers (CTAs, or pairs of them) take in turn from its head.  A unit waits until the units of its matrix's product before it are
+// done, which a counter per matrix says; the list has several matrices' tiles of a product side by side, so that as a rule it is long
+// done.  What a unit waits for stands before it in the list and has been taken by a block that runs, however many run at once.
 // A and A^2 are symmetric: tiles below the diagonal are left out, and each block of 32 x 32 above it is stored twice.
 #pragma once
 #include "../../../include/egeria_ops.h"
@@ -30,7 +31,8 @@ namespace ops {
 constexpr float kNsA = 3.4445f, kNsB = -4.7750f, kNsC = 2.0315f;
 constexpr int kMuonPiece = 8192;     // values of a matrix that a block takes in the elementwise passes
 constexpr int kMuonThreads = 256;
-enum { kMapX0 = 0, kMapX0N, kMapX1, kMapX1N, kMapGram, kMapPoly, kMuonMaps };  // N: boxes of 64 x 64 for the other axis
+// Tile copies of a matrix: loads of 128 rows by 64 columns or (N) 64 by 64 for the other axis, stores (S) of 32 by 32.
+enum { kMapX0 = 0, kMapX0N, kMapX1, kMapX1N, kMapGram, kMapPoly, kMapX0S, kMapX1S, kMapRestS, kMapGramS, kMapPolyS, kMuonMaps };
 
 struct MuonMatrix {
     void *param;
@@ -47,10 +49,11 @@ struct MuonMatrix {
 struct MuonParams {
     const MuonMatrix *matrices;
     const CUtensorMap *maps;         // [matrix][kMuonMaps]
-    const int4 *units;               // matrix, tm | tn << 16, product | k blocks << 8, count that the matrix's counter has to reach
+    const int4 *units;               // matrix | tall << 31, tm | tn << 16, product | k blocks << 8, what the matrix's counter has to reach
     const int2 *pieces;              // matrix, piece
     const void *const *grads;
-    int32_t *done;                   // per matrix
+    int32_t *done;                   // per matrix: tiles (of one CTA) that are stored; -1 for one that is left out
+    int32_t *ticket;                 // units that have been taken
     int32_t *status;
     const float *grad_scale;
     const uint8_t *frozen;
@@ -145,8 +148,9 @@ __global__ void __launch_bounds__(kMuonThreads) muon_momentum_kernel(const MuonP
     __shared__ double part[kMuonThreads / 32];
     ptx::grid_dependency_wait();
     ptx::grid_launch_dependents();
+    if (blockIdx.x == 0 && threadIdx.x == 0) *p.ticket = 0;
     if (blockIdx.x == 0)
-        for (int i = threadIdx.x; i < p.n_matrices; i += kMuonThreads) p.done[i] = 0;
+        for (int i = threadIdx.x; i < p.n_matrices; i += kMuonThreads) p.done[i] = muon_skips(p, p.matrices[i]) ? -1 : 0;
     float scale;
     if (!muon_scale(p, scale)) return;
     const int2 piece = p.pieces[blockIdx.x];
@@ -233,93 +237,120 @@ __global__ void __launch_bounds__(kMuonThreads) muon_normalize_kernel(const Muon
 
 // ---------------------------------------------------------------- products
 // A 32 x 32 piece of the matrices in the workspace, whose rows are padded to whole pieces.  They are written and read by
-// different SMs within one launch: past L1.
+// different SMs within one launch.
 __device__ __forceinline__ void muon_fetch(uint32_t (&r)[16], const uint16_t *base, int64_t ld, const Tile &t) {
-    if (t.lane < t.rows) {
-        const uint4 *p = reinterpret_cast<const uint4 *>(base + (t.row0 + t.lane) * ld + t.col0);
+    if (t.lane < t.rows && t.cols > 0) {
+        const uint16_t *p = base + (t.row0 + t.lane) * ld + t.col0;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const uint4 q = __ldcg(p + i);
-            r[4 * i] = q.x, r[4 * i + 1] = q.y, r[4 * i + 2] = q.z, r[4 * i + 3] = q.w;
-        }
+        for (int i = 0; i < 2; ++i)
+            asm volatile("ld.relaxed.gpu.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                         : "=r"(r[8 * i]), "=r"(r[8 * i + 1]), "=r"(r[8 * i + 2]), "=r"(r[8 * i + 3]), "=r"(r[8 * i + 4]), "=r"(r[8 * i + 5]),
+                           "=r"(r[8 * i + 6]), "=r"(r[8 * i + 7])
+                         : "l"(p + 16 * i)
+                         : "memory");
     } else {
 #pragma unroll
         for (int i = 0; i < 16; ++i) r[i] = 0u;
     }
 }
-__device__ __forceinline__ void muon_store(uint16_t *base, int64_t ld, const uint32_t (&r)[16], const Tile &t) {
-    if (t.lane < t.rows) {
-        uint16_t *p = base + (t.row0 + t.lane) * ld + t.col0;
-        ptx::st_global_v8(reinterpret_cast<float *>(p), r);
-        ptx::st_global_v8(reinterpret_cast<float *>(p + 16), r + 8);
-    }
+// Two 32 x 32 pieces in a warp's shared memory as tile stores take them: 64 bytes a row, whose sixteens change places with the row.
+__device__ __forceinline__ void muon_stage_rows(uint32_t at, const uint32_t (&r)[16], int lane) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at + lane * 64 + ((i ^ (lane >> 1 & 3)) << 4)), "r"(r[4 * i]), "r"(r[4 * i + 1]),
+                     "r"(r[4 * i + 2]), "r"(r[4 * i + 3])
+                     : "memory");
 }
-// A piece of a symmetric matrix and its mirror image.  Pieces below the diagonal are left to their images.
-__device__ __forceinline__ void muon_store_symmetric(uint16_t *base, int64_t ld, const float (&v)[32], const Tile &t) {
-    uint32_t r[16];
+// The mirror image: this lane's row becomes column `lane`.
+__device__ __forceinline__ void muon_stage_mirror(uint32_t at, const uint32_t (&r)[16], int lane) {
 #pragma unroll
-    for (int i = 0; i < 16; ++i) r[i] = pack2<f16>(v[2 * i], v[2 * i + 1]);
-    muon_store(base, ld, r, t);
-    if (t.row0 == t.col0) return;
-    __syncwarp();
-#pragma unroll
-    for (int i = 0; i < 16; ++i) reinterpret_cast<uint32_t *>(t.stage)[t.lane * (kStagePitch / 2) + i] = r[i];
-    __syncwarp();
-#pragma unroll
-    for (int i = 0; i < 16; ++i)
-        r[i] = (uint32_t)t.stage[(2 * i) * kStagePitch + t.lane] | (uint32_t)t.stage[(2 * i + 1) * kStagePitch + t.lane] << 16;
-    Tile s = t;
-    s.row0 = t.col0;
-    s.rows = t.cols;
-    s.col0 = (int32_t)t.row0;
-    muon_store(base, ld, r, s);
+    for (int c = 0; c < 32; ++c) {
+        const uint16_t v = (uint16_t)(c & 1 ? r[c >> 1] >> 16 : r[c >> 1] & 0xffffu);
+        asm volatile("st.shared.b16 [%0], %1;" ::"r"(at + c * 64 + (((lane >> 3) ^ (c >> 1 & 3)) << 4) + (lane & 7) * 2), "h"(v) : "memory");
+    }
 }
 
-// p = p keep - step X of a piece, x: X's values.
+// p = p keep - step X of a piece.  Four values of a row per lane, eight lanes a row: what X's 32 rows in lanes become through the
+// warp's shared memory.
 template <typename T>
-__device__ __forceinline__ void muon_update_values(T *param, float *master, int64_t at, float x, float keep, float step) {
-    const float v = fmaf(master ? master[at] : to_f32(param[at]), keep, -step * x);
-    param[at] = from_f32<T>(v);
-    if (master) master[at] = v;
+__device__ __forceinline__ void muon_weights(uint32_t (&r)[2][16], const MuonMatrix &q, const Tile &t) {
+    const int64_t at = (t.row0 + (t.lane >> 3)) * q.cols + t.col0 + (t.lane & 7) * 4;
+    if ((t.lane & 7) * 4 >= t.cols) return;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        if ((t.lane >> 3) + 4 * i >= t.rows) break;
+        if (q.master || sizeof(T) == 4) {
+            const float *p = (q.master ? q.master : static_cast<const float *>(q.param)) + at + 4 * i * q.cols;
+            const uint4 w = *reinterpret_cast<const uint4 *>(p);
+            uint32_t *to = &r[i >> 2][(i & 3) * 4];
+            to[0] = w.x, to[1] = w.y, to[2] = w.z, to[3] = w.w;
+        } else {
+            const uint2 w = *reinterpret_cast<const uint2 *>(static_cast<const T *>(q.param) + at + 4 * i * q.cols);
+            r[i >> 2][(i & 3) * 4] = w.x, r[i >> 2][(i & 3) * 4 + 1] = w.y;
+        }
+    }
 }
 template <typename T>
-__device__ __forceinline__ void muon_update(const MuonMatrix &q, float (&x)[32], float keep, float step, const Tile &t) {
-    T *param = static_cast<T *>(q.param);
-    if (q.vector && t.cols >= kPiece) {
-        if (t.lane < t.rows) {
-            const int64_t at = (t.row0 + t.lane) * q.cols + t.col0;
+struct Four;
+template <>
+struct Four<float> {
+    static __device__ __forceinline__ void read(float (&v)[4], uint32_t a, uint32_t b) {}
+    static __device__ __forceinline__ void write(void *p, const float (&v)[4]) { *static_cast<float4 *>(p) = make_float4(v[0], v[1], v[2], v[3]); }
+};
+template <typename T>
+struct Four {
+    static __device__ __forceinline__ void read(float (&v)[4], uint32_t a, uint32_t b) {
+        const float2 x = unpack2<T>(a), y = unpack2<T>(b);
+        v[0] = x.x, v[1] = x.y, v[2] = y.x, v[3] = y.y;
+    }
+    static __device__ __forceinline__ void write(void *p, const float (&v)[4]) {
+        *static_cast<uint2 *>(p) = make_uint2(pack2<T>(v[0], v[1]), pack2<T>(v[2], v[3]));
+    }
+};
+constexpr int kUpdatePitch = 36;  // floats
+template <typename T>
+__device__ __forceinline__ void muon_update_wide(const MuonMatrix &q, const uint32_t (&r)[2][16], const float *stage, float keep, float step, const Tile &t) {
+    if ((t.lane & 7) * 4 >= t.cols) return;
+    const int64_t at = (t.row0 + (t.lane >> 3)) * q.cols + t.col0 + (t.lane & 7) * 4;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                float v[8];
-                if (q.master) {
-                    Raw8<float> r;
-                    load8(r, q.master + at + 8 * i);
-                    unpack8(v, r);
-                } else {
-                    Raw8<T> r;
-                    load8(r, param + at + 8 * i);
-                    unpack8(v, r);
-                }
+    for (int i = 0; i < 8; ++i) {
+        const int row = (t.lane >> 3) + 4 * i;
+        if (row >= t.rows) break;
+        const float4 x = *reinterpret_cast<const float4 *>(stage + row * kUpdatePitch + (t.lane & 7) * 4);
+        float v[4];
+        if (q.master || sizeof(T) == 4) {
 #pragma unroll
-                for (int k = 0; k < 8; ++k) v[k] = fmaf(v[k], keep, -step * x[8 * i + k]);
-                store8(param + at + 8 * i, v);
-                if (q.master) store8(q.master + at + 8 * i, v);
-            }
+            for (int k = 0; k < 4; ++k) v[k] = __uint_as_float(r[i >> 2][(i & 3) * 4 + k]);
+        } else {
+            Four<T>::read(v, r[i >> 2][(i & 3) * 4], r[i >> 2][(i & 3) * 4 + 1]);
         }
-        return;
+        v[0] = fmaf(v[0], keep, -step * x.x), v[1] = fmaf(v[1], keep, -step * x.y);
+        v[2] = fmaf(v[2], keep, -step * x.z), v[3] = fmaf(v[3], keep, -step * x.w);
+        const int64_t to = at + 4 * i * q.cols;
+        Four<T>::write(static_cast<T *>(q.param) + to, v);
+        if (q.master) Four<float>::write(q.master + to, v);
     }
-    // row by row, with lane = column, sixteen columns of the piece at a time through shared memory
-    const int rows = min(t.rows, 32), c = t.lane & 15;
-    float *stage = reinterpret_cast<float *>(t.stage);  // [32][17]
-    for (int half = 0; half < 2; ++half) {
-        __syncwarp();
-#pragma unroll
-        for (int i = 0; i < 16; ++i) stage[t.lane * 17 + i] = half ? x[16 + i] : x[i];
-        __syncwarp();
-        if (half * 16 + c < t.cols)
-            for (int k = t.lane >> 4; k < rows; k += 2)
-                muon_update_values(param, q.master, (t.row0 + k) * q.cols + t.col0 + half * 16 + c, stage[k * 17 + c], keep, step);
+}
+// The same value by value, where rows are not whole eights or not aligned.
+template <typename T>
+__device__ __forceinline__ void muon_update_narrow(const MuonMatrix &q, const float *stage, float keep, float step, const Tile &t) {
+    if (t.lane >= t.cols) return;
+    T *param = static_cast<T *>(q.param);
+    for (int row = 0; row < t.rows; ++row) {
+        const int64_t at = (t.row0 + row) * q.cols + t.col0 + t.lane;
+        const float v = fmaf(q.master ? q.master[at] : to_f32(param[at]), keep, -step * stage[row * kUpdatePitch + t.lane]);
+        param[at] = from_f32<T>(v);
+        if (q.master) q.master[at] = v;
     }
+}
+template <typename F>
+__device__ __forceinline__ void with_type(int type, F go) {
+    if (type == EGERIA_F32)
+        go(float());
+    else if (type == EGERIA_BF16)
+        go(bf16());
+    else
+        go(f16());
 }
 
 __device__ __forceinline__ int32_t load_acquire(const int32_t *p) {
@@ -327,11 +358,88 @@ __device__ __forceinline__ int32_t load_acquire(const int32_t *p) {
     asm volatile("ld.acquire.gpu.global.s32 %0, [%1];" : "=r"(v) : "l"(p) : "memory");
     return v;
 }
-// Until the counter has come that far, but not for ever.
-__device__ __forceinline__ bool muon_wait(const int32_t *done, int32_t need, volatile int *abort_flag, uint64_t limit_ns) {
-    if (load_acquire(done) >= need) return true;
+// Until the matrix's counter has come that far, but not for ever: 1; 0 if it gave up, -1 if the matrix is left out.
+__device__ __forceinline__ int muon_wait(const int32_t *done, int32_t need, volatile int *abort_flag, uint64_t limit_ns) {
+    const int32_t v = load_acquire(done);
+    if (v < 0) return -1;
+    if (v >= need) return 1;
     const uint64_t t0 = ptx::globaltimer_ns();
     while (load_acquire(done) < need) {
+        if (*abort_flag) return 0;
+        if (ptx::globaltimer_ns() - t0 > limit_ns) {
+            *abort_flag = 1;
+            return 0;
+        }
+    }
+    return 1;
+}
+__device__ __forceinline__ void fence_proxy_async_all() { asm volatile("fence.proxy.async;" ::: "memory"); }
+
+// Tile stores: a lane issues its own and waits for them.
+__device__ __forceinline__ void tile_store(const CUtensorMap *map, int32_t x, int32_t y, uint32_t src) {
+    asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%1, %2}], [%3];" ::"l"(map), "r"(x), "r"(y), "r"(src) : "memory");
+}
+__device__ __forceinline__ void tile_store_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
+template <int PENDING>
+__device__ __forceinline__ void tile_store_read() {  // what all but the last so many groups read of shared memory may change
+    asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(PENDING) : "memory");
+}
+__device__ __forceinline__ void tile_store_done() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
+
+// As the linear layers' kernel, with a stage less, 8 KB of shared memory for each of the epilogue's warps (two buffers of
+// two pieces), and a warp that stores what they leave there.
+template <int BN, int CG>
+struct MuonCfg : GemmCfg<BN, CG, 1> {
+    using Base = GemmCfg<BN, CG, 1>;
+    static constexpr int kStages = 5;
+    static constexpr int kBuffer = 4096, kWarpStaging = 2 * kBuffer;
+    static constexpr int kThreads = Base::kThreads + 32;
+    static constexpr int kSmem = 1024 + kStages * Base::kStageBytes + kEpiWarps * kWarpStaging + 512;
+    static_assert(kSmem <= 227 * 1024 && Base::kStageBytes % 1024 == 0, "shared memory of a CTA, tiles on their boundary");
+};
+
+struct MuonUnit {
+    int32_t matrix, tm, tn, product, kind, kblocks, need;
+    bool tall;
+    bool same;  // a tile on the diagonal of a symmetric product: its operands are the same rows
+};
+__device__ __forceinline__ MuonUnit muon_unit(const int4 &q) {
+    MuonUnit g;
+    g.matrix = q.x & 0x7fffffff;
+    g.tall = q.x < 0;
+    g.tm = q.y & 0xffff, g.tn = q.y >> 16 & 0xffff;
+    g.product = q.z & 0xff, g.kblocks = (int32_t)((uint32_t)q.z >> 8);
+    g.kind = g.product % 3;
+    g.need = q.w;
+    g.same = g.kind != 2 && g.tm == g.tn;
+    return g;
+}
+// The units that a worker's first producer has taken and found ready, for the other roles and the pair's other CTA: the last
+// kUnitRing of them and how many there have been.  No role falls further behind: the stages hold the loads of five units at most,
+// a unit's products need the accumulator of the unit two before it drained, and the epilogue does not begin a unit before the
+// storing warp has taken the one kUnitLag before it.
+constexpr int kUnitRing = 16, kUnitLag = 4;
+constexpr int kNoMoreUnits = 0x7fffffff;
+// An entry goes as two words of 56 bits, each with the low 8 bits of its number plus one, by which a reader knows it.
+__device__ __forceinline__ void unit_publish(uint32_t ring, const int4 &q, int32_t n) {
+    const uint64_t tag = (uint64_t)(n + 1 & 0xff) << 56;
+    const uint64_t a = tag | (uint64_t)(q.x < 0) << 55 | (uint64_t)((uint32_t)q.x & 0x7fffff) << 32 | (uint32_t)q.y;
+    const uint64_t b = tag | (uint64_t)((uint32_t)q.z & 0x1ffffff) << 31 | (uint32_t)(q.w & 0x7fffffff);
+    const uint32_t to = ring + (uint32_t)(n % kUnitRing) * 16;
+    asm volatile("st.relaxed.cluster.shared::cluster.b64 [%0], %1;" ::"r"(to), "l"(a) : "memory");
+    asm volatile("st.relaxed.cluster.shared::cluster.b64 [%0], %1;" ::"r"(to + 8), "l"(b) : "memory");
+}
+// The number of units that the storing warp of this CTA has taken, and the wait for it.
+__device__ __forceinline__ void units_followed(uint32_t at, int32_t n) { asm volatile("st.release.cta.shared::cta.s32 [%0], %1;" ::"r"(at), "r"(n) : "memory"); }
+__device__ __forceinline__ bool units_wait(uint32_t at, int32_t n, volatile int *abort_flag, uint64_t limit_ns) {
+    auto there = [&] {
+        int32_t r;
+        asm volatile("ld.acquire.cta.shared::cta.s32 %0, [%1];" : "=r"(r) : "r"(at) : "memory");
+        return r >= n;
+    };
+    if (there()) return true;
+    const uint64_t t0 = ptx::globaltimer_ns();
+    while (!there()) {
         if (*abort_flag) return false;
         if (ptx::globaltimer_ns() - t0 > limit_ns) {
             *abort_flag = 1;
@@ -340,32 +448,53 @@ __device__ __forceinline__ bool muon_wait(const int32_t *done, int32_t need, vol
     }
     return true;
 }
-__device__ __forceinline__ void fence_proxy_async_all() { asm volatile("fence.proxy.async;" ::: "memory"); }
-
-struct MuonUnit {
-    int32_t matrix, tm, tn, product, kblocks, need;
-};
-__device__ __forceinline__ MuonUnit muon_unit(const MuonParams &p, int u) {
-    const int4 q = p.units[u];
-    return MuonUnit{q.x, q.y & 0xffff, q.y >> 16 & 0xffff, q.z & 0xff, (int32_t)((uint32_t)q.z >> 8), q.w};
+// Unit n of the worker, once it is there; false at the end and where the wait runs out.  (It says nothing about memory: who
+// reads what other SMs have stored looks at the matrix's counter too.)
+__device__ __forceinline__ bool unit_next(MuonUnit &g, uint32_t ring, int32_t n, volatile int *abort_flag, uint64_t limit_ns) {
+    const uint32_t at = ring + (uint32_t)(n % kUnitRing) * 16;
+    const uint32_t tag = n + 1 & 0xff;
+    uint64_t a, b;
+    auto there = [&] {
+        asm volatile("ld.relaxed.cluster.shared::cta.b64 %0, [%1];" : "=l"(a) : "r"(at) : "memory");
+        asm volatile("ld.relaxed.cluster.shared::cta.b64 %0, [%1];" : "=l"(b) : "r"(at + 8) : "memory");
+        return (uint32_t)(a >> 56) == tag && (uint32_t)(b >> 56) == tag;
+    };
+    bool ok = there();
+    for (int i = 0; !ok && i < 64; ++i) ok = there();
+    if (!ok) {
+        const uint64_t t0 = ptx::globaltimer_ns();
+        while (!there()) {
+            if (*abort_flag) return false;
+            if (ptx::globaltimer_ns() - t0 > limit_ns) {
+                *abort_flag = 1;
+                return false;
+            }
+        }
+    }
+    const uint32_t matrix = (uint32_t)(a >> 32) & 0x7fffff;
+    if (matrix == 0x7fffff) return false;
+    g = muon_unit(make_int4((int)(matrix | (a >> 55 & 1 ? 0x80000000u : 0u)), (int)(uint32_t)a, (int)(uint32_t)(b >> 31 & 0x1ffffff),
+                            (int)(uint32_t)(b & 0x7fffffff)));
+    return true;
 }
 
 template <int BN, int CG>
-__global__ void __launch_bounds__(GemmCfg<BN, CG, 1>::kThreads, 1) muon_products_kernel(const __grid_constant__ MuonParams p) {
-    using Cfg = GemmCfg<BN, CG, 1>;
+__global__ void __launch_bounds__(MuonCfg<BN, CG>::kThreads, 1) muon_products_kernel(const __grid_constant__ MuonParams p) {
+    using Cfg = MuonCfg<BN, CG>;
     extern __shared__ uint8_t smem_raw[];
     const uint32_t smem_base = (ptx::smem_u32(smem_raw) + 1023u) & ~1023u;
     uint8_t *smem = smem_raw + (smem_base - ptx::smem_u32(smem_raw));
-    uint16_t *staging = reinterpret_cast<uint16_t *>(smem + Cfg::kStages * Cfg::kStageBytes);
-    uint64_t *bars = reinterpret_cast<uint64_t *>(smem + Cfg::kStages * Cfg::kStageBytes + Cfg::kStaging);
+    uint8_t *staging = smem + Cfg::kStages * Cfg::kStageBytes;
+    uint64_t *bars = reinterpret_cast<uint64_t *>(staging + kEpiWarps * Cfg::kWarpStaging);
     const uint32_t full0 = ptx::smem_u32(bars), empty0 = full0 + 8 * Cfg::kStages;
-    const uint32_t accfull0 = empty0 + 8 * Cfg::kStages, accempty0 = accfull0 + 16, drain = accempty0 + 16;
-    volatile uint32_t *tmem_holder = reinterpret_cast<volatile uint32_t *>(bars + 2 * Cfg::kStages + 5);
+    const uint32_t accfull0 = empty0 + 8 * Cfg::kStages, accempty0 = accfull0 + 16, staged0 = accempty0 + 16, free0 = staged0 + 16, drain = free0 + 16;
+    volatile uint32_t *tmem_holder = reinterpret_cast<volatile uint32_t *>(bars + 2 * Cfg::kStages + 9);
     volatile int *abort_flag = reinterpret_cast<volatile int *>(tmem_holder + 1);
     volatile uint32_t *issued = tmem_holder + 2;
+    const uint32_t ring = ptx::smem_u32(bars) + 256, followed = ptx::smem_u32(const_cast<uint32_t *>(tmem_holder + 3));  // this worker's units
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = CG == 2 ? cluster_rank() : 0;
-    const int worker = blockIdx.x / CG, workers = gridDim.x / CG;
+    const int worker = blockIdx.x / CG;
     if (threadIdx.x == 0) {
         for (int s = 0; s < Cfg::kStages; ++s) {
             ptx::mbar_init(full0 + 8 * s, 1);
@@ -374,9 +503,13 @@ __global__ void __launch_bounds__(GemmCfg<BN, CG, 1>::kThreads, 1) muon_products
         for (int s = 0; s < 2; ++s) {
             ptx::mbar_init(accfull0 + 8 * s, 1);
             ptx::mbar_init(accempty0 + 8 * s, kEpiWarps * CG);
+            ptx::mbar_init(staged0 + 8 * s, kEpiWarps);
+            ptx::mbar_init(free0 + 8 * s, 1);
         }
         ptx::mbar_init(drain, 1);
         *abort_flag = 0;
+        tmem_holder[3] = 0;
+        for (int i = 0; i < 4 * kUnitRing; ++i) reinterpret_cast<volatile uint32_t *>(bars + 32)[i] = 0;
         ptx::fence_barrier_init();
         ptx::fence_proxy_async();
     }
@@ -386,32 +519,64 @@ __global__ void __launch_bounds__(GemmCfg<BN, CG, 1>::kThreads, 1) muon_products
     if (CG == 2) cluster_sync();
     ptx::tc_fence_after_sync();
     const uint32_t tmem = *tmem_holder;
+    ptx::grid_dependency_wait();
+    ptx::grid_launch_dependents();
     float grad_scale;
     const int n_units = muon_scale(p, grad_scale) ? p.n_units : 0;  // a bad scale leaves the step out
-    auto left_out = [&](const MuonUnit &g) {
-        return !eg_check(g.matrix >= 0 && g.matrix < p.n_matrices, p.status, kCheckMuonUnit, g.matrix) || muon_skips(p, p.matrices[g.matrix]);
-    };
+    int32_t taken = 0;  // of the worker's units, by this thread's role
+    MuonUnit g{};
+    auto next = [&] { return unit_next(g, ring, taken++, abort_flag, p.wait_limit_ns); };
 
     if (warp == 0) {
         if (lane == 0) {
             uint32_t stage = 0, phase = 0, asked = 0;
             bool ok = !(p.stall == 1 && worker == 0);
             const uint32_t full_base = CG == 2 ? map_to_rank(full0, 0) : full0;
-            for (int u = worker; ok && u < n_units; u += workers) {
-                const MuonUnit g = muon_unit(p, u);
-                if (left_out(g)) continue;
-                const MuonMatrix &q = p.matrices[g.matrix];
+            // The pair's first CTA takes the units: a ticket two ahead, its entry one ahead.
+            int32_t at = 0, later = 0;
+            int4 entry{};
+            auto take = [&] { return atomicAdd(p.ticket, 1); };
+            auto look = [&](int32_t u) { return u < n_units ? p.units[u] : make_int4(kNoMoreUnits, 0, 0, 0); };
+            const uint32_t ring1 = CG == 2 ? map_to_rank(ring, 1) : 0;
+            if (rank == 0 && ok) {
+                at = take();
+                later = take();
+                entry = look(at);
+            }
+            auto first_next = [&] {
+                while (true) {
+                    const int4 q = entry;
+                    if (q.x != kNoMoreUnits) {
+                        g = muon_unit(q);
+                        if (!eg_check(g.matrix < p.n_matrices && g.product < p.products, p.status, kCheckMuonUnit, g.matrix)) return false;
+                        const int state = muon_wait(p.done + g.matrix, g.need, abort_flag, p.wait_limit_ns);
+                        if (state == 0) return false;
+                        if (state < 0) {
+                            entry = look(later);
+                            later = take();
+                            continue;
+                        }
+                    }
+                    unit_publish(ring, q, taken);
+                    if (CG == 2) unit_publish(ring1, q, taken);
+                    ++taken;
+                    entry = look(later);
+                    later = take();
+                    return q.x != kNoMoreUnits;
+                }
+            };
+            while (ok && (rank == 0 ? first_next() : next())) {
                 const CUtensorMap *maps = p.maps + (int64_t)g.matrix * kMuonMaps;
-                const int kind = g.product % 3, x = g.product / 3 & 1;
-                // A X^T and X^T X, A A, and the polynomial times X from either side
+                const int x = g.product / 3 & 1;
+                // X X^T or X^T X, A A, and the polynomial times X from either side
                 const CUtensorMap *map_a, *map_b;
                 bool a_mn = false, b_mn = false;
-                if (kind == 0) {
-                    a_mn = b_mn = q.tall;
-                    map_a = map_b = maps + (x ? kMapX1 : kMapX0) + (q.tall ? 1 : 0);
-                } else if (kind == 1) {
+                if (g.kind == 0) {
+                    a_mn = b_mn = g.tall;
+                    map_a = map_b = maps + (x ? kMapX1 : kMapX0) + (g.tall ? 1 : 0);
+                } else if (g.kind == 1) {
                     map_a = map_b = maps + kMapGram;
-                } else if (q.tall) {
+                } else if (g.tall) {
                     map_a = maps + (x ? kMapX1 : kMapX0);
                     map_b = maps + kMapPoly;
                 } else {
@@ -419,9 +584,10 @@ __global__ void __launch_bounds__(GemmCfg<BN, CG, 1>::kThreads, 1) muon_products
                     map_b = maps + (x ? kMapX1N : kMapX0N);
                     b_mn = true;
                 }
+                const uint32_t bytes = CG * (g.same ? Cfg::kABytes : Cfg::kStageBytes);
                 ptx::tensormap_acquire(map_a);
                 ptx::tensormap_acquire(map_b);
-                if (!muon_wait(p.done + g.matrix, g.need, abort_flag, p.wait_limit_ns)) break;
+                if (rank == 1 && muon_wait(p.done + g.matrix, g.need, abort_flag, p.wait_limit_ns) != 1) break;
                 fence_proxy_async_all();  // what other SMs stored is read by tile loads
                 const int32_t m0 = g.tm * Cfg::kTileRows + (int)rank * kGemmM, n0 = g.tn * BN + (int)rank * Cfg::kBRows;
                 for (int kb = 0; kb < g.kblocks; ++kb) {
@@ -430,7 +596,7 @@ __global__ void __launch_bounds__(GemmCfg<BN, CG, 1>::kThreads, 1) muon_products
                         break;
                     }
                     const uint32_t sa = smem_base + stage * Cfg::kStageBytes, sb = sa + Cfg::kABytes;
-                    if (rank == 0) ptx::mbar_arrive_expect_tx(full0 + 8 * stage, CG * Cfg::kStageBytes);
+                    if (rank == 0) ptx::mbar_arrive_expect_tx(full0 + 8 * stage, bytes);
                     const uint32_t bar = full_base + 8 * stage;
                     if (a_mn) {
 #pragma unroll
@@ -438,7 +604,8 @@ __global__ void __launch_bounds__(GemmCfg<BN, CG, 1>::kThreads, 1) muon_products
                     } else {
                         tma_load_g<CG>(sa, map_a, kb * kGemmK, m0, bar);
                     }
-                    if (b_mn) {
+                    if (g.same) {
+                    } else if (b_mn) {
 #pragma unroll
                         for (int s = 0; s < Cfg::kBRows / 64; ++s) tma_load_g<CG>(sb + s * 8192, map_b, n0 + 64 * s, kb * kGemmK, bar);
                     } else {
@@ -460,12 +627,8 @@ __global__ void __launch_bounds__(GemmCfg<BN, CG, 1>::kThreads, 1) muon_products
             uint32_t it = 0, acc = 0, acc_phase = 0;
             bool ok = true;
             const bool stop = p.stall == 2 && worker == 0;
-            for (int u = worker; ok && u < n_units; u += workers) {
-                const MuonUnit g = muon_unit(p, u);
-                if (left_out(g)) continue;
-                const bool tall = p.matrices[g.matrix].tall;
-                const int kind = g.product % 3;
-                const bool a_mn = kind == 0 && tall, b_mn = kind == 0 ? tall : kind == 2 && !tall;
+            while (ok && next()) {
+                const bool a_mn = g.kind == 0 && g.tall, b_mn = g.kind == 0 ? g.tall : g.kind == 2 && !g.tall;
                 const uint32_t idesc = idesc0 | ((uint32_t)a_mn << 15) | ((uint32_t)b_mn << 16);
                 const uint32_t step_a = a_mn ? 2048u >> 4 : 32u >> 4, step_b = b_mn ? 2048u >> 4 : 32u >> 4;
                 const uint64_t base_a = a_mn ? make_desc_mn_sw128(0) : ptx::make_desc_k_sw128(0);
@@ -483,7 +646,7 @@ __global__ void __launch_bounds__(GemmCfg<BN, CG, 1>::kThreads, 1) muon_products
                         break;
                     }
                     ptx::tc_fence_after_sync();
-                    const uint32_t sa = smem_base + s * Cfg::kStageBytes, sb = sa + Cfg::kABytes;
+                    const uint32_t sa = smem_base + s * Cfg::kStageBytes, sb = g.same ? sa : sa + Cfg::kABytes;
                     mma_stage<BN, CG>(tmem + acc * BN, base_a | (sa >> 4), base_b | (sb >> 4), step_a, step_b, idesc, k == 0);
                     mma_commit_g<CG>(empty0 + 8 * s);
                 }
@@ -501,108 +664,208 @@ __global__ void __launch_bounds__(GemmCfg<BN, CG, 1>::kThreads, 1) muon_products
             }
         }
         __syncwarp();
-    } else {
+    } else if (warp < 2 + kEpiWarps) {
         const int e = warp - 2, quarter = warp & 3, strip = e >> 2;
-        uint32_t acc = 0, acc_phase = 0;
+        uint32_t acc = 0, acc_phase = 0, piece = 0;  // piece: pieces staged so far
         const uint32_t release0 = CG == 2 ? map_to_rank(accempty0, 0) : accempty0;
         Tile t;
-        t.stage = staging + e * 32 * kStagePitch;
+        t.stage = reinterpret_cast<uint16_t *>(staging + e * Cfg::kWarpStaging);
         t.lane = lane;
         t.wide = 2;
-        for (int u = worker; u < n_units; u += workers) {
-            const MuonUnit g = muon_unit(p, u);
-            if (left_out(g)) continue;
-            const MuonMatrix &q = p.matrices[g.matrix];
-            const int kind = g.product % 3, x = g.product / 3 & 1;
-            const bool last = g.product + 1 == p.products;
-            const int64_t m = kind == 2 ? q.rows : q.d, n = kind == 2 ? q.cols : q.d;
-            t.row0 = (int64_t)g.tm * Cfg::kTileRows + (int)rank * kGemmM + quarter * 32;
-            t.rows = (int)min(m - t.row0, (int64_t)32);
-            t.col0 = g.tn * BN + strip * Cfg::kColsPerWarp;
-            t.cols = (int)min(n - t.col0, (int64_t)1 << 20);
+        const uint32_t stage_at = ptx::smem_u32(t.stage);
+        bool ok = true;
+        while (ok && __all_sync(0xffffffffu, next())) {
+            if (!__all_sync(0xffffffffu, units_wait(followed, taken - kUnitLag, abort_flag, p.wait_limit_ns))) break;
             // what this warp reads was stored by other SMs
-            bool ok = true;
-            if (lane == 0) ok = muon_wait(p.done + g.matrix, g.need, abort_flag, p.wait_limit_ns);
-            if (!__all_sync(0xffffffffu, ok)) break;
-            const float keep = 1.0f - p.lr * q.wd, step = p.lr * q.scale * q.down;
-            uint32_t hi[16], lo[16];
-            auto fetch = [&] {
-                if (t.rows <= 0 || t.cols <= 0 || kind == 0) return;
-                muon_fetch(hi, kind == 1 ? q.gram : q.x[x], kind == 1 ? q.ldd : q.ldx, t);
-                if (kind == 2) muon_fetch(lo, q.lo, q.ldx, t);
+            int there = 1;
+            if (lane == 0 && g.kind != 0) there = muon_wait(p.done + g.matrix, g.need, abort_flag, p.wait_limit_ns);
+            if (__shfl_sync(0xffffffffu, there, 0) != 1) break;
+            const MuonMatrix q = p.matrices[g.matrix];  // (a copy: memory that may have changed would be read anew at every use)
+            t.row0 = (int64_t)g.tm * Cfg::kTileRows + (int)rank * kGemmM + quarter * 32;
+            t.rows = (int)min((g.kind == 2 ? q.rows : q.d) - t.row0, (int64_t)32);
+            t.col0 = g.tn * BN + strip * Cfg::kColsPerWarp;
+            t.cols = (int)min((g.kind == 2 ? q.cols : q.d) - t.col0, (int64_t)1 << 20);
+            // all that the epilogue reads of the workspace is on its way while the products are computed
+            const bool update = g.product + 1 == p.products;
+            uint32_t ahead[Cfg::kPieces][16];
+            uint32_t weights[2][16];
+            auto fetch_update = [&] {
+                if (t.rows <= 0 || t.cols <= 0) return;
+                muon_fetch(ahead[0], q.lo, q.ldx, t);
+                if (q.vector) with_type(q.param_type, [&](auto type) { muon_weights<decltype(type)>(weights, q, t); });
             };
-            fetch();
+            if (update) {
+                fetch_update();
+            } else if (g.kind != 0) {
+                const uint16_t *from = g.kind == 1 ? q.gram : q.lo;
+                const int64_t ld = g.kind == 1 ? q.ldd : q.ldx;
+                Tile at = t;
+#pragma unroll
+                for (int c = 0; c < Cfg::kPieces; ++c) {
+                    muon_fetch(ahead[c], from, ld, at);
+                    at.col0 += kPiece;
+                    at.cols -= kPiece;
+                }
+            }
             if (!__all_sync(0xffffffffu, ptx::mbar_wait_bounded(accfull0 + 8 * acc, acc_phase, abort_flag, p.wait_limit_ns))) break;
             ptx::tc_fence_after_sync();
             const uint32_t src = tmem + ((uint32_t)(quarter * 32) << 16) + acc * BN + strip * Cfg::kColsPerWarp;
-#pragma unroll 1
-            for (int c = 0; c < Cfg::kPieces; ++c) {
-                float v[32];
-                ptx::tmem_ld_32x32(src + c * kPiece, reinterpret_cast<uint32_t (&)[32]>(v));
-                ptx::tmem_ld_wait();
-                if (c == Cfg::kPieces - 1) {
-                    ptx::tc_fence_before_sync();
-                    if (lane == 0) {
-                        if (CG == 2)
-                            mbar_arrive_cluster(release0 + 8 * acc);
-                        else
-                            ptx::mbar_arrive(release0 + 8 * acc);
-                    }
+            auto release = [&] {
+                ptx::tc_fence_before_sync();
+                if (lane == 0) {
+                    if (CG == 2)
+                        mbar_arrive_cluster(release0 + 8 * acc);
+                    else
+                        ptx::mbar_arrive(release0 + 8 * acc);
                 }
-                if (t.rows > 0 && t.cols > 0) {
-                    if (kind == 2) {
-                        const float a = kNsA;
+            };
+            auto add_rest = [](float (&v)[32], const uint32_t (&rest)[16]) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const float2 l = unpack2<f16>(rest[i]);
+                    v[2 * i] = fmaf(kNsA, l.x, v[2 * i]);
+                    v[2 * i + 1] = fmaf(kNsA, l.y, v[2 * i + 1]);
+                }
+            };
+            if (update) {
+                // (a narrow update goes through this warp's buffers, which may still be being stored)
+                for (uint32_t back = 1; back <= 2 && back <= piece; ++back)
+                    ok = ok && ptx::mbar_wait_bounded(free0 + 8 * ((piece - back) & 1u), ((piece - back) >> 1) & 1u, abort_flag, p.wait_limit_ns);
+                if (!__all_sync(0xffffffffu, ok)) break;
+                const float keep = 1.0f - p.lr * q.wd, by = p.lr * q.scale * q.down;
+                float *stage = reinterpret_cast<float *>(t.stage);
+                with_type(q.param_type, [&](auto type) {
+                    using P = decltype(type);
+#pragma unroll 1
+                    for (int c = 0; c < Cfg::kPieces; ++c) {
+                        float v[32];
+                        ptx::tmem_ld_32x32(src + c * kPiece, reinterpret_cast<uint32_t (&)[32]>(v));
+                        ptx::tmem_ld_wait();
+                        if (c == Cfg::kPieces - 1) release();
+                        if (t.rows > 0 && t.cols > 0) {
+                            add_rest(v, ahead[0]);
+                            __syncwarp();
+#pragma unroll
+                            for (int i = 0; i < 8; ++i)
+                                *reinterpret_cast<float4 *>(stage + lane * kUpdatePitch + 4 * i) = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+                            __syncwarp();
+                            if (q.vector)
+                                muon_update_wide<P>(q, weights, stage, keep, by, t);
+                            else
+                                muon_update_narrow<P>(q, stage, keep, by, t);
+                        }
+                        t.col0 += kPiece;
+                        t.cols -= kPiece;
+                        if (c + 1 < Cfg::kPieces) fetch_update();
+                    }
+                });
+            } else {
+                const float down = q.down * q.down;
+#pragma unroll
+                for (int c = 0; c < Cfg::kPieces; ++c, ++piece) {
+                    float v[32];
+                    ptx::tmem_ld_32x32(src + c * kPiece, reinterpret_cast<uint32_t (&)[32]>(v));
+                    ptx::tmem_ld_wait();
+                    if (c == Cfg::kPieces - 1) release();
+                    uint32_t first[16], second[16];  // X and its rest, or a symmetric piece
+                    if (g.kind == 2) {
+                        add_rest(v, ahead[c]);
+                    } else if (g.kind == 0) {
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) v[i] *= down;
+                    } else {
 #pragma unroll
                         for (int i = 0; i < 16; ++i) {
-                            const float2 h = unpack2<f16>(hi[i]), l = unpack2<f16>(lo[i]);
-                            v[2 * i] = fmaf(a, l.x, fmaf(a, h.x, v[2 * i]));
-                            v[2 * i + 1] = fmaf(a, l.y, fmaf(a, h.y, v[2 * i + 1]));
+                            const float2 h = unpack2<f16>(ahead[c][i]);
+                            v[2 * i] = fmaf(kNsC, v[2 * i], kNsB * h.x);
+                            v[2 * i + 1] = fmaf(kNsC, v[2 * i + 1], kNsB * h.y);
                         }
-                        if (last) {
-                            if (q.param_type == EGERIA_F32)
-                                muon_update<float>(q, v, keep, step, t);
-                            else if (q.param_type == EGERIA_BF16)
-                                muon_update<bf16>(q, v, keep, step, t);
-                            else
-                                muon_update<f16>(q, v, keep, step, t);
-                        } else {
+                        if (t.row0 == t.col0) {
 #pragma unroll
-                            for (int i = 0; i < 16; ++i) {
-                                hi[i] = pack2<f16>(v[2 * i], v[2 * i + 1]);
-                                const float2 h = unpack2<f16>(hi[i]);
-                                lo[i] = pack2<f16>(v[2 * i] - h.x, v[2 * i + 1] - h.y);
-                            }
-                            muon_store(q.x[x ^ 1], q.ldx, hi, t);
-                            muon_store(q.lo, q.ldx, lo, t);
+                            for (int i = 0; i < 32; ++i) v[i] += lane == i ? kNsA : 0.0f;
                         }
-                    } else if (t.row0 <= t.col0) {
-                        if (kind == 0) {
-                            const float s = q.down * q.down;
+                    }
 #pragma unroll
-                            for (int i = 0; i < 32; ++i) v[i] *= s;
-                        } else {
+                    for (int i = 0; i < 16; ++i) first[i] = pack2<f16>(v[2 * i], v[2 * i + 1]);
+                    const uint32_t buffer = piece & 1u, to = stage_at + buffer * Cfg::kBuffer;
+                    ok = ok && ptx::mbar_wait_bounded(free0 + 8 * buffer, (piece >> 1 & 1u) ^ 1u, abort_flag, p.wait_limit_ns);
+                    if (!__all_sync(0xffffffffu, ok)) break;
+                    muon_stage_rows(to, first, lane);
+                    if (g.kind == 2) {
 #pragma unroll
-                            for (int i = 0; i < 16; ++i) {
-                                const float2 h = unpack2<f16>(hi[i]);
-                                v[2 * i] = fmaf(kNsC, v[2 * i], kNsB * h.x);
-                                v[2 * i + 1] = fmaf(kNsC, v[2 * i + 1], kNsB * h.y);
-                            }
+                        for (int i = 0; i < 16; ++i) {
+                            const float2 f = unpack2<f16>(first[i]);
+                            second[i] = pack2<f16>(v[2 * i] - f.x, v[2 * i + 1] - f.y);
                         }
-                        muon_store_symmetric(kind == 0 ? q.gram : q.poly, q.ldd, v, t);
+                        muon_stage_rows(to + 2048, second, lane);
+                    } else if (t.row0 < t.col0) {
+                        muon_stage_mirror(to + 2048, first, lane);
+                    }
+                    ptx::fence_proxy_async();
+                    __syncwarp();
+                    if (lane == 0) ptx::mbar_arrive(staged0 + 8 * buffer);
+                    t.col0 += kPiece;
+                    t.cols -= kPiece;
+                }
+            }
+            acc ^= 1u;
+            if (acc == 0) acc_phase ^= 1u;
+        }
+    } else {
+        // The stores: lane w those of the epilogue's warp w.  Of a symmetric product the pieces on and above the diagonal and, of
+        // the latter, the mirror images; the others are left to theirs.
+        const int w = lane & (kEpiWarps - 1), quarter = (w + 2) & 3, strip = w >> 2;
+        const uint32_t from = ptx::smem_u32(staging) + w * Cfg::kWarpStaging;
+        uint32_t piece = 0;
+        bool ok = true;
+        while (ok && __all_sync(0xffffffffu, next())) {
+            if (lane == 0) units_followed(followed, taken);
+            if (g.product + 1 == p.products) continue;  // the update: stored by the epilogue's warps, and nothing waits for it
+            const MuonMatrix q = p.matrices[g.matrix];
+            const CUtensorMap *maps = p.maps + (int64_t)g.matrix * kMuonMaps;
+            const CUtensorMap *map_first = maps + (g.kind == 0 ? kMapGramS : g.kind == 1 ? kMapPolyS : g.product / 3 & 1 ? kMapX0S : kMapX1S);
+            const CUtensorMap *map_second = g.kind == 2 ? maps + kMapRestS : map_first;
+            const int64_t m = g.kind == 2 ? q.rows : q.d, n = g.kind == 2 ? q.cols : q.d;
+            const int32_t row0 = g.tm * Cfg::kTileRows + (int)rank * kGemmM + quarter * 32;
+            int32_t col0 = g.tn * BN + strip * Cfg::kColsPerWarp;
+            ptx::tensormap_acquire(map_first);
+            ptx::tensormap_acquire(map_second);
+            for (int c = 0; c < Cfg::kPieces; ++c, ++piece, col0 += kPiece) {
+                const uint32_t buffer = piece & 1u;
+                ok = __all_sync(0xffffffffu, ptx::mbar_wait_bounded(staged0 + 8 * buffer, piece >> 1 & 1u, abort_flag, p.wait_limit_ns));
+                if (!ok) break;
+                if (lane < kEpiWarps && row0 < m && col0 < n && (g.kind == 2 || row0 <= col0)) {
+                    tile_store(map_first, col0, row0, from + buffer * Cfg::kBuffer);
+                    if (g.kind == 2)
+                        tile_store(map_second, col0, row0, from + buffer * Cfg::kBuffer + 2048);
+                    else if (row0 < col0)
+                        tile_store(map_second, row0, col0, from + buffer * Cfg::kBuffer + 2048);
+                }
+                tile_store_commit();
+                if (c + 1 < Cfg::kPieces) {
+                    if (c > 0) {
+                        tile_store_read<1>();
+                        __syncwarp();
+                        if (lane == 0) ptx::mbar_arrive(free0 + 8 * (buffer ^ 1u));
+                    }
+                } else {
+                    tile_store_read<0>();
+                    __syncwarp();
+                    if (lane == 0) {
+                        ptx::mbar_arrive(free0 + 8 * (buffer ^ 1u));
+                        ptx::mbar_arrive(free0 + 8 * buffer);
                     }
                 }
-                t.col0 += kPiece;
-                t.cols -= kPiece;
-                if (c + 1 < Cfg::kPieces) fetch();
             }
-            // the tile's share of this warp is there for the loads of any SM
+            if (!ok) break;
+            // the tile is there for the loads of any SM
+            tile_store_done();
             fence_proxy_async_all();
             __threadfence();
             __syncwarp();
             if (lane == 0) atomicAdd(p.done + g.matrix, 1);
-            acc ^= 1u;
-            if (acc == 0) acc_phase ^= 1u;
         }
+        tile_store_done();
     }
     ptx::tc_fence_before_sync();
     __syncthreads();

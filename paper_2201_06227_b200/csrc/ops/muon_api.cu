@@ -66,7 +66,7 @@ static bool muon_layout(int count, const egeria_muon_tensor *t, int steps, MuonL
         int64_t units = 0;
         muon_tiles(d, d, true, 128 * kind.cg, kind.bn, [&](int32_t, int32_t) { ++units; });
         L.n_units += steps * (2 * units + ((rows + 128 * kind.cg - 1) / (128 * kind.cg)) * ((cols + kind.bn - 1) / kind.bn));
-        if (L.n_units > (1 << 28) || L.n_pieces > 0x7fffffff) return false;
+        if (L.n_units > (1 << 28) || L.n_pieces > 0x7fffffff || L.n_matrices >= 0x7fffff) return false;  // (what the units' entries hold)
         MuonPlaces q;
         q.x[0] = take(rows * up32(cols) * 2);
         q.x[1] = take(rows * up32(cols) * 2);
@@ -81,54 +81,17 @@ static bool muon_layout(int count, const egeria_muon_tensor *t, int steps, MuonL
     L.grads = take((int64_t)count * (int64_t)sizeof(void *));
     L.pieces = take(L.n_pieces * (int64_t)sizeof(int2));
     L.units = take(L.n_units * (int64_t)sizeof(int4));
-    L.done = take(L.n_matrices * 4);
+    L.done = take(L.n_matrices * 4 + 4);
     return true;
 }
 
 template <int BN, int CG>
-static cudaError_t muon_workers(int sms, int *workers) {
-    auto kernel = muon_products_kernel<BN, CG>;
-    using Cfg = GemmCfg<BN, CG, 1>;
-    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg::kSmem);
-    if (e != cudaSuccess) return e;
-    // its blocks wait for one another: as many as are sure to run at once
-    cudaLaunchConfig_t c{};
-    c.gridDim = dim3(sms / CG * CG);
-    c.blockDim = dim3(Cfg::kThreads);
-    c.dynamicSmemBytes = Cfg::kSmem;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = CG;
-    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
-    c.attrs = attr;
-    c.numAttrs = 1;
-    int n = 0;
-    if (CG > 1) {
-        e = cudaOccupancyMaxActiveClusters(&n, kernel, &c);
-    } else {
-        e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, kernel, Cfg::kThreads, Cfg::kSmem);
-        n *= sms;
-    }
-    *workers = std::min(n, sms / CG);
-    return e;
+static cudaError_t muon_allow() {
+    return cudaFuncSetAttribute(muon_products_kernel<BN, CG>, cudaFuncAttributeMaxDynamicSharedMemorySize, MuonCfg<BN, CG>::kSmem);
 }
 template <int BN, int CG>
 static cudaError_t muon_launch(const MuonParams &p, int workers, cudaStream_t stream) {
-    using Cfg = GemmCfg<BN, CG, 1>;
-    cudaLaunchConfig_t c{};
-    c.gridDim = dim3(workers * CG);
-    c.blockDim = dim3(Cfg::kThreads);
-    c.dynamicSmemBytes = Cfg::kSmem;
-    c.stream = stream;
-    cudaLaunchAttribute attr[2];
-    attr[0].id = cudaLaunchAttributeCooperative;
-    attr[0].val.cooperative = 1;
-    attr[1].id = cudaLaunchAttributeClusterDimension;
-    attr[1].val.clusterDim.x = CG;
-    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
-    c.attrs = attr;
-    c.numAttrs = CG > 1 ? 2 : 1;
-    return cudaLaunchKernelEx(&c, muon_products_kernel<BN, CG>, p);
+    return launch(muon_products_kernel<BN, CG>, dim3(workers * CG), MuonCfg<BN, CG>::kThreads, MuonCfg<BN, CG>::kSmem, stream, CG, p);
 }
 
 }  // namespace ops
@@ -190,9 +153,8 @@ egeria_status egeria_muon_create(egeria_muon **out, int count, const egeria_muon
         }
         const EncodeTiledFn encode = reinterpret_cast<EncodeTiledFn>(fn);
         const MuonKind kind = muon_kind(count, tensors);
-        int workers = 0;
-        EGO_CUDA((kind.cg == 2 ? muon_workers<256, 2>(sms, &workers) : muon_workers<128, 1>(sms, &workers)));
-        if (workers < 1) return EGERIA_ERR_CUDA;
+        EGO_CUDA((kind.cg == 2 ? muon_allow<256, 2>() : muon_allow<128, 1>()));
+        const int workers = sms / kind.cg;
 
         h = new egeria_muon();
         uint8_t *ws = h->ws = static_cast<uint8_t *>(workspace);
@@ -229,16 +191,19 @@ egeria_status egeria_muon_create(egeria_muon **out, int count, const egeria_muon
             q.pieces = (int32_t)((t.rows * t.cols + kMuonPiece - 1) / kMuonPiece);
             // (the gradient may move: the kernels look at its alignment)
             q.vector = t.cols % 8 == 0 && aligned(t.param, 8 * size_of(t.param_type)) && aligned(t.master, 32) && aligned(t.m, 32);
-            auto map = [&](int which, const uint16_t *p, int64_t rows, int64_t cols, int64_t ld, int box_rows) {
+            auto map = [&](int which, const uint16_t *p, int64_t rows, int64_t cols, int64_t ld, int box_rows, int box_cols = 64) {
                 cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)ld * 2};
-                cuuint32_t box[2] = {64, (cuuint32_t)box_rows}, one[2] = {1, 1};
+                cuuint32_t box[2] = {(cuuint32_t)box_cols, (cuuint32_t)box_rows}, one[2] = {1, 1};
                 return encode(&maps[(size_t)k * kMuonMaps + which], CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2, const_cast<uint16_t *>(p), dims, strides, box, one,
-                              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+                              CU_TENSOR_MAP_INTERLEAVE_NONE, box_cols == 64 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
+                              CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
             };
             bool ok = true;
             for (int s = 0; s < 2; ++s)
                 ok = ok && map(kMapX0 + 2 * s, q.x[s], q.rows, q.cols, q.ldx, 128) && map(kMapX0N + 2 * s, q.x[s], q.rows, q.cols, q.ldx, 64);
+            ok = ok && map(kMapX0S, q.x[0], q.rows, q.cols, q.ldx, 32, 32) && map(kMapX1S, q.x[1], q.rows, q.cols, q.ldx, 32, 32) &&
+                 map(kMapRestS, q.lo, q.rows, q.cols, q.ldx, 32, 32) && map(kMapGramS, q.gram, q.d, q.d, q.ldd, 32, 32) &&
+                 map(kMapPolyS, q.poly, q.d, q.d, q.ldd, 32, 32);
             ok = ok && map(kMapGram, q.gram, q.d, q.d, q.ldd, 128) && map(kMapPoly, q.poly, q.d, q.d, q.ldd, 128);
             if (!ok) {
                 delete h;
@@ -247,8 +212,9 @@ egeria_status egeria_muon_create(egeria_muon **out, int count, const egeria_muon
             matrices.push_back(q);
             for (int s = 0; s < q.pieces; ++s) pieces.push_back(make_int2(k, s));
         }
-        // The units: matrices of like size go together, in groups whose tiles of one product go round the workers a few times;
-        // within a group product by product, so that a unit's matrix has mostly finished the product before.
+        // The units, product by product over all matrices, large ones first, so that a unit's matrix has mostly finished the product
+        // before.  (In groups whose products go round the workers two to eight times, which meet more of their values in L2, the
+        // 24 blocks of width 1024 took 5.75 to 5.18 ms against 5.15: the waits at a group's ends cost more.)
         std::vector<int> order(matrices.size());
         for (size_t i = 0; i < order.size(); ++i) order[i] = (int)i;
         std::stable_sort(order.begin(), order.end(), [&](int a, int b) {
@@ -261,25 +227,16 @@ egeria_status egeria_muon_create(egeria_muon **out, int count, const egeria_muon
         auto add = [&](int k, int product) {
             const MuonMatrix &q = matrices[k];
             const int part = product % 3;
-            const int32_t need = so_far[k] * kEpiWarps * kind.cg;
+            const int32_t need = so_far[k] * kind.cg;
             const int64_t m = part == 2 ? q.rows : q.d, n = part == 2 ? q.cols : q.d, sum = part == 0 ? std::max(q.rows, q.cols) : q.d;
             const int32_t kblocks = (int32_t)((sum + kGemmK - 1) / kGemmK);
             muon_tiles(m, n, part != 2, tile_rows, kind.bn, [&](int32_t tm, int32_t tn) {
-                units.push_back(make_int4(k, tm | tn << 16, product | kblocks << 8, need));
+                units.push_back(make_int4(q.tall ? k | INT32_MIN : k, tm | tn << 16, product | kblocks << 8, need));
                 ++so_far[k];
             });
         };
-        for (size_t first = 0; first < order.size();) {
-            size_t end = first;
-            int64_t tiles = 0;
-            for (; end < order.size() && tiles < 2 * workers; ++end) {
-                const int64_t side = (matrices[order[end]].d + kind.bn - 1) / kind.bn;
-                tiles += side * (side + 1) / 2;
-            }
-            for (int product = 0; product < 3 * steps; ++product)
-                for (size_t i = first; i < end; ++i) add(order[i], product);
-            first = end;
-        }
+        for (int product = 0; product < 3 * steps; ++product)
+            for (const int k : order) add(k, product);
         MuonParams &p = h->params;
         p.matrices = reinterpret_cast<const MuonMatrix *>(ws + L.matrices);
         p.maps = reinterpret_cast<const CUtensorMap *>(ws + L.maps);
@@ -287,6 +244,7 @@ egeria_status egeria_muon_create(egeria_muon **out, int count, const egeria_muon
         p.pieces = reinterpret_cast<const int2 *>(ws + L.pieces);
         p.grads = reinterpret_cast<const void *const *>(ws + L.grads);
         p.done = reinterpret_cast<int32_t *>(ws + L.done);
+        p.ticket = p.done + L.n_matrices;
         p.status = reinterpret_cast<int32_t *>(ws);
         p.n_units = (int32_t)units.size();
         p.n_pieces = (int32_t)pieces.size();

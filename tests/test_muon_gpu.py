@@ -1,12 +1,13 @@
 """GPU parity of the Muon step against the formula in 64 bits.
 
 Tolerances, derived before the first run.  One step of the orthogonalisation is bounded value by value: the products' operands are
-rounded by 2^-11 of themselves (X once, A once, b A + c A^2 once), X beside its product by 2^-21, a value of f16 below 2^-14
-by 2^-25; with N = |X| |X|^T that gives the sums written out in `one_step`.  Over five steps the roundings of one go into the next.
-Near 1, where the singular values end, |b A + c A^2| is at most 2.81 while the step returns at least 0.67 of X, and a step's slope is at
-most 0.72 there: a step adds at most 2^-11 (2.81 + 2.81 + 0.72) / 0.67 = 4.6e-3, five of them 4.6e-3 / (1 - 0.72) = 1.7e-2 of a single
-singular value.  Over a matrix the roundings are independent, of root mean square 2^-11 / sqrt(12) or less: sqrt(2) 2.81 / 0.67 / sqrt(12)
-2^-11 = 8.4e-4 a step for those of the polynomial and of X, 1.2e-3 for five; six times that is allowed for in the 2-norm, 7e-3.
+rounded by 2^-11 of themselves (X once, A once, a I + b A + c A^2 once), what X's rounding leaves by 2^-21 of X and multiplied by a
+alone, a value of f16 below 2^-14 by 2^-25; with N = |X| |X|^T that gives the sums written out in `one_step`.  Over five steps the
+roundings of one go into the next.  Near 1, where the singular values end, |b A + c A^2| is at most 2.81, by which X's rounding is
+multiplied, while the step returns at least 0.67 of X; A's rounding moves it by 0.72 at most, its own by itself; and a step's slope is
+at most 0.72 there: a step adds at most 2^-11 (2.81 + 0.72 + 0.67) / 0.67 = 3.1e-3, five of them 3.1e-3 / (1 - 0.72) = 1.1e-2 of a single
+singular value, and 1.7e-2 is allowed for.  Over a matrix the roundings are independent, of root mean square 2^-11 / sqrt(12) or less:
+sqrt(2) 2.81 / 0.67 / sqrt(12) 2^-11 = 8.4e-4 a step at most, 1.2e-3 for five; six times that is allowed for in the 2-norm, 7e-3.
 """
 import subprocess
 import sys
@@ -72,7 +73,9 @@ def one_step(t):
     want = A * x + (B * a + C * a @ a) @ x
     da = (2.0 ** -10 + 2.0 ** -11 + 2.0 ** -16) * n + 2.0 ** -25
     size = -B * n + C * n @ n
+    size = size + A * torch.eye(len(n), device=DEV, dtype=torch.float64)
     db = -B * da + C * (n @ da + da @ n + da @ da) + 2.0 ** -11 * (size + db_size(da)) + 2.0 ** -25
+    # the product takes X's first value alone, of the second a is taken: what is left out is (b A + c A^2) times it
     tol = db @ x.abs() * (1 + 2.0 ** -10) + 2.0 ** -11 * (size + db) @ x.abs() + 2.0 ** -20 * A * x.abs() + 2.0 ** -20 * want.abs() + 2.0 ** -40
     return (want.t(), tol.t()) if tall else (want, tol)
 

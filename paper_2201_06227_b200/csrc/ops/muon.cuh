@@ -31,8 +31,7 @@ namespace ops {
 constexpr float kNsA = 3.4445f, kNsB = -4.7750f, kNsC = 2.0315f;
 constexpr int kMuonPiece = 8192;     // values of a matrix that a block takes in the elementwise passes
 constexpr int kMuonThreads = 256;
-// Tile copies of a matrix: loads of 128 rows by 64 columns or (N) 64 by 64 for the other axis, stores (S) of 32 by 32.
-enum { kMapX0 = 0, kMapX0N, kMapX1, kMapX1N, kMapGram, kMapPoly, kMapX0S, kMapX1S, kMapRestS, kMapGramS, kMapPolyS, kMuonMaps };
+enum { kMapX0 = 0, kMapX0N, kMapX1, kMapX1N, kMapGram, kMapPoly, kMuonMaps };  // N: boxes of 64 x 64 for the other axis
 
 struct MuonMatrix {
     void *param;
@@ -59,6 +58,7 @@ struct MuonParams {
     const uint8_t *frozen;
     float lr, beta, rest, eps;
     int32_t nesterov, n_units, n_pieces, n_matrices, products;
+    int32_t early;                   // units are taken while the one before is loaded
     uint32_t stall;
     uint64_t wait_limit_ns;
 };
@@ -253,21 +253,45 @@ __device__ __forceinline__ void muon_fetch(uint32_t (&r)[16], const uint16_t *ba
         for (int i = 0; i < 16; ++i) r[i] = 0u;
     }
 }
-// Two 32 x 32 pieces in a warp's shared memory as tile stores take them: 64 bytes a row, whose sixteens change places with the row.
-__device__ __forceinline__ void muon_stage_rows(uint32_t at, const uint32_t (&r)[16], int lane) {
+// Rows of a warp's 32 x 32 piece (this lane's row, as 16 pairs) into its shared memory, from which they are stored by whole lines: a row
+// takes COLS / 8 sixteens of bytes, which change places with the row so that neither side meets a bank twice.
+template <int COLS>
+__device__ __forceinline__ uint32_t stage_place(uint32_t row, uint32_t sixteen) {
+    return COLS == 64 ? row * 128 + ((sixteen ^ (row & 7)) << 4) : row * 64 + ((sixteen ^ (row >> 1 & 3)) << 4);
+}
+template <int COLS>
+__device__ __forceinline__ void stage_rows(uint32_t at, uint32_t first, const uint32_t (&r)[16], int lane) {
 #pragma unroll
     for (int i = 0; i < 4; ++i)
-        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at + lane * 64 + ((i ^ (lane >> 1 & 3)) << 4)), "r"(r[4 * i]), "r"(r[4 * i + 1]),
+        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at + stage_place<COLS>(lane, first + i)), "r"(r[4 * i]), "r"(r[4 * i + 1]),
                      "r"(r[4 * i + 2]), "r"(r[4 * i + 3])
                      : "memory");
 }
-// The mirror image: this lane's row becomes column `lane`.
-__device__ __forceinline__ void muon_stage_mirror(uint32_t at, const uint32_t (&r)[16], int lane) {
+// The mirror image of a piece: this lane's row becomes column `lane`.
+__device__ __forceinline__ void stage_mirror(uint32_t at, const uint32_t (&r)[16], int lane) {
 #pragma unroll
     for (int c = 0; c < 32; ++c) {
         const uint16_t v = (uint16_t)(c & 1 ? r[c >> 1] >> 16 : r[c >> 1] & 0xffffu);
-        asm volatile("st.shared.b16 [%0], %1;" ::"r"(at + c * 64 + (((lane >> 3) ^ (c >> 1 & 3)) << 4) + (lane & 7) * 2), "h"(v) : "memory");
+        asm volatile("st.shared.b16 [%0], %1;" ::"r"(at + stage_place<32>(c, lane >> 3) + (lane & 7) * 2), "h"(v) : "memory");
     }
+}
+// 32 staged rows of COLS values to a matrix in the workspace, at its first of `rows` rows and `cols` columns that are left (rows are padded to
+// whole pieces there).
+template <int COLS>
+__device__ __forceinline__ void store_staged(uint32_t at, uint16_t *to, int64_t ld, int rows, int cols, int lane) {
+    constexpr int kLanes = COLS / 8, kRows = 32 / kLanes;  // lanes of a row, rows at a time
+    const int sixteen = lane % kLanes, row0 = lane / kLanes;
+    if (sixteen * 8 >= cols) return;
+    uint4 v[32 / kRows];
+#pragma unroll
+    for (int i = 0; i < 32 / kRows; ++i)
+        asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
+                     : "=r"(v[i].x), "=r"(v[i].y), "=r"(v[i].z), "=r"(v[i].w)
+                     : "r"(at + stage_place<COLS>(row0 + i * kRows, sixteen))
+                     : "memory");
+#pragma unroll
+    for (int i = 0; i < 32 / kRows; ++i)
+        if (row0 + i * kRows < rows) *reinterpret_cast<uint4 *>(to + (row0 + i * kRows) * ld + sixteen * 8) = v[i];
 }
 
 // p = p keep - step X of a piece.  Four values of a row per lane, eight lanes a row: what X's 32 rows in lanes become through the
@@ -375,25 +399,14 @@ __device__ __forceinline__ int muon_wait(const int32_t *done, int32_t need, vola
 }
 __device__ __forceinline__ void fence_proxy_async_all() { asm volatile("fence.proxy.async;" ::: "memory"); }
 
-// Tile stores: a lane issues its own and waits for them.
-__device__ __forceinline__ void tile_store(const CUtensorMap *map, int32_t x, int32_t y, uint32_t src) {
-    asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%1, %2}], [%3];" ::"l"(map), "r"(x), "r"(y), "r"(src) : "memory");
-}
-__device__ __forceinline__ void tile_store_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
-template <int PENDING>
-__device__ __forceinline__ void tile_store_read() {  // what all but the last so many groups read of shared memory may change
-    asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(PENDING) : "memory");
-}
-__device__ __forceinline__ void tile_store_done() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
-
-// As the linear layers' kernel, with a stage less, 8 KB of shared memory for each of the epilogue's warps (two buffers of
-// two pieces), and a warp that stores what they leave there.
+// As the linear layers' kernel, with a stage less, 8 KB of shared memory for each of the epilogue's warps, a warp that says
+// when a tile is stored, and one that takes the units.
 template <int BN, int CG>
 struct MuonCfg : GemmCfg<BN, CG, 1> {
     using Base = GemmCfg<BN, CG, 1>;
     static constexpr int kStages = 5;
-    static constexpr int kBuffer = 4096, kWarpStaging = 2 * kBuffer;
-    static constexpr int kThreads = Base::kThreads + 32;
+    static constexpr int kWarpStaging = 8192;
+    static constexpr int kThreads = Base::kThreads + 64;
     static constexpr int kSmem = 1024 + kStages * Base::kStageBytes + kEpiWarps * kWarpStaging + 512;
     static_assert(kSmem <= 227 * 1024 && Base::kStageBytes % 1024 == 0, "shared memory of a CTA, tiles on their boundary");
 };
@@ -414,23 +427,28 @@ __device__ __forceinline__ MuonUnit muon_unit(const int4 &q) {
     g.same = g.kind != 2 && g.tm == g.tn;
     return g;
 }
-// The units that a worker's first producer has taken and found ready, for the other roles and the pair's other CTA: the last
-// kUnitRing of them and how many there have been.  No role falls further behind: the stages hold the loads of five units at most,
-// a unit's products need the accumulator of the unit two before it drained, and the epilogue does not begin a unit before the
-// storing warp has taken the one kUnitLag before it.
-constexpr int kUnitRing = 16, kUnitLag = 4;
+// The units that a worker has taken and found ready, for its roles in both CTAs of a pair: the last kUnitRing of them.  One thread
+// takes them, at most one beyond those whose loads have been asked for.  No role falls further behind: the stages hold the loads of
+// five units at most, a unit's products need the accumulator of the unit two before it drained, and the epilogue does not begin a
+// unit before the warp that makes tiles known has taken the one kUnitLag before it, which has then seen the one before that stored.
+constexpr int kUnitRing = 16, kUnitLag = 3;
 constexpr int kNoMoreUnits = 0x7fffffff;
 // An entry goes as two words of 56 bits, each with the low 8 bits of its number plus one, by which a reader knows it.
-__device__ __forceinline__ void unit_publish(uint32_t ring, const int4 &q, int32_t n) {
+template <int CG>
+__device__ __forceinline__ void unit_publish(uint32_t ring, uint32_t other, const int4 &q, int32_t n) {
     const uint64_t tag = (uint64_t)(n + 1 & 0xff) << 56;
     const uint64_t a = tag | (uint64_t)(q.x < 0) << 55 | (uint64_t)((uint32_t)q.x & 0x7fffff) << 32 | (uint32_t)q.y;
     const uint64_t b = tag | (uint64_t)((uint32_t)q.z & 0x1ffffff) << 31 | (uint32_t)(q.w & 0x7fffffff);
-    const uint32_t to = ring + (uint32_t)(n % kUnitRing) * 16;
-    asm volatile("st.relaxed.cluster.shared::cluster.b64 [%0], %1;" ::"r"(to), "l"(a) : "memory");
-    asm volatile("st.relaxed.cluster.shared::cluster.b64 [%0], %1;" ::"r"(to + 8), "l"(b) : "memory");
+    asm volatile("fence.acq_rel.cluster;" ::: "memory");  // what the unit waited for comes before its entry
+#pragma unroll
+    for (int r = 0; r < CG; ++r) {
+        const uint32_t to = (r ? other : ring) + (uint32_t)(n % kUnitRing) * 16;
+        asm volatile("st.relaxed.cluster.shared::cluster.b64 [%0], %1;" ::"r"(to), "l"(a) : "memory");
+        asm volatile("st.relaxed.cluster.shared::cluster.b64 [%0], %1;" ::"r"(to + 8), "l"(b) : "memory");
+    }
 }
-// The number of units that the storing warp of this CTA has taken, and the wait for it.
-__device__ __forceinline__ void units_followed(uint32_t at, int32_t n) { asm volatile("st.release.cta.shared::cta.s32 [%0], %1;" ::"r"(at), "r"(n) : "memory"); }
+// A number of units that one thread of this CTA raises and another waits for.
+__device__ __forceinline__ void units_raise(uint32_t at, int32_t n) { asm volatile("st.release.cta.shared::cta.s32 [%0], %1;" ::"r"(at), "r"(n) : "memory"); }
 __device__ __forceinline__ bool units_wait(uint32_t at, int32_t n, volatile int *abort_flag, uint64_t limit_ns) {
     auto there = [&] {
         int32_t r;
@@ -448,15 +466,15 @@ __device__ __forceinline__ bool units_wait(uint32_t at, int32_t n, volatile int 
     }
     return true;
 }
-// Unit n of the worker, once it is there; false at the end and where the wait runs out.  (It says nothing about memory: who
-// reads what other SMs have stored looks at the matrix's counter too.)
+// Unit n of the worker, once it is there; false at the end and where the wait runs out.  What the unit waited for has then been
+// stored for this thread too.
 __device__ __forceinline__ bool unit_next(MuonUnit &g, uint32_t ring, int32_t n, volatile int *abort_flag, uint64_t limit_ns) {
     const uint32_t at = ring + (uint32_t)(n % kUnitRing) * 16;
     const uint32_t tag = n + 1 & 0xff;
     uint64_t a, b;
     auto there = [&] {
-        asm volatile("ld.relaxed.cluster.shared::cta.b64 %0, [%1];" : "=l"(a) : "r"(at) : "memory");
-        asm volatile("ld.relaxed.cluster.shared::cta.b64 %0, [%1];" : "=l"(b) : "r"(at + 8) : "memory");
+        asm volatile("ld.acquire.cluster.shared::cta.b64 %0, [%1];" : "=l"(a) : "r"(at) : "memory");
+        asm volatile("ld.acquire.cluster.shared::cta.b64 %0, [%1];" : "=l"(b) : "r"(at + 8) : "memory");
         return (uint32_t)(a >> 56) == tag && (uint32_t)(b >> 56) == tag;
     };
     bool ok = there();
@@ -487,11 +505,12 @@ __global__ void __launch_bounds__(MuonCfg<BN, CG>::kThreads, 1) muon_products_ke
     uint8_t *staging = smem + Cfg::kStages * Cfg::kStageBytes;
     uint64_t *bars = reinterpret_cast<uint64_t *>(staging + kEpiWarps * Cfg::kWarpStaging);
     const uint32_t full0 = ptx::smem_u32(bars), empty0 = full0 + 8 * Cfg::kStages;
-    const uint32_t accfull0 = empty0 + 8 * Cfg::kStages, accempty0 = accfull0 + 16, staged0 = accempty0 + 16, free0 = staged0 + 16, drain = free0 + 16;
-    volatile uint32_t *tmem_holder = reinterpret_cast<volatile uint32_t *>(bars + 2 * Cfg::kStages + 9);
+    const uint32_t accfull0 = empty0 + 8 * Cfg::kStages, accempty0 = accfull0 + 16, stored0 = accempty0 + 16, drain = stored0 + 8 * (kUnitLag + 1);
+    volatile uint32_t *tmem_holder = reinterpret_cast<volatile uint32_t *>(bars + 2 * Cfg::kStages + 5 + kUnitLag + 1);
     volatile int *abort_flag = reinterpret_cast<volatile int *>(tmem_holder + 1);
     volatile uint32_t *issued = tmem_holder + 2;
-    const uint32_t ring = ptx::smem_u32(bars) + 256, followed = ptx::smem_u32(const_cast<uint32_t *>(tmem_holder + 3));  // this worker's units
+    const uint32_t ring = ptx::smem_u32(bars) + 256;                                            // this worker's units
+    const uint32_t followed = ptx::smem_u32(const_cast<uint32_t *>(tmem_holder + 3)), loaded = followed + 4;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = CG == 2 ? cluster_rank() : 0;
     const int worker = blockIdx.x / CG;
@@ -503,12 +522,11 @@ __global__ void __launch_bounds__(MuonCfg<BN, CG>::kThreads, 1) muon_products_ke
         for (int s = 0; s < 2; ++s) {
             ptx::mbar_init(accfull0 + 8 * s, 1);
             ptx::mbar_init(accempty0 + 8 * s, kEpiWarps * CG);
-            ptx::mbar_init(staged0 + 8 * s, kEpiWarps);
-            ptx::mbar_init(free0 + 8 * s, 1);
         }
+        for (int s = 0; s <= kUnitLag; ++s) ptx::mbar_init(stored0 + 8 * s, kEpiWarps);
         ptx::mbar_init(drain, 1);
         *abort_flag = 0;
-        tmem_holder[3] = 0;
+        tmem_holder[3] = tmem_holder[4] = 0;
         for (int i = 0; i < 4 * kUnitRing; ++i) reinterpret_cast<volatile uint32_t *>(bars + 32)[i] = 0;
         ptx::fence_barrier_init();
         ptx::fence_proxy_async();
@@ -523,7 +541,7 @@ __global__ void __launch_bounds__(MuonCfg<BN, CG>::kThreads, 1) muon_products_ke
     ptx::grid_launch_dependents();
     float grad_scale;
     const int n_units = muon_scale(p, grad_scale) ? p.n_units : 0;  // a bad scale leaves the step out
-    int32_t taken = 0;  // of the worker's units, by this thread's role
+    int32_t taken = 0;  // of the worker's units, by this thread
     MuonUnit g{};
     auto next = [&] { return unit_next(g, ring, taken++, abort_flag, p.wait_limit_ns); };
 
@@ -532,40 +550,7 @@ __global__ void __launch_bounds__(MuonCfg<BN, CG>::kThreads, 1) muon_products_ke
             uint32_t stage = 0, phase = 0, asked = 0;
             bool ok = !(p.stall == 1 && worker == 0);
             const uint32_t full_base = CG == 2 ? map_to_rank(full0, 0) : full0;
-            // The pair's first CTA takes the units: a ticket two ahead, its entry one ahead.
-            int32_t at = 0, later = 0;
-            int4 entry{};
-            auto take = [&] { return atomicAdd(p.ticket, 1); };
-            auto look = [&](int32_t u) { return u < n_units ? p.units[u] : make_int4(kNoMoreUnits, 0, 0, 0); };
-            const uint32_t ring1 = CG == 2 ? map_to_rank(ring, 1) : 0;
-            if (rank == 0 && ok) {
-                at = take();
-                later = take();
-                entry = look(at);
-            }
-            auto first_next = [&] {
-                while (true) {
-                    const int4 q = entry;
-                    if (q.x != kNoMoreUnits) {
-                        g = muon_unit(q);
-                        if (!eg_check(g.matrix < p.n_matrices && g.product < p.products, p.status, kCheckMuonUnit, g.matrix)) return false;
-                        const int state = muon_wait(p.done + g.matrix, g.need, abort_flag, p.wait_limit_ns);
-                        if (state == 0) return false;
-                        if (state < 0) {
-                            entry = look(later);
-                            later = take();
-                            continue;
-                        }
-                    }
-                    unit_publish(ring, q, taken);
-                    if (CG == 2) unit_publish(ring1, q, taken);
-                    ++taken;
-                    entry = look(later);
-                    later = take();
-                    return q.x != kNoMoreUnits;
-                }
-            };
-            while (ok && (rank == 0 ? first_next() : next())) {
+            while (ok && next()) {
                 const CUtensorMap *maps = p.maps + (int64_t)g.matrix * kMuonMaps;
                 const int x = g.product / 3 & 1;
                 // X X^T or X^T X, A A, and the polynomial times X from either side
@@ -587,7 +572,6 @@ __global__ void __launch_bounds__(MuonCfg<BN, CG>::kThreads, 1) muon_products_ke
                 const uint32_t bytes = CG * (g.same ? Cfg::kABytes : Cfg::kStageBytes);
                 ptx::tensormap_acquire(map_a);
                 ptx::tensormap_acquire(map_b);
-                if (rank == 1 && muon_wait(p.done + g.matrix, g.need, abort_flag, p.wait_limit_ns) != 1) break;
                 fence_proxy_async_all();  // what other SMs stored is read by tile loads
                 const int32_t m0 = g.tm * Cfg::kTileRows + (int)rank * kGemmM, n0 = g.tn * BN + (int)rank * Cfg::kBRows;
                 for (int kb = 0; kb < g.kblocks; ++kb) {
@@ -617,6 +601,7 @@ __global__ void __launch_bounds__(MuonCfg<BN, CG>::kThreads, 1) muon_products_ke
                         phase ^= 1u;
                     }
                 }
+                if (ok && rank == 0) units_raise(loaded, taken);
             }
             *issued = asked;
         }
@@ -666,7 +651,7 @@ __global__ void __launch_bounds__(MuonCfg<BN, CG>::kThreads, 1) muon_products_ke
         __syncwarp();
     } else if (warp < 2 + kEpiWarps) {
         const int e = warp - 2, quarter = warp & 3, strip = e >> 2;
-        uint32_t acc = 0, acc_phase = 0, piece = 0;  // piece: pieces staged so far
+        uint32_t acc = 0, acc_phase = 0;
         const uint32_t release0 = CG == 2 ? map_to_rank(accempty0, 0) : accempty0;
         Tile t;
         t.stage = reinterpret_cast<uint16_t *>(staging + e * Cfg::kWarpStaging);
@@ -676,10 +661,6 @@ __global__ void __launch_bounds__(MuonCfg<BN, CG>::kThreads, 1) muon_products_ke
         bool ok = true;
         while (ok && __all_sync(0xffffffffu, next())) {
             if (!__all_sync(0xffffffffu, units_wait(followed, taken - kUnitLag, abort_flag, p.wait_limit_ns))) break;
-            // what this warp reads was stored by other SMs
-            int there = 1;
-            if (lane == 0 && g.kind != 0) there = muon_wait(p.done + g.matrix, g.need, abort_flag, p.wait_limit_ns);
-            if (__shfl_sync(0xffffffffu, there, 0) != 1) break;
             const MuonMatrix q = p.matrices[g.matrix];  // (a copy: memory that may have changed would be read anew at every use)
             t.row0 = (int64_t)g.tm * Cfg::kTileRows + (int)rank * kGemmM + quarter * 32;
             t.rows = (int)min((g.kind == 2 ? q.rows : q.d) - t.row0, (int64_t)32);
@@ -728,10 +709,6 @@ __global__ void __launch_bounds__(MuonCfg<BN, CG>::kThreads, 1) muon_products_ke
                 }
             };
             if (update) {
-                // (a narrow update goes through this warp's buffers, which may still be being stored)
-                for (uint32_t back = 1; back <= 2 && back <= piece; ++back)
-                    ok = ok && ptx::mbar_wait_bounded(free0 + 8 * ((piece - back) & 1u), ((piece - back) >> 1) & 1u, abort_flag, p.wait_limit_ns);
-                if (!__all_sync(0xffffffffu, ok)) break;
                 const float keep = 1.0f - p.lr * q.wd, by = p.lr * q.scale * q.down;
                 float *stage = reinterpret_cast<float *>(t.stage);
                 with_type(q.param_type, [&](auto type) {
@@ -759,113 +736,114 @@ __global__ void __launch_bounds__(MuonCfg<BN, CG>::kThreads, 1) muon_products_ke
                         if (c + 1 < Cfg::kPieces) fetch_update();
                     }
                 });
+            } else if (g.kind == 2) {
+                // X and its rest, 64 columns at a time
+#pragma unroll
+                for (int c = 0; c < Cfg::kPieces; c += 2) {
+                    __syncwarp();
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        float v[32];
+                        ptx::tmem_ld_32x32(src + (c + h) * kPiece, reinterpret_cast<uint32_t (&)[32]>(v));
+                        ptx::tmem_ld_wait();
+                        if (c + h == Cfg::kPieces - 1) release();
+                        add_rest(v, ahead[c + h]);
+                        uint32_t hi[16], lo[16];
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) {
+                            hi[i] = pack2<f16>(v[2 * i], v[2 * i + 1]);
+                            const float2 f = unpack2<f16>(hi[i]);
+                            lo[i] = pack2<f16>(v[2 * i] - f.x, v[2 * i + 1] - f.y);
+                        }
+                        stage_rows<64>(stage_at, 4 * h, hi, lane);
+                        stage_rows<64>(stage_at + 4096, 4 * h, lo, lane);
+                    }
+                    __syncwarp();
+                    const int64_t to = t.row0 * q.ldx + t.col0;
+                    const int cols = min((int)q.ldx - t.col0, 2 * kPiece);
+                    store_staged<64>(stage_at, (g.product / 3 & 1 ? q.x[0] : q.x[1]) + to, q.ldx, t.rows, cols, lane);
+                    store_staged<64>(stage_at + 4096, q.lo + to, q.ldx, t.rows, cols, lane);
+                    t.col0 += 2 * kPiece;
+                }
             } else {
+                // A, or the polynomial: the pieces on and above the diagonal and the mirror images of the latter
+                uint16_t *const to = g.kind == 0 ? q.gram : q.poly;
                 const float down = q.down * q.down;
 #pragma unroll
-                for (int c = 0; c < Cfg::kPieces; ++c, ++piece) {
+                for (int c = 0; c < Cfg::kPieces; ++c) {
                     float v[32];
                     ptx::tmem_ld_32x32(src + c * kPiece, reinterpret_cast<uint32_t (&)[32]>(v));
                     ptx::tmem_ld_wait();
                     if (c == Cfg::kPieces - 1) release();
-                    uint32_t first[16], second[16];  // X and its rest, or a symmetric piece
-                    if (g.kind == 2) {
-                        add_rest(v, ahead[c]);
-                    } else if (g.kind == 0) {
+                    if (t.rows > 0 && t.cols > 0 && t.row0 <= t.col0) {
+                        if (g.kind == 0) {
 #pragma unroll
-                        for (int i = 0; i < 32; ++i) v[i] *= down;
-                    } else {
+                            for (int i = 0; i < 32; ++i) v[i] *= down;
+                        } else {
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) {
-                            const float2 h = unpack2<f16>(ahead[c][i]);
-                            v[2 * i] = fmaf(kNsC, v[2 * i], kNsB * h.x);
-                            v[2 * i + 1] = fmaf(kNsC, v[2 * i + 1], kNsB * h.y);
+                            for (int i = 0; i < 16; ++i) {
+                                const float2 h = unpack2<f16>(ahead[c][i]);
+                                v[2 * i] = fmaf(kNsC, v[2 * i], kNsB * h.x);
+                                v[2 * i + 1] = fmaf(kNsC, v[2 * i + 1], kNsB * h.y);
+                            }
+                            if (t.row0 == t.col0) {
+#pragma unroll
+                                for (int i = 0; i < 32; ++i) v[i] += lane == i ? kNsA : 0.0f;
+                            }
                         }
-                        if (t.row0 == t.col0) {
+                        uint32_t r[16];
 #pragma unroll
-                            for (int i = 0; i < 32; ++i) v[i] += lane == i ? kNsA : 0.0f;
-                        }
+                        for (int i = 0; i < 16; ++i) r[i] = pack2<f16>(v[2 * i], v[2 * i + 1]);
+                        const uint32_t at = stage_at + (c & 1) * 4096;
+                        __syncwarp();
+                        stage_rows<32>(at, 0, r, lane);
+                        if (t.row0 < t.col0) stage_mirror(at + 2048, r, lane);
+                        __syncwarp();
+                        store_staged<32>(at, to + t.row0 * q.ldd + t.col0, q.ldd, t.rows, kPiece, lane);
+                        if (t.row0 < t.col0) store_staged<32>(at + 2048, to + t.col0 * (int64_t)q.ldd + t.row0, q.ldd, t.cols, kPiece, lane);
                     }
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) first[i] = pack2<f16>(v[2 * i], v[2 * i + 1]);
-                    const uint32_t buffer = piece & 1u, to = stage_at + buffer * Cfg::kBuffer;
-                    ok = ok && ptx::mbar_wait_bounded(free0 + 8 * buffer, (piece >> 1 & 1u) ^ 1u, abort_flag, p.wait_limit_ns);
-                    if (!__all_sync(0xffffffffu, ok)) break;
-                    muon_stage_rows(to, first, lane);
-                    if (g.kind == 2) {
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) {
-                            const float2 f = unpack2<f16>(first[i]);
-                            second[i] = pack2<f16>(v[2 * i] - f.x, v[2 * i + 1] - f.y);
-                        }
-                        muon_stage_rows(to + 2048, second, lane);
-                    } else if (t.row0 < t.col0) {
-                        muon_stage_mirror(to + 2048, first, lane);
-                    }
-                    ptx::fence_proxy_async();
-                    __syncwarp();
-                    if (lane == 0) ptx::mbar_arrive(staged0 + 8 * buffer);
                     t.col0 += kPiece;
                     t.cols -= kPiece;
                 }
             }
+            __syncwarp();
+            if (lane == 0) ptx::mbar_arrive(stored0 + 8 * ((taken - 1) % (kUnitLag + 1)));
             acc ^= 1u;
             if (acc == 0) acc_phase ^= 1u;
         }
-    } else {
-        // The stores: lane w those of the epilogue's warp w.  Of a symmetric product the pieces on and above the diagonal and, of
-        // the latter, the mirror images; the others are left to theirs.
-        const int w = lane & (kEpiWarps - 1), quarter = (w + 2) & 3, strip = w >> 2;
-        const uint32_t from = ptx::smem_u32(staging) + w * Cfg::kWarpStaging;
-        uint32_t piece = 0;
-        bool ok = true;
-        while (ok && __all_sync(0xffffffffu, next())) {
-            if (lane == 0) units_followed(followed, taken);
-            if (g.product + 1 == p.products) continue;  // the update: stored by the epilogue's warps, and nothing waits for it
-            const MuonMatrix q = p.matrices[g.matrix];
-            const CUtensorMap *maps = p.maps + (int64_t)g.matrix * kMuonMaps;
-            const CUtensorMap *map_first = maps + (g.kind == 0 ? kMapGramS : g.kind == 1 ? kMapPolyS : g.product / 3 & 1 ? kMapX0S : kMapX1S);
-            const CUtensorMap *map_second = g.kind == 2 ? maps + kMapRestS : map_first;
-            const int64_t m = g.kind == 2 ? q.rows : q.d, n = g.kind == 2 ? q.cols : q.d;
-            const int32_t row0 = g.tm * Cfg::kTileRows + (int)rank * kGemmM + quarter * 32;
-            int32_t col0 = g.tn * BN + strip * Cfg::kColsPerWarp;
-            ptx::tensormap_acquire(map_first);
-            ptx::tensormap_acquire(map_second);
-            for (int c = 0; c < Cfg::kPieces; ++c, ++piece, col0 += kPiece) {
-                const uint32_t buffer = piece & 1u;
-                ok = __all_sync(0xffffffffu, ptx::mbar_wait_bounded(staged0 + 8 * buffer, piece >> 1 & 1u, abort_flag, p.wait_limit_ns));
-                if (!ok) break;
-                if (lane < kEpiWarps && row0 < m && col0 < n && (g.kind == 2 || row0 <= col0)) {
-                    tile_store(map_first, col0, row0, from + buffer * Cfg::kBuffer);
-                    if (g.kind == 2)
-                        tile_store(map_second, col0, row0, from + buffer * Cfg::kBuffer + 2048);
-                    else if (row0 < col0)
-                        tile_store(map_second, row0, col0, from + buffer * Cfg::kBuffer + 2048);
+    } else if (warp == 2 + kEpiWarps + 1) {
+        if (lane == 0 && rank == 0) {
+            // The units are taken from the head of the list in turn.  Where there are plenty, each while the one before is being loaded;
+            // else not before that, so that none waits here which another worker could begin.
+            const uint32_t ring1 = CG == 2 ? map_to_rank(ring, 1) : 0;
+            while (p.stall != 1 || worker != 0) {
+                if (!units_wait(loaded, taken - p.early, abort_flag, p.wait_limit_ns)) break;
+                const int32_t u = atomicAdd(p.ticket, 1);
+                const int4 q = u < n_units ? p.units[u] : make_int4(kNoMoreUnits, 0, 0, 0);
+                if (q.x != kNoMoreUnits) {
+                    g = muon_unit(q);
+                    if (!eg_check(g.matrix < p.n_matrices && g.product < p.products, p.status, kCheckMuonUnit, g.matrix)) break;
+                    const int state = muon_wait(p.done + g.matrix, g.need, abort_flag, p.wait_limit_ns);
+                    if (state == 0) break;
+                    if (state < 0) continue;
                 }
-                tile_store_commit();
-                if (c + 1 < Cfg::kPieces) {
-                    if (c > 0) {
-                        tile_store_read<1>();
-                        __syncwarp();
-                        if (lane == 0) ptx::mbar_arrive(free0 + 8 * (buffer ^ 1u));
-                    }
-                } else {
-                    tile_store_read<0>();
-                    __syncwarp();
-                    if (lane == 0) {
-                        ptx::mbar_arrive(free0 + 8 * (buffer ^ 1u));
-                        ptx::mbar_arrive(free0 + 8 * buffer);
-                    }
-                }
+                unit_publish<CG>(ring, ring1, q, taken);
+                ++taken;
+                if (q.x == kNoMoreUnits) break;
             }
-            if (!ok) break;
-            // the tile is there for the loads of any SM
-            tile_store_done();
+        }
+        __syncwarp();
+    } else if (lane == 0) {
+        // When all of the epilogue's warps have stored their part of a tile, it is made known.
+        while (next()) {
+            units_raise(followed, taken);
+            const int32_t n = taken - 1;
+            if (!ptx::mbar_wait_bounded(stored0 + 8 * (n % (kUnitLag + 1)), (uint32_t)(n / (kUnitLag + 1)) & 1u, abort_flag, p.wait_limit_ns)) break;
+            if (g.product + 1 == p.products) continue;  // the update, for which nothing waits
             fence_proxy_async_all();
             __threadfence();
-            __syncwarp();
-            if (lane == 0) atomicAdd(p.done + g.matrix, 1);
+            atomicAdd(p.done + g.matrix, 1);
         }
-        tile_store_done();
     }
     ptx::tc_fence_before_sync();
     __syncthreads();

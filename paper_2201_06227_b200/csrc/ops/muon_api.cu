@@ -38,11 +38,12 @@ static void muon_tiles(int64_t m, int64_t n, bool symmetric, int tile_rows, int 
 struct MuonKind {
     int bn, cg;
 };
-// 256 x 256 tiles of a pair of CTAs where they go round all of them, else 128 x 128.
+// 256 x 256 tiles of a pair of CTAs where they go round all of them a few times, else 128 x 128: 54 convolutions of 16 to 64 channels (108
+// tiles of 256) 100 us with the small ones and 131 with the large, 12 matrices of 333 x 333 and 333 x 1332 203 and 263.
 static MuonKind muon_kind(int count, const egeria_muon_tensor *t) {
     int64_t tiles = 0;
     for (int i = 0; i < count; ++i) tiles += ((t[i].rows + 255) / 256) * ((t[i].cols + 255) / 256);
-    return tiles >= kSms / 2 ? MuonKind{256, 2} : MuonKind{128, 1};
+    return tiles >= 2 * kSms ? MuonKind{256, 2} : MuonKind{128, 1};
 }
 static bool muon_layout(int count, const egeria_muon_tensor *t, int steps, MuonLayout &L) {
     const MuonKind kind = muon_kind(count, t);
@@ -191,19 +192,16 @@ egeria_status egeria_muon_create(egeria_muon **out, int count, const egeria_muon
             q.pieces = (int32_t)((t.rows * t.cols + kMuonPiece - 1) / kMuonPiece);
             // (the gradient may move: the kernels look at its alignment)
             q.vector = t.cols % 8 == 0 && aligned(t.param, 8 * size_of(t.param_type)) && aligned(t.master, 32) && aligned(t.m, 32);
-            auto map = [&](int which, const uint16_t *p, int64_t rows, int64_t cols, int64_t ld, int box_rows, int box_cols = 64) {
+            auto map = [&](int which, const uint16_t *p, int64_t rows, int64_t cols, int64_t ld, int box_rows) {
                 cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)ld * 2};
-                cuuint32_t box[2] = {(cuuint32_t)box_cols, (cuuint32_t)box_rows}, one[2] = {1, 1};
+                cuuint32_t box[2] = {64, (cuuint32_t)box_rows}, one[2] = {1, 1};
                 return encode(&maps[(size_t)k * kMuonMaps + which], CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2, const_cast<uint16_t *>(p), dims, strides, box, one,
-                              CU_TENSOR_MAP_INTERLEAVE_NONE, box_cols == 64 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
-                              CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+                              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
             };
             bool ok = true;
             for (int s = 0; s < 2; ++s)
                 ok = ok && map(kMapX0 + 2 * s, q.x[s], q.rows, q.cols, q.ldx, 128) && map(kMapX0N + 2 * s, q.x[s], q.rows, q.cols, q.ldx, 64);
-            ok = ok && map(kMapX0S, q.x[0], q.rows, q.cols, q.ldx, 32, 32) && map(kMapX1S, q.x[1], q.rows, q.cols, q.ldx, 32, 32) &&
-                 map(kMapRestS, q.lo, q.rows, q.cols, q.ldx, 32, 32) && map(kMapGramS, q.gram, q.d, q.d, q.ldd, 32, 32) &&
-                 map(kMapPolyS, q.poly, q.d, q.d, q.ldd, 32, 32);
             ok = ok && map(kMapGram, q.gram, q.d, q.d, q.ldd, 128) && map(kMapPoly, q.poly, q.d, q.d, q.ldd, 128);
             if (!ok) {
                 delete h;
@@ -250,6 +248,7 @@ egeria_status egeria_muon_create(egeria_muon **out, int count, const egeria_muon
         p.n_pieces = (int32_t)pieces.size();
         p.n_matrices = (int32_t)matrices.size();
         p.products = 3 * steps;
+        p.early = p.n_units >= 3 * steps * 4 * workers;
         h->workers = (int)std::min<int64_t>(workers, p.n_units);
         auto put = [&](size_t at, const void *from, size_t bytes) { return bytes ? cudaMemcpy(ws + at, from, bytes, cudaMemcpyHostToDevice) : cudaSuccess; };
         // (first what was enqueued before: it may still write to this memory, and the copies would not wait for it)

@@ -193,6 +193,19 @@ static cudaError_t launch_few_any(const Epilogue &e, const egeria_gated_forward_
     return launch_few<T, 4>(e, a, wide, sms, stream);
 }
 
+template <typename T, int ROWS>
+static cudaError_t launch_down(const Epilogue &e, const egeria_gated_forward_args &a, const T *h, int64_t ldh, bool wide, cudaStream_t stream) {
+    const unsigned grid = (unsigned)((a.out + 8 / kDownWarps - 1) / (8 / kDownWarps));
+    return launch(wide ? gated_down_few_kernel<T, ROWS, true> : gated_down_few_kernel<T, ROWS, false>, dim3(grid), 256, 0, stream, 1, e, (int32_t)a.rows,
+                  (int32_t)a.out, h, ldh, static_cast<const T *>(a.w_down), a.ldw_down, (int32_t)a.hidden);
+}
+template <typename T>
+static cudaError_t launch_down_any(const Epilogue &e, const egeria_gated_forward_args &a, const void *h, int64_t ldh, bool wide, cudaStream_t stream) {
+    if (a.rows <= 1) return launch_down<T, 1>(e, a, static_cast<const T *>(h), ldh, wide, stream);
+    if (a.rows <= 2) return launch_down<T, 2>(e, a, static_cast<const T *>(h), ldh, wide, stream);
+    return launch_down<T, 4>(e, a, static_cast<const T *>(h), ldh, wide, stream);
+}
+
 // Whether any of the written matrices shares a value with another or with one that is read.
 template <int W, int R>
 static bool any_overlap(const Extent (&written)[W], const Extent (&read)[R]) {
@@ -262,6 +275,15 @@ egeria_status egeria_gated_forward(egeria_ops *ops, void *cuda_stream, const ege
         const bool wide = a.inp % 8 == 0 && a.ldw_gate % 8 == 0 && a.ldw_up % 8 == 0 && aligned(a.w_gate, 16) && aligned(a.w_up, 16);
         EGO_CUDA(a.type == EGERIA_BF16 ? launch_few_any<bf16>(e, a, wide, ops->sms, stream) : launch_few_any<f16>(e, a, wide, ops->sms, stream));
         ++ops->launches;
+        Epilogue d{};
+        d.bias = a.b_down;
+        d.extra = a.residual, d.ldx = a.ldr;
+        d.out = a.y, d.ldo = a.ldy;
+        const bool wide_down = a.hidden % 8 == 0 && a.ldw_down % 8 == 0 && aligned(a.w_down, 16);
+        EGO_CUDA(a.type == EGERIA_BF16 ? launch_down_any<bf16>(d, a, e.out, e.ldo, wide_down, stream)
+                                       : launch_down_any<f16>(d, a, e.out, e.ldo, wide_down, stream));
+        ++ops->launches;
+        return EGERIA_OK;
     } else {
         PrepareParams prep{};
         prep.status = reinterpret_cast<int32_t *>(ops->ws);

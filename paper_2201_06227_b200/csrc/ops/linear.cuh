@@ -726,9 +726,12 @@ __global__ void __launch_bounds__(GemmCfg<BN, CG, MB>::kThreads, 1) gemm_kernel(
     if (CG == 2) cluster_sync();
     ptx::tc_fence_after_sync();
     const uint32_t tmem = *tmem_holder;
-    // Up to here nothing depends on the kernel before this one, which may still be running; from here on everything does.
-    ptx::grid_dependency_wait();
-    ptx::grid_launch_dependents();
+    // Up to here nothing depends on the kernel before this one, which may still be running, nor does a role's first unit; from its
+    // `arrived` on everything does.
+    auto arrived = [] {
+        ptx::grid_dependency_wait();
+        ptx::grid_launch_dependents();
+    };
 
     if (warp == 0) {
         if (lane == 0) {
@@ -741,6 +744,7 @@ __global__ void __launch_bounds__(GemmCfg<BN, CG, MB>::kThreads, 1) gemm_kernel(
                 if (u < 0) break;
                 const GemmUnit g = gemm_unit<kProblems>(p, u);
                 const GemmProblem &q = p.problem[g.problem];
+                if (step == 0) arrived();
                 if (!eg_check(gemm_unit_fits(q, g), p.status, kCheckGemmUnit, u)) break;
                 const CUtensorMap *map_a = &q.a, *map_b = &q.b;
                 const bool a_mn = q.a_mn, b_mn = q.b_mn;
@@ -879,6 +883,9 @@ __global__ void __launch_bounds__(GemmCfg<BN, CG, MB>::kThreads, 1) gemm_kernel(
         const int e = warp - 2, quarter = warp & 3, strip = e >> 2;
         uint32_t acc = 0, acc_phase = 0;
         const uint32_t release0 = CG == 2 ? map_to_rank(accempty0, 0) : accempty0;
+        int u = gemm_next(p, worker, workers, 0);
+        GemmUnit g = gemm_unit<kProblems>(p, u);
+        arrived();
         if (MODE == kModeLinear || MODE == kModeStore) {
 #pragma unroll 1
             for (int i = 0; i < (MODE == kModeLinear ? 1 : kMaxSums); ++i)
@@ -900,13 +907,10 @@ __global__ void __launch_bounds__(GemmCfg<BN, CG, MB>::kThreads, 1) gemm_kernel(
                     ptx::mbar_arrive(release0 + 8 * acc);
             }
         };
-        for (int step = 0;; ++step) {
-            const int u = gemm_next(p, worker, workers, step);
-            if (u < 0) break;
-            const GemmUnit g = gemm_unit<kProblems>(p, u);
+        for (int step = 0; u >= 0;) {
             if (!eg_check(gemm_unit_fits(p.problem[g.problem], g), p.status, kCheckGemmUnit, u)) break;
             // (each product with its own copy of this code: what it takes from the parameters is then at fixed places)
-            auto tile = [&](const GemmProblem &q, int half) {
+            auto tile = [&](const GemmProblem &q, int half) __attribute__((always_inline)) {
                 t.wide = q.epi.wide;
                 t.row0 = (int64_t)g.tm * Cfg::kTileRows + (half * CG + (int)rank) * kGemmM + quarter * 32;
                 t.rows = (int)min((int64_t)q.m - t.row0, (int64_t)1 << 20);
@@ -972,10 +976,27 @@ __global__ void __launch_bounds__(GemmCfg<BN, CG, MB>::kThreads, 1) gemm_kernel(
                             float v[32];
 #pragma unroll
                             for (int i = 0; i < 32; ++i) v[i] = 0.0f;
-                            for (int s = 0; s < q.splits; ++s) {
+                            // (two of them on their way at a time)
+                            const float *at = first + (c * 8 * 32 + lane) * 4;
+                            int s = 0;
+#pragma unroll 1
+                            for (; s + 1 < q.splits; s += 2, at += 2 * pitch) {
+                                float4 f[8], h[8];
+#pragma unroll
+                                for (int j = 0; j < 8; ++j) f[j] = __ldcg(reinterpret_cast<const float4 *>(at + j * 128));
+#pragma unroll
+                                for (int j = 0; j < 8; ++j) h[j] = __ldcg(reinterpret_cast<const float4 *>(at + pitch + j * 128));
+#pragma unroll
+                                for (int j = 0; j < 8; ++j)
+                                    v[4 * j] += f[j].x, v[4 * j + 1] += f[j].y, v[4 * j + 2] += f[j].z, v[4 * j + 3] += f[j].w;
+#pragma unroll
+                                for (int j = 0; j < 8; ++j)
+                                    v[4 * j] += h[j].x, v[4 * j + 1] += h[j].y, v[4 * j + 2] += h[j].z, v[4 * j + 3] += h[j].w;
+                            }
+                            if (s < q.splits) {
 #pragma unroll
                                 for (int j = 0; j < 8; ++j) {
-                                    const float4 f = __ldcg(reinterpret_cast<const float4 *>(first + s * pitch + ((c * 8 + j) * 32 + lane) * 4));
+                                    const float4 f = __ldcg(reinterpret_cast<const float4 *>(at + j * 128));
                                     v[4 * j] += f.x, v[4 * j + 1] += f.y, v[4 * j + 2] += f.z, v[4 * j + 3] += f.w;
                                 }
                             }
@@ -999,6 +1020,8 @@ __global__ void __launch_bounds__(GemmCfg<BN, CG, MB>::kThreads, 1) gemm_kernel(
                 if (acc == 0) acc_phase ^= 1u;
             }
             if (!ok) break;
+            u = gemm_next(p, worker, workers, ++step);
+            g = gemm_unit<kProblems>(p, u);
         }
     }
     ptx::tc_fence_before_sync();
@@ -1159,6 +1182,81 @@ __global__ void __launch_bounds__(256) gated_few_kernel(const Epilogue p, int32_
             static_cast<T *>(p.out)[lane * p.ldo + n] = from_f32<T>(vg[0] * vu);
         }
     }
+}
+
+// The second product of a gated block for 1 to 4 rows: w_down's columns are long and few (1024 of 2816), so four warps share one, and
+// what a lane takes of it first is fetched before the hidden values are there: the kernel before this one is the block's first
+// (which writes no weights, and which began when all before it had ended).  1 x 1024 -> 2816 -> 1024: 7.1 us for both, 11.3 with
+// the linear layers' kernel for this one.
+constexpr int kDownWarps = 4;  // warps of a column
+template <typename T, int ROWS, bool WIDE>
+__global__ void __launch_bounds__(256) gated_down_few_kernel(const Epilogue p, int32_t m, int32_t n_cols, const T *h, int64_t ldh, const T *w, int64_t ldw,
+                                                             int32_t k) {
+    __shared__ float part[8][ROWS];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int group = warp / kDownWarps, share = warp % kDownWarps;
+    const int32_t n = blockIdx.x * (8 / kDownWarps) + group;
+    const int rows = min(ROWS, m);
+    const bool mine = n < n_cols;
+    const T *wr = w + (int64_t)(mine ? n : 0) * ldw;
+    float acc[ROWS];
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) acc[r] = 0.0f;
+    if (WIDE) {
+        constexpr int kAhead = 4;
+        Raw8<T> ahead[kAhead];
+        const int first = (share * 32 + lane) * 8, step = kDownWarps * 256;
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i)
+            if (first + i * step < k) load8(ahead[i], wr + first + i * step);
+        ptx::grid_dependency_wait();
+        ptx::grid_launch_dependents();
+        auto add = [&](const Raw8<T> &q, int c) {
+            float wv[8], hv[8];
+            unpack8(wv, q);
+#pragma unroll
+            for (int r = 0; r < ROWS; ++r) {
+                if (r >= rows) break;
+                Raw8<T> s;
+                load8(s, h + r * ldh + c);
+                unpack8(hv, s);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) acc[r] = fmaf(wv[i], hv[i], acc[r]);
+            }
+        };
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i)
+            if (first + i * step < k) add(ahead[i], first + i * step);
+#pragma unroll 4
+        for (int c = first + kAhead * step; c < k; c += step) {
+            Raw8<T> q;
+            load8(q, wr + c);
+            add(q, c);
+        }
+    } else {
+        ptx::grid_dependency_wait();
+        ptx::grid_launch_dependents();
+#pragma unroll 4
+        for (int c = share * 32 + lane; c < k; c += kDownWarps * 32) {
+            const float wv = to_f32(wr[c]);
+#pragma unroll
+            for (int r = 0; r < ROWS; ++r)
+                if (r < rows) acc[r] = fmaf(wv, to_f32(h[r * ldh + c]), acc[r]);
+        }
+    }
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) {
+        acc[r] = warp_sum(acc[r]);
+        if (lane == 0) part[warp][r] = acc[r];
+    }
+    __syncthreads();
+    if (share != 0 || !mine || lane >= rows) return;
+    float v = 0.0f;
+#pragma unroll
+    for (int i = 0; i < kDownWarps; ++i) v += part[warp + i][lane];
+    if (p.bias) v += to_f32(static_cast<const T *>(p.bias)[n]);
+    if (p.extra) v += to_f32(static_cast<const T *>(p.extra)[lane * p.ldx + n]);
+    static_cast<T *>(p.out)[lane * p.ldo + n] = from_f32<T>(v);
 }
 
 // ---------------------------------------------------------------- before the products

@@ -74,6 +74,7 @@ static cudaError_t allow_all() {
     if (e == cudaSuccess) e = allow_smem<T, 256, 1, 1, kModeLinear>();
     if (e == cudaSuccess) e = allow_smem<T, 128, 2, 1, kModeLinear>();
     if (e == cudaSuccess) e = allow_smem<T, 256, 2, 1, kModeLinear>();
+    if (e == cudaSuccess) e = allow_smem<T, 256, 2, 2, kModeLinear>();
     if (e == cudaSuccess) e = allow_few<T, 1>();
     if (e == cudaSuccess) e = allow_few<T, 2>();
     if (e == cudaSuccess) e = allow_few<T, 4>();
@@ -81,7 +82,8 @@ static cudaError_t allow_all() {
 }
 
 template <typename T>
-static cudaError_t launch_gemm_any(int bn, int cg, const GemmParams &p, int ctas, cudaStream_t stream) {
+static cudaError_t launch_gemm_any(int bn, int cg, int mb, const GemmParams &p, int ctas, cudaStream_t stream) {
+    if (mb == 2) return launch_gemm<T, 256, 2, 2, kModeLinear>(p, ctas, stream);
     if (cg == 2) return bn == 128 ? launch_gemm<T, 128, 2, 1, kModeLinear>(p, ctas, stream) : launch_gemm<T, 256, 2, 1, kModeLinear>(p, ctas, stream);
     if (bn == 64) return launch_gemm<T, 64, 1, 1, kModeLinear>(p, ctas, stream);
     return bn == 128 ? launch_gemm<T, 128, 1, 1, kModeLinear>(p, ctas, stream) : launch_gemm<T, 256, 1, 1, kModeLinear>(p, ctas, stream);
@@ -104,13 +106,22 @@ egeria_status run_products(egeria_ops *o, cudaStream_t stream, int type, Product
             for (int j = 0; j < count; ++j) plan[j] = g[j];
         }
     }
+    // Tiles of 512 rows take a quarter less from L2, but nothing hides their epilogue: for long sums with a light one, where they
+    // need no more rounds.  16384 x 2816 -> 1024 with a residual 85 us instead of 92, 8192 x 8192 -> 8192 752 instead of 949; but
+    // 8192 x 2048 -> 2048 93 instead of 86, 16384 x 1024 -> 4096 with activation and z 191 instead of 159.
+    if (count == 1 && plan[0].cg == 2 && plan[0].bn == 256 && plan[0].splits == 1 && jobs[0].k >= 40 * kGemmK && !jobs[0].epi.act && !jobs[0].epi.z &&
+        !jobs[0].epi.slope) {
+        const int64_t workers = o->sms / 2, tall = (jobs[0].m + 511) / 512;
+        auto rounds = [&](int64_t tiles) { return (tiles + workers - 1) / workers; };
+        if (2 * rounds(tall * plan[0].tiles_n) <= rounds((int64_t)plan[0].tiles_m * plan[0].tiles_n)) plan[0].mb = 2, plan[0].tiles_m = (int)tall;
+    }
     GemmParams p;
     int ctas = 0;
     const egeria_status s = fill_products(o, type, kModeLinear, jobs, plan, count, p, ctas);
     if (s != EGERIA_OK) return s;
     p.sums[0] = sums;
-    const int bn = plan[0].bn, cg = plan[0].cg;
-    EGO_CUDA(type == EGERIA_BF16 ? launch_gemm_any<bf16>(bn, cg, p, ctas, stream) : launch_gemm_any<f16>(bn, cg, p, ctas, stream));
+    const int bn = plan[0].bn, cg = plan[0].cg, mb = plan[0].mb;
+    EGO_CUDA(type == EGERIA_BF16 ? launch_gemm_any<bf16>(bn, cg, mb, p, ctas, stream) : launch_gemm_any<f16>(bn, cg, mb, p, ctas, stream));
     ++o->launches;
     return EGERIA_OK;
 }

@@ -292,6 +292,9 @@ egeria_status egeria_gated_forward(egeria_ops *ops, void *cuda_stream, const ege
         make_loadable(ops, job.a, L.x, prep.pack[0]);
         make_loadable(ops, job.b, L.w_gate, prep.pack[1]);
         make_loadable(ops, job.b2, L.w_up, prep.pack[2]);
+        Operand w_down{a.w_down, a.ldw_down, a.out, a.hidden, false};  // of the second product: in the same launch
+        make_loadable(ops, w_down, L.w_down, prep.pack[3]);
+        down.w = w_down.p, down.ldw = w_down.ld;
         if ((s = run_prepare(ops, stream, a.type, prep, false)) != EGERIA_OK) return s;
         const GemmPlan g = plan_single(a.rows, 2 * a.hidden, a.inp, ops->sms, a.g ? 20.0 : 12.0);
         GemmParams p;

@@ -58,6 +58,7 @@ struct MuonParams {
     const uint8_t *frozen;
     float lr, beta, rest, eps;
     int32_t nesterov, n_units, n_pieces, n_matrices, products;
+    int32_t first_small;             // from here on matrices go through muon_small_kernel
     int32_t early;                   // units are taken while the one before is loaded
     uint32_t stall;
     uint64_t wait_limit_ns;
@@ -74,38 +75,29 @@ __device__ __forceinline__ bool muon_vector(const MuonParams &p, const MuonMatri
     const uintptr_t grad = reinterpret_cast<uintptr_t>(p.grads[t.index]);
     return t.vector && grad % (t.grad_type == EGERIA_F32 ? 32 : 16) == 0;
 }
-// Eight gradients from value e of a matrix on; those behind n count as 0.
-template <bool VECTOR>
-__device__ __forceinline__ void muon_grads(float (&g)[8], const void *grad, int type, int64_t e, int64_t n) {
-    auto go = [&](auto *p) {
-        using T = typename std::remove_const<typename std::remove_reference<decltype(*p)>::type>::type;
-        if (VECTOR) {
-            Raw8<T> r;
-            load8(r, p + e);
-            unpack8(g, r);
-        } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) g[i] = e + i < n ? to_f32(p[e + i]) : 0.0f;
-        }
-    };
-    if (type == EGERIA_F32)
-        go(static_cast<const float *>(grad));
-    else if (type == EGERIA_BF16)
-        go(static_cast<const bf16 *>(grad));
-    else
-        go(static_cast<const f16 *>(grad));
-}
-template <bool VECTOR>
-__device__ __forceinline__ void muon_moments(float (&m)[8], const float *p, int64_t e, int64_t n) {
+// Eight gradients (or moments) of a matrix: consecutive ones from value e on, or, where its rows are not whole eights or not aligned,
+// kMuonThreads apart; those behind `end` count as 0.
+template <bool VECTOR, int STRIDE = kMuonThreads, typename T>
+__device__ __forceinline__ void muon_read(float (&v)[8], const T *p, int64_t e, int64_t end) {
     if (VECTOR) {
-        Raw8<float> r;
+        Raw8<T> r;
         load8(r, p + e);
-        unpack8(m, r);
+        unpack8(v, r);
     } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) m[i] = e + i < n ? p[e + i] : 0.0f;
+        for (int i = 0; i < 8; ++i) v[i] = e + i * STRIDE < end ? to_f32(p[e + i * STRIDE]) : 0.0f;
     }
 }
+template <bool VECTOR, int STRIDE = kMuonThreads>
+__device__ __forceinline__ void muon_grads(float (&g)[8], const void *grad, int type, int64_t e, int64_t end) {
+    if (type == EGERIA_F32)
+        muon_read<VECTOR, STRIDE>(g, static_cast<const float *>(grad), e, end);
+    else if (type == EGERIA_BF16)
+        muon_read<VECTOR, STRIDE>(g, static_cast<const bf16 *>(grad), e, end);
+    else
+        muon_read<VECTOR, STRIDE>(g, static_cast<const f16 *>(grad), e, end);
+}
+template <int THREADS = kMuonThreads>
 __device__ __forceinline__ double block_sum(double v, double *part) {
 #pragma unroll
     for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
@@ -113,7 +105,7 @@ __device__ __forceinline__ double block_sum(double v, double *part) {
     __syncthreads();
     v = 0.0;
 #pragma unroll
-    for (int w = 0; w < kMuonThreads / 32; ++w) v += part[w];
+    for (int w = 0; w < THREADS / 32; ++w) v += part[w];
     return v;
 }
 
@@ -123,10 +115,10 @@ __device__ __forceinline__ double muon_momentum_piece(const MuonParams &p, const
     const int64_t n = t.rows * t.cols, end = min(n, e0 + kMuonPiece);
     const void *grad = p.grads[t.index];
     double sum = 0.0;
-    for (int64_t e = e0 + threadIdx.x * 8; e < end; e += kMuonThreads * 8) {
+    for (int64_t e = e0 + threadIdx.x * (VECTOR ? 8 : 1); e < end; e += kMuonThreads * 8) {
         float g[8], m[8];
-        muon_grads<VECTOR>(g, grad, t.grad_type, e, n);
-        muon_moments<VECTOR>(m, t.m, e, n);
+        muon_grads<VECTOR>(g, grad, t.grad_type, e, end);
+        muon_read<VECTOR>(m, t.m, e, end);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             g[i] *= scale;
@@ -139,7 +131,7 @@ __device__ __forceinline__ double muon_momentum_piece(const MuonParams &p, const
         } else {
 #pragma unroll
             for (int i = 0; i < 8; ++i)
-                if (e + i < n) t.m[e + i] = m[i];
+                if (e + i * kMuonThreads < end) t.m[e + i * kMuonThreads] = m[i];
         }
     }
     return sum;
@@ -174,17 +166,18 @@ __device__ __forceinline__ void muon_normalize_piece(const MuonParams &p, const 
     const void *grad = p.grads[t.index];
     const int64_t r0 = e0 / t.cols;
     const uint32_t c0 = (uint32_t)(e0 - r0 * t.cols), cols = (uint32_t)t.cols;
-    for (int64_t e = e0 + threadIdx.x * 8; e < end; e += kMuonThreads * 8) {
+    for (int64_t e = e0 + threadIdx.x * (VECTOR ? 8 : 1); e < end; e += kMuonThreads * 8) {
         float g[8], v[8];
-        muon_moments<VECTOR>(v, t.m, e, n);
+        muon_read<VECTOR>(v, t.m, e, end);
         if (p.nesterov) {
-            muon_grads<VECTOR>(g, grad, t.grad_type, e, n);
+            muon_grads<VECTOR>(g, grad, t.grad_type, e, end);
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[i] = fmaf(p.beta, v[i], p.rest * (g[i] * scale));
         }
-        uint32_t at = c0 + (uint32_t)(e - e0), row = at / cols, col = at - row * cols;
-        uint16_t *x = t.x[0] + (r0 + row) * t.ldx + col, *lo = t.lo + (r0 + row) * t.ldx + col;
+        const uint32_t at = c0 + (uint32_t)(e - e0);
         if (VECTOR) {  // whole eights of a row
+            const uint32_t row = at / cols, col = at - row * cols;
+            uint16_t *x = t.x[0] + (r0 + row) * t.ldx + col, *lo = t.lo + (r0 + row) * t.ldx + col;
             uint32_t h[4], l[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
@@ -199,16 +192,12 @@ __device__ __forceinline__ void muon_normalize_piece(const MuonParams &p, const 
         } else {
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                if (e + i >= n) break;
+                if (e + i * kMuonThreads >= end) break;
+                const uint32_t to = at + i * kMuonThreads, row = to / cols, col = to - row * cols;
                 f16 h, l;
                 muon_split(v[i] * inv, h, l);
-                *x++ = __half_as_ushort(h);
-                *lo++ = __half_as_ushort(l);
-                if (++col == cols) {
-                    col = 0;
-                    x += t.ldx - cols;
-                    lo += t.ldx - cols;
-                }
+                t.x[0][(r0 + row) * t.ldx + col] = __half_as_ushort(h);
+                t.lo[(r0 + row) * t.ldx + col] = __half_as_ushort(l);
             }
         }
     }
@@ -355,16 +344,22 @@ __device__ __forceinline__ void muon_update_wide(const MuonMatrix &q, const uint
         if (q.master) Four<float>::write(q.master + to, v);
     }
 }
-// The same value by value, where rows are not whole eights or not aligned.
+// The same value by value, where rows are not whole eights or not aligned: lane = column, eight rows on their way at a time.
 template <typename T>
-__device__ __forceinline__ void muon_update_narrow(const MuonMatrix &q, const float *stage, float keep, float step, const Tile &t) {
-    if (t.lane >= t.cols) return;
-    T *param = static_cast<T *>(q.param);
-    for (int row = 0; row < t.rows; ++row) {
-        const int64_t at = (t.row0 + row) * q.cols + t.col0 + t.lane;
-        const float v = fmaf(q.master ? q.master[at] : to_f32(param[at]), keep, -step * stage[row * kUpdatePitch + t.lane]);
-        param[at] = from_f32<T>(v);
-        if (q.master) q.master[at] = v;
+__device__ __forceinline__ void muon_update_narrow(T *param, float *master, int64_t cols, const float *stage, float keep, float step, int rows) {
+#pragma unroll 1
+    for (int row = 0; row < rows; row += 8) {
+        float w[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (row + i < rows) w[i] = master ? master[(row + i) * cols] : to_f32(param[(row + i) * cols]);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            if (row + i >= rows) break;
+            const float v = fmaf(w[i], keep, -step * stage[(row + i) * kUpdatePitch]);
+            param[(row + i) * cols] = from_f32<T>(v);
+            if (master) master[(row + i) * cols] = v;
+        }
     }
 }
 template <typename F>
@@ -496,7 +491,9 @@ __device__ __forceinline__ bool unit_next(MuonUnit &g, uint32_t ring, int32_t n,
     return true;
 }
 
-template <int BN, int CG>
+// NARROW: some matrix's rows are not whole eights or not aligned (without that code the other matrices' takes fewer registers: 24 blocks of
+// width 1024 5.00 instead of 5.17 ms).
+template <int BN, int CG, bool NARROW>
 __global__ void __launch_bounds__(MuonCfg<BN, CG>::kThreads, 1) muon_products_kernel(const __grid_constant__ MuonParams p) {
     using Cfg = MuonCfg<BN, CG>;
     extern __shared__ uint8_t smem_raw[];
@@ -673,7 +670,7 @@ __global__ void __launch_bounds__(MuonCfg<BN, CG>::kThreads, 1) muon_products_ke
             auto fetch_update = [&] {
                 if (t.rows <= 0 || t.cols <= 0) return;
                 muon_fetch(ahead[0], q.lo, q.ldx, t);
-                if (q.vector) with_type(q.param_type, [&](auto type) { muon_weights<decltype(type)>(weights, q, t); });
+                if (!NARROW || q.vector) with_type(q.param_type, [&](auto type) { muon_weights<decltype(type)>(weights, q, t); });
             };
             if (update) {
                 fetch_update();
@@ -726,10 +723,11 @@ __global__ void __launch_bounds__(MuonCfg<BN, CG>::kThreads, 1) muon_products_ke
                             for (int i = 0; i < 8; ++i)
                                 *reinterpret_cast<float4 *>(stage + lane * kUpdatePitch + 4 * i) = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
                             __syncwarp();
-                            if (q.vector)
+                            if (!NARROW || q.vector)
                                 muon_update_wide<P>(q, weights, stage, keep, by, t);
-                            else
-                                muon_update_narrow<P>(q, stage, keep, by, t);
+                            else if (lane < t.cols)
+                                muon_update_narrow<P>(static_cast<P *>(q.param) + t.row0 * q.cols + t.col0 + lane,
+                                                      q.master ? q.master + t.row0 * q.cols + t.col0 + lane : nullptr, q.cols, stage + lane, keep, by, t.rows);
                         }
                         t.col0 += kPiece;
                         t.cols -= kPiece;
@@ -866,6 +864,342 @@ __global__ void __launch_bounds__(MuonCfg<BN, CG>::kThreads, 1) muon_products_ke
     if (CG == 2) cluster_sync();
     ptx::tc_fence_after_sync();
     if (warp == 1) tmem_free_g<CG>(tmem, Cfg::kTmemCols);
+}
+
+// ---------------------------------------------------------------- small matrices
+// The whole step of a matrix of at most 128 by 768 in one thread block: X stays in shared memory, as the products' operand from either
+// side (its 64-column panels are A X^T's with the columns consecutive and P X's with them as the other axis), and only what its
+// rounding leaves goes by way of L2.  54 convolutions of 16 to 64 channels: 63 us, 100 through the list of units, where each of the 15
+// products waits for the one before it to be stored, seen and loaded.
+constexpr int kSmallSide = 128, kSmallPanels = 12;
+constexpr int kSmallThreads = 512, kSmallStrips = kSmallThreads / 128, kPanelBytes = kSmallSide * 128;
+constexpr int kSmallSmem = 1024 + (kSmallPanels + 2) * kPanelBytes + 256;
+static_assert(kSmallSmem <= 227 * 1024, "shared memory of a CTA");
+
+// Place of a value in a panel: rows of 64 values, 128 bytes, swizzled as the tensor cores take them.
+__device__ __forceinline__ uint32_t panel_place(uint32_t row, uint32_t col) {
+    return (col >> 6) * kPanelBytes + row * 128 + (((col >> 3 & 7) ^ (row & 7)) << 4) + (col & 7) * 2;
+}
+// Place of a value of X's rest in the workspace: eights of columns, a row per lane.
+__device__ __forceinline__ int32_t rest_place(int32_t row, int32_t col) { return ((col >> 3) * kSmallSide + row) * 8 + (col & 7); }
+// 32 values of a row from a multiple of 32 columns on.
+__device__ __forceinline__ void panel_store(uint32_t base, uint32_t row, uint32_t col, const uint32_t (&r)[16]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(base + panel_place(row, col + 8 * i)), "r"(r[4 * i]), "r"(r[4 * i + 1]),
+                     "r"(r[4 * i + 2]), "r"(r[4 * i + 3])
+                     : "memory");
+}
+
+// Momentum, |t|, and X in the panels with its rest in `lo`.
+template <bool VECTOR>
+__device__ __forceinline__ void small_begin(const MuonParams &p, const MuonMatrix &t, const void *grad, float grad_scale, uint32_t base, double *part) {
+    constexpr int S = VECTOR ? 1 : kSmallThreads;  // between a thread's eight values
+    const int32_t cols = (int32_t)t.cols, n = (int32_t)(t.rows * t.cols), first = threadIdx.x * (VECTOR ? 8 : 1);
+    double sum = 0.0;
+#pragma unroll 2
+    for (int32_t e = first; e < n; e += 8 * kSmallThreads) {
+        float g[8], m[8];
+        muon_grads<VECTOR, S>(g, grad, t.grad_type, e, n);
+        muon_read<VECTOR, S>(m, t.m, e, n);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            g[i] *= grad_scale;
+            m[i] = fmaf(p.beta, m[i], p.rest * g[i]);
+            const float v = p.nesterov ? fmaf(p.beta, m[i], p.rest * g[i]) : m[i];
+            if (VECTOR || e + i * S < n) sum = fma((double)v, (double)v, sum);
+        }
+        if (VECTOR) {
+            store8(t.m + e, m);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (e + i * S < n) t.m[e + i * S] = m[i];
+        }
+    }
+    const float inv = (float)((double)t.up / fmax(sqrt(block_sum<kSmallThreads>(sum, part)), (double)p.eps));
+#pragma unroll 2
+    for (int32_t e = first; e < n; e += 8 * kSmallThreads) {  // (its own values of m again)
+        float g[8], v[8];
+        muon_read<VECTOR, S>(v, t.m, e, n);
+        if (p.nesterov) {
+            muon_grads<VECTOR, S>(g, grad, t.grad_type, e, n);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = fmaf(p.beta, v[i], p.rest * (g[i] * grad_scale));
+        }
+        uint32_t h[4], l[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            h[i] = pack2<f16>(v[2 * i] * inv, v[2 * i + 1] * inv);
+            const float2 f = unpack2<f16>(h[i]);
+            l[i] = pack2<f16>(v[2 * i] * inv - f.x, v[2 * i + 1] * inv - f.y);
+        }
+        const int32_t r = e / cols, c = e - r * cols;
+        if (VECTOR && !t.tall) {  // eight values of a row, which is one of X
+            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(base + panel_place(r, c)), "r"(h[0]), "r"(h[1]), "r"(h[2]), "r"(h[3]) : "memory");
+            *reinterpret_cast<uint4 *>(t.lo + rest_place(r, c)) = make_uint4(l[0], l[1], l[2], l[3]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int32_t at = e + i * S;
+                if (at >= n) break;
+                const int32_t ri = VECTOR ? r : at / cols, ci = VECTOR ? c + i : at - ri * cols, row = t.tall ? ci : ri, col = t.tall ? ri : ci;
+                const uint16_t hi = (uint16_t)(h[i >> 1] >> (i & 1) * 16), lo = (uint16_t)(l[i >> 1] >> (i & 1) * 16);
+                asm volatile("st.shared.b16 [%0], %1;" ::"r"(base + panel_place(row, col)), "h"(hi) : "memory");
+                t.lo[rest_place(row, col)] = lo;
+            }
+        }
+    }
+}
+
+// p = p keep - step X, in the order of the weights.
+template <typename T, bool VECTOR>
+__device__ __forceinline__ void small_end(const MuonParams &p, const MuonMatrix &t, uint32_t base) {
+    constexpr int S = VECTOR ? 1 : kSmallThreads;
+    const int32_t cols = (int32_t)t.cols, n = (int32_t)(t.rows * t.cols);
+    const float keep = 1.0f - p.lr * t.wd, by = p.lr * t.scale * t.down;
+    T *param = static_cast<T *>(t.param);
+    for (int32_t e = threadIdx.x * (VECTOR ? 8 : 1); e < n; e += 8 * kSmallThreads) {
+        float w[8], x[8];
+        if (t.master)
+            muon_read<VECTOR, S>(w, t.master, e, n);
+        else
+            muon_read<VECTOR, S>(w, param, e, n);
+        const int32_t r = e / cols, c = e - r * cols;
+        if (VECTOR && !t.tall) {
+            uint32_t h[4];
+            asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(h[0]), "=r"(h[1]), "=r"(h[2]), "=r"(h[3]) : "r"(base + panel_place(r, c)) : "memory");
+            const uint4 q = *reinterpret_cast<const uint4 *>(t.lo + rest_place(r, c));
+            const uint32_t l[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float2 f = unpack2<f16>(h[i]), g = unpack2<f16>(l[i]);
+                x[2 * i] = f.x + g.x, x[2 * i + 1] = f.y + g.y;
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int32_t at = min(e + i * S, n - 1);
+                const int32_t ri = VECTOR ? r : at / cols, ci = VECTOR ? c + i : at - ri * cols, row = t.tall ? ci : ri, col = t.tall ? ri : ci;
+                uint16_t h;
+                asm volatile("ld.shared.b16 %0, [%1];" : "=h"(h) : "r"(base + panel_place(row, col)) : "memory");
+                x[i] = __half2float(__ushort_as_half(h)) + __half2float(__ushort_as_half(t.lo[rest_place(row, col)]));
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) w[i] = fmaf(w[i], keep, -by * x[i]);
+        if (VECTOR) {
+            store8(param + e, w);
+            if (t.master) store8(t.master + e, w);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (e + i * S < n) {
+                    param[e + i * S] = from_f32<T>(w[i]);
+                    if (t.master) t.master[e + i * S] = w[i];
+                }
+        }
+    }
+}
+
+__global__ void __launch_bounds__(kSmallThreads, 1) muon_small_kernel(const __grid_constant__ MuonParams p) {
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ double part[kSmallThreads / 32];
+    __shared__ uint32_t tmem_holder;
+    __shared__ int abort_word;
+    __shared__ alignas(8) uint64_t bars[3];
+    const uint32_t base = (ptx::smem_u32(smem_raw) + 1023u) & ~1023u, poly = base + kSmallPanels * kPanelBytes;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, quarter = warp & 3, strip = warp >> 2;
+    volatile int *abort_flag = &abort_word;
+    if (threadIdx.x == 0) {
+        ptx::mbar_init(ptx::smem_u32(bars), 1);
+        ptx::mbar_init(ptx::smem_u32(bars + 1), 1);
+        ptx::mbar_init(ptx::smem_u32(bars + 2), 1);
+        abort_word = 0;
+        ptx::fence_barrier_init();
+        ptx::fence_proxy_async();
+    }
+    if (warp == 0) tmem_alloc_g<1>(ptx::smem_u32(&tmem_holder), 512);
+    ptx::tc_fence_before_sync();
+    __syncthreads();
+    ptx::tc_fence_after_sync();
+    const uint32_t tmem = tmem_holder;
+    ptx::grid_dependency_wait();
+    ptx::grid_launch_dependents();
+    float grad_scale;
+    const bool fine = muon_scale(p, grad_scale) && eg_check(p.first_small + (int)blockIdx.x < p.n_matrices, p.status, kCheckMuonUnit, blockIdx.x);
+    const MuonMatrix t = p.matrices[fine ? p.first_small + blockIdx.x : 0];
+    if (fine && !muon_skips(p, t)) {
+        const int32_t d = t.d, len = (int32_t)max(t.rows, t.cols);
+        const int32_t panels = (len + 63) / 64;
+        const void *grad = p.grads[t.index];
+        // the panels' zeros, and those of the rest behind a row's end
+        for (int i = threadIdx.x; i < panels * kPanelBytes / 16; i += kSmallThreads)
+            asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(base + i * 16), "r"(0) : "memory");
+        const bool vector = muon_vector(p, t);
+        __syncthreads();
+        if (vector)
+            small_begin<true>(p, t, grad, grad_scale, base, part);
+        else
+            small_begin<false>(p, t, grad, grad_scale, base, part);
+        const int steps = p.products / 3;
+        uint32_t phase[2] = {0, 0};
+        bool ok = true;
+        const uint32_t row = quarter * 32 + lane;
+        const uint32_t tmem_row = tmem + ((uint32_t)(quarter * 32) << 16);
+        auto idesc = [](int cols, bool b_mn) { return (1u << 4) | ((uint32_t)b_mn << 16) | ((uint32_t)(cols >> 3) << 17) | ((uint32_t)(kSmallSide >> 4) << 24); };
+        // everything that has been stored in shared memory, and read from tensor memory, comes before the products
+        auto meet = [&] {
+            ptx::fence_proxy_async();
+            ptx::tc_fence_before_sync();
+            __syncthreads();
+            ptx::tc_fence_after_sync();
+        };
+        auto wait = [&](int bar) {
+            ok = ok && ptx::mbar_wait_bounded(ptx::smem_u32(bars + bar), phase[bar], abort_flag, p.wait_limit_ns);
+            phase[bar] ^= 1u;
+            ptx::tc_fence_after_sync();
+        };
+        const int ksteps = (d + 15) / 16;  // of a sum over the shorter side
+        // P X for the panels of chunk c into the accumulator of its parity
+        const int chunks = (panels + 3) / 4;
+        auto issue_chunk = [&](int c) {
+            const int wide = min(4, panels - 4 * c) * 64;
+            const uint64_t mn = (uint64_t)(kPanelBytes >> 4) << 16 | (uint64_t)(1024 >> 4) << 32 | (uint64_t)1 << 46 | (uint64_t)2 << 61;
+            for (int k = 0; k < ksteps; ++k)
+                mma_g<1>(tmem + (c & 1) * 256, ptx::make_desc_k_sw128(poly + (k >> 2) * kPanelBytes) + (k & 3) * 2,
+                         mn | (base + 4 * c * kPanelBytes + k * 2048) >> 4, idesc(wide, true), k > 0);
+            mma_commit_g<1>(ptx::smem_u32(bars + (c & 1)));
+        };
+        meet();
+#pragma unroll 1
+        for (int step = 0; step < steps && ok; ++step) {
+            // A = X X^T
+            if (threadIdx.x == 0 && p.stall == 0) {
+                for (int k = 0; k < panels * 4; ++k) {
+                    const uint64_t x = ptx::make_desc_k_sw128(base + (k >> 2) * kPanelBytes) + (k & 3) * 2;
+                    mma_g<1>(tmem, x, x, idesc(kSmallSide, false), k > 0);
+                }
+                mma_commit_g<1>(ptx::smem_u32(bars));
+            }
+            wait(0);
+            ok = __syncthreads_and(ok);
+            if (!ok) break;
+            uint32_t a[16];
+            const float down = t.down * t.down;
+            {
+                float v[32];
+                ptx::tmem_ld_32x32(tmem_row + strip * 32, reinterpret_cast<uint32_t (&)[32]>(v));
+                ptx::tmem_ld_wait();
+#pragma unroll
+                for (int i = 0; i < 16; ++i) a[i] = pack2<f16>(v[2 * i] * down, v[2 * i + 1] * down);
+                panel_store(poly, row, strip * 32, a);
+            }
+            meet();
+            // A A, and P over A
+            if (threadIdx.x == 0) {
+                for (int k = 0; k < ksteps; ++k) {
+                    const uint64_t x = ptx::make_desc_k_sw128(poly + (k >> 2) * kPanelBytes) + (k & 3) * 2;
+                    mma_g<1>(tmem, x, x, idesc(kSmallSide, false), k > 0);
+                }
+                mma_commit_g<1>(ptx::smem_u32(bars));
+            }
+            wait(0);
+            ok = __syncthreads_and(ok);
+            if (!ok) break;
+            {
+                float v[32];
+                ptx::tmem_ld_32x32(tmem_row + strip * 32, reinterpret_cast<uint32_t (&)[32]>(v));
+                ptx::tmem_ld_wait();
+                const int diagonal = (int)row < d ? (int)row - strip * 32 : -1;
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const float2 f = unpack2<f16>(a[i]);
+                    v[2 * i] = fmaf(kNsC, v[2 * i], kNsB * f.x) + (diagonal == 2 * i ? kNsA : 0.0f);
+                    v[2 * i + 1] = fmaf(kNsC, v[2 * i + 1], kNsB * f.y) + (diagonal == 2 * i + 1 ? kNsA : 0.0f);
+                }
+                uint32_t r[16];
+#pragma unroll
+                for (int i = 0; i < 16; ++i) r[i] = pack2<f16>(v[2 * i], v[2 * i + 1]);
+                panel_store(poly, row, strip * 32, r);
+            }
+            meet();
+            // X = P X, four panels at a time, the next four's products beside this one's values
+            if (threadIdx.x == 0) issue_chunk(0);
+#pragma unroll 1
+            for (int c = 0; c < chunks; ++c) {
+                if (threadIdx.x == 0 && c + 1 < chunks) issue_chunk(c + 1);
+                // a warp's pieces of the chunk (two at most); what X's rounding left of them is on its way while the products are computed
+                const int pieces = min(4, panels - 4 * c) * 2;
+                uint32_t lo[2][16];
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    const int at = strip + k * kSmallStrips;
+                    if (at >= pieces || (int)row >= d) continue;
+                    const uint4 *rest = reinterpret_cast<const uint4 *>(t.lo + rest_place(row, c * 256 + at * kPiece));
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const uint4 q = rest[i * kSmallSide];
+                        lo[k][4 * i] = q.x, lo[k][4 * i + 1] = q.y, lo[k][4 * i + 2] = q.z, lo[k][4 * i + 3] = q.w;
+                    }
+                }
+                wait(c & 1);
+                ok = __syncthreads_and(ok);
+                if (!ok) break;
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    const int at = strip + k * kSmallStrips;
+                    if (at >= pieces) continue;
+                    const int32_t col = c * 256 + at * kPiece;
+                    float v[32];
+                    ptx::tmem_ld_32x32(tmem_row + (c & 1) * 256 + at * kPiece, reinterpret_cast<uint32_t (&)[32]>(v));
+                    ptx::tmem_ld_wait();
+                    if ((int)row >= d) continue;  // (whole rows of zeros stay as they are)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        const float2 f = unpack2<f16>(lo[k][i]);
+                        v[2 * i] = col + 2 * i < len ? fmaf(kNsA, f.x, v[2 * i]) : 0.0f;
+                        v[2 * i + 1] = col + 2 * i + 1 < len ? fmaf(kNsA, f.y, v[2 * i + 1]) : 0.0f;
+                    }
+                    uint32_t hi[16];
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        hi[i] = pack2<f16>(v[2 * i], v[2 * i + 1]);
+                        const float2 f = unpack2<f16>(hi[i]);
+                        lo[k][i] = pack2<f16>(v[2 * i] - f.x, v[2 * i + 1] - f.y);
+                    }
+                    panel_store(base, row, col, hi);
+                    uint4 *rest = reinterpret_cast<uint4 *>(t.lo + rest_place(row, col));
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) rest[i * kSmallSide] = make_uint4(lo[k][4 * i], lo[k][4 * i + 1], lo[k][4 * i + 2], lo[k][4 * i + 3]);
+                }
+                // (the accumulator of this chunk is free for the chunk after the next)
+                ptx::tc_fence_before_sync();
+                __syncthreads();
+                ptx::tc_fence_after_sync();
+            }
+            meet();
+        }
+        if (ok)
+            with_type(t.param_type, [&](auto type) {
+                if (t.vector)
+                    small_end<decltype(type), true>(p, t, base);
+                else
+                    small_end<decltype(type), false>(p, t, base);
+            });
+        if (!ok && threadIdx.x == 0) {
+            // gave up: no product of ours may still read shared memory when the block leaves
+            mma_commit_g<1>(ptx::smem_u32(bars + 2));
+            const uint64_t t0 = ptx::globaltimer_ns();
+            while (!ptx::mbar_try_wait(ptx::smem_u32(bars + 2), 0))
+                if (ptx::globaltimer_ns() - t0 > p.wait_limit_ns) break;
+            atomicMax(p.status, 6);
+        }
+    }
+    ptx::tc_fence_before_sync();
+    __syncthreads();
+    ptx::tc_fence_after_sync();
+    if (warp == 0) tmem_free_g<1>(tmem, 512);
 }
 
 }  // namespace ops

@@ -19,6 +19,9 @@ static bool good_muon_tensor(const egeria_muon_tensor &t) {
     return t.param && t.m && aligned(t.param, size_of(t.param_type)) && aligned(t.master, 4) && aligned(t.m, 4);
 }
 
+static bool muon_small(const egeria_muon_tensor &t) {
+    return std::min(t.rows, t.cols) <= kSmallSide && std::max(t.rows, t.cols) <= kSmallPanels * 64;
+}
 // Where things lie in the workspace.  The matrices' own part goes by their sides alone.
 struct MuonPlaces {
     size_t x[2], lo, gram, poly, sums;
@@ -26,7 +29,9 @@ struct MuonPlaces {
 struct MuonLayout {
     size_t matrices, maps, grads, pieces, units, done, total;
     int64_t n_matrices, n_pieces, n_units;
-    std::vector<MuonPlaces> places;   // of the matrices that are not empty, in the caller's order
+    std::vector<int> which;           // the matrices that are not empty, the small ones last
+    std::vector<MuonPlaces> places;   // theirs
+    int large;                        // how many are not small
 };
 static int64_t up32(int64_t v) { return (v + 31) / 32 * 32; }
 // Products of a tile: which columns of tiles a row of them has to take.  Of a symmetric product only those that reach the diagonal.
@@ -42,7 +47,8 @@ struct MuonKind {
 // tiles of 256) 100 us with the small ones and 131 with the large, 12 matrices of 333 x 333 and 333 x 1332 203 and 263.
 static MuonKind muon_kind(int count, const egeria_muon_tensor *t) {
     int64_t tiles = 0;
-    for (int i = 0; i < count; ++i) tiles += ((t[i].rows + 255) / 256) * ((t[i].cols + 255) / 256);
+    for (int i = 0; i < count; ++i)
+        if (!muon_small(t[i])) tiles += ((t[i].rows + 255) / 256) * ((t[i].cols + 255) / 256);
     return tiles >= 2 * kSms ? MuonKind{256, 2} : MuonKind{128, 1};
 }
 static bool muon_layout(int count, const egeria_muon_tensor *t, int steps, MuonLayout &L) {
@@ -55,11 +61,23 @@ static bool muon_layout(int count, const egeria_muon_tensor *t, int steps, MuonL
         L.total = up(L.total + (size_t)n, 1024);
         return at;
     };
-    for (int i = 0; i < count; ++i) {
+    L.which.clear();
+    for (const bool small : {false, true}) {
+        for (int i = 0; i < count; ++i)
+            if (t[i].rows > 0 && t[i].cols > 0 && muon_small(t[i]) == small) L.which.push_back(i);
+        if (!small) L.large = (int)L.which.size();
+    }
+    for (int i = 0; i < count; ++i)
+        if (t[i].rows > kMuonMaxSide || t[i].cols > kMuonMaxSide) return false;
+    for (const int i : L.which) {
         const int64_t rows = t[i].rows, cols = t[i].cols, d = std::min(rows, cols);
-        if (rows > kMuonMaxSide || cols > kMuonMaxSide) return false;
-        if (d == 0) continue;
         ++L.n_matrices;
+        if (muon_small(t[i])) {
+            MuonPlaces q{};
+            q.lo = take(kSmallSide * up(std::max(rows, cols), 64) * 2);
+            L.places.push_back(q);
+            continue;
+        }
         const int64_t pieces = (rows * cols + kMuonPiece - 1) / kMuonPiece;
         L.n_pieces += pieces;
         const int64_t r = (d + 128 * kind.cg - 1) / (128 * kind.cg), c = (d + kind.bn - 1) / kind.bn;
@@ -86,13 +104,22 @@ static bool muon_layout(int count, const egeria_muon_tensor *t, int steps, MuonL
     return true;
 }
 
-template <int BN, int CG>
+template <int BN, int CG, bool NARROW>
 static cudaError_t muon_allow() {
-    return cudaFuncSetAttribute(muon_products_kernel<BN, CG>, cudaFuncAttributeMaxDynamicSharedMemorySize, MuonCfg<BN, CG>::kSmem);
+    return cudaFuncSetAttribute(muon_products_kernel<BN, CG, NARROW>, cudaFuncAttributeMaxDynamicSharedMemorySize, MuonCfg<BN, CG>::kSmem);
+}
+static cudaError_t muon_allow_all() {
+    cudaError_t e = muon_allow<256, 2, false>();
+    if (e == cudaSuccess) e = muon_allow<256, 2, true>();
+    if (e == cudaSuccess) e = muon_allow<128, 1, false>();
+    if (e == cudaSuccess) e = muon_allow<128, 1, true>();
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(muon_small_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmallSmem);
+    return e;
 }
 template <int BN, int CG>
-static cudaError_t muon_launch(const MuonParams &p, int workers, cudaStream_t stream) {
-    return launch(muon_products_kernel<BN, CG>, dim3(workers * CG), MuonCfg<BN, CG>::kThreads, MuonCfg<BN, CG>::kSmem, stream, CG, p);
+static cudaError_t muon_launch(const MuonParams &p, int workers, bool narrow, cudaStream_t stream) {
+    auto kernel = narrow ? muon_products_kernel<BN, CG, true> : muon_products_kernel<BN, CG, false>;
+    return launch(kernel, dim3(workers * CG), MuonCfg<BN, CG>::kThreads, MuonCfg<BN, CG>::kSmem, stream, CG, p);
 }
 
 }  // namespace ops
@@ -111,6 +138,7 @@ struct egeria_muon {
     int64_t launches = 0;
     cudaStream_t last_stream = nullptr;
     uint32_t stall_next = 0;
+    bool narrow = false;             // some matrix takes no whole lines
 };
 
 extern "C" {
@@ -154,7 +182,7 @@ egeria_status egeria_muon_create(egeria_muon **out, int count, const egeria_muon
         }
         const EncodeTiledFn encode = reinterpret_cast<EncodeTiledFn>(fn);
         const MuonKind kind = muon_kind(count, tensors);
-        EGO_CUDA((kind.cg == 2 ? muon_allow<256, 2>() : muon_allow<128, 1>()));
+        EGO_CUDA(muon_allow_all());
         const int workers = sms / kind.cg;
 
         h = new egeria_muon();
@@ -166,11 +194,9 @@ egeria_status egeria_muon_create(egeria_muon **out, int count, const egeria_muon
         std::vector<MuonMatrix> matrices;
         std::vector<CUtensorMap> maps((size_t)L.n_matrices * kMuonMaps);
         std::vector<int2> pieces;
-        for (int i = 0; i < count; ++i) {
+        for (int i = 0; i < count; ++i) h->grad_size.push_back(tensors[i].rows > 0 && tensors[i].cols > 0 ? size_of(tensors[i].grad_type) : 0);
+        for (const int i : L.which) {
             const egeria_muon_tensor &t = tensors[i];
-            const bool there = t.rows > 0 && t.cols > 0;
-            h->grad_size.push_back(there ? size_of(t.grad_type) : 0);
-            if (!there) continue;
             const int k = (int)matrices.size();
             const MuonPlaces &at = L.places[k];
             MuonMatrix q{};
@@ -200,20 +226,21 @@ egeria_status egeria_muon_create(egeria_muon **out, int count, const egeria_muon
                               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
             };
             bool ok = true;
-            for (int s = 0; s < 2; ++s)
+            for (int s = 0; s < 2 && !muon_small(t); ++s)
                 ok = ok && map(kMapX0 + 2 * s, q.x[s], q.rows, q.cols, q.ldx, 128) && map(kMapX0N + 2 * s, q.x[s], q.rows, q.cols, q.ldx, 64);
-            ok = ok && map(kMapGram, q.gram, q.d, q.d, q.ldd, 128) && map(kMapPoly, q.poly, q.d, q.d, q.ldd, 128);
+            if (!muon_small(t)) ok = ok && map(kMapGram, q.gram, q.d, q.d, q.ldd, 128) && map(kMapPoly, q.poly, q.d, q.d, q.ldd, 128);
             if (!ok) {
                 delete h;
                 return EGERIA_ERR_CUDA;
             }
+            h->narrow = h->narrow || (k < L.large && !q.vector);
+            for (int s = 0; s < q.pieces && k < L.large; ++s) pieces.push_back(make_int2(k, s));
             matrices.push_back(q);
-            for (int s = 0; s < q.pieces; ++s) pieces.push_back(make_int2(k, s));
         }
         // The units, product by product over all matrices, large ones first, so that a unit's matrix has mostly finished the product
         // before.  (In groups whose products go round the workers two to eight times, which meet more of their values in L2, the
         // 24 blocks of width 1024 took 5.75 to 5.18 ms against 5.15: the waits at a group's ends cost more.)
-        std::vector<int> order(matrices.size());
+        std::vector<int> order(L.large);
         for (size_t i = 0; i < order.size(); ++i) order[i] = (int)i;
         std::stable_sort(order.begin(), order.end(), [&](int a, int b) {
             const MuonMatrix &p = matrices[a], &q = matrices[b];
@@ -247,9 +274,10 @@ egeria_status egeria_muon_create(egeria_muon **out, int count, const egeria_muon
         p.n_units = (int32_t)units.size();
         p.n_pieces = (int32_t)pieces.size();
         p.n_matrices = (int32_t)matrices.size();
+        p.first_small = L.large;
         p.products = 3 * steps;
         p.early = p.n_units >= 3 * steps * 4 * workers;
-        h->workers = (int)std::min<int64_t>(workers, p.n_units);
+        h->workers = (int)std::min<int64_t>(workers, std::max(p.n_units, 1));
         auto put = [&](size_t at, const void *from, size_t bytes) { return bytes ? cudaMemcpy(ws + at, from, bytes, cudaMemcpyHostToDevice) : cudaSuccess; };
         // (first what was enqueued before: it may still write to this memory, and the copies would not wait for it)
         if ((int64_t)units.size() != L.n_units || cudaDeviceSynchronize() != cudaSuccess || cudaMemset(ws, 0, 256) != cudaSuccess ||
@@ -295,7 +323,6 @@ egeria_status egeria_muon_step(egeria_muon *muon, void *cuda_stream, double lr, 
     cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
     muon->last_stream = stream;
     MuonParams p = muon->params;
-    if (p.n_pieces == 0) return EGERIA_OK;
     p.grad_scale = grad_scale;
     p.frozen = frozen;
     p.lr = (float)lr;
@@ -306,10 +333,17 @@ egeria_status egeria_muon_step(egeria_muon *muon, void *cuda_stream, double lr, 
     p.stall = muon->stall_next;
     p.wait_limit_ns = muon->stall_next ? kTestWaitLimitNs : kWaitLimitNs;
     muon->stall_next = 0;
-    EGO_CUDA(launch(muon_momentum_kernel, dim3(p.n_pieces), kMuonThreads, 0, stream, 1, p));
-    EGO_CUDA(launch(muon_normalize_kernel, dim3(p.n_pieces), kMuonThreads, 0, stream, 1, p));
-    EGO_CUDA((muon->kind.cg == 2 ? muon_launch<256, 2>(p, muon->workers, stream) : muon_launch<128, 1>(p, muon->workers, stream)));
-    muon->launches += 3;
+    if (p.first_small > 0) {
+        EGO_CUDA(launch(muon_momentum_kernel, dim3(p.n_pieces), kMuonThreads, 0, stream, 1, p));
+        EGO_CUDA(launch(muon_normalize_kernel, dim3(p.n_pieces), kMuonThreads, 0, stream, 1, p));
+        EGO_CUDA((muon->kind.cg == 2 ? muon_launch<256, 2>(p, muon->workers, muon->narrow, stream)
+                                     : muon_launch<128, 1>(p, muon->workers, muon->narrow, stream)));
+        muon->launches += 3;
+    }
+    if (p.n_matrices > p.first_small) {
+        EGO_CUDA(launch(muon_small_kernel, dim3(p.n_matrices - p.first_small), kSmallThreads, kSmallSmem, stream, 1, p));
+        ++muon->launches;
+    }
     return EGERIA_OK;
 }
 

@@ -61,7 +61,7 @@ def near(got, want, tol, what=""):
 
 
 SHAPES = [(1, 1), (1, 700), (700, 1), (2, 3), (16, 144), (33, 47), (47, 33), (64, 64), (64, 576), (100, 100), (128, 128), (129, 257), (257, 129),
-          (130, 1000), (519, 519), (333, 1332), (1332, 333), (1024, 256)]
+          (130, 1000), (519, 519), (333, 1332), (1332, 333), (1024, 256), (128, 768), (768, 128), (100, 767), (767, 65), (128, 769), (129, 768), (1, 768), (5, 65)]
 
 
 def one_step(t):

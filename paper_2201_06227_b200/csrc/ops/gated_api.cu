@@ -149,26 +149,28 @@ static int64_t gated_sums(int64_t rows, int64_t hidden) { return (rows + 31) / 3
 static GatedLayout gated_layout(int64_t rows, int64_t inp, int64_t hidden, int64_t out) {
     GatedLayout L;
     size_t off = kHeadBytes;
-    auto take = [&](int64_t n) {
+    // (the largest sizes' products leave 64 bits: no workspace has 2^62 bytes)
+    auto take = [&](int64_t a, int64_t b, int size) {
         const size_t at = off;
-        off = up(off + (size_t)n, 1024);
+        const unsigned __int128 end = (unsigned __int128)off + (unsigned __int128)a * (unsigned __int128)b * (unsigned)size;
+        off = end > ((unsigned __int128)1 << 62) ? (size_t)1 << 62 : up((size_t)end, 1024);
         return at;
     };
-    L.part[0] = take((int64_t)std::max(split_bytes(rows, out, hidden), split_bytes(out, hidden, rows)));  // y, or dw_down
-    L.part[1] = take((int64_t)split_bytes(hidden, inp, rows));
-    L.part[2] = take((int64_t)split_bytes(hidden, inp, rows));
-    L.part[3] = take((int64_t)split_bytes(rows, inp, 2 * hidden));
-    L.x = take(rows * pad8(inp) * 2);
-    L.w_gate = take(hidden * pad8(inp) * 2);
-    L.w_up = take(hidden * pad8(inp) * 2);
-    L.w_down = take(out * pad8(hidden) * 2);
-    L.dy = take(rows * pad8(out) * 2);
-    L.h = take(rows * pad16(hidden) * 2);
-    L.dg = take(rows * pad16(hidden) * 2);
-    L.du = take(rows * pad16(hidden) * 2);
-    L.sums = take(gated_sums(rows, hidden) * 4);
-    L.sums2 = take(gated_sums(rows, hidden) * 4);
-    L.sums_down = take(slope_sums(rows, out) * 4);
+    L.part[0] = take(1, (int64_t)std::max(split_bytes(rows, out, hidden), split_bytes(out, hidden, rows)), 1);  // y, or dw_down
+    L.part[1] = take(1, (int64_t)split_bytes(hidden, inp, rows), 1);
+    L.part[2] = take(1, (int64_t)split_bytes(hidden, inp, rows), 1);
+    L.part[3] = take(1, (int64_t)split_bytes(rows, inp, 2 * hidden), 1);
+    L.x = take(rows, pad8(inp), 2);
+    L.w_gate = take(hidden, pad8(inp), 2);
+    L.w_up = take(hidden, pad8(inp), 2);
+    L.w_down = take(out, pad8(hidden), 2);
+    L.dy = take(rows, pad8(out), 2);
+    L.h = take(rows, pad16(hidden), 2);
+    L.dg = take(rows, pad16(hidden), 2);
+    L.du = take(rows, pad16(hidden), 2);
+    L.sums = take((rows + 31) / 32, hidden, 4);
+    L.sums2 = take((rows + 31) / 32, hidden, 4);
+    L.sums_down = take(1, slope_sums(rows, out), 4);
     L.total = off;
     return L;
 }

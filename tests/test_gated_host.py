@@ -13,6 +13,8 @@ def test_workspace_sizes():
     assert size(0, 64, 64, 64) >= ops.OPS_WORKSPACE_MIN
     for bad in ((-1, 64, 64, 64), (1, 0, 64, 64), (1, 64, 0, 64), (1, 64, 64, 0), (2 ** 31, 64, 64, 64), (1, 2 ** 31, 64, 64), (1, 64, 2 ** 31, 64), (1, 64, 64, 2 ** 31)):
         assert size(*bad) == 0, bad
+    most = 2 ** 31 - 1024                                   # sizes whose products leave 64 bits: more than any workspace has
+    assert size(most, most, most, most) >= 2 ** 61 and size(most, 1, most, 1) >= 2 ** 61 and size(1, most, most, 1) >= 2 ** 61
     # copies of every operand and the three hidden matrices of a backward pass
     assert size(1000, 1001, 999, 1003) >= 2 * (1000 * (1008 + 1008) + 999 * 2 * 1008 + 1003 * 1000 + 3 * 1000 * 1008)
 

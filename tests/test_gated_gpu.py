@@ -10,6 +10,7 @@ import torch
 from paper_2201_06227_b200 import binding as eg
 from paper_2201_06227_b200 import ops
 from test_ops_gpu import ACTS, DEV, TINY, U, act64, close, rand
+from test_ops_gpu import check_forward as check_linear
 
 pytestmark = pytest.mark.gpu
 
@@ -128,7 +129,8 @@ def test_backward(rows, inp, hidden, out, dtype):
     o.check_device_status()
 
 
-@pytest.mark.parametrize("rows,inp,hidden,out", [(4096, 1024, 2816, 1024), (2048, 2048, 5632, 2048), (16384, 256, 768, 256), (1500, 1032, 4104, 520)])
+@pytest.mark.parametrize("rows,inp,hidden,out", [(4096, 1024, 2816, 1024), (2048, 2048, 5632, 2048), (16384, 256, 768, 256), (1500, 1032, 4104, 520),
+                                                   (16000, 128, 2816, 1000)])
 def test_larger(rows, inp, hidden, out):
     """Sizes whose products go over pairs of CTAs, tiles of 512 rows and more than one round of them."""
     o = handle(rows, inp, hidden, out)
@@ -136,6 +138,23 @@ def test_larger(rows, inp, hidden, out):
     w, b = weights(inp, hidden, out, torch.bfloat16, 3)
     _, g, u = check_forward(o, x, w, b, "gelu_tanh", rand(rows, out, seed=4))
     check_backward(o, dy, x, w, g, u, "gelu_tanh", need_db=True)
+    o.check_device_status()
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("rows,inp,out", [(16384, 4096, 1024), (15900, 2700, 1001), (9000, 2624, 2048)])
+def test_linear_layers_of_long_sums(rows, inp, out, dtype):
+    """Where a block's second product, or a linear layer, goes over tiles of 512 rows; the give-up path there too."""
+    o = ops.Ops(ops.egeria_linear_workspace_bytes(rows, inp, out), DEV)
+    x, w = rand(rows, inp, dtype=dtype, seed=1), rand(out, inp, dtype=dtype, seed=2, scale=inp ** -0.5)
+    r, b = rand(rows, out, dtype=dtype, seed=3), rand(out, dtype=dtype, seed=4)
+    check_linear(o, x, w, b, "none", r, False)
+    want = o.egeria_linear_forward(x, w)
+    for kind in (1, 2):
+        o.egeria_ops_debug_stall_next(kind)
+        o.egeria_linear_forward(x, w)
+        assert o.egeria_ops_device_status() == eg.ERR_TIMEOUT
+        assert torch.equal(o.egeria_linear_forward(x, w), want)
     o.check_device_status()
 
 

@@ -3,9 +3,10 @@
  *
  * Next to the plasticity evaluation of egeria.h the library has the operators that a
  * training step of the monitored network spends its time in: linear layers with what
- * surrounds the product in its epilogue and their gradients, the norms of a residual
- * stream with their gate and their gradients, and an AdamW step over all tensors that
- * leaves the frozen modules alone by reading the freeze mask on the device.
+ * surrounds the product in its epilogue and their gradients, gated feed-forward blocks
+ * and their gradients, the norms of a residual stream with their gate and their
+ * gradients, and two optimizer steps, AdamW over all tensors and Muon over matrices, that
+ * leave the frozen modules alone by reading the freeze mask on the device.
  *
  * The conventions of egeria.h hold: device pointers are the caller's, the library
  * allocates no device memory, calls enqueue work on the stream they are given and
@@ -17,8 +18,8 @@
  *     fastest.
  *   - A handle belongs to one stream at a time: its workspace is scratch of the call in
  *     flight.  Handles are not thread-safe.
- *   - The calls of an egeria_ops handle may be captured into a CUDA graph and replayed
- *     in stream order.
+ *   - The calls of a handle may be captured into a CUDA graph and replayed in stream
+ *     order.
  *   - Sums, row statistics and gradients of parameters are accumulated in 32 bits and
  *     rounded once to the output's type.  Results do not depend on timing: the same call
  *     gives the same bits.
@@ -38,7 +39,7 @@ typedef struct egeria_ops egeria_ops;       /* opaque, library-owned host object
 typedef struct egeria_adamw egeria_adamw;
 typedef struct egeria_muon egeria_muon;
 
-/* A handle for the linear and norm calls.
+/* A handle for the calls of linear layers, gated blocks and norms.
  *   workspace  device memory, EGERIA_WORKSPACE_ALIGN-aligned, caller-owned, at least
  *              EGERIA_OPS_WORKSPACE_MIN bytes and as much as the largest call made through
  *              the handle asks for; must outlive the handle
@@ -289,7 +290,8 @@ int64_t egeria_adamw_launch_count(const egeria_adamw *adamw);
 #define EGERIA_MUON_MAX_STEPS 16
 
 /* One matrix of the model, rows x cols consecutive values (a convolution's weight as its output channels by the rest), element-aligned.
- * Fastest where cols is a multiple of 8 and everything 32-byte aligned. */
+ * Fastest where cols is a multiple of 8 and everything 32-byte aligned.  What a step writes (param, master, m of all matrices) shares no
+ * value (EGERIA_ERR_INVALID_ARG): a weight that two layers share stands in the list once. */
 typedef struct {
     void *param;             /* of param_type; written */
     float *master;           /* NULL, or the 32-bit copy that the step works on; param is then its rounding */
@@ -324,8 +326,9 @@ egeria_status egeria_muon_set_grads(egeria_muon *muon, void *cuda_stream, const 
  *   X = t / max(|t|, eps), |t| the root of the sum of squares; then `steps` times
  *       A = X X^T     X = 3.4445 X - 4.7750 A X + 2.0315 A^2 X
  *   p = p (1 - lr weight_decay) - lr scale X
- * The products' operands are rounded to 16 bits of 11 digits, their sums are 32 bits: an update is off by about 2e-3 of itself
- * (root mean square).  A gradient that is not finite makes its whole matrix NaN.
+ * The products' operands are rounded to f16 (11 digits), their sums are 32 bits: X is off by about 1.5e-3 of itself (2-norm; 1.1e-3 to
+ * 2.1e-3 over the shapes and ranks tried).  A gradient that is not finite makes its whole matrix NaN.  The sum of A's products over a
+ * long side is not split: matrices are meant to be many or large, not one of a few rows by millions.
  *   grad_scale  device float [1] or NULL (1).  If it is not finite the whole step is left out.
  *   frozen      device uint8 or NULL, indexed by `module`: the out_mask of egeria_plasticity_evaluate as it is.  A frozen
  *               matrix is neither read nor written.  (Not to be written while the call runs.)

@@ -1,6 +1,8 @@
 // Host side of the Muon step (include/egeria_ops.h): argument checks, the list of units, launches.
+#include <algorithm>
 #include <cmath>
 #include <new>
+#include <utility>
 #include <vector>
 
 #include "muon.cuh"
@@ -19,6 +21,24 @@ static bool good_muon_tensor(const egeria_muon_tensor &t) {
     return t.param && t.m && aligned(t.param, size_of(t.param_type)) && aligned(t.master, 4) && aligned(t.m, 4);
 }
 
+// Whether two of the ranges that a step writes share a byte: a matrix that stands in the list twice would be updated from two workers at a
+// time.  (The sides are within kMuonMaxSide here.)
+static bool muon_overlaps(int count, const egeria_muon_tensor *t) {
+    std::vector<std::pair<uintptr_t, uintptr_t>> written;
+    auto add = [&](const void *p, int64_t bytes) {
+        if (p && bytes > 0) written.emplace_back(reinterpret_cast<uintptr_t>(p), reinterpret_cast<uintptr_t>(p) + (uintptr_t)bytes);
+    };
+    for (int i = 0; i < count; ++i) {
+        const int64_t n = t[i].rows * t[i].cols;
+        add(t[i].param, n * (int64_t)size_of(t[i].param_type));
+        add(t[i].master, n * 4);
+        add(t[i].m, n * 4);
+    }
+    std::sort(written.begin(), written.end());
+    for (size_t i = 1; i < written.size(); ++i)
+        if (written[i].first < written[i - 1].second) return true;
+    return false;
+}
 static bool muon_small(const egeria_muon_tensor &t) {
     return std::min(t.rows, t.cols) <= kSmallSide && std::max(t.rows, t.cols) <= kSmallPanels * 64;
 }
@@ -52,6 +72,8 @@ static MuonKind muon_kind(int count, const egeria_muon_tensor *t) {
     return tiles >= 2 * kSms ? MuonKind{256, 2} : MuonKind{128, 1};
 }
 static bool muon_layout(int count, const egeria_muon_tensor *t, int steps, MuonLayout &L) {
+    for (int i = 0; i < count; ++i)
+        if (t[i].rows > kMuonMaxSide || t[i].cols > kMuonMaxSide) return false;
     const MuonKind kind = muon_kind(count, t);
     L.n_matrices = L.n_pieces = L.n_units = 0;
     L.total = 256;  // status words
@@ -67,8 +89,6 @@ static bool muon_layout(int count, const egeria_muon_tensor *t, int steps, MuonL
             if (t[i].rows > 0 && t[i].cols > 0 && muon_small(t[i]) == small) L.which.push_back(i);
         if (!small) L.large = (int)L.which.size();
     }
-    for (int i = 0; i < count; ++i)
-        if (t[i].rows > kMuonMaxSide || t[i].cols > kMuonMaxSide) return false;
     for (const int i : L.which) {
         const int64_t rows = t[i].rows, cols = t[i].cols, d = std::min(rows, cols);
         ++L.n_matrices;
@@ -169,6 +189,7 @@ egeria_status egeria_muon_create(egeria_muon **out, int count, const egeria_muon
         MuonLayout L;
         if (!muon_layout(count, tensors, steps, L)) return EGERIA_ERR_UNSUPPORTED_SHAPE;
         if (!workspace || !aligned(workspace, EGERIA_WORKSPACE_ALIGN) || workspace_bytes < L.total) return EGERIA_ERR_WORKSPACE;
+        if (muon_overlaps(count, tensors)) return EGERIA_ERR_INVALID_ARG;
         int dev = 0, major = 0, sms = 0;
         EGO_CUDA(cudaGetDevice(&dev));
         EGO_CUDA(cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, dev));

@@ -1,7 +1,7 @@
 """ctypes binding of the training operators (``include/egeria_ops.h``) -- argument marshalling only.
 
-:class:`Ops` has the linear layers, the gated feed-forward blocks and the residual norms, :class:`AdamW` and :class:`Muon` the optimizer steps; their
-methods have the names of the C entry points that they call.  Everything is computed by the CUDA
+:class:`Ops` has the linear layers, the gated feed-forward blocks and the residual norms, :class:`AdamW` and
+:class:`Muon` the optimizer steps; their methods have the names of the C entry points that they call.  Everything is computed by the CUDA
 kernels of ``libegeria.so``; there is no fallback: a call that the library refuses raises
 :class:`~paper_2201_06227_b200.binding.EgeriaError`, a tensor that it cannot take ``ValueError``.
 
@@ -12,7 +12,7 @@ is recorded on every stream that it is called on; it may be dropped with calls i
 
 Autograd does not follow the calls: the gradients are the results of the ``*_backward`` methods.  Where it follows an
 input of a forward call, going back through the result raises an error (under ``torch.no_grad()`` results are plain
-tensors).  ``out`` and the parameters that require grad when an :class:`AdamW` is made get a new version when a call
+tensors).  ``out`` and the parameters that require grad when an :class:`AdamW` or :class:`Muon` is made get a new version when a call
 writes to them (frozen ones too: the mask is not read on the host; a replayed graph raises none).
 """
 from __future__ import annotations
@@ -418,8 +418,8 @@ MUON_MAX_STEPS = 16
 
 
 class Muon(_Handle):
-    """The Muon step of a model's matrices: momentum, five Newton-Schulz products of it, update; all matrices in three launches.
-    Frozen modules are left out on the device.
+    """The Muon step of a model's matrices: momentum, five steps of a Newton-Schulz iteration on it, update; all matrices in three
+    launches, small ones (at most 128 by 768) in one.  Frozen modules are left out on the device.
 
     params, grads, momenta: one contiguous CUDA tensor of two or more dimensions per matrix of the model, the first its rows, the others
     taken together its columns; momenta are float32.  masters: float32 copies that the step works on (entries may be None).

@@ -207,6 +207,21 @@ def test_unaligned_matrices(dtype, shift):
     Model([(64, 64), (40, 96), (33, 17), (300, 264)], dtype, shift=shift, master=dtype != torch.float32).check().check(nesterov=False)
 
 
+def test_matrices_side_by_side_in_one_buffer():
+    """Weights and momenta of all matrices without a gap between them; a neighbour's values stay its own.  The same matrix twice is refused."""
+    model = Model([(33, 17), (64, 64), (300, 264), (7, 5)])
+    flat = torch.cat([t.flatten() for pair in zip(model.params, model.m) for t in pair])
+    at = 0
+    for i, p in enumerate(model.params):
+        for column in (model.params, model.m):
+            column[i] = flat[at:at + p.numel()].view(p.shape)
+            at += p.numel()
+    model.muon = ops.Muon(model.params, model.grads, model.m, weight_decay=model.wd)
+    model.check().check()
+    with pytest.raises(eg.EgeriaError):
+        ops.Muon(model.params + model.params[:1], model.grads + model.grads[:1], model.m + [torch.zeros(33, 17, device=DEV)])
+
+
 @pytest.mark.parametrize("lr,beta,nesterov,wd,gs", [(1e-3, 0.95, True, 0.0, None), (1e-2, 0.0, True, 0.5, 2.0), (0.0, 0.5, False, 0.0, 1.0),
                                                     (1e-2, 0.99, False, 0.1, 2.0 ** -16)])
 def test_settings(lr, beta, nesterov, wd, gs):

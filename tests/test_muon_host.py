@@ -75,3 +75,16 @@ def test_workspace_sizes():
     assert size((0, 8)) > 0
     assert 6 * 1024 * 4096 + 4 * 1024 * 1024 <= size((1024, 4096)) <= 6 * 1024 * 4096 + 4 * 1024 * 1024 + (1 << 18)
     assert size((64, 64)) < size((64, 64), (64, 64)) < size((64, 64), (64, 128))
+    assert size((2 ** 63 - 1, 8)) == size((8, 8), (8, 2 ** 63 - 1)) == 0
+
+
+@pytest.mark.parametrize("second", [dict(param=4096), dict(param=4096 + 158), dict(master=4096), dict(m=8192), dict(m=8192 - 316), dict(m=4096)])
+def test_refuses_matrices_that_share_values(second):
+    """8 x 10: 160 bytes of weights, 320 of a momentum or a master."""
+    first = dict(param=4096, m=8192)
+    assert _create([_matrix(**first), _matrix(**{**dict(param=1 << 16, m=1 << 17), **second})]) == eg.ERR_INVALID_ARG
+
+
+@pytest.mark.parametrize("same", [dict(param=64, m=64), dict(param=64, m=222), dict(param=64, m=1024, master=1024), dict(param=64, m=1024, master=220)])
+def test_refuses_a_matrix_that_shares_values_with_itself(same):
+    assert _create([_matrix(**{k: v // 4 * 4 for k, v in same.items()})]) == eg.ERR_INVALID_ARG

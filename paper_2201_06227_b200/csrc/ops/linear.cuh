@@ -2,6 +2,7 @@
 //
 //   D[m, n] = sum_k A(m, k) B(n, k)         A, B: bf16 or f16 in memory, D accumulated in 32 bits
 //
+// (Of gated blocks too: both projections in one product, and the four products of their backward pass in one launch.)
 // The three products of a layer differ in which axis of an operand is consecutive in memory:
 //   forward  z  = x w^T     A = x  (k consecutive)      B = w  (k consecutive)
 //   backward dx = dz w      A = dz (k consecutive)      B = w  (n consecutive)
@@ -18,13 +19,14 @@
 // can take from L2 in the time of the MMAs (64 bytes a cycle at their full rate; 60 bytes a nanosecond seen).
 //
 // Measured (bf16, GPU time in a replayed graph; floor: 2 m n k at 1669 TFLOP/s, a short product's rate; a long run's is 1435
-// under the power limit, which these meet too): 65536 x 1024 x 4096 (rows, k, columns) alone 487 us of 329, with bias 533, with
-// bias and tanh-gelu 558, with z alone 506, with all of it 576 to 618; k = 4096 and 1024 columns 463 of 329.  dx and dw of
-// 16384 x 4096 x 1024 229 to 261 us of 165, with the slope of dx's tanh-gelu 293 to 313.  By the counters no unit is full at
-// k = 1024: the tensor pipe is busy for 60 % of the time alone and 51 % with all of the epilogue (67 % alone at k = 4096), L2 for 36
-// and 47 %, the issue slots for 16 and 31 %; each part of the epilogue shows in the time although it runs beside the next
-// tile's products.  Small products (under some 500 rows) are bound by the 10 us that a launch, its first loads and its one
-// epilogue take.
+// under the power limit, which these meet too): 65536 x 1024 x 4096 (rows, k, columns) alone 464 us of 329, with bias, tanh-gelu and z
+// 547; k = 4096 and 1024 columns 16384 rows 119 of 82.  dx and dw of 16384 x 4096 x 1024 236 us of 165, with the slope of dx's
+// tanh-gelu 317.  By the counters no unit is full at k = 1024: the tensor pipe is busy for 60 % of the time alone and 51 % with all of
+// the epilogue (67 % alone at k = 4096), the issue slots for 16 and 31 %.  What is full is an SM's intake: tile loads bring 60 to 69
+// bytes a nanosecond into one, whether it loads alone or all 148 do (a kernel that only loads: 59.5 with 16 KB tiles, 68 with contiguous
+// 16 KB), and a 256 x 256 tile wants 32 KB per 64 k, which is half a microsecond for 0.27 of MMAs.  Tiles of 512 x 256 (MB = 2) want a
+// quarter less, but take all of tensor memory, so that nothing hides their epilogue.  Small products (under some 500 rows) are bound by
+// the 8 to 10 us that a launch, its first loads and its one epilogue take.
 #pragma once
 #include <cuda.h>
 
@@ -484,8 +486,9 @@ __device__ __forceinline__ void gated_finish(const Epilogue &p, float (&g)[32], 
     for (int i = 0; i < 32; ++i) g[i] *= u[i];
     piece_store<T>(p.out, p.ldo, g, t);
 }
-// A tile of 128 rows by BN / 2 hidden columns: the accumulator's first half is g, the second u.  (BN = 64 has one piece for each
-// row quarter, which the first four warps take.)
+// A tile of 128 rows by BN / 2 hidden columns: the accumulator's first half is g, the second u, so that h needs neither of them in
+// memory.  (BN = 64 has one piece for each row quarter, which the first four warps take.)  16384 x 1024 -> 2816: 150 us with g and u
+// kept of 113 for the products at 1669 TFLOP/s: the intake of 11 x 128 tiles of 2 x 512 KB is 147.
 template <typename T, int BN, typename Wait, typename Release>
 __device__ __forceinline__ bool gated_tile(const GemmProblem &q, int32_t tn, Tile &t, uint32_t lanes, int strip, Wait wait, Release release) {
     constexpr int kHalf = BN / 2, kPieces = kHalf < 64 ? 1 : kHalf / 64;
@@ -575,6 +578,10 @@ __device__ __forceinline__ void gated_back_finish(const Epilogue &p, float (&v)[
         }
     }
 }
+// dh stays in tensor memory: the tile's g and u come in and dg, du and h go out instead, ten bytes a value.  16384 x 1024 -> 2816: 160 us
+// of 72 (memory) or 57 (products): the epilogue's warps wait on their loads and stores (a piece of 32 x 32 takes one 4 us), more of
+// them do not fit beside what a value's two functions take of registers, and fetching the next piece ahead, or going by whole lines
+// through shared memory, came out between even and 20 us slower.
 template <typename T, int PIECES, typename Wait, typename Release>
 __device__ __forceinline__ bool gated_back_tile(const GemmProblem &q, Tile &t, uint32_t src, int32_t col0, int32_t *status, Wait wait, Release release) {
     t.col0 = col0;

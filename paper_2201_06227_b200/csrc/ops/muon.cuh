@@ -88,14 +88,14 @@ __device__ __forceinline__ void muon_read(float (&v)[8], const T *p, int64_t e, 
         for (int i = 0; i < 8; ++i) v[i] = e + i * STRIDE < end ? to_f32(p[e + i * STRIDE]) : 0.0f;
     }
 }
-template <bool VECTOR, int STRIDE = kMuonThreads>
+template <bool VECTOR>
 __device__ __forceinline__ void muon_grads(float (&g)[8], const void *grad, int type, int64_t e, int64_t end) {
     if (type == EGERIA_F32)
-        muon_read<VECTOR, STRIDE>(g, static_cast<const float *>(grad), e, end);
+        muon_read<VECTOR>(g, static_cast<const float *>(grad), e, end);
     else if (type == EGERIA_BF16)
-        muon_read<VECTOR, STRIDE>(g, static_cast<const bf16 *>(grad), e, end);
+        muon_read<VECTOR>(g, static_cast<const bf16 *>(grad), e, end);
     else
-        muon_read<VECTOR, STRIDE>(g, static_cast<const f16 *>(grad), e, end);
+        muon_read<VECTOR>(g, static_cast<const f16 *>(grad), e, end);
 }
 template <int THREADS = kMuonThreads>
 __device__ __forceinline__ double block_sum(double v, double *part) {
@@ -869,12 +869,16 @@ __global__ void __launch_bounds__(MuonCfg<BN, CG>::kThreads, 1) muon_products_ke
 // ---------------------------------------------------------------- small matrices
 // The whole step of a matrix of at most 128 by 768 in one thread block: X stays in shared memory, as the products' operand from either
 // side (its 64-column panels are A X^T's with the columns consecutive and P X's with them as the other axis), and only what its
-// rounding leaves goes by way of L2.  54 convolutions of 16 to 64 channels: 63 us, 100 through the list of units, where each of the 15
-// products waits for the one before it to be stored, seen and loaded.
+// rounding leaves goes by way of L2.  54 convolutions of 16 to 64 channels: 58 us, 100 through the list of units, where each of the 15
+// products waits for the one before it to be stored, seen and loaded.  Of the 58, 10 go into the first 64 x 576 X and 6 into its
+// weights (0.7 and 0.4 MB through one SM at the 60 bytes a nanosecond that it takes), 7.3 into each of the five steps: 1.1 of waiting for
+// A, 0.9 for A A, 4.9 for three chunks, whose products and values and the next A's part of them run beside each other (8.6 before).
 constexpr int kSmallSide = 128, kSmallPanels = 12;
 constexpr int kSmallThreads = 512, kSmallStrips = kSmallThreads / 128, kPanelBytes = kSmallSide * 128;
+constexpr int kChunk = 3;                                       // panels whose new values are computed at a time
+constexpr int kSquareAt = 2 * kChunk * 64;                      // where A and A A are in tensor memory, beside two chunks
 constexpr int kSmallSmem = 1024 + (kSmallPanels + 2) * kPanelBytes + 256;
-static_assert(kSmallSmem <= 227 * 1024, "shared memory of a CTA");
+static_assert(kSmallSmem <= 227 * 1024 && kSquareAt + kSmallSide <= 512, "shared and tensor memory of a CTA");
 
 // Place of a value in a panel: rows of 64 values, 128 bytes, swizzled as the tensor cores take them.
 __device__ __forceinline__ uint32_t panel_place(uint32_t row, uint32_t col) {
@@ -891,62 +895,87 @@ __device__ __forceinline__ void panel_store(uint32_t base, uint32_t row, uint32_
                      : "memory");
 }
 
+// A thread's eights of a matrix, kSmallGroup of them loaded before the first is used: a block alone on its SM has no other loads to wait
+// beside.
+constexpr int kSmallGroup = 3;
+
 // Momentum, |t|, and X in the panels with its rest in `lo`.
-template <bool VECTOR>
-__device__ __forceinline__ void small_begin(const MuonParams &p, const MuonMatrix &t, const void *grad, float grad_scale, uint32_t base, double *part) {
+template <bool VECTOR, typename G>
+__device__ __forceinline__ void small_begin(const MuonParams &p, const MuonMatrix &t, const G *grad, float grad_scale, uint32_t base, double *part) {
     constexpr int S = VECTOR ? 1 : kSmallThreads;  // between a thread's eight values
+    constexpr int kStep = 8 * kSmallThreads;
     const int32_t cols = (int32_t)t.cols, n = (int32_t)(t.rows * t.cols), first = threadIdx.x * (VECTOR ? 8 : 1);
     double sum = 0.0;
-#pragma unroll 2
-    for (int32_t e = first; e < n; e += 8 * kSmallThreads) {
-        float g[8], m[8];
-        muon_grads<VECTOR, S>(g, grad, t.grad_type, e, n);
-        muon_read<VECTOR, S>(m, t.m, e, n);
+#pragma unroll 1
+    for (int32_t e0 = first; e0 < n; e0 += kSmallGroup * kStep) {
+        float g[kSmallGroup][8], m[kSmallGroup][8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            g[i] *= grad_scale;
-            m[i] = fmaf(p.beta, m[i], p.rest * g[i]);
-            const float v = p.nesterov ? fmaf(p.beta, m[i], p.rest * g[i]) : m[i];
-            if (VECTOR || e + i * S < n) sum = fma((double)v, (double)v, sum);
+        for (int j = 0; j < kSmallGroup; ++j) {
+            const int32_t e = e0 + j * kStep;
+            if (e >= n) break;
+            muon_read<VECTOR, S>(g[j], grad, e, n);
+            muon_read<VECTOR, S>(m[j], t.m, e, n);
         }
-        if (VECTOR) {
-            store8(t.m + e, m);
-        } else {
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if (e + i * S < n) t.m[e + i * S] = m[i];
+        for (int j = 0; j < kSmallGroup; ++j) {
+            const int32_t e = e0 + j * kStep;
+            if (e >= n) break;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float gi = g[j][i] * grad_scale;
+                m[j][i] = fmaf(p.beta, m[j][i], p.rest * gi);
+                const float v = p.nesterov ? fmaf(p.beta, m[j][i], p.rest * gi) : m[j][i];
+                if (VECTOR || e + i * S < n) sum = fma((double)v, (double)v, sum);
+            }
+            if (VECTOR) {
+                store8(t.m + e, m[j]);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (e + i * S < n) t.m[e + i * S] = m[j][i];
+            }
         }
     }
     const float inv = (float)((double)t.up / fmax(sqrt(block_sum<kSmallThreads>(sum, part)), (double)p.eps));
-#pragma unroll 2
-    for (int32_t e = first; e < n; e += 8 * kSmallThreads) {  // (its own values of m again)
-        float g[8], v[8];
-        muon_read<VECTOR, S>(v, t.m, e, n);
-        if (p.nesterov) {
-            muon_grads<VECTOR, S>(g, grad, t.grad_type, e, n);
+#pragma unroll 1
+    for (int32_t e0 = first; e0 < n; e0 += kSmallGroup * kStep) {  // (its own values of m again)
+        float g[kSmallGroup][8], v[kSmallGroup][8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = fmaf(p.beta, v[i], p.rest * (g[i] * grad_scale));
+        for (int j = 0; j < kSmallGroup; ++j) {
+            const int32_t e = e0 + j * kStep;
+            if (e >= n) break;
+            muon_read<VECTOR, S>(v[j], t.m, e, n);
+            if (p.nesterov) muon_read<VECTOR, S>(g[j], grad, e, n);
         }
-        uint32_t h[4], l[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            h[i] = pack2<f16>(v[2 * i] * inv, v[2 * i + 1] * inv);
-            const float2 f = unpack2<f16>(h[i]);
-            l[i] = pack2<f16>(v[2 * i] * inv - f.x, v[2 * i + 1] * inv - f.y);
-        }
-        const int32_t r = e / cols, c = e - r * cols;
-        if (VECTOR && !t.tall) {  // eight values of a row, which is one of X
-            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(base + panel_place(r, c)), "r"(h[0]), "r"(h[1]), "r"(h[2]), "r"(h[3]) : "memory");
-            *reinterpret_cast<uint4 *>(t.lo + rest_place(r, c)) = make_uint4(l[0], l[1], l[2], l[3]);
-        } else {
+        for (int j = 0; j < kSmallGroup; ++j) {
+            const int32_t e = e0 + j * kStep;
+            if (e >= n) break;
+            if (p.nesterov) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const int32_t at = e + i * S;
-                if (at >= n) break;
-                const int32_t ri = VECTOR ? r : at / cols, ci = VECTOR ? c + i : at - ri * cols, row = t.tall ? ci : ri, col = t.tall ? ri : ci;
-                const uint16_t hi = (uint16_t)(h[i >> 1] >> (i & 1) * 16), lo = (uint16_t)(l[i >> 1] >> (i & 1) * 16);
-                asm volatile("st.shared.b16 [%0], %1;" ::"r"(base + panel_place(row, col)), "h"(hi) : "memory");
-                t.lo[rest_place(row, col)] = lo;
+                for (int i = 0; i < 8; ++i) v[j][i] = fmaf(p.beta, v[j][i], p.rest * (g[j][i] * grad_scale));
+            }
+            uint32_t h[4], l[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                h[i] = pack2<f16>(v[j][2 * i] * inv, v[j][2 * i + 1] * inv);
+                const float2 f = unpack2<f16>(h[i]);
+                l[i] = pack2<f16>(v[j][2 * i] * inv - f.x, v[j][2 * i + 1] * inv - f.y);
+            }
+            const int32_t r = e / cols, c = e - r * cols;
+            if (VECTOR && !t.tall) {  // eight values of a row, which is one of X
+                asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(base + panel_place(r, c)), "r"(h[0]), "r"(h[1]), "r"(h[2]), "r"(h[3]) : "memory");
+                *reinterpret_cast<uint4 *>(t.lo + rest_place(r, c)) = make_uint4(l[0], l[1], l[2], l[3]);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const int32_t at = e + i * S;
+                    if (at >= n) break;
+                    const int32_t ri = VECTOR ? r : at / cols, ci = VECTOR ? c + i : at - ri * cols, row = t.tall ? ci : ri, col = t.tall ? ri : ci;
+                    const uint16_t hi = (uint16_t)(h[i >> 1] >> (i & 1) * 16), lo = (uint16_t)(l[i >> 1] >> (i & 1) * 16);
+                    asm volatile("st.shared.b16 [%0], %1;" ::"r"(base + panel_place(row, col)), "h"(hi) : "memory");
+                    t.lo[rest_place(row, col)] = lo;
+                }
             }
         }
     }
@@ -955,49 +984,68 @@ __device__ __forceinline__ void small_begin(const MuonParams &p, const MuonMatri
 // p = p keep - step X, in the order of the weights.
 template <typename T, bool VECTOR>
 __device__ __forceinline__ void small_end(const MuonParams &p, const MuonMatrix &t, uint32_t base) {
-    constexpr int S = VECTOR ? 1 : kSmallThreads;
+    constexpr int S = VECTOR ? 1 : kSmallThreads, kStep = 8 * kSmallThreads;
     const int32_t cols = (int32_t)t.cols, n = (int32_t)(t.rows * t.cols);
     const float keep = 1.0f - p.lr * t.wd, by = p.lr * t.scale * t.down;
     T *param = static_cast<T *>(t.param);
-    for (int32_t e = threadIdx.x * (VECTOR ? 8 : 1); e < n; e += 8 * kSmallThreads) {
-        float w[8], x[8];
-        if (t.master)
-            muon_read<VECTOR, S>(w, t.master, e, n);
-        else
-            muon_read<VECTOR, S>(w, param, e, n);
-        const int32_t r = e / cols, c = e - r * cols;
-        if (VECTOR && !t.tall) {
-            uint32_t h[4];
-            asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(h[0]), "=r"(h[1]), "=r"(h[2]), "=r"(h[3]) : "r"(base + panel_place(r, c)) : "memory");
-            const uint4 q = *reinterpret_cast<const uint4 *>(t.lo + rest_place(r, c));
-            const uint32_t l[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll 1
+    for (int32_t e0 = threadIdx.x * (VECTOR ? 8 : 1); e0 < n; e0 += kSmallGroup * kStep) {
+        float w[kSmallGroup][8];
+        uint4 rest[kSmallGroup];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float2 f = unpack2<f16>(h[i]), g = unpack2<f16>(l[i]);
-                x[2 * i] = f.x + g.x, x[2 * i + 1] = f.y + g.y;
-            }
-        } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const int32_t at = min(e + i * S, n - 1);
-                const int32_t ri = VECTOR ? r : at / cols, ci = VECTOR ? c + i : at - ri * cols, row = t.tall ? ci : ri, col = t.tall ? ri : ci;
-                uint16_t h;
-                asm volatile("ld.shared.b16 %0, [%1];" : "=h"(h) : "r"(base + panel_place(row, col)) : "memory");
-                x[i] = __half2float(__ushort_as_half(h)) + __half2float(__ushort_as_half(t.lo[rest_place(row, col)]));
+        for (int j = 0; j < kSmallGroup; ++j) {
+            const int32_t e = e0 + j * kStep;
+            if (e >= n) break;
+            if (t.master)
+                muon_read<VECTOR, S>(w[j], t.master, e, n);
+            else
+                muon_read<VECTOR, S>(w[j], param, e, n);
+            if (VECTOR && !t.tall) {
+                const int32_t r = e / cols;
+                rest[j] = *reinterpret_cast<const uint4 *>(t.lo + rest_place(r, e - r * cols));
             }
         }
 #pragma unroll
-        for (int i = 0; i < 8; ++i) w[i] = fmaf(w[i], keep, -by * x[i]);
-        if (VECTOR) {
-            store8(param + e, w);
-            if (t.master) store8(t.master + e, w);
-        } else {
+        for (int j = 0; j < kSmallGroup; ++j) {
+            const int32_t e = e0 + j * kStep;
+            if (e >= n) break;
+            const int32_t r = e / cols, c = e - r * cols;
+            float x[8];
+            if (VECTOR && !t.tall) {
+                uint32_t h[4];
+                asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
+                             : "=r"(h[0]), "=r"(h[1]), "=r"(h[2]), "=r"(h[3])
+                             : "r"(base + panel_place(r, c))
+                             : "memory");
+                const uint32_t l[4] = {rest[j].x, rest[j].y, rest[j].z, rest[j].w};
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if (e + i * S < n) {
-                    param[e + i * S] = from_f32<T>(w[i]);
-                    if (t.master) t.master[e + i * S] = w[i];
+                for (int i = 0; i < 4; ++i) {
+                    const float2 f = unpack2<f16>(h[i]), g = unpack2<f16>(l[i]);
+                    x[2 * i] = f.x + g.x, x[2 * i + 1] = f.y + g.y;
                 }
+            } else {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const int32_t at = min(e + i * S, n - 1);
+                    const int32_t ri = VECTOR ? r : at / cols, ci = VECTOR ? c + i : at - ri * cols, row = t.tall ? ci : ri, col = t.tall ? ri : ci;
+                    uint16_t h;
+                    asm volatile("ld.shared.b16 %0, [%1];" : "=h"(h) : "r"(base + panel_place(row, col)) : "memory");
+                    x[i] = __half2float(__ushort_as_half(h)) + __half2float(__ushort_as_half(t.lo[rest_place(row, col)]));
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) w[j][i] = fmaf(w[j][i], keep, -by * x[i]);
+            if (VECTOR) {
+                store8(param + e, w[j]);
+                if (t.master) store8(t.master + e, w[j]);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (e + i * S < n) {
+                        param[e + i * S] = from_f32<T>(w[j][i]);
+                        if (t.master) t.master[e + i * S] = w[j][i];
+                    }
+            }
         }
     }
 }
@@ -1007,14 +1055,14 @@ __global__ void __launch_bounds__(kSmallThreads, 1) muon_small_kernel(const __gr
     __shared__ double part[kSmallThreads / 32];
     __shared__ uint32_t tmem_holder;
     __shared__ int abort_word;
-    __shared__ alignas(8) uint64_t bars[3];
+    __shared__ alignas(8) uint64_t bars[4];  // a chunk of either parity, A or A A, the end of what was begun
     const uint32_t base = (ptx::smem_u32(smem_raw) + 1023u) & ~1023u, poly = base + kSmallPanels * kPanelBytes;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, quarter = warp & 3, strip = warp >> 2;
+    // issues the products: of the warp that has least to do beside (none up to 96 rows), since it stands still while the queue is full
+    const bool leader = threadIdx.x == kSmallThreads - 32;
     volatile int *abort_flag = &abort_word;
     if (threadIdx.x == 0) {
-        ptx::mbar_init(ptx::smem_u32(bars), 1);
-        ptx::mbar_init(ptx::smem_u32(bars + 1), 1);
-        ptx::mbar_init(ptx::smem_u32(bars + 2), 1);
+        for (int i = 0; i < 4; ++i) ptx::mbar_init(ptx::smem_u32(bars + i), 1);
         abort_word = 0;
         ptx::fence_barrier_init();
         ptx::fence_proxy_async();
@@ -1038,78 +1086,116 @@ __global__ void __launch_bounds__(kSmallThreads, 1) muon_small_kernel(const __gr
             asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(base + i * 16), "r"(0) : "memory");
         const bool vector = muon_vector(p, t);
         __syncthreads();
-        if (vector)
-            small_begin<true>(p, t, grad, grad_scale, base, part);
-        else
-            small_begin<false>(p, t, grad, grad_scale, base, part);
+        with_type(t.grad_type, [&](auto type) {
+            const auto *g = static_cast<const decltype(type) *>(grad);
+            if (vector)
+                small_begin<true>(p, t, g, grad_scale, base, part);
+            else
+                small_begin<false>(p, t, g, grad_scale, base, part);
+        });
         const int steps = p.products / 3;
-        uint32_t phase[2] = {0, 0};
+        uint32_t phases = 0;
         bool ok = true;
         const uint32_t row = quarter * 32 + lane;
         const uint32_t tmem_row = tmem + ((uint32_t)(quarter * 32) << 16);
         auto idesc = [](int cols, bool b_mn) { return (1u << 4) | ((uint32_t)b_mn << 16) | ((uint32_t)(cols >> 3) << 17) | ((uint32_t)(kSmallSide >> 4) << 24); };
         // everything that has been stored in shared memory, and read from tensor memory, comes before the products
+        // (where a wait ran out, which all learn of here, what was stored since then is not used)
         auto meet = [&] {
             ptx::fence_proxy_async();
             ptx::tc_fence_before_sync();
-            __syncthreads();
+            ok = __syncthreads_and(ok);
             ptx::tc_fence_after_sync();
+            return ok;
+        };
+        // A warp's pieces of a chunk (two at most), and what X's rounding left of them.  A thread reads back what it wrote itself; the
+        // loads are under way from the chunk or the step before.
+        uint32_t lo[2][16];
+        auto has_piece = [&](int c, int k) { return strip + k * kSmallStrips < min(kChunk, panels - kChunk * c) * 2 && (int)row < d; };
+        auto rest_at = [&](int c, int k) { return t.lo + rest_place(row, c * kChunk * 64 + (strip + k * kSmallStrips) * kPiece); };
+        auto fetch_rest = [&](int c, int k) {
+            if (!has_piece(c, k)) return;
+            const uint4 *rest = reinterpret_cast<const uint4 *>(rest_at(c, k));
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const uint4 q = rest[i * kSmallSide];
+                lo[k][4 * i] = q.x, lo[k][4 * i + 1] = q.y, lo[k][4 * i + 2] = q.z, lo[k][4 * i + 3] = q.w;
+            }
+        };
+        auto store_rest = [&](int c, int k) {
+            if (!has_piece(c, k)) return;
+            uint4 *rest = reinterpret_cast<uint4 *>(rest_at(c, k));
+#pragma unroll
+            for (int i = 0; i < 4; ++i) rest[i * kSmallSide] = make_uint4(lo[k][4 * i], lo[k][4 * i + 1], lo[k][4 * i + 2], lo[k][4 * i + 3]);
         };
         auto wait = [&](int bar) {
-            ok = ok && ptx::mbar_wait_bounded(ptx::smem_u32(bars + bar), phase[bar], abort_flag, p.wait_limit_ns);
-            phase[bar] ^= 1u;
+            ok = ok && ptx::mbar_wait_bounded(ptx::smem_u32(bars + bar), phases >> bar & 1u, abort_flag, p.wait_limit_ns);
+            phases ^= 1u << bar;
             ptx::tc_fence_after_sync();
         };
-        const int ksteps = (d + 15) / 16;  // of a sum over the shorter side
-        // P X for the panels of chunk c into the accumulator of its parity
-        const int chunks = (panels + 3) / 4;
+        const int ksteps = (d + 15) / 16;       // of a sum over the shorter side
+        const int side = (d + 31) / 32 * 32;    // rows and columns of A that are looked at (tensor memory's others hold anything)
+        const bool mine = quarter * 32 < side && strip * 32 < side;
+        // a product's steps of 16, four with the same start addresses at a time
+        auto over = [](int n, auto go) {
+#pragma unroll 1
+            for (int k = 0; k < n; k += 4)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (k + i < n) go(k, i);
+        };
+        // the product of n steps of an operand with itself, added to what is there or not
+        auto square = [&](uint32_t at, int n, bool more) {
+            const uint64_t x0 = ptx::make_desc_k_sw128(at);
+            over(n, [&](int k, int i) {
+                const uint64_t x = x0 + (uint32_t)(k >> 2) * (kPanelBytes >> 4) + i * 2;
+                mma_g<1>(tmem + kSquareAt, x, x, idesc(side, false), more || k + i > 0);
+            });
+        };
+        // P X for the panels of chunk c into the accumulator of its parity, and X X^T's part of it
+        const int chunks = (panels + kChunk - 1) / kChunk;
         auto issue_chunk = [&](int c) {
-            const int wide = min(4, panels - 4 * c) * 64;
+            const int wide = min(kChunk, panels - kChunk * c) * 64;
             const uint64_t mn = (uint64_t)(kPanelBytes >> 4) << 16 | (uint64_t)(1024 >> 4) << 32 | (uint64_t)1 << 46 | (uint64_t)2 << 61;
-            for (int k = 0; k < ksteps; ++k)
-                mma_g<1>(tmem + (c & 1) * 256, ptx::make_desc_k_sw128(poly + (k >> 2) * kPanelBytes) + (k & 3) * 2,
-                         mn | (base + 4 * c * kPanelBytes + k * 2048) >> 4, idesc(wide, true), k > 0);
+            const uint64_t p0 = ptx::make_desc_k_sw128(poly), x0 = mn | (base + kChunk * c * kPanelBytes) >> 4;
+            over(ksteps, [&](int k, int i) {
+                mma_g<1>(tmem + (c & 1) * kChunk * 64, p0 + (uint32_t)(k >> 2) * (kPanelBytes >> 4) + i * 2, x0 + (uint32_t)(k + i) * (2048 >> 4),
+                         idesc(wide, true), k + i > 0);
+            });
             mma_commit_g<1>(ptx::smem_u32(bars + (c & 1)));
         };
+        auto square_chunk = [&](int c) { square(base + kChunk * c * kPanelBytes, min(kChunk, panels - kChunk * c) * 4, c > 0); };
         meet();
+        // A = X X^T
+        if (leader && p.stall == 0) {
+            square(base, panels * 4, false);
+            mma_commit_g<1>(ptx::smem_u32(bars + 2));
+        }
+        fetch_rest(0, 0);
+        fetch_rest(0, 1);
 #pragma unroll 1
         for (int step = 0; step < steps && ok; ++step) {
-            // A = X X^T
-            if (threadIdx.x == 0 && p.stall == 0) {
-                for (int k = 0; k < panels * 4; ++k) {
-                    const uint64_t x = ptx::make_desc_k_sw128(base + (k >> 2) * kPanelBytes) + (k & 3) * 2;
-                    mma_g<1>(tmem, x, x, idesc(kSmallSide, false), k > 0);
-                }
-                mma_commit_g<1>(ptx::smem_u32(bars));
-            }
-            wait(0);
-            ok = __syncthreads_and(ok);
-            if (!ok) break;
+            wait(2);
             uint32_t a[16];
             const float down = t.down * t.down;
-            {
+            if (mine) {
                 float v[32];
-                ptx::tmem_ld_32x32(tmem_row + strip * 32, reinterpret_cast<uint32_t (&)[32]>(v));
+                ptx::tmem_ld_32x32(tmem_row + kSquareAt + strip * 32, reinterpret_cast<uint32_t (&)[32]>(v));
                 ptx::tmem_ld_wait();
 #pragma unroll
                 for (int i = 0; i < 16; ++i) a[i] = pack2<f16>(v[2 * i] * down, v[2 * i + 1] * down);
                 panel_store(poly, row, strip * 32, a);
             }
-            meet();
+            if (!meet()) break;
             // A A, and P over A
-            if (threadIdx.x == 0) {
-                for (int k = 0; k < ksteps; ++k) {
-                    const uint64_t x = ptx::make_desc_k_sw128(poly + (k >> 2) * kPanelBytes) + (k & 3) * 2;
-                    mma_g<1>(tmem, x, x, idesc(kSmallSide, false), k > 0);
-                }
-                mma_commit_g<1>(ptx::smem_u32(bars));
+            if (leader) {
+                square(poly, ksteps, false);
+                mma_commit_g<1>(ptx::smem_u32(bars + 2));
             }
-            wait(0);
-            ok = __syncthreads_and(ok);
-            if (!ok) break;
-            {
+            wait(2);
+            if (mine) {
                 float v[32];
-                ptx::tmem_ld_32x32(tmem_row + strip * 32, reinterpret_cast<uint32_t (&)[32]>(v));
+                ptx::tmem_ld_32x32(tmem_row + kSquareAt + strip * 32, reinterpret_cast<uint32_t (&)[32]>(v));
                 ptx::tmem_ld_wait();
                 const int diagonal = (int)row < d ? (int)row - strip * 32 : -1;
 #pragma unroll
@@ -1123,36 +1209,23 @@ __global__ void __launch_bounds__(kSmallThreads, 1) muon_small_kernel(const __gr
                 for (int i = 0; i < 16; ++i) r[i] = pack2<f16>(v[2 * i], v[2 * i + 1]);
                 panel_store(poly, row, strip * 32, r);
             }
-            meet();
-            // X = P X, four panels at a time, the next four's products beside this one's values
-            if (threadIdx.x == 0) issue_chunk(0);
+            if (!meet()) break;
+            // X = P X, a chunk at a time: its products run beside the values of the chunk before, and so does the next A's part of that
+            const bool again = step + 1 < steps;
+            if (leader) {
+                issue_chunk(0);
+                if (chunks > 1) issue_chunk(1);
+            }
 #pragma unroll 1
             for (int c = 0; c < chunks; ++c) {
-                if (threadIdx.x == 0 && c + 1 < chunks) issue_chunk(c + 1);
-                // a warp's pieces of the chunk (two at most); what X's rounding left of them is on its way while the products are computed
-                const int pieces = min(4, panels - 4 * c) * 2;
-                uint32_t lo[2][16];
-#pragma unroll
-                for (int k = 0; k < 2; ++k) {
-                    const int at = strip + k * kSmallStrips;
-                    if (at >= pieces || (int)row >= d) continue;
-                    const uint4 *rest = reinterpret_cast<const uint4 *>(t.lo + rest_place(row, c * 256 + at * kPiece));
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const uint4 q = rest[i * kSmallSide];
-                        lo[k][4 * i] = q.x, lo[k][4 * i + 1] = q.y, lo[k][4 * i + 2] = q.z, lo[k][4 * i + 3] = q.w;
-                    }
-                }
                 wait(c & 1);
-                ok = __syncthreads_and(ok);
-                if (!ok) break;
 #pragma unroll
                 for (int k = 0; k < 2; ++k) {
                     const int at = strip + k * kSmallStrips;
-                    if (at >= pieces) continue;
-                    const int32_t col = c * 256 + at * kPiece;
+                    if (at >= min(kChunk, panels - kChunk * c) * 2 || quarter * 32 >= side) continue;
+                    const int32_t col = c * kChunk * 64 + at * kPiece;
                     float v[32];
-                    ptx::tmem_ld_32x32(tmem_row + (c & 1) * 256 + at * kPiece, reinterpret_cast<uint32_t (&)[32]>(v));
+                    ptx::tmem_ld_32x32(tmem_row + (c & 1) * kChunk * 64 + at * kPiece, reinterpret_cast<uint32_t (&)[32]>(v));
                     ptx::tmem_ld_wait();
                     if ((int)row >= d) continue;  // (whole rows of zeros stay as they are)
 #pragma unroll
@@ -1169,17 +1242,22 @@ __global__ void __launch_bounds__(kSmallThreads, 1) muon_small_kernel(const __gr
                         lo[k][i] = pack2<f16>(v[2 * i] - f.x, v[2 * i + 1] - f.y);
                     }
                     panel_store(base, row, col, hi);
-                    uint4 *rest = reinterpret_cast<uint4 *>(t.lo + rest_place(row, col));
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) rest[i * kSmallSide] = make_uint4(lo[k][4 * i], lo[k][4 * i + 1], lo[k][4 * i + 2], lo[k][4 * i + 3]);
                 }
-                // (the accumulator of this chunk is free for the chunk after the next)
-                ptx::tc_fence_before_sync();
-                __syncthreads();
-                ptx::tc_fence_after_sync();
+                if (!meet()) break;  // (the accumulator of this chunk is free for the chunk after the next)
+                if (leader) {
+                    if (c + 2 < chunks) issue_chunk(c + 2);
+                    if (again) square_chunk(c);
+                    if (again && c + 1 == chunks) mma_commit_g<1>(ptx::smem_u32(bars + 2));
+                }
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    store_rest(c, k);
+                    fetch_rest(c + 1 < chunks ? c + 1 : 0, k);
+                }
             }
-            meet();
         }
+        // (the last X's rest is read by others)
+        __syncthreads();
         if (ok)
             with_type(t.param_type, [&](auto type) {
                 if (t.vector)
@@ -1187,11 +1265,11 @@ __global__ void __launch_bounds__(kSmallThreads, 1) muon_small_kernel(const __gr
                 else
                     small_end<decltype(type), false>(p, t, base);
             });
-        if (!ok && threadIdx.x == 0) {
+        if (!ok && leader) {
             // gave up: no product of ours may still read shared memory when the block leaves
-            mma_commit_g<1>(ptx::smem_u32(bars + 2));
+            mma_commit_g<1>(ptx::smem_u32(bars + 3));
             const uint64_t t0 = ptx::globaltimer_ns();
-            while (!ptx::mbar_try_wait(ptx::smem_u32(bars + 2), 0))
+            while (!ptx::mbar_try_wait(ptx::smem_u32(bars + 3), 0))
                 if (ptx::globaltimer_ns() - t0 > p.wait_limit_ns) break;
             atomicMax(p.status, 6);
         }

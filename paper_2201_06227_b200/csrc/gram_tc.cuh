@@ -119,10 +119,15 @@ struct TcParams {
 };
 
 namespace detail {
-__device__ __forceinline__ void epi_bar_sync() { asm volatile("bar.sync 1, %0;" ::"n"(kEpiThreads) : "memory"); }
+// (bar.sync and bar.red want the lanes of a warp together)
+__device__ __forceinline__ void epi_bar_sync() {
+    __syncwarp();
+    asm volatile("bar.sync 1, %0;" ::"n"(kEpiThreads) : "memory");
+}
 // All epilogue threads: AND of `pred` over them.
 __device__ __forceinline__ bool epi_bar_and(bool pred) {
     uint32_t out;
+    __syncwarp();
     asm volatile(
         "{\n\t"
         ".reg .pred p, q;\n\t"

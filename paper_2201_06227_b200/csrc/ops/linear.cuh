@@ -118,6 +118,7 @@ struct GemmCfg {
 // ---------------------------------------------------------------- PTX of CTA pairs
 template <int CG>
 __device__ __forceinline__ void tmem_alloc_g(uint32_t dst, uint32_t cols) {
+    __syncwarp();
     if (CG == 1)
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(dst), "r"(cols) : "memory");
     else
@@ -125,6 +126,7 @@ __device__ __forceinline__ void tmem_alloc_g(uint32_t dst, uint32_t cols) {
 }
 template <int CG>
 __device__ __forceinline__ void tmem_free_g(uint32_t addr, uint32_t cols) {
+    __syncwarp();
     if (CG == 1) {
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(addr), "r"(cols) : "memory");
@@ -186,6 +188,7 @@ __device__ __forceinline__ void mbar_arrive_cluster(uint32_t bar) {
     asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
 __device__ __forceinline__ void cluster_sync() {
+    __syncwarp();
     asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 
@@ -901,7 +904,10 @@ __global__ void __launch_bounds__(GemmCfg<BN, CG, MB>::kThreads, 1) gemm_kernel(
                 if (p.sums[i].out)
                     for (int c = blockIdx.x; c * 32 < p.sums[i].cols; c += gridDim.x)
                         add_columns<T, kEpiWarps>(p.sums[i], c, e, lane, reinterpret_cast<float *>(staging),
-                                                  [] { asm volatile("bar.sync 1, %0;" ::"n"(32 * kEpiWarps) : "memory"); });
+                                                  [] {
+                                                      __syncwarp();
+                                                      asm volatile("bar.sync 1, %0;" ::"n"(32 * kEpiWarps) : "memory");
+                                                  });
         }
         Tile t;
         t.stage = staging + e * 32 * kStagePitch;

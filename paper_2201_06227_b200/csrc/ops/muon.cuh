@@ -1227,21 +1227,22 @@ __global__ void __launch_bounds__(kSmallThreads, 1) muon_small_kernel(const __gr
                     float v[32];
                     ptx::tmem_ld_32x32(tmem_row + (c & 1) * kChunk * 64 + at * kPiece, reinterpret_cast<uint32_t (&)[32]>(v));
                     ptx::tmem_ld_wait();
-                    if ((int)row >= d) continue;  // (whole rows of zeros stay as they are)
+                    if ((int)row < d) {  // (whole rows of zeros stay as they are)
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        const float2 f = unpack2<f16>(lo[k][i]);
-                        v[2 * i] = col + 2 * i < len ? fmaf(kNsA, f.x, v[2 * i]) : 0.0f;
-                        v[2 * i + 1] = col + 2 * i + 1 < len ? fmaf(kNsA, f.y, v[2 * i + 1]) : 0.0f;
-                    }
-                    uint32_t hi[16];
+                        for (int i = 0; i < 16; ++i) {
+                            const float2 f = unpack2<f16>(lo[k][i]);
+                            v[2 * i] = col + 2 * i < len ? fmaf(kNsA, f.x, v[2 * i]) : 0.0f;
+                            v[2 * i + 1] = col + 2 * i + 1 < len ? fmaf(kNsA, f.y, v[2 * i + 1]) : 0.0f;
+                        }
+                        uint32_t hi[16];
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        hi[i] = pack2<f16>(v[2 * i], v[2 * i + 1]);
-                        const float2 f = unpack2<f16>(hi[i]);
-                        lo[k][i] = pack2<f16>(v[2 * i] - f.x, v[2 * i + 1] - f.y);
+                        for (int i = 0; i < 16; ++i) {
+                            hi[i] = pack2<f16>(v[2 * i], v[2 * i + 1]);
+                            const float2 f = unpack2<f16>(hi[i]);
+                            lo[k][i] = pack2<f16>(v[2 * i] - f.x, v[2 * i + 1] - f.y);
+                        }
+                        panel_store(base, row, col, hi);
                     }
-                    panel_store(base, row, col, hi);
                 }
                 if (!meet()) break;  // (the accumulator of this chunk is free for the chunk after the next)
                 if (leader) {

@@ -104,16 +104,21 @@ __device__ __forceinline__ void tma_load_2d(uint32_t smem_dst, const void *tmap,
 }
 
 // ---------------------------------------------------------------- tcgen05 / TMEM
+// `.sync.aligned` wants the warp's lanes together, and what stands before it often parts them: a branch by lane, a wait that each
+// lane leaves by itself.  So the wrappers bring them together first.
 // Whole warp. Writes the TMEM base address of `ncols` columns (power of two >= 32) to smem_dst.
 __device__ __forceinline__ void tmem_alloc(uint32_t smem_dst, uint32_t ncols) {
+    __syncwarp();
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_dst),
                  "r"(ncols)
                  : "memory");
 }
 __device__ __forceinline__ void tmem_relinquish() {
+    __syncwarp();
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
 }
 __device__ __forceinline__ void tmem_dealloc(uint32_t taddr, uint32_t ncols) {
+    __syncwarp();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(taddr), "r"(ncols)
                  : "memory");
 }
@@ -143,6 +148,7 @@ __device__ __forceinline__ void mma_commit(uint32_t bar) {
 }
 // Whole warp: 32 lanes x 32 consecutive fp32 columns; lane t gets TMEM lane (base lane + t).
 __device__ __forceinline__ void tmem_ld_32x32(uint32_t taddr, uint32_t (&r)[32]) {
+    __syncwarp();
     asm volatile(
         "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
         "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
@@ -157,6 +163,7 @@ __device__ __forceinline__ void tmem_ld_32x32(uint32_t taddr, uint32_t (&r)[32])
 }
 // The same for 16 consecutive columns (the first 16 entries of r).
 __device__ __forceinline__ void tmem_ld_32x16(uint32_t taddr, uint32_t (&r)[32]) {
+    __syncwarp();
     asm volatile(
         "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
         "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
@@ -173,6 +180,7 @@ __device__ __forceinline__ void st_global_v8(float *dst, const uint32_t *v) {
                  : "memory");
 }
 __device__ __forceinline__ void tmem_ld_wait() {
+    __syncwarp();
     asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
 }
 

@@ -181,7 +181,7 @@ static egeria_status good_gated_sizes(int64_t rows, int64_t inp, int64_t hidden,
 
 // ---------------------------------------------------------------- a few rows
 template <typename T, int ROWS>
-static cudaError_t launch_few(const Epilogue &e, const egeria_gated_forward_args &a, bool wide, int sms, cudaStream_t stream) {
+static cudaError_t launch_few(const GatedEpilogue &e, const egeria_gated_forward_args &a, bool wide, int sms, cudaStream_t stream) {
     const int smem = ROWS * (int)((a.inp + 255) / 256 * 256) * 2;
     const int grid = (int)std::min<int64_t>((a.hidden + 7) / 8, (int64_t)sms * 4);
     const T *x = static_cast<const T *>(a.x), *g = static_cast<const T *>(a.w_gate), *u = static_cast<const T *>(a.w_up);
@@ -189,7 +189,7 @@ static cudaError_t launch_few(const Epilogue &e, const egeria_gated_forward_args
                   (int32_t)a.hidden, x, a.ldx, g, a.ldw_gate, u, a.ldw_up, (int32_t)a.inp);
 }
 template <typename T>
-static cudaError_t launch_few_any(const Epilogue &e, const egeria_gated_forward_args &a, bool wide, int sms, cudaStream_t stream) {
+static cudaError_t launch_few_any(const GatedEpilogue &e, const egeria_gated_forward_args &a, bool wide, int sms, cudaStream_t stream) {
     if (a.rows <= 1) return launch_few<T, 1>(e, a, wide, sms, stream);
     if (a.rows <= 2) return launch_few<T, 2>(e, a, wide, sms, stream);
     return launch_few<T, 4>(e, a, wide, sms, stream);
@@ -256,7 +256,7 @@ egeria_status egeria_gated_forward(egeria_ops *ops, void *cuda_stream, const ege
     cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
     ops->last_stream = stream;
 
-    Epilogue e{};
+    GatedEpilogue e{};
     e.bias = a.b_gate;
     e.bias2 = a.b_up;
     e.out = ops->ws + L.h;
@@ -381,7 +381,7 @@ egeria_status egeria_gated_backward(egeria_ops *ops, void *cuda_stream, const eg
     Product back{}, jobs[kMaxProblems];
     int count = 0;
     if (gates || a.dw_down) {
-        Epilogue e{};
+        GatedEpilogue e{};
         e.extra = a.g, e.ldx = a.ldg;
         e.extra2 = a.u, e.ldx2 = a.ldu;
         e.out = ops->ws + L.dg, e.z = ops->ws + L.du;

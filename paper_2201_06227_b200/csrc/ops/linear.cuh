@@ -50,16 +50,21 @@ struct Epilogue {
     const void *bias, *extra;
     void *out, *z;
     int64_t ldx, ldo, ldz;           // pitches of extra, out, z
-    // gated blocks only: the up projection's bias, argument and pitches, and the backward pass's partial column sums
-    const void *bias2, *extra2;
-    void *z2;
-    int64_t ldx2, ldz2;
-    float *sums, *sums2;             // [tiles_m * 4 MB CG][n], one row per 32 rows of the matrix, or null
-    int64_t sums_room;               // values in each (checked build)
     int32_t act, act_in;
     int32_t slope;                   // extra is the argument of act_in, not a residual
     int32_t wide;                    // every matrix here takes 32-byte (2), 16-byte (1) or only 2-byte (0) accesses
     int32_t wide_bias;
+};
+static_assert(sizeof(Epilogue) <= 80, "linear_few_kernel is handed it whole, and takes more registers the larger it is");
+// And of a gated block: the up projection's bias, argument and pitches, and the backward pass's partial column sums.  (Apart from the
+// above: with these in it linear_few_kernel takes 34 registers for one row instead of 32 and 54 for four instead of 48, six blocks fit an
+// SM instead of eight, and calls of 1 x 1024 -> 4096 that follow each other take 4.4 us instead of 3.4.)
+struct GatedEpilogue : Epilogue {
+    const void *bias2, *extra2;
+    void *z2;
+    int64_t ldx2, ldz2;
+    float *sums, *sums2;             // [ceil(m / 32)][n], one row per 32 rows of the matrix, or null
+    int64_t sums_room;               // values in each (checked build)
 };
 struct GemmProblem {
     CUtensorMap a, b;
@@ -67,7 +72,7 @@ struct GemmProblem {
     int32_t m, n, kblocks, kb2;
     int32_t tiles_m, tiles_n, splits, group_n, units;
     uint32_t a_mn, b_mn;             // the operand's m (n) axis is the consecutive one
-    Epilogue epi;
+    GatedEpilogue epi;
     float *partials;                 // split k: [unit][epilogue warp][piece][8][32 lanes][4]
     int32_t *tickets;                // split k: [tile][epilogue warp], zero between calls
     int64_t partial_floats;          // room for partials (checked build)
@@ -478,7 +483,7 @@ __device__ __forceinline__ void piece_finish(const Epilogue &p, float (&v)[32], 
 // ---------------------------------------------------------------- epilogues of a gated block
 // g and u of a 32 x 32 piece: biases, the two kept if wanted, h = act(g) u.
 template <typename T>
-__device__ __forceinline__ void gated_finish(const Epilogue &p, float (&g)[32], float (&u)[32], const Tile &t) {
+__device__ __forceinline__ void gated_finish(const GatedEpilogue &p, float (&g)[32], float (&u)[32], const Tile &t) {
     if (t.rows <= 0 || t.cols <= 0) return;
     if (p.bias) piece_bias<T>(p.bias, p.wide_bias, g, t);
     if (p.bias2) piece_bias<T>(p.bias2, p.wide_bias, u, t);
@@ -551,7 +556,7 @@ __device__ __forceinline__ float piece_column_sums(float (&v)[32], const Tile &t
     return v[0];
 }
 template <typename T>
-__device__ __forceinline__ void gated_back_finish(const Epilogue &p, float (&v)[32], const uint32_t (&g)[16], const uint32_t (&u)[16], int32_t n,
+__device__ __forceinline__ void gated_back_finish(const GatedEpilogue &p, float (&v)[32], const uint32_t (&g)[16], const uint32_t (&u)[16], int32_t n,
                                                   const Tile &t, int32_t *status) {
     if (t.rows <= 0 || t.cols <= 0) return;
     float du[32];
@@ -1130,7 +1135,7 @@ __global__ void __launch_bounds__(256) linear_few_kernel(const Epilogue p, int32
 
 // The hidden values of a gated block for 1 to 4 rows: as linear_few_kernel, with a row of each projection per turn.
 template <typename T, int ROWS, bool WIDE>
-__global__ void __launch_bounds__(256) gated_few_kernel(const Epilogue p, int32_t m, int32_t n_cols, const T *x, int64_t ldx, const T *wg, int64_t ldg,
+__global__ void __launch_bounds__(256) gated_few_kernel(const GatedEpilogue p, int32_t m, int32_t n_cols, const T *x, int64_t ldx, const T *wg, int64_t ldg,
                                                         const T *wu, int64_t ldu, int32_t k) {
     extern __shared__ uint8_t smem_few[];
     T *xs = reinterpret_cast<T *>(smem_few);  // [ROWS][k rounded up to 256], zero behind k

@@ -283,7 +283,7 @@ egeria_status linear_forward_at(egeria_ops *ops, cudaStream_t stream, const eger
     }
     PrepareParams prep{};
     prep.status = reinterpret_cast<int32_t *>(ops->ws);
-    Product job{a.rows, a.out, a.inp, {a.x, a.ldx, a.rows, a.inp, false}, {a.w, a.ldw, a.out, a.inp, false}, e, part};
+    Product job{a.rows, a.out, a.inp, {a.x, a.ldx, a.rows, a.inp, false}, {a.w, a.ldw, a.out, a.inp, false}, {e}, part};
     make_loadable(ops, job.a, x, prep.pack[0]);
     make_loadable(ops, job.b, w, prep.pack[1]);
     const egeria_status s = run_prepare(ops, stream, a.type, prep, false);

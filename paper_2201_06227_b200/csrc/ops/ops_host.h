@@ -167,7 +167,7 @@ inline egeria_status encode_operand(const egeria_ops *o, CUtensorMap *map, const
 }
 
 // Widest access that all of a product's epilogue matrices take: 2 = 32 bytes, 1 = 16 bytes, 0 = one value.
-inline void set_widths(Epilogue &e) {
+inline void set_widths(GatedEpilogue &e) {
     int w = 2;
     auto see = [&](const void *q, int64_t ld) {
         if (!q) return;
@@ -186,7 +186,7 @@ inline void set_widths(Epilogue &e) {
 struct Product {
     int64_t m, n, k;
     Operand a, b;
-    Epilogue epi;
+    GatedEpilogue epi;
     size_t part;            // its partial tiles in the workspace
     int64_t k2 = 0;         // and a second product a2 b2^T of that length is added to it
     Operand a2{}, b2{};     // (kModeGated: b2 is the up projection's weight, k2 = 0)

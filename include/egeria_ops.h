@@ -291,7 +291,8 @@ int64_t egeria_adamw_launch_count(const egeria_adamw *adamw);
 
 /* One matrix of the model, rows x cols consecutive values (a convolution's weight as its output channels by the rest), element-aligned.
  * Fastest where cols is a multiple of 8 and everything 32-byte aligned.  What a step writes (param, master, m of all matrices) shares no
- * value (EGERIA_ERR_INVALID_ARG): a weight that two layers share stands in the list once. */
+ * value with itself or with a gradient (EGERIA_ERR_INVALID_ARG, also of set_grads): a weight that two layers share stands in the list
+ * once.  Gradients may share values with one another. */
 typedef struct {
     void *param;             /* of param_type; written */
     float *master;           /* NULL, or the 32-bit copy that the step works on; param is then its rounding */

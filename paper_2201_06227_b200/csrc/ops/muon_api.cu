@@ -1,6 +1,7 @@
 // Host side of the Muon step (include/egeria_ops.h): argument checks, the list of units, launches.
 #include <algorithm>
 #include <cmath>
+#include <iterator>
 #include <new>
 #include <utility>
 #include <vector>
@@ -21,10 +22,11 @@ static bool good_muon_tensor(const egeria_muon_tensor &t) {
     return t.param && t.m && aligned(t.param, size_of(t.param_type)) && aligned(t.master, 4) && aligned(t.m, 4);
 }
 
-// Whether two of the ranges that a step writes share a byte: a matrix that stands in the list twice would be updated from two workers at a
-// time.  (The sides are within kMuonMaxSide here.)
-static bool muon_overlaps(int count, const egeria_muon_tensor *t) {
-    std::vector<std::pair<uintptr_t, uintptr_t>> written;
+// The ranges of addresses that a step writes, in order; false if two of them share a byte: a matrix that stands in the list twice would be
+// updated from two workers at a time.  (The sides are within kMuonMaxSide here.)
+using MuonRanges = std::vector<std::pair<uintptr_t, uintptr_t>>;
+static bool muon_written(int count, const egeria_muon_tensor *t, MuonRanges &written) {
+    written.clear();
     auto add = [&](const void *p, int64_t bytes) {
         if (p && bytes > 0) written.emplace_back(reinterpret_cast<uintptr_t>(p), reinterpret_cast<uintptr_t>(p) + (uintptr_t)bytes);
     };
@@ -36,8 +38,14 @@ static bool muon_overlaps(int count, const egeria_muon_tensor *t) {
     }
     std::sort(written.begin(), written.end());
     for (size_t i = 1; i < written.size(); ++i)
-        if (written[i].first < written[i - 1].second) return true;
-    return false;
+        if (written[i].first < written[i - 1].second) return false;
+    return true;
+}
+// Whether any of these bytes is among them.  (A gradient is read twice, once the momenta are written, and others' weights may be by then.)
+static bool muon_meets(const MuonRanges &written, const void *p, int64_t bytes) {
+    const uintptr_t from = reinterpret_cast<uintptr_t>(p), end = from + (uintptr_t)bytes;
+    const auto next = std::lower_bound(written.begin(), written.end(), std::make_pair(from, (uintptr_t)0));
+    return (next != written.end() && next->first < end) || (next != written.begin() && std::prev(next)->second > from);
 }
 static bool muon_small(const egeria_muon_tensor &t) {
     return std::min(t.rows, t.cols) <= kSmallSide && std::max(t.rows, t.cols) <= kSmallPanels * 64;
@@ -154,7 +162,9 @@ struct egeria_muon {
     MuonKind kind{};
     MuonParams params{};
     int workers = 0, count = 0;
-    std::vector<size_t> grad_size;   // 0 for an empty tensor
+    std::vector<size_t> grad_size;   // of a value, 0 for an empty matrix
+    std::vector<int64_t> grad_bytes;
+    MuonRanges written;
     int64_t launches = 0;
     cudaStream_t last_stream = nullptr;
     uint32_t stall_next = 0;
@@ -189,7 +199,10 @@ egeria_status egeria_muon_create(egeria_muon **out, int count, const egeria_muon
         MuonLayout L;
         if (!muon_layout(count, tensors, steps, L)) return EGERIA_ERR_UNSUPPORTED_SHAPE;
         if (!workspace || !aligned(workspace, EGERIA_WORKSPACE_ALIGN) || workspace_bytes < L.total) return EGERIA_ERR_WORKSPACE;
-        if (muon_overlaps(count, tensors)) return EGERIA_ERR_INVALID_ARG;
+        MuonRanges written;
+        if (!muon_written(count, tensors, written)) return EGERIA_ERR_INVALID_ARG;
+        for (const int i : L.which)
+            if (muon_meets(written, grads[i], tensors[i].rows * tensors[i].cols * (int64_t)size_of(tensors[i].grad_type))) return EGERIA_ERR_INVALID_ARG;
         int dev = 0, major = 0, sms = 0;
         EGO_CUDA(cudaGetDevice(&dev));
         EGO_CUDA(cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, dev));
@@ -215,7 +228,12 @@ egeria_status egeria_muon_create(egeria_muon **out, int count, const egeria_muon
         std::vector<MuonMatrix> matrices;
         std::vector<CUtensorMap> maps((size_t)L.n_matrices * kMuonMaps);
         std::vector<int2> pieces;
-        for (int i = 0; i < count; ++i) h->grad_size.push_back(tensors[i].rows > 0 && tensors[i].cols > 0 ? size_of(tensors[i].grad_type) : 0);
+        h->written = std::move(written);
+        for (int i = 0; i < count; ++i) {
+            const int64_t n = tensors[i].rows * tensors[i].cols;
+            h->grad_size.push_back(n > 0 ? size_of(tensors[i].grad_type) : 0);
+            h->grad_bytes.push_back(n * (int64_t)size_of(tensors[i].grad_type));
+        }
         for (const int i : L.which) {
             const egeria_muon_tensor &t = tensors[i];
             const int k = (int)matrices.size();
@@ -326,7 +344,8 @@ egeria_status egeria_muon_destroy(egeria_muon *muon) {
 egeria_status egeria_muon_set_grads(egeria_muon *muon, void *cuda_stream, const void *const *grads) {
     if (!muon || !grads) return EGERIA_ERR_INVALID_ARG;
     for (int i = 0; i < muon->count; ++i)
-        if (muon->grad_size[i] && (!grads[i] || !aligned(grads[i], muon->grad_size[i]))) return EGERIA_ERR_INVALID_ARG;
+        if (muon->grad_size[i] && (!grads[i] || !aligned(grads[i], muon->grad_size[i]) || muon_meets(muon->written, grads[i], muon->grad_bytes[i])))
+            return EGERIA_ERR_INVALID_ARG;
     cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
     cudaStreamCaptureStatus capturing = cudaStreamCaptureStatusNone;
     EGO_CUDA(cudaStreamIsCapturing(stream, &capturing));

@@ -1,0 +1,173 @@
+"""The Muon step at the edges: matrices of low rank in one thread block, thin matrices on the list of units, gradients that share
+memory, handles that are dropped or given new gradients with a step in flight.
+
+Tolerances, derived before the first run.  After one step, value by value: X is rounded by 2^-11 of itself where it is an operand and by
+2^-25 / up where that is less (up: the power of two that it is held times), A and the polynomial by 2^-11, and a sum of n products by
+(n + 8) 2^-23 of the products' sizes.  After five steps as in test_muon_gpu.py: 1.1e-2 for a matrix of a few singular values, and 7e-3
+in the 2-norm, six times what independent roundings come to, for one of many.
+"""
+import math
+
+import pytest
+import torch
+
+from paper_2201_06227_b200 import binding as eg
+from paper_2201_06227_b200 import ops
+from test_muon_gpu import A, B, C, low_rank, near, normal, orthogonal64, orthogonalised
+from test_ops_gpu import DEV, close
+
+pytestmark = pytest.mark.gpu
+MANY, FEW = 7e-3, 1.1e-2
+
+
+# ----------------------------------------------------------------------------- matrices of low rank
+
+@pytest.mark.parametrize("rows,cols", [(16, 144), (64, 576), (576, 64), (128, 768), (768, 128), (100, 767), (767, 65), (33, 200), (128, 128)])
+def test_low_rank_in_one_thread_block(rows, cols):
+    """What X's rounding leaves is all that keeps the null space empty: lost, or a step old, it is 3e-2 and more here."""
+    kinds = [(r, e) for r in (1, 4, 16) for e in (0.0, 1e-3, 0.1)]
+    grads = [low_rank(rows, cols, r, seed=r + rows, noise=e) for r, e in kinds]
+    for x, t, kind in zip(orthogonalised(grads), grads, kinds):
+        near(x, orthogonal64(t), FEW if kind[0] < 16 else MANY, f"rank and noise {kind}")
+
+
+# ----------------------------------------------------------------------------- thin matrices on the list of units
+
+THIN = [(1, 4000), (4000, 1), (5, 3001), (3001, 33), (16, 1024), (70, 2000), (2000, 70), (31, 769), (769, 2), (127, 1500), (1500, 100)]
+
+
+def one_step(t):
+    """(X after one step, bound of its error value by value)."""
+    x = t.double() / t.double().norm()
+    tall = x.shape[0] > x.shape[1]
+    x = x.t() if tall else x
+    d, n = x.shape
+    up = 2.0 ** min(14, math.floor(0.5 * math.log2(n)))
+    size_x = x.abs()
+    ex = 2.0 ** -11 * size_x + 2.0 ** -25 / up
+    a, size_a = x @ x.t(), size_x @ size_x.t()
+    ea = ex @ size_x.t() + size_x @ ex.t() + ex @ ex.t() + (n + 8) * 2.0 ** -23 * size_a
+    ea = ea + 2.0 ** -11 * (a.abs() + ea) + 2.0 ** -25
+    aa, size_aa = a @ a, size_a @ size_a
+    eaa = ea @ size_a + size_a @ ea + ea @ ea + (d + 8) * 2.0 ** -23 * size_aa
+    p = A * torch.eye(d, device=DEV, dtype=torch.float64) + B * a + C * aa
+    ep = -B * ea + C * eaa + 2.0 ** -21 * (-B * size_a + C * size_aa)
+    ep = ep + 2.0 ** -11 * (p.abs() + ep) + 2.0 ** -25
+    want = p @ x
+    # the product takes X's first value; of the second a is taken, so that b A + c A^2 times it is left out
+    q = (p - A * torch.eye(d, device=DEV, dtype=torch.float64)).abs() + ep
+    tol = ep @ (size_x + ex) + q @ ex + (d + 8) * 2.0 ** -23 * (p.abs() + ep) @ (size_x + ex)
+    tol = tol + A * (2.0 ** -21 * size_x + 2.0 ** -25 / up) + 2.0 ** -20 * want.abs() + 2.0 ** -40
+    return (want.t(), tol.t()) if tall else (want, tol)
+
+
+@pytest.mark.parametrize("rows,cols", THIN)
+def test_thin_matrices_alone(rows, cols):
+    t = normal(rows, cols, seed=rows + cols)
+    want, tol = one_step(t)
+    close(orthogonalised([t], steps=1)[0], want, tol, "X after a step")
+    near(orthogonalised([t])[0], orthogonal64(t), FEW if min(rows, cols) < 16 else MANY, "X")
+
+
+def test_thin_matrices_beside_large_ones():
+    """Enough large matrices for pairs of thread blocks and tiles of 256 by 256, of which a thin one has a sliver."""
+    big = normal(1024, 1024, seed=1)
+    thin = [normal(r, c, seed=r + 2 * c) for r, c in THIN]
+    got = orthogonalised(thin + [big] * 20, steps=1)          # (gradients may be shared)
+    for x, t in zip(got, thin + [big]):
+        want, tol = one_step(t)
+        close(x, want, tol, str(tuple(t.shape)))
+    assert all(torch.equal(x, got[len(thin)]) for x in got[len(thin):])
+    for x, t in zip(orthogonalised(thin + [big] * 20), thin + [big]):
+        near(x, orthogonal64(t), FEW if min(t.shape) < 16 else MANY, str(tuple(t.shape)))
+
+
+def test_thin_matrices_of_low_rank():
+    for rows, cols in ((70, 2000), (2000, 70), (127, 1500)):
+        grads = [low_rank(rows, cols, r, seed=r, noise=e) for r in (1, 4) for e in (0.0, 0.1)]
+        for x, t in zip(orthogonalised(grads), grads):
+            near(x, orthogonal64(t), FEW, f"{rows} x {cols}")
+
+
+# ----------------------------------------------------------------------------- memory
+
+def muon(sides, grads=None):
+    params, momenta = ([torch.zeros(s, device=DEV) for s in sides] for _ in range(2))
+    return ops.Muon(params, grads or [normal(*s, seed=k) for k, s in enumerate(sides)], momenta)
+
+
+@pytest.mark.parametrize("side", [(64, 100), (300, 200)])
+def test_gradients_in_what_is_written_are_refused(side):
+    params, momenta = ([torch.zeros(side, device=DEV) for _ in range(2)] for _ in range(2))
+    fresh = [normal(*side, seed=k) for k in range(2)]
+    for bad in (momenta[0], momenta[1], params[0], params[1]):
+        with pytest.raises(eg.EgeriaError) as e:
+            ops.Muon(params, [fresh[0], bad], momenta)
+        assert e.value.status == eg.ERR_INVALID_ARG
+    m = ops.Muon(params, fresh, momenta)
+    for bad in (momenta[0], params[1]):
+        with pytest.raises(eg.EgeriaError) as e:
+            m.egeria_muon_set_grads([bad, fresh[1]])
+        assert e.value.status == eg.ERR_INVALID_ARG
+    m.egeria_muon_step(1.0, beta=0.0, nesterov=False)       # the old ones are in force
+    for p, g in zip(params, fresh):
+        near(-p, 0.2 * max(side) ** 0.5 * orthogonal64(g), MANY)
+
+
+@pytest.mark.parametrize("side", [(64, 100), (300, 200)])
+def test_a_dropped_handle_keeps_its_memory_until_its_step_has_run(side):
+    side_stream = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    torch.cuda.empty_cache()
+    h = muon([side])
+    place, size = h._raw.data_ptr(), h._raw.numel()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side_stream):
+        torch.cuda._sleep(600_000_000)         # about 0.3 s
+        h.egeria_muon_step(1e-3)
+    del h
+    new = [torch.empty(size, dtype=torch.uint8, device=DEV) for _ in range(3)]
+    busy = not side_stream.query()
+    assert busy and place not in {t.data_ptr() for t in new}
+    side_stream.synchronize()
+
+
+@pytest.mark.parametrize("side", [(64, 100), (300, 200)])
+def test_new_gradients_are_kept_for_the_streams_of_the_steps(side):
+    side_stream = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    torch.cuda.empty_cache()
+    first, second = [torch.ones(side, device=DEV)], [torch.ones(side, device=DEV)]
+    m = muon([side], first)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side_stream):
+        m.egeria_muon_step(1e-3)
+        m.egeria_muon_set_grads(second)
+        places = {first[0].data_ptr(), second[0].data_ptr()}
+        torch.cuda._sleep(600_000_000)
+        m.egeria_muon_step(1e-3)
+    del m, first, second
+    new = [torch.empty(side, device=DEV) for _ in range(6)]
+    busy = not side_stream.query()
+    assert busy and not places & {t.data_ptr() for t in new}
+    side_stream.synchronize()
+
+
+@pytest.mark.parametrize("side", [(64, 100), (300, 200)])
+def test_new_gradients_after_a_step_in_flight(side):
+    """Given on the step's stream while that step has not begun: it still takes the old ones, the next the new ones."""
+    stream = torch.cuda.Stream()
+    grads = [normal(*side, seed=k) for k in range(2)]
+    m = muon([side], grads[:1])
+    torch.cuda.synchronize()
+    with torch.cuda.stream(stream):
+        torch.cuda._sleep(100_000_000)
+        m.egeria_muon_step(1.0, beta=0.0, nesterov=False)
+        m.egeria_muon_set_grads(grads[1:])
+        between = m._keep[0][0].clone()
+        m.egeria_muon_step(1.0, beta=0.0, nesterov=False)
+    stream.synchronize()
+    m.check_device_status()
+    scale = 0.2 * max(side) ** 0.5
+    near(-between, scale * orthogonal64(grads[0]), MANY, "the first step")
+    near(between - m._keep[0][0], scale * orthogonal64(grads[1]), MANY, "the second")

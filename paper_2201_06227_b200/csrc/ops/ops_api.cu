@@ -326,7 +326,6 @@ egeria_status egeria_ops_create(egeria_ops **out, void *workspace, size_t worksp
     }
     EGO_CUDA(allow_all<bf16>());
     EGO_CUDA(allow_all<f16>());
-    EGO_CUDA(allow_gated());
     // the workspace may be memory that earlier work of a stream which the default stream does not wait for still writes to
     EGO_CUDA(cudaDeviceSynchronize());
     EGO_CUDA(cudaMemset(workspace, 0, kHeadBytes));

@@ -33,6 +33,7 @@ struct egeria_ops {
     int64_t launches = 0;
     cudaStream_t last_stream = nullptr;
     uint32_t stall_next = 0;  // test hook: give-up path of the next product
+    bool gated = false;       // the gated blocks' kernels are ready
 };
 
 namespace egeria {
@@ -145,7 +146,6 @@ template <typename T, int BN, int CG, int MB, int MODE>
 inline cudaError_t launch_gemm(const GemmParams &p, int ctas, cudaStream_t stream) {
     return launch(gemm_kernel<T, BN, CG, MB, MODE>, dim3(ctas), GemmCfg<BN, CG, MB>::kThreads, GemmCfg<BN, CG, MB>::kSmem, stream, CG, p);
 }
-cudaError_t allow_gated();  // the kernels of gated_api.cu
 
 constexpr int kFewSmem = 96 * 1024;
 constexpr int kFewRows = 4;   // rows that go without the tensor cores: at 1024 x 4096 3.7 us for one row, 6.5 for two, 9.0 for four, 10.0 on the tensor cores

@@ -46,7 +46,7 @@ static cudaError_t allow_gated(egeria_ops *o) {
 }
 
 template <typename T, int MODE>
-static cudaError_t launch_type(const GemmPlan &g, const GemmParams &p, int ctas, cudaStream_t stream) {
+static cudaError_t launch_type(const GemmPlan &g, const GemmParams<MODE> &p, int ctas, cudaStream_t stream) {
     if constexpr (MODE == kModeStore) {
         if (g.mb == 2) return launch_gemm<T, 256, 2, 2, MODE>(p, ctas, stream);
     } else {
@@ -55,7 +55,7 @@ static cudaError_t launch_type(const GemmPlan &g, const GemmParams &p, int ctas,
     return g.cg == 2 ? launch_gemm<T, 256, 2, 1, MODE>(p, ctas, stream) : launch_gemm<T, 128, 1, 1, MODE>(p, ctas, stream);
 }
 template <int MODE>
-static egeria_status launch_mode(egeria_ops *o, cudaStream_t stream, int type, const GemmPlan &g, const GemmParams &p, int ctas) {
+static egeria_status launch_mode(egeria_ops *o, cudaStream_t stream, int type, const GemmPlan &g, const GemmParams<MODE> &p, int ctas) {
     EGO_CUDA((type == EGERIA_BF16 ? launch_type<bf16, MODE>(g, p, ctas, stream) : launch_type<f16, MODE>(g, p, ctas, stream)));
     ++o->launches;
     return EGERIA_OK;
@@ -305,10 +305,10 @@ egeria_status egeria_gated_forward(egeria_ops *ops, void *cuda_stream, const ege
         down.w = w_down.p, down.ldw = w_down.ld;
         if ((s = run_prepare(ops, stream, a.type, prep, false)) != EGERIA_OK) return s;
         const GemmPlan g = plan_single(a.rows, 2 * a.hidden, a.inp, ops->sms, a.g ? 20.0 : 12.0);
-        GemmParams p;
+        GemmParams<kModeGated> p;
         int ctas = 0;
-        if ((s = fill_products(ops, a.type, kModeGated, &job, &g, 1, p, ctas)) != EGERIA_OK) return s;
-        if ((s = launch_mode<kModeGated>(ops, stream, a.type, g, p, ctas)) != EGERIA_OK) return s;
+        if ((s = fill_products(ops, a.type, &job, &g, 1, p, ctas)) != EGERIA_OK) return s;
+        if ((s = launch_mode(ops, stream, a.type, g, p, ctas)) != EGERIA_OK) return s;
     }
     return linear_forward_at(ops, stream, down, L.part[0], 0, L.w_down);
 }
@@ -431,19 +431,20 @@ egeria_status egeria_gated_backward(egeria_ops *ops, void *cuda_stream, const eg
         make_loadable(ops, j.b2, L.w_up, prep.pack[3]);
     }
     if ((s = run_prepare(ops, stream, a.type, prep, wide)) != EGERIA_OK) return s;
-    GemmParams p;
     int ctas = 0;
     if (gates || a.dw_down) {
+        GemmParams<kModeGatedBack> p;
         const GemmPlan g = plan_single(a.rows, a.hidden, a.out, ops->sms, 30.0);
-        if ((s = fill_products(ops, a.type, kModeGatedBack, &back, &g, 1, p, ctas)) != EGERIA_OK) return s;
-        if ((s = launch_mode<kModeGatedBack>(ops, stream, a.type, g, p, ctas)) != EGERIA_OK) return s;
+        if ((s = fill_products(ops, a.type, &back, &g, 1, p, ctas)) != EGERIA_OK) return s;
+        if ((s = launch_mode(ops, stream, a.type, g, p, ctas)) != EGERIA_OK) return s;
     }
     if (count) {
         GemmPlan plan[kMaxProblems];
         plan_store(jobs, count, ops->sms, plan);
-        if ((s = fill_products(ops, a.type, kModeStore, jobs, plan, count, p, ctas)) != EGERIA_OK) return s;
+        GemmParams<kModeStore> p;
+        if ((s = fill_products(ops, a.type, jobs, plan, count, p, ctas)) != EGERIA_OK) return s;
         std::copy(sums, sums + kMaxSums, p.sums);
-        return launch_mode<kModeStore>(ops, stream, a.type, plan[0], p, ctas);
+        return launch_mode(ops, stream, a.type, plan[0], p, ctas);
     }
     for (int i = 0; i < n_sums; ++i) {
         const dim3 grid((unsigned)((sums[i].cols + 31) / 32));

@@ -85,9 +85,16 @@ struct ColumnSums {
     int32_t n, cols;
 };
 constexpr int kMaxProblems = 4, kMaxSums = 3;
+// What a launch computes: linear layers; a gated block's two projections, side by side in one tile, and act(g) * u; the gradients of
+// g and u from that of the hidden values, in the product that makes it; and up to kMaxProblems products that are only stored.
+enum { kModeLinear, kModeGated, kModeGatedBack, kModeStore };
+// (As many products as the mode has: the host writes these parameters and the launch copies them, with room for four 0.3 us more a call.)
+template <int MODE>
 struct GemmParams {
-    GemmProblem problem[kMaxProblems];
-    ColumnSums sums[kMaxSums];       // added up by the epilogue's warps while the first products are computed
+    static constexpr int kProblems = MODE == kModeLinear ? 2 : MODE == kModeStore ? kMaxProblems : 1;
+    static constexpr int kSums = MODE == kModeStore ? kMaxSums : 1;
+    GemmProblem problem[kProblems];
+    ColumnSums sums[kSums];          // added up by the epilogue's warps while the first products are computed
 
     int32_t first, second;           // units of the leading products, which are equally long, and of the last one where there are several
     int32_t fill;                    // units of the last product that each worker without a last unit of the others takes before the rest
@@ -96,10 +103,6 @@ struct GemmParams {
     int32_t *status;
     uint64_t wait_limit_ns;
 };
-
-// What a launch computes: linear layers; a gated block's two projections, side by side in one tile, and act(g) * u; the gradients of
-// g and u from that of the hidden values, in the product that makes it; and up to kMaxProblems products that are only stored.
-enum { kModeLinear, kModeGated, kModeGatedBack, kModeStore };
 
 // MB: blocks of 128 rows per CTA and tile.  With one, tensor memory holds two tiles' accumulators, and a tile's epilogue runs
 // beside the next tile's products.  With two, a tile takes all of it: see mma_tile_pair.
@@ -648,13 +651,13 @@ __device__ __forceinline__ void add_columns(const ColumnSums &s, int strip, int 
 struct GemmUnit {
     int32_t problem, index, tm, tn, tile, split, kb0, kb1;
 };
-template <int PROBLEMS>
-__device__ __forceinline__ GemmUnit gemm_unit(const GemmParams &params, int u) {
+template <int MODE>
+__device__ __forceinline__ GemmUnit gemm_unit(const GemmParams<MODE> &params, int u) {
     GemmUnit g;
     g.problem = 0;
     g.index = u;
 #pragma unroll
-    for (int i = 0; i + 1 < PROBLEMS; ++i)
+    for (int i = 0; i + 1 < GemmParams<MODE>::kProblems; ++i)
         if (g.problem == i && g.index >= params.problem[i].units) {
             g.index -= params.problem[i].units;
             g.problem = i + 1;
@@ -676,7 +679,8 @@ __device__ __forceinline__ bool gemm_unit_fits(const GemmProblem &q, const GemmU
 }
 // The step-th unit of a worker (a CTA or a pair), or -1.  The leading products' units are dealt round; the workers
 // that the last round of them leaves out take `fill` units of the last product each, and then that is dealt round.
-__device__ __forceinline__ int gemm_next(const GemmParams &p, int worker, int workers, int step) {
+template <int MODE>
+__device__ __forceinline__ int gemm_next(const GemmParams<MODE> &p, int worker, int workers, int step) {
     const int first = p.first, second = p.second;
     const int rounds = first / workers, left = first - rounds * workers;
     const int mine = rounds + (worker < left);
@@ -705,9 +709,8 @@ __device__ __forceinline__ void mma_stage(uint32_t d, uint64_t da, uint64_t db, 
 }
 
 template <typename T, int BN, int CG, int MB, int MODE>
-__global__ void __launch_bounds__(GemmCfg<BN, CG, MB>::kThreads, 1) gemm_kernel(const __grid_constant__ GemmParams p) {
+__global__ void __launch_bounds__(GemmCfg<BN, CG, MB>::kThreads, 1) gemm_kernel(const __grid_constant__ GemmParams<MODE> p) {
     using Cfg = GemmCfg<BN, CG, MB>;
-    constexpr int kProblems = MODE == kModeLinear ? 2 : MODE == kModeStore ? kMaxProblems : 1;
     extern __shared__ uint8_t smem_raw[];
     const uint32_t smem_base = (ptx::smem_u32(smem_raw) + 1023u) & ~1023u;
     uint8_t *smem = smem_raw + (smem_base - ptx::smem_u32(smem_raw));
@@ -759,7 +762,7 @@ __global__ void __launch_bounds__(GemmCfg<BN, CG, MB>::kThreads, 1) gemm_kernel(
             for (int step = 0; ok; ++step) {
                 const int u = gemm_next(p, worker, workers, step);
                 if (u < 0) break;
-                const GemmUnit g = gemm_unit<kProblems>(p, u);
+                const GemmUnit g = gemm_unit(p, u);
                 const GemmProblem &q = p.problem[g.problem];
                 if (step == 0) arrived();
                 if (!eg_check(gemm_unit_fits(q, g), p.status, kCheckGemmUnit, u)) break;
@@ -833,7 +836,7 @@ __global__ void __launch_bounds__(GemmCfg<BN, CG, MB>::kThreads, 1) gemm_kernel(
             for (int step = 0; ok; ++step) {
                 const int u = gemm_next(p, worker, workers, step);
                 if (u < 0) break;
-                const GemmUnit g = gemm_unit<kProblems>(p, u);
+                const GemmUnit g = gemm_unit(p, u);
                 const GemmProblem &q = p.problem[g.problem];
                 const uint32_t idesc = idesc0 | (q.a_mn << 15) | (q.b_mn << 16);
                 const uint32_t step_a = q.a_mn ? 2048u >> 4 : 32u >> 4, step_b = q.b_mn ? 2048u >> 4 : 32u >> 4;
@@ -901,11 +904,11 @@ __global__ void __launch_bounds__(GemmCfg<BN, CG, MB>::kThreads, 1) gemm_kernel(
         uint32_t acc = 0, acc_phase = 0;
         const uint32_t release0 = CG == 2 ? map_to_rank(accempty0, 0) : accempty0;
         int u = gemm_next(p, worker, workers, 0);
-        GemmUnit g = gemm_unit<kProblems>(p, u);
+        GemmUnit g = gemm_unit(p, u);
         arrived();
         if (MODE == kModeLinear || MODE == kModeStore) {
 #pragma unroll 1
-            for (int i = 0; i < (MODE == kModeLinear ? 1 : kMaxSums); ++i)
+            for (int i = 0; i < GemmParams<MODE>::kSums; ++i)
                 if (p.sums[i].out)
                     for (int c = blockIdx.x; c * 32 < p.sums[i].cols; c += gridDim.x)
                         add_columns<T, kEpiWarps>(p.sums[i], c, e, lane, reinterpret_cast<float *>(staging),
@@ -1033,7 +1036,7 @@ __global__ void __launch_bounds__(GemmCfg<BN, CG, MB>::kThreads, 1) gemm_kernel(
 #pragma unroll 1
             for (int half = 0; half < MB && ok; ++half) {
                 if (MODE == kModeLinear)
-                    ok = g.problem == 0 ? tile(p.problem[0], half) : tile(p.problem[1], half);
+                    ok = g.problem == 0 ? tile(p.problem[0], half) : tile(p.problem[GemmParams<MODE>::kProblems > 1], half);
                 else
                     ok = tile(p.problem[MODE == kModeStore ? g.problem : 0], half);
                 acc ^= 1u;
@@ -1041,7 +1044,7 @@ __global__ void __launch_bounds__(GemmCfg<BN, CG, MB>::kThreads, 1) gemm_kernel(
             }
             if (!ok) break;
             u = gemm_next(p, worker, workers, ++step);
-            g = gemm_unit<kProblems>(p, u);
+            g = gemm_unit(p, u);
         }
     }
     ptx::tc_fence_before_sync();

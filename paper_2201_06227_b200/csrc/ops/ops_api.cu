@@ -82,7 +82,7 @@ static cudaError_t allow_all() {
 }
 
 template <typename T>
-static cudaError_t launch_gemm_any(int bn, int cg, int mb, const GemmParams &p, int ctas, cudaStream_t stream) {
+static cudaError_t launch_gemm_any(int bn, int cg, int mb, const GemmParams<kModeLinear> &p, int ctas, cudaStream_t stream) {
     if (mb == 2) return launch_gemm<T, 256, 2, 2, kModeLinear>(p, ctas, stream);
     if (cg == 2) return bn == 128 ? launch_gemm<T, 128, 2, 1, kModeLinear>(p, ctas, stream) : launch_gemm<T, 256, 2, 1, kModeLinear>(p, ctas, stream);
     if (bn == 64) return launch_gemm<T, 64, 1, 1, kModeLinear>(p, ctas, stream);
@@ -115,9 +115,9 @@ egeria_status run_products(egeria_ops *o, cudaStream_t stream, int type, Product
         auto rounds = [&](int64_t tiles) { return (tiles + workers - 1) / workers; };
         if (2 * rounds(tall * plan[0].tiles_n) <= rounds((int64_t)plan[0].tiles_m * plan[0].tiles_n)) plan[0].mb = 2, plan[0].tiles_m = (int)tall;
     }
-    GemmParams p;
+    GemmParams<kModeLinear> p;
     int ctas = 0;
-    const egeria_status s = fill_products(o, type, kModeLinear, jobs, plan, count, p, ctas);
+    const egeria_status s = fill_products(o, type, jobs, plan, count, p, ctas);
     if (s != EGERIA_OK) return s;
     p.sums[0] = sums;
     const int bn = plan[0].bn, cg = plan[0].cg, mb = plan[0].mb;

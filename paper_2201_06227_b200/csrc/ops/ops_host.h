@@ -143,7 +143,7 @@ inline cudaError_t allow_smem() {
     return cudaFuncSetAttribute(gemm_kernel<T, BN, CG, MB, MODE>, cudaFuncAttributeMaxDynamicSharedMemorySize, GemmCfg<BN, CG, MB>::kSmem);
 }
 template <typename T, int BN, int CG, int MB, int MODE>
-inline cudaError_t launch_gemm(const GemmParams &p, int ctas, cudaStream_t stream) {
+inline cudaError_t launch_gemm(const GemmParams<MODE> &p, int ctas, cudaStream_t stream) {
     return launch(gemm_kernel<T, BN, CG, MB, MODE>, dim3(ctas), GemmCfg<BN, CG, MB>::kThreads, GemmCfg<BN, CG, MB>::kSmem, stream, CG, p);
 }
 
@@ -194,7 +194,8 @@ struct Product {
 
 // The parameters of a launch of these products under these plans, which share the kind of tile.  Of several, the last may have
 // another length than the others.  sizes of partial tiles go by split_bytes.
-inline egeria_status fill_products(egeria_ops *o, int type, int mode, const Product *jobs, const GemmPlan *plan, int count, GemmParams &p, int &ctas) {
+template <int MODE>
+inline egeria_status fill_products(egeria_ops *o, int type, const Product *jobs, const GemmPlan *plan, int count, GemmParams<MODE> &p, int &ctas) {
     const int bn = plan[0].bn, cg = plan[0].cg, mb = plan[0].mb, workers = o->sms / cg;
     memset(&p, 0, sizeof(p));
     int64_t units = 0, last = 0;
@@ -204,7 +205,7 @@ inline egeria_status fill_products(egeria_ops *o, int type, int mode, const Prod
         GemmProblem &q = p.problem[i];
         if (g.splits > 1 && (mb > 1 || (size_t)g.tiles_m * g.tiles_n * g.splits * cg * 128 * bn * 4 > split_bytes(j.m, j.n, j.k + j.k2)))
             return EGERIA_ERR_WORKSPACE;
-        const int b_rows = mode == kModeGated ? bn / 2 : bn / cg;
+        const int b_rows = MODE == kModeGated ? bn / 2 : bn / cg;
         egeria_status s = encode_operand(o, &q.a, j.a, type, kGemmM);
         if (s == EGERIA_OK) s = encode_operand(o, &q.b, j.b, type, b_rows);
         if (s == EGERIA_OK && j.b2.p) s = encode_operand(o, &q.b2, j.b2, type, b_rows);

@@ -171,3 +171,11 @@ def test_new_gradients_after_a_step_in_flight(side):
     scale = 0.2 * max(side) ** 0.5
     near(-between, scale * orthogonal64(grads[0]), MANY, "the first step")
     near(between - m._keep[0][0], scale * orthogonal64(grads[1]), MANY, "the second")
+
+
+# ----------------------------------------------------------------------------- a few singular values
+
+@pytest.mark.parametrize("rows,cols", [(1, 1), (1, 700), (700, 1), (2, 3), (1, 768), (5, 65), (65, 5), (15, 15), (7, 400)])
+def test_few_singular_values(rows, cols):
+    t = normal(rows, cols, seed=rows + cols)
+    near(orthogonalised([t])[0], orthogonal64(t), FEW)

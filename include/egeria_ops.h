@@ -306,8 +306,8 @@ typedef struct {
     int32_t module;          /* its entry in the freeze mask, -1 = in none */
 } egeria_muon_tensor;
 
-/* Bytes of device workspace: about six per value of the matrices, four per value of the squares of their shorter sides, and the
- * list of the work.  Pure host arithmetic; 0 for invalid arguments. */
+/* Bytes of device workspace: about six per value of the matrices, four per value of the squares of their shorter sides (for a matrix
+ * of at most 128 by 768, instead of both, 256 for each column of its longer side rounded up to 64), and the list of the work.  Pure host arithmetic; 0 for invalid arguments. */
 size_t egeria_muon_workspace_bytes(int count, const egeria_muon_tensor *tensors, int steps);
 
 /* An optimizer over `count` matrices (host array, copied).
@@ -327,8 +327,11 @@ egeria_status egeria_muon_set_grads(egeria_muon *muon, void *cuda_stream, const 
  *   X = t / max(|t|, eps), |t| the root of the sum of squares; then `steps` times
  *       A = X X^T     X = 3.4445 X - 4.7750 A X + 2.0315 A^2 X
  *   p = p (1 - lr weight_decay) - lr scale X
- * The products' operands are rounded to f16 (11 digits), their sums are 32 bits: X is off by about 1.5e-3 of itself (2-norm; 1.1e-3 to
- * 2.1e-3 over the shapes and ranks tried).  A gradient that is not finite makes its whole matrix NaN.  The sum of A's products over a
+ * The products' operands are rounded to f16 (11 digits), their sums are 32 bits: after five steps X is off by about 1.5e-3 of itself
+ * (2-norm; 0.4e-3 to 2.1e-3 over the shapes and ranks tried), after 8 by 3e-3 and after 16 by 4e-3 to 6e-3 where its rank is full.  Where
+ * it is not, each step multiplies by 3.4 whatever rounding has left across the null space, in any arithmetic: 1e-2 after 8 steps, 0.1
+ * after 10 and X itself after 12 (in 32 bits throughout two to three steps later).  More than seven steps are for matrices of full rank.
+ * A gradient that is not finite makes its whole matrix NaN.  The sum of A's products over a
  * long side is not split: matrices are meant to be many or large, not one of a few rows by millions.
  *   grad_scale  device float [1] or NULL (1).  If it is not finite the whole step is left out.
  *   frozen      device uint8 or NULL, indexed by `module`: the out_mask of egeria_plasticity_evaluate as it is.  A frozen

@@ -15,17 +15,18 @@
 // MMAs, the other warps run the epilogue of a tile while the next tile's products go into the other half of
 // tensor memory.  One launch takes up to two products (dx and dw of a layer), so that the second fills
 // the SMs that the first leaves.  CG = 2: a pair of CTAs shares one tile of 256 rows; each loads its 128 rows of A and
-// HALF of B, which is what brings the loads (32 KB per 64 k and CTA instead of 48) near what an SM
-// can take from L2 in the time of the MMAs (64 bytes a cycle at their full rate; 60 bytes a nanosecond seen).
+// HALF of B: 32 KB of loads per 64 k and CTA instead of 48.
 //
 // Measured (bf16, GPU time in a replayed graph; floor: 2 m n k at 1669 TFLOP/s, a short product's rate; a long run's is 1435
 // under the power limit, which these meet too): 65536 x 1024 x 4096 (rows, k, columns) alone 464 us of 329, with bias, tanh-gelu and z
 // 547; k = 4096 and 1024 columns 16384 rows 119 of 82.  dx and dw of 16384 x 4096 x 1024 236 us of 165, with the slope of dx's
 // tanh-gelu 317.  By the counters no unit is full at k = 1024: the tensor pipe is busy for 60 % of the time alone and 51 % with all of
-// the epilogue (67 % alone at k = 4096), the issue slots for 16 and 31 %.  What is full is an SM's intake: tile loads bring 60 to 69
-// bytes a nanosecond into one, whether it loads alone or all 148 do (a kernel that only loads: 59.5 with 16 KB tiles, 68 with contiguous
-// 16 KB), and a 256 x 256 tile wants 32 KB per 64 k, which is half a microsecond for 0.27 of MMAs.  Tiles of 512 x 256 (MB = 2) want a
-// quarter less, but take all of tensor memory, so that nothing hides their epilogue.  Small products (under some 500 rows) are bound by
+// the epilogue (67 % alone at k = 4096), the issue slots for 16 and 31 %.  What it waits for are its loads: they bring 60 to 69
+// bytes a nanosecond into an SM, whether it loads alone or all 148 do (a kernel that only loads: 59.5 with 16 KB tiles, 68 with contiguous
+// 16 KB), and a 256 x 256 tile wants 32 KB per 64 k, which is half a microsecond for 0.27 of MMAs.  That is not the most that an SM takes: the
+// library's product of 8192 x 8192 x 8192 has tiles of the same size for two CTAs and, at 1634 TFLOP/s, brings in 86; what it does
+// otherwise is not known here.  Tiles of 512 x 256 (MB = 2) want a quarter less, but take all of tensor memory, so that nothing hides their
+// epilogue.  Small products (under some 500 rows) are bound by
 // the 8 to 10 us that a launch, its first loads and its one epilogue take.
 #pragma once
 #include <cuda.h>
@@ -105,7 +106,8 @@ struct GemmParams {
 };
 
 // MB: blocks of 128 rows per CTA and tile.  With one, tensor memory holds two tiles' accumulators, and a tile's epilogue runs
-// beside the next tile's products.  With two, a tile takes all of it: see mma_tile_pair.
+// beside the next tile's products.  With two, a tile takes all of it, and its halves run
+// apart at its ends (the kernel's warp 1).
 template <int BN, int CG, int MB>
 struct GemmCfg {
     static constexpr int kABytes = MB * kGemmM * kGemmK * 2;
@@ -499,7 +501,7 @@ __device__ __forceinline__ void gated_finish(const GatedEpilogue &p, float (&g)[
 }
 // A tile of 128 rows by BN / 2 hidden columns: the accumulator's first half is g, the second u, so that h needs neither of them in
 // memory.  (BN = 64 has one piece for each row quarter, which the first four warps take.)  16384 x 1024 -> 2816: 150 us with g and u
-// kept of 113 for the products at 1669 TFLOP/s: the intake of 11 x 128 tiles of 2 x 512 KB is 147.
+// kept of 113 for the products at 1669 TFLOP/s: loading 22 x 64 tiles of 2 x 512 KB takes 147 at 68 bytes a nanosecond and SM.
 template <typename T, int BN, typename Wait, typename Release>
 __device__ __forceinline__ bool gated_tile(const GemmProblem &q, int32_t tn, Tile &t, uint32_t lanes, int strip, Wait wait, Release release) {
     constexpr int kHalf = BN / 2, kPieces = kHalf < 64 ? 1 : kHalf / 64;
@@ -1136,7 +1138,10 @@ __global__ void __launch_bounds__(256) linear_few_kernel(const Epilogue p, int32
     }
 }
 
-// The hidden values of a gated block for 1 to 4 rows: as linear_few_kernel, with a row of each projection per turn.
+// The hidden values of a gated block for 1 to 4 rows: as linear_few_kernel, with a row of each projection per turn.  (Two trips to memory,
+// one after the other: x into shared memory, then the weights.)  h is rounded as the tensor cores' path rounds it, so that a row
+// gives what it gives among others but for the order of sums: y of 1 x 1024 -> 2816 -> 1024 is 1.7e-3 from what 32 bits throughout give, of
+// which nothing is left when h is rounded there too.
 template <typename T, int ROWS, bool WIDE>
 __global__ void __launch_bounds__(256) gated_few_kernel(const GatedEpilogue p, int32_t m, int32_t n_cols, const T *x, int64_t ldx, const T *wg, int64_t ldg,
                                                         const T *wu, int64_t ldu, int32_t k) {

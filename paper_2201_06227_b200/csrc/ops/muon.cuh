@@ -871,7 +871,7 @@ __global__ void __launch_bounds__(MuonCfg<BN, CG>::kThreads, 1) muon_products_ke
 // side (its 64-column panels are A X^T's with the columns consecutive and P X's with them as the other axis), and only what its
 // rounding leaves goes by way of L2.  54 convolutions of 16 to 64 channels: 58 us, 100 through the list of units, where each of the 15
 // products waits for the one before it to be stored, seen and loaded.  Of the 58, 10 go into the first 64 x 576 X and 6 into its
-// weights (0.7 and 0.4 MB through one SM at the 60 bytes a nanosecond that it takes), 7.3 into each of the five steps: 1.1 of waiting for
+// weights (0.7 and 0.4 MB through one SM at the 60 to 70 bytes a nanosecond that these loads get), 7.3 into each of the five steps: 1.1 of waiting for
 // A, 0.9 for A A, 4.9 for three chunks, whose products and values and the next A's part of them run beside each other (8.6 before).
 constexpr int kSmallSide = 128, kSmallPanels = 12;
 constexpr int kSmallThreads = 512, kSmallStrips = kSmallThreads / 128, kPanelBytes = kSmallSide * 128;
@@ -1081,7 +1081,7 @@ __global__ void __launch_bounds__(kSmallThreads, 1) muon_small_kernel(const __gr
         const int32_t d = t.d, len = (int32_t)max(t.rows, t.cols);
         const int32_t panels = (len + 63) / 64;
         const void *grad = p.grads[t.index];
-        // the panels' zeros, and those of the rest behind a row's end
+        // the panels' zeros (the rest holds anything behind a row's end, where it is not looked at)
         for (int i = threadIdx.x; i < panels * kPanelBytes / 16; i += kSmallThreads)
             asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(base + i * 16), "r"(0) : "memory");
         const bool vector = muon_vector(p, t);

@@ -108,7 +108,9 @@ egeria_status run_products(egeria_ops *o, cudaStream_t stream, int type, Product
     }
     // Tiles of 512 rows take a quarter less from L2, but nothing hides their epilogue: for long sums with a light one, where they
     // need no more rounds.  16384 x 2816 -> 1024 with a residual 85 us instead of 92, 8192 x 8192 -> 8192 752 instead of 949; but
-    // 8192 x 2048 -> 2048 93 instead of 86, 16384 x 1024 -> 4096 with activation and z 191 instead of 159.
+    // 8192 x 2048 -> 2048 93 instead of 86, 16384 x 1024 -> 4096 with activation and z 191 instead of 159.  Over sums of 2560 to 8192, 512 to
+    // 4096 columns and 2048 to 32768 rows (96 sizes, both in turn) it gains 0 to 7 % at 2560 and 13 to 15 % at 8192 wherever it is taken; the
+    // one size that came out slower, 4096 x 2560 -> 4096, did by 2 % with 12 % between its runs.
     if (count == 1 && plan[0].cg == 2 && plan[0].bn == 256 && plan[0].splits == 1 && jobs[0].k >= 40 * kGemmK && !jobs[0].epi.act && !jobs[0].epi.z &&
         !jobs[0].epi.slope) {
         const int64_t workers = o->sms / 2, tall = (jobs[0].m + 511) / 512;

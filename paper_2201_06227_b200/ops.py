@@ -424,7 +424,8 @@ class Muon(_Handle):
     params, grads, momenta: one contiguous CUDA tensor of two or more dimensions per matrix of the model, the first its rows, the others
     taken together its columns; momenta are float32.  masters: float32 copies that the step works on (entries may be None).
     scale: "rms" for 0.2 sqrt(max(rows, cols)), with which AdamW's learning rates and decays suit, "spectral" for
-    sqrt(max(1, rows / cols)), or a number per matrix.  modules: each matrix's entry in the freeze mask, -1 for none.  The handle
+    sqrt(max(1, rows / cols)), or a number per matrix.  ns_steps: 1 to 16; with more than seven the rounding across the null space of a
+    matrix whose rank is not full shows (see the header).  The gradients share no memory with what a step writes.  modules: each matrix's entry in the freeze mask, -1 for none.  The handle
     keeps all of them alive.  Vectors (biases, norms) and embeddings are better left to :class:`AdamW`.
     """
 

@@ -328,11 +328,12 @@ egeria_status egeria_muon_set_grads(egeria_muon *muon, void *cuda_stream, const 
  *       A = X X^T     X = 3.4445 X - 4.7750 A X + 2.0315 A^2 X
  *   p = p (1 - lr weight_decay) - lr scale X
  * The products' operands are rounded to f16 (11 digits), their sums are 32 bits: after five steps X is off by about 1.5e-3 of itself
- * (2-norm; 0.4e-3 to 2.1e-3 over the shapes and ranks tried), after 8 by 3e-3 and after 16 by 4e-3 to 6e-3 where its rank is full.  Where
- * it is not, each step multiplies by 3.4 whatever rounding has left across the null space, in any arithmetic: 1e-2 after 8 steps, 0.1
- * after 10 and X itself after 12 (in 32 bits throughout two to three steps later).  More than seven steps are for matrices of full rank.
- * A gradient that is not finite makes its whole matrix NaN.  The sum of A's products over a
- * long side is not split: matrices are meant to be many or large, not one of a few rows by millions.
+ * (2-norm; 0.4e-3 to 2.1e-3 over the shapes and ranks tried; a matrix of two or three singular values by up to 1.6e-2, where one of them
+ * meets the polynomial's steep places), after 8 by 3e-3 and after 16 by 4e-3 to 6e-3 where its rank is full.  Where it is not,
+ * each step multiplies by 3.4 whatever rounding has left across the null space, in any arithmetic: 1e-2 after 8 steps, 0.1 after 10
+ * and X itself after 12 (in 32 bits throughout two to three steps later).  More than seven steps are for matrices of full rank.
+ * A gradient that is not finite makes its whole matrix NaN.  The sum of A's products over a long side is not split: matrices are
+ * meant to be many or large, not one of a few rows by millions.
  *   grad_scale  device float [1] or NULL (1).  If it is not finite the whole step is left out.
  *   frozen      device uint8 or NULL, indexed by `module`: the out_mask of egeria_plasticity_evaluate as it is.  A frozen
  *               matrix is neither read nor written.  (Not to be written while the call runs.)

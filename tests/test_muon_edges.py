@@ -3,8 +3,11 @@ memory, handles that are dropped or given new gradients with a step in flight.
 
 Tolerances, derived before the first run.  After one step, value by value: X is rounded by 2^-11 of itself where it is an operand and by
 2^-25 / up where that is less (up: the power of two that it is held times), A and the polynomial by 2^-11, and a sum of n products by
-(n + 8) 2^-23 of the products' sizes.  After five steps as in test_muon_gpu.py: 1.1e-2 for a matrix of a few singular values, and 7e-3
-in the 2-norm, six times what independent roundings come to, for one of many.
+(n + 8) 2^-23 of the products' sizes.  After five steps as in test_muon_gpu.py: 7e-3 in the 2-norm, six
+times what independent roundings come to, for a matrix of many singular values.  One of a few has no such mean, and a step's slope is not
+at most 0.72 everywhere that a singular value passes: it is -1.6 at 0.84, the polynomial's valley, and 1.7 at 1.13, its largest value, so
+that an error may grow from one step to the next.  The roundings above, simulated in 64 bits on 20000 matrices of each of the sizes 2 x 3 and
+2 x 20, leave 2e-3 as a rule and 1.6e-2 at most; 1.7e-2 is allowed for.
 """
 import math
 
@@ -17,7 +20,7 @@ from test_muon_gpu import A, B, C, low_rank, near, normal, orthogonal64, orthogo
 from test_ops_gpu import DEV, close
 
 pytestmark = pytest.mark.gpu
-MANY, FEW = 7e-3, 1.1e-2
+MANY, FEW = 7e-3, 1.7e-2
 
 
 # ----------------------------------------------------------------------------- matrices of low rank
